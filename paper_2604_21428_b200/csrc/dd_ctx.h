@@ -40,6 +40,8 @@ struct dd_ctx {
     double *gram = nullptr;                   // Gram matrices of two-launch radial-directional merges
     size_t gram_cap = 0;                      // fragments
     int gram_grid[2] = {0, 0};                // [bf16] persistent grid of the Gram launch
+    void *ffn_scratch = nullptr;              // intermediates of the gated feed-forward block
+    size_t ffn_scratch_cap = 0;               // bytes
     ddm::HostPipe *pipe = nullptr;
     char cuda_err[256] = {0};
 };

@@ -1,0 +1,315 @@
+// dd_gated_ffn_forward / dd_gated_ffn_backward: arguments, tensor maps and launches of the gated
+// feed-forward block.  Forward: one launch for gate, up and their product, one for the way down.
+// Backward: one launch for the gradients inside the block, one for dx and the three weights.
+#include <cmath>
+#include <cstring>
+
+#include "dd_ctx.h"
+#include "dd_ffn_gemm.cuh"
+
+namespace ddm {
+
+constexpr unsigned long long kFfnMax = 1ull << 30;
+
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's tensor map encoder, found through the runtime (the library does not link libcuda).
+static EncodeTiled tensor_map_encoder()
+{
+    static const EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            return (EncodeTiled) nullptr;
+        }
+        return (EncodeTiled)p;
+    }();
+    return fn;
+}
+
+struct Matrix {
+    const void *data;
+    unsigned long long rows, cols, ld;      // bf16 elements
+};
+
+static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m)
+{
+    const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * 2};
+    const cuuint32_t box[2] = {64, 64}, step[2] = {1, 1};
+    const EncodeTiled fn = tensor_map_encoder();
+    if (!fn || fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(m.data), dims, strides, box, step,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+        snprintf(ctx->cuda_err, sizeof ctx->cuda_err, "cuTensorMapEncodeTiled failed");
+        return DD_ERR_CUDA;
+    }
+    return DD_OK;
+}
+
+static unsigned blocks_of(unsigned long long n, unsigned b) { return (unsigned)((n + b - 1) / b); }
+
+// Adds a problem of m x n outputs in tiles of 128 x cols; operands are set by the caller.
+static GemmProblem &add_problem(GemmArgs &a, unsigned long long m, unsigned long long n, int cols)
+{
+    GemmProblem &p = a.prob[a.nprob++];
+    p.m = (unsigned)m;
+    p.n = (unsigned)n;
+    p.tiles_m = blocks_of(m, kBM);
+    p.tiles_n = blocks_of(n, cols);
+    a.tiles += p.tiles_m * p.tiles_n;
+    p.tile_end = a.tiles;
+    return p;
+}
+
+template <int EPI, int BN>
+static int launch_gemm(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
+{
+    constexpr size_t smem = gemm_smem_bytes(BN);
+    DD_CUDA(ctx, cudaFuncSetAttribute(ffn_gemm_kernel<EPI, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const unsigned grid = a.tiles < (unsigned)ctx->sm_count ? a.tiles : (unsigned)ctx->sm_count;
+    ffn_gemm_kernel<EPI, BN><<<grid, kGemmThreads, smem, stream>>>(a);
+    DD_CUDA(ctx, cudaGetLastError());
+    return DD_OK;
+}
+
+// Context-owned scratch for callers that bring none.
+static int ensure_ffn_scratch(dd_ctx *ctx, size_t bytes)
+{
+    if (bytes <= ctx->ffn_scratch_cap) return DD_OK;
+    DD_CUDA(ctx, cudaDeviceSynchronize());
+    if (ctx->ffn_scratch) cudaFree(ctx->ffn_scratch);
+    ctx->ffn_scratch = nullptr;
+    ctx->ffn_scratch_cap = 0;
+    DD_CUDA(ctx, cudaMalloc(&ctx->ffn_scratch, bytes));
+    ctx->ffn_scratch_cap = bytes;
+    return DD_OK;
+}
+
+// ---- arguments ---------------------------------------------------------------------------------
+
+struct Extent {
+    const void *p;
+    size_t bytes;
+};
+
+static Extent extent(const void *p, unsigned long long rows, unsigned long long cols, unsigned long long ld, size_t elem = 2)
+{
+    return Extent{p, p && rows ? (size_t)((rows - 1) * ld + cols) * elem : 0};
+}
+
+static bool touches(const Extent &a, const Extent &b)
+{
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+
+static int set_stride(uint64_t &ld, uint64_t cols)
+{
+    if (ld == 0) ld = cols;
+    if (ld < cols) return DD_ERR_INVALID_ARG;
+    if (ld >= kFfnMax) return DD_ERR_TOO_LARGE;
+    return ld % 8 ? DD_ERR_ALIGNMENT : DD_OK;
+}
+
+// Validates the block and fills in its defaults; without gate and up their stride is not looked at.
+static int check_block(const dd_ctx *ctx, dd_gated_ffn &b, bool with_gate)
+{
+    if (!ctx || b.d < 1 || b.f < 1) return DD_ERR_INVALID_ARG;
+    if (b.activation != DD_ACT_SILU && b.activation != DD_ACT_GELU_TANH) return DD_ERR_INVALID_ARG;
+    if (b.tokens >= kFfnMax || b.d >= kFfnMax || b.f >= kFfnMax) return DD_ERR_TOO_LARGE;
+    struct { uint64_t *ld; uint64_t cols; } strides[] = {{&b.ld_x, b.d}, {&b.ld_y, b.d}, {&b.ld_gate, b.f}, {&b.ld_in, b.d}, {&b.ld_down, b.f}};
+    for (auto &s : strides) {
+        if (s.ld == &b.ld_gate && !with_gate) continue;
+        const int rc = set_stride(*s.ld, s.cols);
+        if (rc != DD_OK) return rc;
+    }
+    if (!b.w_gate || !b.w_up || !b.w_down) return DD_ERR_INVALID_ARG;
+    return DD_OK;
+}
+
+static int check_aligned(std::initializer_list<const void *> ptrs)
+{
+    for (const void *p : ptrs)
+        if ((uintptr_t)p & 15u) return DD_ERR_ALIGNMENT;
+    return DD_OK;
+}
+
+// Outputs first: none may touch another output or an input.
+static int check_alias(std::initializer_list<Extent> outs, std::initializer_list<Extent> ins)
+{
+    for (auto o = outs.begin(); o != outs.end(); ++o) {
+        for (auto q = outs.begin(); q != o; ++q)
+            if (touches(*o, *q)) return DD_ERR_ALIAS;
+        for (const Extent &i : ins)
+            if (touches(*o, i)) return DD_ERR_ALIAS;
+    }
+    return DD_OK;
+}
+
+}  // namespace ddm
+
+using namespace ddm;
+
+extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, const void *x, const void *residual,
+                                    void *gate, void *up, void *hidden, void *y, int32_t *status, void *cuda_stream)
+{
+    if (!block) return DD_ERR_INVALID_ARG;
+    dd_gated_ffn b = *block;
+    int rc = check_block(ctx, b, gate != nullptr);
+    if (rc != DD_OK) return rc;
+    if ((gate == nullptr) != (up == nullptr)) return DD_ERR_INVALID_ARG;
+    if (b.tokens > 0 && (!x || !y)) return DD_ERR_INVALID_ARG;
+    if ((uintptr_t)status & 3u) return DD_ERR_ALIGNMENT;
+    rc = check_aligned({x, residual, gate, up, hidden, y, b.w_gate, b.w_up, b.w_down});
+    if (rc != DD_OK) return rc;
+    const uint64_t T = b.tokens, ldh = (b.f + 7) / 8 * 8;
+    const Extent ex = extent(x, T, b.d, b.ld_x), ey = extent(y, T, b.d, b.ld_y), eg = extent(gate, T, b.f, b.ld_gate),
+                 eu = extent(up, T, b.f, b.ld_gate), eh = extent(hidden, T, ldh, ldh), er = extent(residual, T, b.d, b.ld_y),
+                 wg = extent(b.w_gate, b.f, b.d, b.ld_in), wu = extent(b.w_up, b.f, b.d, b.ld_in),
+                 wd = extent(b.w_down, b.d, b.f, b.ld_down);
+    rc = check_alias({ey, eg, eu, eh}, {ex, wg, wu, wd, y == residual ? Extent{nullptr, 0} : er});
+    if (rc == DD_OK && y == residual) rc = check_alias({eg, eu, eh}, {er});
+    if (rc != DD_OK) return rc;
+    if (T == 0) return DD_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return cuda_fail(ctx, cudaErrorInvalidDevice, "cudaSetDevice");
+    if (!hidden) {
+        rc = ensure_ffn_scratch(ctx, (size_t)(T * ldh) * 2);
+        if (rc != DD_OK) return rc;
+        hidden = ctx->ffn_scratch;
+    }
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    GemmArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.activation = b.activation;
+    a.status = status;
+    a.gate = (__nv_bfloat16 *)gate;
+    a.up = (__nv_bfloat16 *)up;
+    a.hidden = (__nv_bfloat16 *)hidden;
+    a.ld_gate = b.ld_gate;
+    a.ld_hidden = ldh;
+    rc = encode(ctx, &a.maps[0], {x, T, b.d, b.ld_x});
+    if (rc == DD_OK) rc = encode(ctx, &a.maps[1], {b.w_gate, b.f, b.d, b.ld_in});
+    if (rc == DD_OK) rc = encode(ctx, &a.maps[2], {b.w_up, b.f, b.d, b.ld_in});
+    if (rc != DD_OK) return rc;
+    GemmProblem &p = add_problem(a, T, b.f, 128);
+    p.kblocks[0] = blocks_of(b.d, kBK);
+    p.a_map[0] = 0;
+    p.b_map[0] = 1;
+    p.b_map[1] = 2;
+    rc = launch_gemm<kEpiGate, 256>(ctx, a, stream);
+    if (rc != DD_OK) return rc;
+
+    a.nprob = 0;
+    a.tiles = 0;
+    rc = encode(ctx, &a.maps[0], {hidden, T, b.f, ldh});
+    if (rc == DD_OK) rc = encode(ctx, &a.maps[1], {b.w_down, b.d, b.f, b.ld_down});
+    if (rc != DD_OK) return rc;
+    GemmProblem &q = add_problem(a, T, b.d, 256);
+    q.kblocks[0] = blocks_of(b.f, kBK);
+    q.b_map[0] = 1;
+    q.out = y;
+    q.ld_out = b.ld_y;
+    q.residual = (const __nv_bfloat16 *)residual;
+    q.ld_residual = b.ld_y;
+    return launch_gemm<kEpiStore, 256>(ctx, a, stream);
+}
+
+extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, const void *x, const void *gate,
+                                     const void *up, const void *dy, void *dx, void *dw_gate, void *dw_up,
+                                     void *dw_down, dd_dtype grad_dtype, int accumulate, void *scratch,
+                                     int32_t *status, void *cuda_stream)
+{
+    if (!block) return DD_ERR_INVALID_ARG;
+    dd_gated_ffn b = *block;
+    int rc = check_block(ctx, b, true);
+    if (rc != DD_OK) return rc;
+    if (grad_dtype != DD_F32 && grad_dtype != DD_BF16) return DD_ERR_INVALID_ARG;
+    if (!dw_gate || !dw_up || !dw_down) return DD_ERR_INVALID_ARG;
+    if (b.tokens > 0 && (!x || !gate || !up || !dy || !dx)) return DD_ERR_INVALID_ARG;
+    if ((uintptr_t)status & 3u) return DD_ERR_ALIGNMENT;
+    rc = check_aligned({x, gate, up, dy, dx, dw_gate, dw_up, dw_down, scratch, b.w_gate, b.w_up, b.w_down});
+    if (rc != DD_OK) return rc;
+    const uint64_t T = b.tokens, ldh = (b.f + 7) / 8 * 8;
+    const size_t ge = grad_dtype == DD_BF16 ? 2 : 4;
+    rc = check_alias({extent(dx, T, b.d, b.ld_x), extent(dw_gate, b.f, b.d, b.ld_in, ge), extent(dw_up, b.f, b.d, b.ld_in, ge),
+                      extent(dw_down, b.d, b.f, b.ld_down, ge), extent(scratch, 3 * T, ldh, ldh)},
+                     {extent(x, T, b.d, b.ld_x), extent(gate, T, b.f, b.ld_gate), extent(up, T, b.f, b.ld_gate),
+                      extent(dy, T, b.d, b.ld_y), extent(b.w_gate, b.f, b.d, b.ld_in), extent(b.w_up, b.f, b.d, b.ld_in),
+                      extent(b.w_down, b.d, b.f, b.ld_down)});
+    if (rc != DD_OK) return rc;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return cuda_fail(ctx, cudaErrorInvalidDevice, "cudaSetDevice");
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    if (T == 0) {                          // sums over no token
+        if (accumulate) return DD_OK;
+        DD_CUDA(ctx, cudaMemset2DAsync(dw_gate, b.ld_in * ge, 0, b.d * ge, b.f, stream));
+        DD_CUDA(ctx, cudaMemset2DAsync(dw_up, b.ld_in * ge, 0, b.d * ge, b.f, stream));
+        DD_CUDA(ctx, cudaMemset2DAsync(dw_down, b.ld_down * ge, 0, b.f * ge, b.d, stream));
+        return DD_OK;
+    }
+    if (!scratch) {
+        rc = ensure_ffn_scratch(ctx, (size_t)(3 * T * ldh) * 2);
+        if (rc != DD_OK) return rc;
+        scratch = ctx->ffn_scratch;
+    }
+    enum { kX, kDy, kWg, kWu, kWd, kDg, kDu, kH };
+    __nv_bfloat16 *dg = (__nv_bfloat16 *)scratch, *du = dg + T * ldh, *h = du + T * ldh;
+    const Matrix mats[kMaxMaps] = {{x, T, b.d, b.ld_x}, {dy, T, b.d, b.ld_y}, {b.w_gate, b.f, b.d, b.ld_in},
+                                   {b.w_up, b.f, b.d, b.ld_in}, {b.w_down, b.d, b.f, b.ld_down},
+                                   {dg, T, b.f, ldh}, {du, T, b.f, ldh}, {h, T, b.f, ldh}};
+    GemmArgs a;
+    std::memset(&a, 0, sizeof a);
+    for (int i = 0; i < kMaxMaps; ++i) {
+        rc = encode(ctx, &a.maps[i], mats[i]);
+        if (rc != DD_OK) return rc;
+    }
+    a.activation = b.activation;
+    a.status = status;
+    a.gate = (__nv_bfloat16 *)const_cast<void *>(gate);
+    a.up = (__nv_bfloat16 *)const_cast<void *>(up);
+    a.dgate = dg;
+    a.dup = du;
+    a.hidden = h;
+    a.ld_gate = b.ld_gate;
+    a.ld_hidden = ldh;
+    // dh = dy w_down: [T, d] x [d, f], and the gradients inside the block in its epilogue
+    GemmProblem &p = add_problem(a, T, b.f, 256);
+    p.kblocks[0] = blocks_of(b.d, kBK);
+    p.a_map[0] = kDy;
+    p.b_map[0] = kWd;
+    p.b_mn = 1;
+    rc = launch_gemm<kEpiBack, 256>(ctx, a, stream);
+    if (rc != DD_OK) return rc;
+
+    std::memset(a.prob, 0, sizeof a.prob);
+    a.nprob = 0;
+    a.tiles = 0;
+    GemmProblem &qx = add_problem(a, T, b.d, 256);        // dgate w_gate + dup w_up
+    qx.kblocks[0] = qx.kblocks[1] = blocks_of(b.f, kBK);
+    qx.a_map[0] = kDg;
+    qx.a_map[1] = kDu;
+    qx.b_map[0] = kWg;
+    qx.b_map[1] = kWu;
+    qx.b_mn = 1;
+    qx.out = dx;
+    qx.ld_out = b.ld_x;
+    struct { int a, b; void *out; uint64_t m, n, ld; } weights[3] = {
+        {kDg, kX, dw_gate, b.f, b.d, b.ld_in}, {kDu, kX, dw_up, b.f, b.d, b.ld_in}, {kDy, kH, dw_down, b.d, b.f, b.ld_down}};
+    for (const auto &w : weights) {
+        GemmProblem &q = add_problem(a, w.m, w.n, 256);
+        q.kblocks[0] = blocks_of(T, kBK);
+        q.a_map[0] = (unsigned char)w.a;
+        q.b_map[0] = (unsigned char)w.b;
+        q.a_mn = q.b_mn = 1;
+        q.out = w.out;
+        q.ld_out = w.ld;
+        q.out_f32 = grad_dtype == DD_F32;
+        q.accumulate = accumulate != 0;
+    }
+    return launch_gemm<kEpiStore, 256>(ctx, a, stream);
+}

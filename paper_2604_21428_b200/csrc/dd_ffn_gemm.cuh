@@ -1,0 +1,445 @@
+// Tensor-core products of the gated feed-forward block: D = sum_s A_s B_s^T over one or two
+// K segments, bf16 operands, float32 accumulators in tensor memory, epilogues of the block.
+//
+// One persistent CTA per SM walks the 128 x BN output tiles of up to four problems.  Warp 4
+// (one lane) has the TMA engine fill a ring of stages of 64 K-elements (128-byte rows, 128-byte
+// swizzle), warp 5 (one lane) issues tcgen05.mma, warps 0-3 turn finished accumulators into
+// results.  Two accumulators alternate, so the epilogue of one tile runs under the products of
+// the next.  Operands are read where they lie in either order -- K contiguous, or M / N contiguous
+// (the descriptor's "major" bit) -- so no product of the backward pass needs a transposed copy.
+//
+// Every wait is bounded: on giving up a role raises the CTA's abort flag, all roles leave their
+// loops, copies and products in flight are awaited (again bounded), tensor memory is freed and
+// the caller's status word says DD_STATUS_WAIT_LIMIT.
+#pragma once
+
+#include <cuda.h>
+
+#include <cuda_bf16.h>
+
+#include "dd_learner.h"
+#include "dd_merge_tma.cuh"
+
+namespace ddm {
+
+constexpr int kGemmThreads = 192;
+constexpr int kBM = 128, kBK = 64;
+constexpr int kChunkBytes = 64 * 128;             // one TMA box: 64 rows of 64 bf16
+constexpr int kMaxMaps = 8, kMaxProblems = 4;
+
+enum GemmEpilogue { kEpiStore = 0, kEpiGate = 1, kEpiBack = 2 };
+
+struct GemmProblem {
+    unsigned m, n;                    // output rows and columns
+    unsigned tiles_m, tiles_n, tile_end;
+    unsigned kblocks[2];              // K blocks of the two segments (second may be 0)
+    unsigned char a_map[2], b_map[2]; // tensor maps of the segments; kEpiGate: b_map = {w_gate, w_up}
+    unsigned char a_mn, b_mn;         // 1: M (N) is the contiguous direction in memory
+    unsigned char out_f32, accumulate;
+    void *out;
+    const __nv_bfloat16 *residual;
+    unsigned long long ld_out, ld_residual;
+};
+
+struct GemmArgs {
+    CUtensorMap maps[kMaxMaps];       // 64 x 64 boxes of row-major bf16 matrices
+    GemmProblem prob[kMaxProblems];
+    int nprob;
+    unsigned tiles;
+    int activation;
+    int *status;
+    // kEpiGate: gate, up (null when not kept) are outputs; kEpiBack: inputs, and dgate, dup, hidden outputs
+    __nv_bfloat16 *gate, *up, *dgate, *dup, *hidden;
+    unsigned long long ld_gate, ld_hidden;
+};
+
+__host__ __device__ constexpr int gemm_stages(int bn) { return bn >= 256 ? 4 : bn >= 128 ? 6 : 8; }
+__host__ __device__ constexpr size_t gemm_stage_bytes(int bn) { return (size_t)(kBM + bn) * kBK * 2; }
+constexpr size_t gemm_smem_bytes(int bn) { return 1024 + gemm_stages(bn) * gemm_stage_bytes(bn) + 256; }
+
+// ---- tcgen05 ----------------------------------------------------------------------------------
+
+__device__ __forceinline__ bool elect_one()
+{
+    unsigned p;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p != 0;
+}
+
+__device__ __forceinline__ void tma_load_2d(unsigned dst, const CUtensorMap *map, int x, int y, unsigned bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void umma_bf16(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                 " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// Arrives on `bar` once every tcgen05.mma this thread has issued so far is complete.
+__device__ __forceinline__ void umma_commit(unsigned bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void mbar_arrive(unsigned bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld32(unsigned addr, unsigned (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// Shared-memory operand descriptor, 128-byte swizzle.  Chunks are 64 rows of 128 bytes.
+//   K contiguous: rows are M (N); groups of 8 rows follow every 1024 bytes, chunks continue them.
+//   M (N) contiguous: rows are K, groups of 8 every 1024 bytes; the next 64 M (N) are one chunk on.
+__device__ __forceinline__ unsigned long long umma_desc(unsigned addr, bool mn)
+{
+    const unsigned long long lead = mn ? kChunkBytes / 16 : 1, stride = 1024 / 16;
+    return ((unsigned long long)(addr >> 4) & 0x3fff) | (lead << 16) | (stride << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// ---- activation ---------------------------------------------------------------------------------
+
+// Both activations are g sigmoid(s(g)); returns a(g) and sets its derivative.  exp and the division
+// are the fast forms (2 ulp): their error is far below the bf16 rounding of what they feed.
+template <bool SLOPE>
+__device__ __forceinline__ float activate(float g, int kind, float *slope)
+{
+    constexpr float k = 1.5957691216057308f, q = 0.044715f;      // 2 sqrt(2 / pi)
+    const float s = kind == DD_ACT_SILU ? g : k * g * fmaf(q * g, g, 1.0f);
+    const float e = __expf(-s);
+    const float sg = __fdividef(1.0f, 1.0f + e);
+    if (SLOPE) {
+        const float ds = kind == DD_ACT_SILU ? 1.0f : k * fmaf(3.0f * q * g, g, 1.0f);
+        *slope = sg * fmaf(g * ds, 1.0f - sg, 1.0f);
+    }
+    return g * sg;
+}
+
+__device__ __forceinline__ unsigned pack2(float lo, float hi)
+{
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const unsigned *>(&b);
+}
+
+// 32 consecutive bf16 of a row: 16-byte pieces as far as the row goes, single elements at its end.
+__device__ __forceinline__ void store_row32(__nv_bfloat16 *dst, const float (&x)[32], unsigned cols)
+{
+#pragma unroll
+    for (int j = 0; j < 32; j += 8) {
+        if (j + 8 <= cols) {
+            *reinterpret_cast<uint4 *>(dst + j) = make_uint4(pack2(x[j], x[j + 1]), pack2(x[j + 2], x[j + 3]),
+                                                             pack2(x[j + 4], x[j + 5]), pack2(x[j + 6], x[j + 7]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (j + i < cols) dst[j + i] = __float2bfloat16_rn(x[j + i]);
+        }
+    }
+}
+
+__device__ __forceinline__ void load_row32(const __nv_bfloat16 *src, float (&x)[32], unsigned cols)
+{
+#pragma unroll
+    for (int j = 0; j < 32; j += 8) {
+        if (j + 8 <= cols) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(src + j);
+            const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[j + 2 * i] = __uint_as_float(u[i] << 16);
+                x[j + 2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[j + i] = j + i < cols ? __bfloat162float(src[j + i]) : 0.0f;
+        }
+    }
+}
+
+__device__ __forceinline__ void store_row32_f32(float *dst, const float (&x)[32], unsigned cols)
+{
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+        if (j + 4 <= cols) {
+            *reinterpret_cast<float4 *>(dst + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (j + i < cols) dst[j + i] = x[j + i];
+        }
+    }
+}
+
+__device__ __forceinline__ void load_row32_f32(const float *src, float (&x)[32], unsigned cols)
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j) x[j] = j < cols ? src[j] : 0.0f;
+}
+
+// ---- tiles ----------------------------------------------------------------------------------------
+
+struct TilePos {
+    int p;                    // problem
+    unsigned m0, n0;          // first output row and column
+};
+
+// Neighbouring tiles (what the SMs hold at one time) cover a block of 16 tile rows, so that both
+// operands of a wave stay in L2.
+template <int COLS>
+__device__ __forceinline__ TilePos tile_pos(const GemmArgs &a, unsigned t)
+{
+    TilePos r;
+    r.p = 0;
+    while (t >= a.prob[r.p].tile_end) ++r.p;
+    const GemmProblem &p = a.prob[r.p];
+    t -= r.p ? a.prob[r.p - 1].tile_end : 0u;
+    const unsigned group = 16 * p.tiles_n, g = t / group, first = 16 * g;
+    const unsigned rows = p.tiles_m - first < 16 ? p.tiles_m - first : 16;
+    t -= g * group;
+    r.m0 = (first + t % rows) * kBM;
+    r.n0 = (t / rows) * COLS;
+    return r;
+}
+
+__device__ __forceinline__ bool gemm_wait(unsigned bar, unsigned parity, volatile int *abort)
+{
+    for (int spins = 0; spins < kWaitLimit; ++spins) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*abort) return false;
+    }
+    *abort = 1;
+    return false;
+}
+
+// BN: accumulator columns of a tile.  kEpiGate puts BN / 2 columns of gate beside BN / 2 of up.
+template <int EPI, int BN>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
+{
+    constexpr int kStages = gemm_stages(BN);
+    constexpr unsigned kStageBytes = (unsigned)gemm_stage_bytes(BN);
+    constexpr int kCols = EPI == kEpiGate ? BN / 2 : BN;      // output columns of a tile
+    constexpr unsigned kTmemCols = 2 * BN < 32 ? 32 : 2 * BN;
+    static_assert((kTmemCols & (kTmemCols - 1)) == 0 && kTmemCols <= 512, "tensor memory is allocated in powers of two");
+
+    extern __shared__ unsigned char smem_raw[];
+    const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const unsigned bars = smem + kStages * kStageBytes;
+    const unsigned full = bars, empty = bars + 8 * kStages, tfull = empty + 8 * kStages, tempty = tfull + 16, drain = tempty + 16;
+    __shared__ int abort_flag;
+    __shared__ unsigned tmem_base;
+    volatile int *abort = &abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int s = 0; s < kStages; ++s) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(full + 8 * s) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(empty + 8 * s) : "memory");
+        }
+        for (int s = 0; s < 2; ++s) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(tfull + 8 * s) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 128;" :: "r"(tempty + 8 * s) : "memory");
+        }
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(drain) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     :: "r"(smem_addr(&tmem_base)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const unsigned tmem = tmem_base;
+
+    if (warp == 4) {
+        if (elect_one()) {
+            unsigned it = 0;              // stages filled so far
+            bool ok = true;
+            for (unsigned t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
+                const TilePos pos = tile_pos<kCols>(a, t);
+                const GemmProblem &p = a.prob[pos.p];
+                for (int seg = 0; ok && seg < 2; ++seg) {
+                    const CUtensorMap *ma = &a.maps[p.a_map[seg]];
+                    for (unsigned kb = 0; kb < p.kblocks[seg]; ++kb, ++it) {
+                        const unsigned s = it % kStages;
+                        if (it >= kStages && !gemm_wait(empty + 8 * s, (it / kStages - 1) & 1, abort)) { ok = false; break; }
+                        if (*abort) { ok = false; break; }
+                        const unsigned st = smem + s * kStageBytes, bar = full + 8 * s;
+                        mbar_arrive_expect_tx(bar, kStageBytes);
+                        const int k0 = (int)kb * kBK;
+#pragma unroll
+                        for (int c = 0; c < kBM / 64; ++c) {
+                            const int m = (int)pos.m0 + 64 * c;
+                            tma_load_2d(st + c * kChunkBytes, ma, p.a_mn ? m : k0, p.a_mn ? k0 : m, bar);
+                        }
+#pragma unroll
+                        for (int c = 0; c < BN / 64; ++c) {
+                            const int half = EPI == kEpiGate && c >= BN / 128;
+                            const CUtensorMap *mb = &a.maps[p.b_map[EPI == kEpiGate ? half : seg]];
+                            const int n = (int)pos.n0 + 64 * (half ? c - BN / 128 : c);
+                            tma_load_2d(st + kBM * kBK * 2 + c * kChunkBytes, mb, p.b_mn ? n : k0, p.b_mn ? k0 : n, bar);
+                        }
+                    }
+                }
+            }
+            // no copy may be in flight when the CTA ends, whoever gave up
+            for (unsigned j = it > kStages ? it - kStages : 0; j < it; ++j)
+                mbar_wait_bounded(full + 8 * (j % kStages), (j / kStages) & 1);
+        }
+    } else if (warp == 5) {
+        if (elect_one()) {
+            unsigned it = 0, acc = 0;     // stages consumed, tiles started
+            bool ok = true;
+            for (unsigned t = blockIdx.x; ok && t < a.tiles; t += gridDim.x, ++acc) {
+                const TilePos pos = tile_pos<kCols>(a, t);
+                const GemmProblem &p = a.prob[pos.p];
+                const unsigned slot = acc & 1;
+                if (acc >= 2 && !gemm_wait(tempty + 8 * slot, (acc / 2 - 1) & 1, abort)) { ok = false; break; }
+                tc_fence_after();
+                // float32 accumulators, bf16 x bf16, the operands' majors, N = BN, M = 128
+                const unsigned idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((unsigned)p.a_mn << 15) |
+                                       ((unsigned)p.b_mn << 16) | ((unsigned)(BN / 8) << 17) | ((kBM / 16) << 24);
+                const unsigned astep = p.a_mn ? 2048 : 32, bstep = p.b_mn ? 2048 : 32;     // bytes per 16 K elements
+                const unsigned blocks = p.kblocks[0] + p.kblocks[1];
+                for (unsigned kb = 0; kb < blocks; ++kb, ++it) {
+                    const unsigned s = it % kStages;
+                    if (!gemm_wait(full + 8 * s, (it / kStages) & 1, abort)) { ok = false; break; }
+                    tc_fence_after();
+                    const unsigned sa = smem + s * kStageBytes, sb = sa + kBM * kBK * 2;
+#pragma unroll
+                    for (int k = 0; k < kBK / 16; ++k)
+                        umma_bf16(tmem + slot * BN, umma_desc(sa + k * astep, p.a_mn), umma_desc(sb + k * bstep, p.b_mn),
+                                  idesc, kb | k);
+                    umma_commit(empty + 8 * s);
+                }
+                if (ok) umma_commit(tfull + 8 * slot);
+            }
+            umma_commit(drain);           // no product may be in flight when tensor memory is freed
+            mbar_wait_bounded(drain, 0);
+        }
+    } else {
+        unsigned acc = 0;
+        for (unsigned t = blockIdx.x; t < a.tiles; t += gridDim.x, ++acc) {
+            const TilePos pos = tile_pos<kCols>(a, t);
+            const GemmProblem &p = a.prob[pos.p];
+            const unsigned slot = acc & 1;
+            const bool ok = gemm_wait(tfull + 8 * slot, (acc / 2) & 1, abort);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            tc_fence_after();
+            const unsigned taddr = tmem + ((unsigned)(warp * 32) << 16) + slot * BN;
+            const unsigned row = pos.m0 + warp * 32 + lane;
+            const bool live = row < p.m;
+#pragma unroll 1
+            for (int c = 0; c < kCols; c += 32) {
+                const unsigned col = pos.n0 + c;
+                if (col >= p.n) break;
+                const unsigned cols = p.n - col < 32 ? p.n - col : 32;
+                unsigned r[32];
+                tmem_ld32(taddr + c, r);
+                float x[32];
+                if (EPI == kEpiGate) {
+                    unsigned r2[32];
+                    tmem_ld32(taddr + BN / 2 + c, r2);
+                    tmem_ld_wait();
+                    float u[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) { x[j] = __uint_as_float(r[j]); u[j] = __uint_as_float(r2[j]); }
+                    if (live) {
+                        const unsigned long long at = (unsigned long long)row * a.ld_gate + col;
+                        if (a.gate) {
+                            store_row32(a.gate + at, x, cols);
+                            store_row32(a.up + at, u, cols);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[j] = activate<false>(x[j], a.activation, nullptr) * u[j];
+                        store_row32(a.hidden + (unsigned long long)row * a.ld_hidden + col, x, cols);
+                    }
+                } else if (EPI == kEpiBack) {
+                    tmem_ld_wait();
+                    if (live) {
+                        float g[32], u[32];
+                        const unsigned long long at = (unsigned long long)row * a.ld_gate + col;
+                        const unsigned long long to = (unsigned long long)row * a.ld_hidden + col;
+                        load_row32(a.gate + at, g, cols);
+                        load_row32(a.up + at, u, cols);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float dh = __uint_as_float(r[j]);
+                            float slope;
+                            const float act = activate<true>(g[j], a.activation, &slope);
+                            x[j] = dh * act;                       // dup
+                            g[j] = dh * u[j] * slope;              // dgate
+                            u[j] = act * u[j];                     // hidden
+                        }
+                        store_row32(a.dup + to, x, cols);
+                        store_row32(a.dgate + to, g, cols);
+                        store_row32(a.hidden + to, u, cols);
+                    }
+                } else {
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
+                    if (live) {
+                        const unsigned long long at = (unsigned long long)row * p.ld_out + col;
+                        float add[32];
+                        if (p.residual) {
+                            load_row32(p.residual + (unsigned long long)row * p.ld_residual + col, add, cols);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) x[j] += add[j];
+                        }
+                        if (p.out_f32) {
+                            float *o = static_cast<float *>(p.out) + at;
+                            if (p.accumulate) {
+                                load_row32_f32(o, add, cols);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) x[j] += add[j];
+                            }
+                            store_row32_f32(o, x, cols);
+                        } else {
+                            __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.out) + at;
+                            if (p.accumulate) {
+                                load_row32(o, add, cols);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) x[j] += add[j];
+                            }
+                            store_row32(o, x, cols);
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+            mbar_arrive(tempty + 8 * slot);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 5)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
+    if (threadIdx.x == 0 && abort_flag && a.status) *a.status = DD_STATUS_WAIT_LIMIT;
+}
+
+}  // namespace ddm

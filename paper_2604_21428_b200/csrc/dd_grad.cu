@@ -1,0 +1,480 @@
+// The learner's optimizer side: global gradient norm, clipping and the AdamW step over lists of
+// tensors.  Every kernel walks one flat tile index over the whole list (persistent grid, tiles of
+// 8192 elements handed out round-robin), so many small tensors cost no launches of their own.
+#include <cmath>
+#include <cstring>
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "dd_ctx.h"
+#include "dd_learner.h"
+
+namespace ddm {
+
+constexpr int kListThreads = 256;
+constexpr int kListTile = 8192;              // elements: 32 per thread
+constexpr int kListSmall = 32, kListMax = 256;
+constexpr int kListCtasPerSm = 8;
+
+// One launch's tensors, by value in the kernel parameters: no staging copy, and nothing for a
+// stream capture to keep alive.  CAP = 32 keeps the parameters of short lists under 2 KB.
+template <int NPTR, int CAP>
+struct ListArgs {
+    void *ptr[NPTR][CAP];
+    unsigned long long n[CAP];
+    unsigned tile_end[CAP];                  // one past the tensor's last flat tile
+    unsigned char bf16[CAP];                 // type of the gradient
+    unsigned char vec[CAP];                  // every pointer is aligned for 16-byte (8-byte bf16) pieces
+    unsigned tiles;
+};
+
+struct NormTail {
+    double *partials;                        // one per CTA of every launch of the call
+    unsigned first, total;                   // this launch's offset; partials of the whole call
+    unsigned *ticket;
+    dd_grad_record *record;
+    float max_norm;
+    int last;                                // the call's last launch reduces
+};
+
+struct AdamwConsts {
+    float beta1, rest1, beta2, rest2, eps, decay, step_size, inv_c2;
+    const dd_grad_record *clip;
+};
+
+// Moves `i` to the tensor that holds flat tile `tile` (tiles are visited in ascending order) and
+// returns the tile's first element within it.
+template <typename A>
+__device__ __forceinline__ unsigned long long seek(const A &a, unsigned tile, int &i)
+{
+    while (tile >= a.tile_end[i]) ++i;
+    const unsigned begin = i ? a.tile_end[i - 1] : 0u;
+    return (unsigned long long)(tile - begin) * kListTile;
+}
+
+__device__ __forceinline__ float lo_bf16(unsigned w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_bf16(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ float load_elem(const void *p, bool bf16, unsigned long long e)
+{
+    return bf16 ? __uint_as_float((unsigned)static_cast<const unsigned short *>(p)[e] << 16)
+                : static_cast<const float *>(p)[e];
+}
+__device__ __forceinline__ unsigned short round_bf16(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi)
+{
+    return (unsigned)round_bf16(lo) | ((unsigned)round_bf16(hi) << 16);
+}
+
+__device__ __forceinline__ double block_sum(double x, double *sm)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = x;
+    __syncthreads();
+    double t = 0.0;
+#pragma unroll
+    for (int w = 0; w < kListThreads / 32; ++w) t += sm[w];
+    __syncthreads();
+    return t;
+}
+
+// sum of g^2: fp32 over the 32 elements a thread takes of a tile, fp64 across tiles, threads and
+// CTAs.  The CTA that draws the last ticket adds the partials in index order, so the result does
+// not depend on which one that is.
+template <int CAP>
+__global__ void __launch_bounds__(kListThreads)
+grad_norm_kernel(const __grid_constant__ ListArgs<1, CAP> a, const __grid_constant__ NormTail t)
+{
+    __shared__ double sm[kListThreads / 32];
+    __shared__ unsigned drawn;
+    double acc = 0.0;
+    int i = 0;
+    for (unsigned tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+        const unsigned long long base = seek(a, tile, i);
+        const void *g = a.ptr[0][i];
+        const unsigned long long left = a.n[i] - base;
+        float s = 0.0f;
+        if (a.vec[i] && left >= kListTile) {
+            if (a.bf16[i]) {
+                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const unsigned short *>(g) + base) + threadIdx.x;
+                uint4 w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = __ldg(p + k * kListThreads);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const unsigned x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s = fmaf(lo_bf16(x[j]), lo_bf16(x[j]), s);
+                        s = fmaf(hi_bf16(x[j]), hi_bf16(x[j]), s);
+                    }
+                }
+            } else {
+                const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(g) + base) + threadIdx.x;
+                float4 w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = __ldg(p + k * kListThreads);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s = fmaf(w[k].x, w[k].x, fmaf(w[k].y, w[k].y, fmaf(w[k].z, w[k].z, fmaf(w[k].w, w[k].w, s))));
+            }
+        } else {
+            const unsigned m = left < kListTile ? (unsigned)left : kListTile;
+#pragma unroll 8
+            for (unsigned e = threadIdx.x; e < m; e += kListThreads) {
+                const float x = load_elem(g, a.bf16[i], base + e);
+                s = fmaf(x, x, s);
+            }
+        }
+        acc += (double)s;
+    }
+    const double part = block_sum(acc, sm);
+    if (threadIdx.x == 0) {
+        t.partials[t.first + blockIdx.x] = part;
+        __threadfence();
+        drawn = t.last ? atomicAdd(t.ticket, 1u) : 0xffffffffu;
+    }
+    __syncthreads();
+    if (drawn != gridDim.x - 1) return;
+    __threadfence();
+    double x = 0.0;
+    for (unsigned k = threadIdx.x; k < t.total; k += kListThreads) x += __ldcg(t.partials + k);
+    x = block_sum(x, sm);
+    if (threadIdx.x == 0) {
+        const float norm = (float)sqrt(x);
+        const bool ok = isfinite(norm);
+        t.record->norm_sq = x;
+        t.record->norm = norm;
+        t.record->scale = ok ? fminf(1.0f, t.max_norm / (norm + 1e-6f)) : 1.0f;
+        t.record->status = ok ? DD_STATUS_OK : DD_STATUS_NONFINITE;
+        t.record->reserved = 0;
+        *t.ticket = 0;
+    }
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kListThreads)
+grad_scale_kernel(const __grid_constant__ ListArgs<2, CAP> a, const dd_grad_record *record, int in_place)
+{
+    const float scale = record->scale;
+    if (record->status != DD_STATUS_OK || (in_place && scale == 1.0f)) return;
+    int i = 0;
+    for (unsigned tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+        const unsigned long long base = seek(a, tile, i);
+        const void *g = a.ptr[0][i];
+        void *o = a.ptr[1][i];
+        const unsigned long long left = a.n[i] - base;
+        if (a.vec[i] && left >= kListTile) {
+            if (a.bf16[i]) {
+                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const unsigned short *>(g) + base) + threadIdx.x;
+                uint4 *q = reinterpret_cast<uint4 *>(static_cast<unsigned short *>(o) + base) + threadIdx.x;
+                uint4 w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = p[k * kListThreads];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    q[k * kListThreads] = make_uint4(pack_bf16(scale * lo_bf16(w[k].x), scale * hi_bf16(w[k].x)),
+                                                     pack_bf16(scale * lo_bf16(w[k].y), scale * hi_bf16(w[k].y)),
+                                                     pack_bf16(scale * lo_bf16(w[k].z), scale * hi_bf16(w[k].z)),
+                                                     pack_bf16(scale * lo_bf16(w[k].w), scale * hi_bf16(w[k].w)));
+            } else {
+                const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(g) + base) + threadIdx.x;
+                float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(o) + base) + threadIdx.x;
+                float4 w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = p[k * kListThreads];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    q[k * kListThreads] = make_float4(scale * w[k].x, scale * w[k].y, scale * w[k].z, scale * w[k].w);
+            }
+        } else {
+            const unsigned m = left < kListTile ? (unsigned)left : kListTile;
+            for (unsigned e = threadIdx.x; e < m; e += kListThreads) {
+                const float x = scale * load_elem(g, a.bf16[i], base + e);
+                if (a.bf16[i]) static_cast<unsigned short *>(o)[base + e] = round_bf16(x);
+                else static_cast<float *>(o)[base + e] = x;
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void adamw_elem(float &p, float &m, float &v, float g, const AdamwConsts &c)
+{
+    m = fmaf(c.beta1, m, c.rest1 * g);
+    v = fmaf(c.beta2, v, c.rest2 * g * g);
+    p = fmaf(p, c.decay, -c.step_size * (m / (sqrtf(v * c.inv_c2) + c.eps)));
+}
+
+// ptr: 0 p, 1 m, 2 v, 3 gradient, 4 bf16 copy (may be null).
+template <int CAP>
+__global__ void __launch_bounds__(kListThreads)
+adamw_kernel(const __grid_constant__ ListArgs<5, CAP> a, const __grid_constant__ AdamwConsts c)
+{
+    float scale = 1.0f;
+    if (c.clip) {
+        if (c.clip->status != DD_STATUS_OK) return;
+        scale = c.clip->scale;
+    }
+    int i = 0;
+    for (unsigned tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+        const unsigned long long base = seek(a, tile, i);
+        float *p = static_cast<float *>(a.ptr[0][i]) + base;
+        float *m = static_cast<float *>(a.ptr[1][i]) + base;
+        float *v = static_cast<float *>(a.ptr[2][i]) + base;
+        unsigned short *o = static_cast<unsigned short *>(a.ptr[4][i]);
+        const unsigned long long left = a.n[i] - base;
+        const bool bf16 = a.bf16[i];
+        const unsigned cnt = left < kListTile ? (unsigned)left : kListTile;
+        const unsigned vec_end = a.vec[i] ? cnt & ~3u : 0u;
+#pragma unroll 2
+        for (unsigned e = 4 * threadIdx.x; e < vec_end; e += 4 * kListThreads) {
+            float4 P = *reinterpret_cast<const float4 *>(p + e), M = *reinterpret_cast<const float4 *>(m + e),
+                   V = *reinterpret_cast<const float4 *>(v + e), G;
+            if (bf16) {
+                const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const unsigned short *>(a.ptr[3][i]) + base + e);
+                G = make_float4(lo_bf16(w.x), hi_bf16(w.x), lo_bf16(w.y), hi_bf16(w.y));
+            } else {
+                G = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.ptr[3][i]) + base + e);
+            }
+            adamw_elem(P.x, M.x, V.x, scale * G.x, c);
+            adamw_elem(P.y, M.y, V.y, scale * G.y, c);
+            adamw_elem(P.z, M.z, V.z, scale * G.z, c);
+            adamw_elem(P.w, M.w, V.w, scale * G.w, c);
+            *reinterpret_cast<float4 *>(p + e) = P;
+            *reinterpret_cast<float4 *>(m + e) = M;
+            *reinterpret_cast<float4 *>(v + e) = V;
+            if (o) *reinterpret_cast<uint2 *>(o + base + e) = make_uint2(pack_bf16(P.x, P.y), pack_bf16(P.z, P.w));
+        }
+        for (unsigned e = vec_end + threadIdx.x; e < cnt; e += kListThreads) {
+            float P = p[e], M = m[e], V = v[e];
+            adamw_elem(P, M, V, scale * load_elem(a.ptr[3][i], bf16, base + e), c);
+            p[e] = P;
+            m[e] = M;
+            v[e] = V;
+            if (o) o[base + e] = round_bf16(P);
+        }
+    }
+}
+
+// ---- host side ----------------------------------------------------------------------------
+
+static bool ranges_overlap(const void *a, size_t abytes, const void *b, size_t bbytes)
+{
+    if (!a || !b || !abytes || !bbytes) return false;
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + bbytes && y < x + abytes;
+}
+
+static int check_list(const dd_ctx *ctx, const uint64_t *sizes, const uint8_t *dtypes, int count)
+{
+    if (!ctx || count < 0 || (count > 0 && (!sizes || !dtypes))) return DD_ERR_INVALID_ARG;
+    for (int i = 0; i < count; ++i) {
+        if (dtypes[i] != DD_F32 && dtypes[i] != DD_BF16) return DD_ERR_INVALID_ARG;
+        if (sizes[i] > kMaxFragmentElems) return DD_ERR_TOO_LARGE;
+    }
+    return DD_OK;
+}
+
+static int check_grads(const void *const *grads, const uint64_t *sizes, const uint8_t *dtypes, int count)
+{
+    if (count > 0 && !grads) return DD_ERR_INVALID_ARG;
+    for (int i = 0; i < count; ++i) {
+        if (sizes[i] == 0) continue;
+        if (!grads[i]) return DD_ERR_INVALID_ARG;
+        if ((uintptr_t)grads[i] & (dtypes[i] == DD_BF16 ? 1u : 3u)) return DD_ERR_ALIGNMENT;
+    }
+    return DD_OK;
+}
+
+// Fills one launch's arguments with tensors [at, ...) and returns the index of the first tensor
+// left over.  Tensors without elements take no tile and are left out.
+template <int NPTR, int CAP, typename F>
+static int fill_list(ListArgs<NPTR, CAP> &a, const uint64_t *sizes, const uint8_t *dtypes, int count, int at, F pointers)
+{
+    int k = 0;
+    a.tiles = 0;
+    for (; at < count && k < CAP; ++at) {
+        if (sizes[at] == 0) continue;
+        void *p[NPTR];
+        a.vec[k] = pointers(at, p);
+        for (int j = 0; j < NPTR; ++j) a.ptr[j][k] = p[j];
+        a.n[k] = sizes[at];
+        a.bf16[k] = dtypes[at] == DD_BF16;
+        a.tiles += (unsigned)((sizes[at] + kListTile - 1) / kListTile);
+        a.tile_end[k++] = a.tiles;
+    }
+    return at;
+}
+
+static unsigned list_grid(const dd_ctx *ctx, unsigned tiles)
+{
+    const unsigned most = (unsigned)(ctx->sm_count * kListCtasPerSm);
+    return tiles < 1 ? 1 : tiles < most ? tiles : most;
+}
+
+template <int CAP>
+static int launch_norm(dd_ctx *ctx, const void *const *grads, const uint64_t *sizes, const uint8_t *dtypes,
+                       int count, float max_norm, dd_grad_record *record, cudaStream_t stream)
+{
+    const size_t launches = count > CAP ? (size_t)(count + CAP - 1) / CAP : 1;
+    const int rc = ensure_workspace(ctx, 1, 1, launches * ctx->sm_count * kListCtasPerSm);
+    if (rc != DD_OK) return rc;
+    NormTail t;
+    t.partials = ctx->partials;
+    t.ticket = ctx->tickets;
+    t.record = record;
+    t.max_norm = max_norm;
+    t.first = 0;
+    int at = 0;
+    do {
+        ListArgs<1, CAP> a;
+        at = fill_list(a, sizes, dtypes, count, at, [&](int i, void **p) {
+            p[0] = const_cast<void *>(grads[i]);
+            return ((uintptr_t)p[0] & 15u) == 0;
+        });
+        const unsigned grid = list_grid(ctx, a.tiles);
+        t.last = at >= count;
+        t.total = t.first + grid;
+        grad_norm_kernel<CAP><<<grid, kListThreads, 0, stream>>>(a, t);
+        DD_CUDA(ctx, cudaGetLastError());
+        t.first += grid;
+    } while (at < count);
+    return DD_OK;
+}
+
+template <int CAP>
+static int launch_scale(dd_ctx *ctx, void *const *grads, void *const *outs, const uint64_t *sizes,
+                        const uint8_t *dtypes, int count, const dd_grad_record *record, cudaStream_t stream)
+{
+    for (int at = 0; at < count;) {
+        ListArgs<2, CAP> a;
+        at = fill_list(a, sizes, dtypes, count, at, [&](int i, void **p) {
+            p[0] = grads[i];
+            p[1] = outs ? outs[i] : grads[i];
+            return (((uintptr_t)p[0] | (uintptr_t)p[1]) & 15u) == 0;
+        });
+        if (!a.tiles) continue;
+        grad_scale_kernel<CAP><<<list_grid(ctx, a.tiles), kListThreads, 0, stream>>>(a, record, outs == nullptr);
+        DD_CUDA(ctx, cudaGetLastError());
+    }
+    return DD_OK;
+}
+
+template <int CAP>
+static int launch_adamw(dd_ctx *ctx, const AdamwConsts &c, float *const *params, const void *const *grads,
+                        float *const *m, float *const *v, void *const *copies, const uint64_t *sizes,
+                        const uint8_t *dtypes, int count, cudaStream_t stream)
+{
+    for (int at = 0; at < count;) {
+        ListArgs<5, CAP> a;
+        at = fill_list(a, sizes, dtypes, count, at, [&](int i, void **p) {
+            p[0] = params[i];
+            p[1] = m[i];
+            p[2] = v[i];
+            p[3] = const_cast<void *>(grads[i]);
+            p[4] = copies ? copies[i] : nullptr;
+            const uintptr_t wide = (uintptr_t)p[0] | (uintptr_t)p[1] | (uintptr_t)p[2];
+            const unsigned gmask = dtypes[i] == DD_BF16 ? 7u : 15u;
+            return (wide & 15u) == 0 && ((uintptr_t)p[3] & gmask) == 0 && ((uintptr_t)p[4] & 7u) == 0;
+        });
+        if (!a.tiles) continue;
+        adamw_kernel<CAP><<<list_grid(ctx, a.tiles), kListThreads, 0, stream>>>(a, c);
+        DD_CUDA(ctx, cudaGetLastError());
+    }
+    return DD_OK;
+}
+
+static int check_norm_args(const dd_ctx *ctx, const void *const *grads, const uint64_t *sizes, const uint8_t *dtypes,
+                           int count, float max_norm, const dd_grad_record *record)
+{
+    int rc = check_list(ctx, sizes, dtypes, count);
+    if (rc != DD_OK) return rc;
+    if (!record || !(max_norm >= 0.0f)) return DD_ERR_INVALID_ARG;
+    if ((uintptr_t)record & 7u) return DD_ERR_ALIGNMENT;
+    return check_grads(grads, sizes, dtypes, count);
+}
+
+}  // namespace ddm
+
+using namespace ddm;
+
+extern "C" int dd_grad_norm(dd_ctx *ctx, const void *const *grads, const uint64_t *sizes, const uint8_t *dtypes,
+                            int count, float max_norm, dd_grad_record *record, void *cuda_stream)
+{
+    const int rc = check_norm_args(ctx, grads, sizes, dtypes, count, max_norm, record);
+    if (rc != DD_OK) return rc;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return cuda_fail(ctx, cudaErrorInvalidDevice, "cudaSetDevice");
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    return count <= kListSmall ? launch_norm<kListSmall>(ctx, grads, sizes, dtypes, count, max_norm, record, stream)
+                               : launch_norm<kListMax>(ctx, grads, sizes, dtypes, count, max_norm, record, stream);
+}
+
+extern "C" int dd_clip_gradients(dd_ctx *ctx, void *const *grads, void *const *outs, const uint64_t *sizes,
+                                 const uint8_t *dtypes, int count, float max_norm, dd_grad_record *record,
+                                 void *cuda_stream)
+{
+    int rc = check_norm_args(ctx, grads, sizes, dtypes, count, max_norm, record);
+    if (rc != DD_OK) return rc;
+    for (int i = 0; outs && i < count; ++i) {
+        if (sizes[i] == 0) continue;
+        const size_t eb = dtypes[i] == DD_BF16 ? 2 : 4;
+        if (!outs[i]) return DD_ERR_INVALID_ARG;
+        if ((uintptr_t)outs[i] & (eb - 1)) return DD_ERR_ALIGNMENT;
+        if (outs[i] != grads[i] && ranges_overlap(outs[i], eb * sizes[i], grads[i], eb * sizes[i])) return DD_ERR_ALIAS;
+    }
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return cuda_fail(ctx, cudaErrorInvalidDevice, "cudaSetDevice");
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    rc = count <= kListSmall ? launch_norm<kListSmall>(ctx, grads, sizes, dtypes, count, max_norm, record, stream)
+                             : launch_norm<kListMax>(ctx, grads, sizes, dtypes, count, max_norm, record, stream);
+    if (rc != DD_OK) return rc;
+    return count <= kListSmall ? launch_scale<kListSmall>(ctx, grads, outs, sizes, dtypes, count, record, stream)
+                               : launch_scale<kListMax>(ctx, grads, outs, sizes, dtypes, count, record, stream);
+}
+
+extern "C" int dd_adamw_step(dd_ctx *ctx, const dd_adamw *opt, float *const *params, const void *const *grads,
+                             float *const *exp_avg, float *const *exp_avg_sq, void *const *copies,
+                             const uint64_t *sizes, const uint8_t *dtypes, int count, const dd_grad_record *clip,
+                             void *cuda_stream)
+{
+    int rc = check_list(ctx, sizes, dtypes, count);
+    if (rc != DD_OK) return rc;
+    if (!opt || opt->step < 1 || !std::isfinite(opt->lr) || !std::isfinite(opt->weight_decay) ||
+        !(opt->beta1 >= 0.0 && opt->beta1 < 1.0) || !(opt->beta2 >= 0.0 && opt->beta2 < 1.0) ||
+        !(opt->eps >= 0.0 && std::isfinite(opt->eps)))
+        return DD_ERR_INVALID_ARG;
+    if (count > 0 && (!params || !exp_avg || !exp_avg_sq)) return DD_ERR_INVALID_ARG;
+    if ((uintptr_t)clip & 7u) return DD_ERR_ALIGNMENT;
+    rc = check_grads(grads, sizes, dtypes, count);
+    if (rc != DD_OK) return rc;
+    for (int i = 0; i < count; ++i) {
+        const size_t n = sizes[i];
+        if (n == 0) continue;
+        const void *p[5] = {params[i], exp_avg[i], exp_avg_sq[i], grads[i], copies ? copies[i] : nullptr};
+        const size_t bytes[5] = {4 * n, 4 * n, 4 * n, (dtypes[i] == DD_BF16 ? 2 : 4) * n, 2 * n};
+        if (!p[0] || !p[1] || !p[2]) return DD_ERR_INVALID_ARG;
+        if ((((uintptr_t)p[0] | (uintptr_t)p[1] | (uintptr_t)p[2]) & 3u) || ((uintptr_t)p[4] & 1u)) return DD_ERR_ALIGNMENT;
+        for (int x = 0; x < 5; ++x)
+            for (int y = 0; y < x; ++y)
+                if (ranges_overlap(p[x], bytes[x], p[y], bytes[y])) return DD_ERR_ALIAS;
+    }
+    AdamwConsts c;
+    const double c1 = -std::expm1((double)opt->step * std::log(opt->beta1));     // 1 - beta1^step
+    const double c2 = -std::expm1((double)opt->step * std::log(opt->beta2));
+    c.beta1 = (float)opt->beta1;
+    c.rest1 = (float)(1.0 - opt->beta1);
+    c.beta2 = (float)opt->beta2;
+    c.rest2 = (float)(1.0 - opt->beta2);
+    c.eps = (float)opt->eps;
+    c.decay = (float)(1.0 - opt->lr * opt->weight_decay);
+    c.step_size = (float)(opt->lr / c1);
+    c.inv_c2 = (float)(1.0 / c2);
+    c.clip = clip;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return cuda_fail(ctx, cudaErrorInvalidDevice, "cudaSetDevice");
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    return count <= kListSmall
+               ? launch_adamw<kListSmall>(ctx, c, params, grads, exp_avg, exp_avg_sq, copies, sizes, dtypes, count, stream)
+               : launch_adamw<kListMax>(ctx, c, params, grads, exp_avg, exp_avg_sq, copies, sizes, dtypes, count, stream);
+}
