@@ -5,7 +5,7 @@
 #include <cstring>
 
 #include "dd_ctx.h"
-#include "dd_ffn_gemm.cuh"
+#include "dd_ffn_stream.cuh"
 
 namespace ddm {
 
@@ -36,10 +36,10 @@ struct Matrix {
     unsigned long long rows, cols, ld;      // bf16 elements
 };
 
-static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m)
+static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m, unsigned box_rows = 64)
 {
     const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * 2};
-    const cuuint32_t box[2] = {64, 64}, step[2] = {1, 1};
+    const cuuint32_t box[2] = {64, box_rows}, step[2] = {1, 1};
     const EncodeTiled fn = tensor_map_encoder();
     if (!fn || fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(m.data), dims, strides, box, step,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -65,15 +65,90 @@ static GemmProblem &add_problem(GemmArgs &a, unsigned long long m, unsigned long
     return p;
 }
 
+// ---- few tokens ----------------------------------------------------------------------------
+
+// Up to here the weight-streaming kernel is ahead of the 128 x 256 tiles.
+constexpr unsigned long long kStreamMaxTokens = 256;
+
+// Ring of a CTA: two CTAs share an SM.
+constexpr unsigned kStreamRing = 96 * 1024;
+
+static int stream_cols(unsigned long long tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128; }
+static unsigned stream_box(unsigned long long tokens) { return stream_cols(tokens) < 64 ? (unsigned)stream_cols(tokens) : 64; }
+
+// Kernels opt in to their shared memory once per process and device.
+template <typename K>
+static int allow_smem(dd_ctx *ctx, K kernel, size_t bytes, bool (&done)[64])
+{
+    const int d = ctx->device;
+    if (d < 64 && done[d]) return DD_OK;
+    DD_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    if (d < 64) done[d] = true;
+    return DD_OK;
+}
+
 template <int EPI, int BN>
 static int launch_gemm(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
 {
     constexpr size_t smem = gemm_smem_bytes(BN);
-    DD_CUDA(ctx, cudaFuncSetAttribute(ffn_gemm_kernel<EPI, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    static bool done[64];
+    const int rc = allow_smem(ctx, ffn_gemm_kernel<EPI, BN>, smem, done);
+    if (rc != DD_OK) return rc;
     const unsigned grid = a.tiles < (unsigned)ctx->sm_count ? a.tiles : (unsigned)ctx->sm_count;
     ffn_gemm_kernel<EPI, BN><<<grid, kGemmThreads, smem, stream>>>(a);
     DD_CUDA(ctx, cudaGetLastError());
     return DD_OK;
+}
+
+template <int EPI, int N>
+static int launch_stream_n(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
+{
+    a.tiles_n = blocks_of(a.n, N);
+    const unsigned tiles = blocks_of(a.m, stream_features(EPI)) * a.tiles_n, blocks = a.kblocks[0] + a.kblocks[1];
+    // One CTA per SM at least, as long as each rank keeps two K blocks
+    unsigned s = 1;
+    while (s < kStreamMaxCluster && tiles * s < (unsigned)ctx->sm_count && blocks >= 4 * s) s *= 2;
+    unsigned stages = kStreamRing / stream_stage_bytes(N);
+    a.cluster = (int)s;
+    a.stages = (int)(stages > kStreamMaxStages ? kStreamMaxStages : stages);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(tiles * s);
+    cfg.blockDim = dim3(kGemmThreads);
+    cfg.dynamicSmemBytes = stream_smem_bytes(N, a.stages);
+    cfg.stream = stream;
+    static bool done[64];
+    const int rc = allow_smem(ctx, ffn_stream_kernel<EPI, N>, cfg.dynamicSmemBytes, done);
+    if (rc != DD_OK) return rc;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {s, 1, 1};
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_stream_kernel<EPI, N>, a));
+    return DD_OK;
+}
+
+template <int EPI>
+static int launch_stream(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
+{
+    switch (stream_cols(a.n)) {
+    case 16: return launch_stream_n<EPI, 16>(ctx, a, stream);
+    case 32: return launch_stream_n<EPI, 32>(ctx, a, stream);
+    case 64: return launch_stream_n<EPI, 64>(ctx, a, stream);
+    default: return launch_stream_n<EPI, 128>(ctx, a, stream);
+    }
+}
+
+static StreamArgs stream_args(const EpilogueArgs &e, uint64_t features, uint64_t tokens)
+{
+    StreamArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.m = (unsigned)features;
+    a.n = (unsigned)tokens;
+    a.e = e;
+    return a;
 }
 
 // Context-owned scratch for callers that bring none.
@@ -183,31 +258,54 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
         hidden = ctx->ffn_scratch;
     }
     cudaStream_t stream = (cudaStream_t)cuda_stream;
+    EpilogueArgs e;
+    std::memset(&e, 0, sizeof e);
+    e.activation = b.activation;
+    e.status = status;
+    e.gate = (__nv_bfloat16 *)gate;
+    e.up = (__nv_bfloat16 *)up;
+    e.hidden = (__nv_bfloat16 *)hidden;
+    e.ld_gate = b.ld_gate;
+    e.ld_hidden = ldh;
+    e.out = (__nv_bfloat16 *)y;
+    e.residual = (const __nv_bfloat16 *)residual;
+    e.ld_out = e.ld_residual = b.ld_y;
+    const Matrix mx = {x, T, b.d, b.ld_x}, mg = {b.w_gate, b.f, b.d, b.ld_in}, mu = {b.w_up, b.f, b.d, b.ld_in},
+                 md = {b.w_down, b.d, b.f, b.ld_down}, mh = {hidden, T, b.f, ldh};
+    if (T <= kStreamMaxTokens) {
+        StreamArgs a = stream_args(e, b.f, T);
+        a.kblocks[0] = blocks_of(b.d, kBK);
+        rc = encode(ctx, &a.w[0], mg);
+        if (rc == DD_OK) rc = encode(ctx, &a.w[1], mu);
+        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mx, stream_box(T));
+        if (rc == DD_OK) rc = launch_stream<kEpiGate>(ctx, a, stream);
+        if (rc != DD_OK) return rc;
+        a.m = (unsigned)b.d;
+        a.kblocks[0] = blocks_of(b.f, kBK);
+        a.own_prior = 1;
+        rc = encode(ctx, &a.w[0], md);
+        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mh, stream_box(T));
+        return rc == DD_OK ? launch_stream<kEpiStore>(ctx, a, stream) : rc;
+    }
     GemmArgs a;
     std::memset(&a, 0, sizeof a);
-    a.activation = b.activation;
-    a.status = status;
-    a.gate = (__nv_bfloat16 *)gate;
-    a.up = (__nv_bfloat16 *)up;
-    a.hidden = (__nv_bfloat16 *)hidden;
-    a.ld_gate = b.ld_gate;
-    a.ld_hidden = ldh;
-    rc = encode(ctx, &a.maps[0], {x, T, b.d, b.ld_x});
-    if (rc == DD_OK) rc = encode(ctx, &a.maps[1], {b.w_gate, b.f, b.d, b.ld_in});
-    if (rc == DD_OK) rc = encode(ctx, &a.maps[2], {b.w_up, b.f, b.d, b.ld_in});
+    a.e = e;
+    rc = encode(ctx, &a.maps[0], mx);
+    if (rc == DD_OK) rc = encode(ctx, &a.maps[1], mg);
+    if (rc == DD_OK) rc = encode(ctx, &a.maps[2], mu);
     if (rc != DD_OK) return rc;
     GemmProblem &p = add_problem(a, T, b.f, 128);
     p.kblocks[0] = blocks_of(b.d, kBK);
-    p.a_map[0] = 0;
     p.b_map[0] = 1;
     p.b_map[1] = 2;
     rc = launch_gemm<kEpiGate, 256>(ctx, a, stream);
     if (rc != DD_OK) return rc;
 
+    std::memset(a.prob, 0, sizeof a.prob);
     a.nprob = 0;
     a.tiles = 0;
-    rc = encode(ctx, &a.maps[0], {hidden, T, b.f, ldh});
-    if (rc == DD_OK) rc = encode(ctx, &a.maps[1], {b.w_down, b.d, b.f, b.ld_down});
+    rc = encode(ctx, &a.maps[0], mh);
+    if (rc == DD_OK) rc = encode(ctx, &a.maps[1], md);
     if (rc != DD_OK) return rc;
     GemmProblem &q = add_problem(a, T, b.d, 256);
     q.kblocks[0] = blocks_of(b.f, kBK);
@@ -264,40 +362,62 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
                                    {dg, T, b.f, ldh}, {du, T, b.f, ldh}, {h, T, b.f, ldh}};
     GemmArgs a;
     std::memset(&a, 0, sizeof a);
+    const bool few = T <= kStreamMaxTokens;
     for (int i = 0; i < kMaxMaps; ++i) {
         rc = encode(ctx, &a.maps[i], mats[i]);
         if (rc != DD_OK) return rc;
     }
-    a.activation = b.activation;
-    a.status = status;
-    a.gate = (__nv_bfloat16 *)const_cast<void *>(gate);
-    a.up = (__nv_bfloat16 *)const_cast<void *>(up);
-    a.dgate = dg;
-    a.dup = du;
-    a.hidden = h;
-    a.ld_gate = b.ld_gate;
-    a.ld_hidden = ldh;
+    EpilogueArgs &e = a.e;
+    e.activation = b.activation;
+    e.status = status;
+    e.gate = (__nv_bfloat16 *)const_cast<void *>(gate);
+    e.up = (__nv_bfloat16 *)const_cast<void *>(up);
+    e.dgate = dg;
+    e.dup = du;
+    e.hidden = h;
+    e.ld_gate = b.ld_gate;
+    e.ld_hidden = ldh;
     // dh = dy w_down: [T, d] x [d, f], and the gradients inside the block in its epilogue
-    GemmProblem &p = add_problem(a, T, b.f, 256);
-    p.kblocks[0] = blocks_of(b.d, kBK);
-    p.a_map[0] = kDy;
-    p.b_map[0] = kWd;
-    p.b_mn = 1;
-    rc = launch_gemm<kEpiBack, 256>(ctx, a, stream);
-    if (rc != DD_OK) return rc;
-
-    std::memset(a.prob, 0, sizeof a.prob);
-    a.nprob = 0;
-    a.tiles = 0;
-    GemmProblem &qx = add_problem(a, T, b.d, 256);        // dgate w_gate + dup w_up
-    qx.kblocks[0] = qx.kblocks[1] = blocks_of(b.f, kBK);
-    qx.a_map[0] = kDg;
-    qx.a_map[1] = kDu;
-    qx.b_map[0] = kWg;
-    qx.b_map[1] = kWu;
-    qx.b_mn = 1;
-    qx.out = dx;
-    qx.ld_out = b.ld_x;
+    if (few) {
+        StreamArgs c = stream_args(e, b.f, T);
+        c.e.out = (__nv_bfloat16 *)dx;
+        c.e.ld_out = b.ld_x;
+        c.kblocks[0] = blocks_of(b.d, kBK);
+        c.w[0] = a.maps[kWd];
+        c.w_mn = 1;
+        rc = encode(ctx, &c.x[0], mats[kDy], stream_box(T));
+        if (rc == DD_OK) rc = launch_stream<kEpiBack>(ctx, c, stream);
+        if (rc != DD_OK) return rc;
+        c.m = (unsigned)b.d;                              // dgate w_gate + dup w_up
+        c.kblocks[0] = c.kblocks[1] = blocks_of(b.f, kBK);
+        c.w[0] = a.maps[kWg];
+        c.w[1] = a.maps[kWu];
+        c.own_prior = 1;
+        rc = encode(ctx, &c.x[0], mats[kDg], stream_box(T));
+        if (rc == DD_OK) rc = encode(ctx, &c.x[1], mats[kDu], stream_box(T));
+        if (rc == DD_OK) rc = launch_stream<kEpiStore>(ctx, c, stream);
+        if (rc != DD_OK) return rc;
+    } else {
+        GemmProblem &p = add_problem(a, T, b.f, 256);
+        p.kblocks[0] = blocks_of(b.d, kBK);
+        p.a_map[0] = kDy;
+        p.b_map[0] = kWd;
+        p.b_mn = 1;
+        rc = launch_gemm<kEpiBack, 256>(ctx, a, stream);
+        if (rc != DD_OK) return rc;
+        std::memset(a.prob, 0, sizeof a.prob);
+        a.nprob = 0;
+        a.tiles = 0;
+        GemmProblem &qx = add_problem(a, T, b.d, 256);
+        qx.kblocks[0] = qx.kblocks[1] = blocks_of(b.f, kBK);
+        qx.a_map[0] = kDg;
+        qx.a_map[1] = kDu;
+        qx.b_map[0] = kWg;
+        qx.b_map[1] = kWu;
+        qx.b_mn = 1;
+        qx.out = dx;
+        qx.ld_out = b.ld_x;
+    }
     struct { int a, b; void *out; uint64_t m, n, ld; } weights[3] = {
         {kDg, kX, dw_gate, b.f, b.d, b.ld_in}, {kDu, kX, dw_up, b.f, b.d, b.ld_in}, {kDy, kH, dw_down, b.d, b.f, b.ld_down}};
     for (const auto &w : weights) {

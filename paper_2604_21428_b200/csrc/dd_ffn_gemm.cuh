@@ -29,6 +29,16 @@ constexpr int kMaxMaps = 8, kMaxProblems = 4;
 
 enum GemmEpilogue { kEpiStore = 0, kEpiGate = 1, kEpiBack = 2 };
 
+// What the epilogues read and write.  kEpiGate: gate and up (null when not kept) and hidden are outputs;
+// kEpiBack: gate and up are inputs, dgate, dup and hidden outputs; kEpiStore: out = sums [+ residual].
+struct EpilogueArgs {
+    __nv_bfloat16 *gate, *up, *dgate, *dup, *hidden, *out;
+    const __nv_bfloat16 *residual;
+    unsigned long long ld_gate, ld_hidden, ld_out, ld_residual;
+    int *status;
+    int activation;
+};
+
 struct GemmProblem {
     unsigned m, n;                    // output rows and columns
     unsigned tiles_m, tiles_n, tile_end;
@@ -46,11 +56,7 @@ struct GemmArgs {
     GemmProblem prob[kMaxProblems];
     int nprob;
     unsigned tiles;
-    int activation;
-    int *status;
-    // kEpiGate: gate, up (null when not kept) are outputs; kEpiBack: inputs, and dgate, dup, hidden outputs
-    __nv_bfloat16 *gate, *up, *dgate, *dup, *hidden;
-    unsigned long long ld_gate, ld_hidden;
+    EpilogueArgs e;                   // kEpiStore: the problems have their own outputs
 };
 
 __host__ __device__ constexpr int gemm_stages(int bn) { return bn >= 256 ? 4 : bn >= 128 ? 6 : 8; }
@@ -367,35 +373,35 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) { x[j] = __uint_as_float(r[j]); u[j] = __uint_as_float(r2[j]); }
                     if (live) {
-                        const unsigned long long at = (unsigned long long)row * a.ld_gate + col;
-                        if (a.gate) {
-                            store_row32(a.gate + at, x, cols);
-                            store_row32(a.up + at, u, cols);
+                        const unsigned long long at = (unsigned long long)row * a.e.ld_gate + col;
+                        if (a.e.gate) {
+                            store_row32(a.e.gate + at, x, cols);
+                            store_row32(a.e.up + at, u, cols);
                         }
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) x[j] = activate<false>(x[j], a.activation, nullptr) * u[j];
-                        store_row32(a.hidden + (unsigned long long)row * a.ld_hidden + col, x, cols);
+                        for (int j = 0; j < 32; ++j) x[j] = activate<false>(x[j], a.e.activation, nullptr) * u[j];
+                        store_row32(a.e.hidden + (unsigned long long)row * a.e.ld_hidden + col, x, cols);
                     }
                 } else if (EPI == kEpiBack) {
                     tmem_ld_wait();
                     if (live) {
                         float g[32], u[32];
-                        const unsigned long long at = (unsigned long long)row * a.ld_gate + col;
-                        const unsigned long long to = (unsigned long long)row * a.ld_hidden + col;
-                        load_row32(a.gate + at, g, cols);
-                        load_row32(a.up + at, u, cols);
+                        const unsigned long long at = (unsigned long long)row * a.e.ld_gate + col;
+                        const unsigned long long to = (unsigned long long)row * a.e.ld_hidden + col;
+                        load_row32(a.e.gate + at, g, cols);
+                        load_row32(a.e.up + at, u, cols);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) {
                             const float dh = __uint_as_float(r[j]);
                             float slope;
-                            const float act = activate<true>(g[j], a.activation, &slope);
+                            const float act = activate<true>(g[j], a.e.activation, &slope);
                             x[j] = dh * act;                       // dup
                             g[j] = dh * u[j] * slope;              // dgate
                             u[j] = act * u[j];                     // hidden
                         }
-                        store_row32(a.dup + to, x, cols);
-                        store_row32(a.dgate + to, g, cols);
-                        store_row32(a.hidden + to, u, cols);
+                        store_row32(a.e.dup + to, x, cols);
+                        store_row32(a.e.dgate + to, g, cols);
+                        store_row32(a.e.hidden + to, u, cols);
                     }
                 } else {
                     tmem_ld_wait();
@@ -439,7 +445,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
     tc_fence_after();
     if (warp == 5)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
-    if (threadIdx.x == 0 && abort_flag && a.status) *a.status = DD_STATUS_WAIT_LIMIT;
+    if (threadIdx.x == 0 && abort_flag && a.e.status) *a.e.status = DD_STATUS_WAIT_LIMIT;
 }
 
 }  // namespace ddm

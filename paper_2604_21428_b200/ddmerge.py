@@ -85,21 +85,6 @@ class CGradRecord(ctypes.Structure):
                 ("reserved", ctypes.c_uint32), ("norm_sq", ctypes.c_double)]
 
 
-class CAdamw(ctypes.Structure):
-    """Mirror of ``dd_adamw``."""
-    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
-                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("step", ctypes.c_uint64)]
-
-
-class CGatedFfn(ctypes.Structure):
-    """Mirror of ``dd_gated_ffn``."""
-    _fields_ = [("tokens", ctypes.c_uint64), ("d", ctypes.c_uint64), ("f", ctypes.c_uint64),
-                ("ld_x", ctypes.c_uint64), ("ld_y", ctypes.c_uint64), ("ld_gate", ctypes.c_uint64),
-                ("ld_in", ctypes.c_uint64), ("ld_down", ctypes.c_uint64),
-                ("w_gate", ctypes.c_void_p), ("w_up", ctypes.c_void_p), ("w_down", ctypes.c_void_p),
-                ("activation", ctypes.c_int32), ("reserved", ctypes.c_int32)]
-
-
 RECORD_BYTES = ctypes.sizeof(CRecord)
 GRAD_RECORD_BYTES = ctypes.sizeof(CGradRecord)
 
@@ -198,16 +183,6 @@ def _load() -> ctypes.CDLL:
     lib.dd_status_string.argtypes = [ctypes.c_int]
     lib.dd_last_cuda_error.restype = ctypes.c_char_p
     lib.dd_last_cuda_error.argtypes = [vp]
-    lib.dd_grad_norm.restype = ctypes.c_int
-    lib.dd_grad_norm.argtypes = [vp, vp, vp, ctypes.c_char_p, ctypes.c_int, ctypes.c_float, vp, vp]
-    lib.dd_clip_gradients.restype = ctypes.c_int
-    lib.dd_clip_gradients.argtypes = [vp, vp, vp, vp, ctypes.c_char_p, ctypes.c_int, ctypes.c_float, vp, vp]
-    lib.dd_adamw_step.restype = ctypes.c_int
-    lib.dd_adamw_step.argtypes = [vp, ctypes.POINTER(CAdamw), vp, vp, vp, vp, vp, vp, ctypes.c_char_p, ctypes.c_int, vp, vp]
-    lib.dd_gated_ffn_forward.restype = ctypes.c_int
-    lib.dd_gated_ffn_forward.argtypes = [vp, ctypes.POINTER(CGatedFfn), vp, vp, vp, vp, vp, vp, vp, vp]
-    lib.dd_gated_ffn_backward.restype = ctypes.c_int
-    lib.dd_gated_ffn_backward.argtypes = [vp, ctypes.POINTER(CGatedFfn)] + [vp] * 8 + [ctypes.c_int, ctypes.c_int, vp, vp, vp]
     lib.dd_launch_geometry.restype = ctypes.c_int
     lib.dd_launch_geometry.argtypes = [vp, ctypes.c_int] + [ctypes.POINTER(ctypes.c_int)] * 3
     lib.dd_launch_shape.restype = ctypes.c_int
@@ -586,23 +561,21 @@ class Context:
             _stream_handle(stream)))
 
 
-    # ---- the learner's inner step ------------------------------------------------------------
+    # ---- the learner's inner step (dd_learner.h), marshalled and checked by _ddtorch ----------
 
     def grad_norm(self, grads, max_norm: float, record, *, stream=None) -> None:
         """``dd_grad_norm``: global norm of a list of contiguous float32 / bfloat16 tensors and the
         clip scale for ``max_norm``, written to ``record`` (``new_grad_record``)."""
-        sizes, dtypes = _list_of(grads)
-        self._check(lib.dd_grad_norm(self._h, _addresses(grads), sizes, dtypes, len(grads), max_norm,
-                                     _ptr(record), _stream_handle(stream)))
+        rc = _native().grad_norm(self._h.value, grads, max_norm, record, _raw_stream(stream))
+        if rc != OK:
+            self._check(rc)
 
     def clip_gradients(self, grads, max_norm: float, record, *, out=None, stream=None) -> None:
         """``dd_clip_gradients``: ``grad_norm``, then every tensor times the clip scale, in place or
         into the tensors of ``out``."""
-        sizes, dtypes = _list_of(grads)
-        if out is not None:
-            _like(out, grads, "out")
-        self._check(lib.dd_clip_gradients(self._h, _addresses(grads), None if out is None else _addresses(out),
-                                          sizes, dtypes, len(grads), max_norm, _ptr(record), _stream_handle(stream)))
+        rc = _native().clip_gradients(self._h.value, grads, out, max_norm, record, _raw_stream(stream))
+        if rc != OK:
+            self._check(rc)
 
     def adamw_step(self, params, grads, exp_avg, exp_avg_sq, step: int, lr: float, *, beta1: float = 0.9,
                    beta2: float = 0.95, eps: float = 1e-8, weight_decay: float = 0.0, copies=None, clip=None,
@@ -610,28 +583,20 @@ class Context:
         """``dd_adamw_step`` over lists of tensors: float32 ``params``, ``exp_avg`` and ``exp_avg_sq`` are
         updated in place, ``copies`` (bfloat16) receive the rounded parameters, ``clip`` is the record
         of an earlier ``grad_norm`` on the stream."""
-        import torch
-        sizes, dtypes = _list_of(grads)
-        for name, ts in (("params", params), ("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq)):
-            _like(ts, grads, name, torch.float32)
-        if copies is not None:
-            _like(copies, grads, "copies", torch.bfloat16)
-        opt = CAdamw(lr, beta1, beta2, eps, weight_decay, step)
-        self._check(lib.dd_adamw_step(
-            self._h, ctypes.byref(opt), _addresses(params), _addresses(grads), _addresses(exp_avg),
-            _addresses(exp_avg_sq), None if copies is None else _addresses(copies), sizes, dtypes, len(grads),
-            _ptr(clip), _stream_handle(stream)))
+        rc = _native().adamw_step(self._h.value, params, grads, exp_avg, exp_avg_sq, copies, clip, step, lr, beta1,
+                                  beta2, eps, weight_decay, _raw_stream(stream))
+        if rc != OK:
+            self._check(rc)
 
     def gated_ffn_forward(self, x, w_gate, w_up, w_down, y, *, activation: int = ACT_SILU, residual=None,
                           gate=None, up=None, hidden=None, status=None, stream=None) -> None:
         """``dd_gated_ffn_forward``: y = [residual +] (a(x w_gate^T) * (x w_up^T)) w_down^T.  bfloat16
         matrices with contiguous rows: ``x``, ``residual``, ``y`` [tokens, d], ``w_gate``, ``w_up`` [f, d],
         ``w_down`` [d, f]; ``gate`` and ``up`` [tokens, f] are kept for the backward pass when given."""
-        b = _block(x, w_gate, w_up, w_down, activation)
-        b.ld_y = _same_rows("y, residual", (b.tokens, b.d), y, residual)
-        b.ld_gate = _same_rows("gate, up", (b.tokens, b.f), gate, up)
-        self._check(lib.dd_gated_ffn_forward(self._h, ctypes.byref(b), _ptr(x), _ptr(residual), _ptr(gate), _ptr(up),
-                                             _ptr(hidden), _ptr(y), _ptr(status), _stream_handle(stream)))
+        rc = _native().gated_ffn_forward(self._h.value, x, w_gate, w_up, w_down, y, residual, gate, up, activation,
+                                         hidden, status, _raw_stream(stream))
+        if rc != OK:
+            self._check(rc)
 
     def gated_ffn_backward(self, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up, dw_down, *,
                            activation: int = ACT_SILU, accumulate: bool = False, scratch=None, status=None,
@@ -639,83 +604,43 @@ class Context:
         """``dd_gated_ffn_backward``: gradients of the block for ``dy`` [tokens, d], given the ``gate`` and
         ``up`` that the forward call kept.  ``dw_gate``, ``dw_up``, ``dw_down`` are all bfloat16 or all
         float32 and have the row strides of the weights."""
+        rc = _native().gated_ffn_backward(self._h.value, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up,
+                                          dw_down, activation, accumulate, scratch, status, _raw_stream(stream))
+        if rc != OK:
+            self._check(rc)
+
+
+_native_module = None
+
+
+def _native():
+    """The ``_ddtorch`` extension; imported with the first call that needs torch."""
+    global _native_module
+    if _native_module is None:
+        import torch  # noqa: F401  (its libraries must be loaded first)
+
+        from . import _ddtorch
+        _native_module = _ddtorch
+    return _native_module
+
+
+def _raw_stream(stream) -> int:
+    if stream is None:
         import torch
-        b = _block(x, w_gate, w_up, w_down, activation)
-        b.ld_y = _same_rows("dy", (b.tokens, b.d), dy)
-        b.ld_gate = _same_rows("gate, up", (b.tokens, b.f), gate, up)
-        kind = dw_down.dtype
-        if (_same_rows("x, dx", (b.tokens, b.d), x, dx) != b.ld_x or
-                _same_rows("dw_gate, dw_up", (b.f, b.d), dw_gate, dw_up, dtype=kind) != b.ld_in or
-                _same_rows("dw_down", (b.d, b.f), dw_down, dtype=kind) != b.ld_down):
-            raise ValueError("gradients must have the row strides of what they belong to")
-        self._check(lib.dd_gated_ffn_backward(
-            self._h, ctypes.byref(b), _ptr(x), _ptr(gate), _ptr(up), _ptr(dy), _ptr(dx), _ptr(dw_gate), _ptr(dw_up),
-            _ptr(dw_down), BF16 if kind == torch.bfloat16 else F32, int(accumulate), _ptr(scratch), _ptr(status),
-            _stream_handle(stream)))
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream if isinstance(stream, int) else int(stream.cuda_stream)
 
 
 def new_grad_record(device=None):
-    """Device buffer for one ``dd_grad_record``: a float32 tensor whose first two elements are the norm
-    and the clip scale."""
+    """Device buffer for one ``dd_grad_record``: a float32 tensor of 32 bytes whose first two elements
+    are the norm and the clip scale."""
     import torch
-    return torch.zeros(GRAD_RECORD_BYTES // 4, dtype=torch.float32, device=device or "cuda")
+    return torch.zeros(8, dtype=torch.float32, device=device or "cuda")
 
 
 def read_grad_record(record) -> CGradRecord:
     """Copies the record to the host (synchronises)."""
     return CGradRecord.from_buffer_copy(record.cpu().numpy().tobytes())
-
-
-def _list_of(grads):
-    """Element counts and dtypes of a tensor list as C arrays; refuses tensors that are not plain."""
-    import torch
-    kinds = {torch.float32: F32, torch.bfloat16: BF16}
-    try:
-        dtypes = bytes([kinds[t.dtype] for t in grads])
-    except KeyError as e:
-        raise ValueError(f"gradients must be float32 or bfloat16, not {e.args[0]}") from None
-    if not all([t.is_contiguous() for t in grads]):
-        raise ValueError("gradients must be contiguous")
-    return (ctypes.c_uint64 * len(grads))(*[t.numel() for t in grads]), dtypes
-
-
-def _like(ts, grads, name: str, dtype=None):
-    if len(ts) != len(grads) or not all([t is None and name == "copies" or
-                                         t.numel() == g.numel() and t.dtype == (dtype or g.dtype) and t.is_contiguous()
-                                         for t, g in zip(ts, grads)]):
-        raise ValueError(f"{name} must match the gradients tensor by tensor: contiguous, same size, "
-                         f"{dtype or 'same dtype'}")
-
-
-def _addresses(ts):
-    return (ctypes.c_void_p * len(ts))(*[None if t is None else t.data_ptr() for t in ts])
-
-
-def _same_rows(name: str, shape, *ts, dtype=None) -> int:
-    """Common row stride of the matrices given (None entries are absent; 0 if all are)."""
-    import torch
-    dtype = dtype or torch.bfloat16
-    ld = 0
-    for t in ts:
-        if t is None:
-            continue
-        if t.dim() != 2 or tuple(t.shape) != tuple(shape) or t.dtype != dtype or (t.shape[1] > 1 and t.stride(1) != 1):
-            raise ValueError(f"{name}: want {dtype} of shape {tuple(shape)} with contiguous rows, "
-                             f"got {t.dtype} {tuple(t.shape)} with strides {tuple(t.stride())}")
-        s = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), (t.shape[1] + 7) // 8 * 8)
-        if ld and s != ld:
-            raise ValueError(f"{name}: row strides differ ({ld} and {s})")
-        ld = s
-    return ld
-
-
-def _block(x, w_gate, w_up, w_down, activation: int) -> CGatedFfn:
-    if x.dim() != 2 or w_gate.dim() != 2:
-        raise ValueError("x and the weights are matrices")
-    T, d, f = x.shape[0], x.shape[1], w_gate.shape[0]
-    return CGatedFfn(T, d, f, _same_rows("x", (T, d), x), 0, 0, _same_rows("w_gate, w_up", (f, d), w_gate, w_up),
-                     _same_rows("w_down", (d, f), w_down), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(),
-                     int(activation), 0)
 
 
 def _pack_descs(fragments, M: int):
