@@ -52,13 +52,13 @@ static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m, unsigned box_r
 
 static unsigned blocks_of(unsigned long long n, unsigned b) { return (unsigned)((n + b - 1) / b); }
 
-// Adds a problem of m x n outputs in tiles of 128 x cols; operands are set by the caller.
+// Adds a problem of m x n outputs in tiles of 256 x cols; operands are set by the caller.
 static GemmProblem &add_problem(GemmArgs &a, unsigned long long m, unsigned long long n, int cols)
 {
     GemmProblem &p = a.prob[a.nprob++];
     p.m = (unsigned)m;
     p.n = (unsigned)n;
-    p.tiles_m = blocks_of(m, kBM);
+    p.tiles_m = blocks_of(m, 2 * kBM);
     p.tiles_n = blocks_of(n, cols);
     a.tiles += p.tiles_m * p.tiles_n;
     p.tile_end = a.tiles;
@@ -94,9 +94,18 @@ static int launch_gemm(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
     static bool done[64];
     const int rc = allow_smem(ctx, ffn_gemm_kernel<EPI, BN>, smem, done);
     if (rc != DD_OK) return rc;
-    const unsigned grid = a.tiles < (unsigned)ctx->sm_count ? a.tiles : (unsigned)ctx->sm_count;
-    ffn_gemm_kernel<EPI, BN><<<grid, kGemmThreads, smem, stream>>>(a);
-    DD_CUDA(ctx, cudaGetLastError());
+    const unsigned pairs = (unsigned)ctx->sm_count / 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * (a.tiles < pairs ? a.tiles : pairs));
+    cfg.blockDim = dim3(kGemmThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_gemm_kernel<EPI, BN>, a));
     return DD_OK;
 }
 

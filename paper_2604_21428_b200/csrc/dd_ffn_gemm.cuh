@@ -1,14 +1,18 @@
 // Tensor-core products of the gated feed-forward block: D = sum_s A_s B_s^T over one or two
 // K segments, bf16 operands, float32 accumulators in tensor memory, epilogues of the block.
 //
-// One persistent CTA per SM walks the 128 x BN output tiles of up to four problems.  Warp 4
-// (one lane) has the TMA engine fill a ring of stages of 64 K-elements (128-byte rows, 128-byte
-// swizzle), warp 5 (one lane) issues tcgen05.mma, warps 0-3 turn finished accumulators into
-// results.  Two accumulators alternate, so the epilogue of one tile runs under the products of
-// the next.  Operands are read where they lie in either order -- K contiguous, or M / N contiguous
-// (the descriptor's "major" bit) -- so no product of the backward pass needs a transposed copy.
+// A pair of SMs (a cluster of two CTAs) computes one 256 x BN tile with tcgen05.mma of
+// cta_group::2: each CTA stages 128 rows of A and BN / 2 rows of B and keeps 128 rows of the
+// accumulator, so that every operand byte in shared memory feeds twice the products that it would
+// for one SM.  Persistent pairs walk the tiles of up to four problems.  In each CTA warp 4 (one lane)
+// has the TMA engine fill a ring of stages of 64 K-elements (128-byte rows, 128-byte swizzle);
+// warp 5 of the first CTA (one lane) issues the products for both; warps 0-3 turn finished
+// accumulators into results.  Two accumulators alternate, so the epilogue of one tile runs under
+// the products of the next.  Operands are read where they lie in either order -- K contiguous, or
+// M / N contiguous (the descriptor's "major" bit) -- so no product of the backward pass needs a
+// transposed copy.
 //
-// Every wait is bounded: on giving up a role raises the CTA's abort flag, all roles leave their
+// Every wait is bounded: on giving up a role raises its CTA's abort flag, the roles leave their
 // loops, copies and products in flight are awaited (again bounded), tensor memory is freed and
 // the caller's status word says DD_STATUS_WAIT_LIMIT.
 #pragma once
@@ -23,9 +27,10 @@
 namespace ddm {
 
 constexpr int kGemmThreads = 192;
-constexpr int kBM = 128, kBK = 64;
+constexpr int kBM = 128, kBK = 64;              // rows of one CTA, K elements of a stage
 constexpr int kChunkBytes = 64 * 128;             // one TMA box: 64 rows of 64 bf16
 constexpr int kMaxMaps = 8, kMaxProblems = 4;
+constexpr unsigned kTileGroup = 8;
 
 enum GemmEpilogue { kEpiStore = 0, kEpiGate = 1, kEpiBack = 2 };
 
@@ -59,9 +64,10 @@ struct GemmArgs {
     EpilogueArgs e;                   // kEpiStore: the problems have their own outputs
 };
 
-__host__ __device__ constexpr int gemm_stages(int bn) { return bn >= 256 ? 4 : bn >= 128 ? 6 : 8; }
-__host__ __device__ constexpr size_t gemm_stage_bytes(int bn) { return (size_t)(kBM + bn) * kBK * 2; }
-constexpr size_t gemm_smem_bytes(int bn) { return 1024 + gemm_stages(bn) * gemm_stage_bytes(bn) + 256; }
+// A stage of one CTA: 128 rows of A and half of the tile's BN rows of B.
+__host__ __device__ constexpr unsigned gemm_stage_bytes(int bn) { return (unsigned)(kBM + bn / 2) * kBK * 2; }
+__host__ __device__ constexpr int gemm_stages(int bn) { return (int)(192 * 1024 / gemm_stage_bytes(bn)); }
+__host__ __device__ constexpr unsigned gemm_smem_bytes(int bn) { return 1024 + gemm_stages(bn) * gemm_stage_bytes(bn); }
 
 // ---- tcgen05 ----------------------------------------------------------------------------------
 
@@ -91,9 +97,43 @@ __device__ __forceinline__ void umma_commit(unsigned bar)
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
 }
 
-__device__ __forceinline__ void mbar_arrive(unsigned bar)
+// The same for a pair: products of both SMs, `bar` in every CTA of `mask`.
+__device__ __forceinline__ void umma_commit_pair(unsigned bar, unsigned short mask)
 {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 :: "r"(bar), "h"(mask) : "memory");
+}
+
+__device__ __forceinline__ void umma_bf16_pair(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                 " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// A copy into this CTA that reports to a barrier (a cluster address) of either CTA of the pair.
+__device__ __forceinline__ void tma_load_2d_pair(unsigned dst, const CUtensorMap *map, int x, int y, unsigned bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+// This CTA's shared-memory address as the cluster address of the same place in CTA `rank`.
+__device__ __forceinline__ unsigned cluster_addr(unsigned addr, unsigned rank)
+{
+    unsigned r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+__device__ __forceinline__ void mbar_arrive_cluster(unsigned bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 __device__ __forceinline__ void tmem_ld32(unsigned addr, unsigned (&r)[32])
@@ -207,7 +247,7 @@ struct TilePos {
     unsigned m0, n0;          // first output row and column
 };
 
-// Neighbouring tiles (what the SMs hold at one time) cover a block of 16 tile rows, so that both
+// Neighbouring tiles (what the GPU holds at one time) cover a block of 8 tile rows, so that both
 // operands of a wave stay in L2.
 template <int COLS>
 __device__ __forceinline__ TilePos tile_pos(const GemmArgs &a, unsigned t)
@@ -217,10 +257,10 @@ __device__ __forceinline__ TilePos tile_pos(const GemmArgs &a, unsigned t)
     while (t >= a.prob[r.p].tile_end) ++r.p;
     const GemmProblem &p = a.prob[r.p];
     t -= r.p ? a.prob[r.p - 1].tile_end : 0u;
-    const unsigned group = 16 * p.tiles_n, g = t / group, first = 16 * g;
-    const unsigned rows = p.tiles_m - first < 16 ? p.tiles_m - first : 16;
+    const unsigned group = kTileGroup * p.tiles_n, g = t / group, first = kTileGroup * g;
+    const unsigned rows = p.tiles_m - first < kTileGroup ? p.tiles_m - first : kTileGroup;
     t -= g * group;
-    r.m0 = (first + t % rows) * kBM;
+    r.m0 = (first + t % rows) * 2 * kBM;
     r.n0 = (t / rows) * COLS;
     return r;
 }
@@ -235,25 +275,104 @@ __device__ __forceinline__ bool gemm_wait(unsigned bar, unsigned parity, volatil
     return false;
 }
 
-// BN: accumulator columns of a tile.  kEpiGate puts BN / 2 columns of gate beside BN / 2 of up.
+// Results of 32 columns from `col` on of one output row, from its accumulator columns at `taddr`
+// (kEpiGate: gate there, up BN / 2 columns on).
 template <int EPI, int BN>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+__device__ __forceinline__ void finish_row32(const GemmArgs &a, const GemmProblem &p, unsigned taddr, unsigned row, bool live, unsigned col)
+{
+    const unsigned cols = p.n - col < 32 ? p.n - col : 32;
+    unsigned r[32];
+    tmem_ld32(taddr, r);
+    float x[32];
+    if (EPI == kEpiGate) {
+        unsigned r2[32];
+        tmem_ld32(taddr + BN / 2, r2);
+        tmem_ld_wait();
+        if (!live) return;
+        float u[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) { x[j] = __uint_as_float(r[j]); u[j] = __uint_as_float(r2[j]); }
+        const unsigned long long at = (unsigned long long)row * a.e.ld_gate + col;
+        if (a.e.gate) {
+            store_row32(a.e.gate + at, x, cols);
+            store_row32(a.e.up + at, u, cols);
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = activate<false>(x[j], a.e.activation, nullptr) * u[j];
+        store_row32(a.e.hidden + (unsigned long long)row * a.e.ld_hidden + col, x, cols);
+    } else if (EPI == kEpiBack) {
+        tmem_ld_wait();
+        if (!live) return;
+        float g[32], u[32];
+        const unsigned long long at = (unsigned long long)row * a.e.ld_gate + col;
+        const unsigned long long to = (unsigned long long)row * a.e.ld_hidden + col;
+        load_row32(a.e.gate + at, g, cols);
+        load_row32(a.e.up + at, u, cols);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float dh = __uint_as_float(r[j]);
+            float slope;
+            const float act = activate<true>(g[j], a.e.activation, &slope);
+            x[j] = dh * act;                       // dup
+            g[j] = dh * u[j] * slope;              // dgate
+            u[j] = act * u[j];                     // hidden
+        }
+        store_row32(a.e.dup + to, x, cols);
+        store_row32(a.e.dgate + to, g, cols);
+        store_row32(a.e.hidden + to, u, cols);
+    } else {
+        tmem_ld_wait();
+        if (!live) return;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
+        const unsigned long long at = (unsigned long long)row * p.ld_out + col;
+        float add[32];
+        if (p.residual) {
+            load_row32(p.residual + (unsigned long long)row * p.ld_residual + col, add, cols);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[j] += add[j];
+        }
+        if (p.out_f32) {
+            float *o = static_cast<float *>(p.out) + at;
+            if (p.accumulate) {
+                load_row32_f32(o, add, cols);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) x[j] += add[j];
+            }
+            store_row32_f32(o, x, cols);
+        } else {
+            __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.out) + at;
+            if (p.accumulate) {
+                load_row32(o, add, cols);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) x[j] += add[j];
+            }
+            store_row32(o, x, cols);
+        }
+    }
+}
+
+// BN: accumulator columns of a pair's tile.  kEpiGate puts BN / 2 columns of gate (the first CTA's
+// share of B) beside BN / 2 of up (the second's).
+template <int EPI, int BN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
 {
     constexpr int kStages = gemm_stages(BN);
-    constexpr unsigned kStageBytes = (unsigned)gemm_stage_bytes(BN);
+    constexpr unsigned kStageBytes = gemm_stage_bytes(BN), kABytes = kBM * kBK * 2;
     constexpr int kCols = EPI == kEpiGate ? BN / 2 : BN;      // output columns of a tile
-    constexpr unsigned kTmemCols = 2 * BN < 32 ? 32 : 2 * BN;
-    static_assert((kTmemCols & (kTmemCols - 1)) == 0 && kTmemCols <= 512, "tensor memory is allocated in powers of two");
+    constexpr unsigned kTmemCols = 2 * BN;
+    static_assert(kTmemCols == 512 || kTmemCols == 256, "tensor memory is allocated in powers of two");
 
     extern __shared__ unsigned char smem_raw[];
     const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const unsigned bars = smem + kStages * kStageBytes;
-    const unsigned full = bars, empty = bars + 8 * kStages, tfull = empty + 8 * kStages, tempty = tfull + 16, drain = tempty + 16;
+    __shared__ alignas(8) unsigned long long bars[2 * kStages + 5];
     __shared__ int abort_flag;
     __shared__ unsigned tmem_base;
+    const unsigned full = smem_addr(bars), empty = full + 8 * kStages, tfull = empty + 8 * kStages, tempty = tfull + 16, drain = tempty + 16;
     volatile int *abort = &abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     if (threadIdx.x == 0) {
         abort_flag = 0;
@@ -263,91 +382,91 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
         }
         for (int s = 0; s < 2; ++s) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(tfull + 8 * s) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], 128;" :: "r"(tempty + 8 * s) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 8;" :: "r"(tempty + 8 * s) : "memory");   // epilogue warps of both CTAs
         }
         asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(drain) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 5) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
                      :: "r"(smem_addr(&tmem_base)), "r"(kTmemCols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
+    __syncwarp();
     tc_fence_before();
-    __syncthreads();
+    cluster_sync();
     tc_fence_after();
     const unsigned tmem = tmem_base;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if (warp == 4) {
         if (elect_one()) {
-            unsigned it = 0;              // stages filled so far
+            const unsigned full0 = cluster_addr(full, 0);      // the first CTA's barriers count both CTAs' bytes
+            unsigned it = 0, s = 0, phase = 1;                 // copies so far, stage, parity of its previous use
             bool ok = true;
-            for (unsigned t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
+            for (unsigned t = pair; ok && t < a.tiles; t += pairs) {
                 const TilePos pos = tile_pos<kCols>(a, t);
                 const GemmProblem &p = a.prob[pos.p];
+                const int m0 = (int)(pos.m0 + rank * kBM), n0 = (int)(pos.n0 + (EPI == kEpiGate ? 0 : rank * (BN / 2)));
                 for (int seg = 0; ok && seg < 2; ++seg) {
-                    const CUtensorMap *ma = &a.maps[p.a_map[seg]];
+                    const CUtensorMap *ma = &a.maps[p.a_map[seg]], *mb = &a.maps[p.b_map[EPI == kEpiGate ? rank : seg]];
                     for (unsigned kb = 0; kb < p.kblocks[seg]; ++kb, ++it) {
-                        const unsigned s = it % kStages;
-                        if (it >= kStages && !gemm_wait(empty + 8 * s, (it / kStages - 1) & 1, abort)) { ok = false; break; }
-                        if (*abort) { ok = false; break; }
-                        const unsigned st = smem + s * kStageBytes, bar = full + 8 * s;
-                        mbar_arrive_expect_tx(bar, kStageBytes);
+                        if ((it >= kStages && !gemm_wait(empty + 8 * s, phase, abort)) || *abort) { ok = false; break; }
+                        const unsigned st = smem + s * kStageBytes, bar = full0 + 8 * s;
+                        if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, 2 * kStageBytes);
                         const int k0 = (int)kb * kBK;
 #pragma unroll
-                        for (int c = 0; c < kBM / 64; ++c) {
-                            const int m = (int)pos.m0 + 64 * c;
-                            tma_load_2d(st + c * kChunkBytes, ma, p.a_mn ? m : k0, p.a_mn ? k0 : m, bar);
-                        }
+                        for (int c = 0; c < kBM / 64; ++c)
+                            tma_load_2d_pair(st + c * kChunkBytes, ma, p.a_mn ? m0 + 64 * c : k0, p.a_mn ? k0 : m0 + 64 * c, bar);
 #pragma unroll
-                        for (int c = 0; c < BN / 64; ++c) {
-                            const int half = EPI == kEpiGate && c >= BN / 128;
-                            const CUtensorMap *mb = &a.maps[p.b_map[EPI == kEpiGate ? half : seg]];
-                            const int n = (int)pos.n0 + 64 * (half ? c - BN / 128 : c);
-                            tma_load_2d(st + kBM * kBK * 2 + c * kChunkBytes, mb, p.b_mn ? n : k0, p.b_mn ? k0 : n, bar);
-                        }
+                        for (int c = 0; c < BN / 128; ++c)
+                            tma_load_2d_pair(st + kABytes + c * kChunkBytes, mb, p.b_mn ? n0 + 64 * c : k0, p.b_mn ? k0 : n0 + 64 * c, bar);
+                        if (++s == kStages) { s = 0; phase ^= 1; }
                     }
                 }
             }
-            // no copy may be in flight when the CTA ends, whoever gave up
-            for (unsigned j = it > kStages ? it - kStages : 0; j < it; ++j)
-                mbar_wait_bounded(full + 8 * (j % kStages), (j / kStages) & 1);
+            // no copy of either CTA may be in flight when the pair ends, whoever gave up
+            if (rank == 0)
+                for (unsigned j = it > kStages ? it - kStages : 0; j < it; ++j)
+                    mbar_wait_bounded(full + 8 * (j % kStages), (j / kStages) & 1);
         }
     } else if (warp == 5) {
-        if (elect_one()) {
-            unsigned it = 0, acc = 0;     // stages consumed, tiles started
+        if (rank == 0 && elect_one()) {
+            unsigned acc = 0, s = 0, phase = 0;                // tiles started, stage, its parity
             bool ok = true;
-            for (unsigned t = blockIdx.x; ok && t < a.tiles; t += gridDim.x, ++acc) {
+            for (unsigned t = pair; ok && t < a.tiles; t += pairs, ++acc) {
                 const TilePos pos = tile_pos<kCols>(a, t);
                 const GemmProblem &p = a.prob[pos.p];
                 const unsigned slot = acc & 1;
                 if (acc >= 2 && !gemm_wait(tempty + 8 * slot, (acc / 2 - 1) & 1, abort)) { ok = false; break; }
                 tc_fence_after();
-                // float32 accumulators, bf16 x bf16, the operands' majors, N = BN, M = 128
+                // float32 accumulators, bf16 x bf16, the operands' majors, N = BN, M = 256
                 const unsigned idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((unsigned)p.a_mn << 15) |
-                                       ((unsigned)p.b_mn << 16) | ((unsigned)(BN / 8) << 17) | ((kBM / 16) << 24);
+                                       ((unsigned)p.b_mn << 16) | ((unsigned)(BN / 8) << 17) | ((2 * kBM / 16) << 24);
                 const unsigned astep = p.a_mn ? 2048 : 32, bstep = p.b_mn ? 2048 : 32;     // bytes per 16 K elements
                 const unsigned blocks = p.kblocks[0] + p.kblocks[1];
-                for (unsigned kb = 0; kb < blocks; ++kb, ++it) {
-                    const unsigned s = it % kStages;
-                    if (!gemm_wait(full + 8 * s, (it / kStages) & 1, abort)) { ok = false; break; }
+                for (unsigned kb = 0; kb < blocks; ++kb) {
+                    if (!gemm_wait(full + 8 * s, phase, abort)) { ok = false; break; }
                     tc_fence_after();
-                    const unsigned sa = smem + s * kStageBytes, sb = sa + kBM * kBK * 2;
+                    const unsigned sa = smem + s * kStageBytes, sb = sa + kABytes;
 #pragma unroll
                     for (int k = 0; k < kBK / 16; ++k)
-                        umma_bf16(tmem + slot * BN, umma_desc(sa + k * astep, p.a_mn), umma_desc(sb + k * bstep, p.b_mn),
-                                  idesc, kb | k);
-                    umma_commit(empty + 8 * s);
+                        umma_bf16_pair(tmem + slot * BN, umma_desc(sa + k * astep, p.a_mn), umma_desc(sb + k * bstep, p.b_mn),
+                                       idesc, kb | k);
+                    umma_commit_pair(empty + 8 * s, 3);
+                    if (++s == kStages) { s = 0; phase ^= 1; }
                 }
-                if (ok) umma_commit(tfull + 8 * slot);
+                if (ok) umma_commit_pair(tfull + 8 * slot, 3);
             }
-            umma_commit(drain);           // no product may be in flight when tensor memory is freed
+            umma_commit_pair(drain, 1);   // no product may be in flight when tensor memory is freed
             mbar_wait_bounded(drain, 0);
         }
     } else {
+        const unsigned tempty0 = cluster_addr(tempty, 0);
         unsigned acc = 0;
-        for (unsigned t = blockIdx.x; t < a.tiles; t += gridDim.x, ++acc) {
+        for (unsigned t = pair; t < a.tiles; t += pairs, ++acc) {
             const TilePos pos = tile_pos<kCols>(a, t);
             const GemmProblem &p = a.prob[pos.p];
             const unsigned slot = acc & 1;
@@ -355,96 +474,21 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
             const unsigned taddr = tmem + ((unsigned)(warp * 32) << 16) + slot * BN;
-            const unsigned row = pos.m0 + warp * 32 + lane;
-            const bool live = row < p.m;
+            const unsigned row = pos.m0 + rank * kBM + warp * 32 + lane;
 #pragma unroll 1
-            for (int c = 0; c < kCols; c += 32) {
-                const unsigned col = pos.n0 + c;
-                if (col >= p.n) break;
-                const unsigned cols = p.n - col < 32 ? p.n - col : 32;
-                unsigned r[32];
-                tmem_ld32(taddr + c, r);
-                float x[32];
-                if (EPI == kEpiGate) {
-                    unsigned r2[32];
-                    tmem_ld32(taddr + BN / 2 + c, r2);
-                    tmem_ld_wait();
-                    float u[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) { x[j] = __uint_as_float(r[j]); u[j] = __uint_as_float(r2[j]); }
-                    if (live) {
-                        const unsigned long long at = (unsigned long long)row * a.e.ld_gate + col;
-                        if (a.e.gate) {
-                            store_row32(a.e.gate + at, x, cols);
-                            store_row32(a.e.up + at, u, cols);
-                        }
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) x[j] = activate<false>(x[j], a.e.activation, nullptr) * u[j];
-                        store_row32(a.e.hidden + (unsigned long long)row * a.e.ld_hidden + col, x, cols);
-                    }
-                } else if (EPI == kEpiBack) {
-                    tmem_ld_wait();
-                    if (live) {
-                        float g[32], u[32];
-                        const unsigned long long at = (unsigned long long)row * a.e.ld_gate + col;
-                        const unsigned long long to = (unsigned long long)row * a.e.ld_hidden + col;
-                        load_row32(a.e.gate + at, g, cols);
-                        load_row32(a.e.up + at, u, cols);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float dh = __uint_as_float(r[j]);
-                            float slope;
-                            const float act = activate<true>(g[j], a.e.activation, &slope);
-                            x[j] = dh * act;                       // dup
-                            g[j] = dh * u[j] * slope;              // dgate
-                            u[j] = act * u[j];                     // hidden
-                        }
-                        store_row32(a.e.dup + to, x, cols);
-                        store_row32(a.e.dgate + to, g, cols);
-                        store_row32(a.e.hidden + to, u, cols);
-                    }
-                } else {
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
-                    if (live) {
-                        const unsigned long long at = (unsigned long long)row * p.ld_out + col;
-                        float add[32];
-                        if (p.residual) {
-                            load_row32(p.residual + (unsigned long long)row * p.ld_residual + col, add, cols);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) x[j] += add[j];
-                        }
-                        if (p.out_f32) {
-                            float *o = static_cast<float *>(p.out) + at;
-                            if (p.accumulate) {
-                                load_row32_f32(o, add, cols);
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) x[j] += add[j];
-                            }
-                            store_row32_f32(o, x, cols);
-                        } else {
-                            __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.out) + at;
-                            if (p.accumulate) {
-                                load_row32(o, add, cols);
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) x[j] += add[j];
-                            }
-                            store_row32(o, x, cols);
-                        }
-                    }
-                }
-            }
+            for (int c = 0; c < kCols && pos.n0 + c < p.n; c += 32)
+                finish_row32<EPI, BN>(a, p, taddr + c, row, row < p.m, pos.n0 + c);
             tc_fence_before();
-            mbar_arrive(tempty + 8 * slot);
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * slot);
         }
     }
     __syncwarp();
     tc_fence_before();
-    __syncthreads();
+    cluster_sync();                       // both CTAs are done with each other's shared and tensor memory
     tc_fence_after();
     if (warp == 5)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
     if (threadIdx.x == 0 && abort_flag && a.e.status) *a.e.status = DD_STATUS_WAIT_LIMIT;
 }
 

@@ -29,11 +29,6 @@ __host__ __device__ constexpr unsigned stream_ring_bytes(int n, int stages)
 }
 __host__ __device__ constexpr unsigned stream_smem_bytes(int n, int stages) { return 1024 + stream_ring_bytes(n, stages) + 256; }
 
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 // Four floats at `addr` (a shared-memory address of this CTA) in the CTA of rank `rank`.
 __device__ __forceinline__ float4 ld_cluster4(unsigned addr, unsigned rank)
 {

@@ -15,7 +15,10 @@ namespace ddm {
 constexpr int kListThreads = 256;
 constexpr int kListTile = 8192;              // elements: 32 per thread
 constexpr int kListSmall = 32, kListMax = 256;
+// Measured at 4 / 8 CTAs of 256 threads per SM: norm of 1.2e9 bf16 375 / 342 us (7.07 TB/s), clip of 151M bf16
+// 156 / 150 us, AdamW on 151M with bf16 gradients and copies 698 / 673 us (6.29 TB/s).
 constexpr int kListCtasPerSm = 8;
+constexpr unsigned char kNoVector = 255;
 
 // One launch's tensors, by value in the kernel parameters: no staging copy, and nothing for a
 // stream capture to keep alive.  CAP = 32 keeps the parameters of short lists under 2 KB.
@@ -25,8 +28,9 @@ struct ListArgs {
     unsigned long long n[CAP];
     unsigned tile_end[CAP];                  // one past the tensor's last flat tile
     unsigned char bf16[CAP];                 // type of the gradient
-    unsigned char vec[CAP];                  // every pointer is aligned for 16-byte (8-byte bf16) pieces
+    unsigned char head[CAP];                 // elements before the first 16-byte boundary; kNoVector: pointers disagree
     unsigned tiles;
+    int count;
 };
 
 struct NormTail {
@@ -42,16 +46,6 @@ struct AdamwConsts {
     float beta1, rest1, beta2, rest2, eps, decay, step_size, inv_c2;
     const dd_grad_record *clip;
 };
-
-// Moves `i` to the tensor that holds flat tile `tile` (tiles are visited in ascending order) and
-// returns the tile's first element within it.
-template <typename A>
-__device__ __forceinline__ unsigned long long seek(const A &a, unsigned tile, int &i)
-{
-    while (tile >= a.tile_end[i]) ++i;
-    const unsigned begin = i ? a.tile_end[i - 1] : 0u;
-    return (unsigned long long)(tile - begin) * kListTile;
-}
 
 __device__ __forceinline__ float lo_bf16(unsigned w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_bf16(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
@@ -79,9 +73,84 @@ __device__ __forceinline__ double block_sum(double x, double *sm)
     return t;
 }
 
-// sum of g^2: fp32 over the 32 elements a thread takes of a tile, fp64 across tiles, threads and
-// CTAs.  The CTA that draws the last ticket adds the partials in index order, so the result does
-// not depend on which one that is.
+// The tensor that holds flat tile `tile`, between the candidates lo and hi (a scan of the table,
+// some 40 cycles a step, took longer than the tiles themselves in lists of 200 tensors).
+template <typename A>
+__device__ __forceinline__ int find_tensor(const A &a, unsigned tile, int lo, int hi)
+{
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (tile < a.tile_end[mid]) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
+// Programmatic launch: the next launch on the stream may be set up under this one, and waits here
+// before it touches memory.
+__device__ __forceinline__ void after_prior_launch()
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// A tile's span within its tensor: vector pieces from `begin` (a boundary of all the tensor's
+// pointers) to `end`; the tensor's first tile also has the `head` elements before.
+struct Span {
+    unsigned long long begin, end;
+    unsigned head;
+    bool vec;
+};
+
+template <typename A>
+__device__ __forceinline__ Span span_of(const A &a, unsigned tile, int i)
+{
+    const unsigned first = i ? a.tile_end[i - 1] : 0u;
+    const unsigned char h = a.head[i];
+    Span s;
+    s.vec = h != kNoVector;
+    const unsigned head = s.vec ? h : 0u;
+    s.begin = head + (unsigned long long)(tile - first) * kListTile;
+    s.end = s.begin + kListTile < a.n[i] ? s.begin + kListTile : a.n[i];
+    s.head = tile == first ? head : 0u;
+    return s;
+}
+
+__device__ __forceinline__ float squares(const uint4 &w)
+{
+    const unsigned x[4] = {w.x, w.y, w.z, w.w};
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        s = fmaf(lo_bf16(x[j]), lo_bf16(x[j]), s);
+        s = fmaf(hi_bf16(x[j]), hi_bf16(x[j]), s);
+    }
+    return s;
+}
+
+__device__ __forceinline__ float squares(const float4 &w) { return fmaf(w.x, w.x, fmaf(w.y, w.y, fmaf(w.z, w.z, w.w * w.w))); }
+
+// Sum of squares of this thread's part of a tile: V holds E elements.
+template <typename V, int E>
+__device__ __forceinline__ float tile_squares(const V *p, unsigned pieces)
+{
+    constexpr int kSteps = kListTile / (E * kListThreads);
+    float s = 0.0f;
+    V w[kSteps];
+    if (pieces == kSteps * kListThreads) {
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) w[k] = p[threadIdx.x + k * kListThreads];
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) s += squares(w[k]);
+    } else {
+        for (unsigned k = threadIdx.x; k < pieces; k += kListThreads) s += squares(p[k]);
+    }
+    return s;
+}
+
+// sum of g^2: fp32 over the 32 elements a thread takes of a tile (and 8 more at a tensor's ends),
+// fp64 across tiles, threads and CTAs.  The CTA that draws the last ticket adds the partials in
+// index order, so the result does not depend on which one that is.
 template <int CAP>
 __global__ void __launch_bounds__(kListThreads)
 grad_norm_kernel(const __grid_constant__ ListArgs<1, CAP> a, const __grid_constant__ NormTail t)
@@ -90,41 +159,23 @@ grad_norm_kernel(const __grid_constant__ ListArgs<1, CAP> a, const __grid_consta
     __shared__ unsigned drawn;
     double acc = 0.0;
     int i = 0;
+    after_prior_launch();
     for (unsigned tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const unsigned long long base = seek(a, tile, i);
+        i = find_tensor(a, tile, i, a.count - 1);
+        const Span sp = span_of(a, tile, i);
         const void *g = a.ptr[0][i];
-        const unsigned long long left = a.n[i] - base;
+        const bool bf16 = a.bf16[i];
+        const unsigned cnt = (unsigned)(sp.end - sp.begin), per = bf16 ? 8 : 4, pieces = sp.vec ? cnt / per : 0;
         float s = 0.0f;
-        if (a.vec[i] && left >= kListTile) {
-            if (a.bf16[i]) {
-                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const unsigned short *>(g) + base) + threadIdx.x;
-                uint4 w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = __ldg(p + k * kListThreads);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const unsigned x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        s = fmaf(lo_bf16(x[j]), lo_bf16(x[j]), s);
-                        s = fmaf(hi_bf16(x[j]), hi_bf16(x[j]), s);
-                    }
-                }
-            } else {
-                const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(g) + base) + threadIdx.x;
-                float4 w[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = __ldg(p + k * kListThreads);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) s = fmaf(w[k].x, w[k].x, fmaf(w[k].y, w[k].y, fmaf(w[k].z, w[k].z, fmaf(w[k].w, w[k].w, s))));
-            }
-        } else {
-            const unsigned m = left < kListTile ? (unsigned)left : kListTile;
-#pragma unroll 8
-            for (unsigned e = threadIdx.x; e < m; e += kListThreads) {
-                const float x = load_elem(g, a.bf16[i], base + e);
-                s = fmaf(x, x, s);
-            }
+        if (bf16) s = tile_squares<uint4, 8>(reinterpret_cast<const uint4 *>(static_cast<const unsigned short *>(g) + sp.begin), pieces);
+        else s = tile_squares<float4, 4>(reinterpret_cast<const float4 *>(static_cast<const float *>(g) + sp.begin), pieces);
+        for (unsigned e = pieces * per + threadIdx.x; e < cnt; e += kListThreads) {
+            const float x = load_elem(g, bf16, sp.begin + e);
+            s = fmaf(x, x, s);
+        }
+        if (threadIdx.x < sp.head) {
+            const float x = load_elem(g, bf16, threadIdx.x);
+            s = fmaf(x, x, s);
         }
         acc += (double)s;
     }
@@ -152,49 +203,57 @@ grad_norm_kernel(const __grid_constant__ ListArgs<1, CAP> a, const __grid_consta
     }
 }
 
+__device__ __forceinline__ uint4 scaled(const uint4 &w, float c)
+{
+    return make_uint4(pack_bf16(c * lo_bf16(w.x), c * hi_bf16(w.x)), pack_bf16(c * lo_bf16(w.y), c * hi_bf16(w.y)),
+                      pack_bf16(c * lo_bf16(w.z), c * hi_bf16(w.z)), pack_bf16(c * lo_bf16(w.w), c * hi_bf16(w.w)));
+}
+
+__device__ __forceinline__ float4 scaled(const float4 &w, float c) { return make_float4(c * w.x, c * w.y, c * w.z, c * w.w); }
+
+template <typename V, int E>
+__device__ __forceinline__ void tile_scale(const V *p, V *q, unsigned pieces, float c)
+{
+    constexpr int kSteps = kListTile / (E * kListThreads);
+    V w[kSteps];
+    if (pieces == kSteps * kListThreads) {
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) w[k] = p[threadIdx.x + k * kListThreads];
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) q[threadIdx.x + k * kListThreads] = scaled(w[k], c);
+    } else {
+        for (unsigned k = threadIdx.x; k < pieces; k += kListThreads) q[k] = scaled(p[k], c);
+    }
+}
+
+// out = scale * g, last tiles first: what the norm read last is what L2 still holds.
 template <int CAP>
 __global__ void __launch_bounds__(kListThreads)
 grad_scale_kernel(const __grid_constant__ ListArgs<2, CAP> a, const dd_grad_record *record, int in_place)
 {
+    after_prior_launch();
     const float scale = record->scale;
     if (record->status != DD_STATUS_OK || (in_place && scale == 1.0f)) return;
-    int i = 0;
-    for (unsigned tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const unsigned long long base = seek(a, tile, i);
+    int i = a.count - 1;
+    for (unsigned step = blockIdx.x; step < a.tiles; step += gridDim.x) {
+        const unsigned tile = a.tiles - 1 - step;
+        i = find_tensor(a, tile, 0, i);
+        const Span sp = span_of(a, tile, i);
         const void *g = a.ptr[0][i];
         void *o = a.ptr[1][i];
-        const unsigned long long left = a.n[i] - base;
-        if (a.vec[i] && left >= kListTile) {
-            if (a.bf16[i]) {
-                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const unsigned short *>(g) + base) + threadIdx.x;
-                uint4 *q = reinterpret_cast<uint4 *>(static_cast<unsigned short *>(o) + base) + threadIdx.x;
-                uint4 w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = p[k * kListThreads];
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    q[k * kListThreads] = make_uint4(pack_bf16(scale * lo_bf16(w[k].x), scale * hi_bf16(w[k].x)),
-                                                     pack_bf16(scale * lo_bf16(w[k].y), scale * hi_bf16(w[k].y)),
-                                                     pack_bf16(scale * lo_bf16(w[k].z), scale * hi_bf16(w[k].z)),
-                                                     pack_bf16(scale * lo_bf16(w[k].w), scale * hi_bf16(w[k].w)));
-            } else {
-                const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(g) + base) + threadIdx.x;
-                float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(o) + base) + threadIdx.x;
-                float4 w[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = p[k * kListThreads];
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    q[k * kListThreads] = make_float4(scale * w[k].x, scale * w[k].y, scale * w[k].z, scale * w[k].w);
-            }
-        } else {
-            const unsigned m = left < kListTile ? (unsigned)left : kListTile;
-            for (unsigned e = threadIdx.x; e < m; e += kListThreads) {
-                const float x = scale * load_elem(g, a.bf16[i], base + e);
-                if (a.bf16[i]) static_cast<unsigned short *>(o)[base + e] = round_bf16(x);
-                else static_cast<float *>(o)[base + e] = x;
-            }
-        }
+        const bool bf16 = a.bf16[i];
+        const unsigned cnt = (unsigned)(sp.end - sp.begin), per = bf16 ? 8 : 4, pieces = sp.vec ? cnt / per : 0;
+        if (bf16) tile_scale<uint4, 8>(reinterpret_cast<const uint4 *>(static_cast<const unsigned short *>(g) + sp.begin),
+                                       reinterpret_cast<uint4 *>(static_cast<unsigned short *>(o) + sp.begin), pieces, scale);
+        else tile_scale<float4, 4>(reinterpret_cast<const float4 *>(static_cast<const float *>(g) + sp.begin),
+                                   reinterpret_cast<float4 *>(static_cast<float *>(o) + sp.begin), pieces, scale);
+        const auto one = [&](unsigned long long e) {
+            const float x = scale * load_elem(g, bf16, e);
+            if (bf16) static_cast<unsigned short *>(o)[e] = round_bf16(x);
+            else static_cast<float *>(o)[e] = x;
+        };
+        for (unsigned e = pieces * per + threadIdx.x; e < cnt; e += kListThreads) one(sp.begin + e);
+        if (threadIdx.x < sp.head) one(threadIdx.x);
     }
 }
 
@@ -210,32 +269,33 @@ template <int CAP>
 __global__ void __launch_bounds__(kListThreads)
 adamw_kernel(const __grid_constant__ ListArgs<5, CAP> a, const __grid_constant__ AdamwConsts c)
 {
+    after_prior_launch();
     float scale = 1.0f;
     if (c.clip) {
         if (c.clip->status != DD_STATUS_OK) return;
         scale = c.clip->scale;
     }
-    int i = 0;
-    for (unsigned tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const unsigned long long base = seek(a, tile, i);
-        float *p = static_cast<float *>(a.ptr[0][i]) + base;
-        float *m = static_cast<float *>(a.ptr[1][i]) + base;
-        float *v = static_cast<float *>(a.ptr[2][i]) + base;
+    const auto grad4 = [&](const void *g, bool bf16, unsigned long long e) {
+        if (!bf16) return *reinterpret_cast<const float4 *>(static_cast<const float *>(g) + e);
+        const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const unsigned short *>(g) + e);
+        return make_float4(lo_bf16(w.x), hi_bf16(w.x), lo_bf16(w.y), hi_bf16(w.y));
+    };
+    int i = a.count - 1;
+    for (unsigned step = blockIdx.x; step < a.tiles; step += gridDim.x) {
+        const unsigned tile = a.tiles - 1 - step;
+        i = find_tensor(a, tile, 0, i);
+        const Span sp = span_of(a, tile, i);
+        float *p = static_cast<float *>(a.ptr[0][i]), *m = static_cast<float *>(a.ptr[1][i]), *v = static_cast<float *>(a.ptr[2][i]);
+        const void *g = a.ptr[3][i];
         unsigned short *o = static_cast<unsigned short *>(a.ptr[4][i]);
-        const unsigned long long left = a.n[i] - base;
         const bool bf16 = a.bf16[i];
-        const unsigned cnt = left < kListTile ? (unsigned)left : kListTile;
-        const unsigned vec_end = a.vec[i] ? cnt & ~3u : 0u;
+        const unsigned cnt = (unsigned)(sp.end - sp.begin), vec = sp.vec ? cnt & ~3u : 0u;
 #pragma unroll 2
-        for (unsigned e = 4 * threadIdx.x; e < vec_end; e += 4 * kListThreads) {
+        for (unsigned k = 4 * threadIdx.x; k < vec; k += 4 * kListThreads) {
+            const unsigned long long e = sp.begin + k;
             float4 P = *reinterpret_cast<const float4 *>(p + e), M = *reinterpret_cast<const float4 *>(m + e),
-                   V = *reinterpret_cast<const float4 *>(v + e), G;
-            if (bf16) {
-                const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const unsigned short *>(a.ptr[3][i]) + base + e);
-                G = make_float4(lo_bf16(w.x), hi_bf16(w.x), lo_bf16(w.y), hi_bf16(w.y));
-            } else {
-                G = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.ptr[3][i]) + base + e);
-            }
+                   V = *reinterpret_cast<const float4 *>(v + e);
+            const float4 G = grad4(g, bf16, e);
             adamw_elem(P.x, M.x, V.x, scale * G.x, c);
             adamw_elem(P.y, M.y, V.y, scale * G.y, c);
             adamw_elem(P.z, M.z, V.z, scale * G.z, c);
@@ -243,16 +303,18 @@ adamw_kernel(const __grid_constant__ ListArgs<5, CAP> a, const __grid_constant__
             *reinterpret_cast<float4 *>(p + e) = P;
             *reinterpret_cast<float4 *>(m + e) = M;
             *reinterpret_cast<float4 *>(v + e) = V;
-            if (o) *reinterpret_cast<uint2 *>(o + base + e) = make_uint2(pack_bf16(P.x, P.y), pack_bf16(P.z, P.w));
+            if (o) *reinterpret_cast<uint2 *>(o + e) = make_uint2(pack_bf16(P.x, P.y), pack_bf16(P.z, P.w));
         }
-        for (unsigned e = vec_end + threadIdx.x; e < cnt; e += kListThreads) {
+        const auto one = [&](unsigned long long e) {
             float P = p[e], M = m[e], V = v[e];
-            adamw_elem(P, M, V, scale * load_elem(a.ptr[3][i], bf16, base + e), c);
+            adamw_elem(P, M, V, scale * load_elem(g, bf16, e), c);
             p[e] = P;
             m[e] = M;
             v[e] = V;
-            if (o) o[base + e] = round_bf16(P);
-        }
+            if (o) o[e] = round_bf16(P);
+        };
+        for (unsigned k = vec + threadIdx.x; k < cnt; k += kListThreads) one(sp.begin + k);
+        if (threadIdx.x < sp.head) one(threadIdx.x);
     }
 }
 
@@ -296,14 +358,23 @@ static int fill_list(ListArgs<NPTR, CAP> &a, const uint64_t *sizes, const uint8_
     for (; at < count && k < CAP; ++at) {
         if (sizes[at] == 0) continue;
         void *p[NPTR];
-        a.vec[k] = pointers(at, p);
+        const unsigned head = pointers(at, p);
         for (int j = 0; j < NPTR; ++j) a.ptr[j][k] = p[j];
         a.n[k] = sizes[at];
         a.bf16[k] = dtypes[at] == DD_BF16;
-        a.tiles += (unsigned)((sizes[at] + kListTile - 1) / kListTile);
+        a.head[k] = (unsigned char)(head != kNoVector && head > sizes[at] ? sizes[at] : head);
+        const uint64_t body = sizes[at] - (head == kNoVector ? 0 : a.head[k]);
+        a.tiles += body ? (unsigned)((body + kListTile - 1) / kListTile) : 1;
         a.tile_end[k++] = a.tiles;
     }
+    a.count = k;
     return at;
+}
+
+// Elements from p to the next boundary of `elems` elements of `size` bytes.
+static unsigned head_of(const void *p, unsigned size, unsigned elems)
+{
+    return (unsigned)((elems - (uintptr_t)p / size % elems) % elems);
 }
 
 static unsigned list_grid(const dd_ctx *ctx, unsigned tiles)
@@ -312,12 +383,28 @@ static unsigned list_grid(const dd_ctx *ctx, unsigned tiles)
     return tiles < 1 ? 1 : tiles < most ? tiles : most;
 }
 
+template <typename... P, typename... Q>
+static int launch_list(dd_ctx *ctx, void (*kernel)(P...), unsigned grid, cudaStream_t stream, const Q &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kListThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, args...));
+    return DD_OK;
+}
+
 template <int CAP>
 static int launch_norm(dd_ctx *ctx, const void *const *grads, const uint64_t *sizes, const uint8_t *dtypes,
                        int count, float max_norm, dd_grad_record *record, cudaStream_t stream)
 {
     const size_t launches = count > CAP ? (size_t)(count + CAP - 1) / CAP : 1;
-    const int rc = ensure_workspace(ctx, 1, 1, launches * ctx->sm_count * kListCtasPerSm);
+    int rc = ensure_workspace(ctx, 1, 1, launches * ctx->sm_count * kListCtasPerSm);
     if (rc != DD_OK) return rc;
     NormTail t;
     t.partials = ctx->partials;
@@ -330,13 +417,14 @@ static int launch_norm(dd_ctx *ctx, const void *const *grads, const uint64_t *si
         ListArgs<1, CAP> a;
         at = fill_list(a, sizes, dtypes, count, at, [&](int i, void **p) {
             p[0] = const_cast<void *>(grads[i]);
-            return ((uintptr_t)p[0] & 15u) == 0;
+            const unsigned eb = dtypes[i] == DD_BF16 ? 2 : 4;
+            return head_of(p[0], eb, 16 / eb);
         });
         const unsigned grid = list_grid(ctx, a.tiles);
         t.last = at >= count;
         t.total = t.first + grid;
-        grad_norm_kernel<CAP><<<grid, kListThreads, 0, stream>>>(a, t);
-        DD_CUDA(ctx, cudaGetLastError());
+        rc = launch_list(ctx, grad_norm_kernel<CAP>, grid, stream, a, t);
+        if (rc != DD_OK) return rc;
         t.first += grid;
     } while (at < count);
     return DD_OK;
@@ -351,11 +439,13 @@ static int launch_scale(dd_ctx *ctx, void *const *grads, void *const *outs, cons
         at = fill_list(a, sizes, dtypes, count, at, [&](int i, void **p) {
             p[0] = grads[i];
             p[1] = outs ? outs[i] : grads[i];
-            return (((uintptr_t)p[0] | (uintptr_t)p[1]) & 15u) == 0;
+            const unsigned eb = dtypes[i] == DD_BF16 ? 2 : 4, h = head_of(p[0], eb, 16 / eb);
+            return h == head_of(p[1], eb, 16 / eb) ? h : (unsigned)kNoVector;
         });
         if (!a.tiles) continue;
-        grad_scale_kernel<CAP><<<list_grid(ctx, a.tiles), kListThreads, 0, stream>>>(a, record, outs == nullptr);
-        DD_CUDA(ctx, cudaGetLastError());
+        const int rc = launch_list(ctx, grad_scale_kernel<CAP>, list_grid(ctx, a.tiles), stream, a, record,
+                                   (int)(outs == nullptr));
+        if (rc != DD_OK) return rc;
     }
     return DD_OK;
 }
@@ -373,13 +463,14 @@ static int launch_adamw(dd_ctx *ctx, const AdamwConsts &c, float *const *params,
             p[2] = v[i];
             p[3] = const_cast<void *>(grads[i]);
             p[4] = copies ? copies[i] : nullptr;
-            const uintptr_t wide = (uintptr_t)p[0] | (uintptr_t)p[1] | (uintptr_t)p[2];
-            const unsigned gmask = dtypes[i] == DD_BF16 ? 7u : 15u;
-            return (wide & 15u) == 0 && ((uintptr_t)p[3] & gmask) == 0 && ((uintptr_t)p[4] & 7u) == 0;
+            const unsigned h = head_of(p[0], 4, 4);
+            const bool same = h == head_of(p[1], 4, 4) && h == head_of(p[2], 4, 4) && h == head_of(p[3], dtypes[i] == DD_BF16 ? 2 : 4, 4) &&
+                              (!p[4] || h == head_of(p[4], 2, 4));
+            return same ? h : (unsigned)kNoVector;
         });
         if (!a.tiles) continue;
-        adamw_kernel<CAP><<<list_grid(ctx, a.tiles), kListThreads, 0, stream>>>(a, c);
-        DD_CUDA(ctx, cudaGetLastError());
+        const int rc = launch_list(ctx, adamw_kernel<CAP>, list_grid(ctx, a.tiles), stream, a, c);
+        if (rc != DD_OK) return rc;
     }
     return DD_OK;
 }
