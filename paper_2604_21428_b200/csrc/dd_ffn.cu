@@ -36,13 +36,14 @@ struct Matrix {
     unsigned long long rows, cols, ld;      // bf16 elements
 };
 
-static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m, unsigned box_rows = 64)
+// Boxes of 64 columns (128-byte rows) for operands, of 32 (64-byte rows) for the epilogues.
+static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m, unsigned box_rows = 64, unsigned box_cols = 64)
 {
     const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * 2};
-    const cuuint32_t box[2] = {64, box_rows}, step[2] = {1, 1};
+    const cuuint32_t box[2] = {box_cols, box_rows}, step[2] = {1, 1};
     const EncodeTiled fn = tensor_map_encoder();
     if (!fn || fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(m.data), dims, strides, box, step,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
         snprintf(ctx->cuda_err, sizeof ctx->cuda_err, "cuTensorMapEncodeTiled failed");
         return DD_ERR_CUDA;
@@ -90,14 +91,14 @@ static int allow_smem(dd_ctx *ctx, K kernel, size_t bytes, bool (&done)[64])
 template <int EPI, int BN>
 static int launch_gemm(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
 {
-    constexpr size_t smem = gemm_smem_bytes(BN);
+    constexpr size_t smem = gemm_smem_bytes(EPI, BN);
     static bool done[64];
     const int rc = allow_smem(ctx, ffn_gemm_kernel<EPI, BN>, smem, done);
     if (rc != DD_OK) return rc;
     const unsigned pairs = (unsigned)ctx->sm_count / 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (a.tiles < pairs ? a.tiles : pairs));
-    cfg.blockDim = dim3(kGemmThreads);
+    cfg.blockDim = dim3(gemm_threads(EPI));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute at;
@@ -122,7 +123,7 @@ static int launch_stream_n(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
     a.stages = (int)(stages > kStreamMaxStages ? kStreamMaxStages : stages);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(tiles * s);
-    cfg.blockDim = dim3(kGemmThreads);
+    cfg.blockDim = dim3(kStreamThreads);
     cfg.dynamicSmemBytes = stream_smem_bytes(N, a.stages);
     cfg.stream = stream;
     static bool done[64];
@@ -302,6 +303,9 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
     rc = encode(ctx, &a.maps[0], mx);
     if (rc == DD_OK) rc = encode(ctx, &a.maps[1], mg);
     if (rc == DD_OK) rc = encode(ctx, &a.maps[2], mu);
+    if (rc == DD_OK) rc = encode(ctx, &a.maps[kOutHidden], mh, 32, 32);
+    if (rc == DD_OK && gate) rc = encode(ctx, &a.maps[kOutGate], {gate, T, b.f, b.ld_gate}, 32, 32);
+    if (rc == DD_OK && gate) rc = encode(ctx, &a.maps[kOutUp], {up, T, b.f, b.ld_gate}, 32, 32);
     if (rc != DD_OK) return rc;
     GemmProblem &p = add_problem(a, T, b.f, 128);
     p.kblocks[0] = blocks_of(b.d, kBK);
@@ -407,16 +411,21 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         if (rc == DD_OK) rc = launch_stream<kEpiStore>(ctx, c, stream);
         if (rc != DD_OK) return rc;
     } else {
-        GemmProblem &p = add_problem(a, T, b.f, 256);
-        p.kblocks[0] = blocks_of(b.d, kBK);
-        p.a_map[0] = kDy;
-        p.b_map[0] = kWd;
-        p.b_mn = 1;
-        rc = launch_gemm<kEpiBack, 256>(ctx, a, stream);
+        GemmArgs c = a;
+        c.maps[0] = a.maps[kDy];
+        c.maps[1] = a.maps[kWd];
+        rc = encode(ctx, &c.maps[kBackGate], {gate, T, b.f, b.ld_gate}, 32, 32);
+        if (rc == DD_OK) rc = encode(ctx, &c.maps[kBackUp], {up, T, b.f, b.ld_gate}, 32, 32);
+        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutHidden], mats[kH], 32, 32);
+        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutGate], mats[kDg], 32, 32);
+        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutUp], mats[kDu], 32, 32);
         if (rc != DD_OK) return rc;
-        std::memset(a.prob, 0, sizeof a.prob);
-        a.nprob = 0;
-        a.tiles = 0;
+        GemmProblem &p = add_problem(c, T, b.f, 256);
+        p.kblocks[0] = blocks_of(b.d, kBK);
+        p.b_map[0] = 1;
+        p.b_mn = 1;
+        rc = launch_gemm<kEpiBack, 256>(ctx, c, stream);
+        if (rc != DD_OK) return rc;
         GemmProblem &qx = add_problem(a, T, b.d, 256);
         qx.kblocks[0] = qx.kblocks[1] = blocks_of(b.f, kBK);
         qx.a_map[0] = kDg;

@@ -26,11 +26,11 @@
 
 namespace ddm {
 
-constexpr int kGemmThreads = 192;
 constexpr int kBM = 128, kBK = 64;              // rows of one CTA, K elements of a stage
 constexpr int kChunkBytes = 64 * 128;             // one TMA box: 64 rows of 64 bf16
 constexpr int kMaxMaps = 8, kMaxProblems = 4;
 constexpr unsigned kTileGroup = 8;
+constexpr int kBoxBytes = 32 * 64;                // an epilogue box: 32 rows of 32 bf16
 
 enum GemmEpilogue { kEpiStore = 0, kEpiGate = 1, kEpiBack = 2 };
 
@@ -56,18 +56,27 @@ struct GemmProblem {
     unsigned long long ld_out, ld_residual;
 };
 
+// Tensor maps of the epilogues' boxes (32 x 32): results, and what kEpiBack reads.
+enum { kOutHidden = 3, kOutGate = 4, kOutUp = 5, kBackGate = 6, kBackUp = 7 };
+
 struct GemmArgs {
-    CUtensorMap maps[kMaxMaps];       // 64 x 64 boxes of row-major bf16 matrices
+    CUtensorMap maps[kMaxMaps];       // operands: 64 x 64 boxes of row-major bf16 matrices
     GemmProblem prob[kMaxProblems];
     int nprob;
     unsigned tiles;
     EpilogueArgs e;                   // kEpiStore: the problems have their own outputs
 };
 
+// Epilogue warps: eight where a row's results cost an activation, four where they are only stored.
+__host__ __device__ constexpr int gemm_epi_warps(int epi) { return epi == kEpiStore ? 4 : 8; }
+__host__ __device__ constexpr int gemm_threads(int epi) { return 32 * gemm_epi_warps(epi) + 64; }
+// Boxes a warp of the epilogue stages: kEpiGate 3 out, kEpiBack 2 in and 3 out.
+__host__ __device__ constexpr int gemm_boxes(int epi) { return epi == kEpiStore ? 0 : epi == kEpiGate ? 3 : 5; }
+__host__ __device__ constexpr unsigned gemm_epi_bytes(int epi) { return gemm_epi_warps(epi) * gemm_boxes(epi) * kBoxBytes; }
 // A stage of one CTA: 128 rows of A and half of the tile's BN rows of B.
 __host__ __device__ constexpr unsigned gemm_stage_bytes(int bn) { return (unsigned)(kBM + bn / 2) * kBK * 2; }
-__host__ __device__ constexpr int gemm_stages(int bn) { return (int)(192 * 1024 / gemm_stage_bytes(bn)); }
-__host__ __device__ constexpr unsigned gemm_smem_bytes(int bn) { return 1024 + gemm_stages(bn) * gemm_stage_bytes(bn); }
+__host__ __device__ constexpr int gemm_stages(int epi, int bn) { return (int)((224 * 1024 - gemm_epi_bytes(epi)) / gemm_stage_bytes(bn)); }
+__host__ __device__ constexpr unsigned gemm_smem_bytes(int epi, int bn) { return 1024 + gemm_stages(epi, bn) * gemm_stage_bytes(bn) + gemm_epi_bytes(epi); }
 
 // ---- tcgen05 ----------------------------------------------------------------------------------
 
@@ -117,6 +126,17 @@ __device__ __forceinline__ void tma_load_2d_pair(unsigned dst, const CUtensorMap
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, int x, int y, unsigned src)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
+                 :: "l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+}
+
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// Shared memory of this thread's stores so far may be written again / their results are in memory.
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // This CTA's shared-memory address as the cluster address of the same place in CTA `rank`.
 __device__ __forceinline__ unsigned cluster_addr(unsigned addr, unsigned rank)
@@ -275,90 +295,89 @@ __device__ __forceinline__ bool gemm_wait(unsigned bar, unsigned parity, volatil
     return false;
 }
 
-// Results of 32 columns from `col` on of one output row, from its accumulator columns at `taddr`
-// (kEpiGate: gate there, up BN / 2 columns on).
-template <int EPI, int BN>
-__device__ __forceinline__ void finish_row32(const GemmArgs &a, const GemmProblem &p, unsigned taddr, unsigned row, bool live, unsigned col)
+// kEpiStore: results of 32 columns from `col` on of one output row, from its accumulator columns at `taddr`.
+__device__ __forceinline__ void store_columns(const GemmProblem &p, unsigned taddr, unsigned row, unsigned col)
 {
     const unsigned cols = p.n - col < 32 ? p.n - col : 32;
     unsigned r[32];
     tmem_ld32(taddr, r);
+    tmem_ld_wait();
+    if (row >= p.m) return;
     float x[32];
-    if (EPI == kEpiGate) {
-        unsigned r2[32];
-        tmem_ld32(taddr + BN / 2, r2);
-        tmem_ld_wait();
-        if (!live) return;
-        float u[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) { x[j] = __uint_as_float(r[j]); u[j] = __uint_as_float(r2[j]); }
-        const unsigned long long at = (unsigned long long)row * a.e.ld_gate + col;
-        if (a.e.gate) {
-            store_row32(a.e.gate + at, x, cols);
-            store_row32(a.e.up + at, u, cols);
-        }
+    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
+    const unsigned long long at = (unsigned long long)row * p.ld_out + col;
+    float add[32];
+    if (p.residual) {
+        load_row32(p.residual + (unsigned long long)row * p.ld_residual + col, add, cols);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) x[j] = activate<false>(x[j], a.e.activation, nullptr) * u[j];
-        store_row32(a.e.hidden + (unsigned long long)row * a.e.ld_hidden + col, x, cols);
-    } else if (EPI == kEpiBack) {
-        tmem_ld_wait();
-        if (!live) return;
-        float g[32], u[32];
-        const unsigned long long at = (unsigned long long)row * a.e.ld_gate + col;
-        const unsigned long long to = (unsigned long long)row * a.e.ld_hidden + col;
-        load_row32(a.e.gate + at, g, cols);
-        load_row32(a.e.up + at, u, cols);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const float dh = __uint_as_float(r[j]);
-            float slope;
-            const float act = activate<true>(g[j], a.e.activation, &slope);
-            x[j] = dh * act;                       // dup
-            g[j] = dh * u[j] * slope;              // dgate
-            u[j] = act * u[j];                     // hidden
-        }
-        store_row32(a.e.dup + to, x, cols);
-        store_row32(a.e.dgate + to, g, cols);
-        store_row32(a.e.hidden + to, u, cols);
-    } else {
-        tmem_ld_wait();
-        if (!live) return;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
-        const unsigned long long at = (unsigned long long)row * p.ld_out + col;
-        float add[32];
-        if (p.residual) {
-            load_row32(p.residual + (unsigned long long)row * p.ld_residual + col, add, cols);
+        for (int j = 0; j < 32; ++j) x[j] += add[j];
+    }
+    if (p.out_f32) {
+        float *o = static_cast<float *>(p.out) + at;
+        if (p.accumulate) {
+            load_row32_f32(o, add, cols);
 #pragma unroll
             for (int j = 0; j < 32; ++j) x[j] += add[j];
         }
-        if (p.out_f32) {
-            float *o = static_cast<float *>(p.out) + at;
-            if (p.accumulate) {
-                load_row32_f32(o, add, cols);
+        store_row32_f32(o, x, cols);
+    } else {
+        __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.out) + at;
+        if (p.accumulate) {
+            load_row32(o, add, cols);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) x[j] += add[j];
-            }
-            store_row32_f32(o, x, cols);
-        } else {
-            __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.out) + at;
-            if (p.accumulate) {
-                load_row32(o, add, cols);
+            for (int j = 0; j < 32; ++j) x[j] += add[j];
+        }
+        store_row32(o, x, cols);
+    }
+}
+
+// A lane's row of a staged box (64-byte rows, 64-byte swizzle: the 16-byte piece j of row r lies at
+// piece j ^ (r / 2 mod 4), so that eight lanes at one piece touch all banks).
+__device__ __forceinline__ unsigned box_piece(unsigned box, int lane, int j) { return box + lane * 64 + ((j ^ (lane >> 1 & 3)) << 4); }
+
+__device__ __forceinline__ void write_box(unsigned box, int lane, const float (&x)[32])
+{
 #pragma unroll
-                for (int j = 0; j < 32; ++j) x[j] += add[j];
-            }
-            store_row32(o, x, cols);
+    for (int j = 0; j < 4; ++j)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                     :: "r"(box_piece(box, lane, j)), "r"(pack2(x[8 * j], x[8 * j + 1])), "r"(pack2(x[8 * j + 2], x[8 * j + 3])),
+                        "r"(pack2(x[8 * j + 4], x[8 * j + 5])), "r"(pack2(x[8 * j + 6], x[8 * j + 7])) : "memory");
+}
+
+__device__ __forceinline__ void read_box(unsigned box, int lane, float (&x)[32])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        unsigned w[4];
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(box_piece(box, lane, j)) : "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[8 * j + 2 * i] = __uint_as_float(w[i] << 16);
+            x[8 * j + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
     }
+}
+
+// Chunks of 32 columns of a tile that an epilogue warp finishes: `half` of the tile's columns, as far
+// as the output goes; none if the warp's rows are past its end.
+template <int COLS>
+__device__ __forceinline__ unsigned chunks_of(const GemmProblem &p, const TilePos &pos, unsigned row0, unsigned half)
+{
+    const unsigned col = pos.n0 + half * (COLS / 2);
+    if (pos.m0 + row0 >= p.m || col >= p.n) return 0;
+    const unsigned c = (p.n - col + 31) / 32;
+    return c < COLS / 64 ? c : COLS / 64;
 }
 
 // BN: accumulator columns of a pair's tile.  kEpiGate puts BN / 2 columns of gate (the first CTA's
 // share of B) beside BN / 2 of up (the second's).
 template <int EPI, int BN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gemm_threads(EPI), 1)
 ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
 {
-    constexpr int kStages = gemm_stages(BN);
+    constexpr int kStages = gemm_stages(EPI, BN), kEpiWarps = gemm_epi_warps(EPI), kProducer = kEpiWarps, kIssuer = kEpiWarps + 1;
     constexpr unsigned kStageBytes = gemm_stage_bytes(BN), kABytes = kBM * kBK * 2;
     constexpr int kCols = EPI == kEpiGate ? BN / 2 : BN;      // output columns of a tile
     constexpr unsigned kTmemCols = 2 * BN;
@@ -366,10 +385,11 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
 
     extern __shared__ unsigned char smem_raw[];
     const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    __shared__ alignas(8) unsigned long long bars[2 * kStages + 5];
+    __shared__ alignas(8) unsigned long long bars[2 * kStages + 5 + kEpiWarps];
     __shared__ int abort_flag;
     __shared__ unsigned tmem_base;
-    const unsigned full = smem_addr(bars), empty = full + 8 * kStages, tfull = empty + 8 * kStages, tempty = tfull + 16, drain = tempty + 16;
+    const unsigned full = smem_addr(bars), empty = full + 8 * kStages, tfull = empty + 8 * kStages, tempty = tfull + 16, drain = tempty + 16,
+                   boxes_in = drain + 8;
     volatile int *abort = &abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
@@ -382,13 +402,14 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
         }
         for (int s = 0; s < 2; ++s) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(tfull + 8 * s) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], 8;" :: "r"(tempty + 8 * s) : "memory");   // epilogue warps of both CTAs
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(tempty + 8 * s), "r"(2 * kEpiWarps) : "memory");   // both CTAs' warps
         }
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(drain) : "memory");
+        for (int s = 0; s < 1 + kEpiWarps; ++s)        // drain, boxes_in
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(drain + 8 * s) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == 5) {
+    if (warp == kIssuer) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
                      :: "r"(smem_addr(&tmem_base)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -401,7 +422,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    if (warp == 4) {
+    if (warp == kProducer) {
         if (elect_one()) {
             const unsigned full0 = cluster_addr(full, 0);      // the first CTA's barriers count both CTAs' bytes
             unsigned it = 0, s = 0, phase = 1;                 // copies so far, stage, parity of its previous use
@@ -432,7 +453,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                 for (unsigned j = it > kStages ? it - kStages : 0; j < it; ++j)
                     mbar_wait_bounded(full + 8 * (j % kStages), (j / kStages) & 1);
         }
-    } else if (warp == 5) {
+    } else if (warp == kIssuer) {
         if (rank == 0 && elect_one()) {
             unsigned acc = 0, s = 0, phase = 0;                // tiles started, stage, its parity
             bool ok = true;
@@ -465,29 +486,116 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
         }
     } else {
         const unsigned tempty0 = cluster_addr(tempty, 0);
+        const unsigned row0 = rank * kBM + (warp & 3) * 32, half = warp >> 2;
+        // kEpiGate, kEpiBack: this warp's boxes; kEpiBack reads gate and up one chunk ahead
+        const unsigned box = smem + kStages * kStageBytes + warp * gemm_boxes(EPI) * kBoxBytes, out = box + (EPI == kEpiBack ? 2 * kBoxBytes : 0);
+        const unsigned landed = boxes_in + 8 * warp;
+        unsigned phase = 0, loads = 0;
+        const auto load_chunk = [&](const TilePos &pos, unsigned c) {
+            if (lane == 0) {
+                const int x = (int)(pos.n0 + half * (kCols / 2) + 32 * c), y = (int)(pos.m0 + row0);
+                mbar_arrive_expect_tx(landed, 2 * kBoxBytes);
+                tma_load_2d(box, &a.maps[kBackGate], x, y, landed);
+                tma_load_2d(box + kBoxBytes, &a.maps[kBackUp], x, y, landed);
+            }
+            ++loads;
+        };
+        const auto load_first_from = [&](unsigned t) {         // the first chunk of the next tile that has one
+            for (; t < a.tiles; t += pairs) {
+                const TilePos pos = tile_pos<kCols>(a, t);
+                if (chunks_of<kCols>(a.prob[pos.p], pos, row0, half)) {
+                    load_chunk(pos, 0);
+                    return;
+                }
+            }
+        };
+        if (EPI == kEpiBack) load_first_from(pair);
         unsigned acc = 0;
-        for (unsigned t = pair; t < a.tiles; t += pairs, ++acc) {
+        bool ok = true;
+        for (unsigned t = pair; ok && t < a.tiles; t += pairs, ++acc) {
             const TilePos pos = tile_pos<kCols>(a, t);
             const GemmProblem &p = a.prob[pos.p];
             const unsigned slot = acc & 1;
-            const bool ok = gemm_wait(tfull + 8 * slot, (acc / 2) & 1, abort);
-            if (!__all_sync(0xffffffffu, ok)) break;
+            ok = __all_sync(0xffffffffu, gemm_wait(tfull + 8 * slot, (acc / 2) & 1, abort));
+            if (!ok) break;
             tc_fence_after();
-            const unsigned taddr = tmem + ((unsigned)(warp * 32) << 16) + slot * BN;
-            const unsigned row = pos.m0 + rank * kBM + warp * 32 + lane;
+            const unsigned taddr = tmem + ((unsigned)((warp & 3) * 32) << 16) + slot * BN;
+            if (EPI == kEpiStore) {
 #pragma unroll 1
-            for (int c = 0; c < kCols && pos.n0 + c < p.n; c += 32)
-                finish_row32<EPI, BN>(a, p, taddr + c, row, row < p.m, pos.n0 + c);
+                for (int c = 0; c < kCols && pos.n0 + c < p.n; c += 32)
+                    store_columns(p, taddr + c, pos.m0 + row0 + lane, pos.n0 + c);
+            } else {
+                const unsigned chunks = chunks_of<kCols>(p, pos, row0, half);
+#pragma unroll 1
+                for (unsigned c = 0; c < chunks; ++c) {
+                    const unsigned col = half * (kCols / 2) + 32 * c;
+                    unsigned r[32];
+                    float x[32], g[32], u[32];
+                    tmem_ld32(taddr + col, r);
+                    if (EPI == kEpiGate) {
+                        unsigned r2[32];
+                        tmem_ld32(taddr + BN / 2 + col, r2);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            g[j] = __uint_as_float(r[j]);
+                            u[j] = __uint_as_float(r2[j]);
+                            x[j] = activate<false>(g[j], a.e.activation, nullptr) * u[j];        // hidden
+                        }
+                    } else {
+                        ok = __all_sync(0xffffffffu, gemm_wait(landed, phase, abort));
+                        if (!ok) break;
+                        phase ^= 1;
+                        read_box(box, lane, g);
+                        read_box(box + kBoxBytes, lane, u);
+                        __syncwarp();
+                        if (c + 1 < chunks) load_chunk(pos, c + 1);
+                        else load_first_from(t + pairs);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float dh = __uint_as_float(r[j]);
+                            float slope;
+                            const float act = activate<true>(g[j], a.e.activation, &slope);
+                            x[j] = act * u[j];                     // hidden
+                            g[j] = dh * u[j] * slope;              // dgate
+                            u[j] = dh * act;                       // dup
+                        }
+                    }
+                    if (lane == 0) bulk_wait_read();               // the boxes of the chunk before
+                    __syncwarp();
+                    const bool all = EPI == kEpiBack || a.e.gate;
+                    write_box(out, lane, x);
+                    if (all) {
+                        write_box(out + kBoxBytes, lane, g);
+                        write_box(out + 2 * kBoxBytes, lane, u);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        const int cx = (int)(pos.n0 + col), cy = (int)(pos.m0 + row0);
+                        tma_store_2d(&a.maps[kOutHidden], cx, cy, out);
+                        if (all) {
+                            tma_store_2d(&a.maps[kOutGate], cx, cy, out + kBoxBytes);
+                            tma_store_2d(&a.maps[kOutUp], cx, cy, out + 2 * kBoxBytes);
+                        }
+                        bulk_commit();
+                    }
+                }
+                if (!ok) break;
+            }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * slot);
         }
+        if (EPI != kEpiStore && lane == 0) bulk_wait();
+        if (EPI == kEpiBack && !ok && loads) mbar_wait_bounded(landed, (loads - 1) & 1);     // a copy may be in flight
     }
     __syncwarp();
     tc_fence_before();
     cluster_sync();                       // both CTAs are done with each other's shared and tensor memory
     tc_fence_after();
-    if (warp == 5)
+    if (warp == kIssuer)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
     if (threadIdx.x == 0 && abort_flag && a.e.status) *a.e.status = DD_STATUS_WAIT_LIMIT;
 }

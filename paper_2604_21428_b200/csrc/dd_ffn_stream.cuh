@@ -16,6 +16,7 @@
 namespace ddm {
 
 constexpr int kRound = 64;                        // tokens reduced per round
+constexpr int kStreamThreads = 192;
 constexpr int kStreamMaxStages = 8, kStreamMaxCluster = 8;
 
 __host__ __device__ constexpr int stream_features(int epi) { return epi == kEpiGate ? kBM / 2 : kBM; }
@@ -127,7 +128,7 @@ struct StreamArgs {
 
 // blockIdx.x = tile * cluster + rank.
 template <int EPI, int N>
-__global__ void __launch_bounds__(kGemmThreads, 2)
+__global__ void __launch_bounds__(kStreamThreads, 2)
 ffn_stream_kernel(const __grid_constant__ StreamArgs p)
 {
     constexpr unsigned kStageBytes = stream_stage_bytes(N), kABytes = kBM * kBK * 2;
