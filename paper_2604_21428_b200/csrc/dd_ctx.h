@@ -42,6 +42,7 @@ struct dd_ctx {
     int gram_grid[2] = {0, 0};                // [bf16] persistent grid of the Gram launch
     void *ffn_scratch = nullptr;              // intermediates of the gated feed-forward block
     size_t ffn_scratch_cap = 0;               // bytes
+    float *ffn_slabs = nullptr;               // float32 partial products of split tiles
     ddm::HostPipe *pipe = nullptr;
     char cuda_err[256] = {0};
 };

@@ -33,17 +33,22 @@ static EncodeTiled tensor_map_encoder()
 
 struct Matrix {
     const void *data;
-    unsigned long long rows, cols, ld;      // bf16 elements
+    unsigned long long rows, cols, ld;      // elements
 };
 
-// Boxes of 64 columns (128-byte rows) for operands, of 32 (64-byte rows) for the epilogues.
-static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m, unsigned box_rows = 64, unsigned box_cols = 64)
+// How a matrix is copied: 64 x rows boxes for operands; 32 x 32 boxes for the epilogues, of bf16
+// (64-byte rows) or float32.
+enum class Box { kOperand, kBf16, kF32 };
+
+static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m, Box kind = Box::kOperand, unsigned rows = 64)
 {
-    const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * 2};
-    const cuuint32_t box[2] = {box_cols, box_rows}, step[2] = {1, 1};
+    const unsigned eb = kind == Box::kF32 ? 4 : 2;
+    const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * eb};
+    const cuuint32_t box[2] = {kind == Box::kOperand ? 64u : 32u, kind == Box::kOperand ? rows : 32u}, step[2] = {1, 1};
     const EncodeTiled fn = tensor_map_encoder();
-    if (!fn || fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(m.data), dims, strides, box, step,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    if (!fn || fn(map, eb == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(m.data),
+                  dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  kind == Box::kBf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
         snprintf(ctx->cuda_err, sizeof ctx->cuda_err, "cuTensorMapEncodeTiled failed");
         return DD_ERR_CUDA;
@@ -53,23 +58,43 @@ static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m, unsigned box_r
 
 static unsigned blocks_of(unsigned long long n, unsigned b) { return (unsigned)((n + b - 1) / b); }
 
-// Adds a problem of m x n outputs in tiles of 256 x cols; operands are set by the caller.
-static GemmProblem &add_problem(GemmArgs &a, unsigned long long m, unsigned long long n, int cols)
+// Adds a problem of m x n outputs in tiles of 256 x cols with its K blocks; the rest is set by the caller.
+static GemmProblem &add_problem(GemmArgs &a, unsigned long long m, unsigned long long n, int cols, unsigned k1, unsigned k2 = 0,
+                                unsigned splits = 1)
 {
     GemmProblem &p = a.prob[a.nprob++];
+    std::memset(&p, 0, sizeof p);
     p.m = (unsigned)m;
     p.n = (unsigned)n;
     p.tiles_m = blocks_of(m, 2 * kBM);
     p.tiles_n = blocks_of(n, cols);
-    a.tiles += p.tiles_m * p.tiles_n;
+    p.kblocks[0] = k1;
+    p.kblocks[1] = k2;
+    p.splits = splits;
+    p.split_rows = p.tiles_m * 2 * kBM;
+    a.tiles += p.tiles_m * p.tiles_n * splits;
     p.tile_end = a.tiles;
     return p;
+}
+
+// Float32 slabs of split products: 256 KB for each of two tiles per pair of SMs.
+static size_t slab_bytes(const dd_ctx *ctx) { return (size_t)ctx->sm_count * (2 * kBM) * 256 * 4; }
+
+// Splits of a problem of `tiles` tiles with `blocks` K blocks each, so that a unit is no longer than
+// half of what each pair has to do when it shares the launch with `other` K blocks of other tiles.
+static unsigned choose_splits(const dd_ctx *ctx, unsigned tiles, unsigned blocks, unsigned long long other)
+{
+    const unsigned pairs = (unsigned)ctx->sm_count / 2;
+    const unsigned long long share = ((unsigned long long)tiles * blocks + other) / pairs + 1;
+    unsigned s = 1;
+    while (s < kMaxSplits && blocks / s > (other ? share / 2 : share) && tiles * (s + 1) <= 2 * pairs && blocks >= 4 * (s + 1)) ++s;
+    return s;
 }
 
 // ---- few tokens ----------------------------------------------------------------------------
 
 // Up to here the weight-streaming kernel is ahead of the 128 x 256 tiles.
-constexpr unsigned long long kStreamMaxTokens = 256;
+constexpr unsigned long long kStreamMaxTokens = 128;
 
 // Ring of a CTA: two CTAs share an SM.
 constexpr unsigned kStreamRing = 96 * 1024;
@@ -98,7 +123,7 @@ static int launch_gemm(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
     const unsigned pairs = (unsigned)ctx->sm_count / 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (a.tiles < pairs ? a.tiles : pairs));
-    cfg.blockDim = dim3(gemm_threads(EPI));
+    cfg.blockDim = dim3(kGemmThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute at;
@@ -107,6 +132,43 @@ static int launch_gemm(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
     cfg.attrs = &at;
     cfg.numAttrs = 1;
     DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_gemm_kernel<EPI, BN>, a));
+    return DD_OK;
+}
+
+// Output of problem `p` through tensor map `map`: the matrix itself, or its splits' slabs.
+static int set_output(dd_ctx *ctx, GemmArgs &a, GemmProblem &p, int map, const Matrix &out, const void *residual, uint64_t ld_residual)
+{
+    p.out_map = (unsigned char)map;
+    if (p.splits > 1) {
+        p.out_f32 = 1;
+        const uint64_t ld = (out.cols + 7) / 8 * 8;
+        return encode(ctx, &a.maps[map], {ctx->ffn_slabs, (uint64_t)p.splits * p.split_rows, out.cols, ld}, Box::kF32);
+    }
+    p.out = const_cast<void *>(out.data);
+    p.ld_out = out.ld;
+    p.ragged = out.cols % 8 != 0;
+    p.residual = (const __nv_bfloat16 *)residual;
+    p.ld_residual = ld_residual;
+    return encode(ctx, &a.maps[map], out, Box::kBf16);
+}
+
+static int launch_reduce(dd_ctx *ctx, const GemmProblem &p, const Matrix &out, const void *residual, uint64_t ld_residual, cudaStream_t stream)
+{
+    const unsigned ld = (unsigned)((out.cols + 7) / 8 * 8);
+    const unsigned long long pieces = (unsigned long long)p.m * (ld / 8), most = (unsigned long long)ctx->sm_count * 8;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((pieces + 255) / 256 < most ? (pieces + 255) / 256 : most));
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_reduce_kernel, (const float *)ctx->ffn_slabs, p.splits,
+                                    (unsigned long long)p.split_rows * ld, ld, p.m, p.n, (const __nv_bfloat16 *)residual,
+                                    (unsigned long long)ld_residual, (__nv_bfloat16 *)const_cast<void *>(out.data),
+                                    (unsigned long long)out.ld));
     return DD_OK;
 }
 
@@ -159,6 +221,14 @@ static StreamArgs stream_args(const EpilogueArgs &e, uint64_t features, uint64_t
     a.n = (unsigned)tokens;
     a.e = e;
     return a;
+}
+
+// The slabs, with the first call of either direction: no later call allocates them.
+static int ensure_ffn_slabs(dd_ctx *ctx)
+{
+    if (ctx->ffn_slabs) return DD_OK;
+    DD_CUDA(ctx, cudaMalloc(&ctx->ffn_slabs, slab_bytes(ctx)));
+    return DD_OK;
 }
 
 // Context-owned scratch for callers that bring none.
@@ -262,6 +332,8 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
     if (T == 0) return DD_OK;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return cuda_fail(ctx, cudaErrorInvalidDevice, "cudaSetDevice");
+    rc = ensure_ffn_slabs(ctx);
+    if (rc != DD_OK) return rc;
     if (!hidden) {
         rc = ensure_ffn_scratch(ctx, (size_t)(T * ldh) * 2);
         if (rc != DD_OK) return rc;
@@ -287,14 +359,14 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
         a.kblocks[0] = blocks_of(b.d, kBK);
         rc = encode(ctx, &a.w[0], mg);
         if (rc == DD_OK) rc = encode(ctx, &a.w[1], mu);
-        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mx, stream_box(T));
+        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mx, Box::kOperand, stream_box(T));
         if (rc == DD_OK) rc = launch_stream<kEpiGate>(ctx, a, stream);
         if (rc != DD_OK) return rc;
         a.m = (unsigned)b.d;
         a.kblocks[0] = blocks_of(b.f, kBK);
         a.own_prior = 1;
         rc = encode(ctx, &a.w[0], md);
-        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mh, stream_box(T));
+        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mh, Box::kOperand, stream_box(T));
         return rc == DD_OK ? launch_stream<kEpiStore>(ctx, a, stream) : rc;
     }
     GemmArgs a;
@@ -303,31 +375,27 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
     rc = encode(ctx, &a.maps[0], mx);
     if (rc == DD_OK) rc = encode(ctx, &a.maps[1], mg);
     if (rc == DD_OK) rc = encode(ctx, &a.maps[2], mu);
-    if (rc == DD_OK) rc = encode(ctx, &a.maps[kOutHidden], mh, 32, 32);
-    if (rc == DD_OK && gate) rc = encode(ctx, &a.maps[kOutGate], {gate, T, b.f, b.ld_gate}, 32, 32);
-    if (rc == DD_OK && gate) rc = encode(ctx, &a.maps[kOutUp], {up, T, b.f, b.ld_gate}, 32, 32);
+    if (rc == DD_OK) rc = encode(ctx, &a.maps[kOutHidden], mh, Box::kBf16);
+    if (rc == DD_OK && gate) rc = encode(ctx, &a.maps[kOutGate], {gate, T, b.f, b.ld_gate}, Box::kBf16);
+    if (rc == DD_OK && gate) rc = encode(ctx, &a.maps[kOutUp], {up, T, b.f, b.ld_gate}, Box::kBf16);
     if (rc != DD_OK) return rc;
-    GemmProblem &p = add_problem(a, T, b.f, 128);
-    p.kblocks[0] = blocks_of(b.d, kBK);
+    GemmProblem &p = add_problem(a, T, b.f, 128, blocks_of(b.d, kBK));
     p.b_map[0] = 1;
     p.b_map[1] = 2;
     rc = launch_gemm<kEpiGate, 256>(ctx, a, stream);
     if (rc != DD_OK) return rc;
 
-    std::memset(a.prob, 0, sizeof a.prob);
     a.nprob = 0;
     a.tiles = 0;
+    const unsigned kf = blocks_of(b.f, kBK);
+    const unsigned splits = choose_splits(ctx, blocks_of(T, 2 * kBM) * blocks_of(b.d, 256), kf, 0);
+    GemmProblem &q = add_problem(a, T, b.d, 256, kf, 0, splits);
+    q.b_map[0] = 1;
     rc = encode(ctx, &a.maps[0], mh);
     if (rc == DD_OK) rc = encode(ctx, &a.maps[1], md);
-    if (rc != DD_OK) return rc;
-    GemmProblem &q = add_problem(a, T, b.d, 256);
-    q.kblocks[0] = blocks_of(b.f, kBK);
-    q.b_map[0] = 1;
-    q.out = y;
-    q.ld_out = b.ld_y;
-    q.residual = (const __nv_bfloat16 *)residual;
-    q.ld_residual = b.ld_y;
-    return launch_gemm<kEpiStore, 256>(ctx, a, stream);
+    if (rc == DD_OK) rc = set_output(ctx, a, q, 2, {y, T, b.d, b.ld_y}, residual, b.ld_y);
+    if (rc == DD_OK) rc = launch_gemm<kEpiStore, 256>(ctx, a, stream);
+    return rc == DD_OK && splits > 1 ? launch_reduce(ctx, q, {y, T, b.d, b.ld_y}, residual, b.ld_y, stream) : rc;
 }
 
 extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, const void *x, const void *gate,
@@ -363,6 +431,8 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         DD_CUDA(ctx, cudaMemset2DAsync(dw_down, b.ld_down * ge, 0, b.f * ge, b.d, stream));
         return DD_OK;
     }
+    rc = ensure_ffn_slabs(ctx);
+    if (rc != DD_OK) return rc;
     if (!scratch) {
         rc = ensure_ffn_scratch(ctx, (size_t)(3 * T * ldh) * 2);
         if (rc != DD_OK) return rc;
@@ -370,13 +440,13 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
     }
     enum { kX, kDy, kWg, kWu, kWd, kDg, kDu, kH };
     __nv_bfloat16 *dg = (__nv_bfloat16 *)scratch, *du = dg + T * ldh, *h = du + T * ldh;
-    const Matrix mats[kMaxMaps] = {{x, T, b.d, b.ld_x}, {dy, T, b.d, b.ld_y}, {b.w_gate, b.f, b.d, b.ld_in},
+    const Matrix mats[kH + 1] = {{x, T, b.d, b.ld_x}, {dy, T, b.d, b.ld_y}, {b.w_gate, b.f, b.d, b.ld_in},
                                    {b.w_up, b.f, b.d, b.ld_in}, {b.w_down, b.d, b.f, b.ld_down},
                                    {dg, T, b.f, ldh}, {du, T, b.f, ldh}, {h, T, b.f, ldh}};
     GemmArgs a;
     std::memset(&a, 0, sizeof a);
     const bool few = T <= kStreamMaxTokens;
-    for (int i = 0; i < kMaxMaps; ++i) {
+    for (int i = 0; i <= kH; ++i) {
         rc = encode(ctx, &a.maps[i], mats[i]);
         if (rc != DD_OK) return rc;
     }
@@ -398,7 +468,7 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         c.kblocks[0] = blocks_of(b.d, kBK);
         c.w[0] = a.maps[kWd];
         c.w_mn = 1;
-        rc = encode(ctx, &c.x[0], mats[kDy], stream_box(T));
+        rc = encode(ctx, &c.x[0], mats[kDy], Box::kOperand, stream_box(T));
         if (rc == DD_OK) rc = launch_stream<kEpiBack>(ctx, c, stream);
         if (rc != DD_OK) return rc;
         c.m = (unsigned)b.d;                              // dgate w_gate + dup w_up
@@ -406,41 +476,46 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         c.w[0] = a.maps[kWg];
         c.w[1] = a.maps[kWu];
         c.own_prior = 1;
-        rc = encode(ctx, &c.x[0], mats[kDg], stream_box(T));
-        if (rc == DD_OK) rc = encode(ctx, &c.x[1], mats[kDu], stream_box(T));
+        rc = encode(ctx, &c.x[0], mats[kDg], Box::kOperand, stream_box(T));
+        if (rc == DD_OK) rc = encode(ctx, &c.x[1], mats[kDu], Box::kOperand, stream_box(T));
         if (rc == DD_OK) rc = launch_stream<kEpiStore>(ctx, c, stream);
         if (rc != DD_OK) return rc;
     } else {
         GemmArgs c = a;
         c.maps[0] = a.maps[kDy];
         c.maps[1] = a.maps[kWd];
-        rc = encode(ctx, &c.maps[kBackGate], {gate, T, b.f, b.ld_gate}, 32, 32);
-        if (rc == DD_OK) rc = encode(ctx, &c.maps[kBackUp], {up, T, b.f, b.ld_gate}, 32, 32);
-        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutHidden], mats[kH], 32, 32);
-        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutGate], mats[kDg], 32, 32);
-        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutUp], mats[kDu], 32, 32);
+        rc = encode(ctx, &c.maps[kBackGate], {gate, T, b.f, b.ld_gate}, Box::kBf16);
+        if (rc == DD_OK) rc = encode(ctx, &c.maps[kBackUp], {up, T, b.f, b.ld_gate}, Box::kBf16);
+        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutHidden], mats[kH], Box::kBf16);
+        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutGate], mats[kDg], Box::kBf16);
+        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutUp], mats[kDu], Box::kBf16);
         if (rc != DD_OK) return rc;
-        GemmProblem &p = add_problem(c, T, b.f, 256);
-        p.kblocks[0] = blocks_of(b.d, kBK);
+        GemmProblem &p = add_problem(c, T, b.f, 256, blocks_of(b.d, kBK));
         p.b_map[0] = 1;
         p.b_mn = 1;
         rc = launch_gemm<kEpiBack, 256>(ctx, c, stream);
         if (rc != DD_OK) return rc;
-        GemmProblem &qx = add_problem(a, T, b.d, 256);
-        qx.kblocks[0] = qx.kblocks[1] = blocks_of(b.f, kBK);
-        qx.a_map[0] = kDg;
-        qx.a_map[1] = kDu;
-        qx.b_map[0] = kWg;
-        qx.b_map[1] = kWu;
-        qx.b_mn = 1;
-        qx.out = dx;
-        qx.ld_out = b.ld_x;
+    }
+    const unsigned kt = blocks_of(T, kBK), kf = blocks_of(b.f, kBK);
+    unsigned splits = 1;
+    GemmProblem *dxp = nullptr;
+    if (!few) {                                           // dgate w_gate + dup w_up
+        const unsigned long long weights = 3ull * kt * blocks_of(b.f, 2 * kBM) * blocks_of(b.d, 256);
+        splits = choose_splits(ctx, blocks_of(T, 2 * kBM) * blocks_of(b.d, 256), 2 * kf, weights);
+        dxp = &add_problem(a, T, b.d, 256, kf, kf, splits);
+        dxp->a_map[0] = kDg;
+        dxp->a_map[1] = kDu;
+        dxp->b_map[0] = kWg;
+        dxp->b_map[1] = kWu;
+        dxp->b_mn = 1;
+        rc = set_output(ctx, a, *dxp, 8, {dx, T, b.d, b.ld_x}, nullptr, 0);
+        if (rc != DD_OK) return rc;
     }
     struct { int a, b; void *out; uint64_t m, n, ld; } weights[3] = {
         {kDg, kX, dw_gate, b.f, b.d, b.ld_in}, {kDu, kX, dw_up, b.f, b.d, b.ld_in}, {kDy, kH, dw_down, b.d, b.f, b.ld_down}};
-    for (const auto &w : weights) {
-        GemmProblem &q = add_problem(a, w.m, w.n, 256);
-        q.kblocks[0] = blocks_of(T, kBK);
+    for (int i = 0; i < 3; ++i) {
+        const auto &w = weights[i];
+        GemmProblem &q = add_problem(a, w.m, w.n, 256, kt);
         q.a_map[0] = (unsigned char)w.a;
         q.b_map[0] = (unsigned char)w.b;
         q.a_mn = q.b_mn = 1;
@@ -448,6 +523,11 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         q.ld_out = w.ld;
         q.out_f32 = grad_dtype == DD_F32;
         q.accumulate = accumulate != 0;
+        q.ragged = w.n * ge % 16 != 0;
+        q.out_map = (unsigned char)(9 + i);
+        rc = encode(ctx, &a.maps[9 + i], {w.out, w.m, w.n, w.ld}, q.out_f32 ? Box::kF32 : Box::kBf16);
+        if (rc != DD_OK) return rc;
     }
-    return launch_gemm<kEpiStore, 256>(ctx, a, stream);
+    rc = launch_gemm<kEpiStore, 256>(ctx, a, stream);
+    return rc == DD_OK && splits > 1 ? launch_reduce(ctx, *dxp, {dx, T, b.d, b.ld_x}, nullptr, 0, stream) : rc;
 }

@@ -28,9 +28,10 @@ namespace ddm {
 
 constexpr int kBM = 128, kBK = 64;              // rows of one CTA, K elements of a stage
 constexpr int kChunkBytes = 64 * 128;             // one TMA box: 64 rows of 64 bf16
-constexpr int kMaxMaps = 8, kMaxProblems = 4;
+constexpr int kMaxMaps = 12, kMaxProblems = 4;
 constexpr unsigned kTileGroup = 8;
-constexpr int kBoxBytes = 32 * 64;                // an epilogue box: 32 rows of 32 bf16
+constexpr int kMaxSplits = 8;
+constexpr int kBoxBytes = 32 * 64;                // an epilogue box: 32 rows of 32 bf16 (of float32: two of them)
 
 enum GemmEpilogue { kEpiStore = 0, kEpiGate = 1, kEpiBack = 2 };
 
@@ -48,10 +49,15 @@ struct GemmProblem {
     unsigned m, n;                    // output rows and columns
     unsigned tiles_m, tiles_n, tile_end;
     unsigned kblocks[2];              // K blocks of the two segments (second may be 0)
+    unsigned splits;                  // K is cut into this many units per tile, split s writing rows split_rows s + ...
+    unsigned split_rows;
     unsigned char a_map[2], b_map[2]; // tensor maps of the segments; kEpiGate: b_map = {w_gate, w_up}
     unsigned char a_mn, b_mn;         // 1: M (N) is the contiguous direction in memory
+    // kEpiStore
+    unsigned char out_map;            // tensor map of the output's boxes
     unsigned char out_f32, accumulate;
-    void *out;
+    unsigned char ragged;             // the output's rows end inside a 16-byte piece
+    void *out;                        // the output itself, for what is not stored by TMA
     const __nv_bfloat16 *residual;
     unsigned long long ld_out, ld_residual;
 };
@@ -67,12 +73,10 @@ struct GemmArgs {
     EpilogueArgs e;                   // kEpiStore: the problems have their own outputs
 };
 
-// Epilogue warps: eight where a row's results cost an activation, four where they are only stored.
-__host__ __device__ constexpr int gemm_epi_warps(int epi) { return epi == kEpiStore ? 4 : 8; }
-__host__ __device__ constexpr int gemm_threads(int epi) { return 32 * gemm_epi_warps(epi) + 64; }
-// Boxes a warp of the epilogue stages: kEpiGate 3 out, kEpiBack 2 in and 3 out.
-__host__ __device__ constexpr int gemm_boxes(int epi) { return epi == kEpiStore ? 0 : epi == kEpiGate ? 3 : 5; }
-__host__ __device__ constexpr unsigned gemm_epi_bytes(int epi) { return gemm_epi_warps(epi) * gemm_boxes(epi) * kBoxBytes; }
+constexpr int kEpiWarps = 8, kGemmThreads = 32 * kEpiWarps + 64;
+// Boxes a warp of the epilogue stages: kEpiStore 2 (alternating), kEpiGate 3 out, kEpiBack 2 in and 3 out.
+__host__ __device__ constexpr int gemm_boxes(int epi) { return epi == kEpiStore ? 2 : epi == kEpiGate ? 3 : 5; }
+__host__ __device__ constexpr unsigned gemm_epi_bytes(int epi) { return kEpiWarps * gemm_boxes(epi) * kBoxBytes; }
 // A stage of one CTA: 128 rows of A and half of the tile's BN rows of B.
 __host__ __device__ constexpr unsigned gemm_stage_bytes(int bn) { return (unsigned)(kBM + bn / 2) * kBK * 2; }
 __host__ __device__ constexpr int gemm_stages(int epi, int bn) { return (int)((224 * 1024 - gemm_epi_bytes(epi)) / gemm_stage_bytes(bn)); }
@@ -135,7 +139,8 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, int x, int 
 
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // Shared memory of this thread's stores so far may be written again / their results are in memory.
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" :: "n"(LEFT) : "memory"); }
 __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // This CTA's shared-memory address as the cluster address of the same place in CTA `rank`.
@@ -265,6 +270,8 @@ __device__ __forceinline__ void load_row32_f32(const float *src, float (&x)[32],
 struct TilePos {
     int p;                    // problem
     unsigned m0, n0;          // first output row and column
+    unsigned split;
+    unsigned kb0, kb1;        // K blocks, counted over both segments
 };
 
 // Neighbouring tiles (what the GPU holds at one time) cover a block of 8 tile rows, so that both
@@ -277,11 +284,16 @@ __device__ __forceinline__ TilePos tile_pos(const GemmArgs &a, unsigned t)
     while (t >= a.prob[r.p].tile_end) ++r.p;
     const GemmProblem &p = a.prob[r.p];
     t -= r.p ? a.prob[r.p - 1].tile_end : 0u;
+    r.split = t % p.splits;
+    t /= p.splits;
     const unsigned group = kTileGroup * p.tiles_n, g = t / group, first = kTileGroup * g;
     const unsigned rows = p.tiles_m - first < kTileGroup ? p.tiles_m - first : kTileGroup;
     t -= g * group;
     r.m0 = (first + t % rows) * 2 * kBM;
     r.n0 = (t / rows) * COLS;
+    const unsigned long long blocks = p.kblocks[0] + p.kblocks[1];
+    r.kb0 = (unsigned)(blocks * r.split / p.splits);
+    r.kb1 = (unsigned)(blocks * (r.split + 1) / p.splits);
     return r;
 }
 
@@ -295,41 +307,26 @@ __device__ __forceinline__ bool gemm_wait(unsigned bar, unsigned parity, volatil
     return false;
 }
 
-// kEpiStore: results of 32 columns from `col` on of one output row, from its accumulator columns at `taddr`.
-__device__ __forceinline__ void store_columns(const GemmProblem &p, unsigned taddr, unsigned row, unsigned col)
+// Up to 32 columns of one row, stored from registers.
+__device__ __forceinline__ void store_columns(const GemmProblem &p, unsigned row, unsigned col, const float (&x)[32])
 {
     const unsigned cols = p.n - col < 32 ? p.n - col : 32;
-    unsigned r[32];
-    tmem_ld32(taddr, r);
-    tmem_ld_wait();
-    if (row >= p.m) return;
-    float x[32];
-#pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
     const unsigned long long at = (unsigned long long)row * p.ld_out + col;
-    float add[32];
-    if (p.residual) {
-        load_row32(p.residual + (unsigned long long)row * p.ld_residual + col, add, cols);
+    if (p.out_f32) store_row32_f32(static_cast<float *>(p.out) + at, x, cols);
+    else store_row32(static_cast<__nv_bfloat16 *>(p.out) + at, x, cols);
+}
+
+// out += x for up to 32 columns of one row.
+__device__ __forceinline__ void add_columns(const GemmProblem &p, unsigned row, unsigned col, float (&x)[32])
+{
+    const unsigned cols = p.n - col < 32 ? p.n - col : 32;
+    const unsigned long long at = (unsigned long long)row * p.ld_out + col;
+    float old[32];
+    if (p.out_f32) load_row32_f32(static_cast<float *>(p.out) + at, old, cols);
+    else load_row32(static_cast<__nv_bfloat16 *>(p.out) + at, old, cols);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) x[j] += add[j];
-    }
-    if (p.out_f32) {
-        float *o = static_cast<float *>(p.out) + at;
-        if (p.accumulate) {
-            load_row32_f32(o, add, cols);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) x[j] += add[j];
-        }
-        store_row32_f32(o, x, cols);
-    } else {
-        __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.out) + at;
-        if (p.accumulate) {
-            load_row32(o, add, cols);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) x[j] += add[j];
-        }
-        store_row32(o, x, cols);
-    }
+    for (int j = 0; j < 32; ++j) x[j] += old[j];
+    store_columns(p, row, col, x);
 }
 
 // A lane's row of a staged box (64-byte rows, 64-byte swizzle: the 16-byte piece j of row r lies at
@@ -343,6 +340,16 @@ __device__ __forceinline__ void write_box(unsigned box, int lane, const float (&
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
                      :: "r"(box_piece(box, lane, j)), "r"(pack2(x[8 * j], x[8 * j + 1])), "r"(pack2(x[8 * j + 2], x[8 * j + 3])),
                         "r"(pack2(x[8 * j + 4], x[8 * j + 5])), "r"(pack2(x[8 * j + 6], x[8 * j + 7])) : "memory");
+}
+
+// The same for 128-byte rows of float32 in the 128-byte swizzle.
+__device__ __forceinline__ void write_box_f32(unsigned box, int lane, const float (&x)[32])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};"
+                     :: "r"(box + lane * 128 + ((j ^ (lane & 7)) << 4)), "f"(x[4 * j]), "f"(x[4 * j + 1]), "f"(x[4 * j + 2]),
+                        "f"(x[4 * j + 3]) : "memory");
 }
 
 __device__ __forceinline__ void read_box(unsigned box, int lane, float (&x)[32])
@@ -374,10 +381,10 @@ __device__ __forceinline__ unsigned chunks_of(const GemmProblem &p, const TilePo
 // BN: accumulator columns of a pair's tile.  kEpiGate puts BN / 2 columns of gate (the first CTA's
 // share of B) beside BN / 2 of up (the second's).
 template <int EPI, int BN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gemm_threads(EPI), 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
 {
-    constexpr int kStages = gemm_stages(EPI, BN), kEpiWarps = gemm_epi_warps(EPI), kProducer = kEpiWarps, kIssuer = kEpiWarps + 1;
+    constexpr int kStages = gemm_stages(EPI, BN), kProducer = kEpiWarps, kIssuer = kEpiWarps + 1;
     constexpr unsigned kStageBytes = gemm_stage_bytes(BN), kABytes = kBM * kBK * 2;
     constexpr int kCols = EPI == kEpiGate ? BN / 2 : BN;      // output columns of a tile
     constexpr unsigned kTmemCols = 2 * BN;
@@ -431,21 +438,19 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                 const TilePos pos = tile_pos<kCols>(a, t);
                 const GemmProblem &p = a.prob[pos.p];
                 const int m0 = (int)(pos.m0 + rank * kBM), n0 = (int)(pos.n0 + (EPI == kEpiGate ? 0 : rank * (BN / 2)));
-                for (int seg = 0; ok && seg < 2; ++seg) {
+                for (unsigned kb = pos.kb0; kb < pos.kb1; ++kb, ++it) {
+                    if ((it >= kStages && !gemm_wait(empty + 8 * s, phase, abort)) || *abort) { ok = false; break; }
+                    const int seg = kb >= p.kblocks[0], k0 = (int)(kb - (seg ? p.kblocks[0] : 0u)) * kBK;
                     const CUtensorMap *ma = &a.maps[p.a_map[seg]], *mb = &a.maps[p.b_map[EPI == kEpiGate ? rank : seg]];
-                    for (unsigned kb = 0; kb < p.kblocks[seg]; ++kb, ++it) {
-                        if ((it >= kStages && !gemm_wait(empty + 8 * s, phase, abort)) || *abort) { ok = false; break; }
-                        const unsigned st = smem + s * kStageBytes, bar = full0 + 8 * s;
-                        if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, 2 * kStageBytes);
-                        const int k0 = (int)kb * kBK;
+                    const unsigned st = smem + s * kStageBytes, bar = full0 + 8 * s;
+                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, 2 * kStageBytes);
 #pragma unroll
-                        for (int c = 0; c < kBM / 64; ++c)
-                            tma_load_2d_pair(st + c * kChunkBytes, ma, p.a_mn ? m0 + 64 * c : k0, p.a_mn ? k0 : m0 + 64 * c, bar);
+                    for (int c = 0; c < kBM / 64; ++c)
+                        tma_load_2d_pair(st + c * kChunkBytes, ma, p.a_mn ? m0 + 64 * c : k0, p.a_mn ? k0 : m0 + 64 * c, bar);
 #pragma unroll
-                        for (int c = 0; c < BN / 128; ++c)
-                            tma_load_2d_pair(st + kABytes + c * kChunkBytes, mb, p.b_mn ? n0 + 64 * c : k0, p.b_mn ? k0 : n0 + 64 * c, bar);
-                        if (++s == kStages) { s = 0; phase ^= 1; }
-                    }
+                    for (int c = 0; c < BN / 128; ++c)
+                        tma_load_2d_pair(st + kABytes + c * kChunkBytes, mb, p.b_mn ? n0 + 64 * c : k0, p.b_mn ? k0 : n0 + 64 * c, bar);
+                    if (++s == kStages) { s = 0; phase ^= 1; }
                 }
             }
             // no copy of either CTA may be in flight when the pair ends, whoever gave up
@@ -467,15 +472,14 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                 const unsigned idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((unsigned)p.a_mn << 15) |
                                        ((unsigned)p.b_mn << 16) | ((unsigned)(BN / 8) << 17) | ((2 * kBM / 16) << 24);
                 const unsigned astep = p.a_mn ? 2048 : 32, bstep = p.b_mn ? 2048 : 32;     // bytes per 16 K elements
-                const unsigned blocks = p.kblocks[0] + p.kblocks[1];
-                for (unsigned kb = 0; kb < blocks; ++kb) {
+                for (unsigned kb = pos.kb0; kb < pos.kb1; ++kb) {
                     if (!gemm_wait(full + 8 * s, phase, abort)) { ok = false; break; }
                     tc_fence_after();
                     const unsigned sa = smem + s * kStageBytes, sb = sa + kABytes;
 #pragma unroll
                     for (int k = 0; k < kBK / 16; ++k)
                         umma_bf16_pair(tmem + slot * BN, umma_desc(sa + k * astep, p.a_mn), umma_desc(sb + k * bstep, p.b_mn),
-                                       idesc, kb | k);
+                                       idesc, kb != pos.kb0 || k);
                     umma_commit_pair(empty + 8 * s, 3);
                     if (++s == kStages) { s = 0; phase ^= 1; }
                 }
@@ -490,7 +494,8 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
         // kEpiGate, kEpiBack: this warp's boxes; kEpiBack reads gate and up one chunk ahead
         const unsigned box = smem + kStages * kStageBytes + warp * gemm_boxes(EPI) * kBoxBytes, out = box + (EPI == kEpiBack ? 2 * kBoxBytes : 0);
         const unsigned landed = boxes_in + 8 * warp;
-        unsigned phase = 0, loads = 0;
+        unsigned phase = 0, loads = 0, stores = 0;
+        bool was_f32 = false;
         const auto load_chunk = [&](const TilePos &pos, unsigned c) {
             if (lane == 0) {
                 const int x = (int)(pos.n0 + half * (kCols / 2) + 32 * c), y = (int)(pos.m0 + row0);
@@ -521,9 +526,53 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             tc_fence_after();
             const unsigned taddr = tmem + ((unsigned)((warp & 3) * 32) << 16) + slot * BN;
             if (EPI == kEpiStore) {
+                const unsigned chunks = chunks_of<kCols>(p, pos, row0, half), row = pos.m0 + row0 + lane;
 #pragma unroll 1
-                for (int c = 0; c < kCols && pos.n0 + c < p.n; c += 32)
-                    store_columns(p, taddr + c, pos.m0 + row0 + lane, pos.n0 + c);
+                for (unsigned c = 0; c < chunks; ++c) {
+                    const unsigned col = half * (kCols / 2) + 32 * c;
+                    unsigned r[32];
+                    float x[32];
+                    tmem_ld32(taddr + col, r);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
+                    if (p.accumulate) {
+                        if (row < p.m) add_columns(p, row, pos.n0 + col, x);
+                        continue;
+                    }
+                    if (p.residual && row < p.m) {
+                        float add[32];
+                        load_row32(p.residual + (unsigned long long)row * p.ld_residual + pos.n0 + col, add, p.n - pos.n0 - col);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[j] += add[j];
+                    }
+                    if (p.ragged && pos.n0 + col + 32 > p.n) {        // TMA stores end on 16-byte pieces
+                        if (row < p.m) store_columns(p, row, pos.n0 + col, x);
+                        continue;
+                    }
+                    unsigned to = box;
+                    if (p.out_f32) {
+                        if (lane == 0) bulk_wait_read<0>();
+                        __syncwarp();
+                        write_box_f32(to, lane, x);
+                    } else {                               // two boxes in turn; a float32 box fills both
+                        to += stores & 1 ? kBoxBytes : 0;
+                        if (lane == 0) {
+                            if (was_f32) bulk_wait_read<0>();
+                            else bulk_wait_read<1>();
+                        }
+                        __syncwarp();
+                        write_box(to, lane, x);
+                    }
+                    was_f32 = p.out_f32;
+                    ++stores;
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(&a.maps[p.out_map], (int)(pos.n0 + col), (int)(pos.split * p.split_rows + pos.m0 + row0), to);
+                        bulk_commit();
+                    }
+                }
             } else {
                 const unsigned chunks = chunks_of<kCols>(p, pos, row0, half);
 #pragma unroll 1
@@ -562,13 +611,21 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                             u[j] = dh * act;                       // dup
                         }
                     }
-                    if (lane == 0) bulk_wait_read();               // the boxes of the chunk before
+                    if (lane == 0) bulk_wait_read<0>();               // the boxes of the chunk before
                     __syncwarp();
-                    const bool all = EPI == kEpiBack || a.e.gate;
+                    // TMA stores end on 16-byte pieces; a row of the caller's that does not is stored from registers
+                    // (what kEpiBack writes lies in scratch with whole pieces)
+                    const bool ragged = EPI == kEpiGate && (p.n & 7) && pos.n0 + col + 32 > p.n;
+                    const bool all = EPI == kEpiBack || (a.e.gate && !ragged);
                     write_box(out, lane, x);
                     if (all) {
                         write_box(out + kBoxBytes, lane, g);
                         write_box(out + 2 * kBoxBytes, lane, u);
+                    }
+                    if (ragged && a.e.gate && pos.m0 + row0 + lane < p.m) {
+                        const unsigned long long at = (unsigned long long)(pos.m0 + row0 + lane) * a.e.ld_gate + pos.n0 + col;
+                        store_row32(a.e.gate + at, g, p.n - pos.n0 - col);
+                        store_row32(a.e.up + at, u, p.n - pos.n0 - col);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
@@ -588,7 +645,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * slot);
         }
-        if (EPI != kEpiStore && lane == 0) bulk_wait();
+        if (lane == 0) bulk_wait();
         if (EPI == kEpiBack && !ok && loads) mbar_wait_bounded(landed, (loads - 1) & 1);     // a copy may be in flight
     }
     __syncwarp();
@@ -598,6 +655,54 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
     if (warp == kIssuer)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
     if (threadIdx.x == 0 && abort_flag && a.e.status) *a.e.status = DD_STATUS_WAIT_LIMIT;
+}
+
+// out = bf16([residual +] sum of the splits' float32 slabs in split order), eight columns a thread.
+__global__ void __launch_bounds__(256)
+ffn_reduce_kernel(const float *__restrict__ slabs, const unsigned splits, const unsigned long long slab, const unsigned ld,
+                  const unsigned m, const unsigned n, const __nv_bfloat16 *residual, const unsigned long long ld_residual,
+                  __nv_bfloat16 *out, const unsigned long long ld_out)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const unsigned pieces = (n + 7) / 8;
+    for (unsigned long long i = (unsigned long long)blockIdx.x * blockDim.x + threadIdx.x; i < (unsigned long long)m * pieces;
+         i += (unsigned long long)gridDim.x * blockDim.x) {
+        const unsigned row = (unsigned)(i / pieces), col = (unsigned)(i % pieces) * 8, cols = n - col < 8 ? n - col : 8;
+        const float *src = slabs + (unsigned long long)row * ld + col;
+        float4 a[kMaxSplits], b[kMaxSplits];
+#pragma unroll
+        for (int s = 0; s < kMaxSplits; ++s)
+            if (s < splits) {
+                a[s] = __ldcg(reinterpret_cast<const float4 *>(src + s * slab));
+                b[s] = __ldcg(reinterpret_cast<const float4 *>(src + s * slab) + 1);
+            }
+        float x[8] = {a[0].x, a[0].y, a[0].z, a[0].w, b[0].x, b[0].y, b[0].z, b[0].w};
+#pragma unroll
+        for (int s = 1; s < kMaxSplits; ++s)
+            if (s < splits) {
+                x[0] += a[s].x; x[1] += a[s].y; x[2] += a[s].z; x[3] += a[s].w;
+                x[4] += b[s].x; x[5] += b[s].y; x[6] += b[s].z; x[7] += b[s].w;
+            }
+        __nv_bfloat16 *o = out + (unsigned long long)row * ld_out + col;
+        const __nv_bfloat16 *r = residual ? residual + (unsigned long long)row * ld_residual + col : nullptr;
+        if (cols == 8) {
+            if (r) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(r);
+                const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[2 * j] += __uint_as_float(u[j] << 16);
+                    x[2 * j + 1] += __uint_as_float(u[j] & 0xffff0000u);
+                }
+            }
+            *reinterpret_cast<uint4 *>(o) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (j < cols) o[j] = __float2bfloat16_rn(r ? x[j] + __bfloat162float(r[j]) : x[j]);
+        }
+    }
 }
 
 }  // namespace ddm

@@ -109,7 +109,8 @@ SIZES = [
     (1, 8, 8), (1, 64, 64), (1, 2048, 512), (2, 40, 24), (3, 1, 1), (5, 72, 136), (8, 256, 1000), (9, 264, 520),
     (16, 512, 512), (17, 96, 200), (31, 1000, 120), (33, 136, 264), (64, 128, 384), (65, 257, 131), (100, 520, 1032),
     (127, 64, 128), (128, 128, 256), (129, 136, 264), (200, 333, 777), (256, 1024, 512), (300, 64, 2048),
-    (515, 200, 312), (1030, 264, 72), (2100, 136, 520),
+    (515, 200, 312), (1030, 264, 72), (2100, 136, 520), (300, 257, 131), (290, 333, 777), (700, 1001, 258),
+    (600, 100, 8200), (1025, 2056, 640),
 ]
 
 
