@@ -33,22 +33,16 @@ static EncodeTiled tensor_map_encoder()
 
 struct Matrix {
     const void *data;
-    unsigned long long rows, cols, ld;      // elements
+    unsigned long long rows, cols, ld;      // bf16 elements
 };
 
-// How a matrix is copied: 64 x rows boxes for operands; 32 x 32 boxes for the epilogues, of bf16
-// (64-byte rows) or float32.
-enum class Box { kOperand, kBf16, kF32 };
-
-static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m, Box kind = Box::kOperand, unsigned rows = 64)
+static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m, unsigned box_rows = 64)
 {
-    const unsigned eb = kind == Box::kF32 ? 4 : 2;
-    const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * eb};
-    const cuuint32_t box[2] = {kind == Box::kOperand ? 64u : 32u, kind == Box::kOperand ? rows : 32u}, step[2] = {1, 1};
+    const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * 2};
+    const cuuint32_t box[2] = {64, box_rows}, step[2] = {1, 1};
     const EncodeTiled fn = tensor_map_encoder();
-    if (!fn || fn(map, eb == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(m.data),
-                  dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  kind == Box::kBf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    if (!fn || fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(m.data), dims, strides, box, step,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
         snprintf(ctx->cuda_err, sizeof ctx->cuda_err, "cuTensorMapEncodeTiled failed");
         return DD_ERR_CUDA;
@@ -113,12 +107,12 @@ static int allow_smem(dd_ctx *ctx, K kernel, size_t bytes, bool (&done)[64])
     return DD_OK;
 }
 
-template <int EPI, int BN>
-static int launch_gemm(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
+template <int EPI, int BN, int ACT>
+static int launch_gemm_act(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
 {
     constexpr size_t smem = gemm_smem_bytes(EPI, BN);
     static bool done[64];
-    const int rc = allow_smem(ctx, ffn_gemm_kernel<EPI, BN>, smem, done);
+    const int rc = allow_smem(ctx, ffn_gemm_kernel<EPI, BN, ACT>, smem, done);
     if (rc != DD_OK) return rc;
     const unsigned pairs = (unsigned)ctx->sm_count / 2;
     cudaLaunchConfig_t cfg = {};
@@ -131,25 +125,30 @@ static int launch_gemm(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
     at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_gemm_kernel<EPI, BN>, a));
+    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_gemm_kernel<EPI, BN, ACT>, a));
     return DD_OK;
 }
 
-// Output of problem `p` through tensor map `map`: the matrix itself, or its splits' slabs.
-static int set_output(dd_ctx *ctx, GemmArgs &a, GemmProblem &p, int map, const Matrix &out, const void *residual, uint64_t ld_residual)
+template <int EPI, int BN>
+static int launch_gemm(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
 {
-    p.out_map = (unsigned char)map;
+    return EPI != kEpiStore && a.e.activation == DD_ACT_GELU_TANH ? launch_gemm_act<EPI, BN, EPI == kEpiStore ? DD_ACT_SILU : DD_ACT_GELU_TANH>(ctx, a, stream)
+                                                                  : launch_gemm_act<EPI, BN, DD_ACT_SILU>(ctx, a, stream);
+}
+
+// Output of problem `p`: the matrix itself, or its splits' slabs.
+static void set_output(const dd_ctx *ctx, GemmProblem &p, const Matrix &out, const void *residual, uint64_t ld_residual)
+{
     if (p.splits > 1) {
         p.out_f32 = 1;
-        const uint64_t ld = (out.cols + 7) / 8 * 8;
-        return encode(ctx, &a.maps[map], {ctx->ffn_slabs, (uint64_t)p.splits * p.split_rows, out.cols, ld}, Box::kF32);
+        p.out = ctx->ffn_slabs;
+        p.ld_out = (out.cols + 7) / 8 * 8;
+        return;
     }
     p.out = const_cast<void *>(out.data);
     p.ld_out = out.ld;
-    p.ragged = out.cols % 8 != 0;
-    p.residual = (const __nv_bfloat16 *)residual;
-    p.ld_residual = ld_residual;
-    return encode(ctx, &a.maps[map], out, Box::kBf16);
+    p.addend = residual;
+    p.ld_addend = ld_residual;
 }
 
 static int launch_reduce(dd_ctx *ctx, const GemmProblem &p, const Matrix &out, const void *residual, uint64_t ld_residual, cudaStream_t stream)
@@ -172,8 +171,8 @@ static int launch_reduce(dd_ctx *ctx, const GemmProblem &p, const Matrix &out, c
     return DD_OK;
 }
 
-template <int EPI, int N>
-static int launch_stream_n(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
+template <int EPI, int N, int ACT>
+static int launch_stream_act(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
 {
     a.tiles_n = blocks_of(a.n, N);
     const unsigned tiles = blocks_of(a.m, stream_features(EPI)) * a.tiles_n, blocks = a.kblocks[0] + a.kblocks[1];
@@ -189,7 +188,7 @@ static int launch_stream_n(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
     cfg.dynamicSmemBytes = stream_smem_bytes(N, a.stages);
     cfg.stream = stream;
     static bool done[64];
-    const int rc = allow_smem(ctx, ffn_stream_kernel<EPI, N>, cfg.dynamicSmemBytes, done);
+    const int rc = allow_smem(ctx, ffn_stream_kernel<EPI, N, ACT>, cfg.dynamicSmemBytes, done);
     if (rc != DD_OK) return rc;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -198,8 +197,15 @@ static int launch_stream_n(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_stream_kernel<EPI, N>, a));
+    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_stream_kernel<EPI, N, ACT>, a));
     return DD_OK;
+}
+
+template <int EPI, int N>
+static int launch_stream_n(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
+{
+    return EPI != kEpiStore && a.e.activation == DD_ACT_GELU_TANH ? launch_stream_act<EPI, N, EPI == kEpiStore ? DD_ACT_SILU : DD_ACT_GELU_TANH>(ctx, a, stream)
+                                                                  : launch_stream_act<EPI, N, DD_ACT_SILU>(ctx, a, stream);
 }
 
 template <int EPI>
@@ -359,14 +365,14 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
         a.kblocks[0] = blocks_of(b.d, kBK);
         rc = encode(ctx, &a.w[0], mg);
         if (rc == DD_OK) rc = encode(ctx, &a.w[1], mu);
-        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mx, Box::kOperand, stream_box(T));
+        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mx, stream_box(T));
         if (rc == DD_OK) rc = launch_stream<kEpiGate>(ctx, a, stream);
         if (rc != DD_OK) return rc;
         a.m = (unsigned)b.d;
         a.kblocks[0] = blocks_of(b.f, kBK);
         a.own_prior = 1;
         rc = encode(ctx, &a.w[0], md);
-        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mh, Box::kOperand, stream_box(T));
+        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mh, stream_box(T));
         return rc == DD_OK ? launch_stream<kEpiStore>(ctx, a, stream) : rc;
     }
     GemmArgs a;
@@ -375,9 +381,6 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
     rc = encode(ctx, &a.maps[0], mx);
     if (rc == DD_OK) rc = encode(ctx, &a.maps[1], mg);
     if (rc == DD_OK) rc = encode(ctx, &a.maps[2], mu);
-    if (rc == DD_OK) rc = encode(ctx, &a.maps[kOutHidden], mh, Box::kBf16);
-    if (rc == DD_OK && gate) rc = encode(ctx, &a.maps[kOutGate], {gate, T, b.f, b.ld_gate}, Box::kBf16);
-    if (rc == DD_OK && gate) rc = encode(ctx, &a.maps[kOutUp], {up, T, b.f, b.ld_gate}, Box::kBf16);
     if (rc != DD_OK) return rc;
     GemmProblem &p = add_problem(a, T, b.f, 128, blocks_of(b.d, kBK));
     p.b_map[0] = 1;
@@ -393,7 +396,7 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
     q.b_map[0] = 1;
     rc = encode(ctx, &a.maps[0], mh);
     if (rc == DD_OK) rc = encode(ctx, &a.maps[1], md);
-    if (rc == DD_OK) rc = set_output(ctx, a, q, 2, {y, T, b.d, b.ld_y}, residual, b.ld_y);
+    set_output(ctx, q, {y, T, b.d, b.ld_y}, residual, b.ld_y);
     if (rc == DD_OK) rc = launch_gemm<kEpiStore, 256>(ctx, a, stream);
     return rc == DD_OK && splits > 1 ? launch_reduce(ctx, q, {y, T, b.d, b.ld_y}, residual, b.ld_y, stream) : rc;
 }
@@ -468,7 +471,7 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         c.kblocks[0] = blocks_of(b.d, kBK);
         c.w[0] = a.maps[kWd];
         c.w_mn = 1;
-        rc = encode(ctx, &c.x[0], mats[kDy], Box::kOperand, stream_box(T));
+        rc = encode(ctx, &c.x[0], mats[kDy], stream_box(T));
         if (rc == DD_OK) rc = launch_stream<kEpiBack>(ctx, c, stream);
         if (rc != DD_OK) return rc;
         c.m = (unsigned)b.d;                              // dgate w_gate + dup w_up
@@ -476,20 +479,15 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         c.w[0] = a.maps[kWg];
         c.w[1] = a.maps[kWu];
         c.own_prior = 1;
-        rc = encode(ctx, &c.x[0], mats[kDg], Box::kOperand, stream_box(T));
-        if (rc == DD_OK) rc = encode(ctx, &c.x[1], mats[kDu], Box::kOperand, stream_box(T));
+        rc = encode(ctx, &c.x[0], mats[kDg], stream_box(T));
+        if (rc == DD_OK) rc = encode(ctx, &c.x[1], mats[kDu], stream_box(T));
         if (rc == DD_OK) rc = launch_stream<kEpiStore>(ctx, c, stream);
         if (rc != DD_OK) return rc;
     } else {
         GemmArgs c = a;
         c.maps[0] = a.maps[kDy];
         c.maps[1] = a.maps[kWd];
-        rc = encode(ctx, &c.maps[kBackGate], {gate, T, b.f, b.ld_gate}, Box::kBf16);
-        if (rc == DD_OK) rc = encode(ctx, &c.maps[kBackUp], {up, T, b.f, b.ld_gate}, Box::kBf16);
-        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutHidden], mats[kH], Box::kBf16);
-        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutGate], mats[kDg], Box::kBf16);
-        if (rc == DD_OK) rc = encode(ctx, &c.maps[kOutUp], mats[kDu], Box::kBf16);
-        if (rc != DD_OK) return rc;
+                    if (rc != DD_OK) return rc;
         GemmProblem &p = add_problem(c, T, b.f, 256, blocks_of(b.d, kBK));
         p.b_map[0] = 1;
         p.b_mn = 1;
@@ -508,25 +506,20 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         dxp->b_map[0] = kWg;
         dxp->b_map[1] = kWu;
         dxp->b_mn = 1;
-        rc = set_output(ctx, a, *dxp, 8, {dx, T, b.d, b.ld_x}, nullptr, 0);
-        if (rc != DD_OK) return rc;
+        set_output(ctx, *dxp, {dx, T, b.d, b.ld_x}, nullptr, 0);
     }
     struct { int a, b; void *out; uint64_t m, n, ld; } weights[3] = {
         {kDg, kX, dw_gate, b.f, b.d, b.ld_in}, {kDu, kX, dw_up, b.f, b.d, b.ld_in}, {kDy, kH, dw_down, b.d, b.f, b.ld_down}};
-    for (int i = 0; i < 3; ++i) {
-        const auto &w = weights[i];
+    for (const auto &w : weights) {
         GemmProblem &q = add_problem(a, w.m, w.n, 256, kt);
         q.a_map[0] = (unsigned char)w.a;
         q.b_map[0] = (unsigned char)w.b;
         q.a_mn = q.b_mn = 1;
         q.out = w.out;
         q.ld_out = w.ld;
-        q.out_f32 = grad_dtype == DD_F32;
-        q.accumulate = accumulate != 0;
-        q.ragged = w.n * ge % 16 != 0;
-        q.out_map = (unsigned char)(9 + i);
-        rc = encode(ctx, &a.maps[9 + i], {w.out, w.m, w.n, w.ld}, q.out_f32 ? Box::kF32 : Box::kBf16);
-        if (rc != DD_OK) return rc;
+        q.out_f32 = q.addend_f32 = grad_dtype == DD_F32;
+        q.addend = accumulate ? w.out : nullptr;
+        q.ld_addend = w.ld;
     }
     rc = launch_gemm<kEpiStore, 256>(ctx, a, stream);
     return rc == DD_OK && splits > 1 ? launch_reduce(ctx, *dxp, {dx, T, b.d, b.ld_x}, nullptr, 0, stream) : rc;

@@ -28,10 +28,10 @@ namespace ddm {
 
 constexpr int kBM = 128, kBK = 64;              // rows of one CTA, K elements of a stage
 constexpr int kChunkBytes = 64 * 128;             // one TMA box: 64 rows of 64 bf16
-constexpr int kMaxMaps = 12, kMaxProblems = 4;
+constexpr int kMaxMaps = 8, kMaxProblems = 4;
 constexpr unsigned kTileGroup = 8;
 constexpr int kMaxSplits = 8;
-constexpr int kBoxBytes = 32 * 64;                // an epilogue box: 32 rows of 32 bf16 (of float32: two of them)
+constexpr int kBoxBytes = 32 * 128;               // an epilogue box: 32 rows of 64 bf16 or 32 float32
 
 enum GemmEpilogue { kEpiStore = 0, kEpiGate = 1, kEpiBack = 2 };
 
@@ -53,20 +53,15 @@ struct GemmProblem {
     unsigned split_rows;
     unsigned char a_map[2], b_map[2]; // tensor maps of the segments; kEpiGate: b_map = {w_gate, w_up}
     unsigned char a_mn, b_mn;         // 1: M (N) is the contiguous direction in memory
-    // kEpiStore
-    unsigned char out_map;            // tensor map of the output's boxes
-    unsigned char out_f32, accumulate;
-    unsigned char ragged;             // the output's rows end inside a 16-byte piece
-    void *out;                        // the output itself, for what is not stored by TMA
-    const __nv_bfloat16 *residual;
-    unsigned long long ld_out, ld_residual;
+    // kEpiStore: out = sums [+ addend]; the addend may be the output itself
+    unsigned char out_f32, addend_f32;
+    void *out;
+    const void *addend;
+    unsigned long long ld_out, ld_addend;
 };
 
-// Tensor maps of the epilogues' boxes (32 x 32): results, and what kEpiBack reads.
-enum { kOutHidden = 3, kOutGate = 4, kOutUp = 5, kBackGate = 6, kBackUp = 7 };
-
 struct GemmArgs {
-    CUtensorMap maps[kMaxMaps];       // operands: 64 x 64 boxes of row-major bf16 matrices
+    CUtensorMap maps[kMaxMaps];       // 64 x 64 boxes of row-major bf16 matrices
     GemmProblem prob[kMaxProblems];
     int nprob;
     unsigned tiles;
@@ -74,8 +69,8 @@ struct GemmArgs {
 };
 
 constexpr int kEpiWarps = 8, kGemmThreads = 32 * kEpiWarps + 64;
-// Boxes a warp of the epilogue stages: kEpiStore 2 (alternating), kEpiGate 3 out, kEpiBack 2 in and 3 out.
-__host__ __device__ constexpr int gemm_boxes(int epi) { return epi == kEpiStore ? 2 : epi == kEpiGate ? 3 : 5; }
+// Boxes that a warp of the epilogue stages results in; kEpiBack also reads gate and up through its two.
+__host__ __device__ constexpr int gemm_boxes(int epi) { return epi == kEpiStore ? 1 : 2; }
 __host__ __device__ constexpr unsigned gemm_epi_bytes(int epi) { return kEpiWarps * gemm_boxes(epi) * kBoxBytes; }
 // A stage of one CTA: 128 rows of A and half of the tile's BN rows of B.
 __host__ __device__ constexpr unsigned gemm_stage_bytes(int bn) { return (unsigned)(kBM + bn / 2) * kBK * 2; }
@@ -131,18 +126,6 @@ __device__ __forceinline__ void tma_load_2d_pair(unsigned dst, const CUtensorMap
                  :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, int x, int y, unsigned src)
-{
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
-                 :: "l"(map), "r"(x), "r"(y), "r"(src) : "memory");
-}
-
-__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-// Shared memory of this thread's stores so far may be written again / their results are in memory.
-template <int LEFT>
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" :: "n"(LEFT) : "memory"); }
-__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
 // This CTA's shared-memory address as the cluster address of the same place in CTA `rank`.
 __device__ __forceinline__ unsigned cluster_addr(unsigned addr, unsigned rank)
 {
@@ -188,20 +171,25 @@ __device__ __forceinline__ unsigned long long umma_desc(unsigned addr, bool mn)
 
 // ---- activation ---------------------------------------------------------------------------------
 
-// Both activations are g sigmoid(s(g)); returns a(g) and sets its derivative.  exp and the division
-// are the fast forms (2 ulp): their error is far below the bf16 rounding of what they feed.
-template <bool SLOPE>
-__device__ __forceinline__ float activate(float g, int kind, float *slope)
+// Both activations are g sigmoid(s(g)); returns a(g) and sets its derivative.  The exponential and the
+// reciprocal are the hardware's approximations (2 ulp and 1 ulp): their error is far below the bf16
+// rounding of what they feed, and the epilogues are bound by their instruction count.  exp overflows
+// to infinity and the sigmoid to 0 where it should.
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ float activate(float g, float *slope)
 {
-    constexpr float k = 1.5957691216057308f, q = 0.044715f;      // 2 sqrt(2 / pi)
-    const float s = kind == DD_ACT_SILU ? g : k * g * fmaf(q * g, g, 1.0f);
-    const float e = __expf(-s);
-    const float sg = __fdividef(1.0f, 1.0f + e);
+    constexpr float k = 1.5957691216057308f, q = 0.044715f, l = -1.4426950408889634f;      // 2 sqrt(2 / pi), -log2(e)
+    const float g2 = g * g;
+    const float z = ACT == DD_ACT_SILU ? l * g : g * fmaf(l * k * q, g2, l * k);            // -s log2(e)
+    float e, sg;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(sg) : "f"(1.0f + e));
+    const float a = g * sg;
     if (SLOPE) {
-        const float ds = kind == DD_ACT_SILU ? 1.0f : k * fmaf(3.0f * q * g, g, 1.0f);
-        *slope = sg * fmaf(g * ds, 1.0f - sg, 1.0f);
+        const float rest = 1.0f - sg;
+        *slope = fmaf(a, ACT == DD_ACT_SILU ? rest : rest * fmaf(3.0f * k * q, g2, k), sg);
     }
-    return g * sg;
+    return a;
 }
 
 __device__ __forceinline__ unsigned pack2(float lo, float hi)
@@ -210,59 +198,30 @@ __device__ __forceinline__ unsigned pack2(float lo, float hi)
     return *reinterpret_cast<const unsigned *>(&b);
 }
 
-// 32 consecutive bf16 of a row: 16-byte pieces as far as the row goes, single elements at its end.
-__device__ __forceinline__ void store_row32(__nv_bfloat16 *dst, const float (&x)[32], unsigned cols)
+// Up to four consecutive bf16, `live` of them inside the row.
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, const float (&x)[4], unsigned live)
 {
+    if (live >= 4) {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
+    } else {
 #pragma unroll
-    for (int j = 0; j < 32; j += 8) {
-        if (j + 8 <= cols) {
-            *reinterpret_cast<uint4 *>(dst + j) = make_uint4(pack2(x[j], x[j + 1]), pack2(x[j + 2], x[j + 3]),
-                                                             pack2(x[j + 4], x[j + 5]), pack2(x[j + 6], x[j + 7]));
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (j + i < cols) dst[j + i] = __float2bfloat16_rn(x[j + i]);
-        }
+        for (int i = 0; i < 3; ++i)
+            if (i < live) p[i] = __float2bfloat16_rn(x[i]);
     }
 }
 
-__device__ __forceinline__ void load_row32(const __nv_bfloat16 *src, float (&x)[32], unsigned cols)
+__device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&x)[4], unsigned live)
 {
+    if (live >= 4) {
+        const uint2 w = *reinterpret_cast<const uint2 *>(p);
+        x[0] = __uint_as_float(w.x << 16);
+        x[1] = __uint_as_float(w.x & 0xffff0000u);
+        x[2] = __uint_as_float(w.y << 16);
+        x[3] = __uint_as_float(w.y & 0xffff0000u);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 32; j += 8) {
-        if (j + 8 <= cols) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(src + j);
-            const unsigned u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[j + 2 * i] = __uint_as_float(u[i] << 16);
-                x[j + 2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[j + i] = j + i < cols ? __bfloat162float(src[j + i]) : 0.0f;
-        }
+        for (int i = 0; i < 4; ++i) x[i] = i < live ? __bfloat162float(p[i]) : 0.0f;
     }
-}
-
-__device__ __forceinline__ void store_row32_f32(float *dst, const float (&x)[32], unsigned cols)
-{
-#pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-        if (j + 4 <= cols) {
-            *reinterpret_cast<float4 *>(dst + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (j + i < cols) dst[j + i] = x[j + i];
-        }
-    }
-}
-
-__device__ __forceinline__ void load_row32_f32(const float *src, float (&x)[32], unsigned cols)
-{
-#pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = j < cols ? src[j] : 0.0f;
 }
 
 // ---- tiles ----------------------------------------------------------------------------------------
@@ -307,80 +266,134 @@ __device__ __forceinline__ bool gemm_wait(unsigned bar, unsigned parity, volatil
     return false;
 }
 
-// Up to 32 columns of one row, stored from registers.
-__device__ __forceinline__ void store_columns(const GemmProblem &p, unsigned row, unsigned col, const float (&x)[32])
+// Results leave a warp through a box in shared memory: in tensor memory a lane holds a row, in
+// global memory eight lanes together write 128 bytes of one.  (Rows written lane by lane cost the
+// load/store unit a pass per row; 64-byte boxes stored by the TMA engine took 1 us a box and warp.)
+// 128-byte rows, the 16-byte piece j of row r at piece j ^ (r mod 8): free of bank conflicts both ways.
+__device__ __forceinline__ unsigned box_piece(unsigned box, int row, int j) { return box + row * 128 + ((j ^ (row & 7)) << 4); }
+
+__device__ __forceinline__ void st_shared(unsigned addr, unsigned a, unsigned b, unsigned c, unsigned d)
 {
-    const unsigned cols = p.n - col < 32 ? p.n - col : 32;
-    const unsigned long long at = (unsigned long long)row * p.ld_out + col;
-    if (p.out_f32) store_row32_f32(static_cast<float *>(p.out) + at, x, cols);
-    else store_row32(static_cast<__nv_bfloat16 *>(p.out) + at, x, cols);
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// out += x for up to 32 columns of one row.
-__device__ __forceinline__ void add_columns(const GemmProblem &p, unsigned row, unsigned col, float (&x)[32])
+__device__ __forceinline__ uint4 ld_shared(unsigned addr)
 {
-    const unsigned cols = p.n - col < 32 ? p.n - col : 32;
-    const unsigned long long at = (unsigned long long)row * p.ld_out + col;
-    float old[32];
-    if (p.out_f32) load_row32_f32(static_cast<float *>(p.out) + at, old, cols);
-    else load_row32(static_cast<__nv_bfloat16 *>(p.out) + at, old, cols);
-#pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] += old[j];
-    store_columns(p, row, col, x);
+    uint4 w;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(addr) : "memory");
+    return w;
 }
 
-// A lane's row of a staged box (64-byte rows, 64-byte swizzle: the 16-byte piece j of row r lies at
-// piece j ^ (r / 2 mod 4), so that eight lanes at one piece touch all banks).
-__device__ __forceinline__ unsigned box_piece(unsigned box, int lane, int j) { return box + lane * 64 + ((j ^ (lane >> 1 & 3)) << 4); }
-
-__device__ __forceinline__ void write_box(unsigned box, int lane, const float (&x)[32])
+// 32 columns of the lane's row, packed bf16, as pieces 4 h .. 4 h + 3.
+__device__ __forceinline__ void write_half(unsigned box, int lane, int h, const unsigned (&w)[16])
 {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                     :: "r"(box_piece(box, lane, j)), "r"(pack2(x[8 * j], x[8 * j + 1])), "r"(pack2(x[8 * j + 2], x[8 * j + 3])),
-                        "r"(pack2(x[8 * j + 4], x[8 * j + 5])), "r"(pack2(x[8 * j + 6], x[8 * j + 7])) : "memory");
+    for (int j = 0; j < 4; ++j) st_shared(box_piece(box, lane, 4 * h + j), w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
 }
 
-// The same for 128-byte rows of float32 in the 128-byte swizzle.
-__device__ __forceinline__ void write_box_f32(unsigned box, int lane, const float (&x)[32])
+__device__ __forceinline__ void pack32(const float (&x)[32], unsigned (&w)[16])
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};"
-                     :: "r"(box + lane * 128 + ((j ^ (lane & 7)) << 4)), "f"(x[4 * j]), "f"(x[4 * j + 1]), "f"(x[4 * j + 2]),
-                        "f"(x[4 * j + 3]) : "memory");
+    for (int j = 0; j < 16; ++j) w[j] = pack2(x[2 * j], x[2 * j + 1]);
 }
 
-__device__ __forceinline__ void read_box(unsigned box, int lane, float (&x)[32])
+// The box to rows row0.. and columns col.. of a bf16 matrix of m x n.
+__device__ __forceinline__ void store_box(unsigned box, int lane, __nv_bfloat16 *out, unsigned long long ld, unsigned row0, unsigned col,
+                                          unsigned m, unsigned n)
 {
+    const unsigned c = col + (lane & 7) * 8;
+    uint4 w[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        unsigned w[4];
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(box_piece(box, lane, j)) : "memory");
+    for (int i = 0; i < 8; ++i) w[i] = ld_shared(box_piece(box, 4 * i + (lane >> 3), lane & 7));
+    __nv_bfloat16 *o = out + (unsigned long long)(row0 + (lane >> 3)) * ld + c;
+    if (row0 + 32 <= m && col + 64 <= n) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[8 * j + 2 * i] = __uint_as_float(w[i] << 16);
-            x[8 * j + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(o + 4 * i * ld) = w[i];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (row0 + 4 * i + (lane >> 3) >= m) break;
+        if (c + 8 <= n) {
+            *reinterpret_cast<uint4 *>(o + 4 * i * ld) = w[i];
+        } else {
+            const unsigned u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+            for (int k = 0; k < 7; ++k)
+                if (c + k < n) reinterpret_cast<unsigned short *>(o + 4 * i * ld)[k] = (unsigned short)(u[k / 2] >> (16 * (k & 1)));
         }
     }
 }
 
-// Chunks of 32 columns of a tile that an epilogue warp finishes: `half` of the tile's columns, as far
+// Rows row0.. and columns col.. of a bf16 matrix to the box; zeros past its end.
+__device__ __forceinline__ void load_box(unsigned box, int lane, const __nv_bfloat16 *in, unsigned long long ld, unsigned row0, unsigned col,
+                                         unsigned m, unsigned n)
+{
+    const unsigned c = col + (lane & 7) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3);
+        const unsigned bytes = row0 + r >= m || c >= n ? 0 : n - c < 8 ? 2 * (n - c) : 16;
+        const __nv_bfloat16 *src = bytes ? in + (unsigned long long)(row0 + r) * ld + c : in;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(box_piece(box, r, lane & 7)), "l"(src), "r"(bytes) : "memory");
+    }
+}
+
+// 32 float32 columns of the lane's row through the box to out [+ addend].
+__device__ __forceinline__ void finish_f32(unsigned box, int lane, const float (&x)[32], const GemmProblem &p, unsigned row0, unsigned out_row0,
+                                           unsigned col)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        st_shared(box_piece(box, lane, j), __float_as_uint(x[4 * j]), __float_as_uint(x[4 * j + 1]), __float_as_uint(x[4 * j + 2]),
+                  __float_as_uint(x[4 * j + 3]));
+    __syncwarp();
+    const unsigned c = col + (lane & 7) * 4, live = c < p.n ? p.n - c : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3);
+        const uint4 w = ld_shared(box_piece(box, r, lane & 7));
+        if (row0 + r >= p.m || !live) continue;
+        float y[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)}, add[4];
+        if (p.addend) {
+            const unsigned long long at = (unsigned long long)(row0 + r) * p.ld_addend + c;
+            if (!p.addend_f32) {
+                load4(static_cast<const __nv_bfloat16 *>(p.addend) + at, add, live);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) add[k] = k < live ? static_cast<const float *>(p.addend)[at + k] : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] += add[k];
+        }
+        const unsigned long long at = (unsigned long long)(out_row0 + r) * p.ld_out + c;
+        if (!p.out_f32) {
+            store4(static_cast<__nv_bfloat16 *>(p.out) + at, y, live);
+        } else if (live >= 4) {
+            *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at) = make_float4(y[0], y[1], y[2], y[3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                if (k < live) static_cast<float *>(p.out)[at + k] = y[k];
+        }
+    }
+    __syncwarp();
+}
+
+// Chunks of WIDTH columns of a tile that an epilogue warp finishes: `half` of the tile's columns, as far
 // as the output goes; none if the warp's rows are past its end.
-template <int COLS>
+template <int COLS, int WIDTH>
 __device__ __forceinline__ unsigned chunks_of(const GemmProblem &p, const TilePos &pos, unsigned row0, unsigned half)
 {
     const unsigned col = pos.n0 + half * (COLS / 2);
     if (pos.m0 + row0 >= p.m || col >= p.n) return 0;
-    const unsigned c = (p.n - col + 31) / 32;
-    return c < COLS / 64 ? c : COLS / 64;
+    const unsigned c = (p.n - col + WIDTH - 1) / WIDTH;
+    return c < COLS / 2 / WIDTH ? c : COLS / 2 / WIDTH;
 }
 
 // BN: accumulator columns of a pair's tile.  kEpiGate puts BN / 2 columns of gate (the first CTA's
 // share of B) beside BN / 2 of up (the second's).
-template <int EPI, int BN>
+template <int EPI, int BN, int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
 {
@@ -392,11 +405,10 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
 
     extern __shared__ unsigned char smem_raw[];
     const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    __shared__ alignas(8) unsigned long long bars[2 * kStages + 5 + kEpiWarps];
+    __shared__ alignas(8) unsigned long long bars[2 * kStages + 5];
     __shared__ int abort_flag;
     __shared__ unsigned tmem_base;
-    const unsigned full = smem_addr(bars), empty = full + 8 * kStages, tfull = empty + 8 * kStages, tempty = tfull + 16, drain = tempty + 16,
-                   boxes_in = drain + 8;
+    const unsigned full = smem_addr(bars), empty = full + 8 * kStages, tfull = empty + 8 * kStages, tempty = tfull + 16, drain = tempty + 16;
     volatile int *abort = &abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
@@ -411,8 +423,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(tfull + 8 * s) : "memory");
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(tempty + 8 * s), "r"(2 * kEpiWarps) : "memory");   // both CTAs' warps
         }
-        for (int s = 0; s < 1 + kEpiWarps; ++s)        // drain, boxes_in
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(drain + 8 * s) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(drain) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -491,162 +502,133 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
     } else {
         const unsigned tempty0 = cluster_addr(tempty, 0);
         const unsigned row0 = rank * kBM + (warp & 3) * 32, half = warp >> 2;
-        // kEpiGate, kEpiBack: this warp's boxes; kEpiBack reads gate and up one chunk ahead
-        const unsigned box = smem + kStages * kStageBytes + warp * gemm_boxes(EPI) * kBoxBytes, out = box + (EPI == kEpiBack ? 2 * kBoxBytes : 0);
-        const unsigned landed = boxes_in + 8 * warp;
-        unsigned phase = 0, loads = 0, stores = 0;
-        bool was_f32 = false;
-        const auto load_chunk = [&](const TilePos &pos, unsigned c) {
-            if (lane == 0) {
-                const int x = (int)(pos.n0 + half * (kCols / 2) + 32 * c), y = (int)(pos.m0 + row0);
-                mbar_arrive_expect_tx(landed, 2 * kBoxBytes);
-                tma_load_2d(box, &a.maps[kBackGate], x, y, landed);
-                tma_load_2d(box + kBoxBytes, &a.maps[kBackUp], x, y, landed);
-            }
-            ++loads;
+        const unsigned box = smem + kStages * kStageBytes + warp * gemm_boxes(EPI) * kBoxBytes, box2 = box + kBoxBytes;
+        // kEpiBack: gate and up of a chunk, asked for before its products are complete
+        const auto load_chunk = [&](const GemmProblem &p, const TilePos &pos, unsigned c) {
+            const unsigned col = pos.n0 + half * (kCols / 2) + 64 * c;
+            load_box(box, lane, a.e.gate, a.e.ld_gate, pos.m0 + row0, col, p.m, p.n);
+            load_box(box2, lane, a.e.up, a.e.ld_gate, pos.m0 + row0, col, p.m, p.n);
         };
-        const auto load_first_from = [&](unsigned t) {         // the first chunk of the next tile that has one
-            for (; t < a.tiles; t += pairs) {
-                const TilePos pos = tile_pos<kCols>(a, t);
-                if (chunks_of<kCols>(a.prob[pos.p], pos, row0, half)) {
-                    load_chunk(pos, 0);
-                    return;
-                }
-            }
-        };
-        if (EPI == kEpiBack) load_first_from(pair);
         unsigned acc = 0;
-        bool ok = true;
-        for (unsigned t = pair; ok && t < a.tiles; t += pairs, ++acc) {
+        for (unsigned t = pair; t < a.tiles; t += pairs, ++acc) {
             const TilePos pos = tile_pos<kCols>(a, t);
             const GemmProblem &p = a.prob[pos.p];
-            const unsigned slot = acc & 1;
-            ok = __all_sync(0xffffffffu, gemm_wait(tfull + 8 * slot, (acc / 2) & 1, abort));
-            if (!ok) break;
+            const unsigned slot = acc & 1, row = pos.m0 + row0;
+            const unsigned chunks = chunks_of<kCols, 64>(p, pos, row0, half);
+            if (EPI == kEpiBack && chunks) load_chunk(p, pos, 0);
+            const bool ok = gemm_wait(tfull + 8 * slot, (acc / 2) & 1, abort);
+            if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
-            const unsigned taddr = tmem + ((unsigned)((warp & 3) * 32) << 16) + slot * BN;
-            if (EPI == kEpiStore) {
-                const unsigned chunks = chunks_of<kCols>(p, pos, row0, half), row = pos.m0 + row0 + lane;
+            const unsigned taddr = tmem + ((unsigned)((warp & 3) * 32) << 16) + slot * BN + half * (kCols / 2);
+            const unsigned col0 = pos.n0 + half * (kCols / 2);
+            if (EPI == kEpiStore && (p.out_f32 || p.addend)) {
 #pragma unroll 1
-                for (unsigned c = 0; c < chunks; ++c) {
-                    const unsigned col = half * (kCols / 2) + 32 * c;
+                for (unsigned c = 0; c < 2 * chunks; ++c) {
                     unsigned r[32];
                     float x[32];
-                    tmem_ld32(taddr + col, r);
+                    tmem_ld32(taddr + 32 * c, r);
                     tmem_ld_wait();
 #pragma unroll
                     for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
-                    if (p.accumulate) {
-                        if (row < p.m) add_columns(p, row, pos.n0 + col, x);
-                        continue;
-                    }
-                    if (p.residual && row < p.m) {
-                        float add[32];
-                        load_row32(p.residual + (unsigned long long)row * p.ld_residual + pos.n0 + col, add, p.n - pos.n0 - col);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) x[j] += add[j];
-                    }
-                    if (p.ragged && pos.n0 + col + 32 > p.n) {        // TMA stores end on 16-byte pieces
-                        if (row < p.m) store_columns(p, row, pos.n0 + col, x);
-                        continue;
-                    }
-                    unsigned to = box;
-                    if (p.out_f32) {
-                        if (lane == 0) bulk_wait_read<0>();
-                        __syncwarp();
-                        write_box_f32(to, lane, x);
-                    } else {                               // two boxes in turn; a float32 box fills both
-                        to += stores & 1 ? kBoxBytes : 0;
-                        if (lane == 0) {
-                            if (was_f32) bulk_wait_read<0>();
-                            else bulk_wait_read<1>();
-                        }
-                        __syncwarp();
-                        write_box(to, lane, x);
-                    }
-                    was_f32 = p.out_f32;
-                    ++stores;
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        tma_store_2d(&a.maps[p.out_map], (int)(pos.n0 + col), (int)(pos.split * p.split_rows + pos.m0 + row0), to);
-                        bulk_commit();
-                    }
+                    finish_f32(box, lane, x, p, row, pos.split * p.split_rows + row, col0 + 32 * c);
                 }
             } else {
-                const unsigned chunks = chunks_of<kCols>(p, pos, row0, half);
 #pragma unroll 1
                 for (unsigned c = 0; c < chunks; ++c) {
-                    const unsigned col = half * (kCols / 2) + 32 * c;
-                    unsigned r[32];
-                    float x[32], g[32], u[32];
-                    tmem_ld32(taddr + col, r);
-                    if (EPI == kEpiGate) {
-                        unsigned r2[32];
-                        tmem_ld32(taddr + BN / 2 + col, r2);
-                        tmem_ld_wait();
+                    const unsigned col = col0 + 64 * c, at = taddr + 64 * c;
+                    unsigned w[16], held[2][16];
+                    if (EPI == kEpiBack) {
+                        asm volatile("cp.async.wait_all;" ::: "memory");
+                        __syncwarp();
+                    }
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            g[j] = __uint_as_float(r[j]);
-                            u[j] = __uint_as_float(r2[j]);
-                            x[j] = activate<false>(g[j], a.e.activation, nullptr) * u[j];        // hidden
+                    for (int h = 0; h < 2; ++h) {
+                        unsigned r[32];
+                        float x[32];
+                        tmem_ld32(at + 32 * h, r);
+                        if (EPI == kEpiStore) {
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
+                            pack32(x, w);
+                            write_half(box, lane, h, w);
+                        } else if (EPI == kEpiGate) {
+                            unsigned r2[32];
+                            float u[32];
+                            tmem_ld32(at + BN / 2 + 32 * h, r2);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                x[j] = __uint_as_float(r[j]);
+                                u[j] = __uint_as_float(r2[j]);
+                            }
+                            if (a.e.gate) {
+                                pack32(x, w);
+                                write_half(box2, lane, h, w);
+                                pack32(u, held[h]);                // up
+                            }
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) x[j] = activate<ACT, false>(x[j], nullptr) * u[j];
+                            pack32(x, w);
+                            write_half(box, lane, h, w);           // hidden
+                        } else {
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {          // a lane's own pieces: gate becomes dgate, up dup
+                                const unsigned pg = box_piece(box, lane, 4 * h + j), pu = box_piece(box2, lane, 4 * h + j);
+                                const uint4 g4 = ld_shared(pg), u4 = ld_shared(pu);
+                                const unsigned gw[4] = {g4.x, g4.y, g4.z, g4.w}, uw[4] = {u4.x, u4.y, u4.z, u4.w};
+                                float dg[8], du[8], hid[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    const float g = __uint_as_float(i & 1 ? gw[i / 2] & 0xffff0000u : gw[i / 2] << 16);
+                                    const float u = __uint_as_float(i & 1 ? uw[i / 2] & 0xffff0000u : uw[i / 2] << 16);
+                                    const float dh = __uint_as_float(r[8 * j + i]);
+                                    float slope;
+                                    const float act = activate<ACT, true>(g, &slope);
+                                    dg[i] = dh * u * slope;
+                                    du[i] = dh * act;
+                                    hid[i] = act * u;
+                                }
+                                st_shared(pg, pack2(dg[0], dg[1]), pack2(dg[2], dg[3]), pack2(dg[4], dg[5]), pack2(dg[6], dg[7]));
+                                st_shared(pu, pack2(du[0], du[1]), pack2(du[2], du[3]), pack2(du[4], du[5]), pack2(du[6], du[7]));
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) held[h][4 * j + i] = pack2(hid[2 * i], hid[2 * i + 1]);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    if (EPI == kEpiStore) {
+                        store_box(box, lane, static_cast<__nv_bfloat16 *>(p.out), p.ld_out, row, col, p.m, p.n);
+                    } else if (EPI == kEpiGate) {
+                        store_box(box, lane, a.e.hidden, a.e.ld_hidden, row, col, p.m, p.n);
+                        if (a.e.gate) {
+                            store_box(box2, lane, a.e.gate, a.e.ld_gate, row, col, p.m, p.n);
+                            __syncwarp();
+                            write_half(box, lane, 0, held[0]);
+                            write_half(box, lane, 1, held[1]);
+                            __syncwarp();
+                            store_box(box, lane, a.e.up, a.e.ld_gate, row, col, p.m, p.n);
                         }
                     } else {
-                        ok = __all_sync(0xffffffffu, gemm_wait(landed, phase, abort));
-                        if (!ok) break;
-                        phase ^= 1;
-                        read_box(box, lane, g);
-                        read_box(box + kBoxBytes, lane, u);
+                        store_box(box, lane, a.e.dgate, a.e.ld_hidden, row, col, p.m, p.n);
+                        store_box(box2, lane, a.e.dup, a.e.ld_hidden, row, col, p.m, p.n);
                         __syncwarp();
-                        if (c + 1 < chunks) load_chunk(pos, c + 1);
-                        else load_first_from(t + pairs);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float dh = __uint_as_float(r[j]);
-                            float slope;
-                            const float act = activate<true>(g[j], a.e.activation, &slope);
-                            x[j] = act * u[j];                     // hidden
-                            g[j] = dh * u[j] * slope;              // dgate
-                            u[j] = dh * act;                       // dup
-                        }
+                        write_half(box, lane, 0, held[0]);
+                        write_half(box, lane, 1, held[1]);
+                        __syncwarp();
+                        store_box(box, lane, a.e.hidden, a.e.ld_hidden, row, col, p.m, p.n);
+                        __syncwarp();
+                        if (c + 1 < chunks) load_chunk(p, pos, c + 1);
                     }
-                    if (lane == 0) bulk_wait_read<0>();               // the boxes of the chunk before
                     __syncwarp();
-                    // TMA stores end on 16-byte pieces; a row of the caller's that does not is stored from registers
-                    // (what kEpiBack writes lies in scratch with whole pieces)
-                    const bool ragged = EPI == kEpiGate && (p.n & 7) && pos.n0 + col + 32 > p.n;
-                    const bool all = EPI == kEpiBack || (a.e.gate && !ragged);
-                    write_box(out, lane, x);
-                    if (all) {
-                        write_box(out + kBoxBytes, lane, g);
-                        write_box(out + 2 * kBoxBytes, lane, u);
-                    }
-                    if (ragged && a.e.gate && pos.m0 + row0 + lane < p.m) {
-                        const unsigned long long at = (unsigned long long)(pos.m0 + row0 + lane) * a.e.ld_gate + pos.n0 + col;
-                        store_row32(a.e.gate + at, g, p.n - pos.n0 - col);
-                        store_row32(a.e.up + at, u, p.n - pos.n0 - col);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        const int cx = (int)(pos.n0 + col), cy = (int)(pos.m0 + row0);
-                        tma_store_2d(&a.maps[kOutHidden], cx, cy, out);
-                        if (all) {
-                            tma_store_2d(&a.maps[kOutGate], cx, cy, out + kBoxBytes);
-                            tma_store_2d(&a.maps[kOutUp], cx, cy, out + 2 * kBoxBytes);
-                        }
-                        bulk_commit();
-                    }
                 }
-                if (!ok) break;
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * slot);
         }
-        if (lane == 0) bulk_wait();
-        if (EPI == kEpiBack && !ok && loads) mbar_wait_bounded(landed, (loads - 1) & 1);     // a copy may be in flight
+        if (EPI == kEpiBack) asm volatile("cp.async.wait_all;" ::: "memory");
     }
     __syncwarp();
     tc_fence_before();

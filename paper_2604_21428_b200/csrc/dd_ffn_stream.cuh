@@ -47,34 +47,8 @@ __device__ __forceinline__ void tmem_ld16(unsigned addr, unsigned (&r)[16])
                  : "r"(addr));
 }
 
-// Up to four consecutive bf16, `live` of them inside the row.
-__device__ __forceinline__ void store4(__nv_bfloat16 *p, const float (&x)[4], unsigned live)
-{
-    if (live >= 4) {
-        *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (i < live) p[i] = __float2bfloat16_rn(x[i]);
-    }
-}
-
-__device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&x)[4], unsigned live)
-{
-    if (live >= 4) {
-        const uint2 w = *reinterpret_cast<const uint2 *>(p);
-        x[0] = __uint_as_float(w.x << 16);
-        x[1] = __uint_as_float(w.x & 0xffff0000u);
-        x[2] = __uint_as_float(w.y << 16);
-        x[3] = __uint_as_float(w.y & 0xffff0000u);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = i < live ? __bfloat162float(p[i]) : 0.0f;
-    }
-}
-
 // Four features from c on of token t, from their finished sums (kEpiGate: x gate, u up).
-template <int EPI>
+template <int EPI, int ACT>
 __device__ __forceinline__ void finish4(const EpilogueArgs &a, unsigned t, unsigned c, unsigned live,
                                         float (&x)[4], float (&u)[4])
 {
@@ -85,7 +59,7 @@ __device__ __forceinline__ void finish4(const EpilogueArgs &a, unsigned t, unsig
             store4(a.up + at, u, live);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = activate<false>(x[i], a.activation, nullptr) * u[i];
+        for (int i = 0; i < 4; ++i) x[i] = activate<ACT, false>(x[i], nullptr) * u[i];
         store4(a.hidden + to, x, live);
     } else if (EPI == kEpiBack) {
         float g[4];
@@ -95,7 +69,7 @@ __device__ __forceinline__ void finish4(const EpilogueArgs &a, unsigned t, unsig
         for (int i = 0; i < 4; ++i) {
             const float dh = x[i];
             float slope;
-            const float act = activate<true>(g[i], a.activation, &slope);
+            const float act = activate<ACT, true>(g[i], &slope);
             x[i] = dh * act;
             g[i] = dh * u[i] * slope;
             u[i] = act * u[i];
@@ -127,7 +101,7 @@ struct StreamArgs {
 };
 
 // blockIdx.x = tile * cluster + rank.
-template <int EPI, int N>
+template <int EPI, int N, int ACT>
 __global__ void __launch_bounds__(kStreamThreads, 2)
 ffn_stream_kernel(const __grid_constant__ StreamArgs p)
 {
@@ -278,7 +252,7 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
                         x[0] += vx[r].x; x[1] += vx[r].y; x[2] += vx[r].z; x[3] += vx[r].w;
                         if (EPI == kEpiGate) { u[0] += vu[r].x; u[1] += vu[r].y; u[2] += vu[r].z; u[3] += vu[r].w; }
                     }
-                finish4<EPI>(p.e, t, feature, live, x, u);
+                finish4<EPI, ACT>(p.e, t, feature, live, x, u);
             }
         }
     }
