@@ -93,9 +93,6 @@ constexpr unsigned long long kStreamMaxTokens = 128;
 // Ring of a CTA: two CTAs share an SM.
 constexpr unsigned kStreamRing = 96 * 1024;
 
-static int stream_cols(unsigned long long tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128; }
-static unsigned stream_box(unsigned long long tokens) { return stream_cols(tokens) < 64 ? (unsigned)stream_cols(tokens) : 64; }
-
 // Kernels opt in to their shared memory once per process and device.
 template <typename K>
 static int allow_smem(dd_ctx *ctx, K kernel, size_t bytes, bool (&done)[64])
@@ -171,52 +168,59 @@ static int launch_reduce(dd_ctx *ctx, const GemmProblem &p, const Matrix &out, c
     return DD_OK;
 }
 
-template <int EPI, int N, int ACT>
-static int launch_stream_act(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
+template <int EPI, int ACT>
+static int launch_stream_act(dd_ctx *ctx, const StreamArgs &a, unsigned grid, cudaStream_t stream)
 {
-    a.tiles_n = blocks_of(a.n, N);
-    const unsigned tiles = blocks_of(a.m, stream_features(EPI)) * a.tiles_n, blocks = a.kblocks[0] + a.kblocks[1];
-    // One CTA per SM at least, as long as each rank keeps two K blocks
-    unsigned s = 1;
-    while (s < kStreamMaxCluster && tiles * s < (unsigned)ctx->sm_count && blocks >= 4 * s) s *= 2;
-    unsigned stages = kStreamRing / stream_stage_bytes(N);
-    a.cluster = (int)s;
-    a.stages = (int)(stages > kStreamMaxStages ? kStreamMaxStages : stages);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles * s);
+    cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(kStreamThreads);
-    cfg.dynamicSmemBytes = stream_smem_bytes(N, a.stages);
+    cfg.dynamicSmemBytes = stream_smem_bytes(a.cols, a.stages);
     cfg.stream = stream;
     static bool done[64];
-    const int rc = allow_smem(ctx, ffn_stream_kernel<EPI, N, ACT>, cfg.dynamicSmemBytes, done);
+    const int rc = allow_smem(ctx, ffn_stream_kernel<EPI, ACT>, kStreamRing + 2048, done);
     if (rc != DD_OK) return rc;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim = {s, 1, 1};
+    at[0].val.clusterDim = {(unsigned)a.cluster, 1, 1};
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_stream_kernel<EPI, N, ACT>, a));
+    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_stream_kernel<EPI, ACT>, a));
     return DD_OK;
 }
 
-template <int EPI, int N>
-static int launch_stream_n(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
-{
-    return EPI != kEpiStore && a.e.activation == DD_ACT_GELU_TANH ? launch_stream_act<EPI, N, EPI == kEpiStore ? DD_ACT_SILU : DD_ACT_GELU_TANH>(ctx, a, stream)
-                                                                  : launch_stream_act<EPI, N, DD_ACT_SILU>(ctx, a, stream);
-}
-
+// Shape and launch: the tokens in equal tiles of at most 128, K over as many CTAs as give every SM
+// one, each with two K blocks at least; x: the token matrices of the K segments.
 template <int EPI>
-static int launch_stream(dd_ctx *ctx, StreamArgs &a, cudaStream_t stream)
+static int launch_stream(dd_ctx *ctx, StreamArgs &a, std::initializer_list<Matrix> x, cudaStream_t stream)
 {
-    switch (stream_cols(a.n)) {
-    case 16: return launch_stream_n<EPI, 16>(ctx, a, stream);
-    case 32: return launch_stream_n<EPI, 32>(ctx, a, stream);
-    case 64: return launch_stream_n<EPI, 64>(ctx, a, stream);
-    default: return launch_stream_n<EPI, 128>(ctx, a, stream);
+    const unsigned rows = blocks_of(a.m, stream_features(EPI)), blocks = a.kblocks[0] + a.kblocks[1], sms = (unsigned)ctx->sm_count;
+    a.tiles_n = blocks_of(a.n, kStreamMaxCols);
+    const auto cluster = [&] {
+        unsigned s = 1;
+        while (s < kStreamMaxCluster && rows * a.tiles_n * s < sms && blocks >= 4 * s) s *= 2;
+        return s;
+    };
+    unsigned s = cluster();
+    while (rows * a.tiles_n * s < sms && a.n / a.tiles_n >= 64) {
+        a.tiles_n *= 2;
+        s = cluster();
     }
+    a.cols = blocks_of(blocks_of(a.n, a.tiles_n), 16) * 16;
+    a.tiles_n = blocks_of(a.n, a.cols);
+    a.cluster = (int)s;
+    const unsigned stages = kStreamRing / stream_stage_bytes(a.cols);
+    a.stages = (int)(stages > kStreamMaxStages ? kStreamMaxStages : stages);
+    int i = 0;
+    for (const Matrix &m : x) {
+        const int rc = encode(ctx, &a.x[i++], m, a.cols);
+        if (rc != DD_OK) return rc;
+    }
+    const unsigned grid = rows * a.tiles_n * s;
+    return EPI != kEpiStore && a.e.activation == DD_ACT_GELU_TANH
+               ? launch_stream_act<EPI, EPI == kEpiStore ? DD_ACT_SILU : DD_ACT_GELU_TANH>(ctx, a, grid, stream)
+               : launch_stream_act<EPI, DD_ACT_SILU>(ctx, a, grid, stream);
 }
 
 static StreamArgs stream_args(const EpilogueArgs &e, uint64_t features, uint64_t tokens)
@@ -365,15 +369,13 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
         a.kblocks[0] = blocks_of(b.d, kBK);
         rc = encode(ctx, &a.w[0], mg);
         if (rc == DD_OK) rc = encode(ctx, &a.w[1], mu);
-        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mx, stream_box(T));
-        if (rc == DD_OK) rc = launch_stream<kEpiGate>(ctx, a, stream);
+        if (rc == DD_OK) rc = launch_stream<kEpiGate>(ctx, a, {mx}, stream);
         if (rc != DD_OK) return rc;
         a.m = (unsigned)b.d;
         a.kblocks[0] = blocks_of(b.f, kBK);
         a.own_prior = 1;
         rc = encode(ctx, &a.w[0], md);
-        if (rc == DD_OK) rc = encode(ctx, &a.x[0], mh, stream_box(T));
-        return rc == DD_OK ? launch_stream<kEpiStore>(ctx, a, stream) : rc;
+        return rc == DD_OK ? launch_stream<kEpiStore>(ctx, a, {mh}, stream) : rc;
     }
     GemmArgs a;
     std::memset(&a, 0, sizeof a);
@@ -471,17 +473,14 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         c.kblocks[0] = blocks_of(b.d, kBK);
         c.w[0] = a.maps[kWd];
         c.w_mn = 1;
-        rc = encode(ctx, &c.x[0], mats[kDy], stream_box(T));
-        if (rc == DD_OK) rc = launch_stream<kEpiBack>(ctx, c, stream);
+        rc = launch_stream<kEpiBack>(ctx, c, {mats[kDy]}, stream);
         if (rc != DD_OK) return rc;
         c.m = (unsigned)b.d;                              // dgate w_gate + dup w_up
         c.kblocks[0] = c.kblocks[1] = blocks_of(b.f, kBK);
         c.w[0] = a.maps[kWg];
         c.w[1] = a.maps[kWu];
-        c.own_prior = 1;
-        rc = encode(ctx, &c.x[0], mats[kDg], stream_box(T));
-        if (rc == DD_OK) rc = encode(ctx, &c.x[1], mats[kDu], stream_box(T));
-        if (rc == DD_OK) rc = launch_stream<kEpiStore>(ctx, c, stream);
+        c.own_prior = c.late_trigger = a.late_wait = 1;
+        rc = launch_stream<kEpiStore>(ctx, c, {mats[kDg], mats[kDu]}, stream);
         if (rc != DD_OK) return rc;
     } else {
         GemmArgs c = a;

@@ -65,6 +65,9 @@ struct GemmArgs {
     GemmProblem prob[kMaxProblems];
     int nprob;
     unsigned tiles;
+    // 1: nothing here depends on the launch before, which itself began after all that does; this launch runs beside
+    // it and only ends after it
+    int late_wait;
     EpilogueArgs e;                   // kEpiStore: the problems have their own outputs
 };
 
@@ -243,16 +246,21 @@ __device__ __forceinline__ TilePos tile_pos(const GemmArgs &a, unsigned t)
     while (t >= a.prob[r.p].tile_end) ++r.p;
     const GemmProblem &p = a.prob[r.p];
     t -= r.p ? a.prob[r.p - 1].tile_end : 0u;
-    r.split = t % p.splits;
-    t /= p.splits;
+    const unsigned blocks = p.kblocks[0] + p.kblocks[1];
+    r.split = 0;
+    r.kb0 = 0;
+    r.kb1 = blocks;
+    if (p.splits > 1) {
+        r.split = t % p.splits;
+        t /= p.splits;
+        r.kb0 = blocks * r.split / p.splits;
+        r.kb1 = blocks * (r.split + 1) / p.splits;
+    }
     const unsigned group = kTileGroup * p.tiles_n, g = t / group, first = kTileGroup * g;
     const unsigned rows = p.tiles_m - first < kTileGroup ? p.tiles_m - first : kTileGroup;
     t -= g * group;
     r.m0 = (first + t % rows) * 2 * kBM;
     r.n0 = (t / rows) * COLS;
-    const unsigned long long blocks = p.kblocks[0] + p.kblocks[1];
-    r.kb0 = (unsigned)(blocks * r.split / p.splits);
-    r.kb1 = (unsigned)(blocks * (r.split + 1) / p.splits);
     return r;
 }
 
@@ -438,7 +446,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
     tc_fence_after();
     const unsigned tmem = tmem_base;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!a.late_wait) asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if (warp == kProducer) {
         if (elect_one()) {
@@ -532,6 +540,30 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                     for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
                     finish_f32(box, lane, x, p, row, pos.split * p.split_rows + row, col0 + 32 * c);
                 }
+            } else if (EPI == kEpiStore) {
+                unsigned r[2][32];
+                if (chunks) {
+                    tmem_ld32(taddr, r[0]);
+                    tmem_ld32(taddr + 32, r[1]);
+                }
+#pragma unroll 1
+                for (unsigned c = 0; c < chunks; ++c) {
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        unsigned w[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) w[j] = pack2(__uint_as_float(r[h][2 * j]), __uint_as_float(r[h][2 * j + 1]));
+                        write_half(box, lane, h, w);
+                    }
+                    __syncwarp();
+                    if (c + 1 < chunks) {                          // on their way while this chunk is stored
+                        tmem_ld32(taddr + 64 * (c + 1), r[0]);
+                        tmem_ld32(taddr + 64 * (c + 1) + 32, r[1]);
+                    }
+                    store_box(box, lane, static_cast<__nv_bfloat16 *>(p.out), p.ld_out, row, col0 + 64 * c, p.m, p.n);
+                    __syncwarp();
+                }
             } else {
 #pragma unroll 1
                 for (unsigned c = 0; c < chunks; ++c) {
@@ -546,13 +578,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                         unsigned r[32];
                         float x[32];
                         tmem_ld32(at + 32 * h, r);
-                        if (EPI == kEpiStore) {
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
-                            pack32(x, w);
-                            write_half(box, lane, h, w);
-                        } else if (EPI == kEpiGate) {
+                        if (EPI == kEpiGate) {
                             unsigned r2[32];
                             float u[32];
                             tmem_ld32(at + BN / 2 + 32 * h, r2);
@@ -598,9 +624,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                         }
                     }
                     __syncwarp();
-                    if (EPI == kEpiStore) {
-                        store_box(box, lane, static_cast<__nv_bfloat16 *>(p.out), p.ld_out, row, col, p.m, p.n);
-                    } else if (EPI == kEpiGate) {
+                    if (EPI == kEpiGate) {
                         store_box(box, lane, a.e.hidden, a.e.ld_hidden, row, col, p.m, p.n);
                         if (a.e.gate) {
                             store_box(box2, lane, a.e.gate, a.e.ld_gate, row, col, p.m, p.n);
@@ -637,6 +661,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
     if (warp == kIssuer)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
     if (threadIdx.x == 0 && abort_flag && a.e.status) *a.e.status = DD_STATUS_WAIT_LIMIT;
+    if (a.late_wait) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // out = bf16([residual +] sum of the splits' float32 slabs in split order), eight columns a thread.

@@ -15,20 +15,21 @@
 
 namespace ddm {
 
-constexpr int kRound = 64;                        // tokens reduced per round
+constexpr unsigned kRound = 64;                   // tokens reduced per round
 constexpr int kStreamThreads = 192;
-constexpr int kStreamMaxStages = 8, kStreamMaxCluster = 8;
+constexpr unsigned kStreamMaxStages = 8, kStreamMaxCluster = 8, kStreamMaxCols = 128;
 
 __host__ __device__ constexpr int stream_features(int epi) { return epi == kEpiGate ? kBM / 2 : kBM; }
-__host__ __device__ constexpr unsigned stream_stage_bytes(int n) { return (unsigned)(kBM + n) * kBK * 2; }
-__host__ __device__ constexpr unsigned stream_round_bytes(int n) { return (unsigned)(n < kRound ? n : kRound) * kBM * 4; }
+// n: tokens of a tile, a multiple of 16
+__host__ __device__ constexpr unsigned stream_stage_bytes(unsigned n) { return (kBM + n) * kBK * 2; }
+__host__ __device__ constexpr unsigned stream_round_bytes(unsigned n) { return (n < kRound ? n : kRound) * kBM * 4; }
 // The reduction reuses the ring: one buffer per round, at most two.
-__host__ __device__ constexpr unsigned stream_ring_bytes(int n, int stages)
+__host__ __device__ constexpr unsigned stream_ring_bytes(unsigned n, unsigned stages)
 {
     const unsigned ring = stages * stream_stage_bytes(n), rounds = (n > kRound ? 2 : 1) * stream_round_bytes(n);
     return ring > rounds ? ring : rounds;
 }
-__host__ __device__ constexpr unsigned stream_smem_bytes(int n, int stages) { return 1024 + stream_ring_bytes(n, stages) + 256; }
+__host__ __device__ constexpr unsigned stream_smem_bytes(unsigned n, unsigned stages) { return 1024 + stream_ring_bytes(n, stages); }
 
 // Four floats at `addr` (a shared-memory address of this CTA) in the CTA of rank `rank`.
 __device__ __forceinline__ float4 ld_cluster4(unsigned addr, unsigned rank)
@@ -47,10 +48,47 @@ __device__ __forceinline__ void tmem_ld16(unsigned addr, unsigned (&r)[16])
                  : "r"(addr));
 }
 
+// What an epilogue reads for four features of a token, asked for before the sums are ready.
+struct Aux {
+    uint2 a, b;                       // kEpiBack: gate, up; kEpiStore: residual
+};
+
+__device__ __forceinline__ uint2 load4_raw(const __nv_bfloat16 *p, unsigned live)
+{
+    if (live >= 4) return *reinterpret_cast<const uint2 *>(p);
+    const unsigned short *q = reinterpret_cast<const unsigned short *>(p);
+    uint2 w = make_uint2(q[0], 0u);
+    if (live > 1) w.x |= (unsigned)q[1] << 16;
+    if (live > 2) w.y = q[2];
+    return w;
+}
+
+__device__ __forceinline__ void unpack4(const uint2 &w, float (&x)[4])
+{
+    x[0] = __uint_as_float(w.x << 16);
+    x[1] = __uint_as_float(w.x & 0xffff0000u);
+    x[2] = __uint_as_float(w.y << 16);
+    x[3] = __uint_as_float(w.y & 0xffff0000u);
+}
+
+template <int EPI>
+__device__ __forceinline__ Aux load_aux(const EpilogueArgs &a, unsigned t, unsigned c, unsigned live)
+{
+    Aux r;
+    r.a = r.b = make_uint2(0u, 0u);
+    if (EPI == kEpiBack) {
+        r.a = load4_raw(a.gate + (unsigned long long)t * a.ld_gate + c, live);
+        r.b = load4_raw(a.up + (unsigned long long)t * a.ld_gate + c, live);
+    } else if (EPI == kEpiStore && a.residual) {
+        r.a = load4_raw(a.residual + (unsigned long long)t * a.ld_residual + c, live);
+    }
+    return r;
+}
+
 // Four features from c on of token t, from their finished sums (kEpiGate: x gate, u up).
 template <int EPI, int ACT>
-__device__ __forceinline__ void finish4(const EpilogueArgs &a, unsigned t, unsigned c, unsigned live,
-                                        float (&x)[4], float (&u)[4])
+__device__ __forceinline__ void finish4(const EpilogueArgs &a, unsigned t, unsigned c, unsigned live, const Aux &aux, float (&x)[4],
+                                        float (&u)[4])
 {
     const unsigned long long at = (unsigned long long)t * a.ld_gate + c, to = (unsigned long long)t * a.ld_hidden + c;
     if (EPI == kEpiGate) {
@@ -63,8 +101,8 @@ __device__ __forceinline__ void finish4(const EpilogueArgs &a, unsigned t, unsig
         store4(a.hidden + to, x, live);
     } else if (EPI == kEpiBack) {
         float g[4];
-        load4(a.gate + at, g, live);
-        load4(a.up + at, u, live);
+        unpack4(aux.a, g);
+        unpack4(aux.b, u);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float dh = x[i];
@@ -78,11 +116,10 @@ __device__ __forceinline__ void finish4(const EpilogueArgs &a, unsigned t, unsig
         store4(a.dgate + to, g, live);
         store4(a.hidden + to, u, live);
     } else {
-        if (a.residual) {
-            load4(a.residual + (unsigned long long)t * a.ld_residual + c, u, live);
+        float r[4];
+        unpack4(aux.a, r);                // zeros without a residual
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] += u[i];
-        }
+        for (int i = 0; i < 4; ++i) x[i] += r[i];
         store4(a.out + (unsigned long long)t * a.ld_out + c, x, live);
     }
 }
@@ -90,25 +127,23 @@ __device__ __forceinline__ void finish4(const EpilogueArgs &a, unsigned t, unsig
 // One launch.  Kept small: 1.5 KB more of parameters cost the host 0.7 us a launch.
 struct StreamArgs {
     CUtensorMap w[2];                 // weights: kEpiGate gate and up, else the K segments
-    CUtensorMap x[2];                 // token matrices of the K segments, boxes of min(N, 64) rows
+    CUtensorMap x[2];                 // token matrices of the K segments, boxes of `cols` rows
     unsigned m, n;                    // features (rows of the output's transpose), tokens
-    unsigned tiles_n;
+    unsigned tiles_n, cols;           // tiles along the tokens, tokens of a tile (a multiple of 16)
     unsigned kblocks[2];              // K blocks of the segments
     int w_mn;                         // 1: the features are the contiguous direction of the weights
     int cluster, stages;              // CTAs per tile, ring stages
     int own_prior;                    // the launch before is this call's own: the weights are not its results
+    int late_trigger;                 // with own_prior: the next launch may start once that one has ended
     EpilogueArgs e;
 };
 
 // blockIdx.x = tile * cluster + rank.
-template <int EPI, int N, int ACT>
+template <int EPI, int ACT>
 __global__ void __launch_bounds__(kStreamThreads, 2)
 ffn_stream_kernel(const __grid_constant__ StreamArgs p)
 {
-    constexpr unsigned kStageBytes = stream_stage_bytes(N), kABytes = kBM * kBK * 2;
-    constexpr unsigned kTmemCols = N < 32 ? 32 : N;
-    constexpr int kBRows = N < 64 ? N : 64;
-    constexpr int kCols = N < kRound ? N : kRound;          // tokens per round
+    constexpr unsigned kABytes = kBM * kBK * 2;
     constexpr int kFeatures = stream_features(EPI), kQuads = kFeatures / 4, kTokensAtOnce = 128 / kQuads;
 
     extern __shared__ unsigned char smem_raw[];
@@ -119,7 +154,8 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
     const unsigned full = smem_addr(bars), empty = full + 8 * kStreamMaxStages, done = empty + 8 * kStreamMaxStages;
     volatile int *abort = &abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const unsigned S = p.cluster, stages = p.stages;
+    const unsigned S = p.cluster, stages = p.stages, N = p.cols, stage_bytes = stream_stage_bytes(N);
+    const unsigned tmem_cols = N <= 32 ? 32 : N <= 64 ? 64 : 128;
     const unsigned rank = blockIdx.x % S, tile = blockIdx.x / S;
     const unsigned m0 = tile / p.tiles_n * kFeatures, n0 = tile % p.tiles_n * N;   // tiles of the same weights are neighbours
     const unsigned blocks = p.kblocks[0] + p.kblocks[1];
@@ -138,14 +174,14 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
     }
     if (warp == 5) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     :: "r"(smem_addr(&tmem_base)), "r"(kTmemCols) : "memory");
+                     :: "r"(smem_addr(&tmem_base)), "r"(tmem_cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const unsigned tmem = tmem_base;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (!p.late_trigger) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (!p.own_prior) asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if (warp == 4) {
@@ -156,18 +192,16 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
                 for (int c = 0; c < 2; ++c) {
                     const CUtensorMap *m = &p.w[EPI == kEpiGate ? c : seg];
                     const int row = (int)m0 + (EPI == kEpiGate ? 0 : 64 * c);
-                    tma_load_2d(smem + s * kStageBytes + c * kChunkBytes, m, p.w_mn ? row : k0, p.w_mn ? k0 : row, full + 8 * s);
+                    tma_load_2d(smem + s * stage_bytes + c * kChunkBytes, m, p.w_mn ? row : k0, p.w_mn ? k0 : row, full + 8 * s);
                 }
             };
             const auto tokens = [&](unsigned kb, unsigned s) {
                 const int seg = kb >= p.kblocks[0], k0 = (int)(kb - (seg ? p.kblocks[0] : 0u)) * kBK;
-#pragma unroll
-                for (int c = 0; c < N / kBRows; ++c)
-                    tma_load_2d(smem + s * kStageBytes + kABytes + c * kChunkBytes, &p.x[seg], k0, (int)n0 + 64 * c, full + 8 * s);
+                tma_load_2d(smem + s * stage_bytes + kABytes, &p.x[seg], k0, (int)n0, full + 8 * s);
             };
             const unsigned first = count < stages ? count : stages;
             for (unsigned i = 0; i < first; ++i) {
-                mbar_arrive_expect_tx(full + 8 * i, kStageBytes);
+                mbar_arrive_expect_tx(full + 8 * i, stage_bytes);
                 weights(kb0 + i, i);
             }
             if (p.own_prior) asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -175,7 +209,7 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
             unsigned it = first, s = 0, phase = 0;          // stage of copy `it`, parity of its previous use
             for (; it < count; ++it) {
                 if (!gemm_wait(empty + 8 * s, phase, abort) || *abort) break;
-                mbar_arrive_expect_tx(full + 8 * s, kStageBytes);
+                mbar_arrive_expect_tx(full + 8 * s, stage_bytes);
                 weights(kb0 + it, s);
                 tokens(kb0 + it, s);
                 if (++s == stages) { s = 0; phase ^= 1; }
@@ -187,12 +221,12 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
     } else if (warp == 5) {
         if (elect_one()) {
             const unsigned idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((unsigned)p.w_mn << 15) |
-                                   ((unsigned)(N / 8) << 17) | ((kBM / 16) << 24);
+                                   ((N / 8) << 17) | ((kBM / 16) << 24);
             const unsigned astep = p.w_mn ? 2048 : 32;
             for (unsigned it = 0, s = 0, phase = 0; it < count; ++it) {
                 if (!gemm_wait(full + 8 * s, phase, abort)) break;
                 tc_fence_after();
-                const unsigned sa = smem + s * kStageBytes, sb = sa + kABytes;
+                const unsigned sa = smem + s * stage_bytes, sb = sa + kABytes;
 #pragma unroll
                 for (int k = 0; k < kBK / 16; ++k)
                     umma_bf16(tmem, umma_desc(sa + k * astep, p.w_mn), umma_desc(sb + k * 32, false), idesc, it | k);
@@ -204,6 +238,7 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
         }
     } else if (p.own_prior) {
         asm volatile("griddepcontrol.wait;" ::: "memory");      // the epilogue may read what the prior launch wrote
+        if (p.late_trigger) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     }
     __syncwarp();
     tc_fence_before();
@@ -212,47 +247,63 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
 
     // This rank's sums to shared memory as [token][128 rows], a round of up to 64 tokens at a time;
     // then every rank adds up, over the ranks in order, the tokens that it owns.
-    const unsigned owned = (kCols + S - 1) / S;
+    const unsigned f4 = threadIdx.x % kQuads * 4, feature = m0 + f4, live = feature < p.m ? p.m - feature : 0;
 #pragma unroll 1
-    for (int c = 0, round = 0; c < N; c += kCols, ++round) {
-        const unsigned buf = smem + (round & 1) * stream_round_bytes(N);
+    for (unsigned c = 0, round = 0; c < N; c += kRound, ++round) {
+        const unsigned buf = smem + (round & 1) * stream_round_bytes(N), cols = N - c < kRound ? N - c : kRound;
+        const unsigned owned = (cols + S - 1) / S, last = (rank + 1) * owned < cols ? (rank + 1) * owned : cols;
+        const unsigned left = p.n > n0 + c ? p.n - n0 - c : 0, end = last < left ? last : left;      // tokens that exist
+        unsigned j = rank * owned + threadIdx.x / kQuads;
+        const bool mine = warp < 4 && live;
+        Aux aux[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            if (mine && j + b * kTokensAtOnce < end) aux[b] = load_aux<EPI>(p.e, n0 + c + j + b * kTokensAtOnce, feature, live);
         if (warp < 4) {
             const unsigned col = tmem + ((unsigned)(warp * 32) << 16) + c, to = buf + threadIdx.x * 4;
-#pragma unroll
-            for (int h = 0; h < kCols; h += 16) {
+#pragma unroll 1
+            for (unsigned h = 0; h < cols; h += 16) {
                 unsigned r[16];
                 tmem_ld16(col + h, r);
                 tmem_ld_wait();
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    asm volatile("st.shared.b32 [%0], %1;" :: "r"(to + (h + j) * kBM * 4), "r"(r[j]) : "memory");
+                for (int i = 0; i < 16; ++i)
+                    asm volatile("st.shared.b32 [%0], %1;" :: "r"(to + (h + i) * kBM * 4), "r"(r[i]) : "memory");
             }
         }
         if (S > 1) cluster_sync();
         else __syncthreads();
-        const unsigned f4 = threadIdx.x % kQuads * 4, feature = m0 + f4;
-        if (warp < 4 && feature < p.m) {
-            const unsigned live = p.m - feature;
-            const unsigned end = (rank + 1) * owned < kCols ? (rank + 1) * owned : kCols;
-            for (unsigned j = rank * owned + threadIdx.x / kQuads; j < end; j += kTokensAtOnce) {
-                const unsigned t = n0 + c + j;
-                if (t >= p.n) break;
-                float4 vx[kStreamMaxCluster], vu[kStreamMaxCluster];
+        // two tokens at a time: the reads from all ranks are on their way together (one at a time, with what the
+        // epilogue reads asked for in between, a round of 64 tokens took 7 us)
+        for (; mine && j < end; j += 2 * kTokensAtOnce) {
+            float4 vx[2][kStreamMaxCluster], vu[2][EPI == kEpiGate ? kStreamMaxCluster : 1];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int r = 0; r < kStreamMaxCluster; ++r)
-                    if (r < S) {
-                        vx[r] = ld_cluster4(buf + (j * kBM + f4) * 4, r);
-                        if (EPI == kEpiGate) vu[r] = ld_cluster4(buf + (j * kBM + kFeatures + f4) * 4, r);
+                    if (r < S && j + b * kTokensAtOnce < end) {
+                        const unsigned from = buf + ((j + b * kTokensAtOnce) * kBM + f4) * 4;
+                        vx[b][r] = ld_cluster4(from, r);
+                        if (EPI == kEpiGate) vu[b][r] = ld_cluster4(from + kFeatures * 4, r);
                     }
-                float x[4] = {vx[0].x, vx[0].y, vx[0].z, vx[0].w}, u[4];
-                if (EPI == kEpiGate) { u[0] = vu[0].x; u[1] = vu[0].y; u[2] = vu[0].z; u[3] = vu[0].w; }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const unsigned k = j + b * kTokensAtOnce;
+                if (k >= end) break;
+                const Aux now = aux[b];
+                if (k + 2 * kTokensAtOnce < end) aux[b] = load_aux<EPI>(p.e, n0 + c + k + 2 * kTokensAtOnce, feature, live);
+                float x[4] = {vx[b][0].x, vx[b][0].y, vx[b][0].z, vx[b][0].w}, u[4];
+                if (EPI == kEpiGate) { u[0] = vu[b][0].x; u[1] = vu[b][0].y; u[2] = vu[b][0].z; u[3] = vu[b][0].w; }
 #pragma unroll
                 for (int r = 1; r < kStreamMaxCluster; ++r)
                     if (r < S) {
-                        x[0] += vx[r].x; x[1] += vx[r].y; x[2] += vx[r].z; x[3] += vx[r].w;
-                        if (EPI == kEpiGate) { u[0] += vu[r].x; u[1] += vu[r].y; u[2] += vu[r].z; u[3] += vu[r].w; }
+                        x[0] += vx[b][r].x; x[1] += vx[b][r].y; x[2] += vx[b][r].z; x[3] += vx[b][r].w;
+                        if (EPI == kEpiGate) {
+                            const float4 v = vu[b][EPI == kEpiGate ? r : 0];
+                            u[0] += v.x; u[1] += v.y; u[2] += v.z; u[3] += v.w;
+                        }
                     }
-                finish4<EPI, ACT>(p.e, t, feature, live, x, u);
+                finish4<EPI, ACT>(p.e, n0 + c + k, feature, live, now, x, u);
             }
         }
     }
@@ -261,7 +312,7 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
     __syncthreads();
     tc_fence_after();
     if (warp == 5)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(tmem_cols) : "memory");
     if (threadIdx.x == 0 && abort_flag && p.e.status) *p.e.status = DD_STATUS_WAIT_LIMIT;
 }
 
