@@ -87,8 +87,10 @@ static unsigned choose_splits(const dd_ctx *ctx, unsigned tiles, unsigned blocks
 
 // ---- few tokens ----------------------------------------------------------------------------
 
-// Up to here the weight-streaming kernel is ahead of the 128 x 256 tiles.
-constexpr unsigned long long kStreamMaxTokens = 128;
+// Up to here the weight-streaming kernel is ahead of the 256-row tiles of the pairs, forward with gate and up kept / backward:
+// 160 tokens, d 2048, f 8192 37 / 84 us (42 / 92), 300 tokens, 1024 x 4096 28 / 48 us (30 / 50); behind at 384 tokens, 2048 x 8192:
+// 66 / 120 us (64 / 116).
+constexpr unsigned long long kStreamMaxTokens = 320;
 
 // Ring of a CTA: two CTAs share an SM.
 constexpr unsigned kStreamRing = 96 * 1024;

@@ -19,6 +19,7 @@ constexpr int kListSmall = 32, kListMax = 256;
 // 156 / 150 us, AdamW on 151M with bf16 gradients and copies 698 / 673 us (6.29 TB/s).
 constexpr int kListCtasPerSm = 8;
 constexpr unsigned char kNoVector = 255;
+constexpr unsigned kKeepBytes = 64u << 20;   // of a list that is read twice, kept in L2 (126 MB) from the first time
 
 // One launch's tensors, by value in the kernel parameters: no staging copy, and nothing for a
 // stream capture to keep alive.  CAP = 32 keeps the parameters of short lists under 2 KB.
@@ -40,6 +41,7 @@ struct NormTail {
     dd_grad_record *record;
     float max_norm;
     int last;                                // the call's last launch reduces
+    unsigned keep_from;                      // AGAIN: first tile to keep in L2
 };
 
 struct AdamwConsts {
@@ -130,16 +132,33 @@ __device__ __forceinline__ float squares(const uint4 &w)
 
 __device__ __forceinline__ float squares(const float4 &w) { return fmaf(w.x, w.x, fmaf(w.y, w.y, fmaf(w.z, w.z, w.w * w.w))); }
 
+__device__ __forceinline__ uint4 load_policy(const uint4 *p, unsigned long long policy)
+{
+    uint4 w;
+    asm volatile("ld.global.L2::cache_hint.v4.b32 {%0, %1, %2, %3}, [%4], %5;"
+                 : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "l"(p), "l"(policy) : "memory");
+    return w;
+}
+
+__device__ __forceinline__ float4 load_policy(const float4 *p, unsigned long long policy)
+{
+    float4 w;
+    asm volatile("ld.global.L2::cache_hint.v4.f32 {%0, %1, %2, %3}, [%4], %5;"
+                 : "=f"(w.x), "=f"(w.y), "=f"(w.z), "=f"(w.w) : "l"(p), "l"(policy) : "memory");
+    return w;
+}
+
 // Sum of squares of this thread's part of a tile: V holds E elements.
-template <typename V, int E>
-__device__ __forceinline__ float tile_squares(const V *p, unsigned pieces)
+template <typename V, int E, bool AGAIN>
+__device__ __forceinline__ float tile_squares(const V *p, unsigned pieces, unsigned long long policy)
 {
     constexpr int kSteps = kListTile / (E * kListThreads);
     float s = 0.0f;
     V w[kSteps];
     if (pieces == kSteps * kListThreads) {
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) w[k] = p[threadIdx.x + k * kListThreads];
+        for (int k = 0; k < kSteps; ++k)
+            w[k] = AGAIN ? load_policy(p + threadIdx.x + k * kListThreads, policy) : p[threadIdx.x + k * kListThreads];
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) s += squares(w[k]);
     } else {
@@ -151,7 +170,10 @@ __device__ __forceinline__ float tile_squares(const V *p, unsigned pieces)
 // sum of g^2: fp32 over the 32 elements a thread takes of a tile (and 8 more at a tensor's ends),
 // fp64 across tiles, threads and CTAs.  The CTA that draws the last ticket adds the partials in
 // index order, so the result does not depend on which one that is.
-template <int CAP>
+// AGAIN: the clip reads everything once more, from the end.  The last 64 MB are then kept in L2 and
+// the rest is marked to go first: 156 -> 148 us for 151M bf16, 294 -> 284 us for 151M fp32 (without
+// the marks, reading from the end gains nothing).
+template <int CAP, bool AGAIN>
 __global__ void __launch_bounds__(kListThreads)
 grad_norm_kernel(const __grid_constant__ ListArgs<1, CAP> a, const __grid_constant__ NormTail t)
 {
@@ -159,6 +181,11 @@ grad_norm_kernel(const __grid_constant__ ListArgs<1, CAP> a, const __grid_consta
     __shared__ unsigned drawn;
     double acc = 0.0;
     int i = 0;
+    unsigned long long keep = 0, drop = 0;
+    if (AGAIN) {
+        asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
+        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(drop));
+    }
     after_prior_launch();
     for (unsigned tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
         i = find_tensor(a, tile, i, a.count - 1);
@@ -166,9 +193,10 @@ grad_norm_kernel(const __grid_constant__ ListArgs<1, CAP> a, const __grid_consta
         const void *g = a.ptr[0][i];
         const bool bf16 = a.bf16[i];
         const unsigned cnt = (unsigned)(sp.end - sp.begin), per = bf16 ? 8 : 4, pieces = sp.vec ? cnt / per : 0;
+        const unsigned long long policy = tile >= t.keep_from ? keep : drop;
         float s = 0.0f;
-        if (bf16) s = tile_squares<uint4, 8>(reinterpret_cast<const uint4 *>(static_cast<const unsigned short *>(g) + sp.begin), pieces);
-        else s = tile_squares<float4, 4>(reinterpret_cast<const float4 *>(static_cast<const float *>(g) + sp.begin), pieces);
+        if (bf16) s = tile_squares<uint4, 8, AGAIN>(reinterpret_cast<const uint4 *>(static_cast<const unsigned short *>(g) + sp.begin), pieces, policy);
+        else s = tile_squares<float4, 4, AGAIN>(reinterpret_cast<const float4 *>(static_cast<const float *>(g) + sp.begin), pieces, policy);
         for (unsigned e = pieces * per + threadIdx.x; e < cnt; e += kListThreads) {
             const float x = load_elem(g, bf16, sp.begin + e);
             s = fmaf(x, x, s);
@@ -226,7 +254,7 @@ __device__ __forceinline__ void tile_scale(const V *p, V *q, unsigned pieces, fl
     }
 }
 
-// out = scale * g, last tiles first: what the norm read last is what L2 still holds.
+// out = scale * g, last tiles first: those the norm kept in L2.
 template <int CAP>
 __global__ void __launch_bounds__(kListThreads)
 grad_scale_kernel(const __grid_constant__ ListArgs<2, CAP> a, const dd_grad_record *record, int in_place)
@@ -399,9 +427,10 @@ static int launch_list(dd_ctx *ctx, void (*kernel)(P...), unsigned grid, cudaStr
     return DD_OK;
 }
 
+// again: the tensors are read once more by a launch that starts from their end.
 template <int CAP>
 static int launch_norm(dd_ctx *ctx, const void *const *grads, const uint64_t *sizes, const uint8_t *dtypes,
-                       int count, float max_norm, dd_grad_record *record, cudaStream_t stream)
+                       int count, float max_norm, dd_grad_record *record, bool again, cudaStream_t stream)
 {
     const size_t launches = count > CAP ? (size_t)(count + CAP - 1) / CAP : 1;
     int rc = ensure_workspace(ctx, 1, 1, launches * ctx->sm_count * kListCtasPerSm);
@@ -412,6 +441,7 @@ static int launch_norm(dd_ctx *ctx, const void *const *grads, const uint64_t *si
     t.record = record;
     t.max_norm = max_norm;
     t.first = 0;
+    t.keep_from = 0;
     int at = 0;
     do {
         ListArgs<1, CAP> a;
@@ -423,7 +453,18 @@ static int launch_norm(dd_ctx *ctx, const void *const *grads, const uint64_t *si
         const unsigned grid = list_grid(ctx, a.tiles);
         t.last = at >= count;
         t.total = t.first + grid;
-        rc = launch_list(ctx, grad_norm_kernel<CAP>, grid, stream, a, t);
+        if (again) {
+            unsigned long long bytes = 0;                  // from the end of this launch's tensors
+            t.keep_from = a.tiles;
+            for (int k = a.count - 1; k >= 0 && bytes < kKeepBytes && t.last; --k) {
+                const unsigned tile_bytes = kListTile * (a.bf16[k] ? 2 : 4), first = k ? a.tile_end[k - 1] : 0u;
+                const unsigned long long room = (kKeepBytes - bytes + tile_bytes - 1) / tile_bytes, n = a.tile_end[k] - first;
+                t.keep_from -= (unsigned)(n < room ? n : room);
+                bytes += n * tile_bytes;
+            }
+        }
+        rc = again ? launch_list(ctx, grad_norm_kernel<CAP, true>, grid, stream, a, t)
+                   : launch_list(ctx, grad_norm_kernel<CAP, false>, grid, stream, a, t);
         if (rc != DD_OK) return rc;
         t.first += grid;
     } while (at < count);
@@ -497,8 +538,8 @@ extern "C" int dd_grad_norm(dd_ctx *ctx, const void *const *grads, const uint64_
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return cuda_fail(ctx, cudaErrorInvalidDevice, "cudaSetDevice");
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    return count <= kListSmall ? launch_norm<kListSmall>(ctx, grads, sizes, dtypes, count, max_norm, record, stream)
-                               : launch_norm<kListMax>(ctx, grads, sizes, dtypes, count, max_norm, record, stream);
+    return count <= kListSmall ? launch_norm<kListSmall>(ctx, grads, sizes, dtypes, count, max_norm, record, false, stream)
+                               : launch_norm<kListMax>(ctx, grads, sizes, dtypes, count, max_norm, record, false, stream);
 }
 
 extern "C" int dd_clip_gradients(dd_ctx *ctx, void *const *grads, void *const *outs, const uint64_t *sizes,
@@ -517,8 +558,8 @@ extern "C" int dd_clip_gradients(dd_ctx *ctx, void *const *grads, void *const *o
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return cuda_fail(ctx, cudaErrorInvalidDevice, "cudaSetDevice");
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    rc = count <= kListSmall ? launch_norm<kListSmall>(ctx, grads, sizes, dtypes, count, max_norm, record, stream)
-                             : launch_norm<kListMax>(ctx, grads, sizes, dtypes, count, max_norm, record, stream);
+    rc = count <= kListSmall ? launch_norm<kListSmall>(ctx, grads, sizes, dtypes, count, max_norm, record, true, stream)
+                             : launch_norm<kListMax>(ctx, grads, sizes, dtypes, count, max_norm, record, true, stream);
     if (rc != DD_OK) return rc;
     return count <= kListSmall ? launch_scale<kListSmall>(ctx, grads, outs, sizes, dtypes, count, record, stream)
                                : launch_scale<kListMax>(ctx, grads, outs, sizes, dtypes, count, record, stream);
