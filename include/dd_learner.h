@@ -123,7 +123,9 @@ typedef struct {
     uint64_t ld_down;       /* w_down and its gradient: d rows of f */
     const void *w_gate, *w_up, *w_down;     /* [device] bf16 */
     int32_t activation;                     /* dd_activation */
-    int32_t reserved;
+    uint32_t flags;                         /* 0; DD_DEBUG_EXPIRE_WAIT (test hook, as in dd_merge.h): the first
+                                             * copies are made to wait for bytes that never come, so the call's
+                                             * bounded waits expire, `status` says so and the context stays usable */
 } dd_gated_ffn;
 
 /*

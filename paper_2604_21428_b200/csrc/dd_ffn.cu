@@ -287,6 +287,7 @@ static int check_block(const dd_ctx *ctx, dd_gated_ffn &b, bool with_gate)
 {
     if (!ctx || b.d < 1 || b.f < 1) return DD_ERR_INVALID_ARG;
     if (b.activation != DD_ACT_SILU && b.activation != DD_ACT_GELU_TANH) return DD_ERR_INVALID_ARG;
+    if (b.flags & ~(uint32_t)DD_DEBUG_EXPIRE_WAIT) return DD_ERR_INVALID_ARG;
     if (b.tokens >= kFfnMax || b.d >= kFfnMax || b.f >= kFfnMax) return DD_ERR_TOO_LARGE;
     struct { uint64_t *ld; uint64_t cols; } strides[] = {{&b.ld_x, b.d}, {&b.ld_y, b.d}, {&b.ld_gate, b.f}, {&b.ld_in, b.d}, {&b.ld_down, b.f}};
     for (auto &s : strides) {
@@ -355,6 +356,7 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
     EpilogueArgs e;
     std::memset(&e, 0, sizeof e);
     e.activation = b.activation;
+    e.expire = b.flags != 0;
     e.status = status;
     e.gate = (__nv_bfloat16 *)gate;
     e.up = (__nv_bfloat16 *)up;
@@ -459,6 +461,7 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
     }
     EpilogueArgs &e = a.e;
     e.activation = b.activation;
+    e.expire = b.flags != 0;
     e.status = status;
     e.gate = (__nv_bfloat16 *)const_cast<void *>(gate);
     e.up = (__nv_bfloat16 *)const_cast<void *>(up);

@@ -43,6 +43,7 @@ struct EpilogueArgs {
     unsigned long long ld_gate, ld_hidden, ld_out, ld_residual;
     int *status;
     int activation;
+    int expire;                       // test hook: the first stage waits for 16 bytes that no copy brings
 };
 
 struct GemmProblem {
@@ -462,7 +463,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                     const int seg = kb >= p.kblocks[0], k0 = (int)(kb - (seg ? p.kblocks[0] : 0u)) * kBK;
                     const CUtensorMap *ma = &a.maps[p.a_map[seg]], *mb = &a.maps[p.b_map[EPI == kEpiGate ? rank : seg]];
                     const unsigned st = smem + s * kStageBytes, bar = full0 + 8 * s;
-                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, 2 * kStageBytes);
+                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, 2 * kStageBytes + (a.e.expire && it == 0 ? 16u : 0u));
 #pragma unroll
                     for (int c = 0; c < kBM / 64; ++c)
                         tma_load_2d_pair(st + c * kChunkBytes, ma, p.a_mn ? m0 + 64 * c : k0, p.a_mn ? k0 : m0 + 64 * c, bar);

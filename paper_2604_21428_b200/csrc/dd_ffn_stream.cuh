@@ -201,7 +201,7 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
             };
             const unsigned first = count < stages ? count : stages;
             for (unsigned i = 0; i < first; ++i) {
-                mbar_arrive_expect_tx(full + 8 * i, stage_bytes);
+                mbar_arrive_expect_tx(full + 8 * i, stage_bytes + (p.e.expire && i == 0 ? 16u : 0u));
                 weights(kb0 + i, i);
             }
             if (p.own_prior) asm volatile("griddepcontrol.wait;" ::: "memory");

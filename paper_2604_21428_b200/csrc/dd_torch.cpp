@@ -156,7 +156,7 @@ void *matrix(PyObject *o, const char *name, uint64_t rows, uint64_t cols, uint64
 }
 
 // (x, w_gate, w_up, w_down) -> block and x
-const void *block_of(PyObject *const *a, PyObject *act, dd_gated_ffn &b)
+const void *block_of(PyObject *const *a, PyObject *act, PyObject *flags, dd_gated_ffn &b)
 {
     const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "w_gate");
     if (x.dim() != 2 || w.dim() != 2) refuse("x and the weights are matrices");
@@ -165,6 +165,7 @@ const void *block_of(PyObject *const *a, PyObject *act, dd_gated_ffn &b)
     b.d = x.size(1);
     b.f = w.size(0);
     b.activation = (int32_t)PyLong_AsLong(act);
+    b.flags = (uint32_t)PyLong_AsUnsignedLong(flags);
     const void *px = matrix(a[0], "x", b.tokens, b.d, b.ld_x);
     b.w_gate = matrix(a[1], "w_gate", b.f, b.d, b.ld_in);
     b.w_up = matrix(a[2], "w_up", b.f, b.d, b.ld_in);
@@ -174,22 +175,22 @@ const void *block_of(PyObject *const *a, PyObject *act, dd_gated_ffn &b)
 
 size_t hidden_bytes(const dd_gated_ffn &b) { return (size_t)b.tokens * ((b.f + 7) / 8 * 8) * 2; }
 
-// (ctx, x, w_gate, w_up, w_down, y, residual, gate, up, activation, hidden, status, stream)
+// (ctx, x, w_gate, w_up, w_down, y, residual, gate, up, activation, hidden, status, stream, flags)
 int gated_ffn_forward(PyObject *const *a)
 {
     dd_gated_ffn b;
-    const void *x = block_of(a + 1, a[9], b);
+    const void *x = block_of(a + 1, a[9], a[13], b);
     void *y = matrix(a[5], "y", b.tokens, b.d, b.ld_y), *res = matrix(a[6], "residual", b.tokens, b.d, b.ld_y);
     void *gate = matrix(a[7], "gate", b.tokens, b.f, b.ld_gate), *up = matrix(a[8], "up", b.tokens, b.f, b.ld_gate);
     return dd_gated_ffn_forward((dd_ctx *)PyLong_AsVoidPtr(a[0]), &b, x, res, gate, up, address(a[10], "hidden", hidden_bytes(b)), y,
                                 (int32_t *)address(a[11], "status", 4), PyLong_AsVoidPtr(a[12]));
 }
 
-// (ctx, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up, dw_down, activation, accumulate, scratch, status, stream)
+// (ctx, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up, dw_down, activation, accumulate, scratch, status, stream, flags)
 int gated_ffn_backward(PyObject *const *a)
 {
     dd_gated_ffn b;
-    const void *x = block_of(a + 1, a[12], b);
+    const void *x = block_of(a + 1, a[12], a[17], b);
     const void *gate = matrix(a[5], "gate", b.tokens, b.f, b.ld_gate), *up = matrix(a[6], "up", b.tokens, b.f, b.ld_gate);
     const void *dy = matrix(a[7], "dy", b.tokens, b.d, b.ld_y);
     void *dx = matrix(a[8], "dx", b.tokens, b.d, b.ld_x);
@@ -220,8 +221,8 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 }
 
 #define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {ENTRY(grad_norm, 5), ENTRY(clip_gradients, 6), ENTRY(adamw_step, 14), ENTRY(gated_ffn_forward, 13),
-                         ENTRY(gated_ffn_backward, 17), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {ENTRY(grad_norm, 5), ENTRY(clip_gradients, 6), ENTRY(adamw_step, 14), ENTRY(gated_ffn_forward, 14),
+                         ENTRY(gated_ffn_backward, 18), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ddtorch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -589,23 +589,23 @@ class Context:
             self._check(rc)
 
     def gated_ffn_forward(self, x, w_gate, w_up, w_down, y, *, activation: int = ACT_SILU, residual=None,
-                          gate=None, up=None, hidden=None, status=None, stream=None) -> None:
+                          gate=None, up=None, hidden=None, status=None, flags: int = 0, stream=None) -> None:
         """``dd_gated_ffn_forward``: y = [residual +] (a(x w_gate^T) * (x w_up^T)) w_down^T.  bfloat16
         matrices with contiguous rows: ``x``, ``residual``, ``y`` [tokens, d], ``w_gate``, ``w_up`` [f, d],
         ``w_down`` [d, f]; ``gate`` and ``up`` [tokens, f] are kept for the backward pass when given."""
         rc = _native().gated_ffn_forward(self._h.value, x, w_gate, w_up, w_down, y, residual, gate, up, activation,
-                                         hidden, status, _raw_stream(stream))
+                                         hidden, status, _raw_stream(stream), flags)
         if rc != OK:
             self._check(rc)
 
     def gated_ffn_backward(self, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up, dw_down, *,
                            activation: int = ACT_SILU, accumulate: bool = False, scratch=None, status=None,
-                           stream=None) -> None:
+                           flags: int = 0, stream=None) -> None:
         """``dd_gated_ffn_backward``: gradients of the block for ``dy`` [tokens, d], given the ``gate`` and
         ``up`` that the forward call kept.  ``dw_gate``, ``dw_up``, ``dw_down`` are all bfloat16 or all
         float32 and have the row strides of the weights."""
         rc = _native().gated_ffn_backward(self._h.value, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up,
-                                          dw_down, activation, accumulate, scratch, status, _raw_stream(stream))
+                                          dw_down, activation, accumulate, scratch, status, _raw_stream(stream), flags)
         if rc != OK:
             self._check(rc)
 

@@ -295,3 +295,27 @@ def test_refusals(dd, ctx):
                  lambda: ctx.gated_ffn_backward(x, *w, gate, up, y, mat(T, d, 11), grads[0].float(), *grads[1:])):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("tokens", [5, 400])
+def test_bounded_waits_expire(dd, ctx, tokens):
+    """The test hook holds back the first copies: the waits run out, the status word says so, and
+    the next call on the same context is right."""
+    d, f = 136, 264
+    x, w = mat(tokens, d, 1), [mat(f, d, 2, 0.1), mat(f, d, 3, 0.1), mat(d, f, 4, 0.1)]
+    y, gate, up = mat(tokens, d, 5), mat(tokens, f, 6), mat(tokens, f, 7)
+    outs = [mat(tokens, d, 8), mat(f, d, 9), mat(f, d, 10), mat(d, f, 11)]
+    status = torch.zeros(2, dtype=torch.int32, device="cuda")
+    ctx.gated_ffn_forward(x, *w, y, gate=gate, up=up, status=status[:1], flags=dd.DEBUG_EXPIRE_WAIT)
+    ctx.gated_ffn_backward(x, *w, mat(tokens, f, 6), mat(tokens, f, 7), mat(tokens, d, 12), *outs, status=status[1:],
+                           flags=dd.DEBUG_EXPIRE_WAIT)
+    torch.cuda.synchronize()
+    assert status.tolist() == [dd.STATUS_WAIT_LIMIT] * 2
+    status.zero_()
+    ctx.gated_ffn_forward(x, *w, y, gate=gate, up=up, status=status[:1])
+    for got, (ref, tol) in zip((y, gate, up), forward64(x, *w, None, 0)):
+        within(got, ref, tol, "after the expiry")
+    ctx.gated_ffn_backward(x, *w, gate, up, mat(tokens, d, 12), *outs, status=status[1:])
+    for got, (ref, tol) in zip(outs, backward64(x, *w, gate, up, mat(tokens, d, 12), 0)):
+        within(got, ref, tol * (1 + UB) + UB * ref.abs(), "after the expiry")
+    assert status.tolist() == [0, 0]
