@@ -31,6 +31,8 @@ constexpr int kChunkBytes = 64 * 128;             // one TMA box: 64 rows of 64 
 constexpr int kMaxMaps = 8, kMaxProblems = 4;
 constexpr unsigned kTileGroup = 8;
 constexpr int kMaxSplits = 8;
+constexpr unsigned kSpinLimit = 1u << 30;
+constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr int kBoxBytes = 32 * 128;               // an epilogue box: 32 rows of 64 bf16 or 32 float32
 
 enum GemmEpilogue { kEpiStore = 0, kEpiGate = 1, kEpiBack = 2 };
@@ -138,14 +140,24 @@ __device__ __forceinline__ unsigned cluster_addr(unsigned addr, unsigned rank)
     return r;
 }
 
+// Relaxed: what it reports is that tensor memory has been read into registers, which the wait on
+// those loads has ensured.  A release would hold the warp until its stores to global memory are
+// acknowledged: 2-5k cycles a tile.
 __device__ __forceinline__ void mbar_arrive_cluster(unsigned bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// The same without ordering memory, for the end of a kernel: a release would wait for the results to be
+// acknowledged, which the end of the launch does anyway.
+__device__ __forceinline__ void cluster_sync_relaxed()
+{
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
 }
 
 __device__ __forceinline__ void tmem_ld32(unsigned addr, unsigned (&r)[32])
@@ -265,11 +277,23 @@ __device__ __forceinline__ TilePos tile_pos(const GemmArgs &a, unsigned t)
     return r;
 }
 
+// Bounded wait of a pipeline role.  No suspend hint: with one (4 us) a role woke up to 3 us after its
+// phase had completed.  The limit is on time, a second, looked at every 256 attempts.
 __device__ __forceinline__ bool gemm_wait(unsigned bar, unsigned parity, volatile int *abort)
 {
-    for (int spins = 0; spins < kWaitLimit; ++spins) {
-        if (mbar_try_wait(bar, parity)) return true;
+    unsigned long long start = 0;
+    for (unsigned spins = 0; spins < kSpinLimit; ++spins) {
+        unsigned ok;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
         if (*abort) return false;
+        if ((spins & 255) == 255) {
+            unsigned long long now;
+            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+            if (!start) start = now;
+            else if (now - start > kWaitNs) break;
+        }
     }
     *abort = 1;
     return false;
@@ -530,6 +554,12 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             tc_fence_after();
             const unsigned taddr = tmem + ((unsigned)((warp & 3) * 32) << 16) + slot * BN + half * (kCols / 2);
             const unsigned col0 = pos.n0 + half * (kCols / 2);
+            const auto release = [&] {                             // this warp has read its part of the accumulator
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * slot);
+            };
+            if (!chunks) release();
             if (EPI == kEpiStore && (p.out_f32 || p.addend)) {
 #pragma unroll 1
                 for (unsigned c = 0; c < 2 * chunks; ++c) {
@@ -539,6 +569,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                     tmem_ld_wait();
 #pragma unroll
                     for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
+                    if (c + 1 == 2 * chunks) release();
                     finish_f32(box, lane, x, p, row, pos.split * p.split_rows + row, col0 + 32 * c);
                 }
             } else if (EPI == kEpiStore) {
@@ -550,6 +581,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
 #pragma unroll 1
                 for (unsigned c = 0; c < chunks; ++c) {
                     tmem_ld_wait();
+                    if (c + 1 == chunks) release();
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         unsigned w[16];
@@ -584,6 +616,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                             float u[32];
                             tmem_ld32(at + BN / 2 + 32 * h, r2);
                             tmem_ld_wait();
+                            if (h == 1 && c + 1 == chunks) release();
 #pragma unroll
                             for (int j = 0; j < 32; ++j) {
                                 x[j] = __uint_as_float(r[j]);
@@ -600,6 +633,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                             write_half(box, lane, h, w);           // hidden
                         } else {
                             tmem_ld_wait();
+                            if (h == 1 && c + 1 == chunks) release();
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {          // a lane's own pieces: gate becomes dgate, up dup
                                 const unsigned pg = box_piece(box, lane, 4 * h + j), pu = box_piece(box2, lane, 4 * h + j);
@@ -649,15 +683,12 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                     __syncwarp();
                 }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * slot);
         }
         if (EPI == kEpiBack) asm volatile("cp.async.wait_all;" ::: "memory");
     }
     __syncwarp();
     tc_fence_before();
-    cluster_sync();                       // both CTAs are done with each other's shared and tensor memory
+    cluster_sync_relaxed();               // both CTAs are done with each other's shared and tensor memory
     tc_fence_after();
     if (warp == kIssuer)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");

@@ -307,7 +307,7 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
             }
         }
     }
-    if (S > 1) cluster_sync();            // nobody leaves while its sums may still be read
+    if (S > 1) cluster_sync_relaxed();    // nobody leaves while its sums may still be read
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
