@@ -74,15 +74,29 @@ static GemmProblem &add_problem(GemmArgs &a, unsigned long long m, unsigned long
 // Float32 slabs of split products: 256 KB for each of two tiles per pair of SMs.
 static size_t slab_bytes(const dd_ctx *ctx) { return (size_t)ctx->sm_count * (2 * kBM) * 256 * 4; }
 
-// Splits of a problem of `tiles` tiles with `blocks` K blocks each, so that a unit is no longer than
-// half of what each pair has to do when it shares the launch with `other` K blocks of other tiles.
+// Splits of a launch's first problem: `tiles` tiles of `blocks` K blocks, beside `other` K blocks of
+// further problems.  Alone, the number that makes the fewest waves of the shortest units (a unit's
+// epilogue counts as 10 blocks, the launch that adds the splits up as 8); with others to fill the
+// gaps, the smallest one whose units are no longer than what each pair has to do anyway.
 static unsigned choose_splits(const dd_ctx *ctx, unsigned tiles, unsigned blocks, unsigned long long other)
 {
     const unsigned pairs = (unsigned)ctx->sm_count / 2;
     const unsigned long long share = ((unsigned long long)tiles * blocks + other) / pairs + 1;
-    unsigned s = 1;
-    while (s < kMaxSplits && blocks / s > (other ? share / 2 : share) && tiles * (s + 1) <= 2 * pairs && blocks >= 4 * (s + 1)) ++s;
-    return s;
+    unsigned best = 1;
+    unsigned long long least = ~0ull;
+    for (unsigned s = 1; s <= kMaxSplits && (s == 1 || (tiles * s <= 2 * pairs && blocks >= 4 * s)); ++s) {
+        if (other) {
+            best = s;
+            if (blocks / s <= share) break;
+            continue;
+        }
+        const unsigned long long cost = (unsigned long long)blocks_of(tiles * s, pairs) * (blocks_of(blocks, s) + 10) + (s > 1 ? 8 : 0);
+        if (cost < least) {
+            least = cost;
+            best = s;
+        }
+    }
+    return best;
 }
 
 // ---- few tokens ----------------------------------------------------------------------------
@@ -107,15 +121,25 @@ static int allow_smem(dd_ctx *ctx, K kernel, size_t bytes, bool (&done)[64])
 }
 
 template <int EPI, int BN, int ACT>
-static int launch_gemm_act(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
+static int launch_gemm_act(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
 {
     constexpr size_t smem = gemm_smem_bytes(EPI, BN);
     static bool done[64];
     const int rc = allow_smem(ctx, ffn_gemm_kernel<EPI, BN, ACT>, smem, done);
     if (rc != DD_OK) return rc;
-    const unsigned pairs = (unsigned)ctx->sm_count / 2;
+    const unsigned most = (unsigned)ctx->sm_count / 2, pairs = a.tiles < most ? a.tiles : most;
+    const GemmProblem &p = a.prob[0];
+    a.first = p.tile_end;
+    a.rest = a.first % pairs;
+    a.extra = 0;
+    if (a.rest && a.nprob > 1) {
+        const unsigned one = (p.kblocks[0] + p.kblocks[1]) / p.splits, next = a.prob[1].kblocks[0] + a.prob[1].kblocks[1];
+        a.extra = (one + next / 2) / next;
+        const unsigned room = (a.tiles - a.first) / (pairs - a.rest);
+        if (a.extra > room) a.extra = room;
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * (a.tiles < pairs ? a.tiles : pairs));
+    cfg.gridDim = dim3(2 * pairs);
     cfg.blockDim = dim3(kGemmThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
@@ -129,7 +153,7 @@ static int launch_gemm_act(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
 }
 
 template <int EPI, int BN>
-static int launch_gemm(dd_ctx *ctx, const GemmArgs &a, cudaStream_t stream)
+static int launch_gemm(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
 {
     return EPI != kEpiStore && a.e.activation == DD_ACT_GELU_TANH ? launch_gemm_act<EPI, BN, EPI == kEpiStore ? DD_ACT_SILU : DD_ACT_GELU_TANH>(ctx, a, stream)
                                                                   : launch_gemm_act<EPI, BN, DD_ACT_SILU>(ctx, a, stream);

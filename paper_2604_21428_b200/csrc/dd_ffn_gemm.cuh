@@ -67,7 +67,8 @@ struct GemmArgs {
     CUtensorMap maps[kMaxMaps];       // 64 x 64 boxes of row-major bf16 matrices
     GemmProblem prob[kMaxProblems];
     int nprob;
-    unsigned tiles;
+    unsigned tiles;                   // units of all problems
+    unsigned first, rest, extra;      // schedule: see unit_of
     // 1: nothing here depends on the launch before, which itself began after all that does; this launch runs beside
     // it and only ends after it
     int late_wait;
@@ -248,6 +249,19 @@ struct TilePos {
     unsigned split;
     unsigned kb0, kb1;        // K blocks, counted over both segments
 };
+
+// The it-th unit of a pair; a.tiles or more: none.  Units of the first problem go round the pairs and
+// may be longer than the others: the `rest` pairs that got one more of them leave the other pairs
+// `extra` units of the following problems to begin with, then those go round all pairs.
+__device__ __forceinline__ unsigned unit_of(const GemmArgs &a, unsigned pair, unsigned pairs, unsigned it)
+{
+    const bool long_pair = pair < a.rest;
+    const unsigned mine = (a.first - a.rest) / pairs + (long_pair ? 1 : 0);
+    if (it < mine) return it * pairs + pair;
+    const unsigned j = it - mine, early = a.extra * (pairs - a.rest);
+    if (long_pair) return a.first + early + j * pairs + pair;
+    return a.first + (j < a.extra ? j * (pairs - a.rest) + pair - a.rest : early + (j - a.extra) * pairs + pair);
+}
 
 // Neighbouring tiles (what the GPU holds at one time) cover a block of 8 tile rows, so that both
 // operands of a wave stay in L2.
@@ -478,7 +492,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             const unsigned full0 = cluster_addr(full, 0);      // the first CTA's barriers count both CTAs' bytes
             unsigned it = 0, s = 0, phase = 1;                 // copies so far, stage, parity of its previous use
             bool ok = true;
-            for (unsigned t = pair; ok && t < a.tiles; t += pairs) {
+            for (unsigned u = 0, t; ok && (t = unit_of(a, pair, pairs, u)) < a.tiles; ++u) {
                 const TilePos pos = tile_pos<kCols>(a, t);
                 const GemmProblem &p = a.prob[pos.p];
                 const int m0 = (int)(pos.m0 + rank * kBM), n0 = (int)(pos.n0 + (EPI == kEpiGate ? 0 : rank * (BN / 2)));
@@ -506,7 +520,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
         if (rank == 0 && elect_one()) {
             unsigned acc = 0, s = 0, phase = 0;                // tiles started, stage, its parity
             bool ok = true;
-            for (unsigned t = pair; ok && t < a.tiles; t += pairs, ++acc) {
+            for (unsigned t; ok && (t = unit_of(a, pair, pairs, acc)) < a.tiles; ++acc) {
                 const TilePos pos = tile_pos<kCols>(a, t);
                 const GemmProblem &p = a.prob[pos.p];
                 const unsigned slot = acc & 1;
@@ -543,7 +557,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             load_box(box2, lane, a.e.up, a.e.ld_gate, pos.m0 + row0, col, p.m, p.n);
         };
         unsigned acc = 0;
-        for (unsigned t = pair; t < a.tiles; t += pairs, ++acc) {
+        for (unsigned t; (t = unit_of(a, pair, pairs, acc)) < a.tiles; ++acc) {
             const TilePos pos = tile_pos<kCols>(a, t);
             const GemmProblem &p = a.prob[pos.p];
             const unsigned slot = acc & 1, row = pos.m0 + row0;
