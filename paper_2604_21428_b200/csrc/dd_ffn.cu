@@ -133,7 +133,8 @@ static int launch_gemm_act(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
     a.rest = a.first % pairs;
     a.extra = 0;
     if (a.rest && a.nprob > 1) {
-        const unsigned one = (p.kblocks[0] + p.kblocks[1]) / p.splits, next = a.prob[1].kblocks[0] + a.prob[1].kblocks[1];
+        const GemmProblem &q = a.prob[1];
+        const unsigned one = (p.kblocks[0] + p.kblocks[1]) / p.splits, next = blocks_of(q.kblocks[0] + q.kblocks[1], q.splits);
         a.extra = (one + next / 2) / next;
         const unsigned room = (a.tiles - a.first) / (pairs - a.rest);
         if (a.extra > room) a.extra = room;
@@ -159,27 +160,44 @@ static int launch_gemm(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
                                                                   : launch_gemm_act<EPI, BN, DD_ACT_SILU>(ctx, a, stream);
 }
 
-// Output of problem `p`: the matrix itself, or its splits' slabs.
-static void set_output(const dd_ctx *ctx, GemmProblem &p, const Matrix &out, const void *residual, uint64_t ld_residual)
+// Slabs handed out so far, and what becomes of them.
+struct Splits {
+    size_t used = 0;                  // floats
+    ReduceArgs r;
+};
+
+// Output of problem `p`, out (ld_out) [+ addend]: directly, or by way of its splits' slabs.
+static void set_output(const dd_ctx *ctx, GemmProblem &p, Splits &sp, void *out, uint64_t ld_out, bool f32, const void *addend,
+                       uint64_t ld_addend, bool addend_f32)
 {
-    if (p.splits > 1) {
-        p.out_f32 = 1;
-        p.out = ctx->ffn_slabs;
-        p.ld_out = (out.cols + 7) / 8 * 8;
+    if (p.splits == 1) {
+        p.out = out;
+        p.ld_out = ld_out;
+        p.out_f32 = f32;
+        p.addend = addend;
+        p.ld_addend = ld_addend;
+        p.addend_f32 = addend_f32;
         return;
     }
-    p.out = const_cast<void *>(out.data);
-    p.ld_out = out.ld;
-    p.addend = residual;
-    p.ld_addend = ld_residual;
+    const unsigned ld = (p.n + 7) / 8 * 8;
+    p.out = ctx->ffn_slabs + sp.used;
+    p.ld_out = ld;
+    p.out_f32 = 1;
+    const unsigned long long slab = (unsigned long long)p.split_rows * ld;
+    ReduceJob &j = sp.r.job[sp.r.count];
+    const unsigned long long before = sp.r.count ? sp.r.job[sp.r.count - 1].end : 0;
+    j = {ctx->ffn_slabs + sp.used, p.splits, p.m, p.n, ld, slab, before + (unsigned long long)p.m * (ld / 8), out, addend, ld_out, ld_addend,
+         f32, addend_f32};
+    ++sp.r.count;
+    sp.used += p.splits * slab;
 }
 
-static int launch_reduce(dd_ctx *ctx, const GemmProblem &p, const Matrix &out, const void *residual, uint64_t ld_residual, cudaStream_t stream)
+static int launch_reduce(dd_ctx *ctx, const Splits &sp, cudaStream_t stream)
 {
-    const unsigned ld = (unsigned)((out.cols + 7) / 8 * 8);
-    const unsigned long long pieces = (unsigned long long)p.m * (ld / 8), most = (unsigned long long)ctx->sm_count * 8;
+    if (!sp.r.count) return DD_OK;
+    const unsigned long long blocks = (sp.r.job[sp.r.count - 1].end + 255) / 256, most = (unsigned long long)ctx->sm_count * 8;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((pieces + 255) / 256 < most ? (pieces + 255) / 256 : most));
+    cfg.gridDim = dim3((unsigned)(blocks < most ? blocks : most));
     cfg.blockDim = dim3(256);
     cfg.stream = stream;
     cudaLaunchAttribute at;
@@ -187,10 +205,7 @@ static int launch_reduce(dd_ctx *ctx, const GemmProblem &p, const Matrix &out, c
     at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_reduce_kernel, (const float *)ctx->ffn_slabs, p.splits,
-                                    (unsigned long long)p.split_rows * ld, ld, p.m, p.n, (const __nv_bfloat16 *)residual,
-                                    (unsigned long long)ld_residual, (__nv_bfloat16 *)const_cast<void *>(out.data),
-                                    (unsigned long long)out.ld));
+    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_reduce_kernel, sp.r));
     return DD_OK;
 }
 
@@ -426,9 +441,11 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
     q.b_map[0] = 1;
     rc = encode(ctx, &a.maps[0], mh);
     if (rc == DD_OK) rc = encode(ctx, &a.maps[1], md);
-    set_output(ctx, q, {y, T, b.d, b.ld_y}, residual, b.ld_y);
+    Splits sp;
+    sp.r.count = 0;
+    set_output(ctx, q, sp, y, b.ld_y, false, residual, b.ld_y, false);
     if (rc == DD_OK) rc = launch_gemm<kEpiStore, 256>(ctx, a, stream);
-    return rc == DD_OK && splits > 1 ? launch_reduce(ctx, q, {y, T, b.d, b.ld_y}, residual, b.ld_y, stream) : rc;
+    return rc == DD_OK ? launch_reduce(ctx, sp, stream) : rc;
 }
 
 extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, const void *x, const void *gate,
@@ -522,33 +539,35 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         rc = launch_gemm<kEpiBack, 256>(ctx, c, stream);
         if (rc != DD_OK) return rc;
     }
-    const unsigned kt = blocks_of(T, kBK), kf = blocks_of(b.f, kBK);
-    unsigned splits = 1;
-    GemmProblem *dxp = nullptr;
+    const unsigned kt = blocks_of(T, kBK), kf = blocks_of(b.f, kBK), pairs = (unsigned)ctx->sm_count / 2;
+    const unsigned wtiles = 3 * blocks_of(b.f, 2 * kBM) * blocks_of(b.d, 256);
+    const unsigned xtiles = few ? 0 : blocks_of(T, 2 * kBM) * blocks_of(b.d, 256);
+    Splits sp;
+    sp.r.count = 0;
     if (!few) {                                           // dgate w_gate + dup w_up
-        const unsigned long long weights = 3ull * kt * blocks_of(b.f, 2 * kBM) * blocks_of(b.d, 256);
-        splits = choose_splits(ctx, blocks_of(T, 2 * kBM) * blocks_of(b.d, 256), 2 * kf, weights);
-        dxp = &add_problem(a, T, b.d, 256, kf, kf, splits);
-        dxp->a_map[0] = kDg;
-        dxp->a_map[1] = kDu;
-        dxp->b_map[0] = kWg;
-        dxp->b_map[1] = kWu;
-        dxp->b_mn = 1;
-        set_output(ctx, *dxp, {dx, T, b.d, b.ld_x}, nullptr, 0);
+        GemmProblem &p = add_problem(a, T, b.d, 256, kf, kf, choose_splits(ctx, xtiles, 2 * kf, (unsigned long long)wtiles * kt));
+        p.a_map[0] = kDg;
+        p.a_map[1] = kDu;
+        p.b_map[0] = kWg;
+        p.b_map[1] = kWu;
+        p.b_mn = 1;
+        set_output(ctx, p, sp, dx, b.ld_x, false, nullptr, 0, false);
     }
+    // Few weights and many tokens: too few tiles for the pairs, so the tokens are split as well, as long
+    // as all units make one wave and it shortens them by more than the reducing launch costs (8192 tokens,
+    // d 256, f 512: 71 -> 39 us; with units left over for a second wave 2000 tokens, 504 x 1200 took 51, not 37)
+    unsigned wsplits = 1;
+    while (wsplits < kMaxSplits && a.tiles + wtiles * (wsplits + 1) <= pairs && kt >= 4 * (wsplits + 1)) ++wsplits;
+    if (kt - kt / wsplits < 16) wsplits = 1;
     struct { int a, b; void *out; uint64_t m, n, ld; } weights[3] = {
         {kDg, kX, dw_gate, b.f, b.d, b.ld_in}, {kDu, kX, dw_up, b.f, b.d, b.ld_in}, {kDy, kH, dw_down, b.d, b.f, b.ld_down}};
     for (const auto &w : weights) {
-        GemmProblem &q = add_problem(a, w.m, w.n, 256, kt);
+        GemmProblem &q = add_problem(a, w.m, w.n, 256, kt, 0, wsplits);
         q.a_map[0] = (unsigned char)w.a;
         q.b_map[0] = (unsigned char)w.b;
         q.a_mn = q.b_mn = 1;
-        q.out = w.out;
-        q.ld_out = w.ld;
-        q.out_f32 = q.addend_f32 = grad_dtype == DD_F32;
-        q.addend = accumulate ? w.out : nullptr;
-        q.ld_addend = w.ld;
+        set_output(ctx, q, sp, w.out, w.ld, grad_dtype == DD_F32, accumulate ? w.out : nullptr, w.ld, grad_dtype == DD_F32);
     }
     rc = launch_gemm<kEpiStore, 256>(ctx, a, stream);
-    return rc == DD_OK && splits > 1 ? launch_reduce(ctx, *dxp, {dx, T, b.d, b.ld_x}, nullptr, 0, stream) : rc;
+    return rc == DD_OK ? launch_reduce(ctx, sp, stream) : rc;
 }

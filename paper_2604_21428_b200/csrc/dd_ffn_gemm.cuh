@@ -241,6 +241,28 @@ __device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&x)[4], uns
     }
 }
 
+__device__ __forceinline__ void load4_f32(const float *p, float (&x)[4], unsigned live)
+{
+    if (live >= 4) {
+        const float4 w = *reinterpret_cast<const float4 *>(p);
+        x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i < live ? p[i] : 0.0f;
+    }
+}
+
+__device__ __forceinline__ void store4_f32(float *p, const float (&x)[4], unsigned live)
+{
+    if (live >= 4) {
+        *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < live) p[i] = x[i];
+    }
+}
+
 // ---- tiles ----------------------------------------------------------------------------------------
 
 struct TilePos {
@@ -404,25 +426,14 @@ __device__ __forceinline__ void finish_f32(unsigned box, int lane, const float (
         float y[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)}, add[4];
         if (p.addend) {
             const unsigned long long at = (unsigned long long)(row0 + r) * p.ld_addend + c;
-            if (!p.addend_f32) {
-                load4(static_cast<const __nv_bfloat16 *>(p.addend) + at, add, live);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) add[k] = k < live ? static_cast<const float *>(p.addend)[at + k] : 0.0f;
-            }
+            if (p.addend_f32) load4_f32(static_cast<const float *>(p.addend) + at, add, live);
+            else load4(static_cast<const __nv_bfloat16 *>(p.addend) + at, add, live);
 #pragma unroll
             for (int k = 0; k < 4; ++k) y[k] += add[k];
         }
         const unsigned long long at = (unsigned long long)(out_row0 + r) * p.ld_out + c;
-        if (!p.out_f32) {
-            store4(static_cast<__nv_bfloat16 *>(p.out) + at, y, live);
-        } else if (live >= 4) {
-            *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at) = make_float4(y[0], y[1], y[2], y[3]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 3; ++k)
-                if (k < live) static_cast<float *>(p.out)[at + k] = y[k];
-        }
+        if (p.out_f32) store4_f32(static_cast<float *>(p.out) + at, y, live);
+        else store4(static_cast<__nv_bfloat16 *>(p.out) + at, y, live);
     }
     __syncwarp();
 }
@@ -710,50 +721,64 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
     if (a.late_wait) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// out = bf16([residual +] sum of the splits' float32 slabs in split order), eight columns a thread.
+// Problems whose K was split: out = [addend +] sum of the splits' float32 slabs, in split order.
+struct ReduceJob {
+    const float *slabs;
+    unsigned splits, m, n, ld;                   // ld: row length of a slab, whole eights
+    unsigned long long slab;                     // elements from one split's slab to the next
+    unsigned long long end;                      // one past the job's last piece of eight columns
+    void *out;
+    const void *addend;                          // the output's type, or bf16 (a residual)
+    unsigned long long ld_out, ld_addend;
+    int out_f32, addend_f32;
+};
+
+struct ReduceArgs {
+    ReduceJob job[kMaxProblems];
+    int count;
+};
+
 __global__ void __launch_bounds__(256)
-ffn_reduce_kernel(const float *__restrict__ slabs, const unsigned splits, const unsigned long long slab, const unsigned ld,
-                  const unsigned m, const unsigned n, const __nv_bfloat16 *residual, const unsigned long long ld_residual,
-                  __nv_bfloat16 *out, const unsigned long long ld_out)
+ffn_reduce_kernel(const __grid_constant__ ReduceArgs a)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const unsigned pieces = (n + 7) / 8;
-    for (unsigned long long i = (unsigned long long)blockIdx.x * blockDim.x + threadIdx.x; i < (unsigned long long)m * pieces;
+    int k = 0;
+    for (unsigned long long i = (unsigned long long)blockIdx.x * blockDim.x + threadIdx.x; i < a.job[a.count - 1].end;
          i += (unsigned long long)gridDim.x * blockDim.x) {
-        const unsigned row = (unsigned)(i / pieces), col = (unsigned)(i % pieces) * 8, cols = n - col < 8 ? n - col : 8;
-        const float *src = slabs + (unsigned long long)row * ld + col;
-        float4 a[kMaxSplits], b[kMaxSplits];
+        while (i >= a.job[k].end) ++k;
+        const ReduceJob &j = a.job[k];
+        const unsigned long long at = i - (k ? a.job[k - 1].end : 0ull);
+        const unsigned pieces = j.ld / 8, row = (unsigned)(at / pieces), col = (unsigned)(at % pieces) * 8;
+        const unsigned cols = j.n - col < 8 ? j.n - col : 8;
+        const float *src = j.slabs + (unsigned long long)row * j.ld + col;
+        float4 v[kMaxSplits][2];
 #pragma unroll
         for (int s = 0; s < kMaxSplits; ++s)
-            if (s < splits) {
-                a[s] = __ldcg(reinterpret_cast<const float4 *>(src + s * slab));
-                b[s] = __ldcg(reinterpret_cast<const float4 *>(src + s * slab) + 1);
+            if (s < j.splits) {
+                v[s][0] = __ldcg(reinterpret_cast<const float4 *>(src + s * j.slab));
+                v[s][1] = __ldcg(reinterpret_cast<const float4 *>(src + s * j.slab) + 1);
             }
-        float x[8] = {a[0].x, a[0].y, a[0].z, a[0].w, b[0].x, b[0].y, b[0].z, b[0].w};
+        float x[2][4];
 #pragma unroll
-        for (int s = 1; s < kMaxSplits; ++s)
-            if (s < splits) {
-                x[0] += a[s].x; x[1] += a[s].y; x[2] += a[s].z; x[3] += a[s].w;
-                x[4] += b[s].x; x[5] += b[s].y; x[6] += b[s].z; x[7] += b[s].w;
+        for (int h = 0; h < 2; ++h) {
+            x[h][0] = v[0][h].x; x[h][1] = v[0][h].y; x[h][2] = v[0][h].z; x[h][3] = v[0][h].w;
+#pragma unroll
+            for (int s = 1; s < kMaxSplits; ++s)
+                if (s < j.splits) { x[h][0] += v[s][h].x; x[h][1] += v[s][h].y; x[h][2] += v[s][h].z; x[h][3] += v[s][h].w; }
+            const unsigned c = col + 4 * h, live = cols > 4 * h ? cols - 4 * h : 0;
+            if (!live) break;
+            if (j.addend) {
+                float add[4];
+                const unsigned long long from = (unsigned long long)row * j.ld_addend + c;
+                if (j.addend_f32) load4_f32(static_cast<const float *>(j.addend) + from, add, live);
+                else load4(static_cast<const __nv_bfloat16 *>(j.addend) + from, add, live);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[h][q] += add[q];
             }
-        __nv_bfloat16 *o = out + (unsigned long long)row * ld_out + col;
-        const __nv_bfloat16 *r = residual ? residual + (unsigned long long)row * ld_residual + col : nullptr;
-        if (cols == 8) {
-            if (r) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(r);
-                const unsigned u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[2 * j] += __uint_as_float(u[j] << 16);
-                    x[2 * j + 1] += __uint_as_float(u[j] & 0xffff0000u);
-                }
-            }
-            *reinterpret_cast<uint4 *>(o) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
-        } else {
-#pragma unroll
-            for (int j = 0; j < 7; ++j)
-                if (j < cols) o[j] = __float2bfloat16_rn(r ? x[j] + __bfloat162float(r[j]) : x[j]);
+            const unsigned long long to = (unsigned long long)row * j.ld_out + c;
+            if (j.out_f32) store4_f32(static_cast<float *>(j.out) + to, x[h], live);
+            else store4(static_cast<__nv_bfloat16 *>(j.out) + to, x[h], live);
         }
     }
 }
