@@ -9,7 +9,7 @@
  *   - the global norm of a list of gradient tensors, and clipping by it;
  *   - the AdamW step over a list of tensors, which applies the clip scale on the way and
  *     writes the bf16 copy that the merge reads.
- * The paper names neither model nor InnerOpt in formulas; the formulas below are fixed here.
+ * The paper gives neither the model nor InnerOpt as formulas; the formulas below are fixed here.
  *
  * The conventions of dd_merge.h hold: borrowed buffers, [device] and [host] pointers, work
  * enqueued on the given stream without waiting, host arrays consumed before return, DD_OK or
@@ -129,6 +129,10 @@ typedef struct {
 } dd_gated_ffn;
 
 /*
+ * Memory: the first call of either direction on a context allocates 256 KB per SM (38 MB on a B200)
+ * for partial products, which it keeps; no later call allocates unless `hidden` / `scratch` is NULL
+ * and has to grow.  Make the first call before a stream capture.
+ *
  * gate = x w_gate^T,  up = x w_up^T,  y = [residual +] (a(gate) * up) w_down^T
  *
  * Sums are float32; the product a(gate) * up is taken from the float32 gate and up and
