@@ -120,6 +120,32 @@ static int allow_smem(dd_ctx *ctx, K kernel, size_t bytes, bool (&done)[64])
     return DD_OK;
 }
 
+// Whether a kEpiStore launch takes 256 x 512 tiles.  They read a quarter fewer operand bytes a product, but
+// fill tensor memory, so that an epilogue has no product to run under, and there are half as many.  The
+// estimate is in cycles: a K block 1060 against 620, the rest of a unit 6000 against 800; one problem
+// runs in waves, several fill the gaps.  Measured, 256 x 256 / 256 x 512: 4096 tokens, d 2048, f 8192 backward
+// 636 / 580 us, forward 317 / 302; 2048 tokens 327 / 307 and 159 / 181; 1024 tokens backward 174 / 212; 8192 tokens,
+// 512 x 2048 123 / 130 (the smaller time is taken in each case).
+static bool wide_tiles(const dd_ctx *ctx, const GemmArgs &a)
+{
+    const unsigned pairs = (unsigned)ctx->sm_count / 2;
+    unsigned long long time[2];
+    for (int w = 0; w < 2; ++w) {
+        unsigned long long sum = 0, longest = 0, tiles = 0;
+        for (int i = 0; i < a.nprob; ++i) {
+            const GemmProblem &p = a.prob[i];
+            if (p.splits > 1) return false;
+            const unsigned long long unit = (unsigned long long)(p.kblocks[0] + p.kblocks[1]) * (w ? 1060 : 620) + (w ? 6000 : 800);
+            tiles = (unsigned long long)p.tiles_m * blocks_of(p.n, w ? 512 : 256);
+            sum += tiles * unit;
+            longest = unit > longest ? unit : longest;
+        }
+        time[w] = a.nprob == 1 ? blocks_of(tiles, pairs) * longest : sum / pairs + longest / 8;
+        if (time[w] < longest) time[w] = longest;
+    }
+    return time[1] < time[0];
+}
+
 template <int EPI, int BN, int ACT>
 static int launch_gemm_act(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
 {
@@ -158,6 +184,19 @@ static int launch_gemm(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
 {
     return EPI != kEpiStore && a.e.activation == DD_ACT_GELU_TANH ? launch_gemm_act<EPI, BN, EPI == kEpiStore ? DD_ACT_SILU : DD_ACT_GELU_TANH>(ctx, a, stream)
                                                                   : launch_gemm_act<EPI, BN, DD_ACT_SILU>(ctx, a, stream);
+}
+
+static int launch_store(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
+{
+    if (!wide_tiles(ctx, a)) return launch_gemm<kEpiStore, 256>(ctx, a, stream);
+    a.tiles = 0;
+    for (int i = 0; i < a.nprob; ++i) {
+        GemmProblem &p = a.prob[i];
+        p.tiles_n = blocks_of(p.n, 512);
+        a.tiles += p.tiles_m * p.tiles_n;
+        p.tile_end = a.tiles;
+    }
+    return launch_gemm<kEpiStore, 512>(ctx, a, stream);
 }
 
 // Slabs handed out so far, and what becomes of them.
@@ -444,7 +483,7 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
     Splits sp;
     sp.r.count = 0;
     set_output(ctx, q, sp, y, b.ld_y, false, residual, b.ld_y, false);
-    if (rc == DD_OK) rc = launch_gemm<kEpiStore, 256>(ctx, a, stream);
+    if (rc == DD_OK) rc = launch_store(ctx, a, stream);
     return rc == DD_OK ? launch_reduce(ctx, sp, stream) : rc;
 }
 
@@ -568,6 +607,6 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         q.a_mn = q.b_mn = 1;
         set_output(ctx, q, sp, w.out, w.ld, grad_dtype == DD_F32, accumulate ? w.out : nullptr, w.ld, grad_dtype == DD_F32);
     }
-    rc = launch_gemm<kEpiStore, 256>(ctx, a, stream);
+    rc = launch_store(ctx, a, stream);
     return rc == DD_OK ? launch_reduce(ctx, sp, stream) : rc;
 }

@@ -4,13 +4,18 @@
 // A pair of SMs (a cluster of two CTAs) computes one 256 x BN tile with tcgen05.mma of
 // cta_group::2: each CTA stages 128 rows of A and BN / 2 rows of B and keeps 128 rows of the
 // accumulator, so that every operand byte in shared memory feeds twice the products that it would
-// for one SM.  Persistent pairs walk the tiles of up to four problems.  In each CTA warp 4 (one lane)
+// for one SM.  Persistent pairs walk the tiles of up to four problems.  In each CTA warp 8 (one lane)
 // has the TMA engine fill a ring of stages of 64 K-elements (128-byte rows, 128-byte swizzle);
-// warp 5 of the first CTA (one lane) issues the products for both; warps 0-3 turn finished
-// accumulators into results.  Two accumulators alternate, so the epilogue of one tile runs under
-// the products of the next.  Operands are read where they lie in either order -- K contiguous, or
-// M / N contiguous (the descriptor's "major" bit) -- so no product of the backward pass needs a
-// transposed copy.
+// warp 9 of the first CTA (one lane) issues the products for both; warps 0-7 turn finished
+// accumulators into results.  With BN = 256 two accumulators alternate, so the epilogue of one tile runs
+// under the products of the next; BN = 512 (long K only) reads fewer operand bytes a product instead.
+// Operands are read where they lie in either order -- K contiguous, or M / N contiguous (the
+// descriptor's "major" bit) -- so no product of the backward pass needs a transposed copy.
+//
+// What bounds it: at 8192 tokens, d 2048, f 8192 the operands come out of L2 at 10-13 TB/s (128 FLOP a
+// byte with BN = 256) with the tensor pipe 68-77 % active, under the 1000 W cap.  Forward 606 us in short
+// runs, 660 sustained; backward 1155 and 1280.  The same passes with the loads taken out after the
+// first ring take 473 us forward, with the products taken out 497.
 //
 // Every wait is bounded: on giving up a role raises its CTA's abort flag, the roles leave their
 // loops, copies and products in flight are awaited (again bounded), tensor memory is freed and
@@ -458,8 +463,8 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
     constexpr int kStages = gemm_stages(EPI, BN), kProducer = kEpiWarps, kIssuer = kEpiWarps + 1;
     constexpr unsigned kStageBytes = gemm_stage_bytes(BN), kABytes = kBM * kBK * 2;
     constexpr int kCols = EPI == kEpiGate ? BN / 2 : BN;      // output columns of a tile
-    constexpr unsigned kTmemCols = 2 * BN;
-    static_assert(kTmemCols == 512 || kTmemCols == 256, "tensor memory is allocated in powers of two");
+    constexpr unsigned kTmemCols = 512, kSlots = kTmemCols / BN;   // accumulators that alternate
+    static_assert(BN == 256 || (BN == 512 && EPI == kEpiStore), "one or two products of 256 columns a step");
 
     extern __shared__ unsigned char smem_raw[];
     const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -506,7 +511,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             for (unsigned u = 0, t; ok && (t = unit_of(a, pair, pairs, u)) < a.tiles; ++u) {
                 const TilePos pos = tile_pos<kCols>(a, t);
                 const GemmProblem &p = a.prob[pos.p];
-                const int m0 = (int)(pos.m0 + rank * kBM), n0 = (int)(pos.n0 + (EPI == kEpiGate ? 0 : rank * (BN / 2)));
+                const int m0 = (int)(pos.m0 + rank * kBM), n0 = (int)(pos.n0 + (EPI == kEpiGate ? 0 : rank * 128));
                 for (unsigned kb = pos.kb0; kb < pos.kb1; ++kb, ++it) {
                     if ((it >= kStages && !gemm_wait(empty + 8 * s, phase, abort)) || *abort) { ok = false; break; }
                     const int seg = kb >= p.kblocks[0], k0 = (int)(kb - (seg ? p.kblocks[0] : 0u)) * kBK;
@@ -517,8 +522,10 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                     for (int c = 0; c < kBM / 64; ++c)
                         tma_load_2d_pair(st + c * kChunkBytes, ma, p.a_mn ? m0 + 64 * c : k0, p.a_mn ? k0 : m0 + 64 * c, bar);
 #pragma unroll
-                    for (int c = 0; c < BN / 128; ++c)
-                        tma_load_2d_pair(st + kABytes + c * kChunkBytes, mb, p.b_mn ? n0 + 64 * c : k0, p.b_mn ? k0 : n0 + 64 * c, bar);
+                    for (int c = 0; c < BN / 128; ++c) {              // this CTA's 128 of every 256 columns
+                        const int n = n0 + c / 2 * 256 + 64 * (c & 1);
+                        tma_load_2d_pair(st + kABytes + c * kChunkBytes, mb, p.b_mn ? n : k0, p.b_mn ? k0 : n, bar);
+                    }
                     if (++s == kStages) { s = 0; phase ^= 1; }
                 }
             }
@@ -534,12 +541,12 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             for (unsigned t; ok && (t = unit_of(a, pair, pairs, acc)) < a.tiles; ++acc) {
                 const TilePos pos = tile_pos<kCols>(a, t);
                 const GemmProblem &p = a.prob[pos.p];
-                const unsigned slot = acc & 1;
-                if (acc >= 2 && !gemm_wait(tempty + 8 * slot, (acc / 2 - 1) & 1, abort)) { ok = false; break; }
+                const unsigned slot = acc % kSlots;
+                if (acc >= kSlots && !gemm_wait(tempty + 8 * slot, (acc / kSlots - 1) & 1, abort)) { ok = false; break; }
                 tc_fence_after();
-                // float32 accumulators, bf16 x bf16, the operands' majors, N = BN, M = 256
+                // float32 accumulators, bf16 x bf16, the operands' majors, N = 256, M = 256
                 const unsigned idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((unsigned)p.a_mn << 15) |
-                                       ((unsigned)p.b_mn << 16) | ((unsigned)(BN / 8) << 17) | ((2 * kBM / 16) << 24);
+                                       ((unsigned)p.b_mn << 16) | ((256u / 8) << 17) | ((2 * kBM / 16) << 24);
                 const unsigned astep = p.a_mn ? 2048 : 32, bstep = p.b_mn ? 2048 : 32;     // bytes per 16 K elements
                 for (unsigned kb = pos.kb0; kb < pos.kb1; ++kb) {
                     if (!gemm_wait(full + 8 * s, phase, abort)) { ok = false; break; }
@@ -547,8 +554,10 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                     const unsigned sa = smem + s * kStageBytes, sb = sa + kABytes;
 #pragma unroll
                     for (int k = 0; k < kBK / 16; ++k)
-                        umma_bf16_pair(tmem + slot * BN, umma_desc(sa + k * astep, p.a_mn), umma_desc(sb + k * bstep, p.b_mn),
-                                       idesc, kb != pos.kb0 || k);
+#pragma unroll
+                        for (int h = 0; h < BN / 256; ++h)
+                            umma_bf16_pair(tmem + slot * BN + 256 * h, umma_desc(sa + k * astep, p.a_mn),
+                                           umma_desc(sb + h * 2 * kChunkBytes + k * bstep, p.b_mn), idesc, kb != pos.kb0 || k);
                     umma_commit_pair(empty + 8 * s, 3);
                     if (++s == kStages) { s = 0; phase ^= 1; }
                 }
@@ -571,10 +580,10 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
         for (unsigned t; (t = unit_of(a, pair, pairs, acc)) < a.tiles; ++acc) {
             const TilePos pos = tile_pos<kCols>(a, t);
             const GemmProblem &p = a.prob[pos.p];
-            const unsigned slot = acc & 1, row = pos.m0 + row0;
+            const unsigned slot = acc % kSlots, row = pos.m0 + row0;
             const unsigned chunks = chunks_of<kCols, 64>(p, pos, row0, half);
             if (EPI == kEpiBack && chunks) load_chunk(p, pos, 0);
-            const bool ok = gemm_wait(tfull + 8 * slot, (acc / 2) & 1, abort);
+            const bool ok = gemm_wait(tfull + 8 * slot, (acc / kSlots) & 1, abort);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
             const unsigned taddr = tmem + ((unsigned)((warp & 3) * 32) << 16) + slot * BN + half * (kCols / 2);
