@@ -215,7 +215,6 @@ static void set_output(const dd_ctx *ctx, GemmProblem &p, Splits &sp, void *out,
         p.out_f32 = f32;
         p.addend = addend;
         p.ld_addend = ld_addend;
-        p.addend_f32 = addend_f32;
         return;
     }
     const unsigned ld = (p.n + 7) / 8 * 8;

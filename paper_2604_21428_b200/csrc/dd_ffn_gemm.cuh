@@ -61,8 +61,8 @@ struct GemmProblem {
     unsigned split_rows;
     unsigned char a_map[2], b_map[2]; // tensor maps of the segments; kEpiGate: b_map = {w_gate, w_up}
     unsigned char a_mn, b_mn;         // 1: M (N) is the contiguous direction in memory
-    // kEpiStore: out = sums [+ addend]; the addend may be the output itself
-    unsigned char out_f32, addend_f32;
+    // kEpiStore: out = sums [+ addend of the output's type]; the addend may be the output itself
+    unsigned char out_f32;
     void *out;
     const void *addend;
     unsigned long long ld_out, ld_addend;
@@ -399,6 +399,30 @@ __device__ __forceinline__ void store_box(unsigned box, int lane, __nv_bfloat16 
     }
 }
 
+// 32 rows from row0 and 64 columns from col on of a bf16 matrix, a lane's share in the order of store_box;
+// zeros past its end.
+__device__ __forceinline__ void load_share(uint4 (&w)[8], int lane, const __nv_bfloat16 *in, unsigned long long ld, unsigned row0,
+                                           unsigned col, unsigned m, unsigned n)
+{
+    const unsigned c = col + (lane & 7) * 8, live = c < n ? n - c : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const unsigned row = row0 + 4 * i + (lane >> 3);
+        w[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (row >= m || !live) continue;
+        const __nv_bfloat16 *src = in + (unsigned long long)row * ld + c;
+        if (live >= 8) {
+            w[i] = *reinterpret_cast<const uint4 *>(src);
+        } else {
+            unsigned u[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int k = 0; k < 7; ++k)
+                if (k < live) u[k / 2] |= (unsigned)reinterpret_cast<const unsigned short *>(src)[k] << (16 * (k & 1));
+            w[i] = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+    }
+}
+
 // Rows row0.. and columns col.. of a bf16 matrix to the box; zeros past its end.
 __device__ __forceinline__ void load_box(unsigned box, int lane, const __nv_bfloat16 *in, unsigned long long ld, unsigned row0, unsigned col,
                                          unsigned m, unsigned n)
@@ -431,14 +455,12 @@ __device__ __forceinline__ void finish_f32(unsigned box, int lane, const float (
         float y[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)}, add[4];
         if (p.addend) {
             const unsigned long long at = (unsigned long long)(row0 + r) * p.ld_addend + c;
-            if (p.addend_f32) load4_f32(static_cast<const float *>(p.addend) + at, add, live);
-            else load4(static_cast<const __nv_bfloat16 *>(p.addend) + at, add, live);
+            load4_f32(static_cast<const float *>(p.addend) + at, add, live);
 #pragma unroll
             for (int k = 0; k < 4; ++k) y[k] += add[k];
         }
         const unsigned long long at = (unsigned long long)(out_row0 + r) * p.ld_out + c;
-        if (p.out_f32) store4_f32(static_cast<float *>(p.out) + at, y, live);
-        else store4(static_cast<__nv_bfloat16 *>(p.out) + at, y, live);
+        store4_f32(static_cast<float *>(p.out) + at, y, live);
     }
     __syncwarp();
 }
@@ -583,6 +605,15 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             const unsigned slot = acc % kSlots, row = pos.m0 + row0;
             const unsigned chunks = chunks_of<kCols, 64>(p, pos, row0, half);
             if (EPI == kEpiBack && chunks) load_chunk(p, pos, 0);
+            // kEpiStore to bf16 with a bf16 addend: its share of a chunk is asked for a chunk ahead
+            const bool add = EPI == kEpiStore && p.addend && !p.out_f32;
+            const auto load_addend = [&](uint4 (&w)[8], unsigned c) {
+                load_share(w, lane, static_cast<const __nv_bfloat16 *>(p.addend), p.ld_addend, row, pos.n0 + half * (kCols / 2) + 64 * c, p.m, p.n);
+            };
+            uint4 share[EPI == kEpiStore ? 8 : 1];
+            if constexpr (EPI == kEpiStore) {
+                if (add && chunks) load_addend(share, 0);
+            }
             const bool ok = gemm_wait(tfull + 8 * slot, (acc / kSlots) & 1, abort);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
@@ -594,7 +625,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                 if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * slot);
             };
             if (!chunks) release();
-            if (EPI == kEpiStore && (p.out_f32 || p.addend)) {
+            if (EPI == kEpiStore && p.out_f32) {
 #pragma unroll 1
                 for (unsigned c = 0; c < 2 * chunks; ++c) {
                     unsigned r[32];
@@ -616,12 +647,31 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                 for (unsigned c = 0; c < chunks; ++c) {
                     tmem_ld_wait();
                     if (c + 1 == chunks) release();
+                    if constexpr (EPI == kEpiStore) {
+                        if (add) {                                 // the addend to rows, where the sums are
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                st_shared(box_piece(box, 4 * i + (lane >> 3), lane & 7), share[i].x, share[i].y, share[i].z, share[i].w);
+                            __syncwarp();
+                            if (c + 1 < chunks) load_addend(share, c + 1);
+                        }
+                    }
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        unsigned w[16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) w[j] = pack2(__uint_as_float(r[h][2 * j]), __uint_as_float(r[h][2 * j + 1]));
-                        write_half(box, lane, h, w);
+                        for (int j = 0; j < 4; ++j) {
+                            const unsigned piece = box_piece(box, lane, 4 * h + j);
+                            float x[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r[h][8 * j + i]);
+                            if (add) {
+                                const uint4 a4 = ld_shared(piece);
+                                const unsigned u[4] = {a4.x, a4.y, a4.z, a4.w};
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) x[i] += __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+                            }
+                            st_shared(piece, pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+                        }
                     }
                     __syncwarp();
                     if (c + 1 < chunks) {                          // on their way while this chunk is stored
