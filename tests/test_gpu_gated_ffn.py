@@ -319,3 +319,25 @@ def test_bounded_waits_expire(dd, ctx, tokens):
     for got, (ref, tol) in zip(outs, backward64(x, *w, gate, up, mat(tokens, d, 12), 0)):
         within(got, ref, tol * (1 + UB) + UB * ref.abs(), "after the expiry")
     assert status.tolist() == [0, 0]
+
+
+def test_beyond_32_bit_offsets(dd, ctx):
+    """gate, up and the intermediates of 270,000 tokens x 8192 lie past 2^32 bytes: the last rows
+    against float64, and against the first rows, which hold the same tokens."""
+    T, d, f = 270_000, 64, 8192
+    rows = mat(300, d, 1)
+    w = [mat(f, d, 2, 0.1), mat(f, d, 3, 0.1), mat(d, f, 4, 0.02)]
+    x = rows.repeat(T // 300, 1)
+    y, gate, up = torch.empty_like(x), torch.empty(T, f, dtype=B, device="cuda"), torch.empty(T, f, dtype=B, device="cuda")
+    ctx.gated_ffn_forward(x, *w, y, gate=gate, up=up)
+    for got, (ref, tol) in zip((y, gate, up), forward64(rows, *w, None, 0)):
+        within(got[-300:], ref, tol, "last rows")
+        within(got[:300], ref, tol, "first rows")
+    dy = torch.zeros_like(x)
+    dy[-1] = 1.0
+    dx, dws = torch.empty_like(x), [torch.empty_like(t) for t in w]
+    ctx.gated_ffn_backward(x, *w, gate, up, dy, dx, *dws)
+    want = backward64(rows[-1:], *w, gate[-1:], up[-1:], dy[-1:], 0)
+    for got, (ref, tol), what in zip((dx[-1:], *dws), want, ("dx", "dw_gate", "dw_up", "dw_down")):
+        within(got, ref, tol * (1 + UB) + UB * ref.abs(), what)
+    assert not bool(dx[:-1].any())
