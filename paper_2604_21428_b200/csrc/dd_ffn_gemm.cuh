@@ -34,9 +34,9 @@ namespace ddm {
 constexpr int kBM = 128, kBK = 64;              // rows of one CTA, K elements of a stage
 constexpr int kChunkBytes = 64 * 128;             // one TMA box: 64 rows of 64 bf16
 constexpr int kMaxMaps = 8, kMaxProblems = 4;
-constexpr unsigned kTileGroup = 8;
+constexpr unsigned kTileGroup = 8;                // 4 / 8 / 16: forward 657 / 646 / 639 us, backward 1305 / 1309 / 1325 (8192 tokens)
 constexpr int kMaxSplits = 8;
-constexpr unsigned kSpinLimit = 1u << 30;
+constexpr unsigned kSpinLimit = 1u << 30;         // attempts and nanoseconds of a bounded wait
 constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr int kBoxBytes = 32 * 128;               // an epilogue box: 32 rows of 64 bf16 or 32 float32
 
