@@ -7,8 +7,10 @@
 // the tokens it owns.  No workspace, no atomics, and with S up to 8 even a 2048 x 8192 matrix
 // spreads over the whole GPU.
 //
-// The launch that follows on the stream may start early (programmatic launch): it fills its ring
-// with weights, which do not depend on this launch, and waits only before it reads activations.
+// The call's second launch starts early (programmatic launch): it fills its ring with weights, which
+// the call's first launch does not write, and waits only before it reads activations.  The launch before
+// the call may well write them -- an optimizer step that leaves the weights' bf16 copies -- so
+// the first launch lets the second one start only once its own wait for that launch is over.
 //
 // d 2048, f 8192, gate and up kept: 1 / 64 / 128 tokens 22 / 28 / 33 us forward, of which the 100.7 MB of
 // weights need 15.4; the rest is two launches' ramp, reduction and hand-over.  A ring of 64 KB took 27.0
@@ -186,8 +188,8 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
     __syncthreads();
     tc_fence_after();
     const unsigned tmem = tmem_base;
+    if (!p.own_prior) asm volatile("griddepcontrol.wait;" ::: "memory");      // before the trigger: see the top of the file
     if (!p.late_trigger) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (!p.own_prior) asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if (warp == 4) {
         if (elect_one()) {
