@@ -147,6 +147,9 @@ void *matrix(PyObject *o, const char *name, uint64_t rows, uint64_t cols, uint64
         (cols > 1 && t.stride(1) != 1))
         refuse(std::string(name) + ": want " + c10::toString(kind) + " [" + std::to_string(rows) + ", " + std::to_string(cols) +
                "] with contiguous rows, got (size by stride) " + shape_of(t));
+    // an expanded matrix has stride 0, which the C calls take as "the row length itself"
+    if (rows > 1 && (uint64_t)t.stride(0) < cols)
+        refuse(std::string(name) + ": rows overlap, got (size by stride) " + shape_of(t));
     if (rows > 1 || ld == 0) {            // a single row takes whatever stride its partners have
         const uint64_t s = rows > 1 ? (uint64_t)t.stride(0) : (cols + 7) / 8 * 8;
         if (ld && s != ld) refuse(std::string(name) + ": row stride " + std::to_string(s) + " differs from " + std::to_string(ld));
