@@ -17,6 +17,41 @@ struct Refused {
 
 [[noreturn]] void refuse(std::string why) { throw Refused{std::move(why)}; }
 
+// Python's own error is set.
+struct Raised {};
+
+// Numbers.  One that does not convert ends the call before it starts: what stands for "error" in the
+// conversions (-1, null) are arguments that the C calls would take.
+void *pointer(PyObject *o)
+{
+    void *p = PyLong_AsVoidPtr(o);
+    if (!p && PyErr_Occurred()) throw Raised{};
+    return p;
+}
+
+double real(PyObject *o)
+{
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) throw Raised{};
+    return x;
+}
+
+long long integer(PyObject *o)
+{
+    const long long x = PyLong_AsLongLong(o);
+    if (x == -1 && PyErr_Occurred()) throw Raised{};
+    return x;
+}
+
+bool truth(PyObject *o)
+{
+    const int x = PyObject_IsTrue(o);
+    if (x < 0) throw Raised{};
+    return x != 0;
+}
+
+dd_ctx *context(PyObject *o) { return static_cast<dd_ctx *>(pointer(o)); }
+
 const at::Tensor &tensor(PyObject *o, const char *name)
 {
     if (!THPVariable_Check(o)) refuse(std::string(name) + ": want a tensor");
@@ -29,7 +64,7 @@ const at::Tensor &tensor(PyObject *o, const char *name)
 void *address(PyObject *o, const char *name, size_t bytes)
 {
     if (o == Py_None) return nullptr;
-    if (PyLong_Check(o)) return PyLong_AsVoidPtr(o);
+    if (PyLong_Check(o)) return pointer(o);
     const at::Tensor &t = tensor(o, name);
     if (!t.is_contiguous() || t.nbytes() < bytes) refuse(std::string(name) + ": want " + std::to_string(bytes) + " contiguous bytes");
     return t.data_ptr();
@@ -104,9 +139,9 @@ std::vector<void *> matching(PyObject *o, const List &grads, const char *name, K
 int grad_norm(PyObject *const *a)
 {
     const List g = gradients(a[1]);
-    return dd_grad_norm((dd_ctx *)PyLong_AsVoidPtr(a[0]), g.ptr.data(), g.n.data(), g.dtype.data(), g.count(),
-                        (float)PyFloat_AsDouble(a[2]), (dd_grad_record *)address(a[3], "record", sizeof(dd_grad_record)),
-                        PyLong_AsVoidPtr(a[4]));
+    return dd_grad_norm(context(a[0]), g.ptr.data(), g.n.data(), g.dtype.data(), g.count(),
+                        (float)real(a[2]), (dd_grad_record *)address(a[3], "record", sizeof(dd_grad_record)),
+                        pointer(a[4]));
 }
 
 // (ctx, grads, out, max_norm, record, stream)
@@ -115,9 +150,9 @@ int clip_gradients(PyObject *const *a)
     const List g = gradients(a[1]);
     std::vector<void *> out;
     if (a[2] != Py_None) out = matching(a[2], g, "out", Kind::kSame);
-    return dd_clip_gradients((dd_ctx *)PyLong_AsVoidPtr(a[0]), g.ptr.data(), a[2] != Py_None ? out.data() : nullptr, g.n.data(),
-                             g.dtype.data(), g.count(), (float)PyFloat_AsDouble(a[3]),
-                             (dd_grad_record *)address(a[4], "record", sizeof(dd_grad_record)), PyLong_AsVoidPtr(a[5]));
+    return dd_clip_gradients(context(a[0]), g.ptr.data(), a[2] != Py_None ? out.data() : nullptr, g.n.data(),
+                             g.dtype.data(), g.count(), (float)real(a[3]),
+                             (dd_grad_record *)address(a[4], "record", sizeof(dd_grad_record)), pointer(a[5]));
 }
 
 // (ctx, params, grads, exp_avg, exp_avg_sq, copies, clip, step, lr, beta1, beta2, eps, weight_decay, stream)
@@ -128,12 +163,12 @@ int adamw_step(PyObject *const *a)
                               v = matching(a[4], g, "exp_avg_sq", Kind::kF32);
     std::vector<void *> copies;
     if (a[5] != Py_None) copies = matching(a[5], g, "copies", Kind::kBF16, true);
-    const long long step = PyLong_AsLongLong(a[7]);
-    const dd_adamw opt = {PyFloat_AsDouble(a[8]), PyFloat_AsDouble(a[9]), PyFloat_AsDouble(a[10]), PyFloat_AsDouble(a[11]),
-                          PyFloat_AsDouble(a[12]), step > 0 ? (uint64_t)step : 0};
-    return dd_adamw_step((dd_ctx *)PyLong_AsVoidPtr(a[0]), &opt, (float *const *)p.data(), g.ptr.data(), (float *const *)m.data(),
+    const long long step = integer(a[7]);
+    const dd_adamw opt = {real(a[8]), real(a[9]), real(a[10]), real(a[11]),
+                          real(a[12]), step > 0 ? (uint64_t)step : 0};
+    return dd_adamw_step(context(a[0]), &opt, (float *const *)p.data(), g.ptr.data(), (float *const *)m.data(),
                          (float *const *)v.data(), a[5] != Py_None ? copies.data() : nullptr, g.n.data(), g.dtype.data(),
-                         g.count(), (const dd_grad_record *)address(a[6], "clip", sizeof(dd_grad_record)), PyLong_AsVoidPtr(a[13]));
+                         g.count(), (const dd_grad_record *)address(a[6], "clip", sizeof(dd_grad_record)), pointer(a[13]));
 }
 
 // ---- matrices -------------------------------------------------------------------------------
@@ -167,8 +202,9 @@ const void *block_of(PyObject *const *a, PyObject *act, PyObject *flags, dd_gate
     b.tokens = x.size(0);
     b.d = x.size(1);
     b.f = w.size(0);
-    b.activation = (int32_t)PyLong_AsLong(act);
-    b.flags = (uint32_t)PyLong_AsUnsignedLong(flags);
+    const long long kind = integer(act), bits = integer(flags);
+    b.activation = kind == (int32_t)kind ? (int32_t)kind : -1;
+    b.flags = bits == (uint32_t)bits ? (uint32_t)bits : ~0u;
     const void *px = matrix(a[0], "x", b.tokens, b.d, b.ld_x);
     b.w_gate = matrix(a[1], "w_gate", b.f, b.d, b.ld_in);
     b.w_up = matrix(a[2], "w_up", b.f, b.d, b.ld_in);
@@ -185,8 +221,8 @@ int gated_ffn_forward(PyObject *const *a)
     const void *x = block_of(a + 1, a[9], a[13], b);
     void *y = matrix(a[5], "y", b.tokens, b.d, b.ld_y), *res = matrix(a[6], "residual", b.tokens, b.d, b.ld_y);
     void *gate = matrix(a[7], "gate", b.tokens, b.f, b.ld_gate), *up = matrix(a[8], "up", b.tokens, b.f, b.ld_gate);
-    return dd_gated_ffn_forward((dd_ctx *)PyLong_AsVoidPtr(a[0]), &b, x, res, gate, up, address(a[10], "hidden", hidden_bytes(b)), y,
-                                (int32_t *)address(a[11], "status", 4), PyLong_AsVoidPtr(a[12]));
+    return dd_gated_ffn_forward(context(a[0]), &b, x, res, gate, up, address(a[10], "hidden", hidden_bytes(b)), y,
+                                (int32_t *)address(a[11], "status", 4), pointer(a[12]));
 }
 
 // (ctx, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up, dw_down, activation, accumulate, scratch, status, stream, flags)
@@ -201,20 +237,21 @@ int gated_ffn_backward(PyObject *const *a)
     if (kind != at::kFloat && kind != at::kBFloat16) refuse("the weights' gradients must be float32 or bfloat16");
     void *dwg = matrix(a[9], "dw_gate", b.f, b.d, b.ld_in, kind), *dwu = matrix(a[10], "dw_up", b.f, b.d, b.ld_in, kind);
     void *dwd = matrix(a[11], "dw_down", b.d, b.f, b.ld_down, kind);
-    return dd_gated_ffn_backward((dd_ctx *)PyLong_AsVoidPtr(a[0]), &b, x, gate, up, dy, dx, dwg, dwu, dwd,
-                                 kind == at::kBFloat16 ? DD_BF16 : DD_F32, PyObject_IsTrue(a[13]),
+    return dd_gated_ffn_backward(context(a[0]), &b, x, gate, up, dy, dx, dwg, dwu, dwd,
+                                 kind == at::kBFloat16 ? DD_BF16 : DD_F32, truth(a[13]),
                                  address(a[14], "scratch", 3 * hidden_bytes(b)), (int32_t *)address(a[15], "status", 4),
-                                 PyLong_AsVoidPtr(a[16]));
+                                 pointer(a[16]));
 }
 
-// Runs a call: refusals become ValueError, numbers that do not convert raise what Python raised.
+// Runs a call: refusals become ValueError, numbers that do not convert raise what Python raised.  Either
+// way nothing has been launched.
 template <int (*CALL)(PyObject *const *), int NARGS>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     if (n != NARGS) return PyErr_Format(PyExc_TypeError, "want %d arguments, got %zd", NARGS, n);
     try {
-        const int rc = CALL(args);
-        return PyErr_Occurred() ? nullptr : PyLong_FromLong(rc);
+        return PyLong_FromLong(CALL(args));
+    } catch (const Raised &) {
     } catch (const Refused &r) {
         PyErr_SetString(PyExc_ValueError, r.why.c_str());
     } catch (const std::exception &e) {
