@@ -266,6 +266,7 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
 #pragma unroll
         for (int b = 0; b < 2; ++b)
             if (mine && j + b * kTokensAtOnce < end) aux[b] = load_aux<EPI>(p.e, n0 + c + j + b * kTokensAtOnce, feature, live);
+        __syncwarp();                     // lanes own different tokens and features; what follows is for whole warps
         if (warp < 4) {
             const unsigned col = tmem + ((unsigned)(warp * 32) << 16) + c, to = buf + threadIdx.x * 4;
 #pragma unroll 1
@@ -313,6 +314,7 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
                 finish4<EPI, ACT>(p.e, n0 + c + k, feature, live, now, x, u);
             }
         }
+        __syncwarp();
     }
     if (S > 1) cluster_sync_relaxed();    // nobody leaves while its sums may still be read
     tc_fence_before();
