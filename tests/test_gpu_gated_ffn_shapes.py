@@ -67,3 +67,110 @@ def test_two_rounds_ragged(ctx, size):
         check_forward(ctx, size, act, True, pad=act)
     check_backward(ctx, size, 0, "bf16")
     check_backward(ctx, size, 1, "f32_acc", pad=1)
+
+
+# Sizes whose way down, or whose gradients, are cut into 256 x 512 tiles, with d and f ending in either half
+# of a tile's columns, tokens inside a tile's rows and K inside a block.  (T, d, f)
+WIDE_FORWARD = [(3647, 1060, 1603), (4725, 829, 1561), (2313, 2049, 2731)]
+WIDE_BACKWARD = [(3614, 790, 1742), (2445, 1333, 1306), (3992, 2569, 1810), (4758, 2561, 2715)]
+
+
+def kernels_of(call):
+    """Names of the kernels that a call launches; None where the profiler does not see any."""
+    from torch.profiler import ProfilerActivity, profile
+    call()
+    torch.cuda.synchronize()
+    with profile(activities=[ProfilerActivity.CUDA]) as prof:
+        call()
+        torch.cuda.synchronize()
+    names = [e.key for e in prof.key_averages()]
+    return names if any("ffn_" in n for n in names) else None
+
+
+def test_sizes_take_wide_tiles(ctx):
+    seen = []
+    for sizes, backward in ((WIDE_FORWARD, False), (WIDE_BACKWARD, True)):
+        for T, d, f in sizes:
+            x, y, w = mat(T, d, 1), mat(T, d, 2), [mat(f, d, 3), mat(f, d, 4), mat(d, f, 5)]
+            gate, up, dws = mat(T, f, 6), mat(T, f, 7), [mat(f, d, 8), mat(f, d, 9), mat(d, f, 10)]
+            if backward:
+                names = kernels_of(lambda: ctx.gated_ffn_backward(x, *w, gate, up, x, y, *dws))
+            else:
+                names = kernels_of(lambda: ctx.gated_ffn_forward(x, *w, y))
+            if names is None:
+                pytest.skip("no kernel names from the profiler")
+            seen.append(any("ffn_gemm_kernel<0, 512" in n for n in names))
+    assert all(seen), seen
+
+
+@pytest.mark.parametrize("with_residual", [False, True])
+@pytest.mark.parametrize("size", WIDE_FORWARD, ids=str)
+def test_wide_forward(ctx, size, with_residual):
+    check_forward(ctx, size, WIDE_FORWARD.index(size) % 2, with_residual, pad=int(with_residual))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "bf16_acc", "f32_acc"])
+@pytest.mark.parametrize("size", WIDE_BACKWARD, ids=str)
+def test_wide_backward(ctx, size, kind):
+    check_backward(ctx, size, WIDE_BACKWARD.index(size) % 2, kind, pad=int(kind.endswith("acc")))
+
+
+LARGE = [(700, 136, 264), (3647, 1060, 1603)]
+
+
+@pytest.mark.parametrize("size", LARGE, ids=str)
+def test_rows_do_not_mix_in_large_products(ctx, size):
+    """NaN and infinities in a token's row stay in that row of the results, in tiles of many rows too."""
+    T, d, f = size
+    x, w = mat(T, d, 1), [mat(f, d, 2, 0.1), mat(f, d, 3, 0.1), mat(d, f, 4, 0.1)]
+    clean, dirty = mat(T, d, 5), mat(T, d, 6)
+    ctx.gated_ffn_forward(x, *w, clean)
+    x2 = mat(T, d, 1)
+    x2[1, 5], x2[T - 1, d - 1] = float("nan"), float("inf")
+    ctx.gated_ffn_forward(x2, *w, dirty)
+    keep = torch.ones(T, dtype=torch.bool, device="cuda")
+    keep[1] = keep[T - 1] = False
+    assert torch.equal(clean[keep], dirty[keep])
+    assert bool(torch.isnan(dirty[1].float()).all()) and not bool(torch.isfinite(dirty[T - 1].float()).any())
+
+
+@pytest.mark.parametrize("scale", [30.0, 3e4])
+def test_large_arguments_in_large_products(ctx, scale):
+    """Gates far out on both sides: the activation saturates without overflow or NaN."""
+    T, d, f = 700, 64, 128
+    for act in (0, 1):
+        x, w = mat(T, d, 1, scale), [mat(f, d, 2), mat(f, d, 3, 0.1), mat(d, f, 4, 0.1)]
+        y, gate, up = mat(T, d, 5), mat(T, f, 6), mat(T, f, 7)
+        ctx.gated_ffn_forward(x, *w, y, activation=act, gate=gate, up=up)
+        assert bool(torch.isfinite(y.float()).all())
+        dx, dws = mat(T, d, 8), [mat(f, d, 9), mat(f, d, 10), mat(d, f, 11)]
+        ctx.gated_ffn_backward(x, *w, gate, up, mat(T, d, 12), dx, *dws, activation=act)
+        assert all(bool(torch.isfinite(t.float()).all()) for t in (dx, *dws))
+
+
+def test_bounded_waits_of_wide_tiles_expire(dd, ctx):
+    """The test hook holds back the first copies of every launch: the waits run out, the status word says so,
+    and the next call on the same context is right."""
+    for (T, d, f), backward in ((WIDE_FORWARD[0], False), (WIDE_BACKWARD[0], True)):
+        x, w = mat(T, d, 1), [mat(f, d, 2, 0.1), mat(f, d, 3, 0.1), mat(d, f, 4, 0.1)]
+        y, gate, up = mat(T, d, 5), mat(T, f, 6), mat(T, f, 7)
+        dws = [mat(f, d, 9), mat(f, d, 10), mat(d, f, 11)]
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+        def call(flags):
+            if backward:
+                ctx.gated_ffn_backward(x, *w, gate, up, x, y, *dws, status=status, flags=flags)
+            else:
+                ctx.gated_ffn_forward(x, *w, y, status=status, flags=flags)
+
+        call(dd.DEBUG_EXPIRE_WAIT)
+        torch.cuda.synchronize()
+        assert status.tolist() == [dd.STATUS_WAIT_LIMIT]
+        status.zero_()
+        call(0)
+        assert status.tolist() == [0]
+        if not backward:
+            within(y, *forward64(x, *w, None, 0)[0], "after the expiry")
+            continue
+        for got, (ref, tol) in zip((y, *dws), backward64(x, *w, gate, up, x, 0)):
+            within(got, ref, tol * (1 + UB) + UB * ref.abs(), "after the expiry")
