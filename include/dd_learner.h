@@ -147,7 +147,8 @@ typedef struct {
  *   y         [device] bf16
  *   status    [device] NULL or a word that the call sets to DD_STATUS_WAIT_LIMIT if a bounded
  *             wait inside a kernel gave up (outputs are then unspecified); never cleared
- * Outputs overlap neither one another nor an input, y == residual excepted (DD_ERR_ALIAS).
+ * Outputs overlap neither one another nor an input, y == residual excepted (DD_ERR_ALIAS).  Matrices of
+ * one stride may lie side by side in the rows of one buffer (gate and up as its halves).
  */
 int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, const void *x, const void *residual,
                          void *gate, void *up, void *hidden, void *y, int32_t *status, void *cuda_stream);

@@ -335,20 +335,28 @@ static int ensure_ffn_scratch(dd_ctx *ctx, size_t bytes)
 
 // ---- arguments ---------------------------------------------------------------------------------
 
+// Rows of a matrix in memory, in bytes; no rows: touches nothing.
 struct Extent {
     const void *p;
-    size_t bytes;
+    size_t rows, width, pitch;
 };
 
 static Extent extent(const void *p, unsigned long long rows, unsigned long long cols, unsigned long long ld, size_t elem = 2)
 {
-    return Extent{p, p && rows ? (size_t)((rows - 1) * ld + cols) * elem : 0};
+    return Extent{p, p ? (size_t)rows : 0, (size_t)cols * elem, (size_t)ld * elem};
 }
 
+// Whether two matrices share a byte.  Rows of one pitch may lie side by side (gate and up as halves of one
+// buffer's rows); of different pitches whatever lies between the ends is taken.
 static bool touches(const Extent &a, const Extent &b)
 {
+    if (!a.rows || !b.rows) return false;
     const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
-    return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+    if (y < x) return touches(b, a);
+    if (y >= x + (a.rows - 1) * a.pitch + a.width) return false;
+    if (a.pitch != b.pitch) return true;
+    const size_t off = (y - x) % a.pitch;
+    return off < a.width || off + b.width > a.pitch;
 }
 
 static int set_stride(uint64_t &ld, uint64_t cols)
@@ -416,7 +424,7 @@ extern "C" int dd_gated_ffn_forward(dd_ctx *ctx, const dd_gated_ffn *block, cons
                  eu = extent(up, T, b.f, b.ld_gate), eh = extent(hidden, T, ldh, ldh), er = extent(residual, T, b.d, b.ld_y),
                  wg = extent(b.w_gate, b.f, b.d, b.ld_in), wu = extent(b.w_up, b.f, b.d, b.ld_in),
                  wd = extent(b.w_down, b.d, b.f, b.ld_down);
-    rc = check_alias({ey, eg, eu, eh}, {ex, wg, wu, wd, y == residual ? Extent{nullptr, 0} : er});
+    rc = check_alias({ey, eg, eu, eh}, {ex, wg, wu, wd, y == residual ? Extent{} : er});
     if (rc == DD_OK && y == residual) rc = check_alias({eg, eu, eh}, {er});
     if (rc != DD_OK) return rc;
     if (T == 0) return DD_OK;

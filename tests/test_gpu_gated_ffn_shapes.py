@@ -174,3 +174,49 @@ def test_bounded_waits_of_wide_tiles_expire(dd, ctx):
             continue
         for got, (ref, tol) in zip((y, *dws), backward64(x, *w, gate, up, x, 0)):
             within(got, ref, tol * (1 + UB) + UB * ref.abs(), "after the expiry")
+
+
+def halves(rows, cols, seeds, std=1.0, dtype=B):
+    """Two matrices side by side in the rows of one buffer, NaN between and behind them."""
+    wide = (cols + 7) // 8 * 8
+    buf = torch.full((rows, 2 * wide + 8), float("nan"), dtype=dtype, device="cuda")
+    pair = buf[:, :cols], buf[:, wide:wide + cols]
+    for t, seed in zip(pair, seeds):
+        t.copy_(mat(rows, cols, seed, std, dtype=dtype))
+    return buf, pair
+
+
+@pytest.mark.parametrize("size", [(1, 64, 64), (2, 40, 24), (37, 65, 131), (300, 136, 257), (900, 257, 333)], ids=str)
+def test_matrices_side_by_side(dd, ctx, size):
+    """gate and up, the two weights and their gradients as halves of one buffer's rows: the same bits as in
+    buffers of their own, and nothing between them is touched."""
+    T, d, f = size
+    x, dy = mat(T, d, 1), mat(T, d, 2)
+    own = [mat(f, d, 3, d ** -0.5), mat(f, d, 4, d ** -0.5), mat(d, f, 5, f ** -0.5)]
+    _, (wg, wu) = halves(f, d, (3, 4), d ** -0.5)
+    kept, (gate, up) = halves(T, f, (6, 7))
+    grads, (dwg, dwu) = halves(f, d, (8, 9))
+    y, y2, dx, dx2 = (mat(T, d, 10 + i) for i in range(4))
+    g2, u2, dwd, dwd2 = mat(T, f, 14), mat(T, f, 15), mat(d, f, 16), mat(d, f, 17)
+    dw2 = [mat(f, d, 18), mat(f, d, 19)]
+    ctx.gated_ffn_forward(x, wg, wu, own[2], y, gate=gate, up=up)
+    ctx.gated_ffn_forward(x, *own, y2, gate=g2, up=u2)
+    ctx.gated_ffn_backward(x, wg, wu, own[2], gate, up, dy, dx, dwg, dwu, dwd)
+    ctx.gated_ffn_backward(x, *own, g2, u2, dy, dx2, *dw2, dwd2)
+    for a, b in zip((y, gate, up, dx, dwg, dwu, dwd), (y2, g2, u2, dx2, *dw2, dwd2)):
+        assert torch.equal(a, b)
+    for buf, n in ((kept, f), (grads, d)):
+        wide = (n + 7) // 8 * 8
+        assert bool(torch.isnan(buf[:, n:wide].float()).all()) and bool(torch.isnan(buf[:, wide + n:].float()).all())
+    # one element into the neighbour: refused
+    if T > 1:
+        wide = (f + 7) // 8 * 8
+        flat = torch.zeros(T * 4 * wide, dtype=B, device="cuda")
+        a = flat.as_strided((T, f), (2 * wide, 1), 0)
+        for start in (wide - 8, 2 * wide - 8):
+            b = flat.as_strided((T, f), (2 * wide, 1), start)
+            if start >= f and start + f <= 2 * wide:
+                continue
+            with pytest.raises(dd.DDMergeError) as e:
+                ctx.gated_ffn_forward(x, *own, y, gate=a, up=b)
+            assert e.value.rc == dd.ERR_ALIAS
