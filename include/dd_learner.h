@@ -53,6 +53,11 @@ typedef struct {
  *   count     >= 0; lists of more than 256 tensors take one launch per 256
  *   max_norm  >= 0, may be infinite (scale 1)
  *   record    [device] 8-byte aligned, required
+ *
+ * The first norm, clip or recorded merge on a context allocates its workspace, which synchronises the
+ * device: make one before a stream capture.  No later norm or clip, of however many tensors, allocates.
+ * (A batched merge of many fragments may replace the workspace; graphs captured before then are not to
+ * be replayed.)
  */
 int dd_grad_norm(dd_ctx *ctx, const void *const *grads, const uint64_t *sizes, const uint8_t *dtypes,
                  int count, float max_norm, dd_grad_record *record, void *cuda_stream);

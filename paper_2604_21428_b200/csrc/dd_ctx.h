@@ -86,6 +86,9 @@ int fill_fragment(DevFrag &d, float *global, float *momentum, void *out_bf16,
                   const void *const *learner_ptrs, const uint64_t *tokens, const uint64_t *steps,
                   uint64_t mask, int K, uint64_t n, int M, size_t learner_bytes);
 int check_common(const dd_ctx *ctx, int M, dd_dtype dtype, float lr, float mu, uint32_t flags);
+// Partial sums that the workspace holds from its first allocation on: every single-fragment call (any M,
+// any flags, any of the library's grids) and every gradient norm.
+inline size_t first_workspace(const dd_ctx *ctx) { return (size_t)(kNumScalarDiag + DD_MAX_LEARNERS) * (size_t)ctx->sm_count * 4; }
 // Grows the diagnostics workspace to P x nq x grid partial sums (and P tickets).
 int ensure_workspace(dd_ctx *ctx, size_t P, size_t nq, size_t grid);
 

@@ -433,8 +433,12 @@ static int launch_norm(dd_ctx *ctx, const void *const *grads, const uint64_t *si
                        int count, float max_norm, dd_grad_record *record, bool again, cudaStream_t stream)
 {
     const size_t launches = count > CAP ? (size_t)(count + CAP - 1) / CAP : 1;
-    int rc = ensure_workspace(ctx, 1, 1, launches * ctx->sm_count * kListCtasPerSm);
+    int rc = ensure_workspace(ctx, 1, 1, launches);
     if (rc != DD_OK) return rc;
+    // The launches of a list share the first workspace, so that no list makes it grow: from 34 launches
+    // (8,449 tensors) on their grids shrink.
+    const size_t share = first_workspace(ctx) / launches;
+    const unsigned most = share < 1 ? 1 : share < 65536 ? (unsigned)share : 65536u;
     NormTail t;
     t.partials = ctx->partials;
     t.ticket = ctx->tickets;
@@ -450,7 +454,7 @@ static int launch_norm(dd_ctx *ctx, const void *const *grads, const uint64_t *si
             const unsigned eb = dtypes[i] == DD_BF16 ? 2 : 4;
             return head_of(p[0], eb, 16 / eb);
         });
-        const unsigned grid = list_grid(ctx, a.tiles);
+        const unsigned wanted = list_grid(ctx, a.tiles), grid = wanted < most ? wanted : most;
         t.last = at >= count;
         t.total = t.first + grid;
         if (again) {

@@ -223,8 +223,7 @@ int check_common(const dd_ctx *ctx, int M, dd_dtype dtype, float lr, float mu, u
 int ensure_workspace(dd_ctx *ctx, size_t P, size_t nq, size_t grid)
 {
     size_t need = P * nq * grid;
-    const size_t single_max = (size_t)(kNumScalarDiag + DD_MAX_LEARNERS) * (size_t)ctx->sm_count * 4;
-    if (need < single_max) need = single_max;
+    if (need < first_workspace(ctx)) need = first_workspace(ctx);
     if (need > ctx->partials_cap) {
         DD_CUDA(ctx, cudaDeviceSynchronize());
         if (ctx->partials) cudaFree(ctx->partials);
