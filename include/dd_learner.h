@@ -28,7 +28,8 @@ extern "C" {
 
 /* ---- gradient norm, clipping, AdamW over many tensors --------------------------------- */
 
-/* dd_grad_record.status beside DD_STATUS_OK: the norm is infinite or NaN. */
+/* dd_grad_record.status beside DD_STATUS_OK: the norm came out infinite or NaN (dd_grad_norm says from
+ * which finite elements on). */
 enum { DD_STATUS_NONFINITE = 4 };
 
 /* Written by the device; readable by the host once the stream has been synchronised. */
@@ -42,8 +43,12 @@ typedef struct {
 
 /*
  * norm = sqrt(sum over all tensors and elements of g^2), and the clip scale for max_norm.
- * Squares and the sums over up to 32 elements are taken in float32, everything beyond in
- * float64, in a fixed order (repeated calls give the same bits).
+ * Squares and the sums over up to 34 elements are taken in float32, everything beyond in
+ * float64, in a fixed order (repeated calls give the same bits).  Range: with every element below
+ * 3e18 no sum overflows; one element past 1.8e19 makes the norm infinite (DD_STATUS_NONFINITE), as an
+ * infinite element does.  norm_sq is within 34 x 2^-24 of itself plus 2^-149 for each element: squares
+ * below float32's normal range (elements below 1.1e-19) lose bits, and those of elements below
+ * 2.6e-23 count as 0.
  *
  *   grads     [host] count device pointers to contiguous tensors, aligned to their element
  *             (16-byte aligned tensors are read in 16-byte pieces)

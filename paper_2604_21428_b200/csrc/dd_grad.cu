@@ -167,7 +167,7 @@ __device__ __forceinline__ float tile_squares(const V *p, unsigned pieces, unsig
     return s;
 }
 
-// sum of g^2: fp32 over the 32 elements a thread takes of a tile (and 8 more at a tensor's ends),
+// sum of g^2: fp32 over the 32 elements a thread takes of a tile (and up to 2 more at a tensor's ends),
 // fp64 across tiles, threads and CTAs.  The CTA that draws the last ticket adds the partials in
 // index order, so the result does not depend on which one that is.
 // AGAIN: the clip reads everything once more, from the end.  The last 64 MB are then kept in L2 and
