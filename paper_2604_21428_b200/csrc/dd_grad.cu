@@ -170,9 +170,10 @@ __device__ __forceinline__ float tile_squares(const V *p, unsigned pieces, unsig
 // sum of g^2: fp32 over the 32 elements a thread takes of a tile (and up to 2 more at a tensor's ends),
 // fp64 across tiles, threads and CTAs.  The CTA that draws the last ticket adds the partials in
 // index order, so the result does not depend on which one that is.
-// AGAIN: the clip reads everything once more, from the end.  The last 64 MB are then kept in L2 and
-// the rest is marked to go first: 156 -> 148 us for 151M bf16, 294 -> 284 us for 151M fp32 (without
-// the marks, reading from the end gains nothing).
+// AGAIN: the clip reads everything once more, from the end.  The last 64 MB then keep L2's ordinary
+// priority and the rest is marked to go first: 156 -> 152 us for 151M bf16 (without the marks, reading from
+// the end gains nothing).  Marking the 64 MB to go last takes 150 but outlives the call: reading
+// 88 MB four times took 110 us after such a clip, 88 after this one, 84 after a norm alone.
 template <int CAP, bool AGAIN>
 __global__ void __launch_bounds__(kListThreads)
 grad_norm_kernel(const __grid_constant__ ListArgs<1, CAP> a, const __grid_constant__ NormTail t)
@@ -183,7 +184,7 @@ grad_norm_kernel(const __grid_constant__ ListArgs<1, CAP> a, const __grid_consta
     int i = 0;
     unsigned long long keep = 0, drop = 0;
     if (AGAIN) {
-        asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
+        asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(keep));
         asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(drop));
     }
     after_prior_launch();
