@@ -1,6 +1,7 @@
 // dd_gated_ffn_forward / dd_gated_ffn_backward: arguments, tensor maps and launches of the gated
 // feed-forward block.  Forward: one launch for gate, up and their product, one for the way down.
 // Backward: one launch for the gradients inside the block, one for dx and the three weights.
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -109,9 +110,10 @@ constexpr unsigned long long kStreamMaxTokens = 320;
 // Ring of a CTA: two CTAs share an SM.
 constexpr unsigned kStreamRing = 96 * 1024;
 
-// Kernels opt in to their shared memory once per process and device.
+// Kernels opt in to their shared memory once per process and device; contexts of several host threads may
+// come by at the same time (opting in twice does no harm).
 template <typename K>
-static int allow_smem(dd_ctx *ctx, K kernel, size_t bytes, bool (&done)[64])
+static int allow_smem(dd_ctx *ctx, K kernel, size_t bytes, std::atomic<bool> (&done)[64])
 {
     const int d = ctx->device;
     if (d < 64 && done[d]) return DD_OK;
@@ -150,7 +152,7 @@ template <int EPI, int BN, int ACT>
 static int launch_gemm_act(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
 {
     constexpr size_t smem = gemm_smem_bytes(EPI, BN);
-    static bool done[64];
+    static std::atomic<bool> done[64];
     const int rc = allow_smem(ctx, ffn_gemm_kernel<EPI, BN, ACT>, smem, done);
     if (rc != DD_OK) return rc;
     const unsigned most = (unsigned)ctx->sm_count / 2, pairs = a.tiles < most ? a.tiles : most;
@@ -255,7 +257,7 @@ static int launch_stream_act(dd_ctx *ctx, const StreamArgs &a, unsigned grid, cu
     cfg.blockDim = dim3(kStreamThreads);
     cfg.dynamicSmemBytes = stream_smem_bytes(a.cols, a.stages);
     cfg.stream = stream;
-    static bool done[64];
+    static std::atomic<bool> done[64];
     const int rc = allow_smem(ctx, ffn_stream_kernel<EPI, ACT>, kStreamRing + 2048, done);
     if (rc != DD_OK) return rc;
     cudaLaunchAttribute at[2];
