@@ -580,7 +580,6 @@ extern "C" int dd_gated_ffn_backward(dd_ctx *ctx, const dd_gated_ffn *block, con
         GemmArgs c = a;
         c.maps[0] = a.maps[kDy];
         c.maps[1] = a.maps[kWd];
-                    if (rc != DD_OK) return rc;
         GemmProblem &p = add_problem(c, T, b.f, 256, blocks_of(b.d, kBK));
         p.b_map[0] = 1;
         p.b_mn = 1;

@@ -160,7 +160,7 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
     __shared__ unsigned tmem_base;
     const unsigned full = smem_addr(bars), empty = full + 8 * kStreamMaxStages, done = empty + 8 * kStreamMaxStages;
     volatile int *abort = &abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5;
     const unsigned S = p.cluster, stages = p.stages, N = p.cols, stage_bytes = stream_stage_bytes(N);
     const unsigned tmem_cols = N <= 32 ? 32 : N <= 64 ? 64 : 128;
     const unsigned rank = blockIdx.x % S, tile = blockIdx.x / S;
