@@ -246,14 +246,17 @@ __device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&x)[4], uns
     }
 }
 
+// Addends are read past L1 (here and in load_share): the launch that runs beside the one before it
+// (GemmArgs::late_wait) adds to what an earlier launch wrote without a wait of its own, and a line that its
+// SM still held from then would be old.
 __device__ __forceinline__ void load4_f32(const float *p, float (&x)[4], unsigned live)
 {
     if (live >= 4) {
-        const float4 w = *reinterpret_cast<const float4 *>(p);
+        const float4 w = __ldcg(reinterpret_cast<const float4 *>(p));
         x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = i < live ? p[i] : 0.0f;
+        for (int i = 0; i < 4; ++i) x[i] = i < live ? __ldcg(p + i) : 0.0f;
     }
 }
 
@@ -412,12 +415,12 @@ __device__ __forceinline__ void load_share(uint4 (&w)[8], int lane, const __nv_b
         if (row >= m || !live) continue;
         const __nv_bfloat16 *src = in + (unsigned long long)row * ld + c;
         if (live >= 8) {
-            w[i] = *reinterpret_cast<const uint4 *>(src);
+            w[i] = __ldcg(reinterpret_cast<const uint4 *>(src));
         } else {
             unsigned u[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
             for (int k = 0; k < 7; ++k)
-                if (k < live) u[k / 2] |= (unsigned)reinterpret_cast<const unsigned short *>(src)[k] << (16 * (k & 1));
+                if (k < live) u[k / 2] |= (unsigned)__ldcg(reinterpret_cast<const unsigned short *>(src) + k) << (16 * (k & 1));
             w[i] = make_uint4(u[0], u[1], u[2], u[3]);
         }
     }

@@ -90,3 +90,32 @@ def test_block_reads_the_weights_of_the_step_before_it(dd, ctx, size, graph):
             assert torch.equal(p, q), (i, k)
     if graph:
         del captured
+
+
+@pytest.mark.parametrize("kind", [B, torch.float32])
+@pytest.mark.parametrize("size", [(1, 264, 520), (5, 72, 136), (130, 257, 131), (320, 1000, 312), (500, 264, 520)], ids=str)
+def test_gradients_accumulate_over_calls(dd, ctx, size, kind):
+    """Micro-batches one after the other into the same gradients, rows that end inside lines: the same bits as
+    with a synchronise after every call."""
+    tokens, d, f = size
+    rows = lambda n: (n + 7) // 8 * 8
+    gen = torch.Generator(device="cuda").manual_seed(9)
+
+    def mat(r, c, dtype=B, std=1.0):
+        return (torch.randn(r, rows(c), generator=gen, device="cuda") * std).to(dtype)[:, :c]
+
+    w = [mat(f, d), mat(f, d), mat(d, f)]
+    x, dy, gate, up, dx = mat(tokens, d), mat(tokens, d), mat(tokens, f), mat(tokens, f), mat(tokens, d)
+    start = [mat(f, d, kind), mat(f, d, kind), mat(d, f, kind)]
+    scratch = torch.zeros(3 * tokens * rows(f), dtype=B, device="cuda")
+    results = []
+    for between in (lambda: None, torch.cuda.synchronize):
+        dws = [mat(f, d, kind), mat(f, d, kind), mat(d, f, kind)]
+        for a, b in zip(dws, start):
+            a.copy_(b)
+        for _ in range(50):
+            ctx.gated_ffn_backward(x, *w, gate, up, dy, dx, *dws, accumulate=True, scratch=scratch)
+            between()
+        results.append([t.clone() for t in (dx, *dws)])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
