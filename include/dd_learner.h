@@ -141,7 +141,8 @@ typedef struct {
 /*
  * Memory: the first call of either direction on a context allocates 256 KB per SM (38 MB on a B200)
  * for partial products, which it keeps; no later call allocates unless `hidden` / `scratch` is NULL
- * and has to grow.  Make the first call before a stream capture.
+ * and has to grow.  Make the first call before a stream capture, and bring `hidden` / `scratch` to a
+ * captured call: a graph that was captured with NULL is not to be replayed once the context's has grown.
  *
  * gate = x w_gate^T,  up = x w_up^T,  y = [residual +] (a(gate) * up) w_down^T
  *

@@ -13,9 +13,10 @@
 // descriptor's "major" bit) -- so no product of the backward pass needs a transposed copy.
 //
 // What bounds it: at 8192 tokens, d 2048, f 8192 the operands come out of L2 at 10-13 TB/s (128 FLOP a
-// byte with BN = 256) with the tensor pipe 68-77 % active, under the 1000 W cap.  Forward 606 us in short
-// runs, 660 sustained; backward 1155 and 1280.  The same passes with the loads taken out after the
-// first ring take 473 us forward, with the products taken out 497.
+// byte with BN = 256) with the tensor pipe 68-77 % active, under the 1000 W cap.  Forward 606-624 us in short
+// runs, 660-716 back to back for seconds; backward 1155-1196 and 1280-1370 (GPUs differ; the library's bare
+// products 560 / 646 and 1130 / 1295 beside the larger of these).  With the loads taken out after the first
+// ring the forward pass takes 473 us, with the products taken out 497 (short runs).
 //
 // Every wait is bounded: on giving up a role raises its CTA's abort flag, the roles leave their
 // loops, copies and products in flight are awaited (again bounded), tensor memory is freed and

@@ -1,6 +1,7 @@
 // The block's products for few tokens: bound by streaming the weights, so the weights take the
-// 128-row side of the tensor-core tile and the tokens its N side (16 to 128 columns), and each
-// weight is read once per 128 tokens however few there are.  Gate and up share a tile: 64 rows each.
+// 128-row side of the tensor-core tile and the tokens its N side (16 to 128 columns).  Each weight is
+// read once per tile of tokens: up to 128 of them, fewer where SMs would be idle otherwise (the second
+// reading comes from L2).  Gate and up share a tile: 64 rows each.
 //
 // One CTA computes a tile over a share of K; the S CTAs of a cluster share one tile's K and add
 // their float32 partial sums through distributed shared memory in rank order, each rank finishing
@@ -12,7 +13,7 @@
 // the call may well write them -- an optimizer step that leaves the weights' bf16 copies -- so
 // the first launch lets the second one start only once its own wait for that launch is over.
 //
-// d 2048, f 8192, gate and up kept: 1 / 64 / 128 tokens 22 / 28 / 33 us forward, of which the 100.7 MB of
+// d 2048, f 8192, gate and up kept: 1 / 64 / 128 tokens 24 / 28 / 35 us forward, of which the 100.7 MB of
 // weights need 15.4; the rest is two launches' ramp, reduction and hand-over.  A ring of 64 KB took 27.0
 // against 24.4 (1 token) and 45 against 38 (128), clusters up to 296 CTAs 25.4 against 22.4, L2 prefetch of
 // what follows the ring 25.2 against 24.4.

@@ -15,8 +15,9 @@ namespace ddm {
 constexpr int kListThreads = 256;
 constexpr int kListTile = 8192;              // elements: 32 per thread
 constexpr int kListSmall = 32, kListMax = 256;
-// Measured at 4 / 8 CTAs of 256 threads per SM: norm of 1.2e9 bf16 375 / 342 us (7.07 TB/s), clip of 151M bf16
-// 156 / 150 us, AdamW on 151M with bf16 gradients and copies 698 / 673 us (6.29 TB/s).
+// CTAs of 256 threads launched per SM; registers let 6 / 5 / 5 of them run at a time (norm, scale, AdamW), the
+// rest follow as those end.  Measured at 4 / 6 / 8: norm of 1.2e9 bf16 453 / 365 / 407 us, clip of 151M bf16
+// 156 / 158 / 152 us, norm and AdamW on 151M fp32 876 / 912 / 828 us (one number for the three).
 constexpr int kListCtasPerSm = 8;
 constexpr unsigned char kNoVector = 255;
 constexpr unsigned kKeepBytes = 64u << 20;   // of a list that is read twice, kept in L2 (126 MB) from the first time

@@ -16,7 +16,8 @@ from . import ddmerge as dd
 
 
 class Learner:
-    """One learner's model, optimizer state and gradients."""
+    """One learner's model, optimizer state and gradients.  ``d`` and ``f`` are multiples of 8: the rows of a
+    fragment's matrices follow one another, and each starts on 16 bytes."""
 
     def __init__(self, ctx: "dd.Context", d: int, f: int, blocks: int, tokens: int, *, lr: float = 1e-3,
                  weight_decay: float = 0.0, max_norm: float = 1.0, activation: int = dd.ACT_SILU, device="cuda"):
