@@ -28,8 +28,8 @@ def attention(name, op, lengths, heads, kv_heads, dim, causal=True, tail=0, pack
                 causal=causal, tail=tail, packed=packed)
 
 
-def loss(name, op, tokens, d, vocab, grad="bf16"):
-    return dict(name=name, op=op, tokens=tokens, d=d, vocab=vocab, grad=grad)
+def loss(name, op, tokens, d, vocab):
+    return dict(name=name, op=op, tokens=tokens, d=d, vocab=vocab)
 
 
 def listed():
@@ -54,8 +54,8 @@ def listed():
         loss("loss_short", "loss_forward", 96, 768, 32000),
         # loss of a training micro-batch of a 1.3B-parameter decoder
         loss("loss_train", "loss_forward", 8192, 2048, 32000),
-        # gradients at odd sizes, the weight's in float32
-        loss("loss_back_odd", "loss_backward", 777, 1001, 5003, grad="f32"),
+        # gradients at odd sizes
+        loss("loss_back_odd", "loss_backward", 777, 1001, 5003),
         # gradients of the training micro-batch above
         loss("loss_back_train", "loss_backward", 8192, 2048, 32000),
     ]
@@ -93,7 +93,7 @@ def draw(rng):
                 d -= d % 8
             if tokens * d * vocab <= LARGEST["loss"] and d * vocab <= 2048 * 32000:
                 break
-        c = loss("", op, tokens, d, vocab, rng.choice(["bf16", "f32"]))
+        c = loss("", op, tokens, d, vocab)
     del c["name"]
     return c
 
@@ -122,7 +122,7 @@ def work(case):
     t, d, v = case["tokens"], case["d"], case["vocab"]
     if op == "loss_forward":
         return {"bytes": 2 * (t * d + v * d) + 16 * t, "flops": 2 * t * d * v}
-    return {"bytes": 2 * (2 * t * d + v * d) + (2 if case["grad"] == "bf16" else 4) * v * d + 16 * t, "flops": 6 * t * d * v}
+    return {"bytes": 4 * (t * d + v * d) + 16 * t, "flops": 6 * t * d * v}
 
 
 # ---- what a program has in hand --------------------------------------------------------------------
@@ -133,8 +133,8 @@ def randn(gen, *shape, std=1.0, dtype=torch.bfloat16):
     return x.mul_(std).to(dtype)[..., : shape[-1]]
 
 
-def empty(*shape, dtype=torch.bfloat16):
-    return torch.zeros(*shape[:-1], rows(shape[-1]), device="cuda", dtype=dtype)[..., : shape[-1]]
+def empty(*shape):
+    return torch.zeros(*shape[:-1], rows(shape[-1]), device="cuda", dtype=torch.bfloat16)[..., : shape[-1]]
 
 
 BASE, TRAINED = 10000.0, 4096      # angles' base, and the context that the frequencies were trained at
@@ -186,8 +186,6 @@ def prepare(case, seed):
             s["do"] = torch.randn(t, h, d, generator=gen, device="cuda").mul_(STD_GRAD).to(torch.bfloat16)
             dqkv = torch.zeros(t, h + 2 * kv, d, device="cuda", dtype=torch.bfloat16)
             s["dq"], s["dk"], s["dv"] = dqkv[:, :h], dqkv[:, h: h + kv], dqkv[:, h + kv:]
-        if own:
-            s["plan"] = library()[0].new_attention_plan(t, len(ls)) if case["packed"] else None
         return s
     t, d, v = case["tokens"], case["d"], case["vocab"]
     s["hidden"] = randn(gen, t, d)
@@ -198,8 +196,7 @@ def prepare(case, seed):
     if op == "loss_backward":
         loss_plain(s)                                                                          # what the forward pass kept
         s["dloss"] = torch.rand(t, generator=gen, device="cuda").add_(0.5).div_(t)             # weights of a mean
-        s["dhidden"] = empty(t, d)
-        s["dweight"] = empty(v, d, dtype=torch.bfloat16 if case["grad"] == "bf16" else torch.float32)
+        s["dhidden"], s["dweight"] = empty(t, d), empty(v, d)
     return s
 
 
@@ -226,44 +223,54 @@ def rotary_plain(s):
 
 
 def documents(s):
-    """For each document and each head of keys: its rows, the head, and the query heads that read it."""
-    c, a = s["case"], 0
-    group = c["heads"] // c["kv_heads"]
+    """The rows of each document."""
+    a = 0
     for n in s["lengths"]:
-        for j in range(c["kv_heads"] if n else 0):
-            yield slice(a, a + n), j, slice(j * group, (j + 1) * group)
+        if n:
+            yield slice(a, a + n)
         a += n
 
 
-def scores(s, rows_, j, heads):
-    q, k = s["q"][rows_, heads].float().transpose(0, 1), s["k"][rows_, j].float()
-    x = q @ k.t() * s["scale"]
+def heads_of(s, name, doc):
+    """Rows of one document in 32 bits, [heads of keys, query heads that read one (or 1), rows, dim]."""
+    x = s[name][doc].float().transpose(0, 1)
+    return x.reshape(s["case"]["kv_heads"], -1, *x.shape[1:])
+
+
+def scores(s, doc):
+    x = heads_of(s, "q", doc) @ heads_of(s, "k", doc).transpose(2, 3) * s["scale"]
     if s["case"]["causal"]:
-        i = torch.arange(k.shape[0], device=k.device)
+        i = torch.arange(x.shape[-1], device=x.device)
         x = x.masked_fill_(i[None, :] > i[:, None], -math.inf)
     return x
 
 
+def put(out, doc, x):
+    """Results of a document, laid out as heads_of() gives them, rounded into `out`."""
+    out[doc] = x.flatten(0, 1).transpose(0, 1).to(out.dtype)
+
+
 def attention_plain(s):
-    for rows_, j, heads in documents(s):
-        x = scores(s, rows_, j, heads)
+    for doc in documents(s):
+        x = scores(s, doc)
         top = x.amax(-1, keepdim=True)
         p = x.sub_(top).exp_()
         total = p.sum(-1, keepdim=True)
-        s["o"][rows_, heads] = ((p @ s["v"][rows_, j].float()) / total).transpose(0, 1).to(torch.bfloat16)
-        s["lse"][heads, rows_] = (top + total.log()).squeeze(-1)
+        put(s["o"], doc, p @ heads_of(s, "v", doc) / total)
+        s["lse"][:, doc] = (top + total.log()).reshape(-1, x.shape[-1])
     return s["o"], s["lse"]
 
 
 def attention_back_plain(s):
-    for rows_, j, heads in documents(s):
-        q, do, o = (s[n][rows_, heads].float().transpose(0, 1) for n in ("q", "do", "o"))
-        k, v = s["k"][rows_, j].float(), s["v"][rows_, j].float()
-        p = scores(s, rows_, j, heads).sub_(s["lse"][heads, rows_, None]).exp_()
-        s["dv"][rows_, j] = (p.transpose(1, 2) @ do).sum(0).to(torch.bfloat16)
-        ds = p * (do @ v.t() - (do * o).sum(-1, keepdim=True)) * s["scale"]
-        s["dq"][rows_, heads] = (ds @ k).transpose(0, 1).to(torch.bfloat16)
-        s["dk"][rows_, j] = (ds.transpose(1, 2) @ q).sum(0).to(torch.bfloat16)
+    for doc in documents(s):
+        p = scores(s, doc)
+        p = p.sub_(s["lse"][:, doc].reshape(*p.shape[:3], 1)).exp_()
+        q, k, v, do = (heads_of(s, name, doc) for name in ("q", "k", "v", "do"))
+        put(s["dv"], doc, (p.transpose(2, 3) @ do).sum(1, keepdim=True))
+        dp = do @ v.transpose(2, 3)
+        ds = p * (dp - (p * dp).sum(-1, keepdim=True)) * s["scale"]
+        put(s["dq"], doc, ds @ k)
+        put(s["dk"], doc, (ds.transpose(2, 3) @ q).sum(1, keepdim=True))
     return s["dq"], s["dk"], s["dv"]
 
 
@@ -314,12 +321,10 @@ def run_own(s):
                    magnitude=s["magnitude"], interleaved=c["layout"] == "interleaved", inverse=c["inverse"])
         return s["q_out"], s["k_out"]
     if c["op"].startswith("attention"):
-        if c["packed"]:
-            ctx.attention_plan(s["offsets"], s["q"].shape[0], s["plan"])       # a micro-batch has lengths of its own
         if c["op"] == "attention_forward":
-            ctx.attention_forward(s["q"], s["k"], s["v"], s["o"], s["lse"], plan=s["plan"], scale=s["scale"], causal=c["causal"])
+            ctx.attention_forward(s["q"], s["k"], s["v"], s["o"], s["lse"], offsets=s["offsets"], scale=s["scale"], causal=c["causal"])
             return s["o"], s["lse"]
-        ctx.attention_backward(s["q"], s["k"], s["v"], s["o"], s["lse"], s["do"], s["dq"], s["dk"], s["dv"], plan=s["plan"],
+        ctx.attention_backward(s["q"], s["k"], s["v"], s["o"], s["lse"], s["do"], s["dq"], s["dk"], s["dv"], offsets=s["offsets"],
                                scale=s["scale"], causal=c["causal"])
         return s["dq"], s["dk"], s["dv"]
     if c["op"] == "loss_forward":
