@@ -12,7 +12,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libddmerge.so")
 BINDING = os.path.join(PKG, "_ddtorch.so")
 SOURCES = ["dd_merge.cu", "dd_host_stream.cu", "dd_noalloc.cu", "dd_broadcast.cu", "dd_int4.cu", "dd_grad.cu",
-           "dd_ffn.cu", "dd_host.cpp"]
+           "dd_ffn.cu", "dd_rotary.cu", "dd_attention.cu", "dd_vocab_loss.cu", "dd_host.cpp"]
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
     "--shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v", "-cudart", "static", "--threads", "0",

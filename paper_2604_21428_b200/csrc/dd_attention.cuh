@@ -1,0 +1,859 @@
+// Attention over packed sequences on tcgen05: scores, weights and gradients of 128 x 128 tiles live in tensor
+// memory and registers, nothing of a tile's size goes to global memory.
+//
+// Roles of a CTA (384 threads): warps 0-7 compute on tiles (a thread owns a row of an accumulator, the
+// lane of tensor memory that it can reach), warp 8 has the TMA engine fill rings of operand tiles, warp 9 issues
+// the products; warps 8-11 give registers to the others (a warpgroup does so as a whole).  An operand tile is 128 tokens of one head: one or two boxes of 64 elements a row
+// (128-byte swizzle), columns past `dim` filled with zeros by the TMA engine.  Tiles may reach past their
+// sequence: scores there are masked, and rows that a product sums over are zeroed in shared memory
+// first, since a weight of 0 does not silence a NaN of the neighbour's.
+//
+// The weights p (and ds) go back into tensor memory as bf16 and are the A operand of the next product from
+// there, so they never pass through shared memory.
+//
+// Every wait is bounded, as in the block's products: on giving up a role raises the abort flag, the roles leave
+// their loops, copies and products in flight are awaited (again bounded), tensor memory is freed and the
+// status word says DD_STATUS_WAIT_LIMIT.
+#pragma once
+
+#include "dd_decoder.h"
+#include "dd_tcgen05.cuh"
+
+namespace ddm {
+
+constexpr int kTile = 128;                        // rows of a tile
+constexpr int kBoxTile = kTile * 128;             // bytes of a box: 128 rows of 64 bf16
+constexpr int kAttnThreads = 384, kAttnProducer = 8, kAttnIssuer = 9;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Tiles of all sequences, those with most work first.
+struct PlanItem {
+    unsigned start, len, tile, pad;               // the sequence's first token and length
+};
+
+struct Plan {
+    unsigned count, pad[3];
+    PlanItem item[1];
+};
+
+struct HeadsOut {
+    __nv_bfloat16 *data;
+    unsigned long long ld_token, ld_head;
+};
+
+struct AttnArgs {
+    CUtensorMap q, k, v, d_o;
+    const Plan *plan;                             // null: one sequence of all tokens
+    unsigned tokens, tiles;                       // tiles of that sequence
+    unsigned heads, group, dim;                   // query heads, query heads per head of keys
+    float scale;
+    int causal, expire;
+    HeadsOut o, dq, dk, dv;
+    float *lse;                                   // [heads][tokens]
+    const float *delta;                           // [heads][tokens]: d_o . o
+    int *status;
+};
+
+// ---- instructions ------------------------------------------------------------------------------
+
+__device__ __forceinline__ void tma_load_heads(unsigned dst, const CUtensorMap *map, int x, int head, int token, unsigned bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(head), "r"(token), "r"(bar) : "memory");
+}
+
+// A from tensor memory: bf16, two of a row's K elements per column.
+__device__ __forceinline__ void umma_bf16_ta(unsigned d, unsigned a, unsigned long long b, unsigned idesc, unsigned accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                 " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+__device__ __forceinline__ void tmem_st32(unsigned addr, const unsigned (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+        :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+           "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+           "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+           "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void init_bar(unsigned bar, unsigned count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void arrive_bar(unsigned bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+
+// Descriptors of operand tiles.  K contiguous: step k covers elements 16 k .. of every row.  Rows are K
+// (the tile's columns are N): step k covers rows 16 k .., the next 64 columns are one box on.
+__device__ __forceinline__ unsigned long long desc_rows(unsigned tile, int k)
+{
+    return umma_desc(tile + (k >> 2) * kBoxTile + (k & 3) * 32, false);
+}
+
+__device__ __forceinline__ unsigned long long desc_cols(unsigned tile, int k)
+{
+    const unsigned addr = tile + k * 2048;
+    return ((unsigned long long)(addr >> 4) & 0x3fff) | ((unsigned long long)(kBoxTile / 16) << 16) | ((unsigned long long)(1024 / 16) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+
+// float32 accumulators, bf16 operands, M = 128; b_mn: B's rows are K.
+__host__ __device__ constexpr unsigned attn_idesc(int n, bool b_mn)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn ? 1u << 16 : 0u) | ((unsigned)(n / 8) << 17) | ((unsigned)(kTile / 16) << 24);
+}
+
+// d (+)= A B^T over the tiles' DP columns.
+template <int DP>
+__device__ __forceinline__ void mma_rows(unsigned d, unsigned a, unsigned b)
+{
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) umma_bf16(d, desc_rows(a, k), desc_rows(b, k), attn_idesc(kTile, false), k != 0);
+}
+
+// d (+)= A B with A (128 x 128 bf16) in tensor memory, its columns 0-63 at `a` and 64-127 at `a` + HALF, and B a
+// tile's 128 rows of DP columns.
+template <int DP, int HALF>
+__device__ __forceinline__ void mma_weights(unsigned d, unsigned a, unsigned b, bool accumulate)
+{
+#pragma unroll
+    for (int k = 0; k < kTile / 16; ++k)
+        umma_bf16_ta(d, a + (k >> 2) * HALF + (k & 3) * 8, desc_cols(b, k), attn_idesc(DP, true), accumulate || k);
+}
+
+// One operand tile: tokens token .. token + 127 of a head.
+template <int DP>
+__device__ __forceinline__ void load_tile(unsigned dst, const CUtensorMap *map, int head, int token, unsigned bar)
+{
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c) tma_load_heads(dst + c * kBoxTile, map, 64 * c, head, token, bar);
+}
+
+// Zeros to the rows from `first` on; by one warp, for the products that it issues next.
+template <int DP>
+__device__ __forceinline__ void zero_rows(unsigned tile, unsigned first, int lane)
+{
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c)
+        for (unsigned r = first + (lane >> 3); r < kTile; r += 4)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" :: "r"(tile + c * kBoxTile + r * 128 + (lane & 7) * 16), "r"(0) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+
+// 32 columns of a row, times `by`, to bf16 columns col .. of an output row; dim is a multiple of 8.
+__device__ __forceinline__ void store_row32(__nv_bfloat16 *row, unsigned col, unsigned dim, const unsigned (&r)[32], float by)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (col + 8 * j >= dim) return;
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack2(__uint_as_float(r[8 * j + 2 * i]) * by, __uint_as_float(r[8 * j + 2 * i + 1]) * by);
+        *reinterpret_cast<uint4 *>(row + col + 8 * j) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// The tile of block-wide index `i`: most work first.  False: there is none.
+__device__ __forceinline__ bool plan_item(const AttnArgs &a, unsigned i, PlanItem &item)
+{
+    if (!a.plan) {
+        item = PlanItem{0u, a.tokens, a.tiles - 1 - i, 0u};
+        return i < a.tiles;
+    }
+    if (i >= a.plan->count) return false;
+    const uint4 w = __ldcg(reinterpret_cast<const uint4 *>(&a.plan->item[i]));
+    item = PlanItem{w.x, w.y, w.z, 0u};
+    return true;
+}
+
+// What all kernels begin and end with.
+struct AttnShared {
+    unsigned long long bars[24];
+    int abort_flag;
+    unsigned tmem_base;
+};
+
+__device__ __forceinline__ unsigned attn_begin(AttnShared &sh, int warp)
+{
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    if (warp == kAttnIssuer) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_addr(&sh.tmem_base)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    // only now: a launch behind this one would take the tensor memory and wait for this one's end
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    return sh.tmem_base;
+}
+
+__device__ __forceinline__ void attn_end(AttnShared &sh, const AttnArgs &a, int warp, unsigned tmem)
+{
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kAttnIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+    if (threadIdx.x == 0 && sh.abort_flag && a.status) *a.status = DD_STATUS_WAIT_LIMIT;
+}
+
+// The launch has 168 registers for each of 384 threads: 208 for two warpgroups and 88 for the third are as many.
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
+
+// Lane 0 of a warp reports that the warp is done with (or has written) its part of tensor memory.
+__device__ __forceinline__ void warp_arrive(unsigned bar, int lane)
+{
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) arrive_bar(bar);
+}
+
+// ---- forward ---------------------------------------------------------------------------------------
+
+// A CTA takes 256 query rows of a head: tile 0 and tile 1 of 128, warps 0-3 and 4-7.  They share every tile
+// of keys and values, and while the weights of one are computed the products of the other run.
+__host__ __device__ constexpr int fwd_stages(int dp) { return dp == 128 ? 4 : 6; }
+__host__ __device__ constexpr unsigned fwd_smem_bytes(int dp) { return 1024 + (2 + fwd_stages(dp)) * kTile * dp * 2; }
+
+template <int DP>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+attention_forward_kernel(const __grid_constant__ AttnArgs a)
+{
+    constexpr int kStages = fwd_stages(DP);
+    constexpr unsigned kBytes = kTile * DP * 2;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ alignas(16) AttnShared sh;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    PlanItem item;
+    if (!plan_item(a, blockIdx.x / a.heads, item)) return;
+    const unsigned head = blockIdx.x % a.heads, row0 = item.tile * 2 * kTile;
+    const unsigned rows = item.len - row0;                                  // from row0 on
+    // tiles of keys that each of the two needs
+    const unsigned all = (item.len + kTile - 1) / kTile, t0 = item.tile * 2;
+    const unsigned n0 = a.causal ? t0 + 1 : all, n1 = rows <= kTile ? 0 : a.causal ? t0 + 2 : all;
+    const unsigned n = n0 > n1 ? n0 : n1;
+
+    const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u, ring = smem + 2 * kBytes;
+    const unsigned bar = smem_addr(sh.bars), q_full = bar, full = bar + 8, empty = full + 8 * kStages, s_full = empty + 8 * kStages,
+                   p_full = s_full + 16, o_full = p_full + 16, drain = o_full + 16;
+    volatile int *abort = &sh.abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        sh.abort_flag = 0;
+        init_bar(q_full, 1);
+        for (int s = 0; s < kStages; ++s) {
+            init_bar(full + 8 * s, 1);
+            init_bar(empty + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            init_bar(s_full + 8 * s, 1);
+            init_bar(p_full + 8 * s, 4);
+            init_bar(o_full + 8 * s, 1);
+        }
+        init_bar(drain, 1);
+    }
+    const unsigned tmem = attn_begin(sh, warp);
+    const unsigned kS = tmem, kO = tmem + 2 * kTile;                         // scores of tile t at kS + 128 t, sums at kO + DP t
+
+    if (warp >= kAttnProducer) {
+        fewer_registers();
+        if (warp == kAttnProducer && elect_one()) {
+            const int token = (int)(item.start + row0), hk = (int)(head / a.group);
+            mbar_arrive_expect_tx(q_full, (n1 ? 2 : 1) * kBytes + (a.expire ? 16u : 0u));
+            load_tile<DP>(smem, &a.q, (int)head, token, q_full);
+            if (n1) load_tile<DP>(smem + kBytes, &a.q, (int)head, token + kTile, q_full);
+            unsigned it = 0;                                                 // keys 0, values 0, keys 1, ...
+            for (; it < 2 * n; ++it) {
+                const unsigned s = it % kStages;
+                if ((it >= kStages && !gemm_wait(empty + 8 * s, (it / kStages - 1) & 1, abort)) || *abort) break;
+                mbar_arrive_expect_tx(full + 8 * s, kBytes);
+                load_tile<DP>(ring + s * kBytes, it & 1 ? &a.v : &a.k, hk, (int)(item.start + (it >> 1) * kTile), full + 8 * s);
+            }
+            mbar_wait_bounded(q_full, 0);
+            for (unsigned j = it > kStages ? it - kStages : 0; j < it; ++j) mbar_wait_bounded(full + 8 * (j % kStages), (j / kStages) & 1);
+        } else if (warp == kAttnIssuer) {
+            const auto tile_of = [&](unsigned it) { return ring + it % kStages * kBytes; };
+            const auto ready = [&](unsigned it) { return gemm_wait(full + 8 * (it % kStages), (it / kStages) & 1, abort); };
+            bool ok = gemm_wait(q_full, 0, abort) && ready(0);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            if (ok && lane == 0) {
+                mma_rows<DP>(kS, smem, tile_of(0));
+                umma_commit(s_full);
+                if (n1) {
+                    mma_rows<DP>(kS + kTile, smem + kBytes, tile_of(0));
+                    umma_commit(s_full + 8);
+                }
+                umma_commit(empty);
+            }
+            for (unsigned j = 0; ok && j < n; ++j) {
+                const unsigned v = tile_of(2 * j + 1), live = item.len - j * kTile;
+                ok = ready(2 * j + 1);
+                if (ok && live < kTile) zero_rows<DP>(v, live, lane);
+                if (ok && j + 1 < n) ok = ready(2 * j + 2);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const unsigned mine = t ? n1 : n0;
+                    if (!ok || j >= mine) continue;
+                    ok = gemm_wait(p_full + 8 * t, j & 1, abort);
+                    tc_fence_after();
+                    if (!ok || lane) continue;
+                    mma_weights<DP, 32>(kO + t * DP, kS + t * kTile, v, j != 0);
+                    if (j + 1 < mine) {
+                        // behind the product that reads the weights, whose place the scores take
+                        mma_rows<DP>(kS + t * kTile, smem + t * kBytes, tile_of(2 * j + 2));
+                        umma_commit(s_full + 8 * t);
+                    } else {
+                        umma_commit(o_full + 8 * t);
+                    }
+                }
+                ok = __all_sync(0xffffffffu, ok);
+                if (ok && lane == 0) {
+                    umma_commit(empty + 8 * ((2 * j + 1) % kStages));
+                    if (j + 1 < n) umma_commit(empty + 8 * ((2 * j + 2) % kStages));
+                }
+            }
+            if (lane == 0) {
+                umma_commit(drain);                                              // no product may be in flight when tensor memory is freed
+                mbar_wait_bounded(drain, 0);
+            }
+        }
+    } else {
+        more_registers();
+        const int t = warp >> 2;
+        const unsigned mine = t ? n1 : n0, local = (warp & 3) * 32 + lane, row = row0 + t * kTile + local;
+        const unsigned at = (unsigned)((warp & 3) * 32) << 16, s_at = kS + t * kTile + at, o_at = kO + t * DP + at;
+        const float c = a.scale * kLog2e;
+        float top = -INFINITY, base = 0.0f, sum = 0.0f;                      // base: top, as the exponents use it
+        bool ok = true;
+        for (unsigned j = 0; j < mine; ++j) {
+            ok = gemm_wait(s_full + 8 * t, j & 1, abort);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            unsigned r[4][32];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32 * i, r[i]);
+            tmem_ld_wait();
+            const unsigned end = a.causal && row + 1 < item.len ? row + 1 : item.len, live = end > j * kTile ? end - j * kTile : 0;
+            if (__any_sync(0xffffffffu, live < kTile)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (32 * i + k >= live) r[i][k] = 0xff800000u;        // -infinity
+            }
+            float m[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                m[i] = __uint_as_float(r[i][0]);
+#pragma unroll
+                for (int k = 1; k < 32; ++k) m[i] = fmaxf(m[i], __uint_as_float(r[i][k]));
+            }
+            const float now = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+            // The sums are moved to a larger maximum only when it has grown by more than 2^8: until then the
+            // weights stay below 2^8, exact in float32 and as far from the end of bf16's range.
+            if (__any_sync(0xffffffffu, !((now - top) * c <= 8.0f))) {
+                const float next = now == -INFINITY ? 0.0f : now;
+                if (j) {
+                    const float by = exp2_fast((base - next) * c);
+                    sum *= by;
+#pragma unroll
+                    for (int i = 0; i < DP / 32; ++i) {
+                        unsigned o[32];
+                        tmem_ld32(o_at + 32 * i, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
+                        tmem_st32(o_at + 32 * i, o);
+                    }
+                }
+                top = now;
+                base = next;
+            }
+            const float off = -base * c;
+            float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                unsigned w[32];
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    const float p0 = exp2_fast(fmaf(__uint_as_float(r[2 * h + k / 16][2 * k % 32]), c, off)),
+                                p1 = exp2_fast(fmaf(__uint_as_float(r[2 * h + k / 16][2 * k % 32 + 1]), c, off));
+                    part[k & 1] += p0;
+                    part[2 + (k & 1)] += p1;
+                    w[k] = pack2(p0, p1);
+                }
+                tmem_st32(s_at + 32 * h, w);
+            }
+            sum += (part[0] + part[1]) + (part[2] + part[3]);
+            tmem_st_wait();
+            warp_arrive(p_full + 8 * t, lane);
+        }
+        if (mine && ok) ok = __all_sync(0xffffffffu, gemm_wait(o_full + 8 * t, 0, abort));
+        if (mine && ok) {
+            tc_fence_after();
+            const unsigned long long token = item.start + row;
+            const float by = 1.0f / sum;
+            __nv_bfloat16 *o = a.o.data + token * a.o.ld_token + head * a.o.ld_head;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) {
+                unsigned w[32];
+                tmem_ld32(o_at + 32 * i, w);
+                tmem_ld_wait();
+                if (row < item.len) store_row32(o, 32 * i, a.dim, w, by);
+            }
+            if (a.lse && row < item.len) a.lse[(unsigned long long)head * a.tokens + token] = fmaf(base, a.scale, logf(sum));
+        }
+    }
+    attn_end(sh, a, warp, tmem);
+}
+
+// ---- backward --------------------------------------------------------------------------------------
+
+// dq of 128 query rows of a head.  Warps 0-3 and 4-7 take 64 columns each of the scores' rows.  Scores of the
+// next tile of keys are made as soon as those of this one are in registers; ds alternates between two places.
+// Two launches (this and the next kernel) form the scores twice, which costs 7 products of a tile instead of 5,
+// but no gradient is added to by several CTAs: no atomics, no float32 copy of dq in memory.
+constexpr unsigned bwd_smem_bytes(int dp) { return 1024 + 6 * kTile * dp * 2; }
+
+template <int DP>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+attention_dq_kernel(const __grid_constant__ AttnArgs a)
+{
+    constexpr unsigned kBytes = kTile * DP * 2;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ alignas(16) AttnShared sh;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    PlanItem item;
+    if (!plan_item(a, blockIdx.x / a.heads, item)) return;
+    const unsigned head = blockIdx.x % a.heads, row0 = item.tile * kTile, all = (item.len + kTile - 1) / kTile;
+    const unsigned n = a.causal ? item.tile + 1 : all;
+
+    const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u, sq = smem, sdo = smem + kBytes, sk = smem + 2 * kBytes, sv = smem + 4 * kBytes;
+    const unsigned bar = smem_addr(sh.bars), q_full = bar, k_full = bar + 8, k_empty = bar + 24, v_full = bar + 40, v_empty = bar + 56,
+                   s_full = bar + 72, s_read = bar + 80, dp_full = bar + 88, ds_full = bar + 96, dq_full = bar + 104, drain = bar + 112;
+    volatile int *abort = &sh.abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        sh.abort_flag = 0;
+        for (int i = 0; i < 15; ++i) init_bar(bar + 8 * i, 1);
+        init_bar(s_read, 8);
+        init_bar(ds_full, 8);
+    }
+    const unsigned tmem = attn_begin(sh, warp);
+    const unsigned kS = tmem, kP = tmem + kTile, kDs = tmem + 2 * kTile, kDq = tmem + 3 * kTile;      // ds at kDs + 64 (j & 1)
+
+    if (warp >= kAttnProducer) {
+        fewer_registers();
+        if (warp == kAttnProducer && elect_one()) {
+            const int token = (int)(item.start + row0), hk = (int)(head / a.group);
+            mbar_arrive_expect_tx(q_full, 2 * kBytes + (a.expire ? 16u : 0u));
+            load_tile<DP>(sq, &a.q, (int)head, token, q_full);
+            load_tile<DP>(sdo, &a.d_o, (int)head, token, q_full);
+            unsigned it = 0;
+            for (; it < 2 * n; ++it) {                                       // keys 0, values 0, keys 1, ...
+                const unsigned j = it >> 1, s = j & 1, full = (it & 1 ? v_full : k_full) + 8 * s, empty = (it & 1 ? v_empty : k_empty) + 8 * s;
+                if ((j >= 2 && !gemm_wait(empty, (j / 2 - 1) & 1, abort)) || *abort) break;
+                mbar_arrive_expect_tx(full, kBytes);
+                load_tile<DP>((it & 1 ? sv : sk) + s * kBytes, it & 1 ? &a.v : &a.k, hk, (int)(item.start + j * kTile), full);
+            }
+            mbar_wait_bounded(q_full, 0);
+            for (unsigned i = it > 4 ? it - 4 : 0; i < it; ++i)
+                mbar_wait_bounded((i & 1 ? v_full : k_full) + 8 * ((i >> 1) & 1), (i >> 2) & 1);
+        } else if (warp == kAttnIssuer) {
+            // scores of tile j; the rows that dq sums over later are zeroed here already
+            const auto scores = [&](unsigned j) {
+                const unsigned k = sk + (j & 1) * kBytes, live = item.len - j * kTile;
+                if (!__all_sync(0xffffffffu, gemm_wait(k_full + 8 * (j & 1), (j >> 1) & 1, abort))) return false;
+                if (live < kTile) zero_rows<DP>(k, live, lane);
+                tc_fence_after();
+                if (lane == 0) {
+                    mma_rows<DP>(kS, sq, k);
+                    umma_commit(s_full);
+                }
+                return true;
+            };
+            const auto weights = [&](unsigned j) {                               // dp of tile j
+                if (!__all_sync(0xffffffffu, gemm_wait(v_full + 8 * (j & 1), (j >> 1) & 1, abort))) return false;
+                tc_fence_after();
+                if (lane == 0) {
+                    mma_rows<DP>(kP, sdo, sv + (j & 1) * kBytes);
+                    umma_commit(dp_full);
+                    umma_commit(v_empty + 8 * (j & 1));
+                }
+                return true;
+            };
+            bool ok = __all_sync(0xffffffffu, gemm_wait(q_full, 0, abort)) && scores(0) && weights(0);
+            for (unsigned j = 0; ok && j < n; ++j) {
+                ok = __all_sync(0xffffffffu, gemm_wait(s_read, j & 1, abort));
+                if (ok && j + 1 < n) ok = scores(j + 1);
+                if (ok) ok = __all_sync(0xffffffffu, gemm_wait(ds_full, j & 1, abort));
+                if (ok && j + 1 < n) ok = weights(j + 1);
+                if (!ok) break;
+                tc_fence_after();
+                if (lane == 0) {
+                    mma_weights<DP, 32>(kDq, kDs + 64 * (j & 1), sk + (j & 1) * kBytes, j != 0);
+                    umma_commit(j + 1 < n ? k_empty + 8 * (j & 1) : dq_full);
+                }
+            }
+            if (lane == 0) {
+                umma_commit(drain);
+                mbar_wait_bounded(drain, 0);
+            }
+        }
+    } else {
+        more_registers();
+        const unsigned half = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16, row = row0 + (warp & 3) * 32 + lane;
+        const unsigned long long token = item.start + row, stat = (unsigned long long)head * a.tokens + token;
+        const float c = a.scale * kLog2e;
+        const float off = row < item.len ? -a.lse[stat] * kLog2e : 0.0f, delta = row < item.len ? a.delta[stat] : 0.0f;
+        // columns below `end` count; a token that sees itself alone has ds = 0
+        const unsigned end = row >= item.len ? 0 : a.causal ? row + 1 : item.len;
+        bool ok = true;
+        for (unsigned j = 0; j < n; ++j) {
+            ok = __all_sync(0xffffffffu, gemm_wait(s_full, j & 1, abort));
+            if (!ok) break;
+            tc_fence_after();
+            unsigned r[2][32];
+            float p[2][32];
+            tmem_ld32(kS + at + 64 * half, r[0]);
+            tmem_ld32(kS + at + 64 * half + 32, r[1]);
+            tmem_ld_wait();
+            warp_arrive(s_read, lane);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int k = 0; k < 32; ++k) p[h][k] = exp2_fast(fmaf(__uint_as_float(r[h][k]), c, off));
+            ok = __all_sync(0xffffffffu, gemm_wait(dp_full, j & 1, abort));
+            if (!ok) break;
+            tc_fence_after();
+            tmem_ld32(kP + at + 64 * half, r[0]);
+            tmem_ld32(kP + at + 64 * half + 32, r[1]);
+            tmem_ld_wait();
+            const unsigned first = j * kTile + 64 * half, live = end == 1 || end <= first ? 0 : end - first;
+            const bool masked = __any_sync(0xffffffffu, live < 64);
+            unsigned w[32];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    float d0 = p[h][2 * k] * (__uint_as_float(r[h][2 * k]) - delta), d1 = p[h][2 * k + 1] * (__uint_as_float(r[h][2 * k + 1]) - delta);
+                    if (masked) {
+                        if (32 * h + 2 * k >= live) d0 = 0.0f;
+                        if (32 * h + 2 * k + 1 >= live) d1 = 0.0f;
+                    }
+                    w[16 * h + k] = pack2(d0, d1);
+                }
+            tmem_st32(kDs + at + 64 * (j & 1) + 32 * half, w);
+            tmem_st_wait();
+            warp_arrive(ds_full, lane);
+        }
+        if (ok) ok = __all_sync(0xffffffffu, gemm_wait(dq_full, 0, abort));
+        if (ok) {
+            tc_fence_after();
+            __nv_bfloat16 *o = a.dq.data + token * a.dq.ld_token + head * a.dq.ld_head;
+#pragma unroll
+            for (int i = 0; i < DP / 64; ++i) {
+                unsigned w[32];
+                const unsigned col = half * (DP / 2) + 32 * i;
+                tmem_ld32(kDq + at + col, w);
+                tmem_ld_wait();
+                if (row < item.len) store_row32(o, col, a.dim, w, a.scale);
+            }
+        }
+    }
+    attn_end(sh, a, warp, tmem);
+}
+
+// dk and dv of 128 rows of a head of keys, over the query heads that share it and their tiles of queries.
+// Scores are made transposed (rows are keys), so that the weights are the A operand of both products as they lie.
+// Products and weights alternate on the same places: dv of a tile, then the next tile's scores, run while ds
+// is computed; dk and the next dp while the next weights are.
+template <int DP>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+attention_dkv_kernel(const __grid_constant__ AttnArgs a)
+{
+    constexpr unsigned kBytes = kTile * DP * 2;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ alignas(16) AttnShared sh;
+    __shared__ alignas(16) float2 stats[2][kTile];                           // -lse log2(e) and delta of a tile's queries
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const unsigned kv_heads = a.heads / a.group;
+    PlanItem item;
+    if (!plan_item(a, blockIdx.x / kv_heads, item)) return;
+    const unsigned hk = blockIdx.x % kv_heads, all = (item.len + kTile - 1) / kTile;
+    const unsigned tile = all - 1 - item.tile, row0 = tile * kTile;          // early keys are read by most queries
+    const unsigned i0 = a.causal ? tile : 0, per = all - i0, n = per * a.group;
+
+    const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u, sk = smem, sv = smem + kBytes, sq = smem + 2 * kBytes, sdo = smem + 4 * kBytes;
+    const unsigned bar = smem_addr(sh.bars), kv_full = bar, q_full = bar + 8, q_empty = bar + 24, do_full = bar + 40, do_empty = bar + 56,
+                   s_full = bar + 72, p_full = bar + 80, dp_full = bar + 88, ds_full = bar + 96, done = bar + 104, drain = bar + 112, st_full = bar + 120;
+    volatile int *abort = &sh.abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        sh.abort_flag = 0;
+        for (int i = 0; i < 16; ++i) init_bar(bar + 8 * i, 1);
+        init_bar(p_full, 8);
+        init_bar(ds_full, 8);
+        init_bar(st_full, 8);
+    }
+    const unsigned tmem = attn_begin(sh, warp);
+    const unsigned kS = tmem, kP = tmem + kTile, kDv = tmem + 2 * kTile, kDk = kDv + DP;
+
+    if (warp >= kAttnProducer) {
+        fewer_registers();
+        if (warp == kAttnProducer && elect_one()) {
+            mbar_arrive_expect_tx(kv_full, 2 * kBytes + (a.expire ? 16u : 0u));
+            load_tile<DP>(sk, &a.k, (int)hk, (int)(item.start + row0), kv_full);
+            load_tile<DP>(sv, &a.v, (int)hk, (int)(item.start + row0), kv_full);
+            unsigned it = 0;
+            for (; it < 2 * n; ++it) {                                       // queries 0, gradients 0, queries 1, ...
+                const unsigned j = it >> 1, s = j & 1, full = (it & 1 ? do_full : q_full) + 8 * s, empty = (it & 1 ? do_empty : q_empty) + 8 * s;
+                const int h = (int)(hk * a.group + j / per), token = (int)(item.start + (i0 + j % per) * kTile);
+                if ((j >= 2 && !gemm_wait(empty, (j / 2 - 1) & 1, abort)) || *abort) break;
+                mbar_arrive_expect_tx(full, kBytes);
+                load_tile<DP>((it & 1 ? sdo : sq) + s * kBytes, it & 1 ? &a.d_o : &a.q, h, token, full);
+            }
+            mbar_wait_bounded(kv_full, 0);
+            for (unsigned i = it > 4 ? it - 4 : 0; i < it; ++i)
+                mbar_wait_bounded((i & 1 ? do_full : q_full) + 8 * ((i >> 1) & 1), (i >> 2) & 1);
+        } else if (warp == kAttnIssuer) {
+            // the product of keys (values) with tile j of queries (their gradients), whose rows past the sequence's end
+            // are summed over later
+            const auto product = [&](unsigned j, bool second) {
+                const unsigned s = j & 1, t = (second ? sdo : sq) + s * kBytes, live = item.len - (i0 + j % per) * kTile;
+                if (!__all_sync(0xffffffffu, gemm_wait((second ? do_full : q_full) + 8 * s, (j >> 1) & 1, abort))) return false;
+                if (live < kTile) zero_rows<DP>(t, live, lane);
+                tc_fence_after();
+                if (lane == 0) {
+                    mma_rows<DP>(second ? kP : kS, second ? sv : sk, t);
+                    umma_commit(second ? dp_full : s_full);
+                }
+                return true;
+            };
+            bool ok = __all_sync(0xffffffffu, gemm_wait(kv_full, 0, abort)) && product(0, false) && product(0, true);
+            for (unsigned j = 0; ok && j < n; ++j) {
+                const unsigned s = j & 1;
+                ok = __all_sync(0xffffffffu, gemm_wait(p_full, j & 1, abort));
+                if (!ok) break;
+                tc_fence_after();
+                if (lane == 0) {
+                    mma_weights<DP, 64>(kDv, kS, sdo + s * kBytes, j != 0);
+                    umma_commit(do_empty + 8 * s);
+                }
+                if (j + 1 < n) ok = product(j + 1, false);
+                if (ok) ok = __all_sync(0xffffffffu, gemm_wait(ds_full, j & 1, abort));
+                if (!ok) break;
+                tc_fence_after();
+                if (lane == 0) {
+                    mma_weights<DP, 64>(kDk, kP, sq + s * kBytes, j != 0);
+                    umma_commit(q_empty + 8 * s);
+                }
+                if (j + 1 < n) ok = product(j + 1, true);
+            }
+            if (lane == 0) {
+                if (ok) umma_commit(done);
+                umma_commit(drain);
+                mbar_wait_bounded(drain, 0);
+            }
+        }
+    } else {
+        more_registers();
+        const unsigned half = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16, row = row0 + (warp & 3) * 32 + lane;
+        const float c = a.scale * kLog2e;
+        // this thread's share of the statistics: lse or delta of one query of tile j
+        const auto stat = [&](unsigned j) {
+            const unsigned i = (i0 + j % per) * kTile + (threadIdx.x & 127), h = hk * a.group + j / per;
+            if (i >= item.len) return 0.0f;
+            const unsigned long long where = (unsigned long long)h * a.tokens + item.start + i;
+            return half ? a.delta[where] : -a.lse[where] * kLog2e;
+        };
+        float next = stat(0);
+        bool ok = true;
+        for (unsigned j = 0; j < n; ++j) {
+            float *put = reinterpret_cast<float *>(&stats[j & 1][threadIdx.x & 127]) + half;
+            *put = next;
+            __syncwarp();
+            if (lane == 0) arrive_bar(st_full);
+            if (j + 1 < n) next = stat(j + 1);
+            const unsigned q0 = (i0 + j % per) * kTile + 64 * half;           // the first of this warp's 64 queries
+            // queries from `from` to `to` count
+            const unsigned to = item.len > q0 ? item.len - q0 : 0, from = a.causal && row > q0 ? row - q0 : 0;
+            const bool masked = __any_sync(0xffffffffu, to < 64 || from > 0) || (a.causal && q0 == 0);
+            ok = gemm_wait(st_full, j & 1, abort) && gemm_wait(s_full, j & 1, abort);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            const float4 *st = reinterpret_cast<const float4 *>(&stats[j & 1][64 * half]);     // two queries each
+            unsigned r[2][32], w[32];
+            float p[2][32];
+            tmem_ld32(kS + at + 64 * half, r[0]);
+            tmem_ld32(kS + at + 64 * half + 32, r[1]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const float4 x = st[16 * h + k];
+                    float p0 = exp2_fast(fmaf(__uint_as_float(r[h][2 * k]), c, x.x)), p1 = exp2_fast(fmaf(__uint_as_float(r[h][2 * k + 1]), c, x.z));
+                    if (masked) {
+                        const unsigned i = 32 * h + 2 * k;
+                        if (i < from || i >= to) p0 = 0.0f;
+                        if (i + 1 < from || i + 1 >= to) p1 = 0.0f;
+                    }
+                    p[h][2 * k] = p0;
+                    p[h][2 * k + 1] = p1;
+                    w[16 * h + k] = pack2(p0, p1);
+                }
+            tmem_st32(kS + at + 64 * half, w);
+            tmem_st_wait();
+            warp_arrive(p_full, lane);
+            ok = __all_sync(0xffffffffu, gemm_wait(dp_full, j & 1, abort));
+            if (!ok) break;
+            tc_fence_after();
+            tmem_ld32(kP + at + 64 * half, r[0]);
+            tmem_ld32(kP + at + 64 * half + 32, r[1]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const float4 x = st[16 * h + k];
+                    float d0 = p[h][2 * k] * (__uint_as_float(r[h][2 * k]) - x.y), d1 = p[h][2 * k + 1] * (__uint_as_float(r[h][2 * k + 1]) - x.w);
+                    if (masked) {
+                        // a dp past the sequence's end may be NaN; a token that sees itself alone has ds = 0
+                        const unsigned i = 32 * h + 2 * k;
+                        if (i < from || i >= to || (a.causal ? q0 + i == 0 : item.len == 1)) d0 = 0.0f;
+                        if (i + 1 < from || i + 1 >= to) d1 = 0.0f;
+                    }
+                    w[16 * h + k] = pack2(d0, d1);
+                }
+            tmem_st32(kP + at + 64 * half, w);
+            tmem_st_wait();
+            warp_arrive(ds_full, lane);
+        }
+        if (ok) ok = __all_sync(0xffffffffu, gemm_wait(done, 0, abort));
+        if (ok) {
+            tc_fence_after();
+            const HeadsOut &out = half ? a.dk : a.dv;
+            __nv_bfloat16 *o = out.data + (unsigned long long)(item.start + row) * out.ld_token + hk * out.ld_head;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) {
+                unsigned w[32];
+                tmem_ld32((half ? kDk : kDv) + at + 32 * i, w);
+                tmem_ld_wait();
+                if (row < item.len) store_row32(o, 32 * i, a.dim, w, half ? a.scale : 1.0f);
+            }
+        }
+    }
+    attn_end(sh, a, warp, tmem);
+}
+
+// delta = d_o . o of every row of every head; LANES = lanes of a row, 8 elements each.
+struct DeltaArgs {
+    const __nv_bfloat16 *o, *d_o;
+    unsigned long long o_token, o_head, d_token, d_head;
+    float *delta;
+    unsigned tokens, heads, dim;
+};
+
+template <int LANES>
+__global__ void __launch_bounds__(256)
+attention_delta_kernel(const DeltaArgs a)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const unsigned long long i = ((unsigned long long)blockIdx.x * 256 + threadIdx.x) / LANES, rows = (unsigned long long)a.tokens * a.heads;
+    const unsigned col = threadIdx.x % LANES * 8;
+    const unsigned long long t = i / a.heads;
+    const unsigned h = (unsigned)(i - t * a.heads);
+    float sum = 0.0f;
+    if (i < rows && col < a.dim) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(a.o + t * a.o_token + h * a.o_head + col),
+                    y = *reinterpret_cast<const uint4 *>(a.d_o + t * a.d_token + h * a.d_head + col);
+        const unsigned u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sum = fmaf(__uint_as_float(u[k] << 16), __uint_as_float(v[k] << 16), sum);
+            sum = fmaf(__uint_as_float(u[k] & 0xffff0000u), __uint_as_float(v[k] & 0xffff0000u), sum);
+        }
+    }
+#pragma unroll
+    for (int s = LANES / 2; s; s /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+    if (i < rows && col == 0) a.delta[(unsigned long long)h * a.tokens + t] = sum;
+}
+
+// ---- plan ------------------------------------------------------------------------------------------
+
+constexpr unsigned kPlanKeys = 4096, kPlanThreads = 1024;
+
+// The tiles of `rows` tokens of all sequences, ordered by their place in the sequence, last first (by counting;
+// the order among tiles of one place does not matter to any result).
+__global__ void __launch_bounds__(kPlanThreads)
+attention_plan_kernel(const int *offsets, unsigned sequences, unsigned tokens, unsigned rows, Plan *plan, int *status)
+{
+    __shared__ unsigned count[kPlanKeys], warp_sum[32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    bool good = offsets[0] >= 0;
+    for (unsigned s = threadIdx.x; s < sequences; s += kPlanThreads)
+        good = good && offsets[s] <= offsets[s + 1] && (unsigned)offsets[s + 1] <= tokens;
+    for (unsigned i = threadIdx.x; i < kPlanKeys; i += kPlanThreads) count[i] = 0;
+    if (!__syncthreads_and(good)) {
+        if (threadIdx.x == 0) {
+            plan->count = 0;
+            if (status) *status = DD_STATUS_BAD_OFFSETS;
+        }
+        return;
+    }
+    unsigned shift = 0;
+    while ((tokens / rows) >> shift >= kPlanKeys) ++shift;
+    const auto key = [&](unsigned tile) { return kPlanKeys - 1 - (tile >> shift); };
+    const auto each = [&](auto &&f) {
+        for (unsigned s = warp; s < sequences; s += kPlanThreads / 32) {
+            const unsigned start = (unsigned)offsets[s], len = (unsigned)offsets[s + 1] - start;
+            for (unsigned t = lane; (unsigned long long)t * rows < len; t += 32) f(start, len, t);
+        }
+    };
+    each([&](unsigned, unsigned, unsigned t) { atomicAdd(&count[key(t)], 1u); });
+    __syncthreads();
+    unsigned mine[kPlanKeys / kPlanThreads], sum = 0;
+    for (unsigned i = 0; i < kPlanKeys / kPlanThreads; ++i) sum += mine[i] = count[threadIdx.x * (kPlanKeys / kPlanThreads) + i];
+    unsigned before = sum;
+    for (int d = 1; d < 32; d *= 2) {
+        const unsigned x = __shfl_up_sync(0xffffffffu, before, d);
+        if (lane >= d) before += x;
+    }
+    if (lane == 31) warp_sum[warp] = before;
+    __syncthreads();
+    unsigned base = 0;
+    for (unsigned w = 0; w < warp; ++w) base += warp_sum[w];
+    base += before - sum;
+    if (threadIdx.x == kPlanThreads - 1) plan->count = base + sum;
+    for (unsigned i = 0; i < kPlanKeys / kPlanThreads; ++i) {
+        count[threadIdx.x * (kPlanKeys / kPlanThreads) + i] = base;
+        base += mine[i];
+    }
+    __syncthreads();
+    each([&](unsigned start, unsigned len, unsigned t) { plan->item[atomicAdd(&count[key(t)], 1u)] = PlanItem{start, len, t, 0u}; });
+}
+
+}  // namespace ddm

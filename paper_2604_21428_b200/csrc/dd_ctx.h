@@ -43,6 +43,8 @@ struct dd_ctx {
     void *ffn_scratch = nullptr;              // intermediates of the gated feed-forward block
     size_t ffn_scratch_cap = 0;               // bytes
     float *ffn_slabs = nullptr;               // float32 partial products of split tiles
+    void *decoder_scratch = nullptr;          // plans, row statistics and pieces of dd_decoder.h
+    size_t decoder_scratch_cap = 0;           // bytes
     ddm::HostPipe *pipe = nullptr;
     char cuda_err[256] = {0};
 };

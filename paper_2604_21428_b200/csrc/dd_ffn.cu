@@ -1,104 +1,12 @@
 // dd_gated_ffn_forward / dd_gated_ffn_backward: arguments, tensor maps and launches of the gated
 // feed-forward block.  Forward: one launch for gate, up and their product, one for the way down.
 // Backward: one launch for the gradients inside the block, one for dx and the three weights.
-#include <atomic>
 #include <cmath>
-#include <cstring>
 
-#include "dd_ctx.h"
 #include "dd_ffn_stream.cuh"
+#include "dd_gemm_launch.cuh"
 
 namespace ddm {
-
-constexpr unsigned long long kFfnMax = 1ull << 30;
-
-typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's tensor map encoder, found through the runtime (the library does not link libcuda).
-static EncodeTiled tensor_map_encoder()
-{
-    static const EncodeTiled fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            return (EncodeTiled) nullptr;
-        }
-        return (EncodeTiled)p;
-    }();
-    return fn;
-}
-
-struct Matrix {
-    const void *data;
-    unsigned long long rows, cols, ld;      // bf16 elements
-};
-
-static int encode(dd_ctx *ctx, CUtensorMap *map, const Matrix &m, unsigned box_rows = 64)
-{
-    const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * 2};
-    const cuuint32_t box[2] = {64, box_rows}, step[2] = {1, 1};
-    const EncodeTiled fn = tensor_map_encoder();
-    if (!fn || fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(m.data), dims, strides, box, step,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
-        snprintf(ctx->cuda_err, sizeof ctx->cuda_err, "cuTensorMapEncodeTiled failed");
-        return DD_ERR_CUDA;
-    }
-    return DD_OK;
-}
-
-static unsigned blocks_of(unsigned long long n, unsigned b) { return (unsigned)((n + b - 1) / b); }
-
-// Adds a problem of m x n outputs in tiles of 256 x cols with its K blocks; the rest is set by the caller.
-static GemmProblem &add_problem(GemmArgs &a, unsigned long long m, unsigned long long n, int cols, unsigned k1, unsigned k2 = 0,
-                                unsigned splits = 1)
-{
-    GemmProblem &p = a.prob[a.nprob++];
-    std::memset(&p, 0, sizeof p);
-    p.m = (unsigned)m;
-    p.n = (unsigned)n;
-    p.tiles_m = blocks_of(m, 2 * kBM);
-    p.tiles_n = blocks_of(n, cols);
-    p.kblocks[0] = k1;
-    p.kblocks[1] = k2;
-    p.splits = splits;
-    p.split_rows = p.tiles_m * 2 * kBM;
-    a.tiles += p.tiles_m * p.tiles_n * splits;
-    p.tile_end = a.tiles;
-    return p;
-}
-
-// Float32 slabs of split products: 256 KB for each of two tiles per pair of SMs.
-static size_t slab_bytes(const dd_ctx *ctx) { return (size_t)ctx->sm_count * (2 * kBM) * 256 * 4; }
-
-// Splits of a launch's first problem: `tiles` tiles of `blocks` K blocks, beside `other` K blocks of
-// further problems.  Alone, the number that makes the fewest waves of the shortest units (a unit's
-// epilogue counts as 10 blocks, the launch that adds the splits up as 8); with others to fill the
-// gaps, the smallest one whose units are no longer than what each pair has to do anyway.
-static unsigned choose_splits(const dd_ctx *ctx, unsigned tiles, unsigned blocks, unsigned long long other)
-{
-    const unsigned pairs = (unsigned)ctx->sm_count / 2;
-    const unsigned long long share = ((unsigned long long)tiles * blocks + other) / pairs + 1;
-    unsigned best = 1;
-    unsigned long long least = ~0ull;
-    for (unsigned s = 1; s <= kMaxSplits && (s == 1 || (tiles * s <= 2 * pairs && blocks >= 4 * s)); ++s) {
-        if (other) {
-            best = s;
-            if (blocks / s <= share) break;
-            continue;
-        }
-        const unsigned long long cost = (unsigned long long)blocks_of(tiles * s, pairs) * (blocks_of(blocks, s) + 10) + (s > 1 ? 8 : 0);
-        if (cost < least) {
-            least = cost;
-            best = s;
-        }
-    }
-    return best;
-}
 
 // ---- few tokens ----------------------------------------------------------------------------
 
@@ -109,18 +17,6 @@ constexpr unsigned long long kStreamMaxTokens = 320;
 
 // Ring of a CTA: two CTAs share an SM.
 constexpr unsigned kStreamRing = 96 * 1024;
-
-// Kernels opt in to their shared memory once per process and device; contexts of several host threads may
-// come by at the same time (opting in twice does no harm).
-template <typename K>
-static int allow_smem(dd_ctx *ctx, K kernel, size_t bytes, std::atomic<bool> (&done)[64])
-{
-    const int d = ctx->device;
-    if (d < 64 && done[d]) return DD_OK;
-    DD_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-    if (d < 64) done[d] = true;
-    return DD_OK;
-}
 
 // Whether a kEpiStore launch takes 256 x 512 tiles.  They read a quarter fewer operand bytes a product, but
 // fill tensor memory, so that an epilogue has no product to run under, and there are half as many.  The
@@ -148,47 +44,7 @@ static bool wide_tiles(const dd_ctx *ctx, const GemmArgs &a)
     return time[1] < time[0];
 }
 
-template <int EPI, int BN, int ACT>
-static int launch_gemm_act(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
-{
-    constexpr size_t smem = gemm_smem_bytes(EPI, BN);
-    static std::atomic<bool> done[64];
-    const int rc = allow_smem(ctx, ffn_gemm_kernel<EPI, BN, ACT>, smem, done);
-    if (rc != DD_OK) return rc;
-    const unsigned most = (unsigned)ctx->sm_count / 2, pairs = a.tiles < most ? a.tiles : most;
-    const GemmProblem &p = a.prob[0];
-    a.first = p.tile_end;
-    a.rest = a.first % pairs;
-    a.extra = 0;
-    if (a.rest && a.nprob > 1) {
-        const GemmProblem &q = a.prob[1];
-        const unsigned one = (p.kblocks[0] + p.kblocks[1]) / p.splits, next = blocks_of(q.kblocks[0] + q.kblocks[1], q.splits);
-        a.extra = (one + next / 2) / next;
-        const unsigned room = (a.tiles - a.first) / (pairs - a.rest);
-        if (a.extra > room) a.extra = room;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * pairs);
-    cfg.blockDim = dim3(kGemmThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_gemm_kernel<EPI, BN, ACT>, a));
-    return DD_OK;
-}
-
-template <int EPI, int BN>
-static int launch_gemm(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
-{
-    return EPI != kEpiStore && a.e.activation == DD_ACT_GELU_TANH ? launch_gemm_act<EPI, BN, EPI == kEpiStore ? DD_ACT_SILU : DD_ACT_GELU_TANH>(ctx, a, stream)
-                                                                  : launch_gemm_act<EPI, BN, DD_ACT_SILU>(ctx, a, stream);
-}
-
-static int launch_store(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
+int launch_store(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
 {
     if (!wide_tiles(ctx, a)) return launch_gemm<kEpiStore, 256>(ctx, a, stream);
     a.tiles = 0;
@@ -201,38 +57,52 @@ static int launch_store(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
     return launch_gemm<kEpiStore, 512>(ctx, a, stream);
 }
 
-// Slabs handed out so far, and what becomes of them.
-struct Splits {
-    size_t used = 0;                  // floats
-    ReduceArgs r;
-};
-
-// Output of problem `p`, out (ld_out) [+ addend]: directly, or by way of its splits' slabs.
-static void set_output(const dd_ctx *ctx, GemmProblem &p, Splits &sp, void *out, uint64_t ld_out, bool f32, const void *addend,
-                       uint64_t ld_addend, bool addend_f32)
+__global__ void __launch_bounds__(256)
+ffn_reduce_kernel(const __grid_constant__ ReduceArgs a)
 {
-    if (p.splits == 1) {
-        p.out = out;
-        p.ld_out = ld_out;
-        p.out_f32 = f32;
-        p.addend = addend;
-        p.ld_addend = ld_addend;
-        return;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    int k = 0;
+    for (unsigned long long i = (unsigned long long)blockIdx.x * blockDim.x + threadIdx.x; i < a.job[a.count - 1].end;
+         i += (unsigned long long)gridDim.x * blockDim.x) {
+        while (i >= a.job[k].end) ++k;
+        const ReduceJob &j = a.job[k];
+        const unsigned long long at = i - (k ? a.job[k - 1].end : 0ull);
+        const unsigned pieces = j.ld / 8, row = (unsigned)(at / pieces), col = (unsigned)(at % pieces) * 8;
+        const unsigned cols = j.n - col < 8 ? j.n - col : 8;
+        const float *src = j.slabs + (unsigned long long)row * j.ld + col;
+        float4 v[kMaxSplits][2];
+#pragma unroll
+        for (int s = 0; s < kMaxSplits; ++s)
+            if (s < j.splits) {
+                v[s][0] = __ldcg(reinterpret_cast<const float4 *>(src + s * j.slab));
+                v[s][1] = __ldcg(reinterpret_cast<const float4 *>(src + s * j.slab) + 1);
+            }
+        float x[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            x[h][0] = v[0][h].x; x[h][1] = v[0][h].y; x[h][2] = v[0][h].z; x[h][3] = v[0][h].w;
+#pragma unroll
+            for (int s = 1; s < kMaxSplits; ++s)
+                if (s < j.splits) { x[h][0] += v[s][h].x; x[h][1] += v[s][h].y; x[h][2] += v[s][h].z; x[h][3] += v[s][h].w; }
+            const unsigned c = col + 4 * h, live = cols > 4 * h ? cols - 4 * h : 0;
+            if (!live) break;
+            if (j.addend) {
+                float add[4];
+                const unsigned long long from = (unsigned long long)row * j.ld_addend + c;
+                if (j.addend_f32) load4_f32(static_cast<const float *>(j.addend) + from, add, live);
+                else load4(static_cast<const __nv_bfloat16 *>(j.addend) + from, add, live);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[h][q] += add[q];
+            }
+            const unsigned long long to = (unsigned long long)row * j.ld_out + c;
+            if (j.out_f32) store4_f32(static_cast<float *>(j.out) + to, x[h], live);
+            else store4(static_cast<__nv_bfloat16 *>(j.out) + to, x[h], live);
+        }
     }
-    const unsigned ld = (p.n + 7) / 8 * 8;
-    p.out = ctx->ffn_slabs + sp.used;
-    p.ld_out = ld;
-    p.out_f32 = 1;
-    const unsigned long long slab = (unsigned long long)p.split_rows * ld;
-    ReduceJob &j = sp.r.job[sp.r.count];
-    const unsigned long long before = sp.r.count ? sp.r.job[sp.r.count - 1].end : 0;
-    j = {ctx->ffn_slabs + sp.used, p.splits, p.m, p.n, ld, slab, before + (unsigned long long)p.m * (ld / 8), out, addend, ld_out, ld_addend,
-         f32, addend_f32};
-    ++sp.r.count;
-    sp.used += p.splits * slab;
 }
 
-static int launch_reduce(dd_ctx *ctx, const Splits &sp, cudaStream_t stream)
+int launch_reduce(dd_ctx *ctx, const Splits &sp, cudaStream_t stream)
 {
     if (!sp.r.count) return DD_OK;
     const unsigned long long blocks = (sp.r.job[sp.r.count - 1].end + 255) / 256, most = (unsigned long long)ctx->sm_count * 8;
@@ -314,14 +184,6 @@ static StreamArgs stream_args(const EpilogueArgs &e, uint64_t features, uint64_t
     return a;
 }
 
-// The slabs, with the first call of either direction: no later call allocates them.
-static int ensure_ffn_slabs(dd_ctx *ctx)
-{
-    if (ctx->ffn_slabs) return DD_OK;
-    DD_CUDA(ctx, cudaMalloc(&ctx->ffn_slabs, slab_bytes(ctx)));
-    return DD_OK;
-}
-
 // Context-owned scratch for callers that bring none.
 static int ensure_ffn_scratch(dd_ctx *ctx, size_t bytes)
 {
@@ -337,38 +199,6 @@ static int ensure_ffn_scratch(dd_ctx *ctx, size_t bytes)
 
 // ---- arguments ---------------------------------------------------------------------------------
 
-// Rows of a matrix in memory, in bytes; no rows: touches nothing.
-struct Extent {
-    const void *p;
-    size_t rows, width, pitch;
-};
-
-static Extent extent(const void *p, unsigned long long rows, unsigned long long cols, unsigned long long ld, size_t elem = 2)
-{
-    return Extent{p, p ? (size_t)rows : 0, (size_t)cols * elem, (size_t)ld * elem};
-}
-
-// Whether two matrices share a byte.  Rows of one pitch may lie side by side (gate and up as halves of one
-// buffer's rows); of different pitches whatever lies between the ends is taken.
-static bool touches(const Extent &a, const Extent &b)
-{
-    if (!a.rows || !b.rows) return false;
-    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
-    if (y < x) return touches(b, a);
-    if (y >= x + (a.rows - 1) * a.pitch + a.width) return false;
-    if (a.pitch != b.pitch) return true;
-    const size_t off = (y - x) % a.pitch;
-    return off < a.width || off + b.width > a.pitch;
-}
-
-static int set_stride(uint64_t &ld, uint64_t cols)
-{
-    if (ld == 0) ld = cols;
-    if (ld < cols) return DD_ERR_INVALID_ARG;
-    if (ld >= kFfnMax) return DD_ERR_TOO_LARGE;
-    return ld % 8 ? DD_ERR_ALIGNMENT : DD_OK;
-}
-
 // Validates the block and fills in its defaults; without gate and up their stride is not looked at.
 static int check_block(const dd_ctx *ctx, dd_gated_ffn &b, bool with_gate)
 {
@@ -383,25 +213,6 @@ static int check_block(const dd_ctx *ctx, dd_gated_ffn &b, bool with_gate)
         if (rc != DD_OK) return rc;
     }
     if (!b.w_gate || !b.w_up || !b.w_down) return DD_ERR_INVALID_ARG;
-    return DD_OK;
-}
-
-static int check_aligned(std::initializer_list<const void *> ptrs)
-{
-    for (const void *p : ptrs)
-        if ((uintptr_t)p & 15u) return DD_ERR_ALIGNMENT;
-    return DD_OK;
-}
-
-// Outputs first: none may touch another output or an input.
-static int check_alias(std::initializer_list<Extent> outs, std::initializer_list<Extent> ins)
-{
-    for (auto o = outs.begin(); o != outs.end(); ++o) {
-        for (auto q = outs.begin(); q != o; ++q)
-            if (touches(*o, *q)) return DD_ERR_ALIAS;
-        for (const Extent &i : ins)
-            if (touches(*o, i)) return DD_ERR_ALIAS;
-    }
     return DD_OK;
 }
 

@@ -23,36 +23,39 @@
 // the caller's status word says DD_STATUS_WAIT_LIMIT.
 #pragma once
 
-#include <cuda.h>
-
-#include <cuda_bf16.h>
-
 #include "dd_learner.h"
-#include "dd_merge_tma.cuh"
+#include "dd_tcgen05.cuh"
 
 namespace ddm {
 
 constexpr int kBM = 128, kBK = 64;              // rows of one CTA, K elements of a stage
-constexpr int kChunkBytes = 64 * 128;             // one TMA box: 64 rows of 64 bf16
 constexpr int kMaxMaps = 8, kMaxProblems = 4;
 constexpr unsigned kTileGroup = 8;                // 4 / 8 / 16: forward 657 / 646 / 639 us, backward 1305 / 1309 / 1325 (8192 tokens)
 constexpr int kMaxSplits = 8;
-constexpr unsigned kSpinLimit = 1u << 30;         // attempts and nanoseconds of a bounded wait
-constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr int kBoxBytes = 32 * 128;               // an epilogue box: 32 rows of 64 bf16 or 32 float32
 
-enum GemmEpilogue { kEpiStore = 0, kEpiGate = 1, kEpiBack = 2 };
+enum GemmEpilogue { kEpiStore = 0, kEpiGate = 1, kEpiBack = 2, kEpiLoss = 3, kEpiSoft = 4 };
 
 // What the epilogues read and write.  kEpiGate: gate and up (null when not kept) and hidden are outputs;
 // kEpiBack: gate and up are inputs, dgate, dup and hidden outputs; kEpiStore: out = sums [+ residual].
+// The sums as logits of tokens (rows) and a piece of the vocabulary (columns), of which nothing is stored:
+// kEpiLoss leaves each row's largest and its sum of exponentials over 128 columns in `partial`, and the target's
+// logit in `loss`; kEpiSoft the gradient dloss (exp(z - lse) - [target]) in hidden.
 struct EpilogueArgs {
     __nv_bfloat16 *gate, *up, *dgate, *dup, *hidden, *out;
     const __nv_bfloat16 *residual;
     unsigned long long ld_gate, ld_hidden, ld_out, ld_residual;
     int *status;
+    const long long *targets;         // by row; outside 0 .. vocab - 1: none
+    const float *lse, *dloss;         // kEpiSoft, by row
+    float *loss;                      // kEpiLoss
+    float2 *partial;                  // [columns / 128][rows]: largest logit, sum of exp(z - largest)
+    long long first, vocab;           // kEpiSoft: the piece's first column
     int activation;
     int expire;                       // test hook: the first stage waits for 16 bytes that no copy brings
 };
+
+enum { kOutBf16 = 0, kOutF32 = 1, kOutSum = 2 };
 
 struct GemmProblem {
     unsigned m, n;                    // output rows and columns
@@ -63,7 +66,7 @@ struct GemmProblem {
     unsigned char a_map[2], b_map[2]; // tensor maps of the segments; kEpiGate: b_map = {w_gate, w_up}
     unsigned char a_mn, b_mn;         // 1: M (N) is the contiguous direction in memory
     // kEpiStore: out = sums [+ addend of the output's type]; the addend may be the output itself
-    unsigned char out_f32;
+    unsigned char out_f32;            // kOutBf16, kOutF32, or kOutSum: bf16 with a float32 addend
     void *out;
     const void *addend;
     unsigned long long ld_out, ld_addend;
@@ -83,114 +86,12 @@ struct GemmArgs {
 
 constexpr int kEpiWarps = 8, kGemmThreads = 32 * kEpiWarps + 64;
 // Boxes that a warp of the epilogue stages results in; kEpiBack also reads gate and up through its two.
-__host__ __device__ constexpr int gemm_boxes(int epi) { return epi == kEpiStore ? 1 : 2; }
+__host__ __device__ constexpr int gemm_boxes(int epi) { return epi == kEpiLoss ? 0 : epi == kEpiStore || epi == kEpiSoft ? 1 : 2; }
 __host__ __device__ constexpr unsigned gemm_epi_bytes(int epi) { return kEpiWarps * gemm_boxes(epi) * kBoxBytes; }
 // A stage of one CTA: 128 rows of A and half of the tile's BN rows of B.
 __host__ __device__ constexpr unsigned gemm_stage_bytes(int bn) { return (unsigned)(kBM + bn / 2) * kBK * 2; }
 __host__ __device__ constexpr int gemm_stages(int epi, int bn) { return (int)((224 * 1024 - gemm_epi_bytes(epi)) / gemm_stage_bytes(bn)); }
 __host__ __device__ constexpr unsigned gemm_smem_bytes(int epi, int bn) { return 1024 + gemm_stages(epi, bn) * gemm_stage_bytes(bn) + gemm_epi_bytes(epi); }
-
-// ---- tcgen05 ----------------------------------------------------------------------------------
-
-__device__ __forceinline__ bool elect_one()
-{
-    unsigned p;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
-    return p != 0;
-}
-
-__device__ __forceinline__ void tma_load_2d(unsigned dst, const CUtensorMap *map, int x, int y, unsigned bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-
-__device__ __forceinline__ void umma_bf16(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate)
-{
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-                 " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-
-// Arrives on `bar` once every tcgen05.mma this thread has issued so far is complete.
-__device__ __forceinline__ void umma_commit(unsigned bar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
-}
-
-// The same for a pair: products of both SMs, `bar` in every CTA of `mask`.
-__device__ __forceinline__ void umma_commit_pair(unsigned bar, unsigned short mask)
-{
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 :: "r"(bar), "h"(mask) : "memory");
-}
-
-__device__ __forceinline__ void umma_bf16_pair(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate)
-{
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-                 " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-
-// A copy into this CTA that reports to a barrier (a cluster address) of either CTA of the pair.
-__device__ __forceinline__ void tma_load_2d_pair(unsigned dst, const CUtensorMap *map, int x, int y, unsigned bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-
-// This CTA's shared-memory address as the cluster address of the same place in CTA `rank`.
-__device__ __forceinline__ unsigned cluster_addr(unsigned addr, unsigned rank)
-{
-    unsigned r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-
-// Relaxed: what it reports is that tensor memory has been read into registers, which the wait on
-// those loads has ensured.  A release would hold the warp until its stores to global memory are
-// acknowledged: 2-5k cycles a tile.
-__device__ __forceinline__ void mbar_arrive_cluster(unsigned bar)
-{
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
-}
-
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-// The same without ordering memory, for the end of a kernel: a release would wait for the results to be
-// acknowledged, which the end of the launch does anyway.
-__device__ __forceinline__ void cluster_sync_relaxed()
-{
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
-}
-
-__device__ __forceinline__ void tmem_ld32(unsigned addr, unsigned (&r)[32])
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr));
-}
-
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-// Shared-memory operand descriptor, 128-byte swizzle.  Chunks are 64 rows of 128 bytes.
-//   K contiguous: rows are M (N); groups of 8 rows follow every 1024 bytes, chunks continue them.
-//   M (N) contiguous: rows are K, groups of 8 every 1024 bytes; the next 64 M (N) are one chunk on.
-__device__ __forceinline__ unsigned long long umma_desc(unsigned addr, bool mn)
-{
-    const unsigned long long lead = mn ? kChunkBytes / 16 : 1, stride = 1024 / 16;
-    return ((unsigned long long)(addr >> 4) & 0x3fff) | (lead << 16) | (stride << 32) | (1ull << 46) | (2ull << 61);
-}
 
 // ---- activation ---------------------------------------------------------------------------------
 
@@ -213,12 +114,6 @@ __device__ __forceinline__ float activate(float g, float *slope)
         *slope = fmaf(a, ACT == DD_ACT_SILU ? rest : rest * fmaf(3.0f * k * q, g2, k), sg);
     }
     return a;
-}
-
-__device__ __forceinline__ unsigned pack2(float lo, float hi)
-{
-    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const unsigned *>(&b);
 }
 
 // Up to four consecutive bf16, `live` of them inside the row.
@@ -322,28 +217,6 @@ __device__ __forceinline__ TilePos tile_pos(const GemmArgs &a, unsigned t)
     return r;
 }
 
-// Bounded wait of a pipeline role.  No suspend hint: with one (4 us) a role woke up to 3 us after its
-// phase had completed.  The limit is on time, a second, looked at every 256 attempts.
-__device__ __forceinline__ bool gemm_wait(unsigned bar, unsigned parity, volatile int *abort)
-{
-    unsigned long long start = 0;
-    for (unsigned spins = 0; spins < kSpinLimit; ++spins) {
-        unsigned ok;
-        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        if (ok) return true;
-        if (*abort) return false;
-        if ((spins & 255) == 255) {
-            unsigned long long now;
-            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
-            if (!start) start = now;
-            else if (now - start > kWaitNs) break;
-        }
-    }
-    *abort = 1;
-    return false;
-}
-
 // Results leave a warp through a box in shared memory: in tensor memory a lane holds a row, in
 // global memory eight lanes together write 128 bytes of one.  (Rows written lane by lane cost the
 // load/store unit a pass per row; 64-byte boxes stored by the TMA engine took 1 us a box and warp.)
@@ -441,7 +314,7 @@ __device__ __forceinline__ void load_box(unsigned box, int lane, const __nv_bflo
     }
 }
 
-// 32 float32 columns of the lane's row through the box to out [+ addend].
+// 32 float32 columns of the lane's row through the box to out [+ addend]; kOutSum rounds what goes out.
 __device__ __forceinline__ void finish_f32(unsigned box, int lane, const float (&x)[32], const GemmProblem &p, unsigned row0, unsigned out_row0,
                                            unsigned col)
 {
@@ -464,7 +337,8 @@ __device__ __forceinline__ void finish_f32(unsigned box, int lane, const float (
             for (int k = 0; k < 4; ++k) y[k] += add[k];
         }
         const unsigned long long at = (unsigned long long)(out_row0 + r) * p.ld_out + c;
-        store4_f32(static_cast<float *>(p.out) + at, y, live);
+        if (p.out_f32 == kOutF32) store4_f32(static_cast<float *>(p.out) + at, y, live);
+        else store4(static_cast<__nv_bfloat16 *>(p.out) + at, y, live);
     }
     __syncwarp();
 }
@@ -618,6 +492,18 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
             if constexpr (EPI == kEpiStore) {
                 if (add && chunks) load_addend(share, 0);
             }
+            long long target = -1;
+            float soft_off = 0.0f, soft_by = 0.0f;
+            if constexpr (EPI == kEpiLoss || EPI == kEpiSoft) {
+                if (chunks && row + lane < p.m) target = a.e.targets[row + lane];
+                if (EPI == kEpiSoft && target >= 0 && target < a.e.vocab) {
+                    soft_off = -a.e.lse[row + lane] * 1.4426950408889634f;
+                    soft_by = a.e.dloss[row + lane];
+                } else if (EPI == kEpiSoft) {
+                    soft_off = -INFINITY;                          // no gradient
+                    target = -1;
+                }
+            }
             const bool ok = gemm_wait(tfull + 8 * slot, (acc / kSlots) & 1, abort);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
@@ -629,7 +515,67 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                 if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * slot);
             };
             if (!chunks) release();
-            if (EPI == kEpiStore && p.out_f32) {
+            if constexpr (EPI == kEpiLoss) {
+                constexpr float l = 1.4426950408889634f;
+                float top = -INFINITY, sum = 0.0f;
+#pragma unroll 1
+                for (unsigned c = 0; c < 2 * chunks; ++c) {
+                    unsigned r[32];
+                    float x[32];
+                    tmem_ld32(taddr + 32 * c, r);
+                    tmem_ld_wait();
+                    if (c + 1 == 2 * chunks) release();
+                    const unsigned col = col0 + 32 * c, live = col < p.n ? p.n - col : 0;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] = live >= 32 || j < live ? __uint_as_float(r[j]) : -INFINITY;
+                    float m = x[0];
+#pragma unroll
+                    for (int j = 1; j < 32; ++j) m = fmaxf(m, x[j]);
+                    m = fmaxf(m, top);
+                    const float base = m == -INFINITY ? 0.0f : m, off = -base * l;
+                    float part[2] = {0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) part[j & 1] += exp2_fast(fmaf(x[j], l, off));
+                    sum = fmaf(sum, exp2_fast((top - base) * l), part[0] + part[1]);
+                    top = m;
+                    const bool here = target >= col && target < (long long)col + 32;
+                    if (__any_sync(0xffffffffu, here)) {
+                        float z = 0.0f;
+                        const int at = here ? (int)(target - col) : -1;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z = at == j ? x[j] : z;
+                        if (here) a.e.loss[row + lane] = z;
+                    }
+                }
+                if (chunks && row + lane < p.m) a.e.partial[(unsigned long long)(col0 / 128) * p.m + row + lane] = make_float2(top, sum);
+            } else if constexpr (EPI == kEpiSoft) {
+                constexpr float l = 1.4426950408889634f;
+#pragma unroll 1
+                for (unsigned c = 0; c < chunks; ++c) {
+                    const unsigned col = col0 + 64 * c;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        unsigned r[32], w[16];
+                        float x[32];
+                        tmem_ld32(taddr + 64 * c + 32 * h, r);
+                        tmem_ld_wait();
+                        if (h == 1 && c + 1 == chunks) release();
+                        const long long rel = target - a.e.first - col - 32 * h;
+                        const int at = rel >= 0 && rel < 32 ? (int)rel : -1;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[j] = exp2_fast(fmaf(__uint_as_float(r[j]), l, soft_off)) * soft_by;
+                        if (__any_sync(0xffffffffu, at >= 0)) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) x[j] = at == j ? (exp2_fast(fmaf(__uint_as_float(r[j]), l, soft_off)) - 1.0f) * soft_by : x[j];
+                        }
+                        pack32(x, w);
+                        write_half(box, lane, h, w);
+                    }
+                    __syncwarp();
+                    store_box(box, lane, a.e.hidden, a.e.ld_hidden, row, col, p.m, p.n);
+                    __syncwarp();
+                }
+            } else if (EPI == kEpiStore && p.out_f32) {
 #pragma unroll 1
                 for (unsigned c = 0; c < 2 * chunks; ++c) {
                     unsigned r[32];
@@ -685,7 +631,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
                     store_box(box, lane, static_cast<__nv_bfloat16 *>(p.out), p.ld_out, row, col0 + 64 * c, p.m, p.n);
                     __syncwarp();
                 }
-            } else {
+            } else if constexpr (EPI == kEpiGate || EPI == kEpiBack) {
 #pragma unroll 1
                 for (unsigned c = 0; c < chunks; ++c) {
                     const unsigned col = col0 + 64 * c, at = taddr + 64 * c;
@@ -800,50 +746,5 @@ struct ReduceArgs {
     ReduceJob job[kMaxProblems];
     int count;
 };
-
-__global__ void __launch_bounds__(256)
-ffn_reduce_kernel(const __grid_constant__ ReduceArgs a)
-{
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    int k = 0;
-    for (unsigned long long i = (unsigned long long)blockIdx.x * blockDim.x + threadIdx.x; i < a.job[a.count - 1].end;
-         i += (unsigned long long)gridDim.x * blockDim.x) {
-        while (i >= a.job[k].end) ++k;
-        const ReduceJob &j = a.job[k];
-        const unsigned long long at = i - (k ? a.job[k - 1].end : 0ull);
-        const unsigned pieces = j.ld / 8, row = (unsigned)(at / pieces), col = (unsigned)(at % pieces) * 8;
-        const unsigned cols = j.n - col < 8 ? j.n - col : 8;
-        const float *src = j.slabs + (unsigned long long)row * j.ld + col;
-        float4 v[kMaxSplits][2];
-#pragma unroll
-        for (int s = 0; s < kMaxSplits; ++s)
-            if (s < j.splits) {
-                v[s][0] = __ldcg(reinterpret_cast<const float4 *>(src + s * j.slab));
-                v[s][1] = __ldcg(reinterpret_cast<const float4 *>(src + s * j.slab) + 1);
-            }
-        float x[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            x[h][0] = v[0][h].x; x[h][1] = v[0][h].y; x[h][2] = v[0][h].z; x[h][3] = v[0][h].w;
-#pragma unroll
-            for (int s = 1; s < kMaxSplits; ++s)
-                if (s < j.splits) { x[h][0] += v[s][h].x; x[h][1] += v[s][h].y; x[h][2] += v[s][h].z; x[h][3] += v[s][h].w; }
-            const unsigned c = col + 4 * h, live = cols > 4 * h ? cols - 4 * h : 0;
-            if (!live) break;
-            if (j.addend) {
-                float add[4];
-                const unsigned long long from = (unsigned long long)row * j.ld_addend + c;
-                if (j.addend_f32) load4_f32(static_cast<const float *>(j.addend) + from, add, live);
-                else load4(static_cast<const __nv_bfloat16 *>(j.addend) + from, add, live);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) x[h][q] += add[q];
-            }
-            const unsigned long long to = (unsigned long long)row * j.ld_out + c;
-            if (j.out_f32) store4_f32(static_cast<float *>(j.out) + to, x[h], live);
-            else store4(static_cast<__nv_bfloat16 *>(j.out) + to, x[h], live);
-        }
-    }
-}
 
 }  // namespace ddm

@@ -339,6 +339,7 @@ extern "C" int dd_destroy(dd_ctx *ctx)
     if (ctx->gram) cudaFree(ctx->gram);
     if (ctx->ffn_scratch) cudaFree(ctx->ffn_scratch);
     if (ctx->ffn_slabs) cudaFree(ctx->ffn_slabs);
+    if (ctx->decoder_scratch) cudaFree(ctx->decoder_scratch);
     host_pipe_destroy(ctx);
     for (Slot &s : ctx->slots) {
         if (s.host) cudaFreeHost(s.host);

@@ -1,13 +1,14 @@
-// _ddtorch: torch tensors to the C calls of dd_learner.h.  A parameter list of a model has hundreds
+// _ddtorch: torch tensors to the C calls of dd_learner.h and dd_decoder.h.  A parameter list of a model has hundreds
 // of tensors; reading their addresses, sizes and types one by one from Python takes longer than
 // the kernels (190 us for 5 x 192 tensors, against 12 us here).  Checks and marshalling only.
+#include <cmath>
 #include <cstdint>
 #include <string>
 #include <vector>
 
 #include <torch/csrc/autograd/python_variable.h>
 
-#include "dd_learner.h"
+#include "dd_decoder.h"
 
 namespace {
 
@@ -243,6 +244,151 @@ int gated_ffn_backward(PyObject *const *a)
                                  pointer(a[16]));
 }
 
+// ---- the decoder's operators ------------------------------------------------------------------
+
+// A contiguous vector of `n` elements, or null for None.
+void *vector(PyObject *o, const char *name, uint64_t n, at::ScalarType kind)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o, name);
+    if (t.scalar_type() != kind || (uint64_t)t.numel() != n || !t.is_contiguous())
+        refuse(std::string(name) + ": want " + std::to_string(n) + " contiguous " + c10::toString(kind) + ", got (size by stride) " + shape_of(t));
+    return t.data_ptr();
+}
+
+// [tokens, heads, dim] with contiguous heads; None: no tensor.
+dd_heads heads_of(PyObject *o, const char *name, uint64_t tokens, uint64_t heads, uint64_t dim, at::ScalarType kind = at::kBFloat16)
+{
+    if (o == Py_None) return dd_heads{};
+    const at::Tensor &t = tensor(o, name);
+    if (t.dim() != 3 || (uint64_t)t.size(0) != tokens || (uint64_t)t.size(1) != heads || (uint64_t)t.size(2) != dim || t.scalar_type() != kind ||
+        (dim > 1 && t.stride(2) != 1))
+        refuse(std::string(name) + ": want " + c10::toString(kind) + " [" + std::to_string(tokens) + ", " + std::to_string(heads) + ", " +
+               std::to_string(dim) + "] with contiguous heads, got (size by stride) " + shape_of(t));
+    // an expanded tensor has stride 0, which the C calls take as a contiguous tensor's
+    if ((tokens > 1 && t.stride(0) < (int64_t)dim) || (heads > 1 && t.stride(1) < (int64_t)dim))
+        refuse(std::string(name) + ": rows overlap, got (size by stride) " + shape_of(t));
+    return dd_heads{t.data_ptr(), tokens > 1 ? (uint64_t)t.stride(0) : 0, heads > 1 ? (uint64_t)t.stride(1) : 0};
+}
+
+// (ctx, q, k, positions, frequencies, q_out, k_out, magnitude, interleaved, inverse, stream)
+int rotary_apply(PyObject *const *a)
+{
+    const at::Tensor &q = tensor(a[1], "q"), &f = tensor(a[4], "frequencies"), &p = tensor(a[3], "positions");
+    if (q.dim() != 3) refuse("q: want [tokens, heads, dim]");
+    const at::ScalarType kind = q.scalar_type();
+    if (kind != at::kFloat && kind != at::kBFloat16) refuse(std::string("q must be float32 or bfloat16, not ") + c10::toString(kind));
+    if (p.scalar_type() != at::kInt && p.scalar_type() != at::kLong) refuse(std::string("positions must be int32 or int64, not ") + c10::toString(p.scalar_type()));
+    dd_rotary r{};
+    r.tokens = q.size(0);
+    r.heads = q.size(1);
+    r.dim = q.size(2);
+    r.rotary_dim = 2 * (uint64_t)f.numel();
+    if (a[2] != Py_None) {
+        const at::Tensor &k = tensor(a[2], "k");
+        if (k.dim() != 3) refuse("k: want [tokens, heads, dim]");
+        r.kv_heads = k.size(1);
+    }
+    r.dtype = kind == at::kBFloat16 ? DD_BF16 : DD_F32;
+    r.interleaved = truth(a[8]);
+    r.inverse = truth(a[9]);
+    r.positions_64 = p.scalar_type() == at::kLong;
+    r.magnitude = (float)real(a[7]);
+    if ((a[6] == Py_None) != (a[2] == Py_None)) refuse("k and k_out: want both or neither");
+    const dd_heads x = heads_of(a[1], "q", r.tokens, r.heads, r.dim, kind), y = heads_of(a[2], "k", r.tokens, r.kv_heads, r.dim, kind),
+                   xo = heads_of(a[5], "q_out", r.tokens, r.heads, r.dim, kind), yo = heads_of(a[6], "k_out", r.tokens, r.kv_heads, r.dim, kind);
+    return dd_rotary_apply(context(a[0]), &r, &x, &y, &xo, &yo, vector(a[3], "positions", r.tokens, p.scalar_type()),
+                           (const double *)vector(a[4], "frequencies", f.numel(), at::kDouble), pointer(a[10]));
+}
+
+// (q, k) and the settings -> attention
+dd_attention attention_of(PyObject *q_, PyObject *k_, PyObject *offsets, PyObject *scale, PyObject *causal, PyObject *flags)
+{
+    const at::Tensor &q = tensor(q_, "q"), &k = tensor(k_, "k");
+    if (q.dim() != 3 || k.dim() != 3) refuse("q and k: want [tokens, heads, dim]");
+    dd_attention b{};
+    b.tokens = q.size(0);
+    b.heads = q.size(1);
+    b.dim = q.size(2);
+    b.kv_heads = k.size(1);
+    if (offsets != Py_None) {
+        const at::Tensor &o = tensor(offsets, "offsets");
+        if (o.numel() < 1) refuse("offsets: want one more than there are sequences");
+        b.sequences = o.numel() - 1;
+        b.offsets = (const int32_t *)vector(offsets, "offsets", o.numel(), at::kInt);
+    }
+    b.scale = scale == Py_None ? 1.0f / std::sqrt((float)b.dim) : (float)real(scale);
+    b.causal = truth(causal);
+    const long long bits = integer(flags);
+    b.flags = bits == (uint32_t)bits ? (uint32_t)bits : ~0u;
+    return b;
+}
+
+// (ctx, q, k, v, o, lse, offsets, scale, causal, scratch, status, stream, flags)
+int attention_forward(PyObject *const *a)
+{
+    const dd_attention b = attention_of(a[1], a[2], a[6], a[7], a[8], a[12]);
+    const dd_heads q = heads_of(a[1], "q", b.tokens, b.heads, b.dim), k = heads_of(a[2], "k", b.tokens, b.kv_heads, b.dim),
+                   v = heads_of(a[3], "v", b.tokens, b.kv_heads, b.dim), o = heads_of(a[4], "o", b.tokens, b.heads, b.dim);
+    return dd_attention_forward(context(a[0]), &b, &q, &k, &v, &o, (float *)vector(a[5], "lse", b.heads * b.tokens, at::kFloat),
+                                address(a[9], "scratch", dd_attention_scratch_bytes(&b, 0)), (int32_t *)address(a[10], "status", 4), pointer(a[11]));
+}
+
+// (ctx, q, k, v, o, lse, d_o, dq, dk, dv, offsets, scale, causal, scratch, status, stream, flags)
+int attention_backward(PyObject *const *a)
+{
+    const dd_attention b = attention_of(a[1], a[2], a[10], a[11], a[12], a[16]);
+    const dd_heads q = heads_of(a[1], "q", b.tokens, b.heads, b.dim), k = heads_of(a[2], "k", b.tokens, b.kv_heads, b.dim),
+                   v = heads_of(a[3], "v", b.tokens, b.kv_heads, b.dim), o = heads_of(a[4], "o", b.tokens, b.heads, b.dim),
+                   d_o = heads_of(a[6], "d_o", b.tokens, b.heads, b.dim), dq = heads_of(a[7], "dq", b.tokens, b.heads, b.dim),
+                   dk = heads_of(a[8], "dk", b.tokens, b.kv_heads, b.dim), dv = heads_of(a[9], "dv", b.tokens, b.kv_heads, b.dim);
+    return dd_attention_backward(context(a[0]), &b, &q, &k, &v, &o, (const float *)vector(a[5], "lse", b.heads * b.tokens, at::kFloat), &d_o, &dq,
+                                 &dk, &dv, address(a[13], "scratch", dd_attention_scratch_bytes(&b, 1)), (int32_t *)address(a[14], "status", 4),
+                                 pointer(a[15]));
+}
+
+// (hidden, weight, targets) -> loss and hidden
+const void *loss_of(PyObject *hidden, PyObject *weight, PyObject *targets, PyObject *flags, dd_vocab_loss &l)
+{
+    const at::Tensor &h = tensor(hidden, "hidden"), &w = tensor(weight, "weight");
+    if (h.dim() != 2 || w.dim() != 2) refuse("hidden and weight are matrices");
+    l = dd_vocab_loss{};
+    l.tokens = h.size(0);
+    l.d = h.size(1);
+    l.vocab = w.size(0);
+    const long long bits = integer(flags);
+    l.flags = bits == (uint32_t)bits ? (uint32_t)bits : ~0u;
+    const void *x = matrix(hidden, "hidden", l.tokens, l.d, l.ld_hidden);
+    l.weight = matrix(weight, "weight", l.vocab, l.d, l.ld_weight);
+    l.targets = (const int64_t *)vector(targets, "targets", l.tokens, at::kLong);
+    return x;
+}
+
+// (ctx, hidden, weight, targets, loss, lse, scratch, status, stream, flags)
+int vocab_loss_forward(PyObject *const *a)
+{
+    dd_vocab_loss l;
+    const void *x = loss_of(a[1], a[2], a[3], a[9], l);
+    dd_ctx *ctx = context(a[0]);
+    return dd_vocab_loss_forward(ctx, &l, x, (float *)vector(a[4], "loss", l.tokens, at::kFloat), (float *)vector(a[5], "lse", l.tokens, at::kFloat),
+                                 address(a[6], "scratch", dd_vocab_loss_scratch_bytes(ctx, &l, 0)), (int32_t *)address(a[7], "status", 4), pointer(a[8]));
+}
+
+// (ctx, hidden, weight, targets, lse, dloss, dhidden, dweight, accumulate, scratch, status, stream, flags)
+int vocab_loss_backward(PyObject *const *a)
+{
+    dd_vocab_loss l;
+    const void *x = loss_of(a[1], a[2], a[3], a[12], l);
+    dd_ctx *ctx = context(a[0]);
+    const at::ScalarType kind = tensor(a[7], "dweight").scalar_type();
+    if (kind != at::kFloat && kind != at::kBFloat16) refuse("dweight must be float32 or bfloat16");
+    void *dx = matrix(a[6], "dhidden", l.tokens, l.d, l.ld_hidden), *dw = matrix(a[7], "dweight", l.vocab, l.d, l.ld_weight, kind);
+    return dd_vocab_loss_backward(ctx, &l, x, (const float *)vector(a[4], "lse", l.tokens, at::kFloat),
+                                  (const float *)vector(a[5], "dloss", l.tokens, at::kFloat), dx, dw, kind == at::kBFloat16 ? DD_BF16 : DD_F32,
+                                  truth(a[8]), address(a[9], "scratch", dd_vocab_loss_scratch_bytes(ctx, &l, 1)), (int32_t *)address(a[10], "status", 4),
+                                  pointer(a[11]));
+}
+
 // Runs a call: refusals become ValueError, numbers that do not convert raise what Python raised.  Either
 // way nothing has been launched.
 template <int (*CALL)(PyObject *const *), int NARGS>
@@ -262,7 +408,8 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 
 #define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(grad_norm, 5), ENTRY(clip_gradients, 6), ENTRY(adamw_step, 14), ENTRY(gated_ffn_forward, 14),
-                         ENTRY(gated_ffn_backward, 18), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(gated_ffn_backward, 18), ENTRY(rotary_apply, 11), ENTRY(attention_forward, 13), ENTRY(attention_backward, 17),
+                         ENTRY(vocab_loss_forward, 10), ENTRY(vocab_loss_backward, 13), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ddtorch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -20,7 +20,7 @@ STATUS_OK, STATUS_QUORUM_NOT_MET, STATUS_ZERO_WEIGHT, STATUS_WAIT_LIMIT = 0, 1, 
 HEAVY_BALL, DIAG_PER_LEARNER, DIAG_STATE, RDA_THREE_PASS = 1, 2, 4, 8
 DEBUG_EXPIRE_WAIT = 1 << 30
 MERGE_AVG, MERGE_RDA = 0, 1
-STATUS_NONFINITE = 4
+STATUS_NONFINITE, STATUS_BAD_OFFSETS = 4, 5
 ACT_SILU, ACT_GELU_TANH = 0, 1
 RDA_PASS_NORMS, RDA_PASS_DIRECTION, RDA_PASS_APPLY = 0, 1, 2
 FRAG_LAYER, FRAG_TENSOR, FRAG_BALANCED = 0, 1, 2
@@ -39,6 +39,8 @@ EXPORTS = (
     "dd_launch_geometry", "dd_launch_shape",
     "dd_grad_norm", "dd_clip_gradients", "dd_adamw_step",
     "dd_gated_ffn_forward", "dd_gated_ffn_backward",
+    "dd_rotary_apply", "dd_attention_scratch_bytes", "dd_attention_forward", "dd_attention_backward",
+    "dd_vocab_loss_scratch_bytes", "dd_vocab_loss_forward", "dd_vocab_loss_backward",
 )
 
 
@@ -606,6 +608,59 @@ class Context:
         float32 and have the row strides of the weights."""
         rc = _native().gated_ffn_backward(self._h.value, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up,
                                           dw_down, activation, accumulate, scratch, status, _raw_stream(stream), flags)
+        if rc != OK:
+            self._check(rc)
+
+    # ---- the rest of a decoder's step (dd_decoder.h), marshalled and checked by _ddtorch ----------
+
+    def rotary(self, q, k, positions, frequencies, *, q_out=None, k_out=None, magnitude: float = 1.0,
+               interleaved: bool = False, inverse: bool = False, stream=None) -> None:
+        """``dd_rotary_apply``: turns the pairs of ``q`` [tokens, heads, dim] and ``k`` [tokens, kv_heads, dim]
+        (or None), float32 or bfloat16, by ``positions`` (int32 or int64; negative: no token) times
+        ``frequencies`` (float64, one per pair, ``rotary_frequencies``), in place or into ``q_out`` and
+        ``k_out``.  ``inverse`` takes gradients back."""
+        rc = _native().rotary_apply(self._h.value, q, k, positions, frequencies, q if q_out is None else q_out,
+                                    k if k_out is None else k_out, magnitude, interleaved, inverse, _raw_stream(stream))
+        if rc != OK:
+            self._check(rc)
+
+    def attention_forward(self, q, k, v, o, lse=None, *, offsets=None, scale: float | None = None, causal: bool = True,
+                          scratch=None, status=None, flags: int = 0, stream=None) -> None:
+        """``dd_attention_forward``: bfloat16 ``q``, ``o`` [tokens, heads, dim], ``k``, ``v`` [tokens, kv_heads, dim],
+        heads contiguous; ``lse`` [heads, tokens] float32 is kept for the backward pass when given.  ``offsets``:
+        int32, the first token of each sequence and the end of the last, or None for one sequence.  ``scale``:
+        1 / sqrt(dim) by default."""
+        rc = _native().attention_forward(self._h.value, q, k, v, o, lse, offsets, scale, causal, scratch, status,
+                                         _raw_stream(stream), flags)
+        if rc != OK:
+            self._check(rc)
+
+    def attention_backward(self, q, k, v, o, lse, d_o, dq, dk, dv, *, offsets=None, scale: float | None = None,
+                           causal: bool = True, scratch=None, status=None, flags: int = 0, stream=None) -> None:
+        """``dd_attention_backward``: gradients for ``d_o``, given the ``o`` and ``lse`` that the forward call
+        left; all bfloat16, each with strides of its own."""
+        rc = _native().attention_backward(self._h.value, q, k, v, o, lse, d_o, dq, dk, dv, offsets, scale, causal, scratch,
+                                          status, _raw_stream(stream), flags)
+        if rc != OK:
+            self._check(rc)
+
+    def vocab_loss_forward(self, hidden, weight, targets, loss, lse, *, scratch=None, status=None, flags: int = 0,
+                           stream=None) -> None:
+        """``dd_vocab_loss_forward``: softmax cross entropy of ``hidden`` [tokens, d] against the rows of
+        ``weight`` [vocab, d] (bfloat16) for int64 ``targets`` (negative: none), into float32 ``loss`` and
+        ``lse``, one per token."""
+        rc = _native().vocab_loss_forward(self._h.value, hidden, weight, targets, loss, lse, scratch, status,
+                                          _raw_stream(stream), flags)
+        if rc != OK:
+            self._check(rc)
+
+    def vocab_loss_backward(self, hidden, weight, targets, lse, dloss, dhidden, dweight, *, accumulate: bool = False,
+                            scratch=None, status=None, flags: int = 0, stream=None) -> None:
+        """``dd_vocab_loss_backward``: gradients for ``dloss`` (float32, one per token), given the forward call's
+        ``lse``: ``dhidden`` in bfloat16, ``dweight`` in bfloat16 or float32 with the row strides of
+        ``weight``."""
+        rc = _native().vocab_loss_backward(self._h.value, hidden, weight, targets, lse, dloss, dhidden, dweight, accumulate,
+                                           scratch, status, _raw_stream(stream), flags)
         if rc != OK:
             self._check(rc)
 
