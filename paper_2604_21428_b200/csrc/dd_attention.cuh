@@ -50,7 +50,7 @@ struct AttnArgs {
     int causal, expire;
     HeadsOut o, dq, dk, dv;
     float *lse;                                   // [heads][tokens]
-    const float *delta;                           // [heads][tokens]: d_o . o
+    float *delta;                                 // [heads][tokens]: sum_j p_ij dp_ij
     int *status;
 };
 
@@ -431,6 +431,11 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
 // next tile of keys are made as soon as those of this one are in registers; ds alternates between two places.
 // Two launches (this and the next kernel) form the scores twice, which costs 7 products of a tile instead of 5,
 // but no gradient is added to by several CTAs: no atomics, no float32 copy of dq in memory.
+//
+// delta_i = sum_j p_ij dp_ij is d_o_i . o_i, but o's rounding to bf16 is then in it, and where few keys share a row's
+// weight dp - delta is a small difference.  So rows whose keys are all in one tile, the short sequences and the
+// beginnings of long ones, take the sum itself and leave it for the next launch (two keys: gradients within
+// 0.25 % instead of 0.75 %).
 constexpr unsigned bwd_smem_bytes(int dp) { return 1024 + 6 * kTile * dp * 2; }
 
 template <int DP>
@@ -440,6 +445,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
     constexpr unsigned kBytes = kTile * DP * 2;
     extern __shared__ unsigned char smem_raw[];
     __shared__ alignas(16) AttnShared sh;
+    __shared__ float halves[2][kTile];            // a row's two shares of delta
     asm volatile("griddepcontrol.wait;" ::: "memory");
     PlanItem item;
     if (!plan_item(a, blockIdx.x / a.heads, item)) return;
@@ -448,12 +454,13 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
 
     const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u, sq = smem, sdo = smem + kBytes, sk = smem + 2 * kBytes, sv = smem + 4 * kBytes;
     const unsigned bar = smem_addr(sh.bars), q_full = bar, k_full = bar + 8, k_empty = bar + 24, v_full = bar + 40, v_empty = bar + 56,
-                   s_full = bar + 72, s_read = bar + 80, dp_full = bar + 88, ds_full = bar + 96, dq_full = bar + 104, drain = bar + 112;
+                   s_full = bar + 72, s_read = bar + 80, dp_full = bar + 88, ds_full = bar + 96, dq_full = bar + 104, drain = bar + 112, sum_full = bar + 120;
     volatile int *abort = &sh.abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         for (int i = 0; i < 15; ++i) init_bar(bar + 8 * i, 1);
+        init_bar(sum_full, 8);
         init_bar(s_read, 8);
         init_bar(ds_full, 8);
     }
@@ -523,7 +530,8 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
         const unsigned half = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16, row = row0 + (warp & 3) * 32 + lane;
         const unsigned long long token = item.start + row, stat = (unsigned long long)head * a.tokens + token;
         const float c = a.scale * kLog2e;
-        const float off = row < item.len ? -a.lse[stat] * kLog2e : 0.0f, delta = row < item.len ? a.delta[stat] : 0.0f;
+        const float off = row < item.len ? -a.lse[stat] * kLog2e : 0.0f;
+        float delta = row < item.len && n > 1 ? a.delta[stat] : 0.0f;
         // columns below `end` count; a token that sees itself alone has ds = 0
         const unsigned end = row >= item.len ? 0 : a.causal ? row + 1 : item.len;
         bool ok = true;
@@ -549,6 +557,21 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             tmem_ld_wait();
             const unsigned first = j * kTile + 64 * half, live = end == 1 || end <= first ? 0 : end - first;
             const bool masked = __any_sync(0xffffffffu, live < 64);
+            if (n == 1) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (32 * h + k < live) sum = fmaf(p[h][k], __uint_as_float(r[h][k]), sum);
+                halves[half][row - row0] = sum;
+                __syncwarp();
+                if (lane == 0) arrive_bar(sum_full);
+                ok = __all_sync(0xffffffffu, gemm_wait(sum_full, 0, abort));
+                if (!ok) break;
+                delta = halves[0][row - row0] + halves[1][row - row0];
+                if (half == 0 && row < item.len) a.delta[stat] = delta;
+            }
             unsigned w[32];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
