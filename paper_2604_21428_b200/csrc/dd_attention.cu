@@ -65,7 +65,7 @@ static int launch_forward(dd_ctx *ctx, const dd_attention &b, const AttnArgs &a,
     static std::atomic<bool> done[64];
     const int rc = allow_smem(ctx, attention_forward_kernel<DP>, fwd_smem_bytes(DP), done);
     if (rc != DD_OK) return rc;
-    return launch_after(ctx, attention_forward_kernel<DP>, most_tiles(b, 2 * kTile) * b.heads, kAttnThreads, fwd_smem_bytes(DP), stream, a);
+    return launch_after(ctx, attention_forward_kernel<DP>, most_tiles(b, 2 * kTile) * b.heads, 32 * (kFwdWarps + 4), fwd_smem_bytes(DP), stream, a);
 }
 
 template <int DP>
@@ -77,8 +77,8 @@ static int launch_backward(dd_ctx *ctx, const dd_attention &b, const AttnArgs &a
     constexpr int lanes = DP / 8;
     if (rc == DD_OK) rc = launch_after(ctx, attention_delta_kernel<lanes>, (b.tokens * b.heads * lanes + 255) / 256, 256, 0, stream, d);
     const uint64_t tiles = most_tiles(b, kTile);
-    if (rc == DD_OK) rc = launch_after(ctx, attention_dq_kernel<DP>, tiles * b.heads, kAttnThreads, bwd_smem_bytes(DP), stream, a);
-    if (rc == DD_OK) rc = launch_after(ctx, attention_dkv_kernel<DP>, tiles * b.kv_heads, kAttnThreads, bwd_smem_bytes(DP), stream, a);
+    if (rc == DD_OK) rc = launch_after(ctx, attention_dq_kernel<DP>, tiles * b.heads, 32 * (kBwdWarps + 4), bwd_smem_bytes(DP), stream, a);
+    if (rc == DD_OK) rc = launch_after(ctx, attention_dkv_kernel<DP>, tiles * b.kv_heads, 32 * (kBwdWarps + 4), bwd_smem_bytes(DP), stream, a);
     return rc;
 }
 

@@ -1,9 +1,10 @@
 // Attention over packed sequences on tcgen05: scores, weights and gradients of 128 x 128 tiles live in tensor
 // memory and registers, nothing of a tile's size goes to global memory.
 //
-// Roles of a CTA (384 threads): warps 0-7 compute on tiles (a thread owns a row of an accumulator, the
-// lane of tensor memory that it can reach), warp 8 has the TMA engine fill rings of operand tiles, warp 9 issues
-// the products; warps 8-11 give registers to the others (a warpgroup does so as a whole).  An operand tile is 128 tokens of one head: one or two boxes of 64 elements a row
+// Roles of a CTA: warps 0-7 (backward 0-15) compute on tiles (a thread owns a row of an accumulator, the lane of
+// tensor memory that it can reach, or some columns of it); of the four warps behind them one has the TMA engine
+// fill rings of operand tiles, one issues the products, and all give registers to the others (a warpgroup does so
+// as a whole).  An operand tile is 128 tokens of one head: one or two boxes of 64 elements a row
 // (128-byte swizzle), columns past `dim` filled with zeros by the TMA engine.  Tiles may reach past their
 // sequence: scores there are masked, and rows that a product sums over are zeroed in shared memory
 // first, since a weight of 0 does not silence a NaN of the neighbour's.
@@ -23,7 +24,7 @@ namespace ddm {
 
 constexpr int kTile = 128;                        // rows of a tile
 constexpr int kBoxTile = kTile * 128;             // bytes of a box: 128 rows of 64 bf16
-constexpr int kAttnThreads = 384, kAttnProducer = 8, kAttnIssuer = 9;
+constexpr int kFwdWarps = 8, kBwdWarps = 16;      // that compute; four more follow
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Tiles of all sequences, those with most work first.
@@ -82,6 +83,15 @@ __device__ __forceinline__ void tmem_st32(unsigned addr, const unsigned (&r)[32]
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_st16(unsigned addr, const unsigned (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+        :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+           "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+        : "memory");
+}
+
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void init_bar(unsigned bar, unsigned count)
@@ -122,14 +132,14 @@ __device__ __forceinline__ void mma_rows(unsigned d, unsigned a, unsigned b)
     for (int k = 0; k < DP / 16; ++k) umma_bf16(d, desc_rows(a, k), desc_rows(b, k), attn_idesc(kTile, false), k != 0);
 }
 
-// d (+)= A B with A (128 x 128 bf16) in tensor memory, its columns 0-63 at `a` and 64-127 at `a` + HALF, and B a
+// d (+)= A B with A (128 x 128 bf16) in tensor memory, every 32 of its columns STEP columns of it on, and B a
 // tile's 128 rows of DP columns.
-template <int DP, int HALF>
+template <int DP, int STEP>
 __device__ __forceinline__ void mma_weights(unsigned d, unsigned a, unsigned b, bool accumulate)
 {
 #pragma unroll
     for (int k = 0; k < kTile / 16; ++k)
-        umma_bf16_ta(d, a + (k >> 2) * HALF + (k & 3) * 8, desc_cols(b, k), attn_idesc(DP, true), accumulate || k);
+        umma_bf16_ta(d, a + (k >> 1) * STEP + (k & 1) * 8, desc_cols(b, k), attn_idesc(DP, true), accumulate || k);
 }
 
 // One operand tile: tokens token .. token + 127 of a head.
@@ -165,6 +175,20 @@ __device__ __forceinline__ void store_row32(__nv_bfloat16 *row, unsigned col, un
     }
 }
 
+// 2^(x c + off) of two scores.
+__device__ __forceinline__ float2 exp2_pair(unsigned x0, unsigned x1, float c, float2 off)
+{
+    const float2 x = __ffma2_rn(make_float2(__uint_as_float(x0), __uint_as_float(x1)), make_float2(c, c), off);
+    return make_float2(exp2_fast(x.x), exp2_fast(x.y));
+}
+
+// p (dp - delta) of two, as bf16.
+__device__ __forceinline__ unsigned ds_pair(float2 p, unsigned dp0, unsigned dp1, float2 minus_delta)
+{
+    const float2 d = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(dp0), __uint_as_float(dp1)), minus_delta));
+    return pack2(d.x, d.y);
+}
+
 // The tile of block-wide index `i`: most work first.  False: there is none.
 __device__ __forceinline__ bool plan_item(const AttnArgs &a, unsigned i, PlanItem &item)
 {
@@ -185,11 +209,12 @@ struct AttnShared {
     unsigned tmem_base;
 };
 
+template <int WARPS>
 __device__ __forceinline__ unsigned attn_begin(AttnShared &sh, int warp)
 {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    if (warp == kAttnIssuer) {
+    if (warp == WARPS + 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_addr(&sh.tmem_base)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -202,19 +227,29 @@ __device__ __forceinline__ unsigned attn_begin(AttnShared &sh, int warp)
     return sh.tmem_base;
 }
 
+template <int WARPS>
 __device__ __forceinline__ void attn_end(AttnShared &sh, const AttnArgs &a, int warp, unsigned tmem)
 {
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == kAttnIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+    if (warp == WARPS + 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
     if (threadIdx.x == 0 && sh.abort_flag && a.status) *a.status = DD_STATUS_WAIT_LIMIT;
 }
 
-// The launch has 168 registers for each of 384 threads: 208 for two warpgroups and 88 for the third are as many.
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
+// A launch has 168 registers for each of 384 threads (forward) or 96 for each of 640 (backward): 208 for two
+// warpgroups and 88 for the third, or 104 for four and 64 for the fifth, are as many.
+template <int WARPS>
+__device__ __forceinline__ void more_registers()
+{
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(WARPS == kFwdWarps ? 208 : 104));
+}
+template <int WARPS>
+__device__ __forceinline__ void fewer_registers()
+{
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(WARPS == kFwdWarps ? 88 : 64));
+}
 
 // Lane 0 of a warp reports that the warp is done with (or has written) its part of tensor memory.
 __device__ __forceinline__ void warp_arrive(unsigned bar, int lane)
@@ -232,7 +267,7 @@ __host__ __device__ constexpr int fwd_stages(int dp) { return dp == 128 ? 4 : 6;
 __host__ __device__ constexpr unsigned fwd_smem_bytes(int dp) { return 1024 + (2 + fwd_stages(dp)) * kTile * dp * 2; }
 
 template <int DP>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+__global__ void __launch_bounds__(32 * (kFwdWarps + 4), 1)
 attention_forward_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr int kStages = fwd_stages(DP);
@@ -268,12 +303,12 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
         }
         init_bar(drain, 1);
     }
-    const unsigned tmem = attn_begin(sh, warp);
+    const unsigned tmem = attn_begin<kFwdWarps>(sh, warp);
     const unsigned kS = tmem, kO = tmem + 2 * kTile;                         // scores of tile t at kS + 128 t, sums at kO + DP t
 
-    if (warp >= kAttnProducer) {
-        fewer_registers();
-        if (warp == kAttnProducer && elect_one()) {
+    if (warp >= kFwdWarps) {
+        fewer_registers<kFwdWarps>();
+        if (warp == kFwdWarps && elect_one()) {
             const int token = (int)(item.start + row0), hk = (int)(head / a.group);
             mbar_arrive_expect_tx(q_full, (n1 ? 2 : 1) * kBytes + (a.expire ? 16u : 0u));
             load_tile<DP>(smem, &a.q, (int)head, token, q_full);
@@ -287,7 +322,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             }
             mbar_wait_bounded(q_full, 0);
             for (unsigned j = it > kStages ? it - kStages : 0; j < it; ++j) mbar_wait_bounded(full + 8 * (j % kStages), (j / kStages) & 1);
-        } else if (warp == kAttnIssuer) {
+        } else if (warp == kFwdWarps + 1) {
             const auto tile_of = [&](unsigned it) { return ring + it % kStages * kBytes; };
             const auto ready = [&](unsigned it) { return gemm_wait(full + 8 * (it % kStages), (it / kStages) & 1, abort); };
             bool ok = gemm_wait(q_full, 0, abort) && ready(0);
@@ -314,7 +349,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                     ok = gemm_wait(p_full + 8 * t, j & 1, abort);
                     tc_fence_after();
                     if (!ok || lane) continue;
-                    mma_weights<DP, 32>(kO + t * DP, kS + t * kTile, v, j != 0);
+                    mma_weights<DP, 16>(kO + t * DP, kS + t * kTile, v, j != 0);
                     if (j + 1 < mine) {
                         // behind the product that reads the weights, whose place the scores take
                         mma_rows<DP>(kS + t * kTile, smem + t * kBytes, tile_of(2 * j + 2));
@@ -335,7 +370,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             }
         }
     } else {
-        more_registers();
+        more_registers<kFwdWarps>();
         const int t = warp >> 2;
         const unsigned mine = t ? n1 : n0, local = (warp & 3) * 32 + lane, row = row0 + t * kTile + local;
         const unsigned at = (unsigned)((warp & 3) * 32) << 16, s_at = kS + t * kTile + at, o_at = kO + t * DP + at;
@@ -422,12 +457,12 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             if (a.lse && row < item.len) a.lse[(unsigned long long)head * a.tokens + token] = fmaf(base, a.scale, logf(sum));
         }
     }
-    attn_end(sh, a, warp, tmem);
+    attn_end<kFwdWarps>(sh, a, warp, tmem);
 }
 
 // ---- backward --------------------------------------------------------------------------------------
 
-// dq of 128 query rows of a head.  Warps 0-3 and 4-7 take 64 columns each of the scores' rows.  Scores of the
+// dq of 128 query rows of a head.  Every four warps take 32 columns of the scores' rows.  Scores of the
 // next tile of keys are made as soon as those of this one are in registers; ds alternates between two places.
 // Two launches (this and the next kernel) form the scores twice, which costs 7 products of a tile instead of 5,
 // but no gradient is added to by several CTAs: no atomics, no float32 copy of dq in memory.
@@ -439,13 +474,13 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
 constexpr unsigned bwd_smem_bytes(int dp) { return 1024 + 6 * kTile * dp * 2; }
 
 template <int DP>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+__global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dq_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr unsigned kBytes = kTile * DP * 2;
     extern __shared__ unsigned char smem_raw[];
     __shared__ alignas(16) AttnShared sh;
-    __shared__ float halves[2][kTile];            // a row's two shares of delta
+    __shared__ float shares[4][kTile];            // of a row's delta
     asm volatile("griddepcontrol.wait;" ::: "memory");
     PlanItem item;
     if (!plan_item(a, blockIdx.x / a.heads, item)) return;
@@ -460,16 +495,16 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         for (int i = 0; i < 15; ++i) init_bar(bar + 8 * i, 1);
-        init_bar(sum_full, 8);
-        init_bar(s_read, 8);
-        init_bar(ds_full, 8);
+        init_bar(sum_full, kBwdWarps);
+        init_bar(s_read, kBwdWarps);
+        init_bar(ds_full, kBwdWarps);
     }
-    const unsigned tmem = attn_begin(sh, warp);
+    const unsigned tmem = attn_begin<kBwdWarps>(sh, warp);
     const unsigned kS = tmem, kP = tmem + kTile, kDs = tmem + 2 * kTile, kDq = tmem + 3 * kTile;      // ds at kDs + 64 (j & 1)
 
-    if (warp >= kAttnProducer) {
-        fewer_registers();
-        if (warp == kAttnProducer && elect_one()) {
+    if (warp >= kBwdWarps) {
+        fewer_registers<kBwdWarps>();
+        if (warp == kBwdWarps && elect_one()) {
             const int token = (int)(item.start + row0), hk = (int)(head / a.group);
             mbar_arrive_expect_tx(q_full, 2 * kBytes + (a.expire ? 16u : 0u));
             load_tile<DP>(sq, &a.q, (int)head, token, q_full);
@@ -484,7 +519,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             mbar_wait_bounded(q_full, 0);
             for (unsigned i = it > 4 ? it - 4 : 0; i < it; ++i)
                 mbar_wait_bounded((i & 1 ? v_full : k_full) + 8 * ((i >> 1) & 1), (i >> 2) & 1);
-        } else if (warp == kAttnIssuer) {
+        } else if (warp == kBwdWarps + 1) {
             // scores of tile j; the rows that dq sums over later are zeroed here already
             const auto scores = [&](unsigned j) {
                 const unsigned k = sk + (j & 1) * kBytes, live = item.len - j * kTile;
@@ -516,7 +551,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
                 if (!ok) break;
                 tc_fence_after();
                 if (lane == 0) {
-                    mma_weights<DP, 32>(kDq, kDs + 64 * (j & 1), sk + (j & 1) * kBytes, j != 0);
+                    mma_weights<DP, 16>(kDq, kDs + 64 * (j & 1), sk + (j & 1) * kBytes, j != 0);
                     umma_commit(j + 1 < n ? k_empty + 8 * (j & 1) : dq_full);
                 }
             }
@@ -526,8 +561,8 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             }
         }
     } else {
-        more_registers();
-        const unsigned half = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16, row = row0 + (warp & 3) * 32 + lane;
+        more_registers<kBwdWarps>();
+        const unsigned share = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16, row = row0 + (warp & 3) * 32 + lane;
         const unsigned long long token = item.start + row, stat = (unsigned long long)head * a.tokens + token;
         const float c = a.scale * kLog2e;
         const float off = row < item.len ? -a.lse[stat] * kLog2e : 0.0f;
@@ -539,70 +574,57 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             ok = __all_sync(0xffffffffu, gemm_wait(s_full, j & 1, abort));
             if (!ok) break;
             tc_fence_after();
-            unsigned r[2][32];
-            float p[2][32];
-            tmem_ld32(kS + at + 64 * half, r[0]);
-            tmem_ld32(kS + at + 64 * half + 32, r[1]);
+            unsigned r[32], w[16];
+            float2 p[16];
+            tmem_ld32(kS + at + 32 * share, r);
             tmem_ld_wait();
             warp_arrive(s_read, lane);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int k = 0; k < 32; ++k) p[h][k] = exp2_fast(fmaf(__uint_as_float(r[h][k]), c, off));
+            for (int k = 0; k < 16; ++k) p[k] = exp2_pair(r[2 * k], r[2 * k + 1], c, make_float2(off, off));
             ok = __all_sync(0xffffffffu, gemm_wait(dp_full, j & 1, abort));
             if (!ok) break;
             tc_fence_after();
-            tmem_ld32(kP + at + 64 * half, r[0]);
-            tmem_ld32(kP + at + 64 * half + 32, r[1]);
+            tmem_ld32(kP + at + 32 * share, r);
             tmem_ld_wait();
-            const unsigned first = j * kTile + 64 * half, live = end == 1 || end <= first ? 0 : end - first;
-            const bool masked = __any_sync(0xffffffffu, live < 64);
+            const unsigned first = j * kTile + 32 * share, live = end == 1 || end <= first ? 0 : end - first;
             if (n == 1) {
                 float sum = 0.0f;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (32 * h + k < live) sum = fmaf(p[h][k], __uint_as_float(r[h][k]), sum);
-                halves[half][row - row0] = sum;
+                for (int k = 0; k < 32; ++k)
+                    if (k < live) sum = fmaf(k & 1 ? p[k / 2].y : p[k / 2].x, __uint_as_float(r[k]), sum);
+                shares[share][row - row0] = sum;
                 __syncwarp();
                 if (lane == 0) arrive_bar(sum_full);
                 ok = __all_sync(0xffffffffu, gemm_wait(sum_full, 0, abort));
                 if (!ok) break;
-                delta = halves[0][row - row0] + halves[1][row - row0];
-                if (half == 0 && row < item.len) a.delta[stat] = delta;
+                delta = (shares[0][row - row0] + shares[1][row - row0]) + (shares[2][row - row0] + shares[3][row - row0]);
+                if (share == 0 && row < item.len) a.delta[stat] = delta;
             }
-            unsigned w[32];
+            if (__any_sync(0xffffffffu, live < 32)) {
+                // masked: a weight of 0, and a dp that may be NaN past the sequence's end counts as delta
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    float d0 = p[h][2 * k] * (__uint_as_float(r[h][2 * k]) - delta), d1 = p[h][2 * k + 1] * (__uint_as_float(r[h][2 * k + 1]) - delta);
-                    if (masked) {
-                        if (32 * h + 2 * k >= live) d0 = 0.0f;
-                        if (32 * h + 2 * k + 1 >= live) d1 = 0.0f;
+                for (int k = 0; k < 32; ++k)
+                    if (k >= live) {
+                        r[k] = __float_as_uint(delta);
+                        (k & 1 ? p[k / 2].y : p[k / 2].x) = 0.0f;
                     }
-                    w[16 * h + k] = pack2(d0, d1);
-                }
-            tmem_st32(kDs + at + 64 * (j & 1) + 32 * half, w);
+            }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k] = ds_pair(p[k], r[2 * k], r[2 * k + 1], make_float2(-delta, -delta));
+            tmem_st16(kDs + at + 64 * (j & 1) + 16 * share, w);
             tmem_st_wait();
             warp_arrive(ds_full, lane);
         }
         if (ok) ok = __all_sync(0xffffffffu, gemm_wait(dq_full, 0, abort));
-        if (ok) {
+        if (ok && 32 * share < DP) {
             tc_fence_after();
-            __nv_bfloat16 *o = a.dq.data + token * a.dq.ld_token + head * a.dq.ld_head;
-#pragma unroll
-            for (int i = 0; i < DP / 64; ++i) {
-                unsigned w[32];
-                const unsigned col = half * (DP / 2) + 32 * i;
-                tmem_ld32(kDq + at + col, w);
-                tmem_ld_wait();
-                if (row < item.len) store_row32(o, col, a.dim, w, a.scale);
-            }
+            unsigned w[32];
+            tmem_ld32(kDq + at + 32 * share, w);
+            tmem_ld_wait();
+            if (row < item.len) store_row32(a.dq.data + token * a.dq.ld_token + head * a.dq.ld_head, 32 * share, a.dim, w, a.scale);
         }
     }
-    attn_end(sh, a, warp, tmem);
+    attn_end<kBwdWarps>(sh, a, warp, tmem);
 }
 
 // dk and dv of 128 rows of a head of keys, over the query heads that share it and their tiles of queries.
@@ -610,13 +632,13 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
 // Products and weights alternate on the same places: dv of a tile, then the next tile's scores, run while ds
 // is computed; dk and the next dp while the next weights are.
 template <int DP>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+__global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dkv_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr unsigned kBytes = kTile * DP * 2;
     extern __shared__ unsigned char smem_raw[];
     __shared__ alignas(16) AttnShared sh;
-    __shared__ alignas(16) float2 stats[2][kTile];                           // -lse log2(e) and delta of a tile's queries
+    __shared__ alignas(16) float stats[2][2][kTile];                         // -lse log2(e) and -delta of a tile's queries
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const unsigned kv_heads = a.heads / a.group;
     PlanItem item;
@@ -633,16 +655,16 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         for (int i = 0; i < 16; ++i) init_bar(bar + 8 * i, 1);
-        init_bar(p_full, 8);
-        init_bar(ds_full, 8);
+        init_bar(p_full, kBwdWarps);
+        init_bar(ds_full, kBwdWarps);
         init_bar(st_full, 8);
     }
-    const unsigned tmem = attn_begin(sh, warp);
+    const unsigned tmem = attn_begin<kBwdWarps>(sh, warp);
     const unsigned kS = tmem, kP = tmem + kTile, kDv = tmem + 2 * kTile, kDk = kDv + DP;
 
-    if (warp >= kAttnProducer) {
-        fewer_registers();
-        if (warp == kAttnProducer && elect_one()) {
+    if (warp >= kBwdWarps) {
+        fewer_registers<kBwdWarps>();
+        if (warp == kBwdWarps && elect_one()) {
             mbar_arrive_expect_tx(kv_full, 2 * kBytes + (a.expire ? 16u : 0u));
             load_tile<DP>(sk, &a.k, (int)hk, (int)(item.start + row0), kv_full);
             load_tile<DP>(sv, &a.v, (int)hk, (int)(item.start + row0), kv_full);
@@ -657,7 +679,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             mbar_wait_bounded(kv_full, 0);
             for (unsigned i = it > 4 ? it - 4 : 0; i < it; ++i)
                 mbar_wait_bounded((i & 1 ? do_full : q_full) + 8 * ((i >> 1) & 1), (i >> 2) & 1);
-        } else if (warp == kAttnIssuer) {
+        } else if (warp == kBwdWarps + 1) {
             // the product of keys (values) with tile j of queries (their gradients), whose rows past the sequence's end
             // are summed over later
             const auto product = [&](unsigned j, bool second) {
@@ -678,7 +700,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                 if (!ok) break;
                 tc_fence_after();
                 if (lane == 0) {
-                    mma_weights<DP, 64>(kDv, kS, sdo + s * kBytes, j != 0);
+                    mma_weights<DP, 32>(kDv, kS, sdo + s * kBytes, j != 0);
                     umma_commit(do_empty + 8 * s);
                 }
                 if (j + 1 < n) ok = product(j + 1, false);
@@ -686,7 +708,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                 if (!ok) break;
                 tc_fence_after();
                 if (lane == 0) {
-                    mma_weights<DP, 64>(kDk, kP, sq + s * kBytes, j != 0);
+                    mma_weights<DP, 32>(kDk, kP, sq + s * kBytes, j != 0);
                     umma_commit(q_empty + 8 * s);
                 }
                 if (j + 1 < n) ok = product(j + 1, true);
@@ -698,95 +720,92 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             }
         }
     } else {
-        more_registers();
-        const unsigned half = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16, row = row0 + (warp & 3) * 32 + lane;
+        more_registers<kBwdWarps>();
+        const unsigned share = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16, row = row0 + (warp & 3) * 32 + lane;
         const float c = a.scale * kLog2e;
-        // this thread's share of the statistics: lse or delta of one query of tile j
+        // the first 256 threads fetch the statistics: lse or delta of one query of tile j
         const auto stat = [&](unsigned j) {
             const unsigned i = (i0 + j % per) * kTile + (threadIdx.x & 127), h = hk * a.group + j / per;
-            if (i >= item.len) return 0.0f;
+            if (share >= 2 || i >= item.len) return 0.0f;
             const unsigned long long where = (unsigned long long)h * a.tokens + item.start + i;
-            return half ? a.delta[where] : -a.lse[where] * kLog2e;
+            return share ? -a.delta[where] : -a.lse[where] * kLog2e;
         };
         float next = stat(0);
         bool ok = true;
         for (unsigned j = 0; j < n; ++j) {
-            float *put = reinterpret_cast<float *>(&stats[j & 1][threadIdx.x & 127]) + half;
-            *put = next;
-            __syncwarp();
-            if (lane == 0) arrive_bar(st_full);
-            if (j + 1 < n) next = stat(j + 1);
-            const unsigned q0 = (i0 + j % per) * kTile + 64 * half;           // the first of this warp's 64 queries
+            if (share < 2) {
+                stats[j & 1][share][threadIdx.x & 127] = next;
+                __syncwarp();
+                if (lane == 0) arrive_bar(st_full);
+                if (j + 1 < n) next = stat(j + 1);
+            }
+            const unsigned q0 = (i0 + j % per) * kTile + 32 * share;          // the first of this warp's 32 queries
             // queries from `from` to `to` count
             const unsigned to = item.len > q0 ? item.len - q0 : 0, from = a.causal && row > q0 ? row - q0 : 0;
-            const bool masked = __any_sync(0xffffffffu, to < 64 || from > 0) || (a.causal && q0 == 0);
+            const bool masked = __any_sync(0xffffffffu, to < 32 || from > 0) || (a.causal && q0 == 0);
             ok = gemm_wait(st_full, j & 1, abort) && gemm_wait(s_full, j & 1, abort);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
-            const float4 *st = reinterpret_cast<const float4 *>(&stats[j & 1][64 * half]);     // two queries each
-            unsigned r[2][32], w[32];
-            float p[2][32];
-            tmem_ld32(kS + at + 64 * half, r[0]);
-            tmem_ld32(kS + at + 64 * half + 32, r[1]);
+            const float4 *offs = reinterpret_cast<const float4 *>(&stats[j & 1][0][32 * share]), *deltas = offs + kTile / 4;
+            unsigned r[32], w[16];
+            float2 p[16];
+            tmem_ld32(kS + at + 32 * share, r);
             tmem_ld_wait();
+            if (masked) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int k = 0; k < 32; ++k)
+                    if (k < from || k >= to) r[k] = 0xff800000u;
+            }
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const float4 x = st[16 * h + k];
-                    float p0 = exp2_fast(fmaf(__uint_as_float(r[h][2 * k]), c, x.x)), p1 = exp2_fast(fmaf(__uint_as_float(r[h][2 * k + 1]), c, x.z));
-                    if (masked) {
-                        const unsigned i = 32 * h + 2 * k;
-                        if (i < from || i >= to) p0 = 0.0f;
-                        if (i + 1 < from || i + 1 >= to) p1 = 0.0f;
-                    }
-                    p[h][2 * k] = p0;
-                    p[h][2 * k + 1] = p1;
-                    w[16 * h + k] = pack2(p0, p1);
-                }
-            tmem_st32(kS + at + 64 * half, w);
+            for (int k = 0; k < 8; ++k) {
+                const float4 x = offs[k];
+                p[2 * k] = exp2_pair(r[4 * k], r[4 * k + 1], c, make_float2(x.x, x.y));
+                p[2 * k + 1] = exp2_pair(r[4 * k + 2], r[4 * k + 3], c, make_float2(x.z, x.w));
+                w[2 * k] = pack2(p[2 * k].x, p[2 * k].y);
+                w[2 * k + 1] = pack2(p[2 * k + 1].x, p[2 * k + 1].y);
+            }
+            tmem_st16(kS + at + 32 * share, w);
             tmem_st_wait();
             warp_arrive(p_full, lane);
             ok = __all_sync(0xffffffffu, gemm_wait(dp_full, j & 1, abort));
             if (!ok) break;
             tc_fence_after();
-            tmem_ld32(kP + at + 64 * half, r[0]);
-            tmem_ld32(kP + at + 64 * half + 32, r[1]);
+            tmem_ld32(kP + at + 32 * share, r);
             tmem_ld_wait();
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int k = 0; k < 8; ++k) {
+                const float4 x = deltas[k];
+                w[2 * k] = ds_pair(p[2 * k], r[4 * k], r[4 * k + 1], make_float2(x.x, x.y));
+                w[2 * k + 1] = ds_pair(p[2 * k + 1], r[4 * k + 2], r[4 * k + 3], make_float2(x.z, x.w));
+            }
+            if (masked) {
+                // whatever dp was: past the sequence's end it may be NaN; a token that sees itself alone has ds = 0
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const float4 x = st[16 * h + k];
-                    float d0 = p[h][2 * k] * (__uint_as_float(r[h][2 * k]) - x.y), d1 = p[h][2 * k + 1] * (__uint_as_float(r[h][2 * k + 1]) - x.w);
-                    if (masked) {
-                        // a dp past the sequence's end may be NaN; a token that sees itself alone has ds = 0
-                        const unsigned i = 32 * h + 2 * k;
-                        if (i < from || i >= to || (a.causal ? q0 + i == 0 : item.len == 1)) d0 = 0.0f;
-                        if (i + 1 < from || i + 1 >= to) d1 = 0.0f;
-                    }
-                    w[16 * h + k] = pack2(d0, d1);
-                }
-            tmem_st32(kP + at + 64 * half, w);
+                for (int k = 0; k < 32; ++k)
+                    if (k < from || k >= to || (k == 0 && (a.causal ? q0 == 0 : item.len == 1))) w[k / 2] &= k & 1 ? 0x0000ffffu : 0xffff0000u;
+            }
+            tmem_st16(kP + at + 32 * share, w);
             tmem_st_wait();
             warp_arrive(ds_full, lane);
         }
         if (ok) ok = __all_sync(0xffffffffu, gemm_wait(done, 0, abort));
         if (ok) {
             tc_fence_after();
-            const HeadsOut &out = half ? a.dk : a.dv;
+            const bool key = share >= 2;
+            const HeadsOut &out = key ? a.dk : a.dv;
             __nv_bfloat16 *o = out.data + (unsigned long long)(item.start + row) * out.ld_token + hk * out.ld_head;
 #pragma unroll
-            for (int i = 0; i < DP / 32; ++i) {
+            for (int i = 0; i < DP / 64; ++i) {
                 unsigned w[32];
-                tmem_ld32((half ? kDk : kDv) + at + 32 * i, w);
+                const unsigned col = (share & 1) * (DP / 2) + 32 * i;
+                tmem_ld32((key ? kDk : kDv) + at + col, w);
                 tmem_ld_wait();
-                if (row < item.len) store_row32(o, 32 * i, a.dim, w, half ? a.scale : 1.0f);
+                if (row < item.len) store_row32(o, col, a.dim, w, key ? a.scale : 1.0f);
             }
         }
     }
-    attn_end(sh, a, warp, tmem);
+    attn_end<kBwdWarps>(sh, a, warp, tmem);
 }
 
 // delta = d_o . o of every row of every head; LANES = lanes of a row, 8 elements each.
