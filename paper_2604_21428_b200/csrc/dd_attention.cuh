@@ -63,14 +63,6 @@ __device__ __forceinline__ void tma_load_heads(unsigned dst, const CUtensorMap *
                  :: "r"(dst), "l"(map), "r"(x), "r"(head), "r"(token), "r"(bar) : "memory");
 }
 
-// A from tensor memory: bf16, two of a row's K elements per column.
-__device__ __forceinline__ void umma_bf16_ta(unsigned d, unsigned a, unsigned long long b, unsigned idesc, unsigned accumulate)
-{
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-                 " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-
 __device__ __forceinline__ void tmem_st32(unsigned addr, const unsigned (&r)[32])
 {
     asm volatile(
@@ -104,18 +96,23 @@ __device__ __forceinline__ void arrive_bar(unsigned bar)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
 }
 
-// Descriptors of operand tiles.  K contiguous: step k covers elements 16 k .. of every row.  Rows are K
-// (the tile's columns are N): step k covers rows 16 k .., the next 64 columns are one box on.
-__device__ __forceinline__ unsigned long long desc_rows(unsigned tile, int k)
+// Descriptors of operand tiles: the upper half is the same for all (128-byte swizzle, groups of 8 rows every
+// 1024 bytes), the lower half is the address and, where rows are K, the step to the next 64 columns.  They are
+// kept as halves, and everything they are made of is warp-uniform, because the products are fed from uniform
+// registers: with 64-bit descriptors put together for each product from per-lane values, issuing one took 115 cycles
+// and not the 64 that it runs for.
+constexpr unsigned kDescUpper = (1024 / 16) | (1u << 14) | (2u << 29);
+
+// K contiguous: step k covers elements 16 k .. of every row.
+__device__ __forceinline__ unsigned desc_rows(unsigned tile, int k)
 {
-    return umma_desc(tile + (k >> 2) * kBoxTile + (k & 3) * 32, false);
+    return ((tile >> 4) | (1u << 16)) + (k >> 2) * (kBoxTile / 16) + (k & 3) * 2;
 }
 
-__device__ __forceinline__ unsigned long long desc_cols(unsigned tile, int k)
+// Rows are K (the tile's columns are N): step k covers rows 16 k .., the next 64 columns are one box on.
+__device__ __forceinline__ unsigned desc_cols(unsigned tile, int k)
 {
-    const unsigned addr = tile + k * 2048;
-    return ((unsigned long long)(addr >> 4) & 0x3fff) | ((unsigned long long)(kBoxTile / 16) << 16) | ((unsigned long long)(1024 / 16) << 32) |
-           (1ull << 46) | (2ull << 61);
+    return ((tile >> 4) | ((unsigned)(kBoxTile / 16) << 16)) + k * 128;
 }
 
 // float32 accumulators, bf16 operands, M = 128; b_mn: B's rows are K.
@@ -129,17 +126,23 @@ template <int DP>
 __device__ __forceinline__ void mma_rows(unsigned d, unsigned a, unsigned b)
 {
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k) umma_bf16(d, desc_rows(a, k), desc_rows(b, k), attn_idesc(kTile, false), k != 0);
+    for (int k = 0; k < DP / 16; ++k)
+        asm volatile("{\n .reg .pred p;\n .reg .b64 a, b;\n mov.b64 a, {%1, %4};\n mov.b64 b, {%2, %4};\n setp.ne.b32 p, %5, 0;\n"
+                     " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}"
+                     :: "r"(d), "r"(desc_rows(a, k)), "r"(desc_rows(b, k)), "r"(attn_idesc(kTile, false)), "r"(kDescUpper), "r"(k ? 1u : 0u) : "memory");
 }
 
-// d (+)= A B with A (128 x 128 bf16) in tensor memory, every 32 of its columns STEP columns of it on, and B a
-// tile's 128 rows of DP columns.
+// d (+)= A B with A (128 x 128 bf16, two of a row's elements per column) in tensor memory, every 32 of its columns
+// STEP columns of it on, and B a tile's 128 rows of DP columns.
 template <int DP, int STEP>
 __device__ __forceinline__ void mma_weights(unsigned d, unsigned a, unsigned b, bool accumulate)
 {
 #pragma unroll
     for (int k = 0; k < kTile / 16; ++k)
-        umma_bf16_ta(d, a + (k >> 1) * STEP + (k & 1) * 8, desc_cols(b, k), attn_idesc(DP, true), accumulate || k);
+        asm volatile("{\n .reg .pred p;\n .reg .b64 b;\n mov.b64 b, {%2, %4};\n setp.ne.b32 p, %5, 0;\n"
+                     " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}"
+                     :: "r"(d), "r"(a + (k >> 1) * STEP + (k & 1) * 8), "r"(desc_cols(b, k)), "r"(attn_idesc(DP, true)), "r"(kDescUpper),
+                        "r"(k ? 1u : (unsigned)accumulate) : "memory");
 }
 
 // One operand tile: tokens token .. token + 127 of a head.
@@ -224,7 +227,7 @@ __device__ __forceinline__ unsigned attn_begin(AttnShared &sh, int warp)
     tc_fence_after();
     // only now: a launch behind this one would take the tensor memory and wait for this one's end
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    return sh.tmem_base;
+    return __shfl_sync(0xffffffffu, sh.tmem_base, 0);
 }
 
 template <int WARPS>
@@ -288,7 +291,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
     const unsigned bar = smem_addr(sh.bars), q_full = bar, full = bar + 8, empty = full + 8 * kStages, s_full = empty + 8 * kStages,
                    p_full = s_full + 16, o_full = p_full + 16, drain = o_full + 16;
     volatile int *abort = &sh.abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         init_bar(q_full, 1);
@@ -328,7 +331,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             bool ok = gemm_wait(q_full, 0, abort) && ready(0);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
-            if (ok && lane == 0) {
+            if (ok && elect_one()) {
                 mma_rows<DP>(kS, smem, tile_of(0));
                 umma_commit(s_full);
                 if (n1) {
@@ -339,16 +342,16 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             }
             for (unsigned j = 0; ok && j < n; ++j) {
                 const unsigned v = tile_of(2 * j + 1), live = item.len - j * kTile;
-                ok = ready(2 * j + 1);
+                ok = __all_sync(0xffffffffu, ready(2 * j + 1));
                 if (ok && live < kTile) zero_rows<DP>(v, live, lane);
-                if (ok && j + 1 < n) ok = ready(2 * j + 2);
+                if (ok && j + 1 < n) ok = __all_sync(0xffffffffu, ready(2 * j + 2));
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const unsigned mine = t ? n1 : n0;
                     if (!ok || j >= mine) continue;
-                    ok = gemm_wait(p_full + 8 * t, j & 1, abort);
+                    ok = __all_sync(0xffffffffu, gemm_wait(p_full + 8 * t, j & 1, abort));
                     tc_fence_after();
-                    if (!ok || lane) continue;
+                    if (!ok || !elect_one()) continue;
                     mma_weights<DP, 16>(kO + t * DP, kS + t * kTile, v, j != 0);
                     if (j + 1 < mine) {
                         // behind the product that reads the weights, whose place the scores take
@@ -358,13 +361,12 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                         umma_commit(o_full + 8 * t);
                     }
                 }
-                ok = __all_sync(0xffffffffu, ok);
-                if (ok && lane == 0) {
+                if (ok && elect_one()) {
                     umma_commit(empty + 8 * ((2 * j + 1) % kStages));
                     if (j + 1 < n) umma_commit(empty + 8 * ((2 * j + 2) % kStages));
                 }
             }
-            if (lane == 0) {
+            if (elect_one()) {
                 umma_commit(drain);                                              // no product may be in flight when tensor memory is freed
                 mbar_wait_bounded(drain, 0);
             }
@@ -491,7 +493,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
     const unsigned bar = smem_addr(sh.bars), q_full = bar, k_full = bar + 8, k_empty = bar + 24, v_full = bar + 40, v_empty = bar + 56,
                    s_full = bar + 72, s_read = bar + 80, dp_full = bar + 88, ds_full = bar + 96, dq_full = bar + 104, drain = bar + 112, sum_full = bar + 120;
     volatile int *abort = &sh.abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         for (int i = 0; i < 15; ++i) init_bar(bar + 8 * i, 1);
@@ -526,7 +528,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
                 if (!__all_sync(0xffffffffu, gemm_wait(k_full + 8 * (j & 1), (j >> 1) & 1, abort))) return false;
                 if (live < kTile) zero_rows<DP>(k, live, lane);
                 tc_fence_after();
-                if (lane == 0) {
+                if (elect_one()) {
                     mma_rows<DP>(kS, sq, k);
                     umma_commit(s_full);
                 }
@@ -535,7 +537,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             const auto weights = [&](unsigned j) {                               // dp of tile j
                 if (!__all_sync(0xffffffffu, gemm_wait(v_full + 8 * (j & 1), (j >> 1) & 1, abort))) return false;
                 tc_fence_after();
-                if (lane == 0) {
+                if (elect_one()) {
                     mma_rows<DP>(kP, sdo, sv + (j & 1) * kBytes);
                     umma_commit(dp_full);
                     umma_commit(v_empty + 8 * (j & 1));
@@ -550,12 +552,12 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
                 if (ok && j + 1 < n) ok = weights(j + 1);
                 if (!ok) break;
                 tc_fence_after();
-                if (lane == 0) {
+                if (elect_one()) {
                     mma_weights<DP, 16>(kDq, kDs + 64 * (j & 1), sk + (j & 1) * kBytes, j != 0);
                     umma_commit(j + 1 < n ? k_empty + 8 * (j & 1) : dq_full);
                 }
             }
-            if (lane == 0) {
+            if (elect_one()) {
                 umma_commit(drain);
                 mbar_wait_bounded(drain, 0);
             }
@@ -651,7 +653,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
     const unsigned bar = smem_addr(sh.bars), kv_full = bar, q_full = bar + 8, q_empty = bar + 24, do_full = bar + 40, do_empty = bar + 56,
                    s_full = bar + 72, p_full = bar + 80, dp_full = bar + 88, ds_full = bar + 96, done = bar + 104, drain = bar + 112, st_full = bar + 120;
     volatile int *abort = &sh.abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         for (int i = 0; i < 16; ++i) init_bar(bar + 8 * i, 1);
@@ -687,7 +689,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                 if (!__all_sync(0xffffffffu, gemm_wait((second ? do_full : q_full) + 8 * s, (j >> 1) & 1, abort))) return false;
                 if (live < kTile) zero_rows<DP>(t, live, lane);
                 tc_fence_after();
-                if (lane == 0) {
+                if (elect_one()) {
                     mma_rows<DP>(second ? kP : kS, second ? sv : sk, t);
                     umma_commit(second ? dp_full : s_full);
                 }
@@ -699,7 +701,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                 ok = __all_sync(0xffffffffu, gemm_wait(p_full, j & 1, abort));
                 if (!ok) break;
                 tc_fence_after();
-                if (lane == 0) {
+                if (elect_one()) {
                     mma_weights<DP, 32>(kDv, kS, sdo + s * kBytes, j != 0);
                     umma_commit(do_empty + 8 * s);
                 }
@@ -707,13 +709,13 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                 if (ok) ok = __all_sync(0xffffffffu, gemm_wait(ds_full, j & 1, abort));
                 if (!ok) break;
                 tc_fence_after();
-                if (lane == 0) {
+                if (elect_one()) {
                     mma_weights<DP, 32>(kDk, kP, sq + s * kBytes, j != 0);
                     umma_commit(q_empty + 8 * s);
                 }
                 if (j + 1 < n) ok = product(j + 1, true);
             }
-            if (lane == 0) {
+            if (elect_one()) {
                 if (ok) umma_commit(done);
                 umma_commit(drain);
                 mbar_wait_bounded(drain, 0);
