@@ -178,11 +178,44 @@ __device__ __forceinline__ void store_row32(__nv_bfloat16 *row, unsigned col, un
     }
 }
 
-// 2^(x c + off) of two scores.
-__device__ __forceinline__ float2 exp2_pair(unsigned x0, unsigned x1, float c, float2 off)
+// 2^x of two numbers on the multiply-add pipe: x = n + f with n the nearest integer (the sum with 1.5 2^23 rounds to it
+// and holds it in its low bits), 2^f by a polynomial on [-1/2, 1/2], n into the exponent.  The coefficients are
+// a minimax fit of the relative error with 2^0 = 1 held (a weighted least-squares iteration): 2.9e-6 with degree 4,
+// 1.9e-7 with degree 5 in float32, sums included.  Below -127 the result is 0, near -126.5 it is off by less than 2^-126.
+template <int DEGREE>
+__device__ __forceinline__ float2 exp2_poly(float2 x)
+{
+    static_assert(DEGREE == 4 || DEGREE == 5, "a fit for each degree");
+    constexpr float c4[] = {0.6931241750717163f, 0.24024099111557007f, 0.055906426161527634f, 0.009582852944731712f},
+                    c5[] = {0.6931470036506653f, 0.24022242426872253f, 0.05550733581185341f, 0.009671512991189957f, 0.001326472731307149f};
+    constexpr float kRound = 12582912.0f;
+    x.x = fmaxf(x.x, -127.0f);
+    x.y = fmaxf(x.y, -127.0f);
+    const float2 t = __fadd2_rn(x, make_float2(kRound, kRound)), n = __fadd2_rn(t, make_float2(-kRound, -kRound)),
+                 f = __ffma2_rn(n, make_float2(-1.0f, -1.0f), x);
+    const auto both = [](float c) { return make_float2(c, c); };
+    float2 p = both(DEGREE == 4 ? c4[3] : c5[4]);
+#pragma unroll
+    for (int i = DEGREE - 2; i >= 0; --i) p = __ffma2_rn(p, f, both(DEGREE == 4 ? c4[i < 4 ? i : 3] : c5[i]));
+    p = __ffma2_rn(p, f, both(1.0f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+
+// 2^(x c + off) of two scores, by the special function unit (16 a clock and SM, which alone would hold the kernels up)
+// or, for some of the pairs, by the polynomial.
+template <int DEGREE>
+__device__ __forceinline__ float2 exp2_pair(unsigned x0, unsigned x1, float c, float2 off, bool poly)
 {
     const float2 x = __ffma2_rn(make_float2(__uint_as_float(x0), __uint_as_float(x1)), make_float2(c, c), off);
-    return make_float2(exp2_fast(x.x), exp2_fast(x.y));
+    return poly ? exp2_poly<DEGREE>(x) : make_float2(exp2_fast(x.x), exp2_fast(x.y));
+}
+
+// Maximum of three; a NaN among them is the result.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float m;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
 }
 
 // p (dp - delta) of two, as bf16.
@@ -261,6 +294,13 @@ __device__ __forceinline__ void warp_arrive(unsigned bar, int lane)
     __syncwarp();
     if (lane == 0) arrive_bar(bar);
 }
+
+// Of eight pairs, those whose exponentials are polynomials (a bit each).
+#ifndef DD_FWD_POLY
+#define DD_FWD_POLY 0x4a
+#define DD_BWD_POLY 0x55
+#endif
+constexpr unsigned kFwdPoly = DD_FWD_POLY, kBwdPoly = DD_BWD_POLY;
 
 // ---- forward ---------------------------------------------------------------------------------------
 
@@ -399,11 +439,11 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             float m[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                m[i] = __uint_as_float(r[i][0]);
+                m[i] = max3(__uint_as_float(r[i][0]), __uint_as_float(r[i][1]), i ? -INFINITY : top);
 #pragma unroll
-                for (int k = 1; k < 32; ++k) m[i] = fmaxf(m[i], __uint_as_float(r[i][k]));
+                for (int k = 2; k < 32; k += 2) m[i] = max3(m[i], __uint_as_float(r[i][k]), __uint_as_float(r[i][k + 1]));
             }
-            const float now = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+            const float now = max3(m[0], m[1], max3(m[2], m[3], -INFINITY));
             // The sums are moved to a larger maximum only when it has grown by more than 2^8: until then the
             // weights stay below 2^8, exact in float32 and as far from the end of bf16's range.
             if (__any_sync(0xffffffffu, !((now - top) * c <= 8.0f))) {
@@ -425,21 +465,19 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                 base = next;
             }
             const float off = -base * c;
-            float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                unsigned w[32];
+            for (int h = 0; h < 4; ++h) {
+                unsigned w[16];
 #pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    const float p0 = exp2_fast(fmaf(__uint_as_float(r[2 * h + k / 16][2 * k % 32]), c, off)),
-                                p1 = exp2_fast(fmaf(__uint_as_float(r[2 * h + k / 16][2 * k % 32 + 1]), c, off));
-                    part[k & 1] += p0;
-                    part[2 + (k & 1)] += p1;
-                    w[k] = pack2(p0, p1);
+                for (int k = 0; k < 16; ++k) {
+                    const float2 p = exp2_pair<5>(r[h][2 * k], r[h][2 * k + 1], c, make_float2(off, off), kFwdPoly >> (k % 8) & 1);
+                    part[k & 1] = __fadd2_rn(part[k & 1], p);
+                    w[k] = pack2(p.x, p.y);
                 }
-                tmem_st32(s_at + 32 * h, w);
+                tmem_st16(s_at + 16 * h, w);
             }
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
+            sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
             tmem_st_wait();
             warp_arrive(p_full + 8 * t, lane);
         }
@@ -473,30 +511,38 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
 // weight dp - delta is a small difference.  So rows whose keys are all in one tile, the short sequences and the
 // beginnings of long ones, take the sum itself and leave it for the next launch (two keys: gradients within
 // 0.25 % instead of 0.75 %).
-constexpr unsigned bwd_smem_bytes(int dp) { return 1024 + 6 * kTile * dp * 2; }
+// What a backward CTA has in shared memory: two tiles that stay, rings of three and of two for the others
+// (the ring whose tiles two products read, one of them late, is the longer one), and the rest.
+struct BwdShared {
+    AttnShared sh;
+    alignas(16) float row[4][kTile];
+};
+constexpr unsigned bwd_smem_bytes(int dp) { return 7 * kTile * dp * 2 + sizeof(BwdShared); }
+static_assert(bwd_smem_bytes(128) <= 227 * 1024, "shared memory of an SM");
 
 template <int DP>
 __global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dq_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr unsigned kBytes = kTile * DP * 2;
-    extern __shared__ unsigned char smem_raw[];
-    __shared__ alignas(16) AttnShared sh;
-    __shared__ float shares[4][kTile];            // of a row's delta
+    extern __shared__ __align__(1024) unsigned char smem_tiles[];
+    BwdShared &rest = *reinterpret_cast<BwdShared *>(smem_tiles + 7 * kBytes);
+    AttnShared &sh = rest.sh;
+    float (&shares)[4][kTile] = rest.row;         // of a row's delta
     asm volatile("griddepcontrol.wait;" ::: "memory");
     PlanItem item;
     if (!plan_item(a, blockIdx.x / a.heads, item)) return;
     const unsigned head = blockIdx.x % a.heads, row0 = item.tile * kTile, all = (item.len + kTile - 1) / kTile;
     const unsigned n = a.causal ? item.tile + 1 : all;
 
-    const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u, sq = smem, sdo = smem + kBytes, sk = smem + 2 * kBytes, sv = smem + 4 * kBytes;
-    const unsigned bar = smem_addr(sh.bars), q_full = bar, k_full = bar + 8, k_empty = bar + 24, v_full = bar + 40, v_empty = bar + 56,
-                   s_full = bar + 72, s_read = bar + 80, dp_full = bar + 88, ds_full = bar + 96, dq_full = bar + 104, drain = bar + 112, sum_full = bar + 120;
+    const unsigned smem = smem_addr(smem_tiles), sq = smem, sdo = smem + kBytes, sk = smem + 2 * kBytes, sv = smem + 5 * kBytes;
+    const unsigned bar = smem_addr(sh.bars), k_full = bar, k_empty = bar + 24, v_full = bar + 48, v_empty = bar + 64, q_full = bar + 80,
+                   s_full = bar + 88, s_read = bar + 96, dp_full = bar + 104, ds_full = bar + 112, dq_full = bar + 120, drain = bar + 128, sum_full = bar + 136;
     volatile int *abort = &sh.abort_flag;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
-        for (int i = 0; i < 15; ++i) init_bar(bar + 8 * i, 1);
+        for (int i = 0; i < 17; ++i) init_bar(bar + 8 * i, 1);
         init_bar(sum_full, kBwdWarps);
         init_bar(s_read, kBwdWarps);
         init_bar(ds_full, kBwdWarps);
@@ -513,19 +559,22 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             load_tile<DP>(sdo, &a.d_o, (int)head, token, q_full);
             unsigned it = 0;
             for (; it < 2 * n; ++it) {                                       // keys 0, values 0, keys 1, ...
-                const unsigned j = it >> 1, s = j & 1, full = (it & 1 ? v_full : k_full) + 8 * s, empty = (it & 1 ? v_empty : k_empty) + 8 * s;
-                if ((j >= 2 && !gemm_wait(empty, (j / 2 - 1) & 1, abort)) || *abort) break;
+                const unsigned j = it >> 1, slots = it & 1 ? 2 : 3, s = j % slots, full = (it & 1 ? v_full : k_full) + 8 * s,
+                               empty = (it & 1 ? v_empty : k_empty) + 8 * s;
+                if ((j >= slots && !gemm_wait(empty, (j / slots - 1) & 1, abort)) || *abort) break;
                 mbar_arrive_expect_tx(full, kBytes);
                 load_tile<DP>((it & 1 ? sv : sk) + s * kBytes, it & 1 ? &a.v : &a.k, hk, (int)(item.start + j * kTile), full);
             }
             mbar_wait_bounded(q_full, 0);
-            for (unsigned i = it > 4 ? it - 4 : 0; i < it; ++i)
-                mbar_wait_bounded((i & 1 ? v_full : k_full) + 8 * ((i >> 1) & 1), (i >> 2) & 1);
+            for (unsigned i = it > 6 ? it - 6 : 0; i < it; ++i) {
+                const unsigned j = i >> 1, slots = i & 1 ? 2 : 3;
+                if (j + slots >= (it + 1 - (i & 1)) / 2) mbar_wait_bounded((i & 1 ? v_full : k_full) + 8 * (j % slots), (j / slots) & 1);
+            }
         } else if (warp == kBwdWarps + 1) {
             // scores of tile j; the rows that dq sums over later are zeroed here already
             const auto scores = [&](unsigned j) {
-                const unsigned k = sk + (j & 1) * kBytes, live = item.len - j * kTile;
-                if (!__all_sync(0xffffffffu, gemm_wait(k_full + 8 * (j & 1), (j >> 1) & 1, abort))) return false;
+                const unsigned k = sk + j % 3 * kBytes, live = item.len - j * kTile;
+                if (!__all_sync(0xffffffffu, gemm_wait(k_full + 8 * (j % 3), j / 3 & 1, abort))) return false;
                 if (live < kTile) zero_rows<DP>(k, live, lane);
                 tc_fence_after();
                 if (elect_one()) {
@@ -553,8 +602,8 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
-                    mma_weights<DP, 16>(kDq, kDs + 64 * (j & 1), sk + (j & 1) * kBytes, j != 0);
-                    umma_commit(j + 1 < n ? k_empty + 8 * (j & 1) : dq_full);
+                    mma_weights<DP, 16>(kDq, kDs + 64 * (j & 1), sk + j % 3 * kBytes, j != 0);
+                    umma_commit(j + 1 < n ? k_empty + 8 * (j % 3) : dq_full);
                 }
             }
             if (elect_one()) {
@@ -582,7 +631,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             tmem_ld_wait();
             warp_arrive(s_read, lane);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) p[k] = exp2_pair(r[2 * k], r[2 * k + 1], c, make_float2(off, off));
+            for (int k = 0; k < 16; ++k) p[k] = exp2_pair<4>(r[2 * k], r[2 * k + 1], c, make_float2(off, off), kBwdPoly >> (k % 8) & 1);
             ok = __all_sync(0xffffffffu, gemm_wait(dp_full, j & 1, abort));
             if (!ok) break;
             tc_fence_after();
@@ -638,9 +687,10 @@ __global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dkv_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr unsigned kBytes = kTile * DP * 2;
-    extern __shared__ unsigned char smem_raw[];
-    __shared__ alignas(16) AttnShared sh;
-    __shared__ alignas(16) float stats[2][2][kTile];                         // -lse log2(e) and -delta of a tile's queries
+    extern __shared__ __align__(1024) unsigned char smem_tiles[];
+    BwdShared &rest = *reinterpret_cast<BwdShared *>(smem_tiles + 7 * kBytes);
+    AttnShared &sh = rest.sh;
+    float (*stats)[2][kTile] = reinterpret_cast<float (*)[2][kTile]>(rest.row);   // of every other tile: -lse log2(e) and -delta of its queries
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const unsigned kv_heads = a.heads / a.group;
     PlanItem item;
@@ -649,14 +699,14 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
     const unsigned tile = all - 1 - item.tile, row0 = tile * kTile;          // early keys are read by most queries
     const unsigned i0 = a.causal ? tile : 0, per = all - i0, n = per * a.group;
 
-    const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u, sk = smem, sv = smem + kBytes, sq = smem + 2 * kBytes, sdo = smem + 4 * kBytes;
-    const unsigned bar = smem_addr(sh.bars), kv_full = bar, q_full = bar + 8, q_empty = bar + 24, do_full = bar + 40, do_empty = bar + 56,
-                   s_full = bar + 72, p_full = bar + 80, dp_full = bar + 88, ds_full = bar + 96, done = bar + 104, drain = bar + 112, st_full = bar + 120;
+    const unsigned smem = smem_addr(smem_tiles), sk = smem, sv = smem + kBytes, sq = smem + 2 * kBytes, sdo = smem + 5 * kBytes;
+    const unsigned bar = smem_addr(sh.bars), q_full = bar, q_empty = bar + 24, do_full = bar + 48, do_empty = bar + 64, kv_full = bar + 80,
+                   s_full = bar + 88, p_full = bar + 96, dp_full = bar + 104, ds_full = bar + 112, done = bar + 120, drain = bar + 128, st_full = bar + 136;
     volatile int *abort = &sh.abort_flag;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
-        for (int i = 0; i < 16; ++i) init_bar(bar + 8 * i, 1);
+        for (int i = 0; i < 17; ++i) init_bar(bar + 8 * i, 1);
         init_bar(p_full, kBwdWarps);
         init_bar(ds_full, kBwdWarps);
         init_bar(st_full, 8);
@@ -672,21 +722,24 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             load_tile<DP>(sv, &a.v, (int)hk, (int)(item.start + row0), kv_full);
             unsigned it = 0;
             for (; it < 2 * n; ++it) {                                       // queries 0, gradients 0, queries 1, ...
-                const unsigned j = it >> 1, s = j & 1, full = (it & 1 ? do_full : q_full) + 8 * s, empty = (it & 1 ? do_empty : q_empty) + 8 * s;
+                const unsigned j = it >> 1, slots = it & 1 ? 2 : 3, s = j % slots, full = (it & 1 ? do_full : q_full) + 8 * s,
+                               empty = (it & 1 ? do_empty : q_empty) + 8 * s;
                 const int h = (int)(hk * a.group + j / per), token = (int)(item.start + (i0 + j % per) * kTile);
-                if ((j >= 2 && !gemm_wait(empty, (j / 2 - 1) & 1, abort)) || *abort) break;
+                if ((j >= slots && !gemm_wait(empty, (j / slots - 1) & 1, abort)) || *abort) break;
                 mbar_arrive_expect_tx(full, kBytes);
                 load_tile<DP>((it & 1 ? sdo : sq) + s * kBytes, it & 1 ? &a.d_o : &a.q, h, token, full);
             }
             mbar_wait_bounded(kv_full, 0);
-            for (unsigned i = it > 4 ? it - 4 : 0; i < it; ++i)
-                mbar_wait_bounded((i & 1 ? do_full : q_full) + 8 * ((i >> 1) & 1), (i >> 2) & 1);
+            for (unsigned i = it > 6 ? it - 6 : 0; i < it; ++i) {
+                const unsigned j = i >> 1, slots = i & 1 ? 2 : 3;
+                if (j + slots >= (it + 1 - (i & 1)) / 2) mbar_wait_bounded((i & 1 ? do_full : q_full) + 8 * (j % slots), (j / slots) & 1);
+            }
         } else if (warp == kBwdWarps + 1) {
             // the product of keys (values) with tile j of queries (their gradients), whose rows past the sequence's end
             // are summed over later
             const auto product = [&](unsigned j, bool second) {
-                const unsigned s = j & 1, t = (second ? sdo : sq) + s * kBytes, live = item.len - (i0 + j % per) * kTile;
-                if (!__all_sync(0xffffffffu, gemm_wait((second ? do_full : q_full) + 8 * s, (j >> 1) & 1, abort))) return false;
+                const unsigned slots = second ? 2 : 3, s = j % slots, t = (second ? sdo : sq) + s * kBytes, live = item.len - (i0 + j % per) * kTile;
+                if (!__all_sync(0xffffffffu, gemm_wait((second ? do_full : q_full) + 8 * s, j / slots & 1, abort))) return false;
                 if (live < kTile) zero_rows<DP>(t, live, lane);
                 tc_fence_after();
                 if (elect_one()) {
@@ -697,21 +750,20 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             };
             bool ok = __all_sync(0xffffffffu, gemm_wait(kv_full, 0, abort)) && product(0, false) && product(0, true);
             for (unsigned j = 0; ok && j < n; ++j) {
-                const unsigned s = j & 1;
                 ok = __all_sync(0xffffffffu, gemm_wait(p_full, j & 1, abort));
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
-                    mma_weights<DP, 32>(kDv, kS, sdo + s * kBytes, j != 0);
-                    umma_commit(do_empty + 8 * s);
+                    mma_weights<DP, 32>(kDv, kS, sdo + (j & 1) * kBytes, j != 0);
+                    umma_commit(do_empty + 8 * (j & 1));
                 }
                 if (j + 1 < n) ok = product(j + 1, false);
                 if (ok) ok = __all_sync(0xffffffffu, gemm_wait(ds_full, j & 1, abort));
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
-                    mma_weights<DP, 32>(kDk, kP, sq + s * kBytes, j != 0);
-                    umma_commit(q_empty + 8 * s);
+                    mma_weights<DP, 32>(kDk, kP, sq + j % 3 * kBytes, j != 0);
+                    umma_commit(q_empty + 8 * (j % 3));
                 }
                 if (j + 1 < n) ok = product(j + 1, true);
             }
@@ -762,8 +814,8 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const float4 x = offs[k];
-                p[2 * k] = exp2_pair(r[4 * k], r[4 * k + 1], c, make_float2(x.x, x.y));
-                p[2 * k + 1] = exp2_pair(r[4 * k + 2], r[4 * k + 3], c, make_float2(x.z, x.w));
+                p[2 * k] = exp2_pair<4>(r[4 * k], r[4 * k + 1], c, make_float2(x.x, x.y), kBwdPoly >> (2 * k % 8) & 1);
+                p[2 * k + 1] = exp2_pair<4>(r[4 * k + 2], r[4 * k + 3], c, make_float2(x.z, x.w), kBwdPoly >> ((2 * k + 1) % 8) & 1);
                 w[2 * k] = pack2(p[2 * k].x, p[2 * k].y);
                 w[2 * k + 1] = pack2(p[2 * k + 1].x, p[2 * k + 1].y);
             }
