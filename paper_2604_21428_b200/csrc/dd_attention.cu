@@ -195,6 +195,10 @@ extern "C" int dd_attention_backward(dd_ctx *ctx, const dd_attention *attention,
     if (rc == DD_OK) rc = encode_heads(ctx, &a.d_o, d_o, T, b.heads, b.dim);
     if (rc == DD_OK && plan) rc = launch_plan(ctx, b, kTile, plan, status, stream);
     if (rc != DD_OK) return rc;
+    a.q_rows = out_of(q);
+    a.k_rows = out_of(k);
+    a.v_rows = out_of(v);
+    a.do_rows = out_of(d_o);
     a.dq = out_of(dq);
     a.dk = out_of(dk);
     a.dv = out_of(dv);

@@ -2,9 +2,9 @@
 // memory and registers, nothing of a tile's size goes to global memory.
 //
 // Roles of a CTA: warps 0-7 (backward 0-15) compute on tiles (a thread owns a row of an accumulator, the lane of
-// tensor memory that it can reach, or some columns of it); of the four warps behind them one has the TMA engine
-// fill rings of operand tiles, one issues the products, and all give registers to the others (a warpgroup does so
-// as a whole).  An operand tile is 128 tokens of one head: one or two boxes of 64 elements a row
+// tensor memory that it can reach, or some columns of it).  Of the four warps behind them one (a lane) has the TMA
+// engine fill rings of operand tiles, one (a lane) issues the products, one zeroes rows past a sequence's end, and
+// all give registers to the others (a warpgroup does so as a whole).  An operand tile is 128 tokens of one head: one or two boxes of 64 elements a row
 // (128-byte swizzle), columns past `dim` filled with zeros by the TMA engine.  Tiles may reach past their
 // sequence: scores there are masked, and rows that a product sums over are zeroed in shared memory
 // first, since a weight of 0 does not silence a NaN of the neighbour's.
@@ -50,6 +50,7 @@ struct AttnArgs {
     float scale;
     int causal, expire;
     HeadsOut o, dq, dk, dv;
+    HeadsOut q_rows, k_rows, v_rows, do_rows;     // inputs once more, for operands that are kept in tensor memory
     float *lse;                                   // [heads][tokens]
     float *delta;                                 // [heads][tokens]: sum_j p_ij dp_ij
     int *status;
@@ -132,6 +133,18 @@ __device__ __forceinline__ void mma_rows(unsigned d, unsigned a, unsigned b)
                      :: "r"(d), "r"(desc_rows(a, k)), "r"(desc_rows(b, k)), "r"(attn_idesc(kTile, false)), "r"(kDescUpper), "r"(k ? 1u : 0u) : "memory");
 }
 
+// The same with A in tensor memory, two of a row's elements per column.  Both operands in shared memory ask for
+// 8 KB a product of 64 cycles, all that it gives; B alone leaves room for the copies.
+template <int DP>
+__device__ __forceinline__ void mma_held(unsigned d, unsigned a, unsigned b)
+{
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k)
+        asm volatile("{\n .reg .pred p;\n .reg .b64 b;\n mov.b64 b, {%2, %4};\n setp.ne.b32 p, %5, 0;\n"
+                     " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}"
+                     :: "r"(d), "r"(a + k * 8), "r"(desc_rows(b, k)), "r"(attn_idesc(kTile, false)), "r"(kDescUpper), "r"(k ? 1u : 0u) : "memory");
+}
+
 // d (+)= A B with A (128 x 128 bf16, two of a row's elements per column) in tensor memory, every 32 of its columns
 // STEP columns of it on, and B a tile's 128 rows of DP columns.
 template <int DP, int STEP>
@@ -153,9 +166,15 @@ __device__ __forceinline__ void load_tile(unsigned dst, const CUtensorMap *map, 
     for (int c = 0; c < DP / 64; ++c) tma_load_heads(dst + c * kBoxTile, map, 64 * c, head, token, bar);
 }
 
-// Zeros to the rows from `first` on; by one warp, for the products that it issues next.
+// The whole warp's wait, with one answer for all.
+__device__ __forceinline__ bool warp_wait(unsigned bar, unsigned parity, volatile int *abort)
+{
+    return __all_sync(0xffffffffu, gemm_wait(bar, parity, abort));
+}
+
+// Zeros to the rows from `first` on, by one warp, which reports it to `bar`.
 template <int DP>
-__device__ __forceinline__ void zero_rows(unsigned tile, unsigned first, int lane)
+__device__ __forceinline__ void zero_rows(unsigned tile, unsigned first, int lane, unsigned bar)
 {
 #pragma unroll
     for (int c = 0; c < DP / 64; ++c)
@@ -163,6 +182,22 @@ __device__ __forceinline__ void zero_rows(unsigned tile, unsigned first, int lan
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" :: "r"(tile + c * kBoxTile + r * 128 + (lane & 7) * 16), "r"(0) : "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
+    if (lane == 0) arrive_bar(bar);
+}
+
+// Columns col .. col + 31 of a row (null: zeros) to 16 columns of tensor memory, as operand A; dim is a multiple of 8.
+__device__ __forceinline__ void hold_row32(unsigned at, const __nv_bfloat16 *row, unsigned col, unsigned dim)
+{
+    unsigned w[16];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint4 x = row && col + 8 * j < dim ? __ldg(reinterpret_cast<const uint4 *>(row + col + 8 * j)) : make_uint4(0u, 0u, 0u, 0u);
+        w[4 * j] = x.x;
+        w[4 * j + 1] = x.y;
+        w[4 * j + 2] = x.z;
+        w[4 * j + 3] = x.w;
+    }
+    tmem_st16(at, w);
 }
 
 // 32 columns of a row, times `by`, to bf16 columns col .. of an output row; dim is a multiple of 8.
@@ -240,7 +275,7 @@ __device__ __forceinline__ bool plan_item(const AttnArgs &a, unsigned i, PlanIte
 
 // What all kernels begin and end with.
 struct AttnShared {
-    unsigned long long bars[24];
+    unsigned long long bars[28];
     int abort_flag;
     unsigned tmem_base;
 };
@@ -329,7 +364,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
 
     const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u, ring = smem + 2 * kBytes;
     const unsigned bar = smem_addr(sh.bars), q_full = bar, full = bar + 8, empty = full + 8 * kStages, s_full = empty + 8 * kStages,
-                   p_full = s_full + 16, o_full = p_full + 16, drain = o_full + 16;
+                   p_full = s_full + 16, o_full = p_full + 16, drain = o_full + 16, clean = drain + 8, tail = clean + 8;
     volatile int *abort = &sh.abort_flag;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -345,6 +380,8 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             init_bar(o_full + 8 * s, 1);
         }
         init_bar(drain, 1);
+        init_bar(clean, 1);
+        init_bar(tail, 1);
     }
     const unsigned tmem = attn_begin<kFwdWarps>(sh, warp);
     const unsigned kS = tmem, kO = tmem + 2 * kTile;                         // scores of tile t at kS + 128 t, sums at kO + DP t
@@ -360,18 +397,19 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             for (; it < 2 * n; ++it) {
                 const unsigned s = it % kStages;
                 if ((it >= kStages && !gemm_wait(empty + 8 * s, (it / kStages - 1) & 1, abort)) || *abort) break;
-                mbar_arrive_expect_tx(full + 8 * s, kBytes);
-                load_tile<DP>(ring + s * kBytes, it & 1 ? &a.v : &a.k, hk, (int)(item.start + (it >> 1) * kTile), full + 8 * s);
+                const bool cut = it == 2 * n - 1 && item.len - (n - 1) * kTile < kTile;
+                if (cut) arrive_bar(full + 8 * s);
+                mbar_arrive_expect_tx(cut ? tail : full + 8 * s, kBytes);
+                load_tile<DP>(ring + s * kBytes, it & 1 ? &a.v : &a.k, hk, (int)(item.start + (it >> 1) * kTile), cut ? tail : full + 8 * s);
+                if (cut) mbar_wait_bounded(tail, 0);
             }
             mbar_wait_bounded(q_full, 0);
             for (unsigned j = it > kStages ? it - kStages : 0; j < it; ++j) mbar_wait_bounded(full + 8 * (j % kStages), (j / kStages) & 1);
-        } else if (warp == kFwdWarps + 1) {
+        } else if (warp == kFwdWarps + 1 && elect_one()) {
             const auto tile_of = [&](unsigned it) { return ring + it % kStages * kBytes; };
             const auto ready = [&](unsigned it) { return gemm_wait(full + 8 * (it % kStages), (it / kStages) & 1, abort); };
             bool ok = gemm_wait(q_full, 0, abort) && ready(0);
-            ok = __all_sync(0xffffffffu, ok);
-            tc_fence_after();
-            if (ok && elect_one()) {
+            if (ok) {
                 mma_rows<DP>(kS, smem, tile_of(0));
                 umma_commit(s_full);
                 if (n1) {
@@ -381,35 +419,38 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                 umma_commit(empty);
             }
             for (unsigned j = 0; ok && j < n; ++j) {
-                const unsigned v = tile_of(2 * j + 1), live = item.len - j * kTile;
-                ok = __all_sync(0xffffffffu, ready(2 * j + 1));
-                if (ok && live < kTile) zero_rows<DP>(v, live, lane);
-                if (ok && j + 1 < n) ok = __all_sync(0xffffffffu, ready(2 * j + 2));
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
+                ok = ready(2 * j + 1) && (item.len - j * kTile >= kTile || gemm_wait(clean, 0, abort)) && (j + 1 == n || ready(2 * j + 2));
+#pragma unroll 1
+                for (unsigned t = 0; ok && t < 2; ++t) {
                     const unsigned mine = t ? n1 : n0;
-                    if (!ok || j >= mine) continue;
-                    ok = __all_sync(0xffffffffu, gemm_wait(p_full + 8 * t, j & 1, abort));
+                    if (j >= mine) continue;
+                    ok = gemm_wait(p_full + 8 * t, j & 1, abort);
+                    if (!ok) break;
                     tc_fence_after();
-                    if (!ok || !elect_one()) continue;
-                    mma_weights<DP, 16>(kO + t * DP, kS + t * kTile, v, j != 0);
-                    if (j + 1 < mine) {
-                        // behind the product that reads the weights, whose place the scores take
-                        mma_rows<DP>(kS + t * kTile, smem + t * kBytes, tile_of(2 * j + 2));
-                        umma_commit(s_full + 8 * t);
-                    } else {
-                        umma_commit(o_full + 8 * t);
+                    {
+                        mma_weights<DP, 16>(kO + t * DP, kS + t * kTile, tile_of(2 * j + 1), j != 0);
+                        if (j + 1 < mine) {
+                            // behind the product that reads the weights, whose place the scores take
+                            mma_rows<DP>(kS + t * kTile, smem + t * kBytes, tile_of(2 * j + 2));
+                            umma_commit(s_full + 8 * t);
+                        } else {
+                            umma_commit(o_full + 8 * t);
+                        }
                     }
                 }
-                if (ok && elect_one()) {
+                if (ok) {
                     umma_commit(empty + 8 * ((2 * j + 1) % kStages));
                     if (j + 1 < n) umma_commit(empty + 8 * ((2 * j + 2) % kStages));
                 }
             }
-            if (elect_one()) {
-                umma_commit(drain);                                              // no product may be in flight when tensor memory is freed
+            {
+                umma_commit(drain);                                          // no product may be in flight when tensor memory is freed
                 mbar_wait_bounded(drain, 0);
             }
+        } else if (warp == kFwdWarps + 2 && item.len - (n - 1) * kTile < kTile) {
+            // the last tile of values reports here and not to the issuer
+            if (warp_wait(tail, 0, abort))
+                zero_rows<DP>(ring + (2 * n - 1) % kStages * kBytes, item.len - (n - 1) * kTile, lane, clean);
         }
     } else {
         more_registers<kFwdWarps>();
@@ -420,30 +461,37 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
         float top = -INFINITY, base = 0.0f, sum = 0.0f;                      // base: top, as the exponents use it
         bool ok = true;
         for (unsigned j = 0; j < mine; ++j) {
-            ok = gemm_wait(s_full + 8 * t, j & 1, abort);
-            ok = __all_sync(0xffffffffu, ok);
+            ok = warp_wait(s_full + 8 * t, j & 1, abort);
             if (!ok) break;
             tc_fence_after();
-            unsigned r[4][32];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32 * i, r[i]);
-            tmem_ld_wait();
             const unsigned end = a.causal && row + 1 < item.len ? row + 1 : item.len, live = end > j * kTile ? end - j * kTile : 0;
-            if (__any_sync(0xffffffffu, live < kTile)) {
+            const bool masked = __any_sync(0xffffffffu, live < kTile);
+            // Scores are read twice, 32 at a time, for their maximum and for the weights: kept in registers they
+            // and the code, unrolled over all of them, are too much (it falls out of the instruction cache each time
+            // round, and the warp that issues the products waits for it).
+            unsigned r[2][32];
+            const auto mask = [&](unsigned (&x)[32], unsigned first) {
+                if (!masked) return;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int k = 0; k < 32; ++k)
+                    if (first + k >= live) x[k] = 0xff800000u;                // -infinity
+            };
+            float now = top;
+#pragma unroll 1
+            for (int i = 0; i < 4; i += 2) {
+                tmem_ld32(s_at + 32 * i, r[0]);
+                tmem_ld32(s_at + 32 * i + 32, r[1]);
+                tmem_ld_wait();
+                mask(r[0], 32 * i);
+                mask(r[1], 32 * i + 32);
+                float m[4] = {now, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (32 * i + k >= live) r[i][k] = 0xff800000u;        // -infinity
+                for (int k = 0; k < 32; k += 2) {
+                    m[k / 2 & 1] = max3(m[k / 2 & 1], __uint_as_float(r[0][k]), __uint_as_float(r[0][k + 1]));
+                    m[2 + (k / 2 & 1)] = max3(m[2 + (k / 2 & 1)], __uint_as_float(r[1][k]), __uint_as_float(r[1][k + 1]));
+                }
+                now = max3(max3(m[0], m[1], m[2]), m[3], -INFINITY);
             }
-            float m[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                m[i] = max3(__uint_as_float(r[i][0]), __uint_as_float(r[i][1]), i ? -INFINITY : top);
-#pragma unroll
-                for (int k = 2; k < 32; k += 2) m[i] = max3(m[i], __uint_as_float(r[i][k]), __uint_as_float(r[i][k + 1]));
-            }
-            const float now = max3(m[0], m[1], max3(m[2], m[3], -INFINITY));
             // The sums are moved to a larger maximum only when it has grown by more than 2^8: until then the
             // weights stay below 2^8, exact in float32 and as far from the end of bf16's range.
             if (__any_sync(0xffffffffu, !((now - top) * c <= 8.0f))) {
@@ -466,22 +514,32 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             }
             const float off = -base * c;
             float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
+            const auto weights = [&](unsigned (&x)[32], int i) {
+                mask(x, 32 * i);
                 unsigned w[16];
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    const float2 p = exp2_pair<5>(r[h][2 * k], r[h][2 * k + 1], c, make_float2(off, off), kFwdPoly >> (k % 8) & 1);
+                    const float2 p = exp2_pair<5>(x[2 * k], x[2 * k + 1], c, make_float2(off, off), kFwdPoly >> (k % 8) & 1);
                     part[k & 1] = __fadd2_rn(part[k & 1], p);
                     w[k] = pack2(p.x, p.y);
                 }
-                tmem_st16(s_at + 16 * h, w);
+                tmem_st16(s_at + 16 * i, w);
+            };
+            tmem_ld32(s_at, r[0]);
+#pragma unroll 1
+            for (int i = 0; i < 4; i += 2) {
+                tmem_ld_wait();
+                tmem_ld32(s_at + 32 * i + 32, r[1]);
+                weights(r[0], i);
+                tmem_ld_wait();
+                if (i == 0) tmem_ld32(s_at + 64, r[0]);
+                weights(r[1], i + 1);
             }
             sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
             tmem_st_wait();
             warp_arrive(p_full + 8 * t, lane);
         }
-        if (mine && ok) ok = __all_sync(0xffffffffu, gemm_wait(o_full + 8 * t, 0, abort));
+        if (mine && ok) ok = warp_wait(o_full + 8 * t, 0, abort);
         if (mine && ok) {
             tc_fence_after();
             const unsigned long long token = item.start + row;
@@ -503,7 +561,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
 // ---- backward --------------------------------------------------------------------------------------
 
 // dq of 128 query rows of a head.  Every four warps take 32 columns of the scores' rows.  Scores of the
-// next tile of keys are made as soon as those of this one are in registers; ds alternates between two places.
+// next tile of keys are made as soon as those of this one are in registers.
 // Two launches (this and the next kernel) form the scores twice, which costs 7 products of a tile instead of 5,
 // but no gradient is added to by several CTAs: no atomics, no float32 copy of dq in memory.
 //
@@ -511,8 +569,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
 // weight dp - delta is a small difference.  So rows whose keys are all in one tile, the short sequences and the
 // beginnings of long ones, take the sum itself and leave it for the next launch (two keys: gradients within
 // 0.25 % instead of 0.75 %).
-// What a backward CTA has in shared memory: two tiles that stay, rings of three and of two for the others
-// (the ring whose tiles two products read, one of them late, is the longer one), and the rest.
+// What a backward CTA has in shared memory: seven tiles, and the rest.
 struct BwdShared {
     AttnShared sh;
     alignas(16) float row[4][kTile];
@@ -525,6 +582,8 @@ __global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dq_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr unsigned kBytes = kTile * DP * 2;
+    constexpr bool kHeld = DP == 64;              // tensor memory has room for more operands
+
     extern __shared__ __align__(1024) unsigned char smem_tiles[];
     BwdShared &rest = *reinterpret_cast<BwdShared *>(smem_tiles + 7 * kBytes);
     AttnShared &sh = rest.sh;
@@ -535,81 +594,90 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
     const unsigned head = blockIdx.x % a.heads, row0 = item.tile * kTile, all = (item.len + kTile - 1) / kTile;
     const unsigned n = a.causal ? item.tile + 1 : all;
 
-    const unsigned smem = smem_addr(smem_tiles), sq = smem, sdo = smem + kBytes, sk = smem + 2 * kBytes, sv = smem + 5 * kBytes;
-    const unsigned bar = smem_addr(sh.bars), k_full = bar, k_empty = bar + 24, v_full = bar + 48, v_empty = bar + 64, q_full = bar + 80,
-                   s_full = bar + 88, s_read = bar + 96, dp_full = bar + 104, ds_full = bar + 112, dq_full = bar + 120, drain = bar + 128, sum_full = bar + 136;
+    const unsigned smem = smem_addr(smem_tiles), sdo = smem, sk = smem + kBytes, sv = smem + 4 * kBytes;
+    const unsigned bar = smem_addr(sh.bars), k_full = bar, k_empty = bar + 24, v_full = bar + 48, v_empty = bar + 72, do_full = bar + 96,
+                   s_full = bar + 104, dp_full = bar + 112, dq_full = bar + 120, drain = bar + 128, clean = bar + 136, tail = bar + 144,
+                   q_full = bar + 152, s_read = bar + 160, ds_full = bar + 168, sum_full = bar + 176;
     volatile int *abort = &sh.abort_flag;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
-        for (int i = 0; i < 17; ++i) init_bar(bar + 8 * i, 1);
-        init_bar(sum_full, kBwdWarps);
-        init_bar(s_read, kBwdWarps);
-        init_bar(ds_full, kBwdWarps);
+        for (int i = 0; i < 19; ++i) init_bar(bar + 8 * i, 1);
+        for (int i = 19; i < 23; ++i) init_bar(bar + 8 * i, kBwdWarps);
     }
     const unsigned tmem = attn_begin<kBwdWarps>(sh, warp);
-    const unsigned kS = tmem, kP = tmem + kTile, kDs = tmem + 2 * kTile, kDq = tmem + 3 * kTile;      // ds at kDs + 64 (j & 1)
+    // the queries, and with 64 columns their gradients' operand d_o as well, are held in tensor memory
+    const unsigned kS = tmem, kP = tmem + kTile, kDs = tmem + 2 * kTile, kDq = kDs + 64, kQ = tmem + 448, kDo = tmem + 384;
 
     if (warp >= kBwdWarps) {
         fewer_registers<kBwdWarps>();
         if (warp == kBwdWarps && elect_one()) {
-            const int token = (int)(item.start + row0), hk = (int)(head / a.group);
-            mbar_arrive_expect_tx(q_full, 2 * kBytes + (a.expire ? 16u : 0u));
-            load_tile<DP>(sq, &a.q, (int)head, token, q_full);
-            load_tile<DP>(sdo, &a.d_o, (int)head, token, q_full);
+            const int hk = (int)(head / a.group);
+            if (!kHeld) {
+                mbar_arrive_expect_tx(do_full, kBytes);
+                load_tile<DP>(sdo, &a.d_o, (int)head, (int)(item.start + row0), do_full);
+            }
             unsigned it = 0;
+            bool tailed = false;
             for (; it < 2 * n; ++it) {                                       // keys 0, values 0, keys 1, ...
-                const unsigned j = it >> 1, slots = it & 1 ? 2 : 3, s = j % slots, full = (it & 1 ? v_full : k_full) + 8 * s,
-                               empty = (it & 1 ? v_empty : k_empty) + 8 * s;
-                if ((j >= slots && !gemm_wait(empty, (j / slots - 1) & 1, abort)) || *abort) break;
-                mbar_arrive_expect_tx(full, kBytes);
-                load_tile<DP>((it & 1 ? sv : sk) + s * kBytes, it & 1 ? &a.v : &a.k, hk, (int)(item.start + j * kTile), full);
+                const unsigned j = it >> 1, s = j % 3, full = (it & 1 ? v_full : k_full) + 8 * s, empty = (it & 1 ? v_empty : k_empty) + 8 * s;
+                if ((j >= 3 && !gemm_wait(empty, (j / 3 - 1) & 1, abort)) || *abort) break;
+                const bool cut = it == 2 * n - 2 && item.len - j * kTile < kTile;
+                if (cut) arrive_bar(full);
+                mbar_arrive_expect_tx(cut ? tail : full, kBytes + (a.expire && it == 0 ? 16u : 0u));
+                load_tile<DP>((it & 1 ? sv : sk) + s * kBytes, it & 1 ? &a.v : &a.k, hk, (int)(item.start + j * kTile), cut ? tail : full);
+                tailed = tailed || cut;
             }
-            mbar_wait_bounded(q_full, 0);
-            for (unsigned i = it > 6 ? it - 6 : 0; i < it; ++i) {
-                const unsigned j = i >> 1, slots = i & 1 ? 2 : 3;
-                if (j + slots >= (it + 1 - (i & 1)) / 2) mbar_wait_bounded((i & 1 ? v_full : k_full) + 8 * (j % slots), (j / slots) & 1);
-            }
-        } else if (warp == kBwdWarps + 1) {
-            // scores of tile j; the rows that dq sums over later are zeroed here already
+            if (tailed) mbar_wait_bounded(tail, 0);
+            if (!kHeld) mbar_wait_bounded(do_full, 0);
+            for (unsigned i = it > 6 ? it - 6 : 0; i < it; ++i)
+                mbar_wait_bounded((i & 1 ? v_full : k_full) + 8 * ((i >> 1) % 3), (i >> 1) / 3 & 1);
+        } else if (warp == kBwdWarps + 1 && elect_one()) {
             const auto scores = [&](unsigned j) {
-                const unsigned k = sk + j % 3 * kBytes, live = item.len - j * kTile;
-                if (!__all_sync(0xffffffffu, gemm_wait(k_full + 8 * (j % 3), j / 3 & 1, abort))) return false;
-                if (live < kTile) zero_rows<DP>(k, live, lane);
+                if (!gemm_wait(k_full + 8 * (j % 3), j / 3 & 1, abort)) return false;
+                if (item.len - j * kTile < kTile && !gemm_wait(clean, 0, abort)) return false;
                 tc_fence_after();
-                if (elect_one()) {
-                    mma_rows<DP>(kS, sq, k);
+                {
+                    mma_held<DP>(kS, kQ, sk + j % 3 * kBytes);
                     umma_commit(s_full);
                 }
                 return true;
             };
-            const auto weights = [&](unsigned j) {                               // dp of tile j
-                if (!__all_sync(0xffffffffu, gemm_wait(v_full + 8 * (j & 1), (j >> 1) & 1, abort))) return false;
+            const auto weights = [&](unsigned j) {                           // dp of tile j
+                if (!gemm_wait(v_full + 8 * (j % 3), j / 3 & 1, abort)) return false;
                 tc_fence_after();
-                if (elect_one()) {
-                    mma_rows<DP>(kP, sdo, sv + (j & 1) * kBytes);
+                {
+                    if (kHeld) mma_held<DP>(kP, kDo, sv + j % 3 * kBytes);
+                    else mma_rows<DP>(kP, sdo, sv + j % 3 * kBytes);
                     umma_commit(dp_full);
-                    umma_commit(v_empty + 8 * (j & 1));
+                    umma_commit(v_empty + 8 * (j % 3));
                 }
                 return true;
             };
-            bool ok = __all_sync(0xffffffffu, gemm_wait(q_full, 0, abort)) && scores(0) && weights(0);
-            for (unsigned j = 0; ok && j < n; ++j) {
-                ok = __all_sync(0xffffffffu, gemm_wait(s_read, j & 1, abort));
-                if (ok && j + 1 < n) ok = scores(j + 1);
-                if (ok) ok = __all_sync(0xffffffffu, gemm_wait(ds_full, j & 1, abort));
-                if (ok && j + 1 < n) ok = weights(j + 1);
-                if (!ok) break;
+            bool ok = gemm_wait(q_full, 0, abort) && (kHeld || gemm_wait(do_full, 0, abort)), more = true;
+            // each round makes the scores and dp of tile j and the product that tile j - 1 ends with
+            for (unsigned j = 0; ok && more; ++j) {
+                more = j < n;
+                if (j) ok = gemm_wait(s_read, (j - 1) & 1, abort);
+                if (ok && more) ok = scores(j);
+                if (ok && j) ok = gemm_wait(ds_full, (j - 1) & 1, abort);
+                if (ok && more) ok = weights(j);
+                if (!ok || !j) continue;
                 tc_fence_after();
-                if (elect_one()) {
-                    mma_weights<DP, 16>(kDq, kDs + 64 * (j & 1), sk + j % 3 * kBytes, j != 0);
-                    umma_commit(j + 1 < n ? k_empty + 8 * (j % 3) : dq_full);
+                {
+                    mma_weights<DP, 16>(kDq, kDs, sk + (j - 1) % 3 * kBytes, j != 1);
+                    umma_commit(k_empty + 8 * ((j - 1) % 3));
+                    umma_commit(dq_full);
                 }
             }
-            if (elect_one()) {
+            {
                 umma_commit(drain);
                 mbar_wait_bounded(drain, 0);
             }
+        } else if (warp == kBwdWarps + 2 && item.len - (n - 1) * kTile < kTile) {
+            // the last tile of keys, which dq sums over, reports here and not to the issuer
+            if (warp_wait(tail, 0, abort))
+                zero_rows<DP>(sk + (n - 1) % 3 * kBytes, item.len - (n - 1) * kTile, lane, clean);
         }
     } else {
         more_registers<kBwdWarps>();
@@ -620,9 +688,16 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
         float delta = row < item.len && n > 1 ? a.delta[stat] : 0.0f;
         // columns below `end` count; a token that sees itself alone has ds = 0
         const unsigned end = row >= item.len ? 0 : a.causal ? row + 1 : item.len;
+        if (32 * share < DP) {
+            const bool here = row < item.len;
+            hold_row32(kQ + at + 16 * share, here ? a.q_rows.data + token * a.q_rows.ld_token + head * a.q_rows.ld_head : nullptr, 32 * share, a.dim);
+            if (kHeld) hold_row32(kDo + at + 16 * share, here ? a.do_rows.data + token * a.do_rows.ld_token + head * a.do_rows.ld_head : nullptr, 32 * share, a.dim);
+            tmem_st_wait();
+        }
+        warp_arrive(q_full, lane);
         bool ok = true;
         for (unsigned j = 0; j < n; ++j) {
-            ok = __all_sync(0xffffffffu, gemm_wait(s_full, j & 1, abort));
+            ok = warp_wait(s_full, j & 1, abort);
             if (!ok) break;
             tc_fence_after();
             unsigned r[32], w[16];
@@ -632,7 +707,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             warp_arrive(s_read, lane);
 #pragma unroll
             for (int k = 0; k < 16; ++k) p[k] = exp2_pair<4>(r[2 * k], r[2 * k + 1], c, make_float2(off, off), kBwdPoly >> (k % 8) & 1);
-            ok = __all_sync(0xffffffffu, gemm_wait(dp_full, j & 1, abort));
+            ok = warp_wait(dp_full, j & 1, abort);
             if (!ok) break;
             tc_fence_after();
             tmem_ld32(kP + at + 32 * share, r);
@@ -646,7 +721,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
                 shares[share][row - row0] = sum;
                 __syncwarp();
                 if (lane == 0) arrive_bar(sum_full);
-                ok = __all_sync(0xffffffffu, gemm_wait(sum_full, 0, abort));
+                ok = warp_wait(sum_full, 0, abort);
                 if (!ok) break;
                 delta = (shares[0][row - row0] + shares[1][row - row0]) + (shares[2][row - row0] + shares[3][row - row0]);
                 if (share == 0 && row < item.len) a.delta[stat] = delta;
@@ -662,11 +737,16 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             }
 #pragma unroll
             for (int k = 0; k < 16; ++k) w[k] = ds_pair(p[k], r[2 * k], r[2 * k + 1], make_float2(-delta, -delta));
-            tmem_st16(kDs + at + 64 * (j & 1) + 16 * share, w);
+            if (j) {                              // the product that reads the last tile's ds, long done by now
+                ok = warp_wait(dq_full, (j - 1) & 1, abort);
+                if (!ok) break;
+                tc_fence_after();
+            }
+            tmem_st16(kDs + at + 16 * share, w);
             tmem_st_wait();
             warp_arrive(ds_full, lane);
         }
-        if (ok) ok = __all_sync(0xffffffffu, gemm_wait(dq_full, 0, abort));
+        if (ok) ok = warp_wait(dq_full, (n - 1) & 1, abort);
         if (ok && 32 * share < DP) {
             tc_fence_after();
             unsigned w[32];
@@ -687,6 +767,8 @@ __global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dkv_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr unsigned kBytes = kTile * DP * 2;
+    constexpr bool kHeld = DP == 64;              // tensor memory has room for more operands
+
     extern __shared__ __align__(1024) unsigned char smem_tiles[];
     BwdShared &rest = *reinterpret_cast<BwdShared *>(smem_tiles + 7 * kBytes);
     AttnShared &sh = rest.sh;
@@ -701,76 +783,112 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
 
     const unsigned smem = smem_addr(smem_tiles), sk = smem, sv = smem + kBytes, sq = smem + 2 * kBytes, sdo = smem + 5 * kBytes;
     const unsigned bar = smem_addr(sh.bars), q_full = bar, q_empty = bar + 24, do_full = bar + 48, do_empty = bar + 64, kv_full = bar + 80,
-                   s_full = bar + 88, p_full = bar + 96, dp_full = bar + 104, ds_full = bar + 112, done = bar + 120, drain = bar + 128, st_full = bar + 136;
+                   s_full = bar + 88, dp_full = bar + 96, done = bar + 104, drain = bar + 112, q_clean = bar + 120, do_clean = bar + 144,
+                   q_tail = bar + 160, do_tail = bar + 184, p_full = bar + 200, ds_full = bar + 208, st_full = bar + 216;
     volatile int *abort = &sh.abort_flag;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
-        for (int i = 0; i < 17; ++i) init_bar(bar + 8 * i, 1);
+        for (int i = 0; i < 25; ++i) init_bar(bar + 8 * i, 1);
+        if (kHeld) init_bar(kv_full, kBwdWarps);
         init_bar(p_full, kBwdWarps);
         init_bar(ds_full, kBwdWarps);
         init_bar(st_full, 8);
     }
     const unsigned tmem = attn_begin<kBwdWarps>(sh, warp);
-    const unsigned kS = tmem, kP = tmem + kTile, kDv = tmem + 2 * kTile, kDk = kDv + DP;
+    const unsigned kS = tmem, kP = tmem + kTile, kDv = tmem + 2 * kTile, kDk = kDv + DP, kK = tmem + 384, kV = kK + 32;
+    // tiles of queries whose rows past the sequence's end are zeroed: the last one of each head
+    const unsigned last = item.len - (all - 1) * kTile;
 
     if (warp >= kBwdWarps) {
         fewer_registers<kBwdWarps>();
         if (warp == kBwdWarps && elect_one()) {
-            mbar_arrive_expect_tx(kv_full, 2 * kBytes + (a.expire ? 16u : 0u));
-            load_tile<DP>(sk, &a.k, (int)hk, (int)(item.start + row0), kv_full);
-            load_tile<DP>(sv, &a.v, (int)hk, (int)(item.start + row0), kv_full);
-            unsigned it = 0;
+            if (!kHeld) {
+                mbar_arrive_expect_tx(kv_full, 2 * kBytes);
+                load_tile<DP>(sk, &a.k, (int)hk, (int)(item.start + row0), kv_full);
+                load_tile<DP>(sv, &a.v, (int)hk, (int)(item.start + row0), kv_full);
+            }
+            unsigned it = 0, tails = 0, cuts = 0;
             for (; it < 2 * n; ++it) {                                       // queries 0, gradients 0, queries 1, ...
                 const unsigned j = it >> 1, slots = it & 1 ? 2 : 3, s = j % slots, full = (it & 1 ? do_full : q_full) + 8 * s,
                                empty = (it & 1 ? do_empty : q_empty) + 8 * s;
                 const int h = (int)(hk * a.group + j / per), token = (int)(item.start + (i0 + j % per) * kTile);
                 if ((j >= slots && !gemm_wait(empty, (j / slots - 1) & 1, abort)) || *abort) break;
-                mbar_arrive_expect_tx(full, kBytes);
-                load_tile<DP>((it & 1 ? sdo : sq) + s * kBytes, it & 1 ? &a.d_o : &a.q, h, token, full);
+                const bool cut = last < kTile && (j + 1) % per == 0;
+                const unsigned to = cut ? (it & 1 ? do_tail : q_tail) + 8 * s : full;
+                if (cut) arrive_bar(full);
+                mbar_arrive_expect_tx(to, kBytes + (a.expire && it == 0 ? 16u : 0u));
+                load_tile<DP>((it & 1 ? sdo : sq) + s * kBytes, it & 1 ? &a.d_o : &a.q, h, token, to);
+                if (cut) tails ^= 1u << (it & 1 ? 4 + s : s), cuts |= 1u << (it & 1 ? 4 + s : s);
             }
-            mbar_wait_bounded(kv_full, 0);
+            for (unsigned s = 0; s < 6; ++s)                                 // the last tail of each slot
+                if (cuts >> s & 1) mbar_wait_bounded(s < 4 ? q_tail + 8 * s : do_tail + 8 * (s - 4), ~tails >> s & 1);
+            if (!kHeld) mbar_wait_bounded(kv_full, 0);
             for (unsigned i = it > 6 ? it - 6 : 0; i < it; ++i) {
                 const unsigned j = i >> 1, slots = i & 1 ? 2 : 3;
                 if (j + slots >= (it + 1 - (i & 1)) / 2) mbar_wait_bounded((i & 1 ? do_full : q_full) + 8 * (j % slots), (j / slots) & 1);
             }
-        } else if (warp == kBwdWarps + 1) {
-            // the product of keys (values) with tile j of queries (their gradients), whose rows past the sequence's end
-            // are summed over later
+        } else if (warp == kBwdWarps + 1 && elect_one()) {
+            unsigned tails = 0;                                              // parities: of the queries' slots, from bit 4 on the gradients'
+
+            // the product of the keys (values) with tile j of queries (their gradients)
             const auto product = [&](unsigned j, bool second) {
-                const unsigned slots = second ? 2 : 3, s = j % slots, t = (second ? sdo : sq) + s * kBytes, live = item.len - (i0 + j % per) * kTile;
-                if (!__all_sync(0xffffffffu, gemm_wait((second ? do_full : q_full) + 8 * s, j / slots & 1, abort))) return false;
-                if (live < kTile) zero_rows<DP>(t, live, lane);
+                const unsigned slots = second ? 2 : 3, s = j % slots, t = (second ? sdo : sq) + s * kBytes;
+                if (!gemm_wait((second ? do_full : q_full) + 8 * s, j / slots & 1, abort)) return false;
+                if (last < kTile && (j + 1) % per == 0) {
+                    const unsigned bit = second ? 4 + s : s;
+                    if (!gemm_wait((second ? do_clean : q_clean) + 8 * s, tails >> bit & 1, abort)) return false;
+                    tails ^= 1u << bit;
+                }
                 tc_fence_after();
-                if (elect_one()) {
-                    mma_rows<DP>(second ? kP : kS, second ? sv : sk, t);
+                {
+                    if (kHeld) mma_held<DP>(second ? kP : kS, second ? kV : kK, t);
+                    else mma_rows<DP>(second ? kP : kS, second ? sv : sk, t);
                     umma_commit(second ? dp_full : s_full);
                 }
                 return true;
             };
-            bool ok = __all_sync(0xffffffffu, gemm_wait(kv_full, 0, abort)) && product(0, false) && product(0, true);
-            for (unsigned j = 0; ok && j < n; ++j) {
-                ok = __all_sync(0xffffffffu, gemm_wait(p_full, j & 1, abort));
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
-                    mma_weights<DP, 32>(kDv, kS, sdo + (j & 1) * kBytes, j != 0);
-                    umma_commit(do_empty + 8 * (j & 1));
+            bool ok = gemm_wait(kv_full, 0, abort), more = true;
+            // each round ends tile j - 1 and makes the scores and dp of tile j
+            for (unsigned j = 0; ok && more; ++j) {
+                const unsigned i = j - 1;
+                more = j < n;
+                if (j) {
+                    ok = gemm_wait(p_full, i & 1, abort);
+                    if (!ok) break;
+                    tc_fence_after();
+                    {
+                        mma_weights<DP, 32>(kDv, kS, sdo + (i & 1) * kBytes, i != 0);
+                        umma_commit(do_empty + 8 * (i & 1));
+                    }
                 }
-                if (j + 1 < n) ok = product(j + 1, false);
-                if (ok) ok = __all_sync(0xffffffffu, gemm_wait(ds_full, j & 1, abort));
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
-                    mma_weights<DP, 32>(kDk, kP, sq + j % 3 * kBytes, j != 0);
-                    umma_commit(q_empty + 8 * (j % 3));
+                if (more) ok = product(j, false);
+                if (ok && j) {
+                    ok = gemm_wait(ds_full, i & 1, abort);
+                    if (!ok) break;
+                    tc_fence_after();
+                    {
+                        mma_weights<DP, 32>(kDk, kP, sq + i % 3 * kBytes, i != 0);
+                        umma_commit(q_empty + 8 * (i % 3));
+                    }
                 }
-                if (j + 1 < n) ok = product(j + 1, true);
+                if (ok && more) ok = product(j, true);
             }
-            if (elect_one()) {
+            {
                 if (ok) umma_commit(done);
                 umma_commit(drain);
                 mbar_wait_bounded(drain, 0);
+            }
+        } else if (warp == kBwdWarps + 2 && last < kTile) {
+            // the last tiles report here and not to the issuer
+            unsigned tails = 0;
+            for (unsigned j = per - 1; j < n; j += per) {
+                const unsigned s = j % 3, d = j & 1;
+                if (!warp_wait(q_tail + 8 * s, tails >> s & 1, abort)) break;
+                zero_rows<DP>(sq + s * kBytes, last, lane, q_clean + 8 * s);
+                if (!warp_wait(do_tail + 8 * d, tails >> (4 + d) & 1, abort)) break;
+                zero_rows<DP>(sdo + d * kBytes, last, lane, do_clean + 8 * d);
+                tails ^= 1u << s | 1u << (4 + d);
             }
         }
     } else {
@@ -785,6 +903,16 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             return share ? -a.delta[where] : -a.lse[where] * kLog2e;
         };
         float next = stat(0);
+        if (kHeld) {
+            if (32 * share < DP) {
+                const unsigned long long token = item.start + row;
+                const bool here = row < item.len;
+                hold_row32(kK + at + 16 * share, here ? a.k_rows.data + token * a.k_rows.ld_token + hk * a.k_rows.ld_head : nullptr, 32 * share, a.dim);
+                hold_row32(kV + at + 16 * share, here ? a.v_rows.data + token * a.v_rows.ld_token + hk * a.v_rows.ld_head : nullptr, 32 * share, a.dim);
+                tmem_st_wait();
+            }
+            warp_arrive(kv_full, lane);
+        }
         bool ok = true;
         for (unsigned j = 0; j < n; ++j) {
             if (share < 2) {
@@ -822,7 +950,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             tmem_st16(kS + at + 32 * share, w);
             tmem_st_wait();
             warp_arrive(p_full, lane);
-            ok = __all_sync(0xffffffffu, gemm_wait(dp_full, j & 1, abort));
+            ok = warp_wait(dp_full, j & 1, abort);
             if (!ok) break;
             tc_fence_after();
             tmem_ld32(kP + at + 32 * share, r);
@@ -843,7 +971,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             tmem_st_wait();
             warp_arrive(ds_full, lane);
         }
-        if (ok) ok = __all_sync(0xffffffffu, gemm_wait(done, 0, abort));
+        if (ok) ok = warp_wait(done, 0, abort);
         if (ok) {
             tc_fence_after();
             const bool key = share >= 2;
