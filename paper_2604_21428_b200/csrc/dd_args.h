@@ -126,22 +126,31 @@ inline int ensure_decoder_scratch(dd_ctx *ctx, size_t bytes)
     return DD_OK;
 }
 
-// A launch that may begin while the one before it on the stream ends; the kernel waits for it itself.
+// Launches that may begin while the one before them on the stream ends; the kernels wait for it themselves.
 template <typename K, typename... A>
-inline int launch_after(dd_ctx *ctx, K kernel, unsigned long long grid, unsigned threads, size_t smem, cudaStream_t stream, const A &...args)
+inline int launch_clusters(dd_ctx *ctx, K kernel, unsigned long long grid, unsigned threads, size_t smem, unsigned cluster, cudaStream_t stream,
+                           const A &...args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim = {cluster, 1, 1};
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, args...));
     return DD_OK;
+}
+
+template <typename K, typename... A>
+inline int launch_after(dd_ctx *ctx, K kernel, unsigned long long grid, unsigned threads, size_t smem, cudaStream_t stream, const A &...args)
+{
+    return launch_clusters(ctx, kernel, grid, threads, smem, 1, stream, args...);
 }
 
 }  // namespace ddm

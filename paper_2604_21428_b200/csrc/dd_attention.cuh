@@ -49,6 +49,7 @@ struct AttnArgs {
     unsigned heads, group, dim;                   // query heads, query heads per head of keys
     float scale;
     int causal, expire;
+    unsigned cluster;                             // CTAs that share a tile of keys in the last kernel
     HeadsOut o, dq, dk, dv;
     HeadsOut q_rows, k_rows, v_rows, do_rows;     // inputs once more, for operands that are kept in tensor memory
     float *lse;                                   // [heads][tokens]
@@ -85,6 +86,14 @@ __device__ __forceinline__ void tmem_st16(unsigned addr, const unsigned (&r)[16]
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld16(unsigned addr, unsigned (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+}
+
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void init_bar(unsigned bar, unsigned count)
@@ -98,7 +107,8 @@ __device__ __forceinline__ void arrive_bar(unsigned bar)
 }
 
 // Descriptors of operand tiles: the upper half is the same for all (128-byte swizzle, groups of 8 rows every
-// 1024 bytes), the lower half is the address and, where rows are K, the step to the next 64 columns.  They are
+// 1024 bytes), the lower half is the address and, where rows are K, the step to the next 64 columns (in a cluster an address has the
+// CTA's rank in its upper bits, which do not belong there).  They are
 // kept as halves, and everything they are made of is warp-uniform, because the products are fed from uniform
 // registers: with 64-bit descriptors put together for each product from per-lane values, issuing one took 115 cycles
 // and not the 64 that it runs for.
@@ -107,13 +117,13 @@ constexpr unsigned kDescUpper = (1024 / 16) | (1u << 14) | (2u << 29);
 // K contiguous: step k covers elements 16 k .. of every row.
 __device__ __forceinline__ unsigned desc_rows(unsigned tile, int k)
 {
-    return ((tile >> 4) | (1u << 16)) + (k >> 2) * (kBoxTile / 16) + (k & 3) * 2;
+    return ((tile >> 4 & 0x3fff) | (1u << 16)) + (k >> 2) * (kBoxTile / 16) + (k & 3) * 2;
 }
 
 // Rows are K (the tile's columns are N): step k covers rows 16 k .., the next 64 columns are one box on.
 __device__ __forceinline__ unsigned desc_cols(unsigned tile, int k)
 {
-    return ((tile >> 4) | ((unsigned)(kBoxTile / 16) << 16)) + k * 128;
+    return ((tile >> 4 & 0x3fff) | ((unsigned)(kBoxTile / 16) << 16)) + k * 128;
 }
 
 // float32 accumulators, bf16 operands, M = 128; b_mn: B's rows are K.
@@ -185,6 +195,18 @@ __device__ __forceinline__ void zero_rows(unsigned tile, unsigned first, int lan
     if (lane == 0) arrive_bar(bar);
 }
 
+// Four floats at `addr` (a shared-memory address of this CTA) in the CTA of rank `rank`.
+__device__ __forceinline__ float4 ld_cluster4(unsigned addr, unsigned rank)
+{
+    float4 x;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(cluster_addr(addr, rank)) : "memory");
+    return x;
+}
+
+// Where four columns of a row of 2 DP float32 sums are kept: eight rows' pieces of one column lie in different banks.
+template <int DP>
+__device__ __forceinline__ unsigned sums_piece(unsigned base, unsigned row, unsigned piece) { return base + row * (2 * DP * 4) + ((piece ^ (row & 7)) << 4); }
+
 // Columns col .. col + 31 of a row (null: zeros) to 16 columns of tensor memory, as operand A; dim is a multiple of 8.
 __device__ __forceinline__ void hold_row32(unsigned at, const __nv_bfloat16 *row, unsigned col, unsigned dim)
 {
@@ -215,34 +237,26 @@ __device__ __forceinline__ void store_row32(__nv_bfloat16 *row, unsigned col, un
 
 // 2^x of two numbers on the multiply-add pipe: x = n + f with n the nearest integer (the sum with 1.5 2^23 rounds to it
 // and holds it in its low bits), 2^f by a polynomial on [-1/2, 1/2], n into the exponent.  The coefficients are
-// a minimax fit of the relative error with 2^0 = 1 held (a weighted least-squares iteration): 2.9e-6 with degree 4,
-// 1.9e-7 with degree 5 in float32, sums included.  Below -127 the result is 0, near -126.5 it is off by less than 2^-126.
-template <int DEGREE>
+// a minimax fit of the relative error with 2^0 = 1 held (a weighted least-squares iteration): 2.9e-6 in float32, far
+// below the bf16 rounding that follows.  Below -127 the result is 0, near -126.5 it is off by less than 2^-126.
 __device__ __forceinline__ float2 exp2_poly(float2 x)
 {
-    static_assert(DEGREE == 4 || DEGREE == 5, "a fit for each degree");
-    constexpr float c4[] = {0.6931241750717163f, 0.24024099111557007f, 0.055906426161527634f, 0.009582852944731712f},
-                    c5[] = {0.6931470036506653f, 0.24022242426872253f, 0.05550733581185341f, 0.009671512991189957f, 0.001326472731307149f};
-    constexpr float kRound = 12582912.0f;
-    x.x = fmaxf(x.x, -127.0f);
-    x.y = fmaxf(x.y, -127.0f);
+    constexpr float c[] = {1.0f, 0.6931241750717163f, 0.24024099111557007f, 0.055906426161527634f, 0.009582852944731712f}, kRound = 12582912.0f;
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-127.0f));               // a NaN goes on, and ends as an infinity
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-127.0f));
     const float2 t = __fadd2_rn(x, make_float2(kRound, kRound)), n = __fadd2_rn(t, make_float2(-kRound, -kRound)),
                  f = __ffma2_rn(n, make_float2(-1.0f, -1.0f), x);
-    const auto both = [](float c) { return make_float2(c, c); };
-    float2 p = both(DEGREE == 4 ? c4[3] : c5[4]);
+    float2 p = make_float2(c[4], c[4]);
 #pragma unroll
-    for (int i = DEGREE - 2; i >= 0; --i) p = __ffma2_rn(p, f, both(DEGREE == 4 ? c4[i < 4 ? i : 3] : c5[i]));
-    p = __ffma2_rn(p, f, both(1.0f));
+    for (int i = 3; i >= 0; --i) p = __ffma2_rn(p, f, make_float2(c[i], c[i]));
     return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 
-// 2^(x c + off) of two scores, by the special function unit (16 a clock and SM, which alone would hold the kernels up)
-// or, for some of the pairs, by the polynomial.
-template <int DEGREE>
-__device__ __forceinline__ float2 exp2_pair(unsigned x0, unsigned x1, float c, float2 off, bool poly)
+// 2^(x c + off) of two scores.
+__device__ __forceinline__ float2 exp2_pair(unsigned x0, unsigned x1, float c, float2 off, bool poly = false)
 {
     const float2 x = __ffma2_rn(make_float2(__uint_as_float(x0), __uint_as_float(x1)), make_float2(c, c), off);
-    return poly ? exp2_poly<DEGREE>(x) : make_float2(exp2_fast(x.x), exp2_fast(x.y));
+    return poly ? exp2_poly(x) : make_float2(exp2_fast(x.x), exp2_fast(x.y));
 }
 
 // Maximum of three; a NaN among them is the result.
@@ -329,13 +343,6 @@ __device__ __forceinline__ void warp_arrive(unsigned bar, int lane)
     __syncwarp();
     if (lane == 0) arrive_bar(bar);
 }
-
-// Of eight pairs, those whose exponentials are polynomials (a bit each).
-#ifndef DD_FWD_POLY
-#define DD_FWD_POLY 0x4a
-#define DD_BWD_POLY 0x55
-#endif
-constexpr unsigned kFwdPoly = DD_FWD_POLY, kBwdPoly = DD_BWD_POLY;
 
 // ---- forward ---------------------------------------------------------------------------------------
 
@@ -464,34 +471,26 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             ok = warp_wait(s_full + 8 * t, j & 1, abort);
             if (!ok) break;
             tc_fence_after();
+            unsigned r[4][32];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32 * i, r[i]);
+            tmem_ld_wait();
             const unsigned end = a.causal && row + 1 < item.len ? row + 1 : item.len, live = end > j * kTile ? end - j * kTile : 0;
-            const bool masked = __any_sync(0xffffffffu, live < kTile);
-            // Scores are read twice, 32 at a time, for their maximum and for the weights: kept in registers they
-            // and the code, unrolled over all of them, are too much (it falls out of the instruction cache each time
-            // round, and the warp that issues the products waits for it).
-            unsigned r[2][32];
-            const auto mask = [&](unsigned (&x)[32], unsigned first) {
-                if (!masked) return;
+            if (__any_sync(0xffffffffu, live < kTile)) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k)
-                    if (first + k >= live) x[k] = 0xff800000u;                // -infinity
-            };
-            float now = top;
-#pragma unroll 1
-            for (int i = 0; i < 4; i += 2) {
-                tmem_ld32(s_at + 32 * i, r[0]);
-                tmem_ld32(s_at + 32 * i + 32, r[1]);
-                tmem_ld_wait();
-                mask(r[0], 32 * i);
-                mask(r[1], 32 * i + 32);
-                float m[4] = {now, -INFINITY, -INFINITY, -INFINITY};
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int k = 0; k < 32; k += 2) {
-                    m[k / 2 & 1] = max3(m[k / 2 & 1], __uint_as_float(r[0][k]), __uint_as_float(r[0][k + 1]));
-                    m[2 + (k / 2 & 1)] = max3(m[2 + (k / 2 & 1)], __uint_as_float(r[1][k]), __uint_as_float(r[1][k + 1]));
-                }
-                now = max3(max3(m[0], m[1], m[2]), m[3], -INFINITY);
+                    for (int k = 0; k < 32; ++k)
+                        if (32 * i + k >= live) r[i][k] = 0xff800000u;        // -infinity
             }
+            float m[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                m[i] = max3(__uint_as_float(r[i][0]), __uint_as_float(r[i][1]), i ? -INFINITY : top);
+#pragma unroll
+                for (int k = 2; k < 32; k += 2) m[i] = max3(m[i], __uint_as_float(r[i][k]), __uint_as_float(r[i][k + 1]));
+            }
+            const float now = max3(m[0], m[1], max3(m[2], m[3], -INFINITY));
             // The sums are moved to a larger maximum only when it has grown by more than 2^8: until then the
             // weights stay below 2^8, exact in float32 and as far from the end of bf16's range.
             if (__any_sync(0xffffffffu, !((now - top) * c <= 8.0f))) {
@@ -499,14 +498,14 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                 if (j) {
                     const float by = exp2_fast((base - next) * c);
                     sum *= by;
-#pragma unroll
-                    for (int i = 0; i < DP / 32; ++i) {
-                        unsigned o[32];
-                        tmem_ld32(o_at + 32 * i, o);
+#pragma unroll 1
+                    for (int i = 0; i < DP / 16; ++i) {
+                        unsigned o[16];
+                        tmem_ld16(o_at + 16 * i, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
-                        tmem_st32(o_at + 32 * i, o);
+                        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
+                        tmem_st16(o_at + 16 * i, o);
                     }
                 }
                 top = now;
@@ -514,26 +513,16 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             }
             const float off = -base * c;
             float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-            const auto weights = [&](unsigned (&x)[32], int i) {
-                mask(x, 32 * i);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
                 unsigned w[16];
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    const float2 p = exp2_pair<5>(x[2 * k], x[2 * k + 1], c, make_float2(off, off), kFwdPoly >> (k % 8) & 1);
+                    const float2 p = exp2_pair(r[h][2 * k], r[h][2 * k + 1], c, make_float2(off, off));
                     part[k & 1] = __fadd2_rn(part[k & 1], p);
                     w[k] = pack2(p.x, p.y);
                 }
-                tmem_st16(s_at + 16 * i, w);
-            };
-            tmem_ld32(s_at, r[0]);
-#pragma unroll 1
-            for (int i = 0; i < 4; i += 2) {
-                tmem_ld_wait();
-                tmem_ld32(s_at + 32 * i + 32, r[1]);
-                weights(r[0], i);
-                tmem_ld_wait();
-                if (i == 0) tmem_ld32(s_at + 64, r[0]);
-                weights(r[1], i + 1);
+                tmem_st16(s_at + 16 * h, w);
             }
             sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
             tmem_st_wait();
@@ -569,6 +558,11 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
 // weight dp - delta is a small difference.  So rows whose keys are all in one tile, the short sequences and the
 // beginnings of long ones, take the sum itself and leave it for the next launch (two keys: gradients within
 // 0.25 % instead of 0.75 %).
+// The pairs whose weights are polynomials, three of eight: all weights of a tile are wanted at one time, and the
+// special function unit makes 16 a clock and SM (8192 tokens, 16 heads of 64: 636 -> 604 us, of 128 0.6 % less; in
+// the forward pass, whose two tiles take turns, the same costs 3-7 %).
+__host__ __device__ constexpr bool poly_pair(int k) { return 0x4a >> (k % 8) & 1; }
+
 // What a backward CTA has in shared memory: seven tiles, and the rest.
 struct BwdShared {
     AttnShared sh;
@@ -706,7 +700,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             tmem_ld_wait();
             warp_arrive(s_read, lane);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) p[k] = exp2_pair<4>(r[2 * k], r[2 * k + 1], c, make_float2(off, off), kBwdPoly >> (k % 8) & 1);
+            for (int k = 0; k < 16; ++k) p[k] = exp2_pair(r[2 * k], r[2 * k + 1], c, make_float2(off, off), poly_pair(k));
             ok = warp_wait(dp_full, j & 1, abort);
             if (!ok) break;
             tc_fence_after();
@@ -762,6 +756,10 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
 // Scores are made transposed (rows are keys), so that the weights are the A operand of both products as they lie.
 // Products and weights alternate on the same places: dv of a tile, then the next tile's scores, run while ds
 // is computed; dk and the next dp while the next weights are.
+//
+// The first keys of a long sequence are read by all its queries, in every query head of the group: where that is
+// much beside what an SM has to do, the CTAs of a cluster take equal parts of those tiles and add their sums up through
+// distributed shared memory, in rank order.
 template <int DP>
 __global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dkv_kernel(const __grid_constant__ AttnArgs a)
@@ -776,10 +774,16 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const unsigned kv_heads = a.heads / a.group;
     PlanItem item;
-    if (!plan_item(a, blockIdx.x / kv_heads, item)) return;
-    const unsigned hk = blockIdx.x % kv_heads, all = (item.len + kTile - 1) / kTile;
+    const unsigned rank = blockIdx.x % a.cluster, unit = blockIdx.x / a.cluster;
+    if (!plan_item(a, unit / kv_heads, item)) return;                        // (the cluster as a whole)
+    const unsigned hk = unit % kv_heads, all = (item.len + kTile - 1) / kTile;
     const unsigned tile = all - 1 - item.tile, row0 = tile * kTile;          // early keys are read by most queries
-    const unsigned i0 = a.causal ? tile : 0, per = all - i0, n = per * a.group;
+    // tiles of queries: `per` of each head that shares the keys, of which this CTA takes n from `start` on
+    const unsigned i0 = a.causal ? tile : 0, per = all - i0, total = per * a.group;
+    const unsigned start = (unsigned)((unsigned long long)total * rank / a.cluster), n = (unsigned)((unsigned long long)total * (rank + 1) / a.cluster) - start;
+    const auto head_of = [&](unsigned j) { return hk * a.group + (start + j) / per; };
+    const auto tile_of = [&](unsigned j) { return i0 + (start + j) % per; };
+    const auto is_last = [&](unsigned j) { return tile_of(j) == all - 1; };
 
     const unsigned smem = smem_addr(smem_tiles), sk = smem, sv = smem + kBytes, sq = smem + 2 * kBytes, sdo = smem + 5 * kBytes;
     const unsigned bar = smem_addr(sh.bars), q_full = bar, q_empty = bar + 24, do_full = bar + 48, do_empty = bar + 64, kv_full = bar + 80,
@@ -812,9 +816,9 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             for (; it < 2 * n; ++it) {                                       // queries 0, gradients 0, queries 1, ...
                 const unsigned j = it >> 1, slots = it & 1 ? 2 : 3, s = j % slots, full = (it & 1 ? do_full : q_full) + 8 * s,
                                empty = (it & 1 ? do_empty : q_empty) + 8 * s;
-                const int h = (int)(hk * a.group + j / per), token = (int)(item.start + (i0 + j % per) * kTile);
+                const int h = (int)head_of(j), token = (int)(item.start + tile_of(j) * kTile);
                 if ((j >= slots && !gemm_wait(empty, (j / slots - 1) & 1, abort)) || *abort) break;
-                const bool cut = last < kTile && (j + 1) % per == 0;
+                const bool cut = last < kTile && is_last(j);
                 const unsigned to = cut ? (it & 1 ? do_tail : q_tail) + 8 * s : full;
                 if (cut) arrive_bar(full);
                 mbar_arrive_expect_tx(to, kBytes + (a.expire && it == 0 ? 16u : 0u));
@@ -835,7 +839,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             const auto product = [&](unsigned j, bool second) {
                 const unsigned slots = second ? 2 : 3, s = j % slots, t = (second ? sdo : sq) + s * kBytes;
                 if (!gemm_wait((second ? do_full : q_full) + 8 * s, j / slots & 1, abort)) return false;
-                if (last < kTile && (j + 1) % per == 0) {
+                if (last < kTile && is_last(j)) {
                     const unsigned bit = second ? 4 + s : s;
                     if (!gemm_wait((second ? do_clean : q_clean) + 8 * s, tails >> bit & 1, abort)) return false;
                     tails ^= 1u << bit;
@@ -848,7 +852,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                 }
                 return true;
             };
-            bool ok = gemm_wait(kv_full, 0, abort), more = true;
+            bool ok = gemm_wait(kv_full, 0, abort), more = n > 0;
             // each round ends tile j - 1 and makes the scores and dp of tile j
             for (unsigned j = 0; ok && more; ++j) {
                 const unsigned i = j - 1;
@@ -882,7 +886,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
         } else if (warp == kBwdWarps + 2 && last < kTile) {
             // the last tiles report here and not to the issuer
             unsigned tails = 0;
-            for (unsigned j = per - 1; j < n; j += per) {
+            for (unsigned j = all - 1 - tile_of(0); j < n; j += per) {
                 const unsigned s = j % 3, d = j & 1;
                 if (!warp_wait(q_tail + 8 * s, tails >> s & 1, abort)) break;
                 zero_rows<DP>(sq + s * kBytes, last, lane, q_clean + 8 * s);
@@ -891,14 +895,19 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                 tails ^= 1u << s | 1u << (4 + d);
             }
         }
+        if (a.cluster > 1) {                      // as the other warps do
+            __syncwarp();
+            cluster_sync();
+            cluster_sync();
+        }
     } else {
         more_registers<kBwdWarps>();
         const unsigned share = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16, row = row0 + (warp & 3) * 32 + lane;
         const float c = a.scale * kLog2e;
         // the first 256 threads fetch the statistics: lse or delta of one query of tile j
         const auto stat = [&](unsigned j) {
-            const unsigned i = (i0 + j % per) * kTile + (threadIdx.x & 127), h = hk * a.group + j / per;
-            if (share >= 2 || i >= item.len) return 0.0f;
+            const unsigned i = tile_of(j) * kTile + (threadIdx.x & 127), h = head_of(j);
+            if (share >= 2 || j >= n || i >= item.len) return 0.0f;
             const unsigned long long where = (unsigned long long)h * a.tokens + item.start + i;
             return share ? -a.delta[where] : -a.lse[where] * kLog2e;
         };
@@ -921,7 +930,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                 if (lane == 0) arrive_bar(st_full);
                 if (j + 1 < n) next = stat(j + 1);
             }
-            const unsigned q0 = (i0 + j % per) * kTile + 32 * share;          // the first of this warp's 32 queries
+            const unsigned q0 = tile_of(j) * kTile + 32 * share;          // the first of this warp's 32 queries
             // queries from `from` to `to` count
             const unsigned to = item.len > q0 ? item.len - q0 : 0, from = a.causal && row > q0 ? row - q0 : 0;
             const bool masked = __any_sync(0xffffffffu, to < 32 || from > 0) || (a.causal && q0 == 0);
@@ -942,8 +951,8 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const float4 x = offs[k];
-                p[2 * k] = exp2_pair<4>(r[4 * k], r[4 * k + 1], c, make_float2(x.x, x.y), kBwdPoly >> (2 * k % 8) & 1);
-                p[2 * k + 1] = exp2_pair<4>(r[4 * k + 2], r[4 * k + 3], c, make_float2(x.z, x.w), kBwdPoly >> ((2 * k + 1) % 8) & 1);
+                p[2 * k] = exp2_pair(r[4 * k], r[4 * k + 1], c, make_float2(x.x, x.y), poly_pair(2 * k));
+                p[2 * k + 1] = exp2_pair(r[4 * k + 2], r[4 * k + 3], c, make_float2(x.z, x.w), poly_pair(2 * k + 1));
                 w[2 * k] = pack2(p[2 * k].x, p[2 * k].y);
                 w[2 * k + 1] = pack2(p[2 * k + 1].x, p[2 * k + 1].y);
             }
@@ -983,8 +992,44 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                 const unsigned col = (share & 1) * (DP / 2) + 32 * i;
                 tmem_ld32((key ? kDk : kDv) + at + col, w);
                 tmem_ld_wait();
-                if (row < item.len) store_row32(o, col, a.dim, w, key ? a.scale : 1.0f);
+                if (a.cluster > 1) {              // to where the operands were
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4) {
+                        if (!n) w[k] = w[k + 1] = w[k + 2] = w[k + 3] = 0u;
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(sums_piece<DP>(smem, row - row0, ((key ? DP : 0) + col + k) / 4)),
+                                     "r"(w[k]), "r"(w[k + 1]), "r"(w[k + 2]), "r"(w[k + 3]) : "memory");
+                    }
+                } else if (row < item.len) {
+                    store_row32(o, col, a.dim, w, key ? a.scale : 1.0f);
+                }
             }
+        }
+        if (a.cluster > 1) {
+            __syncwarp();
+            cluster_sync();
+            // this CTA's share of the rows, in pieces of four columns
+            const unsigned rows = kTile / a.cluster, first = rank * rows;
+#pragma unroll 2
+            for (unsigned i = threadIdx.x; i < rows * (2 * DP / 4); i += 32 * kBwdWarps) {
+                const unsigned r = first + i / (2 * DP / 4), piece = i % (2 * DP / 4), col = 4 * piece;
+                float4 y[8];
+#pragma unroll
+                for (int other = 0; other < 8; ++other)
+                    if (other < a.cluster) y[other] = ld_cluster4(sums_piece<DP>(smem, r, piece), other);
+                float4 x = y[0];
+#pragma unroll
+                for (int other = 1; other < 8; ++other)
+                    if (other < a.cluster) x.x += y[other].x, x.y += y[other].y, x.z += y[other].z, x.w += y[other].w;
+                const bool key = col >= DP;
+                const unsigned c4 = key ? col - DP : col;
+                const HeadsOut &out = key ? a.dk : a.dv;
+                const float by = key ? a.scale : 1.0f;
+                if (row0 + r < item.len && c4 < a.dim)
+                    *reinterpret_cast<uint2 *>(out.data + (unsigned long long)(item.start + row0 + r) * out.ld_token + hk * out.ld_head + c4) =
+                        make_uint2(pack2(x.x * by, x.y * by), pack2(x.z * by, x.w * by));
+            }
+            __syncwarp();
+            cluster_sync();                           // nobody reads this CTA's sums any more
         }
     }
     attn_end<kBwdWarps>(sh, a, warp, tmem);
