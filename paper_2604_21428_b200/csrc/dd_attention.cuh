@@ -491,12 +491,13 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                 for (int k = 2; k < 32; k += 2) m[i] = max3(m[i], __uint_as_float(r[i][k]), __uint_as_float(r[i][k + 1]));
             }
             const float now = max3(m[0], m[1], max3(m[2], m[3], -INFINITY));
-            // The sums are moved to a larger maximum only when it has grown by more than 2^8: until then the
+            // A row's sums are moved to a larger maximum only when it has grown by more than 2^8: until then the
             // weights stay below 2^8, exact in float32 and as far from the end of bf16's range.
-            if (__any_sync(0xffffffffu, !((now - top) * c <= 8.0f))) {
-                const float next = now == -INFINITY ? 0.0f : now;
+            const bool grown = !((now - top) * c <= 8.0f);
+            if (__any_sync(0xffffffffu, grown)) {
+                const float next = !grown ? base : now == -INFINITY ? 0.0f : now;
                 if (j) {
-                    const float by = exp2_fast((base - next) * c);
+                    const float by = grown && top != -INFINITY ? exp2_fast((base - next) * c) : 1.0f;      // (sums of nothing are 0)
                     sum *= by;
 #pragma unroll 1
                     for (int i = 0; i < DP / 16; ++i) {
@@ -508,7 +509,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                         tmem_st16(o_at + 16 * i, o);
                     }
                 }
-                top = now;
+                top = grown ? now : top;
                 base = next;
             }
             const float off = -base * c;

@@ -81,6 +81,19 @@ class CGraceController(ctypes.Structure):
                 ("xi_sync", ctypes.c_double), ("n_obs", ctypes.c_int32)]
 
 
+class CAttention(ctypes.Structure):
+    """Mirror of ``dd_attention``."""
+    _fields_ = [("tokens", ctypes.c_uint64), ("heads", ctypes.c_uint64), ("kv_heads", ctypes.c_uint64), ("dim", ctypes.c_uint64),
+                ("sequences", ctypes.c_uint64), ("offsets", ctypes.c_void_p), ("scale", ctypes.c_float), ("causal", ctypes.c_int32),
+                ("flags", ctypes.c_uint32)]
+
+
+class CVocabLoss(ctypes.Structure):
+    """Mirror of ``dd_vocab_loss``."""
+    _fields_ = [("tokens", ctypes.c_uint64), ("d", ctypes.c_uint64), ("vocab", ctypes.c_uint64), ("ld_hidden", ctypes.c_uint64),
+                ("ld_weight", ctypes.c_uint64), ("weight", ctypes.c_void_p), ("targets", ctypes.c_void_p), ("flags", ctypes.c_uint32)]
+
+
 class CGradRecord(ctypes.Structure):
     """Mirror of ``dd_grad_record``."""
     _fields_ = [("norm", ctypes.c_float), ("scale", ctypes.c_float), ("status", ctypes.c_int32),
@@ -187,6 +200,10 @@ def _load() -> ctypes.CDLL:
     lib.dd_last_cuda_error.argtypes = [vp]
     lib.dd_launch_geometry.restype = ctypes.c_int
     lib.dd_launch_geometry.argtypes = [vp, ctypes.c_int] + [ctypes.POINTER(ctypes.c_int)] * 3
+    lib.dd_attention_scratch_bytes.restype = ctypes.c_uint64
+    lib.dd_attention_scratch_bytes.argtypes = [ctypes.POINTER(CAttention), ctypes.c_int]
+    lib.dd_vocab_loss_scratch_bytes.restype = ctypes.c_uint64
+    lib.dd_vocab_loss_scratch_bytes.argtypes = [vp, ctypes.POINTER(CVocabLoss), ctypes.c_int]
     lib.dd_launch_shape.restype = ctypes.c_int
     lib.dd_launch_shape.argtypes = [ctypes.c_int] * 4 + [ctypes.POINTER(ctypes.c_int)] * 2
     return lib
@@ -644,6 +661,12 @@ class Context:
         if rc != OK:
             self._check(rc)
 
+    def vocab_loss_scratch_bytes(self, tokens: int, d: int, vocab: int, *, backward: bool = False) -> int:
+        """``dd_vocab_loss_scratch_bytes``: bytes that ``scratch`` of such a call needs."""
+        ld = (int(d) + 7) // 8 * 8
+        loss = CVocabLoss(tokens=tokens, d=d, vocab=vocab, ld_hidden=ld, ld_weight=ld, weight=16, targets=16)
+        return int(lib.dd_vocab_loss_scratch_bytes(self._h, ctypes.byref(loss), int(bool(backward))))
+
     def vocab_loss_forward(self, hidden, weight, targets, loss, lse, *, scratch=None, status=None, flags: int = 0,
                            stream=None) -> None:
         """``dd_vocab_loss_forward``: softmax cross entropy of ``hidden`` [tokens, d] against the rows of
@@ -684,6 +707,39 @@ def _raw_stream(stream) -> int:
         import torch
         return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream if isinstance(stream, int) else int(stream.cuda_stream)
+
+
+def attention_scratch_bytes(tokens: int, heads: int, kv_heads: int, dim: int, sequences: int | None = None, *,
+                            backward: bool = False) -> int:
+    """``dd_attention_scratch_bytes``: bytes that ``scratch`` of such a call needs at most; ``sequences`` None: no
+    offsets."""
+    a = CAttention(tokens=tokens, heads=heads, kv_heads=kv_heads, dim=dim, sequences=sequences or 0,
+                   offsets=None if sequences is None else 16, scale=1.0, causal=1)
+    return int(lib.dd_attention_scratch_bytes(ctypes.byref(a), int(bool(backward))))
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, *, factor: float = 1.0, trained: int | None = None,
+                       low: float = 1.0, high: float = 32.0, device=None):
+    """Frequencies for ``Context.rotary`` (a float64 tensor of ``rotary_dim`` / 2: radians per position) and the
+    magnitude that goes with them.
+
+    Pair i turns by ``base ** (-2 i / rotary_dim)`` a position.  For contexts ``factor`` times as long as what
+    a model was trained on: without ``trained`` all positions are divided by the factor; with it, the context
+    that the model was trained on, by parts -- pairs that turn ``high`` times and more in it stay as they are, those that
+    turn ``low`` times and less are divided, a linear ramp lies between -- and the magnitude is 0.1 log(factor) + 1."""
+    import math
+
+    import torch
+    if rotary_dim < 2 or rotary_dim % 2 or not base > 0 or not factor >= 1 or not high > low:
+        raise ValueError("rotary_dim must be even and positive, base positive, factor at least 1, high above low")
+    f = torch.tensor([base ** (-2 * i / rotary_dim) for i in range(rotary_dim // 2)], dtype=torch.float64)
+    magnitude = 1.0
+    if factor > 1 and trained is None:
+        f = f / factor
+    elif factor > 1:
+        keep = ((trained * f / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+        f, magnitude = f * (keep + (1 - keep) / factor), 0.1 * math.log(factor) + 1.0
+    return f.to(device or "cuda"), magnitude
 
 
 def new_grad_record(device=None):
