@@ -336,16 +336,6 @@ __device__ __forceinline__ void fewer_registers()
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(WARPS == kFwdWarps ? 88 : 64));
 }
 
-// Roles by number, 0 .. WARPS - 1 those that compute, WARPS the copies, WARPS + 1 the products, WARPS + 2 the zeroes.  The
-// four that do not compute are the CTA's first warps, the products' the very first: it shares its scheduler
-// with warps that have something to issue all the time, and goes before them where it is older (MEASURED).
-template <int WARPS>
-__device__ __forceinline__ int role_of()
-{
-    const int w = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
-    return w >= 4 ? w - 4 : w == 0 ? WARPS + 1 : w == 1 ? WARPS : WARPS + w;
-}
-
 // Lane 0 of a warp reports that the warp is done with (or has written) its part of tensor memory.
 __device__ __forceinline__ void warp_arrive(unsigned bar, int lane)
 {
@@ -383,7 +373,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
     const unsigned bar = smem_addr(sh.bars), q_full = bar, full = bar + 8, empty = full + 8 * kStages, s_full = empty + 8 * kStages,
                    p_full = s_full + 16, o_full = p_full + 16, drain = o_full + 16, clean = drain + 8, tail = clean + 8;
     volatile int *abort = &sh.abort_flag;
-    const int warp = role_of<kFwdWarps>(), lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         init_bar(q_full, 1);
@@ -604,7 +594,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
                    s_full = bar + 104, dp_full = bar + 112, dq_full = bar + 120, drain = bar + 128, clean = bar + 136, tail = bar + 144,
                    q_full = bar + 152, s_read = bar + 160, ds_full = bar + 168, sum_full = bar + 176;
     volatile int *abort = &sh.abort_flag;
-    const int warp = role_of<kBwdWarps>(), lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         for (int i = 0; i < 19; ++i) init_bar(bar + 8 * i, 1);
@@ -801,7 +791,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                    s_full = bar + 88, dp_full = bar + 96, done = bar + 104, drain = bar + 112, q_clean = bar + 120, do_clean = bar + 144,
                    q_tail = bar + 160, do_tail = bar + 184, p_full = bar + 200, ds_full = bar + 208, st_full = bar + 216;
     volatile int *abort = &sh.abort_flag;
-    const int warp = role_of<kBwdWarps>(), lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         for (int i = 0; i < 25; ++i) init_bar(bar + 8 * i, 1);
@@ -917,7 +907,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
         const float c = a.scale * kLog2e;
         // the first 256 threads fetch the statistics: lse or delta of one query of tile j
         const auto stat = [&](unsigned j) {
-            const unsigned i = tile_of(j) * kTile + (warp & 3) * 32 + lane, h = head_of(j);
+            const unsigned i = tile_of(j) * kTile + (threadIdx.x & 127), h = head_of(j);
             if (share >= 2 || j >= n || i >= item.len) return 0.0f;
             const unsigned long long where = (unsigned long long)h * a.tokens + item.start + i;
             return share ? -a.delta[where] : -a.lse[where] * kLog2e;
@@ -936,7 +926,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
         bool ok = true;
         for (unsigned j = 0; j < n; ++j) {
             if (share < 2) {
-                stats[j & 1][share][(warp & 3) * 32 + lane] = next;
+                stats[j & 1][share][threadIdx.x & 127] = next;
                 __syncwarp();
                 if (lane == 0) arrive_bar(st_full);
                 if (j + 1 < n) next = stat(j + 1);
@@ -1021,7 +1011,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             // this CTA's share of the rows, in pieces of four columns
             const unsigned rows = kTile / a.cluster, first = rank * rows;
 #pragma unroll 2
-            for (unsigned i = warp * 32 + lane; i < rows * (2 * DP / 4); i += 32 * kBwdWarps) {
+            for (unsigned i = threadIdx.x; i < rows * (2 * DP / 4); i += 32 * kBwdWarps) {
                 const unsigned r = first + i / (2 * DP / 4), piece = i % (2 * DP / 4), col = 4 * piece;
                 float4 y[8];
 #pragma unroll
