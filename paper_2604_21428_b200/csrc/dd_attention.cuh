@@ -359,16 +359,6 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
     constexpr unsigned kBytes = kTile * DP * 2;
     extern __shared__ unsigned char smem_raw[];
     __shared__ alignas(16) AttnShared sh;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    PlanItem item;
-    if (!plan_item(a, blockIdx.x / a.heads, item)) return;
-    const unsigned head = blockIdx.x % a.heads, row0 = item.tile * 2 * kTile;
-    const unsigned rows = item.len - row0;                                  // from row0 on
-    // tiles of keys that each of the two needs
-    const unsigned all = (item.len + kTile - 1) / kTile, t0 = item.tile * 2;
-    const unsigned n0 = a.causal ? t0 + 1 : all, n1 = rows <= kTile ? 0 : a.causal ? t0 + 2 : all;
-    const unsigned n = n0 > n1 ? n0 : n1;
-
     const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u, ring = smem + 2 * kBytes;
     const unsigned bar = smem_addr(sh.bars), q_full = bar, full = bar + 8, empty = full + 8 * kStages, s_full = empty + 8 * kStages,
                    p_full = s_full + 16, o_full = p_full + 16, drain = o_full + 16, clean = drain + 8, tail = clean + 8;
@@ -391,6 +381,19 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
         init_bar(tail, 1);
     }
     const unsigned tmem = attn_begin<kFwdWarps>(sh, warp);
+    // all so far without waiting for the launch before
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    PlanItem item;
+    if (!plan_item(a, blockIdx.x / a.heads, item)) {
+        attn_end<kFwdWarps>(sh, a, warp, tmem);
+        return;
+    }
+    const unsigned head = blockIdx.x % a.heads, row0 = item.tile * 2 * kTile;
+    const unsigned rows = item.len - row0;                                  // from row0 on
+    // tiles of keys that each of the two needs
+    const unsigned all = (item.len + kTile - 1) / kTile, t0 = item.tile * 2;
+    const unsigned n0 = a.causal ? t0 + 1 : all, n1 = rows <= kTile ? 0 : a.causal ? t0 + 2 : all;
+    const unsigned n = n0 > n1 ? n0 : n1;
     const unsigned kS = tmem, kO = tmem + 2 * kTile;                         // scores of tile t at kS + 128 t, sums at kO + DP t
 
     if (warp >= kFwdWarps) {
@@ -583,12 +586,6 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
     BwdShared &rest = *reinterpret_cast<BwdShared *>(smem_tiles + 7 * kBytes);
     AttnShared &sh = rest.sh;
     float (&shares)[4][kTile] = rest.row;         // of a row's delta
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    PlanItem item;
-    if (!plan_item(a, blockIdx.x / a.heads, item)) return;
-    const unsigned head = blockIdx.x % a.heads, row0 = item.tile * kTile, all = (item.len + kTile - 1) / kTile;
-    const unsigned n = a.causal ? item.tile + 1 : all;
-
     const unsigned smem = smem_addr(smem_tiles), sdo = smem, sk = smem + kBytes, sv = smem + 4 * kBytes;
     const unsigned bar = smem_addr(sh.bars), k_full = bar, k_empty = bar + 24, v_full = bar + 48, v_empty = bar + 72, do_full = bar + 96,
                    s_full = bar + 104, dp_full = bar + 112, dq_full = bar + 120, drain = bar + 128, clean = bar + 136, tail = bar + 144,
@@ -601,6 +598,15 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
         for (int i = 19; i < 23; ++i) init_bar(bar + 8 * i, kBwdWarps);
     }
     const unsigned tmem = attn_begin<kBwdWarps>(sh, warp);
+    // all so far without waiting for the launch before
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    PlanItem item;
+    if (!plan_item(a, blockIdx.x / a.heads, item)) {
+        attn_end<kBwdWarps>(sh, a, warp, tmem);
+        return;
+    }
+    const unsigned head = blockIdx.x % a.heads, row0 = item.tile * kTile, all = (item.len + kTile - 1) / kTile;
+    const unsigned n = a.causal ? item.tile + 1 : all;
     // the queries, and with 64 columns their gradients' operand d_o as well, are held in tensor memory
     const unsigned kS = tmem, kP = tmem + kTile, kDs = tmem + 2 * kTile, kDq = kDs + 64, kQ = tmem + 448, kDo = tmem + 384;
 
@@ -772,20 +778,6 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
     BwdShared &rest = *reinterpret_cast<BwdShared *>(smem_tiles + 7 * kBytes);
     AttnShared &sh = rest.sh;
     float (*stats)[2][kTile] = reinterpret_cast<float (*)[2][kTile]>(rest.row);   // of every other tile: -lse log2(e) and -delta of its queries
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const unsigned kv_heads = a.heads / a.group;
-    PlanItem item;
-    const unsigned rank = blockIdx.x % a.cluster, unit = blockIdx.x / a.cluster;
-    if (!plan_item(a, unit / kv_heads, item)) return;                        // (the cluster as a whole)
-    const unsigned hk = unit % kv_heads, all = (item.len + kTile - 1) / kTile;
-    const unsigned tile = all - 1 - item.tile, row0 = tile * kTile;          // early keys are read by most queries
-    // tiles of queries: `per` of each head that shares the keys, of which this CTA takes n from `start` on
-    const unsigned i0 = a.causal ? tile : 0, per = all - i0, total = per * a.group;
-    const unsigned start = (unsigned)((unsigned long long)total * rank / a.cluster), n = (unsigned)((unsigned long long)total * (rank + 1) / a.cluster) - start;
-    const auto head_of = [&](unsigned j) { return hk * a.group + (start + j) / per; };
-    const auto tile_of = [&](unsigned j) { return i0 + (start + j) % per; };
-    const auto is_last = [&](unsigned j) { return tile_of(j) == all - 1; };
-
     const unsigned smem = smem_addr(smem_tiles), sk = smem, sv = smem + kBytes, sq = smem + 2 * kBytes, sdo = smem + 5 * kBytes;
     const unsigned bar = smem_addr(sh.bars), q_full = bar, q_empty = bar + 24, do_full = bar + 48, do_empty = bar + 64, kv_full = bar + 80,
                    s_full = bar + 88, dp_full = bar + 96, done = bar + 104, drain = bar + 112, q_clean = bar + 120, do_clean = bar + 144,
@@ -801,6 +793,22 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
         init_bar(st_full, 8);
     }
     const unsigned tmem = attn_begin<kBwdWarps>(sh, warp);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const unsigned kv_heads = a.heads / a.group;
+    PlanItem item;
+    const unsigned rank = blockIdx.x % a.cluster, unit = blockIdx.x / a.cluster;
+    if (!plan_item(a, unit / kv_heads, item)) {                              // (the cluster as a whole)
+        attn_end<kBwdWarps>(sh, a, warp, tmem);
+        return;
+    }
+    const unsigned hk = unit % kv_heads, all = (item.len + kTile - 1) / kTile;
+    const unsigned tile = all - 1 - item.tile, row0 = tile * kTile;          // early keys are read by most queries
+    // tiles of queries: `per` of each head that shares the keys, of which this CTA takes n from `start` on
+    const unsigned i0 = a.causal ? tile : 0, per = all - i0, total = per * a.group;
+    const unsigned start = (unsigned)((unsigned long long)total * rank / a.cluster), n = (unsigned)((unsigned long long)total * (rank + 1) / a.cluster) - start;
+    const auto head_of = [&](unsigned j) { return hk * a.group + (start + j) / per; };
+    const auto tile_of = [&](unsigned j) { return i0 + (start + j) % per; };
+    const auto is_last = [&](unsigned j) { return tile_of(j) == all - 1; };
     const unsigned kS = tmem, kP = tmem + kTile, kDv = tmem + 2 * kTile, kDk = kDv + DP, kK = tmem + 384, kV = kK + 32;
     // tiles of queries whose rows past the sequence's end are zeroed: the last one of each head
     const unsigned last = item.len - (all - 1) * kTile;

@@ -11,13 +11,15 @@
 
 namespace ddm {
 
-// lse = log sum exp over the partial sums of a token, and the loss; 32 tokens a block, eight warps taking every
-// eighth of their partial sums.
-__global__ void __launch_bounds__(256)
+// lse = log sum exp over the partial sums of a token, and the loss; 32 tokens a block, its 32 warps taking every
+// 32nd of their partial sums, eight of them asked for at a time.
+constexpr unsigned kJoinWarps = 32;
+
+__global__ void __launch_bounds__(32 * kJoinWarps)
 vocab_loss_join_kernel(const float2 *partial, unsigned parts, unsigned tokens, const long long *targets, long long vocab, float *loss, float *lse)
 {
     constexpr float l = 1.4426950408889634f;
-    __shared__ float2 share[8][32];
+    __shared__ float2 share[kJoinWarps][33];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = blockIdx.x * 32 + lane;
@@ -27,17 +29,35 @@ vocab_loss_join_kernel(const float2 *partial, unsigned parts, unsigned tokens, c
         a.x = m;
     };
     float2 mine = make_float2(-INFINITY, 0.0f);
-    if (t < tokens)
-#pragma unroll 4
-        for (unsigned p = warp; p < parts; p += 8) join(mine, __ldcg(partial + (unsigned long long)p * tokens + t));
+    for (unsigned p0 = warp; p0 < parts; p0 += 8 * kJoinWarps) {
+        float2 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const unsigned p = p0 + i * kJoinWarps;
+            x[i] = p < parts && t < tokens ? __ldcg(partial + (unsigned long long)p * tokens + t) : make_float2(-INFINITY, 0.0f);
+        }
+#pragma unroll
+        for (int d = 1; d < 8; d *= 2)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2 * d) join(x[i], x[i + d]);
+        join(mine, x[0]);
+    }
     share[warp][lane] = mine;
     __syncthreads();
-    if (warp || t >= tokens) return;
-    for (int w = 1; w < 8; ++w) join(mine, share[w][lane]);
-    const float z = mine.x + logf(mine.y);
-    const long long target = targets[t];
-    lse[t] = z;
-    loss[t] = target < 0 ? 0.0f : target >= vocab ? NAN : z - loss[t];
+    // now a warp has a token, its lanes the warps' shares
+    const unsigned mt = blockIdx.x * 32 + warp;
+    if (mt >= tokens) return;
+    float2 x = share[lane][warp];
+#pragma unroll
+    for (int d = 16; d; d /= 2) {
+        const float2 y = make_float2(__shfl_xor_sync(0xffffffffu, x.x, d), __shfl_xor_sync(0xffffffffu, x.y, d));
+        join(x, y);
+    }
+    if (lane) return;
+    const float z = x.x + logf(x.y);
+    const long long target = targets[mt];
+    lse[mt] = z;
+    loss[mt] = target < 0 ? 0.0f : target >= vocab ? NAN : z - loss[mt];
 }
 
 static uint64_t rows8(uint64_t n) { return (n + 7) / 8 * 8; }
@@ -142,7 +162,7 @@ extern "C" int dd_vocab_loss_forward(dd_ctx *ctx, const dd_vocab_loss *l_, const
     if (rc == DD_OK) rc = encode(ctx, &a.maps[1], {l.weight, l.vocab, l.d, l.ld_weight});
     if (rc == DD_OK) rc = launch_logits<kEpiLoss>(ctx, a, T, l.vocab, l.d, stream);
     if (rc != DD_OK) return rc;
-    return launch_after(ctx, vocab_loss_join_kernel, blocks_of(T, 32), 256, 0, stream, a.e.partial, blocks_of(l.vocab, 128), (unsigned)T, a.e.targets,
+    return launch_after(ctx, vocab_loss_join_kernel, blocks_of(T, 32), 32 * kJoinWarps, 0, stream, a.e.partial, blocks_of(l.vocab, 128), (unsigned)T, a.e.targets,
                         a.e.vocab, loss, lse);
 }
 
