@@ -91,12 +91,12 @@ typedef struct {
     uint64_t tokens, heads, kv_heads, dim;
     uint64_t sequences;                     /* < 2^24 */
     const int32_t *offsets;
-    float scale;                            /* finite */
+    float scale;                            /* finite, above 0 */
     int32_t causal;
     uint32_t flags;                         /* 0 or DD_DEBUG_EXPIRE_WAIT, as for dd_gated_ffn */
 } dd_attention;
 
-/* Bytes of `scratch` below, at most; 0 for arguments that the calls refuse. */
+/* Bytes of `scratch` below, at most; 0 where none is needed, and for arguments that the calls refuse. */
 uint64_t dd_attention_scratch_bytes(const dd_attention *attention, int backward);
 
 /*
@@ -132,7 +132,8 @@ int dd_attention_backward(dd_ctx *ctx, const dd_attention *attention, const dd_h
  *   lse_t = log sum_v exp(z_tv),  loss_t = lse_t - z_t,target
  *
  * A negative target is none: loss 0 and no gradient.  A target from `vocab` on is an error of the data:
- * loss NaN and no gradient.  Matrices as in dd_learner.h: bf16, rows contiguous, strides in elements and
+ * loss NaN and no gradient.  The hidden row of a token without a target still takes part in products, with
+ * weight 0, and has to be finite.  Matrices as in dd_learner.h: bf16, rows contiguous, strides in elements and
  * multiples of 8, 16-byte aligned, 0 meaning the row length.  tokens may be 0; 1 <= d, vocab; sizes and
  * strides < 2^30 (DD_ERR_TOO_LARGE).
  */

@@ -1,5 +1,5 @@
 // dd_attention_forward / dd_attention_backward: arguments, tensor maps and launches.  Forward: the plan (with
-// offsets) and one launch.  Backward: the plan, delta = d_o . o, dq, then dk and dv.
+// offsets) and one launch.  Backward: the plan and delta = d_o . o in one, dq, then dk and dv.
 #include <cmath>
 
 #include "dd_args.h"
@@ -54,9 +54,9 @@ static uint64_t most_tiles(const dd_attention &a, unsigned rows)
 static uint64_t round16(uint64_t n) { return (n + 15) / 16 * 16; }
 static uint64_t plan_bytes(const dd_attention &a, unsigned rows) { return a.offsets ? 16 + 16 * most_tiles(a, rows) : 0; }
 
-static int launch_plan(dd_ctx *ctx, const dd_attention &a, unsigned rows, Plan *plan, int32_t *status, cudaStream_t stream)
+static PlanArgs plan_args(const dd_attention &a, unsigned rows, Plan *plan, int32_t *status)
 {
-    return launch_after(ctx, attention_plan_kernel, 1, kPlanThreads, 0, stream, a.offsets, (unsigned)a.sequences, (unsigned)a.tokens, rows, plan, status);
+    return {a.offsets, (unsigned)a.sequences, (unsigned)a.tokens, rows, plan, status};
 }
 
 template <int DP>
@@ -90,13 +90,13 @@ static unsigned dkv_cluster(const dd_ctx *ctx, const dd_attention &b)
 }
 
 template <int DP>
-static int launch_backward(dd_ctx *ctx, const dd_attention &b, AttnArgs &a, const DeltaArgs &d, cudaStream_t stream)
+static int launch_backward(dd_ctx *ctx, const dd_attention &b, AttnArgs &a, const DeltaArgs &d, const PlanArgs &plan, cudaStream_t stream)
 {
     static std::atomic<bool> done_q[64], done_kv[64];
     int rc = allow_smem(ctx, attention_dq_kernel<DP>, bwd_smem_bytes(DP), done_q);
     if (rc == DD_OK) rc = allow_smem(ctx, attention_dkv_kernel<DP>, bwd_smem_bytes(DP), done_kv);
     constexpr int lanes = DP / 8;
-    if (rc == DD_OK) rc = launch_after(ctx, attention_delta_kernel<lanes>, (b.tokens * b.heads * lanes + 255) / 256, 256, 0, stream, d);
+    if (rc == DD_OK) rc = launch_after(ctx, attention_delta_kernel<lanes>, (b.tokens * b.heads * lanes + 255) / 256 + (plan.plan ? 1 : 0), 256, 0, stream, d, plan);
     const uint64_t tiles = most_tiles(b, kTile);
     if (rc == DD_OK) rc = launch_after(ctx, attention_dq_kernel<DP>, tiles * b.heads, 32 * (kBwdWarps + 4), bwd_smem_bytes(DP), stream, a);
     a.cluster = dkv_cluster(ctx, b);
@@ -171,7 +171,7 @@ extern "C" int dd_attention_forward(dd_ctx *ctx, const dd_attention *attention, 
     if (rc == DD_OK) rc = encode_heads(ctx, &a.v, v, T, b.kv_heads, b.dim);
     a.o = out_of(o);
     a.lse = lse;
-    if (rc == DD_OK && plan) rc = launch_plan(ctx, b, 2 * kTile, plan, status, stream);
+    if (rc == DD_OK && plan) rc = launch_after(ctx, attention_plan_kernel, 1, kPlanThreads, 0, stream, plan_args(b, 2 * kTile, plan, status));
     if (rc != DD_OK) return rc;
     return b.dim <= 64 ? launch_forward<64>(ctx, b, a, stream) : launch_forward<128>(ctx, b, a, stream);
 }
@@ -216,7 +216,6 @@ extern "C" int dd_attention_backward(dd_ctx *ctx, const dd_attention *attention,
     if (rc == DD_OK) rc = encode_heads(ctx, &a.k, k, T, b.kv_heads, b.dim);
     if (rc == DD_OK) rc = encode_heads(ctx, &a.v, v, T, b.kv_heads, b.dim);
     if (rc == DD_OK) rc = encode_heads(ctx, &a.d_o, d_o, T, b.heads, b.dim);
-    if (rc == DD_OK && plan) rc = launch_plan(ctx, b, kTile, plan, status, stream);
     if (rc != DD_OK) return rc;
     a.q_rows = out_of(q);
     a.k_rows = out_of(k);
@@ -229,5 +228,6 @@ extern "C" int dd_attention_backward(dd_ctx *ctx, const dd_attention *attention,
     a.delta = delta;
     const DeltaArgs d = {static_cast<const __nv_bfloat16 *>(o.data), static_cast<const __nv_bfloat16 *>(d_o.data), o.ld_token, o.ld_head,
                          d_o.ld_token, d_o.ld_head, delta, (unsigned)T, (unsigned)b.heads, (unsigned)b.dim};
-    return b.dim <= 64 ? launch_backward<64>(ctx, b, a, d, stream) : launch_backward<128>(ctx, b, a, d, stream);
+    const PlanArgs p = plan_args(b, kTile, plan, status);
+    return b.dim <= 64 ? launch_backward<64>(ctx, b, a, d, p, stream) : launch_backward<128>(ctx, b, a, d, p, stream);
 }

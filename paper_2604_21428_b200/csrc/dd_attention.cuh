@@ -213,7 +213,7 @@ __device__ __forceinline__ void hold_row32(unsigned at, const __nv_bfloat16 *row
     unsigned w[16];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint4 x = row && col + 8 * j < dim ? __ldg(reinterpret_cast<const uint4 *>(row + col + 8 * j)) : make_uint4(0u, 0u, 0u, 0u);
+        const uint4 x = row && col + 8 * j < dim ? __ldcg(reinterpret_cast<const uint4 *>(row + col + 8 * j)) : make_uint4(0u, 0u, 0u, 0u);
         w[4 * j] = x.x;
         w[4 * j + 1] = x.y;
         w[4 * j + 2] = x.z;
@@ -295,10 +295,12 @@ struct AttnShared {
 };
 
 template <int WARPS>
-__device__ __forceinline__ unsigned attn_begin(AttnShared &sh, int warp)
+__device__ __forceinline__ unsigned attn_begin(AttnShared &sh, const AttnArgs &a, int warp)
 {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    if (threadIdx.x == 32 * WARPS)
+        for (const CUtensorMap *m : {&a.q, &a.k, &a.v, a.delta ? &a.d_o : &a.q}) asm volatile("prefetch.tensormap [%0];" :: "l"(m) : "memory");
     if (warp == WARPS + 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_addr(&sh.tmem_base)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -380,7 +382,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
         init_bar(clean, 1);
         init_bar(tail, 1);
     }
-    const unsigned tmem = attn_begin<kFwdWarps>(sh, warp);
+    const unsigned tmem = attn_begin<kFwdWarps>(sh, a, warp);
     // all so far without waiting for the launch before
     asm volatile("griddepcontrol.wait;" ::: "memory");
     PlanItem item;
@@ -597,7 +599,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
         for (int i = 0; i < 19; ++i) init_bar(bar + 8 * i, 1);
         for (int i = 19; i < 23; ++i) init_bar(bar + 8 * i, kBwdWarps);
     }
-    const unsigned tmem = attn_begin<kBwdWarps>(sh, warp);
+    const unsigned tmem = attn_begin<kBwdWarps>(sh, a, warp);
     // all so far without waiting for the launch before
     asm volatile("griddepcontrol.wait;" ::: "memory");
     PlanItem item;
@@ -792,7 +794,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
         init_bar(ds_full, kBwdWarps);
         init_bar(st_full, 8);
     }
-    const unsigned tmem = attn_begin<kBwdWarps>(sh, warp);
+    const unsigned tmem = attn_begin<kBwdWarps>(sh, a, warp);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const unsigned kv_heads = a.heads / a.group;
     PlanItem item;
@@ -1044,52 +1046,25 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
     attn_end<kBwdWarps>(sh, a, warp, tmem);
 }
 
-// delta = d_o . o of every row of every head; LANES = lanes of a row, 8 elements each.
-struct DeltaArgs {
-    const __nv_bfloat16 *o, *d_o;
-    unsigned long long o_token, o_head, d_token, d_head;
-    float *delta;
-    unsigned tokens, heads, dim;
-};
-
-template <int LANES>
-__global__ void __launch_bounds__(256)
-attention_delta_kernel(const DeltaArgs a)
-{
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const unsigned long long i = ((unsigned long long)blockIdx.x * 256 + threadIdx.x) / LANES, rows = (unsigned long long)a.tokens * a.heads;
-    const unsigned col = threadIdx.x % LANES * 8;
-    const unsigned long long t = i / a.heads;
-    const unsigned h = (unsigned)(i - t * a.heads);
-    float sum = 0.0f;
-    if (i < rows && col < a.dim) {
-        const uint4 x = *reinterpret_cast<const uint4 *>(a.o + t * a.o_token + h * a.o_head + col),
-                    y = *reinterpret_cast<const uint4 *>(a.d_o + t * a.d_token + h * a.d_head + col);
-        const unsigned u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            sum = fmaf(__uint_as_float(u[k] << 16), __uint_as_float(v[k] << 16), sum);
-            sum = fmaf(__uint_as_float(u[k] & 0xffff0000u), __uint_as_float(v[k] & 0xffff0000u), sum);
-        }
-    }
-#pragma unroll
-    for (int s = LANES / 2; s; s /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-    if (i < rows && col == 0) a.delta[(unsigned long long)h * a.tokens + t] = sum;
-}
-
 // ---- plan ------------------------------------------------------------------------------------------
 
-constexpr unsigned kPlanKeys = 4096, kPlanThreads = 1024;
+constexpr unsigned kPlanKeys = 4096, kPlanThreads = 256;
 
 // The tiles of `rows` tokens of all sequences, ordered by their place in the sequence, last first (by counting;
 // the order among tiles of one place does not matter to any result).
-__global__ void __launch_bounds__(kPlanThreads)
-attention_plan_kernel(const int *offsets, unsigned sequences, unsigned tokens, unsigned rows, Plan *plan, int *status)
+struct PlanArgs {
+    const int *offsets;
+    unsigned sequences, tokens, rows;
+    Plan *plan;                                   // null: none wanted
+    int *status;
+};
+
+__device__ __forceinline__ void make_plan(const PlanArgs &a)
 {
-    __shared__ unsigned count[kPlanKeys], warp_sum[32];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ unsigned count[kPlanKeys], warp_sum[kPlanThreads / 32];
+    const int *offsets = a.offsets;
+    const unsigned sequences = a.sequences, tokens = a.tokens, rows = a.rows;
+    Plan *plan = a.plan;
     const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     bool good = offsets[0] >= 0;
     for (unsigned s = threadIdx.x; s < sequences; s += kPlanThreads)
@@ -1098,7 +1073,7 @@ attention_plan_kernel(const int *offsets, unsigned sequences, unsigned tokens, u
     if (!__syncthreads_and(good)) {
         if (threadIdx.x == 0) {
             plan->count = 0;
-            if (status) *status = DD_STATUS_BAD_OFFSETS;
+            if (a.status) *a.status = DD_STATUS_BAD_OFFSETS;
         }
         return;
     }
@@ -1132,6 +1107,56 @@ attention_plan_kernel(const int *offsets, unsigned sequences, unsigned tokens, u
     }
     __syncthreads();
     each([&](unsigned start, unsigned len, unsigned t) { plan->item[atomicAdd(&count[key(t)], 1u)] = PlanItem{start, len, t, 0u}; });
+}
+
+__global__ void __launch_bounds__(kPlanThreads)
+attention_plan_kernel(const PlanArgs a)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    make_plan(a);
+}
+
+// ---- delta ---------------------------------------------------------------------------------------
+
+// delta = d_o . o of every row of every head; LANES = lanes of a row, 8 elements each.  With offsets the first block
+// makes the plan instead.
+struct DeltaArgs {
+    const __nv_bfloat16 *o, *d_o;
+    unsigned long long o_token, o_head, d_token, d_head;
+    float *delta;
+    unsigned tokens, heads, dim;
+};
+
+template <int LANES>
+__global__ void __launch_bounds__(kPlanThreads)
+attention_delta_kernel(const DeltaArgs a, const PlanArgs plan)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const unsigned planning = plan.plan ? 1 : 0;
+    if (blockIdx.x < planning) {
+        make_plan(plan);
+        return;
+    }
+    const unsigned long long i = ((unsigned long long)(blockIdx.x - planning) * 256 + threadIdx.x) / LANES, rows = (unsigned long long)a.tokens * a.heads;
+    const unsigned col = threadIdx.x % LANES * 8;
+    const unsigned long long t = i / a.heads;
+    const unsigned h = (unsigned)(i - t * a.heads);
+    float sum = 0.0f;
+    if (i < rows && col < a.dim) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(a.o + t * a.o_token + h * a.o_head + col),
+                    y = *reinterpret_cast<const uint4 *>(a.d_o + t * a.d_token + h * a.d_head + col);
+        const unsigned u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sum = fmaf(__uint_as_float(u[k] << 16), __uint_as_float(v[k] << 16), sum);
+            sum = fmaf(__uint_as_float(u[k] & 0xffff0000u), __uint_as_float(v[k] & 0xffff0000u), sum);
+        }
+    }
+#pragma unroll
+    for (int s = LANES / 2; s; s /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+    if (i < rows && col == 0) a.delta[(unsigned long long)h * a.tokens + t] = sum;
 }
 
 }  // namespace ddm

@@ -71,20 +71,26 @@ ffn_reduce_kernel(const __grid_constant__ ReduceArgs a)
         const unsigned pieces = j.ld / 8, row = (unsigned)(at / pieces), col = (unsigned)(at % pieces) * 8;
         const unsigned cols = j.n - col < 8 ? j.n - col : 8;
         const float *src = j.slabs + (unsigned long long)row * j.ld + col;
-        float4 v[kMaxSplits][2];
-#pragma unroll
-        for (int s = 0; s < kMaxSplits; ++s)
-            if (s < j.splits) {
-                v[s][0] = __ldcg(reinterpret_cast<const float4 *>(src + s * j.slab));
-                v[s][1] = __ldcg(reinterpret_cast<const float4 *>(src + s * j.slab) + 1);
-            }
         float x[2][4];
+        for (unsigned s0 = 0; s0 < j.splits; s0 += kMaxSplits) {          // in split order, eight asked for at a time
+            float4 v[kMaxSplits][2];
+#pragma unroll
+            for (int s = 0; s < kMaxSplits; ++s)
+                if (s0 + s < j.splits) {
+                    v[s][0] = __ldcg(reinterpret_cast<const float4 *>(src + (s0 + s) * j.slab));
+                    v[s][1] = __ldcg(reinterpret_cast<const float4 *>(src + (s0 + s) * j.slab) + 1);
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (!s0) { x[h][0] = v[0][h].x; x[h][1] = v[0][h].y; x[h][2] = v[0][h].z; x[h][3] = v[0][h].w; }
+                else { x[h][0] += v[0][h].x; x[h][1] += v[0][h].y; x[h][2] += v[0][h].z; x[h][3] += v[0][h].w; }
+#pragma unroll
+                for (int s = 1; s < kMaxSplits; ++s)
+                    if (s0 + s < j.splits) { x[h][0] += v[s][h].x; x[h][1] += v[s][h].y; x[h][2] += v[s][h].z; x[h][3] += v[s][h].w; }
+            }
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            x[h][0] = v[0][h].x; x[h][1] = v[0][h].y; x[h][2] = v[0][h].z; x[h][3] = v[0][h].w;
-#pragma unroll
-            for (int s = 1; s < kMaxSplits; ++s)
-                if (s < j.splits) { x[h][0] += v[s][h].x; x[h][1] += v[s][h].y; x[h][2] += v[s][h].z; x[h][3] += v[s][h].w; }
             const unsigned c = col + 4 * h, live = cols > 4 * h ? cols - 4 * h : 0;
             if (!live) break;
             if (j.addend) {

@@ -54,13 +54,13 @@ inline size_t slab_bytes(const dd_ctx *ctx) { return (size_t)ctx->sm_count * (2 
 // further problems.  Alone, the number that makes the fewest waves of the shortest units (a unit's
 // epilogue counts as 10 blocks, the launch that adds the splits up as 8); with others to fill the
 // gaps, the smallest one whose units are no longer than what each pair has to do anyway.
-inline unsigned choose_splits(const dd_ctx *ctx, unsigned tiles, unsigned blocks, unsigned long long other)
+inline unsigned choose_splits(const dd_ctx *ctx, unsigned tiles, unsigned blocks, unsigned long long other, unsigned most = kMaxSplits)
 {
     const unsigned pairs = (unsigned)ctx->sm_count / 2;
     const unsigned long long share = ((unsigned long long)tiles * blocks + other) / pairs + 1;
     unsigned best = 1;
     unsigned long long least = ~0ull;
-    for (unsigned s = 1; s <= kMaxSplits && (s == 1 || (tiles * s <= 2 * pairs && blocks >= 4 * s)); ++s) {
+    for (unsigned s = 1; s <= most && (s == 1 || (tiles * s <= 2 * pairs && blocks >= 4 * s)); ++s) {
         if (other) {
             best = s;
             if (blocks / s <= share) break;
@@ -74,6 +74,11 @@ inline unsigned choose_splits(const dd_ctx *ctx, unsigned tiles, unsigned blocks
     }
     return best;
 }
+
+// K blocks that a unit's epilogue takes as long as (256 x 256 outputs: 2.7 us): with fewer, the schedule counts these.
+// (One token, d 2048, 32000 columns of the vocabulary, whose gradient has one K block a tile: 224 us without, 111 with.)
+constexpr unsigned kEpilogueBlocks = 8;
+inline unsigned unit_blocks(unsigned blocks) { return blocks > kEpilogueBlocks ? blocks : kEpilogueBlocks; }
 
 template <int EPI, int BN, int ACT>
 inline int launch_gemm_act(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
@@ -89,7 +94,8 @@ inline int launch_gemm_act(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream)
     a.extra = 0;
     if (a.rest && a.nprob > 1) {
         const GemmProblem &q = a.prob[1];
-        const unsigned one = (p.kblocks[0] + p.kblocks[1]) / p.splits, next = blocks_of(q.kblocks[0] + q.kblocks[1], q.splits);
+        // a unit costs its K blocks, or its epilogue, which runs under the next unit's, where that is longer
+        const unsigned one = unit_blocks((p.kblocks[0] + p.kblocks[1]) / p.splits), next = unit_blocks(blocks_of(q.kblocks[0] + q.kblocks[1], q.splits));
         a.extra = (one + next / 2) / next;
         const unsigned room = (a.tiles - a.first) / (pairs - a.rest);
         if (a.extra > room) a.extra = room;

@@ -296,6 +296,8 @@ def test_refusals(dd, ctx):
     with pytest.raises(dd.DDMergeError) as e:
         ctx.attention_backward(c.q, c.k, c.v, c.o, c.lse, c.d_o, c.dq, c.dk, c.dk)
     assert e.value.rc == dd.ERR_ALIAS
-    empty = Case([], 2, 1, 64)
-    empty.forward(ctx)
-    empty.backward(ctx)
+    for empty in (Case([], 2, 1, 64), Case([0, 0], 2, 1, 64, before=3, after=2), Case([], 2, 1, 64, after=4)):
+        empty.forward(ctx)
+        empty.backward(ctx)
+        empty.check(True)
+        empty.check_back(True)
