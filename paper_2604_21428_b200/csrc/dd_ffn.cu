@@ -3,20 +3,9 @@
 // Backward: one launch for the gradients inside the block, one for dx and the three weights.
 #include <cmath>
 
-#include "dd_ffn_stream.cuh"
 #include "dd_gemm_launch.cuh"
 
 namespace ddm {
-
-// ---- few tokens ----------------------------------------------------------------------------
-
-// Up to here the weight-streaming kernel is ahead of the 256-row tiles of the pairs, forward with gate and up kept / backward:
-// 160 tokens, d 2048, f 8192 37 / 84 us (42 / 92), 300 tokens, 1024 x 4096 28 / 48 us (30 / 50); behind at 384 tokens, 2048 x 8192:
-// 66 / 120 us (64 / 116).
-constexpr unsigned long long kStreamMaxTokens = 320;
-
-// Ring of a CTA: two CTAs share an SM.
-constexpr unsigned kStreamRing = 96 * 1024;
 
 // Whether a kEpiStore launch takes 256 x 512 tiles.  They read a quarter fewer operand bytes a product, but
 // fill tensor memory, so that an epilogue has no product to run under, and there are half as many.  The
@@ -123,71 +112,6 @@ int launch_reduce(dd_ctx *ctx, const Splits &sp, cudaStream_t stream)
     cfg.numAttrs = 1;
     DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_reduce_kernel, sp.r));
     return DD_OK;
-}
-
-template <int EPI, int ACT>
-static int launch_stream_act(dd_ctx *ctx, const StreamArgs &a, unsigned grid, cudaStream_t stream)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(kStreamThreads);
-    cfg.dynamicSmemBytes = stream_smem_bytes(a.cols, a.stages);
-    cfg.stream = stream;
-    static std::atomic<bool> done[64];
-    const int rc = allow_smem(ctx, ffn_stream_kernel<EPI, ACT>, kStreamRing + 2048, done);
-    if (rc != DD_OK) return rc;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim = {(unsigned)a.cluster, 1, 1};
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_stream_kernel<EPI, ACT>, a));
-    return DD_OK;
-}
-
-// Shape and launch: the tokens in equal tiles of at most 128, K over as many CTAs as give every SM
-// one, each with two K blocks at least; x: the token matrices of the K segments.
-template <int EPI>
-static int launch_stream(dd_ctx *ctx, StreamArgs &a, std::initializer_list<Matrix> x, cudaStream_t stream)
-{
-    const unsigned rows = blocks_of(a.m, stream_features(EPI)), blocks = a.kblocks[0] + a.kblocks[1], sms = (unsigned)ctx->sm_count;
-    a.tiles_n = blocks_of(a.n, kStreamMaxCols);
-    const auto cluster = [&] {
-        unsigned s = 1;
-        while (s < kStreamMaxCluster && rows * a.tiles_n * s < sms && blocks >= 4 * s) s *= 2;
-        return s;
-    };
-    unsigned s = cluster();
-    while (rows * a.tiles_n * s < sms && a.n / a.tiles_n >= 64) {
-        a.tiles_n *= 2;
-        s = cluster();
-    }
-    a.cols = blocks_of(blocks_of(a.n, a.tiles_n), 16) * 16;
-    a.tiles_n = blocks_of(a.n, a.cols);
-    a.cluster = (int)s;
-    const unsigned stages = kStreamRing / stream_stage_bytes(a.cols);
-    a.stages = (int)(stages > kStreamMaxStages ? kStreamMaxStages : stages);
-    int i = 0;
-    for (const Matrix &m : x) {
-        const int rc = encode(ctx, &a.x[i++], m, a.cols);
-        if (rc != DD_OK) return rc;
-    }
-    const unsigned grid = rows * a.tiles_n * s;
-    return EPI != kEpiStore && a.e.activation == DD_ACT_GELU_TANH
-               ? launch_stream_act<EPI, EPI == kEpiStore ? DD_ACT_SILU : DD_ACT_GELU_TANH>(ctx, a, grid, stream)
-               : launch_stream_act<EPI, DD_ACT_SILU>(ctx, a, grid, stream);
-}
-
-static StreamArgs stream_args(const EpilogueArgs &e, uint64_t features, uint64_t tokens)
-{
-    StreamArgs a;
-    std::memset(&a, 0, sizeof a);
-    a.m = (unsigned)features;
-    a.n = (unsigned)tokens;
-    a.e = e;
-    return a;
 }
 
 // Context-owned scratch for callers that bring none.

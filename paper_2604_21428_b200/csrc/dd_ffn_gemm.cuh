@@ -51,6 +51,7 @@ struct EpilogueArgs {
     float *loss;                      // kEpiLoss
     float2 *partial;                  // [columns / 128][rows]: largest logit, sum of exp(z - largest)
     long long first, vocab;           // kEpiSoft: the piece's first column
+    unsigned tokens;                  // kEpiLoss: row length of `partial`
     int activation;
     int expire;                       // test hook: the first stage waits for 16 bytes that no copy brings
 };

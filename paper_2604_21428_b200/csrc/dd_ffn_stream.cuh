@@ -59,6 +59,8 @@ __device__ __forceinline__ void tmem_ld16(unsigned addr, unsigned (&r)[16])
 // What an epilogue reads for four features of a token, asked for before the sums are ready.
 struct Aux {
     uint2 a, b;                       // kEpiBack: gate, up; kEpiStore: residual
+    long long target;                 // kEpiLoss, kEpiSoft
+    float lse, dloss;                 // kEpiSoft
 };
 
 __device__ __forceinline__ uint2 load4_raw(const __nv_bfloat16 *p, unsigned live)
@@ -87,6 +89,12 @@ __device__ __forceinline__ Aux load_aux(const EpilogueArgs &a, unsigned t, unsig
     if (EPI == kEpiBack) {
         r.a = load4_raw(a.gate + (unsigned long long)t * a.ld_gate + c, live);
         r.b = load4_raw(a.up + (unsigned long long)t * a.ld_gate + c, live);
+    } else if (EPI == kEpiLoss || EPI == kEpiSoft) {
+        r.target = a.targets[t];
+        if (EPI == kEpiSoft) {
+            r.lse = a.lse[t];
+            r.dloss = a.dloss[t];
+        }
     } else if (EPI == kEpiStore && a.residual) {
         r.a = load4_raw(a.residual + (unsigned long long)t * a.ld_residual + c, live);
     }
@@ -123,6 +131,32 @@ __device__ __forceinline__ void finish4(const EpilogueArgs &a, unsigned t, unsig
         store4(a.dup + to, x, live);
         store4(a.dgate + to, g, live);
         store4(a.hidden + to, u, live);
+    } else if (EPI == kEpiLoss) {             // the warp's 128 logits of the token
+        constexpr float l = 1.4426950408889634f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i >= live) x[i] = -INFINITY;
+            else if (aux.target == (long long)c + i) a.loss[t] = x[i];
+        }
+        float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+#pragma unroll
+        for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float base = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += exp2_fast((x[i] - base) * l);
+#pragma unroll
+        for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (threadIdx.x % 32 == 0) a.partial[(unsigned long long)(c / 128) * a.tokens + t] = make_float2(top, sum);
+    } else if (EPI == kEpiSoft) {
+        constexpr float l = 1.4426950408889634f;
+        const bool some = aux.target >= 0 && aux.target < a.vocab;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float p = exp2_fast(fmaf(x[i], l, some ? -aux.lse * l : -INFINITY));
+            x[i] = (some && aux.target - a.first == (long long)c + i ? p - 1.0f : p) * (some ? aux.dloss : 0.0f);
+        }
+        store4(a.hidden + to, x, live);
     } else {
         float r[4];
         unpack4(aux.a, r);                // zeros without a residual
@@ -262,7 +296,7 @@ ffn_stream_kernel(const __grid_constant__ StreamArgs p)
         const unsigned owned = (cols + S - 1) / S, last = (rank + 1) * owned < cols ? (rank + 1) * owned : cols;
         const unsigned left = p.n > n0 + c ? p.n - n0 - c : 0, end = last < left ? last : left;      // tokens that exist
         unsigned j = rank * owned + threadIdx.x / kQuads;
-        const bool mine = warp < 4 && live;
+        const bool mine = warp < 4 && (live || EPI == kEpiLoss);              // (whose warps stay together)
         Aux aux[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b)

@@ -3,7 +3,7 @@
 #pragma once
 
 #include "dd_args.h"
-#include "dd_ffn_gemm.cuh"
+#include "dd_ffn_stream.cuh"
 
 namespace ddm {
 
@@ -76,7 +76,7 @@ inline unsigned choose_splits(const dd_ctx *ctx, unsigned tiles, unsigned blocks
 }
 
 // K blocks that a unit's epilogue takes as long as (256 x 256 outputs: 2.7 us): with fewer, the schedule counts these.
-// (One token, d 2048, 32000 columns of the vocabulary, whose gradient has one K block a tile: 224 us without, 111 with.)
+// (One token, d 2048, 32000 columns of the vocabulary, whose gradient has one K block a tile: the backward pass 224 us without, 111 with.)
 constexpr unsigned kEpilogueBlocks = 8;
 inline unsigned unit_blocks(unsigned blocks) { return blocks > kEpilogueBlocks ? blocks : kEpilogueBlocks; }
 
@@ -167,6 +167,83 @@ inline int set_stride(uint64_t &ld, uint64_t cols)
     if (ld >= kFfnMax) return DD_ERR_TOO_LARGE;
     return ld % 8 ? DD_ERR_ALIGNMENT : DD_OK;
 }
+
+// ---- few tokens ----------------------------------------------------------------------------
+
+// Up to here the weight-streaming kernel is ahead of the 256-row tiles of the pairs, forward with gate and up kept / backward:
+// 160 tokens, d 2048, f 8192 37 / 84 us (42 / 92), 300 tokens, 1024 x 4096 28 / 48 us (30 / 50); behind at 384 tokens, 2048 x 8192:
+// 66 / 120 us (64 / 116).
+constexpr unsigned long long kStreamMaxTokens = 320;
+
+// Ring of a CTA: two CTAs share an SM.
+constexpr unsigned kStreamRing = 96 * 1024;
+
+template <int EPI, int ACT>
+inline int launch_stream_act(dd_ctx *ctx, const StreamArgs &a, unsigned grid, cudaStream_t stream)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kStreamThreads);
+    cfg.dynamicSmemBytes = stream_smem_bytes(a.cols, a.stages);
+    cfg.stream = stream;
+    static std::atomic<bool> done[64];
+    const int rc = allow_smem(ctx, ffn_stream_kernel<EPI, ACT>, kStreamRing + 2048, done);
+    if (rc != DD_OK) return rc;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {(unsigned)a.cluster, 1, 1};
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    DD_CUDA(ctx, cudaLaunchKernelEx(&cfg, ffn_stream_kernel<EPI, ACT>, a));
+    return DD_OK;
+}
+
+// Shape and launch: the tokens in equal tiles of at most 128, K over as many CTAs as give every SM
+// one, each with two K blocks at least; x: the token matrices of the K segments.
+template <int EPI>
+inline int launch_stream(dd_ctx *ctx, StreamArgs &a, std::initializer_list<Matrix> x, cudaStream_t stream)
+{
+    const unsigned rows = blocks_of(a.m, stream_features(EPI)), blocks = a.kblocks[0] + a.kblocks[1], sms = (unsigned)ctx->sm_count;
+    a.tiles_n = blocks_of(a.n, kStreamMaxCols);
+    const auto cluster = [&] {
+        unsigned s = 1;
+        while (s < kStreamMaxCluster && rows * a.tiles_n * s < sms && blocks >= 4 * s) s *= 2;
+        return s;
+    };
+    unsigned s = cluster();
+    while (rows * a.tiles_n * s < sms && a.n / a.tiles_n >= 64) {
+        a.tiles_n *= 2;
+        s = cluster();
+    }
+    a.cols = blocks_of(blocks_of(a.n, a.tiles_n), 16) * 16;
+    a.tiles_n = blocks_of(a.n, a.cols);
+    a.cluster = (int)s;
+    const unsigned stages = kStreamRing / stream_stage_bytes(a.cols);
+    a.stages = (int)(stages > kStreamMaxStages ? kStreamMaxStages : stages);
+    int i = 0;
+    for (const Matrix &m : x) {
+        const int rc = encode(ctx, &a.x[i++], m, a.cols);
+        if (rc != DD_OK) return rc;
+    }
+    const unsigned grid = rows * a.tiles_n * s;
+    constexpr bool kActs = EPI == kEpiGate || EPI == kEpiBack;
+    return kActs && a.e.activation == DD_ACT_GELU_TANH ? launch_stream_act<EPI, kActs ? DD_ACT_GELU_TANH : DD_ACT_SILU>(ctx, a, grid, stream)
+                                                       : launch_stream_act<EPI, DD_ACT_SILU>(ctx, a, grid, stream);
+}
+
+inline StreamArgs stream_args(const EpilogueArgs &e, uint64_t features, uint64_t tokens)
+{
+    StreamArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.m = (unsigned)features;
+    a.n = (unsigned)tokens;
+    a.e = e;
+    return a;
+}
+
+// ---- many tokens ----------------------------------------------------------------------------
 
 // Launches of kEpiStore problems, in tiles of 256 or 512 columns, and of what adds their splits up (dd_ffn.cu).
 int launch_store(dd_ctx *ctx, GemmArgs &a, cudaStream_t stream);

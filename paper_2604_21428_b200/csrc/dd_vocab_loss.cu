@@ -3,7 +3,10 @@
 // piece of the vocabulary: the logits once more, as their gradient in bf16; then the products of that with the
 // weight and with the hidden rows, side by side.
 //
-// Bound by the products: 2 T d V of them forward, 6 T d V backward beside 2 T d V for the logits again.
+// Bound by the products, 2 T d V of them forward, 6 T d V backward beside 2 T d V for the logits again: 8192 tokens,
+// d 2048, 32000 columns 773 us forward in short runs and 875 sustained under the 1000 W cap (1390 and 1230 TFLOP/s), 2610 and
+// 2825 us backward (1650 and 1520 TFLOP/s with the logits).  With few tokens by the weights' bytes, read once forward; backward
+// reads them twice and writes as many (4 tokens: 29 and 97 us, of which the bytes need 20 and 40).
 #include <cmath>
 
 #include "dd_decoder.h"
@@ -64,6 +67,13 @@ vocab_loss_join_kernel(const float2 *partial, unsigned parts, unsigned tokens, c
 // d 231, 8075 columns: 17 us for the second launch with 8 splits, 12 with more).
 constexpr unsigned kLossSplits = 32;
 
+// Up to here the logits (forward), and with them dhidden (backward), are made by the kernel that streams weights past few
+// tokens; it reads the weights at 4.5 TB/s where the products' kernel reads them at 3.3, but its epilogues take longer
+// for each token.  us, this / the other kernel: d 2048, 32000 columns, 4 / 32 / 64 tokens forward 29 / 33 / 38 (41 / 37 / 38),
+// d 768 15 / 19 / 23 (21 / 21 / 24); backward with 4 / 64 / 96 tokens, d 2048 97 / 103 / 111 (108 / 110 / 111), d 512, 5000
+// columns 15 / 17 / 19 (21 / 25 / 25), d 768, 32000 columns 48 / 56 / 63 (51 / 57 / 56).
+constexpr uint64_t kLossFewForward = 48, kLossFewBackward = 80;
+
 static uint64_t rows8(uint64_t n) { return (n + 7) / 8 * 8; }
 
 // Columns of the vocabulary whose gradients are held at one time: as many as make 128 MB, so that what the
@@ -103,6 +113,16 @@ static int launch_logits(dd_ctx *ctx, GemmArgs &a, uint64_t tokens, uint64_t col
     GemmProblem &p = add_problem(a, tokens, columns, 256, blocks_of(d, kBK));
     p.b_map[0] = 1;
     return launch_gemm_act<EPI, 256, DD_ACT_SILU>(ctx, a, stream);
+}
+
+// The same for few tokens, by the kernel that streams the weights past them.
+template <int EPI>
+static int launch_few_logits(dd_ctx *ctx, const EpilogueArgs &e, const Matrix &hidden, const Matrix &weight, cudaStream_t stream)
+{
+    StreamArgs a = stream_args(e, weight.rows, hidden.rows);
+    a.kblocks[0] = blocks_of(weight.cols, kBK);
+    const int rc = encode(ctx, &a.w[0], weight);
+    return rc == DD_OK ? launch_stream<EPI>(ctx, a, {hidden}, stream) : rc;
 }
 
 static EpilogueArgs loss_epilogue(const dd_vocab_loss &l, int32_t *status)
@@ -162,9 +182,15 @@ extern "C" int dd_vocab_loss_forward(dd_ctx *ctx, const dd_vocab_loss *l_, const
     a.e = loss_epilogue(l, status);
     a.e.loss = loss;
     a.e.partial = static_cast<float2 *>(scratch);
-    rc = encode(ctx, &a.maps[0], {hidden, T, l.d, l.ld_hidden});
-    if (rc == DD_OK) rc = encode(ctx, &a.maps[1], {l.weight, l.vocab, l.d, l.ld_weight});
-    if (rc == DD_OK) rc = launch_logits<kEpiLoss>(ctx, a, T, l.vocab, l.d, stream);
+    a.e.tokens = (unsigned)T;
+    const Matrix h = {hidden, T, l.d, l.ld_hidden}, w = {l.weight, l.vocab, l.d, l.ld_weight};
+    if (T <= kLossFewForward) {
+        rc = launch_few_logits<kEpiLoss>(ctx, a.e, h, w, stream);
+    } else {
+        rc = encode(ctx, &a.maps[0], h);
+        if (rc == DD_OK) rc = encode(ctx, &a.maps[1], w);
+        if (rc == DD_OK) rc = launch_logits<kEpiLoss>(ctx, a, T, l.vocab, l.d, stream);
+    }
     if (rc != DD_OK) return rc;
     return launch_after(ctx, vocab_loss_join_kernel, blocks_of(T, 32), 32 * kJoinWarps, 0, stream, a.e.partial, blocks_of(l.vocab, 128), (unsigned)T, a.e.targets,
                         a.e.vocab, loss, lse);
@@ -210,6 +236,7 @@ extern "C" int dd_vocab_loss_backward(dd_ctx *ctx, const dd_vocab_loss *l_, cons
     a.e.hidden = g;
     a.e.ld_hidden = ldg;
     const unsigned kt = blocks_of(T, kBK), pairs = (unsigned)ctx->sm_count / 2;
+    const bool few = T <= kLossFewBackward && cols == l.vocab;
     for (uint64_t first = 0; first < l.vocab; first += cols) {
         const uint64_t n = l.vocab - first < cols ? l.vocab - first : cols;
         const bool last = first + n == l.vocab;
@@ -218,19 +245,33 @@ extern "C" int dd_vocab_loss_backward(dd_ctx *ctx, const dd_vocab_loss *l_, cons
         rc = encode(ctx, &a.maps[0], {hidden, T, l.d, l.ld_hidden});
         if (rc == DD_OK) rc = encode(ctx, &a.maps[1], w);
         if (rc == DD_OK) rc = encode(ctx, &a.maps[2], {g, T, n, ldg});
-        if (rc == DD_OK) rc = launch_logits<kEpiSoft>(ctx, a, T, n, l.d, stream);
+        if (rc == DD_OK && few) {
+            rc = launch_few_logits<kEpiSoft>(ctx, a.e, {hidden, T, l.d, l.ld_hidden}, w, stream);
+            // dhidden by the same kernel; dweight beside it, as in the block's backward pass
+            StreamArgs c = stream_args(a.e, l.d, T);
+            c.e.out = static_cast<__nv_bfloat16 *>(dhidden);
+            c.e.ld_out = l.ld_hidden;
+            c.kblocks[0] = blocks_of(n, kBK);
+            c.w[0] = a.maps[1];
+            c.w_mn = c.own_prior = c.late_trigger = a.late_wait = 1;
+            if (rc == DD_OK) rc = launch_stream<kEpiStore>(ctx, c, {{g, T, n, ldg}}, stream);
+        } else if (rc == DD_OK) {
+            rc = launch_logits<kEpiSoft>(ctx, a, T, n, l.d, stream);
+        }
         if (rc != DD_OK) return rc;
         a.nprob = 0;
         a.tiles = 0;
         Splits sp;
         sp.r.count = 0;
         const unsigned wtiles = blocks_of(n, 2 * kBM) * blocks_of(l.d, 256), xtiles = blocks_of(T, 2 * kBM) * blocks_of(l.d, 256), kn = blocks_of(n, kBK);
-        GemmProblem &x = add_problem(a, T, l.d, 256, kn, 0, choose_splits(ctx, xtiles, kn, (unsigned long long)wtiles * unit_blocks(kt), kLossSplits));
-        x.a_map[0] = 2;
-        x.b_map[0] = 1;
-        x.b_mn = 1;
-        if (last) set_output(ctx, x, sp, dhidden, l.ld_hidden, false, first ? sums : nullptr, ldd, true);
-        else set_output(ctx, x, sp, sums, ldd, true, first ? sums : nullptr, ldd, true);
+        if (!few) {
+            GemmProblem &x = add_problem(a, T, l.d, 256, kn, 0, choose_splits(ctx, xtiles, kn, (unsigned long long)wtiles * unit_blocks(kt), kLossSplits));
+            x.a_map[0] = 2;
+            x.b_map[0] = 1;
+            x.b_mn = 1;
+            if (last) set_output(ctx, x, sp, dhidden, l.ld_hidden, false, first ? sums : nullptr, ldd, true);
+            else set_output(ctx, x, sp, sums, ldd, true, first ? sums : nullptr, ldd, true);
+        }
         // few weights and many tokens: the tokens are split as well, as in the block's backward pass
         unsigned splits = 1;
         while (splits < kMaxSplits && a.tiles + wtiles * (splits + 1) <= pairs && kt >= 4 * (splits + 1)) ++splits;
