@@ -122,7 +122,7 @@ static AttnArgs attention_args(const dd_attention &b, unsigned rows, const Plan 
     return a;
 }
 
-static HeadsOut out_of(const dd_heads &x) { return {static_cast<__nv_bfloat16 *>(x.data), x.ld_token, x.ld_head}; }
+static HeadRows rows_of(const dd_heads &x) { return {static_cast<__nv_bfloat16 *>(x.data), x.ld_token, x.ld_head}; }
 
 }  // namespace ddm
 
@@ -169,7 +169,7 @@ extern "C" int dd_attention_forward(dd_ctx *ctx, const dd_attention *attention, 
     rc = encode_heads(ctx, &a.q, q, T, b.heads, b.dim);
     if (rc == DD_OK) rc = encode_heads(ctx, &a.k, k, T, b.kv_heads, b.dim);
     if (rc == DD_OK) rc = encode_heads(ctx, &a.v, v, T, b.kv_heads, b.dim);
-    a.o = out_of(o);
+    a.o = rows_of(o);
     a.lse = lse;
     if (rc == DD_OK && plan) rc = launch_after(ctx, attention_plan_kernel, 1, kPlanThreads, 0, stream, plan_args(b, 2 * kTile, plan, status));
     if (rc != DD_OK) return rc;
@@ -217,13 +217,13 @@ extern "C" int dd_attention_backward(dd_ctx *ctx, const dd_attention *attention,
     if (rc == DD_OK) rc = encode_heads(ctx, &a.v, v, T, b.kv_heads, b.dim);
     if (rc == DD_OK) rc = encode_heads(ctx, &a.d_o, d_o, T, b.heads, b.dim);
     if (rc != DD_OK) return rc;
-    a.q_rows = out_of(q);
-    a.k_rows = out_of(k);
-    a.v_rows = out_of(v);
-    a.do_rows = out_of(d_o);
-    a.dq = out_of(dq);
-    a.dk = out_of(dk);
-    a.dv = out_of(dv);
+    a.q_rows = rows_of(q);
+    a.k_rows = rows_of(k);
+    a.v_rows = rows_of(v);
+    a.do_rows = rows_of(d_o);
+    a.dq = rows_of(dq);
+    a.dk = rows_of(dk);
+    a.dv = rows_of(dv);
     a.lse = const_cast<float *>(lse);
     a.delta = delta;
     const DeltaArgs d = {static_cast<const __nv_bfloat16 *>(o.data), static_cast<const __nv_bfloat16 *>(d_o.data), o.ld_token, o.ld_head,

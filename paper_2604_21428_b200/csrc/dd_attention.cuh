@@ -4,10 +4,10 @@
 // Roles of a CTA: warps 0-7 (backward 0-15) compute on tiles (a thread owns a row of an accumulator, the lane of
 // tensor memory that it can reach, or some columns of it).  Of the four warps behind them one (a lane) has the TMA
 // engine fill rings of operand tiles, one (a lane) issues the products, one zeroes rows past a sequence's end, and
-// all give registers to the others (a warpgroup does so as a whole).  An operand tile is 128 tokens of one head: one or two boxes of 64 elements a row
-// (128-byte swizzle), columns past `dim` filled with zeros by the TMA engine.  Tiles may reach past their
-// sequence: scores there are masked, and rows that a product sums over are zeroed in shared memory
-// first, since a weight of 0 does not silence a NaN of the neighbour's.
+// all give registers to the others (a warpgroup does so as a whole).  An operand tile is 128 tokens of one head:
+// one or two boxes of 64 elements a row (128-byte swizzle), columns past `dim` filled with zeros by the TMA
+// engine.  Tiles may reach past their sequence: scores there are masked, and rows that a product sums over are
+// zeroed in shared memory first, since a weight of 0 does not silence a NaN of the neighbour's.
 //
 // The weights p (and ds) go back into tensor memory as bf16 and are the A operand of the next product from
 // there, so they never pass through shared memory.
@@ -37,7 +37,7 @@ struct Plan {
     PlanItem item[1];
 };
 
-struct HeadsOut {
+struct HeadRows {
     __nv_bfloat16 *data;
     unsigned long long ld_token, ld_head;
 };
@@ -50,8 +50,8 @@ struct AttnArgs {
     float scale;
     int causal, expire;
     unsigned cluster;                             // CTAs that share a tile of keys in the last kernel
-    HeadsOut o, dq, dk, dv;
-    HeadsOut q_rows, k_rows, v_rows, do_rows;     // inputs once more, for operands that are kept in tensor memory
+    HeadRows o, dq, dk, dv;
+    HeadRows q_rows, k_rows, v_rows, do_rows;     // inputs once more, for operands that are kept in tensor memory
     float *lse;                                   // [heads][tokens]
     float *delta;                                 // [heads][tokens]: sum_j p_ij dp_ij
     int *status;
@@ -63,18 +63,6 @@ __device__ __forceinline__ void tma_load_heads(unsigned dst, const CUtensorMap *
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  :: "r"(dst), "l"(map), "r"(x), "r"(head), "r"(token), "r"(bar) : "memory");
-}
-
-__device__ __forceinline__ void tmem_st32(unsigned addr, const unsigned (&r)[32])
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
-        :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-           "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-           "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-           "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
-        : "memory");
 }
 
 __device__ __forceinline__ void tmem_st16(unsigned addr, const unsigned (&r)[16])
@@ -107,11 +95,11 @@ __device__ __forceinline__ void arrive_bar(unsigned bar)
 }
 
 // Descriptors of operand tiles: the upper half is the same for all (128-byte swizzle, groups of 8 rows every
-// 1024 bytes), the lower half is the address and, where rows are K, the step to the next 64 columns (in a cluster an address has the
-// CTA's rank in its upper bits, which do not belong there).  They are
-// kept as halves, and everything they are made of is warp-uniform, because the products are fed from uniform
-// registers: with 64-bit descriptors put together for each product from per-lane values, issuing one took 115 cycles
-// and not the 64 that it runs for.
+// 1024 bytes), the lower half is the address and, where rows are K, the step to the next 64 columns (in a cluster
+// an address has the CTA's rank in its upper bits, which do not belong there).  They are kept as halves, and
+// everything they are made of is warp-uniform, because the products are fed from uniform registers: with 64-bit
+// descriptors put together for each product from per-lane values, issuing one took 115 cycles and not the 64 that
+// it runs for.
 constexpr unsigned kDescUpper = (1024 / 16) | (1u << 14) | (2u << 29);
 
 // K contiguous: step k covers elements 16 k .. of every row.
@@ -350,6 +338,10 @@ __device__ __forceinline__ void warp_arrive(unsigned bar, int lane)
 
 // A CTA takes 256 query rows of a head: tile 0 and tile 1 of 128, warps 0-3 and 4-7.  They share every tile
 // of keys and values, and while the weights of one are computed the products of the other run.
+// For 128 columns a tile's two products and its exponentials both take 1024 cycles of their units, so the kernel is bound
+// by both and by the steps between them: each is busy for 60 % of the time (8192 tokens, 8 heads of 128, causal).
+// 16384 tokens: 420-430 us, 1290 TFLOP/s of products, on a cool GPU, 490 in a long run, where the power limit
+// takes the clock to 1.5 GHz; 16 computing warps took 517, two issuing threads the same as one.
 __host__ __device__ constexpr int fwd_stages(int dp) { return dp == 128 ? 4 : 6; }
 __host__ __device__ constexpr unsigned fwd_smem_bytes(int dp) { return 1024 + (2 + fwd_stages(dp)) * kTile * dp * 2; }
 
@@ -439,15 +431,13 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                     ok = gemm_wait(p_full + 8 * t, j & 1, abort);
                     if (!ok) break;
                     tc_fence_after();
-                    {
-                        mma_weights<DP, 16>(kO + t * DP, kS + t * kTile, tile_of(2 * j + 1), j != 0);
-                        if (j + 1 < mine) {
-                            // behind the product that reads the weights, whose place the scores take
-                            mma_rows<DP>(kS + t * kTile, smem + t * kBytes, tile_of(2 * j + 2));
-                            umma_commit(s_full + 8 * t);
-                        } else {
-                            umma_commit(o_full + 8 * t);
-                        }
+                    mma_weights<DP, 16>(kO + t * DP, kS + t * kTile, tile_of(2 * j + 1), j != 0);
+                    if (j + 1 < mine) {
+                        // behind the product that reads the weights, whose place the scores take
+                        mma_rows<DP>(kS + t * kTile, smem + t * kBytes, tile_of(2 * j + 2));
+                        umma_commit(s_full + 8 * t);
+                    } else {
+                        umma_commit(o_full + 8 * t);
                     }
                 }
                 if (ok) {
@@ -455,10 +445,8 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                     if (j + 1 < n) umma_commit(empty + 8 * ((2 * j + 2) % kStages));
                 }
             }
-            {
-                umma_commit(drain);                                          // no product may be in flight when tensor memory is freed
-                mbar_wait_bounded(drain, 0);
-            }
+            umma_commit(drain);                                              // no product may be in flight when tensor memory is freed
+            mbar_wait_bounded(drain, 0);
         } else if (warp == kFwdWarps + 2 && item.len - (n - 1) * kTile < kTile) {
             // the last tile of values reports here and not to the issuer
             if (warp_wait(tail, 0, abort))
@@ -555,15 +543,6 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
 
 // ---- backward --------------------------------------------------------------------------------------
 
-// dq of 128 query rows of a head.  Every four warps take 32 columns of the scores' rows.  Scores of the
-// next tile of keys are made as soon as those of this one are in registers.
-// Two launches (this and the next kernel) form the scores twice, which costs 7 products of a tile instead of 5,
-// but no gradient is added to by several CTAs: no atomics, no float32 copy of dq in memory.
-//
-// delta_i = sum_j p_ij dp_ij is d_o_i . o_i, but o's rounding to bf16 is then in it, and where few keys share a row's
-// weight dp - delta is a small difference.  So rows whose keys are all in one tile, the short sequences and the
-// beginnings of long ones, take the sum itself and leave it for the next launch (two keys: gradients within
-// 0.25 % instead of 0.75 %).
 // The pairs whose weights are polynomials, three of eight: all weights of a tile are wanted at one time, and the
 // special function unit makes 16 a clock and SM (8192 tokens, 16 heads of 64: 636 -> 604 us, of 128 0.6 % less; in
 // the forward pass, whose two tiles take turns, the same costs 3-7 %).
@@ -577,6 +556,19 @@ struct BwdShared {
 constexpr unsigned bwd_smem_bytes(int dp) { return 7 * kTile * dp * 2 + sizeof(BwdShared); }
 static_assert(bwd_smem_bytes(128) <= 227 * 1024, "shared memory of an SM");
 
+// dq of 128 query rows of a head.  Every four warps take 32 columns of the scores' rows.  Scores of the
+// next tile of keys are made as soon as those of this one are in registers.
+// Two launches (this and the next kernel) form the scores twice, which costs 7 products of a tile instead of 5,
+// but no gradient is added to by several CTAs: no atomics, no float32 copy of dq in memory.
+//
+// delta_i = sum_j p_ij dp_ij is d_o_i . o_i, but o's rounding to bf16 is then in it, and where few keys share a row's
+// weight dp - delta is a small difference.  So rows whose keys are all in one tile, the short sequences and the
+// beginnings of long ones, take the sum itself and leave it for the next launch (two keys: gradients within
+// 0.25 % instead of 0.75 %).
+//
+// Bound, like the next kernel, by the products (512 cycles each of a pair of tiles: 3 here, 4 there, 59-61 % of the
+// time) and by the steps from one to the next.  8192 tokens, 8 heads of 128, causal: 190 and 240 us at 1.5 GHz; 16384
+// tokens: 1455-1475 us with delta, 1310 TFLOP/s of executed products.
 template <int DP>
 __global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dq_kernel(const __grid_constant__ AttnArgs a)
@@ -640,21 +632,17 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
                 if (!gemm_wait(k_full + 8 * (j % 3), j / 3 & 1, abort)) return false;
                 if (item.len - j * kTile < kTile && !gemm_wait(clean, 0, abort)) return false;
                 tc_fence_after();
-                {
-                    mma_held<DP>(kS, kQ, sk + j % 3 * kBytes);
-                    umma_commit(s_full);
-                }
+                mma_held<DP>(kS, kQ, sk + j % 3 * kBytes);
+                umma_commit(s_full);
                 return true;
             };
             const auto weights = [&](unsigned j) {                           // dp of tile j
                 if (!gemm_wait(v_full + 8 * (j % 3), j / 3 & 1, abort)) return false;
                 tc_fence_after();
-                {
-                    if (kHeld) mma_held<DP>(kP, kDo, sv + j % 3 * kBytes);
-                    else mma_rows<DP>(kP, sdo, sv + j % 3 * kBytes);
-                    umma_commit(dp_full);
-                    umma_commit(v_empty + 8 * (j % 3));
-                }
+                if (kHeld) mma_held<DP>(kP, kDo, sv + j % 3 * kBytes);
+                else mma_rows<DP>(kP, sdo, sv + j % 3 * kBytes);
+                umma_commit(dp_full);
+                umma_commit(v_empty + 8 * (j % 3));
                 return true;
             };
             bool ok = gemm_wait(q_full, 0, abort) && (kHeld || gemm_wait(do_full, 0, abort)), more = true;
@@ -667,16 +655,12 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
                 if (ok && more) ok = weights(j);
                 if (!ok || !j) continue;
                 tc_fence_after();
-                {
-                    mma_weights<DP, 16>(kDq, kDs, sk + (j - 1) % 3 * kBytes, j != 1);
-                    umma_commit(k_empty + 8 * ((j - 1) % 3));
-                    umma_commit(dq_full);
-                }
+                mma_weights<DP, 16>(kDq, kDs, sk + (j - 1) % 3 * kBytes, j != 1);
+                umma_commit(k_empty + 8 * ((j - 1) % 3));
+                umma_commit(dq_full);
             }
-            {
-                umma_commit(drain);
-                mbar_wait_bounded(drain, 0);
-            }
+            umma_commit(drain);
+            mbar_wait_bounded(drain, 0);
         } else if (warp == kBwdWarps + 2 && item.len - (n - 1) * kTile < kTile) {
             // the last tile of keys, which dq sums over, reports here and not to the issuer
             if (warp_wait(tail, 0, abort))
@@ -856,11 +840,9 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                     tails ^= 1u << bit;
                 }
                 tc_fence_after();
-                {
-                    if (kHeld) mma_held<DP>(second ? kP : kS, second ? kV : kK, t);
-                    else mma_rows<DP>(second ? kP : kS, second ? sv : sk, t);
-                    umma_commit(second ? dp_full : s_full);
-                }
+                if (kHeld) mma_held<DP>(second ? kP : kS, second ? kV : kK, t);
+                else mma_rows<DP>(second ? kP : kS, second ? sv : sk, t);
+                umma_commit(second ? dp_full : s_full);
                 return true;
             };
             bool ok = gemm_wait(kv_full, 0, abort), more = n > 0;
@@ -872,28 +854,22 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                     ok = gemm_wait(p_full, i & 1, abort);
                     if (!ok) break;
                     tc_fence_after();
-                    {
-                        mma_weights<DP, 32>(kDv, kS, sdo + (i & 1) * kBytes, i != 0);
-                        umma_commit(do_empty + 8 * (i & 1));
-                    }
+                    mma_weights<DP, 32>(kDv, kS, sdo + (i & 1) * kBytes, i != 0);
+                    umma_commit(do_empty + 8 * (i & 1));
                 }
                 if (more) ok = product(j, false);
                 if (ok && j) {
                     ok = gemm_wait(ds_full, i & 1, abort);
                     if (!ok) break;
                     tc_fence_after();
-                    {
-                        mma_weights<DP, 32>(kDk, kP, sq + i % 3 * kBytes, i != 0);
-                        umma_commit(q_empty + 8 * (i % 3));
-                    }
+                    mma_weights<DP, 32>(kDk, kP, sq + i % 3 * kBytes, i != 0);
+                    umma_commit(q_empty + 8 * (i % 3));
                 }
                 if (ok && more) ok = product(j, true);
             }
-            {
-                if (ok) umma_commit(done);
-                umma_commit(drain);
-                mbar_wait_bounded(drain, 0);
-            }
+            if (ok) umma_commit(done);
+            umma_commit(drain);
+            mbar_wait_bounded(drain, 0);
         } else if (warp == kBwdWarps + 2 && last < kTile) {
             // the last tiles report here and not to the issuer
             unsigned tails = 0;
@@ -995,7 +971,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
         if (ok) {
             tc_fence_after();
             const bool key = share >= 2;
-            const HeadsOut &out = key ? a.dk : a.dv;
+            const HeadRows &out = key ? a.dk : a.dv;
             __nv_bfloat16 *o = out.data + (unsigned long long)(item.start + row) * out.ld_token + hk * out.ld_head;
 #pragma unroll
             for (int i = 0; i < DP / 64; ++i) {
@@ -1033,7 +1009,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
                     if (other < a.cluster) x.x += y[other].x, x.y += y[other].y, x.z += y[other].z, x.w += y[other].w;
                 const bool key = col >= DP;
                 const unsigned c4 = key ? col - DP : col;
-                const HeadsOut &out = key ? a.dk : a.dv;
+                const HeadRows &out = key ? a.dk : a.dv;
                 const float by = key ? a.scale : 1.0f;
                 if (row0 + r < item.len && c4 < a.dim)
                     *reinterpret_cast<uint2 *>(out.data + (unsigned long long)(item.start + row0 + r) * out.ld_token + hk * out.ld_head + c4) =

@@ -2,6 +2,8 @@
 //
 // Bound by memory: every element is read and written once, and a block forms the angles of its few tokens
 // once for all heads (float64 product and reduction to a part of a turn, float32 sine and cosine of that).
+// 16384 tokens, 20 heads of 128, bf16: 31 us, 5.4 TB/s.  Loads issued before the angles took 45 us (fewer blocks
+// an SM), blocks of 2048 to 8192 units 34-55.
 #include <cmath>
 
 #include "dd_args.h"
