@@ -6,7 +6,7 @@
 // Bound by the products, 2 T d V of them forward, 6 T d V backward beside 2 T d V for the logits again: 8192 tokens,
 // d 2048, 32000 columns 773 us forward in short runs and 875 sustained under the 1000 W cap (1390 and 1230 TFLOP/s), 2610 and
 // 2825 us backward (1650 and 1520 TFLOP/s with the logits).  With few tokens by the weights' bytes, read once forward; backward
-// reads them twice and writes as many (4 tokens: 29 and 97 us, of which the bytes need 20 and 40).
+// reads them twice and writes as many (4 tokens: 27 and 97 us, of which the bytes need 20 and 40).
 #include <cmath>
 
 #include "dd_decoder.h"
@@ -68,11 +68,19 @@ vocab_loss_join_kernel(const float2 *partial, unsigned parts, unsigned tokens, c
 constexpr unsigned kLossSplits = 32;
 
 // Up to here the logits (forward), and with them dhidden (backward), are made by the kernel that streams weights past few
-// tokens; it reads the weights at 4.5 TB/s where the products' kernel reads them at 3.3, but its epilogues take longer
-// for each token.  us, this / the other kernel: d 2048, 32000 columns, 4 / 32 / 64 tokens forward 29 / 33 / 38 (41 / 37 / 38),
-// d 768 15 / 19 / 23 (21 / 21 / 24); backward with 4 / 64 / 96 tokens, d 2048 97 / 103 / 111 (108 / 110 / 111), d 512, 5000
-// columns 15 / 17 / 19 (21 / 25 / 25), d 768, 32000 columns 48 / 56 / 63 (51 / 57 / 56).
-constexpr uint64_t kLossFewForward = 48, kLossFewBackward = 80;
+// tokens; it reads the weights at 4.5 TB/s where the products' kernel reads them at 3.3, but reads the tokens for every
+// 128 columns and finishes a tile after its products, which costs most where a cluster shares the tile's K: forward
+// it goes as far as a tile of tokens where the columns' tiles give every SM one without that.  us from a cold L2, this / the
+// other kernel: forward, 4 / 32 / 64 / 128 tokens, d 2048, 32000 columns 39 / 41 / 41 / 45 (49 / 45 / 46 / 47), d 768 22.5 / 24 /
+// 25 / 28 (27 / 28 / 31 / 29), 192 tokens 37 (29); clusters, d 512, 5000 columns 14.4 / 16.4 / 18.4 / 22.5 (16.4 all).  From a
+// warm L2, backward with 4 / 64 / 96 tokens, d 2048, 32000 columns 97 / 103 / 111 (108 / 110 / 111), d 512, 5000 columns 15 / 17 /
+// 19 (21 / 25 / 25), d 768, 32000 columns 48 / 56 / 63 (51 / 57 / 56).
+constexpr uint64_t kLossFewForward = 32, kLossFewBackward = 80;
+
+static bool few_forward(const dd_ctx *ctx, const dd_vocab_loss &l)
+{
+    return l.tokens <= (blocks_of(l.vocab, kBM) >= (unsigned)ctx->sm_count ? kStreamMaxCols : kLossFewForward);
+}
 
 static uint64_t rows8(uint64_t n) { return (n + 7) / 8 * 8; }
 
@@ -184,7 +192,7 @@ extern "C" int dd_vocab_loss_forward(dd_ctx *ctx, const dd_vocab_loss *l_, const
     a.e.partial = static_cast<float2 *>(scratch);
     a.e.tokens = (unsigned)T;
     const Matrix h = {hidden, T, l.d, l.ld_hidden}, w = {l.weight, l.vocab, l.d, l.ld_weight};
-    if (T <= kLossFewForward) {
+    if (few_forward(ctx, l)) {
         rc = launch_few_logits<kEpiLoss>(ctx, a.e, h, w, stream);
     } else {
         rc = encode(ctx, &a.maps[0], h);

@@ -75,6 +75,29 @@ def test_against_float64(ctx, size):
         assert pads_untouched(dweight) and pads_untouched(c.dhidden)
 
 
+@pytest.mark.parametrize("T", [2, 17, 32, 95, 96, 128, 129])
+@pytest.mark.parametrize("large", [False, True])
+def test_few_tokens_and_many_columns(ctx, T, large):
+    """Enough columns for a tile of them on every SM: targets in the first, a middle and the last, cut tile and of
+    no column, logits up to a few hundred as well, a NaN token beside the others; the same bits twice."""
+    c = Case(T, 200, 19001, seed=T, std=1.0 if large else None)
+    c.targets[0], c.targets[-1], c.targets[T // 2] = 0, 19000, 18944
+    c.targets[T // 3] = -2 ** 63 if T > 16 else c.targets[T // 3]
+    nan = T // 4 if T > 16 else -1
+    if nan >= 0:
+        c.hidden[nan, 7] = NAN
+    c.forward(ctx)
+    (loss, e_loss), (lse, e_lse), _ = loss64(c.hidden, c.weight, c.targets)
+    rows = [t for t in range(T) if t != nan]
+    within(c.loss[rows], loss[rows], e_loss[rows], "loss")
+    within(c.lse[rows], lse[rows], e_lse[rows], "lse")
+    assert nan < 0 or bool(c.lse[nan].isnan())
+    first = torch.stack([c.loss, c.lse]).clone()
+    c.loss.fill_(5.0), c.lse.fill_(5.0)
+    c.forward(ctx)
+    assert torch.equal(first.view(torch.int32), torch.stack([c.loss, c.lse]).view(torch.int32))
+
+
 def test_pieces_of_the_vocabulary(ctx):
     """More columns than are held at one time: dhidden is summed over the pieces, the last one of odd width."""
     c = Case(12000, 72, 12345, seed=3)
