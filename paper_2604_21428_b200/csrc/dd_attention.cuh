@@ -342,8 +342,55 @@ __device__ __forceinline__ void warp_arrive(unsigned bar, int lane)
 // by both and by the steps between them: each is busy for 60 % of the time (8192 tokens, 8 heads of 128, causal).
 // 16384 tokens: 420-430 us, 1290 TFLOP/s of products, on a cool GPU, 490 in a long run, where the power limit
 // takes the clock to 1.5 GHz; 16 computing warps took 517, two issuing threads the same as one.
+// A CTA that has issued its last copy takes the place of one that has not been launched yet (the hardware hands them out,
+// most work first), so that the next queries and keys arrive, and their scores are made, while the last rows are written.
+// 16384 tokens, 16 heads on 4 of 128, documents of 128 / 256 / 1024 / 4096 tokens: 84 -> 58, 83 -> 66, 112 -> 94, 253 -> 238 us.
 __host__ __device__ constexpr int fwd_stages(int dp) { return dp == 128 ? 4 : 6; }
 __host__ __device__ constexpr unsigned fwd_smem_bytes(int dp) { return 1024 + (2 + fwd_stages(dp)) * kTile * dp * 2; }
+
+// 256 rows of a head and the tiles of keys that each half needs.
+struct FwdWork {
+    unsigned start, len, head, row0, n0, n1, n;
+    bool cut;                                     // the last tile of values goes past the sequence's end
+};
+
+__device__ __forceinline__ FwdWork fwd_work(const AttnArgs &a, const PlanItem &item)
+{
+    FwdWork w;
+    w.start = item.start;
+    w.len = item.len;
+    w.head = item.pad;
+    w.row0 = item.tile * 2 * kTile;
+    const unsigned all = (item.len + kTile - 1) / kTile, t0 = item.tile * 2;
+    w.n0 = a.causal ? t0 + 1 : all;
+    w.n1 = item.len - w.row0 <= kTile ? 0 : a.causal ? t0 + 2 : all;
+    w.n = w.n0 > w.n1 ? w.n0 : w.n1;
+    w.cut = item.len - (w.n - 1) * kTile < kTile;
+    return w;
+}
+
+// The block that a launch would have started next, which then does not start; ~0: none.  Not to be asked again after that.
+__device__ __forceinline__ unsigned take_block(unsigned reply, unsigned bar, unsigned parity, volatile int *abort)
+{
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    mbar_arrive_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" :: "r"(reply), "r"(bar) : "memory");
+    if (!mbar_wait_bounded(bar, parity)) {
+        *abort = 1;
+        return ~0u;
+    }
+    unsigned block = ~0u;
+    asm volatile("{\n .reg .b128 r;\n .reg .pred p;\n .reg .b32 y, z, w;\n ld.shared.b128 r, [%1];\n"
+                 " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n"
+                 " @p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, y, z, w}, r;\n}" : "+r"(block) : "r"(reply) : "memory");
+    return block;
+}
+
+struct FwdShared {
+    AttnShared sh;
+    alignas(16) uint4 reply;
+    PlanItem item[2];                             // what comes after the item of every other turn; no length: nothing
+};
 
 template <int DP>
 __global__ void __launch_bounds__(32 * (kFwdWarps + 4), 1)
@@ -352,10 +399,13 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
     constexpr int kStages = fwd_stages(DP);
     constexpr unsigned kBytes = kTile * DP * 2;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ alignas(16) AttnShared sh;
+    __shared__ FwdShared rest;
+    AttnShared &sh = rest.sh;
     const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u, ring = smem + 2 * kBytes;
     const unsigned bar = smem_addr(sh.bars), q_full = bar, full = bar + 8, empty = full + 8 * kStages, s_full = empty + 8 * kStages,
-                   p_full = s_full + 16, o_full = p_full + 16, drain = o_full + 16, clean = drain + 8, tail = clean + 8;
+                   p_full = s_full + 16, o_full = p_full + 16, drain = o_full + 16, clean = drain + 8, tail = clean + 16,
+                   q_empty = tail + 16, next_full = q_empty + 8, next_empty = next_full + 16, reply_full = next_empty + 16;
+    static_assert(sizeof sh.bars >= 8 * (2 * kStages + 16), "barriers");
     volatile int *abort = &sh.abort_flag;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -369,10 +419,14 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
             init_bar(s_full + 8 * s, 1);
             init_bar(p_full + 8 * s, 4);
             init_bar(o_full + 8 * s, 1);
+            init_bar(clean + 8 * s, 1);
+            init_bar(tail + 8 * s, 1);
+            init_bar(next_full + 8 * s, 1);
+            init_bar(next_empty + 8 * s, kFwdWarps + 2);
         }
         init_bar(drain, 1);
-        init_bar(clean, 1);
-        init_bar(tail, 1);
+        init_bar(q_empty, 1);
+        init_bar(reply_full, 1);
     }
     const unsigned tmem = attn_begin<kFwdWarps>(sh, a, warp);
     // all so far without waiting for the launch before
@@ -382,161 +436,217 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
         attn_end<kFwdWarps>(sh, a, warp, tmem);
         return;
     }
-    const unsigned head = blockIdx.x % a.heads, row0 = item.tile * 2 * kTile;
-    const unsigned rows = item.len - row0;                                  // from row0 on
-    // tiles of keys that each of the two needs
-    const unsigned all = (item.len + kTile - 1) / kTile, t0 = item.tile * 2;
-    const unsigned n0 = a.causal ? t0 + 1 : all, n1 = rows <= kTile ? 0 : a.causal ? t0 + 2 : all;
-    const unsigned n = n0 > n1 ? n0 : n1;
+    item.pad = blockIdx.x % a.heads;
     const unsigned kS = tmem, kO = tmem + 2 * kTile;                         // scores of tile t at kS + 128 t, sums at kO + DP t
+    // what follows turn k: whether there is anything
+    const auto next = [&](unsigned k) {
+        if (!gemm_wait(next_full + 8 * (k & 1), k >> 1 & 1, abort)) return false;
+        item = rest.item[k & 1];
+        return true;
+    };
+    const auto warp_next = [&](unsigned k) {
+        if (!__all_sync(0xffffffffu, next(k))) return false;
+        __syncwarp();
+        if (lane == 0) arrive_bar(next_empty + 8 * (k & 1));
+        return item.len != 0;
+    };
 
     if (warp >= kFwdWarps) {
         fewer_registers<kFwdWarps>();
         if (warp == kFwdWarps && elect_one()) {
-            const int token = (int)(item.start + row0), hk = (int)(head / a.group);
-            mbar_arrive_expect_tx(q_full, (n1 ? 2 : 1) * kBytes + (a.expire ? 16u : 0u));
-            load_tile<DP>(smem, &a.q, (int)head, token, q_full);
-            if (n1) load_tile<DP>(smem + kBytes, &a.q, (int)head, token + kTile, q_full);
-            unsigned it = 0;                                                 // keys 0, values 0, keys 1, ...
-            for (; it < 2 * n; ++it) {
-                const unsigned s = it % kStages;
-                if ((it >= kStages && !gemm_wait(empty + 8 * s, (it / kStages - 1) & 1, abort)) || *abort) break;
-                const bool cut = it == 2 * n - 1 && item.len - (n - 1) * kTile < kTile;
-                if (cut) arrive_bar(full + 8 * s);
-                mbar_arrive_expect_tx(cut ? tail : full + 8 * s, kBytes);
-                load_tile<DP>(ring + s * kBytes, it & 1 ? &a.v : &a.k, hk, (int)(item.start + (it >> 1) * kTile), cut ? tail : full + 8 * s);
-                if (cut) mbar_wait_bounded(tail, 0);
+            unsigned it = 0, k = 0, cuts = 0;                                // keys 0, values 0, keys 1, ...; turns; cut tiles
+            for (;; ++k) {
+                const FwdWork w = fwd_work(a, item);
+                const int token = (int)(w.start + w.row0), hk = (int)(w.head / a.group);
+                if (k && !gemm_wait(q_empty, (k - 1) & 1, abort)) break;
+                mbar_arrive_expect_tx(q_full, (w.n1 ? 2 : 1) * kBytes + (a.expire && k == 0 ? 16u : 0u));
+                load_tile<DP>(smem, &a.q, (int)w.head, token, q_full);
+                if (w.n1) load_tile<DP>(smem + kBytes, &a.q, (int)w.head, token + kTile, q_full);
+                unsigned i = 0;
+                for (; i < 2 * w.n; ++i, ++it) {
+                    const unsigned s = it % kStages;
+                    if ((it >= kStages && !gemm_wait(empty + 8 * s, (it / kStages - 1) & 1, abort)) || *abort) break;
+                    const bool cut = i == 2 * w.n - 1 && w.cut;
+                    if (cut) arrive_bar(full + 8 * s);
+                    // two such tiles at most are under way: the third one's queries wait for the first one's products
+                    const unsigned to = cut ? tail + 8 * (cuts++ & 1) : full + 8 * s;
+                    mbar_arrive_expect_tx(to, kBytes);
+                    load_tile<DP>(ring + s * kBytes, i & 1 ? &a.v : &a.k, hk, (int)(w.start + (i >> 1) * kTile), to);
+                }
+                if (i < 2 * w.n || (k >= 2 && !gemm_wait(next_empty + 8 * (k & 1), (k >> 1) - 1 & 1, abort))) {
+                    ++k;
+                    break;
+                }
+                const unsigned block = take_block(smem_addr(&rest.reply), reply_full, k & 1, abort);
+                item.len = 0;
+                if (block != ~0u && plan_item(a, block / a.heads, item)) item.pad = block % a.heads;
+                else item.len = 0;
+                rest.item[k & 1] = item;
+                arrive_bar(next_full + 8 * (k & 1));
+                if (!item.len) {
+                    ++k;
+                    break;
+                }
             }
-            mbar_wait_bounded(q_full, 0);
+            mbar_wait_bounded(q_full, (k - 1) & 1);
             for (unsigned j = it > kStages ? it - kStages : 0; j < it; ++j) mbar_wait_bounded(full + 8 * (j % kStages), (j / kStages) & 1);
+            for (unsigned j = cuts > 2 ? cuts - 2 : 0; j < cuts; ++j) mbar_wait_bounded(tail + 8 * (j & 1), j >> 1 & 1);
         } else if (warp == kFwdWarps + 1 && elect_one()) {
             const auto tile_of = [&](unsigned it) { return ring + it % kStages * kBytes; };
             const auto ready = [&](unsigned it) { return gemm_wait(full + 8 * (it % kStages), (it / kStages) & 1, abort); };
-            bool ok = gemm_wait(q_full, 0, abort) && ready(0);
-            if (ok) {
-                mma_rows<DP>(kS, smem, tile_of(0));
-                umma_commit(s_full);
-                if (n1) {
-                    mma_rows<DP>(kS + kTile, smem + kBytes, tile_of(0));
-                    umma_commit(s_full + 8);
-                }
-                umma_commit(empty);
-            }
-            for (unsigned j = 0; ok && j < n; ++j) {
-                ok = ready(2 * j + 1) && (item.len - j * kTile >= kTile || gemm_wait(clean, 0, abort)) && (j + 1 == n || ready(2 * j + 2));
-#pragma unroll 1
-                for (unsigned t = 0; ok && t < 2; ++t) {
-                    const unsigned mine = t ? n1 : n0;
-                    if (j >= mine) continue;
-                    ok = gemm_wait(p_full + 8 * t, j & 1, abort);
-                    if (!ok) break;
+            unsigned it = 0, cuts = 0, past0 = 0, past1 = 0;                 // tiles, cut ones, and those of each half, before this turn
+            bool ok = true;
+            for (unsigned k = 0; ok; ++k) {
+                const FwdWork w = fwd_work(a, item);
+                ok = gemm_wait(q_full, k & 1, abort) && ready(it);
+                if (ok) {
                     tc_fence_after();
-                    mma_weights<DP, 16>(kO + t * DP, kS + t * kTile, tile_of(2 * j + 1), j != 0);
-                    if (j + 1 < mine) {
-                        // behind the product that reads the weights, whose place the scores take
-                        mma_rows<DP>(kS + t * kTile, smem + t * kBytes, tile_of(2 * j + 2));
-                        umma_commit(s_full + 8 * t);
-                    } else {
-                        umma_commit(o_full + 8 * t);
+                    mma_rows<DP>(kS, smem, tile_of(it));
+                    umma_commit(s_full);
+                    if (w.n1) {
+                        mma_rows<DP>(kS + kTile, smem + kBytes, tile_of(it));
+                        umma_commit(s_full + 8);
+                    }
+                    umma_commit(empty + 8 * (it % kStages));
+                    if (w.n == 1) umma_commit(q_empty);
+                }
+                for (unsigned j = 0; ok && j < w.n; ++j) {
+                    const bool last = j + 1 == w.n;
+                    ok = ready(it + 2 * j + 1) && (!last || !w.cut || gemm_wait(clean + 8 * (cuts & 1), cuts >> 1 & 1, abort)) && (last || ready(it + 2 * j + 2));
+#pragma unroll 1
+                    for (unsigned t = 0; ok && t < 2; ++t) {
+                        const unsigned mine = t ? w.n1 : w.n0;
+                        if (j >= mine) continue;
+                        ok = gemm_wait(p_full + 8 * t, (t ? past1 : past0) + j & 1, abort);
+                        if (!ok) break;
+                        tc_fence_after();
+                        mma_weights<DP, 16>(kO + t * DP, kS + t * kTile, tile_of(it + 2 * j + 1), j != 0);
+                        if (j + 1 < mine) {
+                            // behind the product that reads the weights, whose place the scores take
+                            mma_rows<DP>(kS + t * kTile, smem + t * kBytes, tile_of(it + 2 * j + 2));
+                            umma_commit(s_full + 8 * t);
+                        } else {
+                            umma_commit(o_full + 8 * t);
+                        }
+                    }
+                    if (ok) {
+                        umma_commit(empty + 8 * ((it + 2 * j + 1) % kStages));
+                        if (!last) umma_commit(empty + 8 * ((it + 2 * j + 2) % kStages));
+                        if (j + 2 == w.n) umma_commit(q_empty);
                     }
                 }
-                if (ok) {
-                    umma_commit(empty + 8 * ((2 * j + 1) % kStages));
-                    if (j + 1 < n) umma_commit(empty + 8 * ((2 * j + 2) % kStages));
-                }
+                it += 2 * w.n;
+                past0 += w.n0;
+                past1 += w.n1;
+                cuts += w.cut;
+                ok = ok && next(k);
+                if (!ok || !item.len) break;
+                arrive_bar(next_empty + 8 * (k & 1));
             }
             umma_commit(drain);                                              // no product may be in flight when tensor memory is freed
             mbar_wait_bounded(drain, 0);
-        } else if (warp == kFwdWarps + 2 && item.len - (n - 1) * kTile < kTile) {
+        } else if (warp == kFwdWarps + 2) {
             // the last tile of values reports here and not to the issuer
-            if (warp_wait(tail, 0, abort))
-                zero_rows<DP>(ring + (2 * n - 1) % kStages * kBytes, item.len - (n - 1) * kTile, lane, clean);
+            unsigned it = 0, cuts = 0, k = 0;
+            do {
+                const FwdWork w = fwd_work(a, item);
+                it += 2 * w.n;
+                if (!w.cut) continue;
+                if (!warp_wait(tail + 8 * (cuts & 1), cuts >> 1 & 1, abort)) break;
+                zero_rows<DP>(ring + (it - 1) % kStages * kBytes, w.len - (w.n - 1) * kTile, lane, clean + 8 * (cuts & 1));
+                ++cuts;
+            } while (warp_next(k++));
         }
     } else {
         more_registers<kFwdWarps>();
         const int t = warp >> 2;
-        const unsigned mine = t ? n1 : n0, local = (warp & 3) * 32 + lane, row = row0 + t * kTile + local;
         const unsigned at = (unsigned)((warp & 3) * 32) << 16, s_at = kS + t * kTile + at, o_at = kO + t * DP + at;
         const float c = a.scale * kLog2e;
-        float top = -INFINITY, base = 0.0f, sum = 0.0f;                      // base: top, as the exponents use it
+        unsigned past = 0, outs = 0, k = 0;                                  // tiles and turns with any before this turn
         bool ok = true;
-        for (unsigned j = 0; j < mine; ++j) {
-            ok = warp_wait(s_full + 8 * t, j & 1, abort);
-            if (!ok) break;
-            tc_fence_after();
-            unsigned r[4][32];
+        do {
+            const FwdWork w = fwd_work(a, item);
+            const unsigned mine = t ? w.n1 : w.n0, row = w.row0 + t * kTile + (warp & 3) * 32 + lane;
+            float top = -INFINITY, base = 0.0f, sum = 0.0f;                  // base: top, as the exponents use it
+            for (unsigned j = 0; j < mine; ++j) {
+                ok = warp_wait(s_full + 8 * t, past + j & 1, abort);
+                if (!ok) break;
+                tc_fence_after();
+                unsigned r[4][32];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32 * i, r[i]);
-            tmem_ld_wait();
-            const unsigned end = a.causal && row + 1 < item.len ? row + 1 : item.len, live = end > j * kTile ? end - j * kTile : 0;
-            if (__any_sync(0xffffffffu, live < kTile)) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (32 * i + k >= live) r[i][k] = 0xff800000u;        // -infinity
-            }
-            float m[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                m[i] = max3(__uint_as_float(r[i][0]), __uint_as_float(r[i][1]), i ? -INFINITY : top);
-#pragma unroll
-                for (int k = 2; k < 32; k += 2) m[i] = max3(m[i], __uint_as_float(r[i][k]), __uint_as_float(r[i][k + 1]));
-            }
-            const float now = max3(m[0], m[1], max3(m[2], m[3], -INFINITY));
-            // A row's sums are moved to a larger maximum only when it has grown by more than 2^8: until then the
-            // weights stay below 2^8, exact in float32 and as far from the end of bf16's range.
-            const bool grown = !((now - top) * c <= 8.0f);
-            if (__any_sync(0xffffffffu, grown)) {
-                const float next = !grown ? base : now == -INFINITY ? 0.0f : now;
-                if (j) {
-                    const float by = grown && top != -INFINITY ? exp2_fast((base - next) * c) : 1.0f;      // (sums of nothing are 0)
-                    sum *= by;
-#pragma unroll 1
-                    for (int i = 0; i < DP / 16; ++i) {
-                        unsigned o[16];
-                        tmem_ld16(o_at + 16 * i, o);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
-                        tmem_st16(o_at + 16 * i, o);
-                    }
-                }
-                top = grown ? now : top;
-                base = next;
-            }
-            const float off = -base * c;
-            float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                unsigned w[16];
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const float2 p = exp2_pair(r[h][2 * k], r[h][2 * k + 1], c, make_float2(off, off));
-                    part[k & 1] = __fadd2_rn(part[k & 1], p);
-                    w[k] = pack2(p.x, p.y);
-                }
-                tmem_st16(s_at + 16 * h, w);
-            }
-            sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
-            tmem_st_wait();
-            warp_arrive(p_full + 8 * t, lane);
-        }
-        if (mine && ok) ok = warp_wait(o_full + 8 * t, 0, abort);
-        if (mine && ok) {
-            tc_fence_after();
-            const unsigned long long token = item.start + row;
-            const float by = 1.0f / sum;
-            __nv_bfloat16 *o = a.o.data + token * a.o.ld_token + head * a.o.ld_head;
-#pragma unroll
-            for (int i = 0; i < DP / 32; ++i) {
-                unsigned w[32];
-                tmem_ld32(o_at + 32 * i, w);
+                for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32 * i, r[i]);
                 tmem_ld_wait();
-                if (row < item.len) store_row32(o, 32 * i, a.dim, w, by);
+                const unsigned end = a.causal && row + 1 < w.len ? row + 1 : w.len, live = end > j * kTile ? end - j * kTile : 0;
+                if (__any_sync(0xffffffffu, live < kTile)) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (32 * i + k >= live) r[i][k] = 0xff800000u;        // -infinity
+                }
+                float m[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    m[i] = max3(__uint_as_float(r[i][0]), __uint_as_float(r[i][1]), i ? -INFINITY : top);
+#pragma unroll
+                    for (int k = 2; k < 32; k += 2) m[i] = max3(m[i], __uint_as_float(r[i][k]), __uint_as_float(r[i][k + 1]));
+                }
+                const float now = max3(m[0], m[1], max3(m[2], m[3], -INFINITY));
+                // A row's sums are moved to a larger maximum only when it has grown by more than 2^8: until then the
+                // weights stay below 2^8, exact in float32 and as far from the end of bf16's range.
+                const bool grown = !((now - top) * c <= 8.0f);
+                if (__any_sync(0xffffffffu, grown)) {
+                    const float next = !grown ? base : now == -INFINITY ? 0.0f : now;
+                    if (j) {
+                        const float by = grown && top != -INFINITY ? exp2_fast((base - next) * c) : 1.0f;      // (sums of nothing are 0)
+                        sum *= by;
+#pragma unroll 1
+                        for (int i = 0; i < DP / 16; ++i) {
+                            unsigned o[16];
+                            tmem_ld16(o_at + 16 * i, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * by);
+                            tmem_st16(o_at + 16 * i, o);
+                        }
+                    }
+                    top = grown ? now : top;
+                    base = next;
+                }
+                const float off = -base * c;
+                float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    unsigned u[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const float2 p = exp2_pair(r[h][2 * k], r[h][2 * k + 1], c, make_float2(off, off));
+                        part[k & 1] = __fadd2_rn(part[k & 1], p);
+                        u[k] = pack2(p.x, p.y);
+                    }
+                    tmem_st16(s_at + 16 * h, u);
+                }
+                sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
+                tmem_st_wait();
+                warp_arrive(p_full + 8 * t, lane);
             }
-            if (a.lse && row < item.len) a.lse[(unsigned long long)head * a.tokens + token] = fmaf(base, a.scale, logf(sum));
-        }
+            if (mine && ok) ok = warp_wait(o_full + 8 * t, outs++ & 1, abort);
+            if (mine && ok) {
+                tc_fence_after();
+                const unsigned long long token = w.start + row;
+                const float by = 1.0f / sum;
+                __nv_bfloat16 *o = a.o.data + token * a.o.ld_token + w.head * a.o.ld_head;
+#pragma unroll
+                for (int i = 0; i < DP / 32; ++i) {
+                    unsigned u[32];
+                    tmem_ld32(o_at + 32 * i, u);
+                    tmem_ld_wait();
+                    if (row < w.len) store_row32(o, 32 * i, a.dim, u, by);
+                }
+                if (a.lse && row < w.len) a.lse[(unsigned long long)w.head * a.tokens + token] = fmaf(base, a.scale, logf(sum));
+            }
+            past += mine;
+        } while (ok && warp_next(k++));
     }
     attn_end<kFwdWarps>(sh, a, warp, tmem);
 }

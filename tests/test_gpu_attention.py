@@ -92,6 +92,33 @@ def test_against_float64(ctx, shape, causal):
     c.check_back(causal)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_more_tiles_than_the_gpu_takes_at_once(ctx, dim, causal):
+    """Documents of whole and cut tiles, of one tile of queries and of more, in turn; every third one is NaN throughout, its
+    neighbours are not; the same bits twice."""
+    lengths = [(37 * i) % 300 for i in range(45)] + [640, 128, 256, 1, 700, 384, 128, 128, 255]
+    c = Case(lengths, 16, 4, dim, seed=dim, before=2, after=3)
+    for d in c.docs[1::3]:
+        c.q[d], c.k[d], c.v[d], c.d_o[d] = NAN, NAN, NAN, NAN
+    bad = torch.zeros_like(c.inside)
+    for d in c.docs[1::3]:
+        bad[d] = True
+    c.forward(ctx, causal=causal)
+    c.backward(ctx, causal=causal)
+    first = [t.clone().view(torch.int16) for t in (c.o, c.dq, c.dk, c.dv)]
+    for t in (c.o, c.dq, c.dk, c.dv):
+        t[c.inside] = 7.0
+    c.forward(ctx, causal=causal)
+    c.backward(ctx, causal=causal)
+    good = c.inside & ~bad
+    assert all(torch.equal(a[good], b.view(torch.int16)[good]) for a, b in zip(first, (c.o, c.dq, c.dk, c.dv)))
+    assert bool(c.o[bad].isnan().all())
+    c.docs = [d for i, d in enumerate(c.docs) if i % 3 != 1]
+    c.check(causal)
+    c.check_back(causal)
+
+
 @pytest.mark.parametrize("std", [4.0, 12.0])
 def test_sharp_rows(ctx, std):
     """Scores of hundreds: most weights vanish, and the maximum grows from tile to tile."""
