@@ -277,7 +277,7 @@ __device__ __forceinline__ bool plan_item(const AttnArgs &a, unsigned i, PlanIte
 
 // What all kernels begin and end with.
 struct AttnShared {
-    unsigned long long bars[28];
+    unsigned long long bars[29];
     int abort_flag;
     unsigned tmem_base;
 };
@@ -887,6 +887,7 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
         init_bar(p_full, kBwdWarps);
         init_bar(ds_full, kBwdWarps);
         init_bar(st_full, 8);
+        init_bar(st_full + 8, 8);
     }
     const unsigned tmem = attn_begin<kBwdWarps>(sh, a, warp);
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -1024,14 +1025,16 @@ attention_dkv_kernel(const __grid_constant__ AttnArgs a)
             if (share < 2) {
                 stats[j & 1][share][threadIdx.x & 127] = next;
                 __syncwarp();
-                if (lane == 0) arrive_bar(st_full);
+                if (lane == 0) arrive_bar(st_full + 8 * (j & 1));
                 if (j + 1 < n) next = stat(j + 1);
             }
             const unsigned q0 = tile_of(j) * kTile + 32 * share;          // the first of this warp's 32 queries
             // queries from `from` to `to` count
             const unsigned to = item.len > q0 ? item.len - q0 : 0, from = a.causal && row > q0 ? row - q0 : 0;
             const bool masked = __any_sync(0xffffffffu, to < 32 || from > 0) || (a.causal && q0 == 0);
-            ok = gemm_wait(st_full, j & 1, abort) && gemm_wait(s_full, j & 1, abort);
+            // (every other tile's statistics have a barrier of their own: with one, those of tile j + 1 could all be there
+            // before a late warp has seen that those of tile j are, and it would wait for tile j + 2's)
+            ok = gemm_wait(st_full + 8 * (j & 1), j >> 1 & 1, abort) && gemm_wait(s_full, j & 1, abort);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();

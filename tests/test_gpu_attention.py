@@ -205,6 +205,22 @@ def test_same_bits_every_time(ctx):
         assert all(torch.equal(a, b) for a, b in zip(results[0], r))
 
 
+@pytest.mark.parametrize("lengths", [[1024] * 16, [4096] * 4, [2900, 17, 1, 1333, 0, 640, 2048, 999, 129, 65]], ids=str)
+def test_no_wait_runs_out_in_many_calls(ctx, lengths):
+    """A warp that is late may not miss a barrier's turn: many tiles, many times, without a status and with the same bits."""
+    c = Case(lengths, 16, 4, 128)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    first = None
+    for _ in range(40):
+        for t in (c.o, c.dq, c.dk, c.dv):
+            t.fill_(7.0)
+        c.forward(ctx, status=status)
+        c.backward(ctx, status=status)
+        got = torch.cat([t.reshape(-1).view(torch.int16) for t in (c.o.clone(), c.dq.clone(), c.dk.clone(), c.dv.clone())])
+        first = got if first is None else first
+        assert torch.equal(first, got) and int(status) == 0
+
+
 def test_captured_calls_take_new_lengths(dd, ctx):
     """Forward and backward in a graph with scratch of their own, on a stream of its own: replayed with other
     offsets, they give what eager calls give."""
