@@ -277,7 +277,7 @@ __device__ __forceinline__ bool plan_item(const AttnArgs &a, unsigned i, PlanIte
 
 // What all kernels begin and end with.
 struct AttnShared {
-    unsigned long long bars[29];
+    unsigned long long bars[31];
     int abort_flag;
     unsigned tmem_base;
 };
@@ -334,6 +334,63 @@ __device__ __forceinline__ void warp_arrive(unsigned bar, int lane)
     if (lane == 0) arrive_bar(bar);
 }
 
+// ---- turns -----------------------------------------------------------------------------------------
+
+// Forward and in dq's kernel, a CTA that has issued the last copy of a block's work takes the place of a block that has not been
+// launched yet (the hardware hands them out, most work first): the next operands arrive while the last rows are
+// written, and a CTA's own beginning is paid once.
+
+// The block that a launch would have started next, which then does not start; ~0: none.  Not to be asked again after that.
+__device__ __forceinline__ unsigned take_block(unsigned reply, unsigned bar, unsigned parity, volatile int *abort)
+{
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    mbar_arrive_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" :: "r"(reply), "r"(bar) : "memory");
+    if (!mbar_wait_bounded(bar, parity)) {
+        *abort = 1;
+        return ~0u;
+    }
+    unsigned block = ~0u;
+    asm volatile("{\n .reg .b128 r;\n .reg .pred p;\n .reg .b32 y, z, w;\n ld.shared.b128 r, [%1];\n"
+                 " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n"
+                 " @p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, y, z, w}, r;\n}" : "+r"(block) : "r"(reply) : "memory");
+    return block;
+}
+
+// What comes after every other turn, as the copies' role found it; no length: nothing.
+struct Turns {
+    uint4 reply;
+    PlanItem item[2];
+};
+
+// After turn k: the next block's item, its head in `pad`, for all roles; without length if there is none.
+__device__ __forceinline__ PlanItem publish_next(Turns &turns, const AttnArgs &a, unsigned k, unsigned reply_full, unsigned next_full, volatile int *abort)
+{
+    const unsigned block = take_block(smem_addr(&turns.reply), reply_full, k & 1, abort);
+    PlanItem item{0u, 0u, 0u, 0u};
+    if (block != ~0u && plan_item(a, block / a.heads, item)) item.pad = block % a.heads;
+    else item.len = 0;
+    turns.item[k & 1] = item;
+    arrive_bar(next_full + 8 * (k & 1));
+    return item;
+}
+
+__device__ __forceinline__ bool read_next(const Turns &turns, unsigned k, unsigned next_full, PlanItem &item, volatile int *abort)
+{
+    if (!gemm_wait(next_full + 8 * (k & 1), k >> 1 & 1, abort)) return false;
+    item = turns.item[k & 1];
+    return true;
+}
+
+// The same by a whole warp, which reports that it has read: whether there is anything.
+__device__ __forceinline__ bool warp_next(const Turns &turns, unsigned k, unsigned next_full, unsigned next_empty, PlanItem &item, int lane, volatile int *abort)
+{
+    if (!__all_sync(0xffffffffu, read_next(turns, k, next_full, item, abort))) return false;
+    __syncwarp();
+    if (lane == 0) arrive_bar(next_empty + 8 * (k & 1));
+    return item.len != 0;
+}
+
 // ---- forward ---------------------------------------------------------------------------------------
 
 // A CTA takes 256 query rows of a head: tile 0 and tile 1 of 128, warps 0-3 and 4-7.  They share every tile
@@ -342,9 +399,7 @@ __device__ __forceinline__ void warp_arrive(unsigned bar, int lane)
 // by both and by the steps between them: each is busy for 60 % of the time (8192 tokens, 8 heads of 128, causal).
 // 16384 tokens: 420-430 us, 1290 TFLOP/s of products, on a cool GPU, 490 in a long run, where the power limit
 // takes the clock to 1.5 GHz; 16 computing warps took 517, two issuing threads the same as one.
-// A CTA that has issued its last copy takes the place of one that has not been launched yet (the hardware hands them out,
-// most work first), so that the next queries and keys arrive, and their scores are made, while the last rows are written.
-// 16384 tokens, 16 heads on 4 of 128, documents of 128 / 256 / 1024 / 4096 tokens: 84 -> 58, 83 -> 66, 112 -> 94, 253 -> 238 us.
+// Taking turns: 16384 tokens, 16 heads on 4 of 128, documents of 128 / 256 / 1024 / 4096 tokens: 84 -> 58, 83 -> 66, 112 -> 94, 253 -> 238 us.
 __host__ __device__ constexpr int fwd_stages(int dp) { return dp == 128 ? 4 : 6; }
 __host__ __device__ constexpr unsigned fwd_smem_bytes(int dp) { return 1024 + (2 + fwd_stages(dp)) * kTile * dp * 2; }
 
@@ -369,29 +424,6 @@ __device__ __forceinline__ FwdWork fwd_work(const AttnArgs &a, const PlanItem &i
     return w;
 }
 
-// The block that a launch would have started next, which then does not start; ~0: none.  Not to be asked again after that.
-__device__ __forceinline__ unsigned take_block(unsigned reply, unsigned bar, unsigned parity, volatile int *abort)
-{
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    mbar_arrive_expect_tx(bar, 16);
-    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" :: "r"(reply), "r"(bar) : "memory");
-    if (!mbar_wait_bounded(bar, parity)) {
-        *abort = 1;
-        return ~0u;
-    }
-    unsigned block = ~0u;
-    asm volatile("{\n .reg .b128 r;\n .reg .pred p;\n .reg .b32 y, z, w;\n ld.shared.b128 r, [%1];\n"
-                 " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n"
-                 " @p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, y, z, w}, r;\n}" : "+r"(block) : "r"(reply) : "memory");
-    return block;
-}
-
-struct FwdShared {
-    AttnShared sh;
-    alignas(16) uint4 reply;
-    PlanItem item[2];                             // what comes after the item of every other turn; no length: nothing
-};
-
 template <int DP>
 __global__ void __launch_bounds__(32 * (kFwdWarps + 4), 1)
 attention_forward_kernel(const __grid_constant__ AttnArgs a)
@@ -399,8 +431,8 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
     constexpr int kStages = fwd_stages(DP);
     constexpr unsigned kBytes = kTile * DP * 2;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ FwdShared rest;
-    AttnShared &sh = rest.sh;
+    __shared__ alignas(16) AttnShared sh;
+    __shared__ alignas(16) Turns turns;
     const unsigned smem = (smem_addr(smem_raw) + 1023u) & ~1023u, ring = smem + 2 * kBytes;
     const unsigned bar = smem_addr(sh.bars), q_full = bar, full = bar + 8, empty = full + 8 * kStages, s_full = empty + 8 * kStages,
                    p_full = s_full + 16, o_full = p_full + 16, drain = o_full + 16, clean = drain + 8, tail = clean + 16,
@@ -438,19 +470,6 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
     }
     item.pad = blockIdx.x % a.heads;
     const unsigned kS = tmem, kO = tmem + 2 * kTile;                         // scores of tile t at kS + 128 t, sums at kO + DP t
-    // what follows turn k: whether there is anything
-    const auto next = [&](unsigned k) {
-        if (!gemm_wait(next_full + 8 * (k & 1), k >> 1 & 1, abort)) return false;
-        item = rest.item[k & 1];
-        return true;
-    };
-    const auto warp_next = [&](unsigned k) {
-        if (!__all_sync(0xffffffffu, next(k))) return false;
-        __syncwarp();
-        if (lane == 0) arrive_bar(next_empty + 8 * (k & 1));
-        return item.len != 0;
-    };
-
     if (warp >= kFwdWarps) {
         fewer_registers<kFwdWarps>();
         if (warp == kFwdWarps && elect_one()) {
@@ -477,12 +496,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                     ++k;
                     break;
                 }
-                const unsigned block = take_block(smem_addr(&rest.reply), reply_full, k & 1, abort);
-                item.len = 0;
-                if (block != ~0u && plan_item(a, block / a.heads, item)) item.pad = block % a.heads;
-                else item.len = 0;
-                rest.item[k & 1] = item;
-                arrive_bar(next_full + 8 * (k & 1));
+                item = publish_next(turns, a, k, reply_full, next_full, abort);
                 if (!item.len) {
                     ++k;
                     break;
@@ -539,7 +553,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                 past0 += w.n0;
                 past1 += w.n1;
                 cuts += w.cut;
-                ok = ok && next(k);
+                ok = ok && read_next(turns, k, next_full, item, abort);
                 if (!ok || !item.len) break;
                 arrive_bar(next_empty + 8 * (k & 1));
             }
@@ -555,7 +569,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                 if (!warp_wait(tail + 8 * (cuts & 1), cuts >> 1 & 1, abort)) break;
                 zero_rows<DP>(ring + (it - 1) % kStages * kBytes, w.len - (w.n - 1) * kTile, lane, clean + 8 * (cuts & 1));
                 ++cuts;
-            } while (warp_next(k++));
+            } while (warp_next(turns, k++, next_full, next_empty, item, lane, abort));
         }
     } else {
         more_registers<kFwdWarps>();
@@ -646,7 +660,7 @@ attention_forward_kernel(const __grid_constant__ AttnArgs a)
                 if (a.lse && row < w.len) a.lse[(unsigned long long)w.head * a.tokens + token] = fmaf(base, a.scale, logf(sum));
             }
             past += mine;
-        } while (ok && warp_next(k++));
+        } while (ok && warp_next(turns, k++, next_full, next_empty, item, lane, abort));
     }
     attn_end<kFwdWarps>(sh, a, warp, tmem);
 }
@@ -662,9 +676,22 @@ __host__ __device__ constexpr bool poly_pair(int k) { return 0x4a >> (k % 8) & 1
 struct BwdShared {
     AttnShared sh;
     alignas(16) float row[4][kTile];
+    Turns turns;
 };
 constexpr unsigned bwd_smem_bytes(int dp) { return 7 * kTile * dp * 2 + sizeof(BwdShared); }
 static_assert(bwd_smem_bytes(128) <= 227 * 1024, "shared memory of an SM");
+
+// 128 rows of a head.
+struct DqWork {
+    unsigned start, len, head, row0, n;
+    bool cut;                                     // the last tile of keys goes past the sequence's end
+};
+
+__device__ __forceinline__ DqWork dq_work(const AttnArgs &a, const PlanItem &item)
+{
+    const unsigned n = a.causal ? item.tile + 1 : (item.len + kTile - 1) / kTile;
+    return {item.start, item.len, item.pad, item.tile * kTile, n, item.len - (n - 1) * kTile < kTile};
+}
 
 // dq of 128 query rows of a head.  Every four warps take 32 columns of the scores' rows.  Scores of the
 // next tile of keys are made as soon as those of this one are in registers.
@@ -693,13 +720,17 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
     const unsigned smem = smem_addr(smem_tiles), sdo = smem, sk = smem + kBytes, sv = smem + 4 * kBytes;
     const unsigned bar = smem_addr(sh.bars), k_full = bar, k_empty = bar + 24, v_full = bar + 48, v_empty = bar + 72, do_full = bar + 96,
                    s_full = bar + 104, dp_full = bar + 112, dq_full = bar + 120, drain = bar + 128, clean = bar + 136, tail = bar + 144,
-                   q_full = bar + 152, s_read = bar + 160, ds_full = bar + 168, sum_full = bar + 176;
+                   q_full = bar + 152, s_read = bar + 160, ds_full = bar + 168, sum_full = bar + 176,
+                   next_full = bar + 184, next_empty = bar + 200, reply_full = bar + 216, turned = bar + 224, clean2 = bar + 232, tail2 = bar + 240;
+    const auto clean_of = [&](unsigned c) { return c & 1 ? clean2 : clean; };
+    const auto tail_of = [&](unsigned c) { return c & 1 ? tail2 : tail; };
     volatile int *abort = &sh.abort_flag;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         for (int i = 0; i < 19; ++i) init_bar(bar + 8 * i, 1);
         for (int i = 19; i < 23; ++i) init_bar(bar + 8 * i, kBwdWarps);
+        for (int i = 23; i < 31; ++i) init_bar(bar + 8 * i, i == 25 || i == 26 ? kBwdWarps + 2 : 1);
     }
     const unsigned tmem = attn_begin<kBwdWarps>(sh, a, warp);
     // all so far without waiting for the launch before
@@ -709,148 +740,191 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
         attn_end<kBwdWarps>(sh, a, warp, tmem);
         return;
     }
-    const unsigned head = blockIdx.x % a.heads, row0 = item.tile * kTile, all = (item.len + kTile - 1) / kTile;
-    const unsigned n = a.causal ? item.tile + 1 : all;
+    item.pad = blockIdx.x % a.heads;
     // the queries, and with 64 columns their gradients' operand d_o as well, are held in tensor memory
     const unsigned kS = tmem, kP = tmem + kTile, kDs = tmem + 2 * kTile, kDq = kDs + 64, kQ = tmem + 448, kDo = tmem + 384;
 
     if (warp >= kBwdWarps) {
         fewer_registers<kBwdWarps>();
         if (warp == kBwdWarps && elect_one()) {
-            const int hk = (int)(head / a.group);
-            if (!kHeld) {
-                mbar_arrive_expect_tx(do_full, kBytes);
-                load_tile<DP>(sdo, &a.d_o, (int)head, (int)(item.start + row0), do_full);
+            unsigned it = 0, k = 0, cuts = 0;                                // keys 0, values 0, keys 1, ...; turns; cut tiles
+            for (;; ++k) {
+                const DqWork w = dq_work(a, item);
+                const int hk = (int)(w.head / a.group);
+                // all products of the turn before but the last are issued
+                if (k && !gemm_wait(turned, (k - 1) & 1, abort)) break;
+                if (!kHeld) {
+                    mbar_arrive_expect_tx(do_full, kBytes);
+                    load_tile<DP>(sdo, &a.d_o, (int)w.head, (int)(w.start + w.row0), do_full);
+                }
+                unsigned i = 0;
+                for (; i < 2 * w.n; ++i, ++it) {
+                    const unsigned j = it >> 1, s = j % 3, full = (it & 1 ? v_full : k_full) + 8 * s, empty = (it & 1 ? v_empty : k_empty) + 8 * s;
+                    if ((j >= 3 && !gemm_wait(empty, (j / 3 - 1) & 1, abort)) || *abort) break;
+                    const bool cut = i == 2 * w.n - 2 && w.cut;
+                    if (cut) arrive_bar(full);
+                    // two such tiles at most are under way: the third one's turn waits for the first one's products
+                    const unsigned to = cut ? tail_of(cuts++) : full;
+                    mbar_arrive_expect_tx(to, kBytes + (a.expire && it == 0 ? 16u : 0u));
+                    load_tile<DP>((it & 1 ? sv : sk) + s * kBytes, it & 1 ? &a.v : &a.k, hk, (int)(w.start + (i >> 1) * kTile), to);
+                }
+                if (i < 2 * w.n || (k >= 2 && !gemm_wait(next_empty + 8 * (k & 1), (k >> 1) - 1 & 1, abort))) {
+                    ++k;
+                    break;
+                }
+                item = publish_next(rest.turns, a, k, reply_full, next_full, abort);
+                if (!item.len) {
+                    ++k;
+                    break;
+                }
             }
-            unsigned it = 0;
-            bool tailed = false;
-            for (; it < 2 * n; ++it) {                                       // keys 0, values 0, keys 1, ...
-                const unsigned j = it >> 1, s = j % 3, full = (it & 1 ? v_full : k_full) + 8 * s, empty = (it & 1 ? v_empty : k_empty) + 8 * s;
-                if ((j >= 3 && !gemm_wait(empty, (j / 3 - 1) & 1, abort)) || *abort) break;
-                const bool cut = it == 2 * n - 2 && item.len - j * kTile < kTile;
-                if (cut) arrive_bar(full);
-                mbar_arrive_expect_tx(cut ? tail : full, kBytes + (a.expire && it == 0 ? 16u : 0u));
-                load_tile<DP>((it & 1 ? sv : sk) + s * kBytes, it & 1 ? &a.v : &a.k, hk, (int)(item.start + j * kTile), cut ? tail : full);
-                tailed = tailed || cut;
-            }
-            if (tailed) mbar_wait_bounded(tail, 0);
-            if (!kHeld) mbar_wait_bounded(do_full, 0);
+            for (unsigned c = cuts > 2 ? cuts - 2 : 0; c < cuts; ++c) mbar_wait_bounded(tail_of(c), c >> 1 & 1);
+            if (!kHeld) mbar_wait_bounded(do_full, (k - 1) & 1);
             for (unsigned i = it > 6 ? it - 6 : 0; i < it; ++i)
                 mbar_wait_bounded((i & 1 ? v_full : k_full) + 8 * ((i >> 1) % 3), (i >> 1) / 3 & 1);
         } else if (warp == kBwdWarps + 1 && elect_one()) {
+            unsigned past = 0, cuts = 0;                                     // tiles and cut ones before this turn
+            DqWork w;
             const auto scores = [&](unsigned j) {
-                if (!gemm_wait(k_full + 8 * (j % 3), j / 3 & 1, abort)) return false;
-                if (item.len - j * kTile < kTile && !gemm_wait(clean, 0, abort)) return false;
+                const unsigned g = past + j;
+                if (!gemm_wait(k_full + 8 * (g % 3), g / 3 & 1, abort)) return false;
+                if (j + 1 == w.n && w.cut && !gemm_wait(clean_of(cuts), cuts >> 1 & 1, abort)) return false;
                 tc_fence_after();
-                mma_held<DP>(kS, kQ, sk + j % 3 * kBytes);
+                mma_held<DP>(kS, kQ, sk + g % 3 * kBytes);
                 umma_commit(s_full);
                 return true;
             };
             const auto weights = [&](unsigned j) {                           // dp of tile j
-                if (!gemm_wait(v_full + 8 * (j % 3), j / 3 & 1, abort)) return false;
+                const unsigned g = past + j;
+                if (!gemm_wait(v_full + 8 * (g % 3), g / 3 & 1, abort)) return false;
                 tc_fence_after();
-                if (kHeld) mma_held<DP>(kP, kDo, sv + j % 3 * kBytes);
-                else mma_rows<DP>(kP, sdo, sv + j % 3 * kBytes);
+                if (kHeld) mma_held<DP>(kP, kDo, sv + g % 3 * kBytes);
+                else mma_rows<DP>(kP, sdo, sv + g % 3 * kBytes);
                 umma_commit(dp_full);
-                umma_commit(v_empty + 8 * (j % 3));
+                umma_commit(v_empty + 8 * (g % 3));
+                if (j + 1 == w.n) umma_commit(turned);
                 return true;
             };
-            bool ok = gemm_wait(q_full, 0, abort) && (kHeld || gemm_wait(do_full, 0, abort)), more = true;
-            // each round makes the scores and dp of tile j and the product that tile j - 1 ends with
-            for (unsigned j = 0; ok && more; ++j) {
-                more = j < n;
-                if (j) ok = gemm_wait(s_read, (j - 1) & 1, abort);
-                if (ok && more) ok = scores(j);
-                if (ok && j) ok = gemm_wait(ds_full, (j - 1) & 1, abort);
-                if (ok && more) ok = weights(j);
-                if (!ok || !j) continue;
-                tc_fence_after();
-                mma_weights<DP, 16>(kDq, kDs, sk + (j - 1) % 3 * kBytes, j != 1);
-                umma_commit(k_empty + 8 * ((j - 1) % 3));
-                umma_commit(dq_full);
+            bool ok = true;
+            for (unsigned k = 0; ok; ++k) {
+                w = dq_work(a, item);
+                ok = gemm_wait(q_full, k & 1, abort) && (kHeld || gemm_wait(do_full, k & 1, abort));
+                bool more = true;
+                // each round makes the scores and dp of tile j and the product that tile j - 1 ends with
+                for (unsigned j = 0; ok && more; ++j) {
+                    const unsigned i = past + j - 1;
+                    more = j < w.n;
+                    if (j) ok = gemm_wait(s_read, i & 1, abort);
+                    if (ok && more) ok = scores(j);
+                    if (ok && j) ok = gemm_wait(ds_full, i & 1, abort);
+                    if (ok && more) ok = weights(j);
+                    if (!ok || !j) continue;
+                    tc_fence_after();
+                    mma_weights<DP, 16>(kDq, kDs, sk + i % 3 * kBytes, j != 1);
+                    umma_commit(k_empty + 8 * (i % 3));
+                    umma_commit(dq_full);
+                }
+                past += w.n;
+                cuts += w.cut;
+                ok = ok && read_next(rest.turns, k, next_full, item, abort);
+                if (!ok || !item.len) break;
+                arrive_bar(next_empty + 8 * (k & 1));
             }
             umma_commit(drain);
             mbar_wait_bounded(drain, 0);
-        } else if (warp == kBwdWarps + 2 && item.len - (n - 1) * kTile < kTile) {
+        } else if (warp == kBwdWarps + 2) {
             // the last tile of keys, which dq sums over, reports here and not to the issuer
-            if (warp_wait(tail, 0, abort))
-                zero_rows<DP>(sk + (n - 1) % 3 * kBytes, item.len - (n - 1) * kTile, lane, clean);
+            unsigned past = 0, cuts = 0, k = 0;
+            do {
+                const DqWork w = dq_work(a, item);
+                past += w.n;
+                if (!w.cut) continue;
+                if (!warp_wait(tail_of(cuts), cuts >> 1 & 1, abort)) break;
+                zero_rows<DP>(sk + (past - 1) % 3 * kBytes, w.len - (w.n - 1) * kTile, lane, clean_of(cuts));
+                ++cuts;
+            } while (warp_next(rest.turns, k++, next_full, next_empty, item, lane, abort));
         }
     } else {
         more_registers<kBwdWarps>();
-        const unsigned share = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16, row = row0 + (warp & 3) * 32 + lane;
-        const unsigned long long token = item.start + row, stat = (unsigned long long)head * a.tokens + token;
+        const unsigned share = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16;
         const float c = a.scale * kLog2e;
-        const float off = row < item.len ? -a.lse[stat] * kLog2e : 0.0f;
-        float delta = row < item.len && n > 1 ? a.delta[stat] : 0.0f;
-        // columns below `end` count; a token that sees itself alone has ds = 0
-        const unsigned end = row >= item.len ? 0 : a.causal ? row + 1 : item.len;
-        if (32 * share < DP) {
-            const bool here = row < item.len;
-            hold_row32(kQ + at + 16 * share, here ? a.q_rows.data + token * a.q_rows.ld_token + head * a.q_rows.ld_head : nullptr, 32 * share, a.dim);
-            if (kHeld) hold_row32(kDo + at + 16 * share, here ? a.do_rows.data + token * a.do_rows.ld_token + head * a.do_rows.ld_head : nullptr, 32 * share, a.dim);
-            tmem_st_wait();
-        }
-        warp_arrive(q_full, lane);
+        unsigned past = 0, sums = 0, k = 0;                                  // tiles and turns of one tile before this turn
         bool ok = true;
-        for (unsigned j = 0; j < n; ++j) {
-            ok = warp_wait(s_full, j & 1, abort);
-            if (!ok) break;
-            tc_fence_after();
-            unsigned r[32], w[16];
-            float2 p[16];
-            tmem_ld32(kS + at + 32 * share, r);
-            tmem_ld_wait();
-            warp_arrive(s_read, lane);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) p[k] = exp2_pair(r[2 * k], r[2 * k + 1], c, make_float2(off, off), poly_pair(k));
-            ok = warp_wait(dp_full, j & 1, abort);
-            if (!ok) break;
-            tc_fence_after();
-            tmem_ld32(kP + at + 32 * share, r);
-            tmem_ld_wait();
-            const unsigned first = j * kTile + 32 * share, live = end == 1 || end <= first ? 0 : end - first;
-            if (n == 1) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int k = 0; k < 32; ++k)
-                    if (k < live) sum = fmaf(k & 1 ? p[k / 2].y : p[k / 2].x, __uint_as_float(r[k]), sum);
-                shares[share][row - row0] = sum;
-                __syncwarp();
-                if (lane == 0) arrive_bar(sum_full);
-                ok = warp_wait(sum_full, 0, abort);
-                if (!ok) break;
-                delta = (shares[0][row - row0] + shares[1][row - row0]) + (shares[2][row - row0] + shares[3][row - row0]);
-                if (share == 0 && row < item.len) a.delta[stat] = delta;
+        do {
+            const DqWork w = dq_work(a, item);
+            const unsigned row = w.row0 + (warp & 3) * 32 + lane;
+            const unsigned long long token = w.start + row, stat = (unsigned long long)w.head * a.tokens + token;
+            const float off = row < w.len ? -a.lse[stat] * kLog2e : 0.0f;
+            float delta = row < w.len && w.n > 1 ? a.delta[stat] : 0.0f;
+            // columns below `end` count; a token that sees itself alone has ds = 0
+            const unsigned end = row >= w.len ? 0 : a.causal ? row + 1 : w.len;
+            if (32 * share < DP) {
+                const bool here = row < w.len;
+                hold_row32(kQ + at + 16 * share, here ? a.q_rows.data + token * a.q_rows.ld_token + w.head * a.q_rows.ld_head : nullptr, 32 * share, a.dim);
+                if (kHeld) hold_row32(kDo + at + 16 * share, here ? a.do_rows.data + token * a.do_rows.ld_token + w.head * a.do_rows.ld_head : nullptr, 32 * share, a.dim);
+                tmem_st_wait();
             }
-            if (__any_sync(0xffffffffu, live < 32)) {
-                // masked: a weight of 0, and a dp that may be NaN past the sequence's end counts as delta
-#pragma unroll
-                for (int k = 0; k < 32; ++k)
-                    if (k >= live) {
-                        r[k] = __float_as_uint(delta);
-                        (k & 1 ? p[k / 2].y : p[k / 2].x) = 0.0f;
-                    }
-            }
-#pragma unroll
-            for (int k = 0; k < 16; ++k) w[k] = ds_pair(p[k], r[2 * k], r[2 * k + 1], make_float2(-delta, -delta));
-            if (j) {                              // the product that reads the last tile's ds, long done by now
-                ok = warp_wait(dq_full, (j - 1) & 1, abort);
+            warp_arrive(q_full, lane);
+            for (unsigned j = 0; j < w.n; ++j) {
+                ok = warp_wait(s_full, past + j & 1, abort);
                 if (!ok) break;
                 tc_fence_after();
+                unsigned r[32], u[16];
+                float2 p[16];
+                tmem_ld32(kS + at + 32 * share, r);
+                tmem_ld_wait();
+                warp_arrive(s_read, lane);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) p[k] = exp2_pair(r[2 * k], r[2 * k + 1], c, make_float2(off, off), poly_pair(k));
+                ok = warp_wait(dp_full, past + j & 1, abort);
+                if (!ok) break;
+                tc_fence_after();
+                tmem_ld32(kP + at + 32 * share, r);
+                tmem_ld_wait();
+                const unsigned first = j * kTile + 32 * share, live = end == 1 || end <= first ? 0 : end - first;
+                if (w.n == 1) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (k < live) sum = fmaf(k & 1 ? p[k / 2].y : p[k / 2].x, __uint_as_float(r[k]), sum);
+                    shares[share][row - w.row0] = sum;
+                    __syncwarp();
+                    if (lane == 0) arrive_bar(sum_full);
+                    ok = warp_wait(sum_full, sums++ & 1, abort);
+                    if (!ok) break;
+                    delta = (shares[0][row - w.row0] + shares[1][row - w.row0]) + (shares[2][row - w.row0] + shares[3][row - w.row0]);
+                    if (share == 0 && row < w.len) a.delta[stat] = delta;
+                }
+                if (__any_sync(0xffffffffu, live < 32)) {
+                    // masked: a weight of 0, and a dp that may be NaN past the sequence's end counts as delta
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (k >= live) {
+                            r[k] = __float_as_uint(delta);
+                            (k & 1 ? p[k / 2].y : p[k / 2].x) = 0.0f;
+                        }
+                }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) u[k] = ds_pair(p[k], r[2 * k], r[2 * k + 1], make_float2(-delta, -delta));
+                if (j) {                              // the product that reads the last tile's ds, long done by now
+                    ok = warp_wait(dq_full, past + j - 1 & 1, abort);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                tmem_st16(kDs + at + 16 * share, u);
+                tmem_st_wait();
+                warp_arrive(ds_full, lane);
             }
-            tmem_st16(kDs + at + 16 * share, w);
-            tmem_st_wait();
-            warp_arrive(ds_full, lane);
-        }
-        if (ok) ok = warp_wait(dq_full, (n - 1) & 1, abort);
-        if (ok && 32 * share < DP) {
-            tc_fence_after();
-            unsigned w[32];
-            tmem_ld32(kDq + at + 32 * share, w);
-            tmem_ld_wait();
-            if (row < item.len) store_row32(a.dq.data + token * a.dq.ld_token + head * a.dq.ld_head, 32 * share, a.dim, w, a.scale);
-        }
+            if (ok) ok = warp_wait(dq_full, past + w.n - 1 & 1, abort);
+            if (ok && 32 * share < DP) {
+                tc_fence_after();
+                unsigned u[32];
+                tmem_ld32(kDq + at + 32 * share, u);
+                tmem_ld_wait();
+                if (row < w.len) store_row32(a.dq.data + token * a.dq.ld_token + w.head * a.dq.ld_head, 32 * share, a.dim, u, a.scale);
+            }
+            past += w.n;
+        } while (ok && warp_next(rest.turns, k++, next_full, next_empty, item, lane, abort));
     }
     attn_end<kBwdWarps>(sh, a, warp, tmem);
 }
