@@ -195,10 +195,9 @@ __device__ __forceinline__ float4 ld_cluster4(unsigned addr, unsigned rank)
 template <int DP>
 __device__ __forceinline__ unsigned sums_piece(unsigned base, unsigned row, unsigned piece) { return base + row * (2 * DP * 4) + ((piece ^ (row & 7)) << 4); }
 
-// Columns col .. col + 31 of a row (null: zeros) to 16 columns of tensor memory, as operand A; dim is a multiple of 8.
-__device__ __forceinline__ void hold_row32(unsigned at, const __nv_bfloat16 *row, unsigned col, unsigned dim)
+// Columns col .. col + 31 of a row (null: zeros), and to 16 columns of tensor memory, as operand A; dim is a multiple of 8.
+__device__ __forceinline__ void load_row32(const __nv_bfloat16 *row, unsigned col, unsigned dim, unsigned (&w)[16])
 {
-    unsigned w[16];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint4 x = row && col + 8 * j < dim ? __ldcg(reinterpret_cast<const uint4 *>(row + col + 8 * j)) : make_uint4(0u, 0u, 0u, 0u);
@@ -207,6 +206,12 @@ __device__ __forceinline__ void hold_row32(unsigned at, const __nv_bfloat16 *row
         w[4 * j + 2] = x.z;
         w[4 * j + 3] = x.w;
     }
+}
+
+__device__ __forceinline__ void hold_row32(unsigned at, const __nv_bfloat16 *row, unsigned col, unsigned dim)
+{
+    unsigned w[16];
+    load_row32(row, col, dim, w);
     tmem_st16(at, w);
 }
 
@@ -849,19 +854,30 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
         const unsigned share = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16;
         const float c = a.scale * kLog2e;
         unsigned past = 0, sums = 0, k = 0;                                  // tiles and turns of one tile before this turn
-        bool ok = true;
+        unsigned held[kHeld ? 2 : 1][16];                                    // the next turn's operands
+        float off, delta;
+        // what a turn begins with, asked for before the last one ends
+        const auto fetch = [&](const DqWork &w) {
+            const unsigned row = w.row0 + (warp & 3) * 32 + lane;
+            const unsigned long long token = w.start + row, stat = (unsigned long long)w.head * a.tokens + token;
+            const bool here = row < w.len;
+            off = here ? -a.lse[stat] * kLog2e : 0.0f;
+            delta = here && w.n > 1 ? a.delta[stat] : 0.0f;
+            if (32 * share >= DP) return;
+            load_row32(here ? a.q_rows.data + token * a.q_rows.ld_token + w.head * a.q_rows.ld_head : nullptr, 32 * share, a.dim, held[0]);
+            if (kHeld) load_row32(here ? a.do_rows.data + token * a.do_rows.ld_token + w.head * a.do_rows.ld_head : nullptr, 32 * share, a.dim, held[kHeld]);
+        };
+        bool ok = true, more;
+        fetch(dq_work(a, item));
         do {
             const DqWork w = dq_work(a, item);
             const unsigned row = w.row0 + (warp & 3) * 32 + lane;
             const unsigned long long token = w.start + row, stat = (unsigned long long)w.head * a.tokens + token;
-            const float off = row < w.len ? -a.lse[stat] * kLog2e : 0.0f;
-            float delta = row < w.len && w.n > 1 ? a.delta[stat] : 0.0f;
             // columns below `end` count; a token that sees itself alone has ds = 0
             const unsigned end = row >= w.len ? 0 : a.causal ? row + 1 : w.len;
             if (32 * share < DP) {
-                const bool here = row < w.len;
-                hold_row32(kQ + at + 16 * share, here ? a.q_rows.data + token * a.q_rows.ld_token + w.head * a.q_rows.ld_head : nullptr, 32 * share, a.dim);
-                if (kHeld) hold_row32(kDo + at + 16 * share, here ? a.do_rows.data + token * a.do_rows.ld_token + w.head * a.do_rows.ld_head : nullptr, 32 * share, a.dim);
+                tmem_st16(kQ + at + 16 * share, held[0]);
+                if (kHeld) tmem_st16(kDo + at + 16 * share, held[kHeld]);
                 tmem_st_wait();
             }
             warp_arrive(q_full, lane);
@@ -915,6 +931,8 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
                 tmem_st_wait();
                 warp_arrive(ds_full, lane);
             }
+            more = ok && warp_next(rest.turns, k++, next_full, next_empty, item, lane, abort);
+            if (more) fetch(dq_work(a, item));
             if (ok) ok = warp_wait(dq_full, past + w.n - 1 & 1, abort);
             if (ok && 32 * share < DP) {
                 tc_fence_after();
@@ -924,7 +942,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
                 if (row < w.len) store_row32(a.dq.data + token * a.dq.ld_token + w.head * a.dq.ld_head, 32 * share, a.dim, u, a.scale);
             }
             past += w.n;
-        } while (ok && warp_next(rest.turns, k++, next_full, next_empty, item, lane, abort));
+        } while (ok && more);
     }
     attn_end<kBwdWarps>(sh, a, warp, tmem);
 }
