@@ -710,7 +710,9 @@ __device__ __forceinline__ DqWork dq_work(const AttnArgs &a, const PlanItem &ite
 //
 // Bound, like the next kernel, by the products (512 cycles each of a pair of tiles: 3 here, 4 there, 59-61 % of the
 // time) and by the steps from one to the next.  8192 tokens, 8 heads of 128, causal: 190 and 240 us at 1.5 GHz; 16384
-// tokens: 1455-1475 us with delta, 1310 TFLOP/s of executed products.
+// tokens: 1455-1475 us with delta, 1310 TFLOP/s of executed products.  Taking turns, with the next turn's queries on
+// their way: 16384 tokens, 16 heads on 4 of 128, documents of 128 / 1024 / 4096 tokens, the whole backward pass 285 -> 242,
+// 405 -> 366, 877 -> 850 us; 8192 tokens, 8 heads on 2: 403 -> 387.
 template <int DP>
 __global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dq_kernel(const __grid_constant__ AttnArgs a)
@@ -854,9 +856,10 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
         const unsigned share = warp >> 2, at = (unsigned)((warp & 3) * 32) << 16;
         const float c = a.scale * kLog2e;
         unsigned past = 0, sums = 0, k = 0;                                  // tiles and turns of one tile before this turn
-        unsigned held[kHeld ? 2 : 1][16];                                    // the next turn's operands
+        unsigned held[16];                                                   // the next turn's queries
         float off, delta;
-        // what a turn begins with, asked for before the last one ends
+        // what a turn begins with, asked for before the last one ends (d_o's rows, where they are held too, would take
+        // registers that spill: 64 columns, 4 documents of 4096 tokens 687 -> 694 us)
         const auto fetch = [&](const DqWork &w) {
             const unsigned row = w.row0 + (warp & 3) * 32 + lane;
             const unsigned long long token = w.start + row, stat = (unsigned long long)w.head * a.tokens + token;
@@ -864,8 +867,7 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             off = here ? -a.lse[stat] * kLog2e : 0.0f;
             delta = here && w.n > 1 ? a.delta[stat] : 0.0f;
             if (32 * share >= DP) return;
-            load_row32(here ? a.q_rows.data + token * a.q_rows.ld_token + w.head * a.q_rows.ld_head : nullptr, 32 * share, a.dim, held[0]);
-            if (kHeld) load_row32(here ? a.do_rows.data + token * a.do_rows.ld_token + w.head * a.do_rows.ld_head : nullptr, 32 * share, a.dim, held[kHeld]);
+            load_row32(here ? a.q_rows.data + token * a.q_rows.ld_token + w.head * a.q_rows.ld_head : nullptr, 32 * share, a.dim, held);
         };
         bool ok = true, more;
         fetch(dq_work(a, item));
@@ -876,8 +878,10 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
             // columns below `end` count; a token that sees itself alone has ds = 0
             const unsigned end = row >= w.len ? 0 : a.causal ? row + 1 : w.len;
             if (32 * share < DP) {
-                tmem_st16(kQ + at + 16 * share, held[0]);
-                if (kHeld) tmem_st16(kDo + at + 16 * share, held[kHeld]);
+                tmem_st16(kQ + at + 16 * share, held);
+                if (kHeld)
+                    hold_row32(kDo + at + 16 * share, row < w.len ? a.do_rows.data + token * a.do_rows.ld_token + w.head * a.do_rows.ld_head : nullptr,
+                               32 * share, a.dim);
                 tmem_st_wait();
             }
             warp_arrive(q_full, lane);
