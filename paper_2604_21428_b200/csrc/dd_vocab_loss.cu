@@ -67,19 +67,23 @@ vocab_loss_join_kernel(const float2 *partial, unsigned parts, unsigned tokens, c
 // d 231, 8075 columns: 17 us for the second launch with 8 splits, 12 with more).
 constexpr unsigned kLossSplits = 32;
 
-// Up to here the logits (forward), and with them dhidden (backward), are made by the kernel that streams weights past few
-// tokens; it reads the weights at 4.5 TB/s where the products' kernel reads them at 3.3, but reads the tokens for every
-// 128 columns and finishes a tile after its products, which costs most where a cluster shares the tile's K: forward
-// it goes as far as a tile of tokens where the columns' tiles give every SM one without that.  us from a cold L2, this / the
-// other kernel: forward, 4 / 32 / 64 / 128 tokens, d 2048, 32000 columns 39 / 41 / 41 / 45 (49 / 45 / 46 / 47), d 768 22.5 / 24 /
-// 25 / 28 (27 / 28 / 31 / 29), 192 tokens 37 (29); clusters, d 512, 5000 columns 14.4 / 16.4 / 18.4 / 22.5 (16.4 all).  From a
-// warm L2, backward with 4 / 64 / 96 tokens, d 2048, 32000 columns 97 / 103 / 111 (108 / 110 / 111), d 512, 5000 columns 15 / 17 /
-// 19 (21 / 25 / 25), d 768, 32000 columns 48 / 56 / 63 (51 / 57 / 56).
-constexpr uint64_t kLossFewForward = 32, kLossFewBackward = 80;
-
-static bool few_forward(const dd_ctx *ctx, const dd_vocab_loss &l)
+// Tokens up to which the logits (forward), and with them dhidden (backward), are made by the kernel that streams weights
+// past few tokens.  It reads the weights at 4.5 TB/s where the products' kernel reads them at 3.3, and its clusters split
+// the sum over d, which the other kernel's epilogues cannot do; but it reads the tokens for every 128 columns and finishes
+// a tile after its products.  So it goes furthest where the other kernel's tiles of 256 columns would leave three
+// quarters of the pairs of SMs idle, and, forward, as far as one tile of tokens where its own tiles give every SM one
+// without clusters.  us from a cold L2, this / the other kernel:
+//   forward   2344 x 1643 (d x columns), 16 / 105 / 256 tokens 14 / 16 / 22 (23 / 26 / 28), 4096 x 3000 18 / 24 / 28 (33 / 35 / 35);
+//             512 x 5000, 16 / 48 / 80 tokens 14 / 16 / 18 (16 all), 2048 x 8192 20 / 22 / 25 (25 / 25 / 26);
+//             768 x 32000, 4 / 64 / 128 / 192 tokens 22 / 25 / 28 / 37 (27 / 31 / 29 / 29), 2048 x 32000 39 / 41 / 45 / 59 (49 / 46 / 47 / 47)
+//   backward  2344 x 1643, 16 / 105 / 256 tokens 24 / 30 / 37 (38 / 41 / 43), 4096 x 3000 31 / 42 / 49 (51 / 55 / 57);
+//             512 x 5000, 16 / 105 / 128 / 160 tokens 18 / 24 / 29 / 28 (25 / 29 / 29 / 29), 1024 x 16000 38 / 47 / 49 / 53 (47 / 49 / 49 / 50);
+//             768 x 32000 from a warm L2, 4 / 64 / 96 tokens 48 / 56 / 63 (51 / 57 / 56)
+static bool few_tokens(const dd_ctx *ctx, const dd_vocab_loss &l, bool backward)
 {
-    return l.tokens <= (blocks_of(l.vocab, kBM) >= (unsigned)ctx->sm_count ? kStreamMaxCols : kLossFewForward);
+    const unsigned sms = (unsigned)ctx->sm_count;
+    const bool narrow = blocks_of(l.vocab, 256) * 4 <= sms / 2, wide = blocks_of(l.vocab, kBM) >= sms;
+    return l.tokens <= (narrow ? 256 : backward ? (wide ? 80 : 128) : wide ? kStreamMaxCols : 48);
 }
 
 static uint64_t rows8(uint64_t n) { return (n + 7) / 8 * 8; }
@@ -192,7 +196,7 @@ extern "C" int dd_vocab_loss_forward(dd_ctx *ctx, const dd_vocab_loss *l_, const
     a.e.partial = static_cast<float2 *>(scratch);
     a.e.tokens = (unsigned)T;
     const Matrix h = {hidden, T, l.d, l.ld_hidden}, w = {l.weight, l.vocab, l.d, l.ld_weight};
-    if (few_forward(ctx, l)) {
+    if (few_tokens(ctx, l, false)) {
         rc = launch_few_logits<kEpiLoss>(ctx, a.e, h, w, stream);
     } else {
         rc = encode(ctx, &a.maps[0], h);
@@ -244,7 +248,7 @@ extern "C" int dd_vocab_loss_backward(dd_ctx *ctx, const dd_vocab_loss *l_, cons
     a.e.hidden = g;
     a.e.ld_hidden = ldg;
     const unsigned kt = blocks_of(T, kBK), pairs = (unsigned)ctx->sm_count / 2;
-    const bool few = T <= kLossFewBackward && cols == l.vocab;
+    const bool few = few_tokens(ctx, l, true) && cols == l.vocab;
     for (uint64_t first = 0; first < l.vocab; first += cols) {
         const uint64_t n = l.vocab - first < cols ? l.vocab - first : cols;
         const bool last = first + n == l.vocab;

@@ -75,6 +75,12 @@ def test_against_float64(ctx, size):
         assert pads_untouched(dweight) and pads_untouched(c.dhidden)
 
 
+@pytest.mark.parametrize("size", [(48, 200, 4700), (49, 200, 4700), (128, 136, 5000), (129, 136, 5000), (160, 905, 1187), (256, 520, 1301),
+                                  (257, 520, 1301), (200, 2344, 643), (81, 72, 19001)], ids=str)
+def test_where_another_kernel_takes_over(ctx, size):
+    test_against_float64(ctx, size)
+
+
 @pytest.mark.parametrize("T", [2, 17, 32, 95, 96, 128, 129])
 @pytest.mark.parametrize("large", [False, True])
 def test_few_tokens_and_many_columns(ctx, T, large):
