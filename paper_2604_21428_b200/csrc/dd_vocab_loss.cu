@@ -6,7 +6,8 @@
 // Bound by the products, 2 T d V of them forward, 6 T d V backward beside 2 T d V for the logits again: 8192 tokens,
 // d 2048, 32000 columns 773 us forward in short runs and 875 sustained under the 1000 W cap (1390 and 1230 TFLOP/s), 2610 and
 // 2825 us backward (1650 and 1520 TFLOP/s with the logits).  With few tokens by the weights' bytes, read once forward; backward
-// reads them twice and writes as many (4 tokens: 27 and 97 us, of which the bytes need 20 and 40).
+// reads them twice and writes as many (4 tokens: 39 us from a cold L2 and 97 from a warm one, of which the bytes
+// need 20 and 40).
 #include <cmath>
 
 #include "dd_decoder.h"
