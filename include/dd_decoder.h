@@ -29,7 +29,8 @@ enum { DD_STATUS_BAD_OFFSETS = 5 };
 
 /* One tensor of [tokens, heads, dim]: the elements of a head are contiguous, strides are in elements;
  * 0 stands for those of a contiguous tensor.  Tokens and heads may be in either order in memory, and
- * several tensors may share the rows of one buffer (a projection's queries, keys and values). */
+ * several tensors may share the rows of one buffer (a projection's queries, keys and values), one behind the other or head by
+ * head. */
 typedef struct {
     void *data;             /* [device] */
     uint64_t ld_token, ld_head;

@@ -35,25 +35,32 @@ inline EncodeTiled tensor_map_encoder()
 
 inline unsigned blocks_of(unsigned long long n, unsigned b) { return (unsigned)((n + b - 1) / b); }
 
-// Rows of a matrix in memory, in bytes; no rows: touches nothing.
+// Rows of a matrix in memory, in bytes; no rows: touches nothing.  A row may be a comb: pieces of `tooth` bytes every
+// `step` of them (the heads of a token, what lies between belonging to others); step 0: all of it.
 struct Extent {
     const void *p;
     size_t rows, width, pitch;
+    size_t tooth, step;
 };
 
 inline Extent extent(const void *p, unsigned long long rows, unsigned long long cols, unsigned long long ld, size_t elem = 2)
 {
-    return Extent{p, p ? (size_t)rows : 0, (size_t)cols * elem, (size_t)ld * elem};
+    return Extent{p, p ? (size_t)rows : 0, (size_t)cols * elem, (size_t)ld * elem, (size_t)cols * elem, 0};
 }
 
 // Whether two matrices share a byte.  Rows of one pitch may lie side by side (gate and up as halves of one
-// buffer's rows); of different pitches whatever lies between the ends is taken.
+// buffer's rows), and combs of one step between each other's teeth (queries, keys and values of a head side by side); otherwise
+// whatever lies between the ends is taken.
 inline bool touches(const Extent &a, const Extent &b)
 {
     if (!a.rows || !b.rows) return false;
     const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
     if (y < x) return touches(b, a);
     if (y >= x + (a.rows - 1) * a.pitch + a.width) return false;
+    if (a.step && a.step == b.step && a.pitch % a.step == 0 && b.pitch % a.step == 0) {      // all teeth at one place of a step
+        const size_t off = (y - x) % a.step;
+        if (off >= a.tooth && off + b.tooth <= a.step) return false;
+    }
     if (a.pitch != b.pitch) return true;
     const size_t off = (y - x) % a.pitch;
     return off < a.width || off + b.width > a.pitch;
@@ -78,8 +85,14 @@ inline int check_heads(dd_heads &x, uint64_t tokens, uint64_t heads, uint64_t di
 inline Extent heads_extent(const dd_heads &x, uint64_t tokens, uint64_t heads, uint64_t dim, size_t elem = 2)
 {
     if (!tokens) return Extent{};
-    if (heads == 1 || x.ld_token >= x.ld_head) return extent(x.data, tokens, (heads - 1) * x.ld_head + dim, x.ld_token, elem);
-    return extent(x.data, heads, (tokens - 1) * x.ld_token + dim, x.ld_head, elem);
+    if (tokens == 1) return extent(x.data, heads, dim, x.ld_head, elem);
+    if (heads == 1) return extent(x.data, tokens, dim, x.ld_token, elem);
+    const bool heads_inside = x.ld_token >= x.ld_head;
+    const uint64_t inner = heads_inside ? x.ld_head : x.ld_token, outer = heads_inside ? x.ld_token : x.ld_head, n = heads_inside ? heads : tokens;
+    Extent e = extent(x.data, heads_inside ? tokens : heads, (n - 1) * inner + dim, outer, elem);
+    e.tooth = dim * elem;
+    e.step = inner * elem;
+    return e;
 }
 
 inline int check_aligned(std::initializer_list<const void *> ptrs)
