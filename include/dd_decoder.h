@@ -55,7 +55,7 @@ typedef struct {
  *   positions [device] int32, or int64 with positions_64; a token with a negative position is none:
  *             its rows are left as they are
  *   frequencies [device] rotary_dim / 2 float64, radians per position
- * tokens may be 0; tokens, heads, kv_heads < 2^24, 1 <= dim <= 1024 (DD_ERR_TOO_LARGE), rotary_dim even,
+ * tokens may be 0; tokens < 2^24, heads, kv_heads < 2^16, 1 <= dim <= 1024 (DD_ERR_TOO_LARGE), rotary_dim even,
  * 2 <= rotary_dim <= dim.  Data is aligned to its element; where pointers and strides allow it moves in
  * 16-byte pieces.
  */
