@@ -29,8 +29,8 @@ enum { DD_STATUS_BAD_OFFSETS = 5 };
 
 /* One tensor of [tokens, heads, dim]: the elements of a head are contiguous, strides are in elements;
  * 0 stands for those of a contiguous tensor.  Tokens and heads may be in either order in memory, and
- * several tensors may share the rows of one buffer (a projection's queries, keys and values), one behind the other or head by
- * head. */
+ * several tensors may share the rows of one buffer (a projection's queries, keys and values), one behind
+ * the other or head by head. */
 typedef struct {
     void *data;             /* [device] */
     uint64_t ld_token, ld_head;
@@ -46,7 +46,9 @@ typedef struct {
  * where (a, b) are the elements (i, i + rotary_dim / 2) of a head, or (2 i, 2 i + 1) with `interleaved`.
  * `inverse` turns by -w: with it the call takes the gradients of its results to those of its inputs.
  * Elements from rotary_dim on are copied.  Angles are formed in float64 and reduced to a part of a turn
- * there, so that far positions lose nothing; the rest is float32, rounded once.
+ * there, the rest is float32, rounded once: beside that rounding a' and b' are within
+ * magnitude (|a| + |b|) (2^-21 + 2^-51 |w|) of the formula's values.  Angles of up to 2^29 radians lose less
+ * there than in float32; from 2^50 on little of an angle is left.
  *
  * Scaled contexts come in through `frequencies` and `magnitude`.
  *

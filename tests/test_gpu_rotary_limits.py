@@ -38,3 +38,19 @@ def test_heads(dd, ctx):
         with pytest.raises(dd.DDMergeError) as e:
             ctx.rotary(q, k, positions[:1], f)
         assert e.value.rc == dd.ERR_TOO_LARGE
+
+
+@pytest.mark.parametrize("reach", [28, 31, 40, 50])
+def test_far_positions(ctx, reach):
+    """Angles of up to 2^reach radians.  Three float64 roundings of a turn count are 2^-51 of the angle at most, beside
+    the bound of near ones; frequencies whose products with the positions are exact in float64."""
+    f = torch.tensor([1.0, 0.75, 0.5, 0.125], dtype=torch.float64, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(reach)
+    positions = (1 << reach) - torch.randint(0, 1 << 20, (200,), generator=gen, device="cuda")
+    x = torch.randn(200, 2, 8, generator=gen, device="cuda")
+    y = torch.empty_like(x)
+    ctx.rotary(x, None, positions, f, q_out=y)
+    want, e = turned64(x, positions, f, 1.0, False, False)
+    a, b = x.double().abs()[..., :4], x.double().abs()[..., 4:]
+    off = (positions.double()[:, None, None] * f) * 2.0 ** -51 * (a + b)
+    within(y, want, e + torch.cat([off, off], -1) + U * want.abs(), "far")
