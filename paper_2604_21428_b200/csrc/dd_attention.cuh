@@ -232,10 +232,12 @@ __device__ __forceinline__ void store_row32(__nv_bfloat16 *row, unsigned col, un
 // and holds it in its low bits), 2^f by a polynomial on [-1/2, 1/2], n into the exponent.  The coefficients are
 // a minimax fit of the relative error with 2^0 = 1 held (a weighted least-squares iteration): 2.9e-6 in float32, far
 // below the bf16 rounding that follows.  Below -127 the result is 0, near -126.5 it is off by less than 2^-126.
+// A NaN ends as the largest float, since the last sum is one of integers: as a bf16 operand that is an infinity, and in ds
+// the row's delta, which has weights of the other kind in it, is NaN.
 __device__ __forceinline__ float2 exp2_poly(float2 x)
 {
     constexpr float c[] = {1.0f, 0.6931241750717163f, 0.24024099111557007f, 0.055906426161527634f, 0.009582852944731712f}, kRound = 12582912.0f;
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-127.0f));               // a NaN goes on, and ends as an infinity
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-127.0f));               // a NaN goes on
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-127.0f));
     const float2 t = __fadd2_rn(x, make_float2(kRound, kRound)), n = __fadd2_rn(t, make_float2(-kRound, -kRound)),
                  f = __ffma2_rn(n, make_float2(-1.0f, -1.0f), x);
