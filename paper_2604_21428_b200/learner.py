@@ -236,14 +236,14 @@ class DecoderLearner:
             dx = dx + normed_backward(self.dx.float(), keep["y2"], keep["r2"])
             dy = dx.to(bf)
             self.d_o.copy_((dy @ w_o).view_as(self.d_o))
-            dw_o.copy_(dy.t() @ keep["o"].flatten(1))
+            torch.mm(dy.t(), keep["o"].flatten(1), out_dtype=torch.float32, out=dw_o)      # sums are not rounded to bf16
             q, k, v = self._split(keep["qkv"])
             dq, dk, dv = self._split(self.dqkv)
             self.dqkv.zero_()                                  # rows behind the last document stay as they are
             self.ctx.attention_backward(q, k, v, keep["o"], keep["lse"], self.d_o, dq, dk, dv, offsets=offsets, scratch=self.attention_scratch)
             self.ctx.rotary(dq, dk, positions, self.frequencies, inverse=True)
             dqkv = self.dqkv.flatten(1)
-            dw_qkv.copy_(dqkv.t() @ keep["h1"])
+            torch.mm(dqkv.t(), keep["h1"], out_dtype=torch.float32, out=dw_qkv)
             dx = dx + normed_backward((dqkv @ w_qkv).float(), keep["y1"], keep["r1"])
         d_embedding.zero_().index_put_((ids,), dx, accumulate=True)
 
