@@ -248,9 +248,10 @@ class DecoderLearner:
         d_embedding.zero_().index_put_((ids,), dx, accumulate=True)
 
     def step(self, ids, targets, positions, offsets) -> torch.Tensor:
-        """One inner step on the mean loss of the tokens that have a target; returns it (a device scalar)."""
+        """One inner step on the mean loss of the tokens that have a target; returns it (a device scalar).  Without any
+        the loss and its gradients are 0."""
         loss = self.forward(ids, targets, positions, offsets)
-        count = (targets >= 0).sum()
+        count = (targets >= 0).sum().clamp(min=1)
         self.backward((1.0 / count).float().expand(self.tokens).contiguous())
         self.ctx.grad_norm(self.grads, self.max_norm, self.record)
         self.steps += 1

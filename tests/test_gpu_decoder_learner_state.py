@@ -35,3 +35,16 @@ def test_gradients_of_the_projections_are_float32(mods):
         assert not torch.equal(g, g.to(torch.bfloat16).float())
     a, b = m.dqkv.flatten(1).double(), m.kept[0]["h1"].double()
     within(dw_qkv, a.t() @ b, (SIZES["tokens"] + 16) * 2 * U * (a.abs().t() @ b.abs()) + 1e-38, "dw_qkv")
+
+
+def test_a_batch_without_targets(mods):
+    """Documents of one token have no target: the loss is 0 and nothing moves."""
+    m, _ = start(mods, lr=1e-2)
+    before = [p.clone() for p in m.params]
+    T = SIZES["tokens"]
+    ids, targets = torch.zeros(T, dtype=torch.int64, device="cuda"), torch.full((T,), -100, dtype=torch.int64, device="cuda")
+    positions = torch.full((T,), -1, dtype=torch.int64, device="cuda")
+    positions[:3] = 0
+    assert float(m.step(ids, targets, positions, torch.arange(4, dtype=torch.int32, device="cuda"))) == 0.0
+    assert not any(bool(g.any()) for g in m.grads)
+    assert all(torch.equal(a, b) for a, b in zip(before, m.params))
