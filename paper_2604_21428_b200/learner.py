@@ -4,7 +4,8 @@
 is a flat concatenation of w_gate, w_up and w_down, held as float32 parameters with AdamW's moments,
 float32 gradients, and the bf16 copy that the block computes with and ``dd_merge_fragment`` reads.
 An inner step is forward, backward, the gradients' global norm, and AdamW with the clip scale; the
-syncer's merge then pushes the new global fragment into the copies.
+syncer's merge then pushes the new global fragment into the copies.  What the operators report in a learner's status word
+(a wait that ran out, offsets that make no sense) holds its steps back until ``check`` has raised it, before a merge.
 
 ``DecoderLearner``'s model is a decoder: embedding, layers of attention and gated feed-forward block, and the
 loss over the vocabulary, trained on documents packed end to end.  Its fragments are the layers and, last, the
@@ -21,6 +22,19 @@ import sys
 import torch
 
 from . import ddmerge as dd
+
+
+def hold_back(record, status) -> None:
+    """A step whose operators reported something is not applied, like one whose gradients are not finite."""
+    record.view(torch.int32)[2:3].bitwise_or_(status)          # the record's own status
+
+
+def raise_status(status) -> None:
+    """Raises what operators reported since the last time, if anything; waits for them."""
+    code = int(status)
+    if code:
+        status.zero_()
+        raise RuntimeError(f"inner steps were not applied: an operator reported status {code}")
 
 
 class Learner:
@@ -50,6 +64,7 @@ class Learner:
         self.dx = rows(d)
         self.scratch = torch.empty(3 * tokens * ((f + 7) // 8 * 8), dtype=torch.bfloat16, device=device)
         self.record = dd.new_grad_record(device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
 
     def _views(self, flat):
         d, f = self.d, self.f
@@ -64,14 +79,14 @@ class Learner:
         self.x[0].copy_(x)
         for i, w in enumerate(self.weights):
             self.ctx.gated_ffn_forward(self.x[i], *w, self.x[i + 1], activation=self.activation, residual=self.x[i],
-                                       gate=self.gate[i], up=self.up[i], hidden=self.scratch)
+                                       gate=self.gate[i], up=self.up[i], hidden=self.scratch, status=self.status)
         return self.x[-1]
 
     def backward(self, dy) -> None:
         """Gradients of every block for the output's gradient ``dy`` (bfloat16), into ``grads``."""
         for i in reversed(range(len(self.weights))):
             self.ctx.gated_ffn_backward(self.x[i], *self.weights[i], self.gate[i], self.up[i], dy, self.dx,
-                                        *self.weight_grads[i], activation=self.activation, scratch=self.scratch)
+                                        *self.weight_grads[i], activation=self.activation, scratch=self.scratch, status=self.status)
             dy = dy + self.dx                                  # the residual branch
 
     def step(self, x, target) -> torch.Tensor:
@@ -79,10 +94,15 @@ class Learner:
         diff = self.forward(x).float() - target.float()
         self.backward((diff * (2.0 / diff.numel())).to(torch.bfloat16))
         self.ctx.grad_norm(self.grads, self.max_norm, self.record)
+        hold_back(self.record, self.status)
         self.steps += 1
         self.ctx.adamw_step(self.params, self.grads, self.exp_avg, self.exp_avg_sq, self.steps, self.lr,
                             weight_decay=self.weight_decay, copies=self.copies, clip=self.record)
         return diff.square().mean()
+
+    def check(self) -> None:
+        """Raises if steps since the last check were held back by what an operator reported."""
+        raise_status(self.status)
 
 
 def train(ctx: "dd.Context", *, learners: int = 4, d: int = 256, f: int = 512, blocks: int = 2, tokens: int = 512,
@@ -113,6 +133,8 @@ def train(ctx: "dd.Context", *, learners: int = 4, d: int = 256, f: int = 512, b
                 x = randn(tokens, d).to(torch.bfloat16)
                 total += m.step(x, teacher.forward(x))
         history.append(float(total) / (inner_steps * learners))
+        for m in (teacher, *group):
+            m.check()
         frags = [dict(global_=theta[p], momentum=momentum[p], learners=[m.copies[p] for m in group],
                       tokens=[inner_steps * tokens] * learners, quorum_mask=everyone, K=learners, n=3 * d * f)
                  for p in range(blocks)]
@@ -173,6 +195,7 @@ class DecoderLearner:
         self.attention_scratch = room(dd.attention_scratch_bytes(tokens, heads, kv_heads, dim, sequences, backward=True), dtype=torch.uint8)
         self.loss_scratch = room(ctx.vocab_loss_scratch_bytes(tokens, d, vocab, backward=True), dtype=torch.uint8)
         self.record = dd.new_grad_record(device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
 
     def _views(self, p, flat):
         views, at = [], 0
@@ -212,27 +235,30 @@ class DecoderLearner:
             keep["qkv"].copy_((keep["h1"] @ w_qkv.t()).view_as(keep["qkv"]))
             q, k, v = self._split(keep["qkv"])
             self.ctx.rotary(q, k, positions, self.frequencies)
-            self.ctx.attention_forward(q, k, v, keep["o"], keep["lse"], offsets=offsets, scratch=self.attention_scratch)
+            self.ctx.attention_forward(q, k, v, keep["o"], keep["lse"], offsets=offsets, scratch=self.attention_scratch, status=self.status)
             x = x + keep["o"].flatten(1) @ w_o.t()
             keep["y2"], keep["r2"] = normed(x)
             keep["h2"] = keep["y2"].to(bf)
             y = torch.empty_like(x)
-            self.ctx.gated_ffn_forward(keep["h2"], *block, y, residual=x, gate=keep["gate"], up=keep["up"], hidden=self.scratch)
+            self.ctx.gated_ffn_forward(keep["h2"], *block, y, residual=x, gate=keep["gate"], up=keep["up"], hidden=self.scratch,
+                                       status=self.status)
             x = y
         self.y, self.r = normed(x)
         self.hidden = self.y.to(bf)
-        self.ctx.vocab_loss_forward(self.hidden, head, targets, self.loss, self.lse, scratch=self.loss_scratch)
+        self.ctx.vocab_loss_forward(self.hidden, head, targets, self.loss, self.lse, scratch=self.loss_scratch, status=self.status)
         return self.loss
 
     def backward(self, dloss) -> None:
         """Gradients for ``dloss``, the derivative by each token's loss (float32), into ``grads``."""
         bf, (ids, targets, positions, offsets) = torch.bfloat16, self.batch
         d_embedding, d_head = self.weight_grads[-1]
-        self.ctx.vocab_loss_backward(self.hidden, self.weights[-1][1], targets, self.lse, dloss, self.dx, d_head, scratch=self.loss_scratch)
+        self.ctx.vocab_loss_backward(self.hidden, self.weights[-1][1], targets, self.lse, dloss, self.dx, d_head, scratch=self.loss_scratch,
+                                     status=self.status)
         dx = normed_backward(self.dx.float(), self.y, self.r)
         for i in reversed(range(len(self.kept))):
             keep, (w_qkv, w_o, *block), (dw_qkv, dw_o, *dblock) = self.kept[i], self.weights[i], self.weight_grads[i]
-            self.ctx.gated_ffn_backward(keep["h2"], *block, keep["gate"], keep["up"], dx.to(bf), self.dx, *dblock, scratch=self.scratch)
+            self.ctx.gated_ffn_backward(keep["h2"], *block, keep["gate"], keep["up"], dx.to(bf), self.dx, *dblock, scratch=self.scratch,
+                                        status=self.status)
             dx = dx + normed_backward(self.dx.float(), keep["y2"], keep["r2"])
             dy = dx.to(bf)
             self.d_o.copy_((dy @ w_o).view_as(self.d_o))
@@ -240,7 +266,8 @@ class DecoderLearner:
             q, k, v = self._split(keep["qkv"])
             dq, dk, dv = self._split(self.dqkv)
             self.dqkv.zero_()                                  # rows behind the last document stay as they are
-            self.ctx.attention_backward(q, k, v, keep["o"], keep["lse"], self.d_o, dq, dk, dv, offsets=offsets, scratch=self.attention_scratch)
+            self.ctx.attention_backward(q, k, v, keep["o"], keep["lse"], self.d_o, dq, dk, dv, offsets=offsets, scratch=self.attention_scratch,
+                                        status=self.status)
             self.ctx.rotary(dq, dk, positions, self.frequencies, inverse=True)
             dqkv = self.dqkv.flatten(1)
             torch.mm(dqkv.t(), keep["h1"], out_dtype=torch.float32, out=dw_qkv)
@@ -254,10 +281,15 @@ class DecoderLearner:
         count = (targets >= 0).sum().clamp(min=1)
         self.backward((1.0 / count).float().expand(self.tokens).contiguous())
         self.ctx.grad_norm(self.grads, self.max_norm, self.record)
+        hold_back(self.record, self.status)
         self.steps += 1
         self.ctx.adamw_step(self.params, self.grads, self.exp_avg, self.exp_avg_sq, self.steps, self.lr,
                             weight_decay=self.weight_decay, copies=self.copies, clip=self.record)
         return loss.sum() / count
+
+    def check(self) -> None:
+        """Raises if steps since the last check were held back by what an operator reported."""
+        raise_status(self.status)
 
 
 def packed_documents(gen, tokens: int, sequences: int, vocab: int, device="cuda"):
@@ -299,6 +331,8 @@ def train_decoder(ctx: "dd.Context", *, learners: int = 2, vocab: int = 512, d: 
             for m in group:
                 total += m.step(*packed_documents(gen, tokens, sequences, vocab))
         history.append(float(total) / (inner_steps * learners))
+        for m in group:
+            m.check()
         frags = [dict(global_=theta[p], momentum=momentum[p], learners=[m.copies[p] for m in group],
                       tokens=[inner_steps * tokens] * learners, quorum_mask=everyone, K=learners, n=theta[p].numel())
                  for p in range(len(theta))]

@@ -48,3 +48,43 @@ def test_a_batch_without_targets(mods):
     assert float(m.step(ids, targets, positions, torch.arange(4, dtype=torch.int32, device="cuda"))) == 0.0
     assert not any(bool(g.any()) for g in m.grads)
     assert all(torch.equal(a, b) for a, b in zip(before, m.params))
+
+
+def test_bad_offsets_change_nothing_and_are_reported(mods):
+    """Attention writes nothing for offsets that decrease: the step leaves parameters, moments and copies alone, and the
+    learner says so before a merge; after that it goes on."""
+    dd, lm, _ = mods
+    m, gen = start(mods, lr=1e-2)
+    batch = lm.packed_documents(gen, SIZES["tokens"], SIZES["sequences"], SIZES["vocab"])
+    m.step(*batch)
+    m.check()
+    held = [*m.params, *m.exp_avg, *m.exp_avg_sq, *m.copies]
+    before = [t.clone() for t in held]
+    ids, targets, positions, _ = batch
+    bad = torch.tensor([0, 90, 50, 200], dtype=torch.int32, device="cuda")
+    m.step(ids, targets, positions, bad)
+    m.step(*batch)                                        # until it is looked at
+    assert all(torch.equal(a, b) for a, b in zip(before, held))
+    with pytest.raises(RuntimeError, match=str(dd.STATUS_BAD_OFFSETS)):
+        m.check()
+    m.step(*batch)
+    m.check()
+    assert not any(torch.equal(a, b) for a, b in zip(before, held))
+
+
+def test_learners_of_blocks_report_too(mods):
+    _, lm, ctx = mods
+    m = lm.Learner(ctx, 64, 128, 2, 32, lr=1e-2)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for p in range(2):
+        m.receive(p, torch.randn(3 * 64 * 128, generator=gen, device="cuda") * 0.1)
+    x = torch.randn(32, 64, generator=gen, device="cuda").to(torch.bfloat16)
+    before = [t.clone() for t in m.params]
+    m.status.fill_(mods[0].STATUS_WAIT_LIMIT)             # as an expired wait leaves it
+    m.step(x, x)
+    assert all(torch.equal(a, b) for a, b in zip(before, m.params))
+    with pytest.raises(RuntimeError):
+        m.check()
+    m.step(x, x)
+    m.check()
+    assert not any(torch.equal(a, b) for a, b in zip(before, m.params))
