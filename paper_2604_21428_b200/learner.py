@@ -196,6 +196,7 @@ class DecoderLearner:
         self.loss_scratch = room(ctx.vocab_loss_scratch_bytes(tokens, d, vocab, backward=True), dtype=torch.uint8)
         self.record = dd.new_grad_record(device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self.trained = torch.zeros((), dtype=torch.int64, device=device)            # tokens with a target, of applied steps
 
     def _views(self, p, flat):
         views, at = [], 0
@@ -278,13 +279,15 @@ class DecoderLearner:
         """One inner step on the mean loss of the tokens that have a target; returns it (a device scalar).  Without any
         the loss and its gradients are 0."""
         loss = self.forward(ids, targets, positions, offsets)
-        count = (targets >= 0).sum().clamp(min=1)
+        some = (targets >= 0).sum()
+        count = some.clamp(min=1)
         self.backward((1.0 / count).float().expand(self.tokens).contiguous())
         self.ctx.grad_norm(self.grads, self.max_norm, self.record)
         hold_back(self.record, self.status)
         self.steps += 1
         self.ctx.adamw_step(self.params, self.grads, self.exp_avg, self.exp_avg_sq, self.steps, self.lr,
                             weight_decay=self.weight_decay, copies=self.copies, clip=self.record)
+        self.trained += some * (self.record.view(torch.int32)[2] == dd.STATUS_OK)
         return loss.sum() / count
 
     def check(self) -> None:
@@ -313,7 +316,8 @@ def train_decoder(ctx: "dd.Context", *, learners: int = 2, vocab: int = 512, d: 
                   kv_heads: int = 2, dim: int = 32, tokens: int = 512, sequences: int = 6, rounds: int = 5, inner_steps: int = 20,
                   lr: float = 3e-3, outer_lr: float = 0.7, outer_mu: float = 0.9, seed: int = 0):
     """``learners`` learners train one decoder; after every ``inner_steps`` steps each fragment is merged over all
-    of them and pushed back.  Returns the mean loss of each round."""
+    of them and pushed back, each learner weighed by the tokens with a target that it trained on.  Returns the mean loss of
+    each round."""
     gen = torch.Generator(device="cuda").manual_seed(seed)
     sizes = dict(vocab=vocab, d=d, f=f, layers=layers, heads=heads, kv_heads=kv_heads, dim=dim, tokens=tokens, sequences=sequences)
     group = [DecoderLearner(ctx, **sizes, lr=lr) for _ in range(learners)]
@@ -333,8 +337,11 @@ def train_decoder(ctx: "dd.Context", *, learners: int = 2, vocab: int = 512, d: 
         history.append(float(total) / (inner_steps * learners))
         for m in group:
             m.check()
+        trained = [int(m.trained) for m in group]
+        for m in group:
+            m.trained.zero_()
         frags = [dict(global_=theta[p], momentum=momentum[p], learners=[m.copies[p] for m in group],
-                      tokens=[inner_steps * tokens] * learners, quorum_mask=everyone, K=learners, n=theta[p].numel())
+                      tokens=trained, quorum_mask=everyone, K=learners, n=theta[p].numel())
                  for p in range(len(theta))]
         ctx.merge_fragments_batched_push(frags, [everyone] * len(theta), learners, dd.BF16, outer_lr, outer_mu, records=records)
         for p in range(len(theta)):

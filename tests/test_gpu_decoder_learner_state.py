@@ -88,3 +88,42 @@ def test_learners_of_blocks_report_too(mods):
     m.step(x, x)
     m.check()
     assert not any(torch.equal(a, b) for a, b in zip(before, m.params))
+
+
+def test_merges_count_trained_tokens_and_learners_hold_the_result(mods, monkeypatch):
+    """The merge weighs each learner by the tokens with a target that it trained on since the last one; after the push every
+    learner holds the global fragments."""
+    _, lm, ctx = mods
+    learners, counts, merges = [], [], []
+    documents = lm.packed_documents
+
+    class Kept(lm.DecoderLearner):
+        def __init__(self, *a, **kw):
+            super().__init__(*a, **kw)
+            learners.append(self)
+
+    class Seen:
+        def __getattr__(self, name):
+            return getattr(ctx, name)
+
+        def merge_fragments_batched_push(self, frags, *a, **kw):
+            merges.append(frags)
+            return ctx.merge_fragments_batched_push(frags, *a, **kw)
+
+    def counted(*a, **kw):
+        batch = documents(*a, **kw)
+        counts.append(int((batch[1] >= 0).sum()))
+        return batch
+
+    monkeypatch.setattr(lm, "DecoderLearner", Kept)
+    monkeypatch.setattr(lm, "packed_documents", counted)
+    rounds, steps = 2, 3
+    lm.train_decoder(Seen(), learners=2, rounds=rounds, inner_steps=steps, **SIZES)
+    assert len(merges) == rounds and len(counts) == rounds * steps * 2
+    for r, frags in enumerate(merges):
+        mine = counts[r * steps * 2: (r + 1) * steps * 2]
+        assert all(f["tokens"] == [sum(mine[0::2]), sum(mine[1::2])] for f in frags)
+    assert sum(counts[0::2]) != sum(counts[1::2])         # or the test would say little
+    for p, f in enumerate(merges[-1]):
+        for m in learners:
+            assert torch.equal(m.params[p], f["global_"]) and torch.equal(m.copies[p], f["global_"].to(torch.bfloat16))
