@@ -193,7 +193,7 @@ class DecoderLearner:
         self.dx = room(tokens, d)
         self.scratch = room(3 * tokens * ((f + 7) // 8 * 8))
         self.attention_scratch = room(dd.attention_scratch_bytes(tokens, heads, kv_heads, dim, sequences, backward=True), dtype=torch.uint8)
-        self.loss_scratch = room(ctx.vocab_loss_scratch_bytes(tokens, d, vocab, backward=True), dtype=torch.uint8)
+        self.loss_scratch = room(max(ctx.vocab_loss_scratch_bytes(tokens, d, vocab, backward=b) for b in (False, True)), dtype=torch.uint8)
         self.record = dd.new_grad_record(device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.trained = torch.zeros((), dtype=torch.int64, device=device)            # tokens with a target, of applied steps

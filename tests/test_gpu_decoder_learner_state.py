@@ -127,3 +127,16 @@ def test_merges_count_trained_tokens_and_learners_hold_the_result(mods, monkeypa
     for p, f in enumerate(merges[-1]):
         for m in learners:
             assert torch.equal(m.params[p], f["global_"]) and torch.equal(m.copies[p], f["global_"].to(torch.bfloat16))
+
+
+def test_room_for_the_loss_of_a_wide_vocabulary(mods):
+    """Many columns, small d and many tokens: forward, the loss needs more scratch than backward."""
+    _, lm, ctx = mods
+    sizes = dict(vocab=80000, d=16, f=16, layers=1, heads=1, kv_heads=1, dim=16, tokens=32768, sequences=40)
+    assert ctx.vocab_loss_scratch_bytes(32768, 16, 80000) > ctx.vocab_loss_scratch_bytes(32768, 16, 80000, backward=True)
+    m = lm.DecoderLearner(ctx, **sizes, lr=1e-3)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for p, fragment in enumerate(m.initial(gen)):
+        m.receive(p, fragment)
+    assert 0.0 < float(m.step(*lm.packed_documents(gen, 32768, 40, 80000))) < 20.0        # log(80000) = 11.3
+    m.check()
