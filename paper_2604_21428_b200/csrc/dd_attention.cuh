@@ -74,14 +74,6 @@ __device__ __forceinline__ void tmem_st16(unsigned addr, const unsigned (&r)[16]
         : "memory");
 }
 
-__device__ __forceinline__ void tmem_ld16(unsigned addr, unsigned (&r)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(addr));
-}
-
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void init_bar(unsigned bar, unsigned count)
@@ -181,14 +173,6 @@ __device__ __forceinline__ void zero_rows(unsigned tile, unsigned first, int lan
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) arrive_bar(bar);
-}
-
-// Four floats at `addr` (a shared-memory address of this CTA) in the CTA of rank `rank`.
-__device__ __forceinline__ float4 ld_cluster4(unsigned addr, unsigned rank)
-{
-    float4 x;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(cluster_addr(addr, rank)) : "memory");
-    return x;
 }
 
 // Where four columns of a row of 2 DP float32 sums are kept: eight rows' pieces of one column lie in different banks.

@@ -39,23 +39,6 @@ __host__ __device__ constexpr unsigned stream_ring_bytes(unsigned n, unsigned st
 }
 __host__ __device__ constexpr unsigned stream_smem_bytes(unsigned n, unsigned stages) { return 1024 + stream_ring_bytes(n, stages); }
 
-// Four floats at `addr` (a shared-memory address of this CTA) in the CTA of rank `rank`.
-__device__ __forceinline__ float4 ld_cluster4(unsigned addr, unsigned rank)
-{
-    float4 x;
-    asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %4, %5;\n ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [r];\n}"
-                 : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr), "r"(rank) : "memory");
-    return x;
-}
-
-__device__ __forceinline__ void tmem_ld16(unsigned addr, unsigned (&r)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(addr));
-}
-
 // What an epilogue reads for four features of a token, asked for before the sums are ready.
 struct Aux {
     uint2 a, b;                       // kEpiBack: gate, up; kEpiStore: residual

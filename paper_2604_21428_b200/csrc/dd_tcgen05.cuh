@@ -71,6 +71,15 @@ __device__ __forceinline__ unsigned cluster_addr(unsigned addr, unsigned rank)
     return r;
 }
 
+// Four floats at `addr` (a shared-memory address of this CTA) in the CTA of rank `rank`.
+__device__ __forceinline__ float4 ld_cluster4(unsigned addr, unsigned rank)
+{
+    float4 x;
+    asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %4, %5;\n ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [r];\n}"
+                 : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr), "r"(rank) : "memory");
+    return x;
+}
+
 // Relaxed: what it reports is that tensor memory has been read into registers, which the wait on
 // those loads has ensured.  A release would hold the warp until its stores to global memory are
 // acknowledged: 2-5k cycles a tile.
@@ -101,6 +110,14 @@ __device__ __forceinline__ void tmem_ld32(unsigned addr, unsigned (&r)[32])
           "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
           "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(addr));
+}
+
+__device__ __forceinline__ void tmem_ld16(unsigned addr, unsigned (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
 }
 
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
