@@ -316,8 +316,9 @@ __device__ __forceinline__ void load_box(unsigned box, int lane, const __nv_bflo
 }
 
 // 32 float32 columns of the lane's row through the box to out [+ addend]; SUM (kOutSum) rounds what goes out.  The
-// choice is made outside: made for every piece it holds the stores up (d 2048, f 8192, float32 gradients: 512 tokens
-// backward 160 -> 181 us, 100 tokens 116 -> 129; d 256, f 1024, 321 tokens forward 25 -> 28).
+// choice is made outside, and launches without such a problem have a kernel without it: made for every piece it holds the
+// stores up (d 2048, f 8192, float32 gradients: 512 tokens backward 160 -> 181 us, 100 tokens 116 -> 129; d 256, f 1024, 321
+// tokens forward 25 -> 28), and the longer kernel alone costs small blocks 1 us (d 512, f 2048, 512 tokens backward 40 -> 41).
 template <bool SUM>
 __device__ __forceinline__ void finish_f32(unsigned box, int lane, const float (&x)[32], const GemmProblem &p, unsigned row0, unsigned out_row0,
                                            unsigned col)
@@ -359,8 +360,8 @@ __device__ __forceinline__ unsigned chunks_of(const GemmProblem &p, const TilePo
 }
 
 // BN: accumulator columns of a pair's tile.  kEpiGate puts BN / 2 columns of gate (the first CTA's
-// share of B) beside BN / 2 of up (the second's).
-template <int EPI, int BN, int ACT>
+// share of B) beside BN / 2 of up (the second's).  SUM: kEpiStore with a kOutSum problem.
+template <int EPI, int BN, int ACT, bool SUM>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
 {
@@ -589,8 +590,8 @@ ffn_gemm_kernel(const __grid_constant__ GemmArgs a)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
                     if (c + 1 == 2 * chunks) release();
-                    if (p.out_f32 == kOutF32) finish_f32<false>(box, lane, x, p, row, pos.split * p.split_rows + row, col0 + 32 * c);
-                    else finish_f32<true>(box, lane, x, p, row, pos.split * p.split_rows + row, col0 + 32 * c);
+                    if (SUM && p.out_f32 == kOutSum) finish_f32<true>(box, lane, x, p, row, row, col0 + 32 * c);
+                    else finish_f32<false>(box, lane, x, p, row, pos.split * p.split_rows + row, col0 + 32 * c);
                 }
             } else if (EPI == kEpiStore) {
                 unsigned r[2][32];
