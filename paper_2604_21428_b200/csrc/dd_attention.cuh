@@ -390,7 +390,9 @@ __device__ __forceinline__ bool warp_next(const Turns &turns, unsigned k, unsign
 // by both and by the steps between them: each is busy for 60 % of the time (8192 tokens, 8 heads of 128, causal).
 // 16384 tokens: 420-430 us, 1290 TFLOP/s of products, on a cool GPU, 490 in a long run, where the power limit
 // takes the clock to 1.5 GHz; 16 computing warps took 517, two issuing threads the same as one.
-// Taking turns: 16384 tokens, 16 heads on 4 of 128, documents of 128 / 256 / 1024 / 4096 tokens: 84 -> 58, 83 -> 66, 112 -> 94, 253 -> 238 us.
+// Taking turns: 16384 tokens, 16 heads on 4 of 128, documents of 128 / 256 / 1024 / 4096 tokens: 84 -> 67, 83 -> 61, 112 -> 91, 253 -> 237 us.
+// Every token of two documents of 4096 seeing all: 242 us, 264 in a long run.  168 registers at launch hold a thread's state but
+// for 96 bytes in local memory (64 columns: 140).
 __host__ __device__ constexpr int fwd_stages(int dp) { return dp == 128 ? 4 : 6; }
 __host__ __device__ constexpr unsigned fwd_smem_bytes(int dp) { return 1024 + (2 + fwd_stages(dp)) * kTile * dp * 2; }
 
@@ -698,7 +700,7 @@ __device__ __forceinline__ DqWork dq_work(const AttnArgs &a, const PlanItem &ite
 // time) and by the steps from one to the next.  8192 tokens, 8 heads of 128, causal: 190 and 240 us at 1.5 GHz; 16384
 // tokens: 1455-1475 us with delta, 1310 TFLOP/s of executed products.  Taking turns, with the next turn's queries on
 // their way: 16384 tokens, 16 heads on 4 of 128, documents of 128 / 1024 / 4096 tokens, the whole backward pass 285 -> 242,
-// 405 -> 366, 877 -> 850 us; 8192 tokens, 8 heads on 2: 403 -> 387.
+// 405 -> 367, 877 -> 864 us; 8192 tokens, 8 heads on 2: 403 -> 393.
 template <int DP>
 __global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dq_kernel(const __grid_constant__ AttnArgs a)
@@ -945,6 +947,9 @@ attention_dq_kernel(const __grid_constant__ AttnArgs a)
 // The first keys of a long sequence are read by all its queries, in every query head of the group: where that is
 // much beside what an SM has to do, the CTAs of a cluster take equal parts of those tiles and add their sums up through
 // distributed shared memory, in rank order.
+//
+// 96 registers are few for a tile's statistics, scores and both weights: 52 bytes a thread are kept in local memory and 212 read
+// back (64 columns: 44 and 192).
 template <int DP>
 __global__ void __launch_bounds__(32 * (kBwdWarps + 4), 1)
 attention_dkv_kernel(const __grid_constant__ AttnArgs a)

@@ -4,10 +4,10 @@
 // weight and with the hidden rows, side by side.
 //
 // Bound by the products, 2 T d V of them forward, 6 T d V backward beside 2 T d V for the logits again: 8192 tokens,
-// d 2048, 32000 columns 773 us forward in short runs and 875 sustained under the 1000 W cap (1390 and 1230 TFLOP/s), 2610 and
-// 2825 us backward (1650 and 1520 TFLOP/s with the logits).  With few tokens by the weights' bytes, read once forward; backward
-// reads them twice and writes as many (4 tokens: 39 us from a cold L2 and 97 from a warm one, of which the bytes
-// need 20 and 40).
+// d 2048, 32000 columns 762 us forward in short runs and 865 sustained under the 1000 W cap (1410 and 1240 TFLOP/s), 2440 and
+// 2795 us backward (1760 and 1540 TFLOP/s with the logits); float32 dweight 2465 and 2850, added to 2695 and
+// 3065.  With few tokens by the weights' bytes, read once forward; backward reads them twice and writes as many (4 tokens: 39 us
+// from a cold L2 and 97 from a warm one, of which the bytes need 20 and 40).
 //
 // The logits' gradient is rounded to bf16 because it is an operand of both products: in the results that is one rounding
 // beside their own (1.2-1.5 times the error of theirs alone; 1.9 were seen with one or two tokens, where the target's
