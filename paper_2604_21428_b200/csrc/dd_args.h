@@ -57,13 +57,13 @@ inline bool touches(const Extent &a, const Extent &b)
     const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
     if (y < x) return touches(b, a);
     if (y >= x + (a.rows - 1) * a.pitch + a.width) return false;
-    if (a.step && a.step == b.step && a.pitch % a.step == 0 && b.pitch % a.step == 0) {      // all teeth at one place of a step
-        const size_t off = (y - x) % a.step;
-        if (off >= a.tooth && off + b.tooth <= a.step) return false;
-    }
+    const auto between = [&](size_t off) { return off % a.step >= a.tooth && off % a.step + b.tooth <= a.step; };
+    const bool combs = a.step && a.step == b.step;
+    if (combs && a.pitch % a.step == 0 && b.pitch % a.step == 0 && between(y - x)) return false;      // all teeth at one place of a step
     if (a.pitch != b.pitch) return true;
     const size_t off = (y - x) % a.pitch;
-    return off < a.width || off + b.width > a.pitch;
+    if (off + b.width > a.pitch) return true;
+    return off < a.width && !(combs && between(off));
 }
 
 // Fills in a tensor's default strides.  Its rows of `dim` elements must not overlap, with the tokens' rows

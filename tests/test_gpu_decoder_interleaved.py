@@ -21,11 +21,14 @@ def ctx(dd):
 
 
 def parts(order, T, heads, dim, fill=None):
-    """Three [T, heads, dim] tensors of one buffer: [T, heads, 3, dim], [heads, T, 3, dim], or the first with longer rows."""
+    """Three [T, heads, dim] tensors of one buffer: [T, heads, 3, dim], [heads, T, 3, dim], or the first with longer rows, by
+    whole heads or by eight elements."""
     if order == "heads first":
         buf = torch.zeros(heads, T, 3, dim, dtype=B, device="cuda").transpose(0, 1)
     elif order == "longer rows":
         buf = torch.zeros(T, heads + 2, 3, dim, dtype=B, device="cuda")[:, 1: heads + 1]
+    elif order == "padded rows":
+        buf = torch.zeros(T, heads * 3 * dim + 8, dtype=B, device="cuda")[:, :-8].unflatten(1, (heads, 3, dim))
     else:
         buf = torch.zeros(T, heads, 3, dim, dtype=B, device="cuda")
     for i in range(3):
@@ -34,7 +37,7 @@ def parts(order, T, heads, dim, fill=None):
     return [buf[:, :, i] for i in range(3)]
 
 
-ORDERS = ["tokens first", "heads first", "longer rows"]
+ORDERS = ["tokens first", "heads first", "longer rows", "padded rows"]
 SIZES = [(1, 4, 64), (1, 1, 64), (2, 1, 128), (300, 4, 64), (131, 3, 80)]
 
 
@@ -91,13 +94,20 @@ def test_keys_and_values_beside_a_group_of_queries(ctx):
 
 def test_what_shares_elements_is_still_refused(dd, ctx):
     T, heads, dim = 6, 4, 16
-    flat = torch.zeros((T + 1) * heads * 3 * dim, dtype=B, device="cuda")
+    flat = torch.zeros((T + 2) * heads * 3 * dim, dtype=B, device="cuda")
     positions, (f, _) = torch.arange(T, device="cuda"), dd.rotary_frequencies(dim)
 
     def at(start, step=3 * dim):
         return flat.as_strided((T, heads, dim), (heads * 3 * dim, step, 1), start)
 
     for q, k in ((at(0), at(8)), (at(0), at(0)), (at(0), at(3 * dim - 8)), (at(0), at(3 * dim)), (at(dim), at(3 * dim + 8)), (at(0), at(dim, 2 * dim))):
+        with pytest.raises(dd.DDMergeError) as e:
+            ctx.rotary(q, k, positions, f)
+        assert e.value.rc == dd.ERR_ALIAS
+    def padded(start):
+        return flat.as_strided((T, heads, dim), ((heads * 3 + 1) * dim - 8, 3 * dim, 1), start)
+
+    for q, k in ((padded(0), padded(dim - 8)), (padded(0), padded(3 * dim - 8)), (padded(dim), padded((heads * 3 + 2) * dim - 8))):
         with pytest.raises(dd.DDMergeError) as e:
             ctx.rotary(q, k, positions, f)
         assert e.value.rc == dd.ERR_ALIAS
