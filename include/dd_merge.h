@@ -51,8 +51,9 @@ typedef enum { DD_MERGE_AVG = 0, DD_MERGE_RDA = 1 } dd_merge_kind;
 typedef enum {
     DD_OK = 0,
     DD_ERR_INVALID_ARG = -1,        /* null where not allowed, M / K / P out of range, non-finite lr or mu */
-    DD_ERR_ALIGNMENT = -2,          /* a device pointer is not 16-byte aligned */
-    DD_ERR_ALIAS = -3,              /* a participating learner buffer overlaps Theta, v or out_bf16 */
+    DD_ERR_ALIGNMENT = -2,          /* a device pointer (merges: 16 bytes) or a stride is not aligned */
+    DD_ERR_ALIAS = -3,              /* merges: a participating learner buffer overlaps Theta, v or out_bf16;
+                                     * other calls: an output overlaps another output or an input */
     DD_ERR_TOO_MANY_LEARNERS = -4,  /* M > DD_MAX_LEARNERS */
     DD_ERR_CUDA = -5,               /* a CUDA runtime call failed; see dd_last_cuda_error */
     DD_ERR_TOO_LARGE = -6           /* a size exceeds what the entry point supports */

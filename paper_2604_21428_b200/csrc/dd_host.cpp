@@ -130,8 +130,8 @@ extern "C" const char *dd_status_string(int rc)
     switch (rc) {
     case DD_OK: return "ok";
     case DD_ERR_INVALID_ARG: return "invalid argument";
-    case DD_ERR_ALIGNMENT: return "device pointer not 16-byte aligned";
-    case DD_ERR_ALIAS: return "learner buffer overlaps the global fragment, the momentum or the bf16 output";
+    case DD_ERR_ALIGNMENT: return "device pointer or stride not aligned as the call requires";
+    case DD_ERR_ALIAS: return "an output overlaps another buffer of the call";
     case DD_ERR_TOO_MANY_LEARNERS: return "more than DD_MAX_LEARNERS learners";
     case DD_ERR_CUDA: return "CUDA runtime error (see dd_last_cuda_error)";
     case DD_ERR_TOO_LARGE: return "size exceeds what this entry point supports";

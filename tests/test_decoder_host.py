@@ -65,3 +65,10 @@ def test_packed_documents():
             if b > a:
                 assert torch.equal(targets[a: b - 1], ids[a + 1: b]) and int(targets[b - 1]) < 0
         assert bool((targets[ends[-1]:] < 0).all()) and bool((positions[ends[-1]:] < 0).all())
+
+
+def test_refusals_name_no_buffer_of_another_call(dd):
+    """Codes that merges and the learner's operators share say what holds for both."""
+    for rc in (dd.ERR_INVALID_ARG, dd.ERR_ALIGNMENT, dd.ERR_ALIAS, dd.ERR_TOO_LARGE):
+        text = dd.lib.dd_status_string(rc).decode()
+        assert not any(word in text for word in ("fragment", "momentum", "learner", "16-byte")), text
