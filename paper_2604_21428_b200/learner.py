@@ -236,6 +236,7 @@ class DecoderLearner:
             keep["qkv"].copy_((keep["h1"] @ w_qkv.t()).view_as(keep["qkv"]))
             q, k, v = self._split(keep["qkv"])
             self.ctx.rotary(q, k, positions, self.frequencies)
+            keep["o"].zero_()                                  # rows behind the last document stay as they are
             self.ctx.attention_forward(q, k, v, keep["o"], keep["lse"], offsets=offsets, scratch=self.attention_scratch, status=self.status)
             x = x + keep["o"].flatten(1) @ w_o.t()
             keep["y2"], keep["r2"] = normed(x)
@@ -266,7 +267,7 @@ class DecoderLearner:
             torch.mm(dy.t(), keep["o"].flatten(1), out_dtype=torch.float32, out=dw_o)      # sums are not rounded to bf16
             q, k, v = self._split(keep["qkv"])
             dq, dk, dv = self._split(self.dqkv)
-            self.dqkv.zero_()                                  # rows behind the last document stay as they are
+            self.dqkv.zero_()                                  # as above
             self.ctx.attention_backward(q, k, v, keep["o"], keep["lse"], self.d_o, dq, dk, dv, offsets=offsets, scratch=self.attention_scratch,
                                         status=self.status)
             self.ctx.rotary(dq, dk, positions, self.frequencies, inverse=True)

@@ -140,3 +140,25 @@ def test_room_for_the_loss_of_a_wide_vocabulary(mods):
         m.receive(p, fragment)
     assert 0.0 < float(m.step(*lm.packed_documents(gen, 32768, 40, 80000))) < 20.0        # log(80000) = 11.3
     m.check()
+
+
+def test_rows_behind_the_documents_forget_earlier_batches(mods):
+    """Attention leaves rows behind the last document as they are: what an earlier batch left there, NaN included, reaches
+    neither loss nor gradients."""
+    _, lm, _ = mods
+    T = SIZES["tokens"]
+    results = []
+    for left in (0.0, float("nan")):
+        m, gen = start(mods, lr=0.0)
+        ids, targets, positions, offsets = lm.packed_documents(gen, T, SIZES["sequences"], SIZES["vocab"])
+        offsets = offsets.clamp(max=150)                   # 50 rows of room
+        behind = torch.arange(T, device="cuda") >= 150
+        targets, positions = targets.masked_fill(behind, -100), positions.masked_fill(behind, -1)
+        for keep in m.kept:
+            keep["o"].fill_(left)
+        m.dqkv.fill_(left)
+        loss = m.step(ids, targets, positions, offsets)
+        m.check()
+        results.append([loss.clone(), *(g.clone() for g in m.grads)])
+    for a, b in zip(*results):
+        assert bool(b.isfinite().all()) and torch.equal(a, b)
